@@ -138,7 +138,7 @@ def _encode(x, fmt, s):
     m = scale.unsqueeze(2)
     c = ((a > 0.25 * m).to(torch.uint8) + (a >= 0.75 * m) + (a > 1.25 * m) + (a >= 1.75 * m) + (a > 2.5 * m)
          + (a >= 3.5 * m) + (a > 5.0 * m)) * (m > 0)
-    return (c + 8 * torch.signbit(v)).view(x.shape[0], -1), byte
+    return (c + 8 * torch.signbit(v).to(torch.uint8)).view(x.shape[0], -1), byte
 
 
 def _store(codes, byte, cols):
