@@ -518,6 +518,128 @@ int bitsmoe_shared_basis(int side, const float* W, int E, int d, int D, float* p
  * T == 0 writes zeros.  Never allocates, never synchronises; one launch. */
 int bitsmoe_calibration_gram(const void* x, const float* g, int64_t T, int D, float* H, void* stream);
 
+/* Element types of dense rows in the calls below. */
+#define BITSMOE_F32  0
+#define BITSMOE_BF16 1
+
+/* A microscaled 4-bit matrix (no counterpart in the paper, which leaves the
+ * dense matrices beside the routed experts in 16 bits; the shared expert's
+ * projections, for instance).  Elements are E2M1 (0, 1/2, 1, 3/2, 2, 3, 4, 6
+ * and their negatives: code = sign << 3 | index), a block of consecutive
+ * columns of a row shares a scale byte, and
+ *     value[r][k] = element * block scale * scale.
+ *   format  BITSMOE_MICRO_E8M0: blocks of 32, block scale 2^(byte - 127), 255 = NaN
+ *           BITSMOE_MICRO_E4M3: blocks of 16, block scale an fp8 E4M3 value
+ *           (sign bit 0; 127 = NaN)
+ *   rows, cols  0 .. 2^24, 1 .. 2^20
+ *   scale   tensor scale, positive and finite (host value)
+ *   codes   device, rows x 16 ceil(cols / 32) bytes, 16-byte aligned: two codes
+ *           a byte, the even column in the lower half; codes past cols are 0
+ *   scales  device, ceil(rows / 128) x ceil(blocks / 4) tiles of 512 bytes,
+ *           16-byte aligned, blocks = ceil(cols / block): the byte of block b of
+ *           row r is at ((r / 128) * ceil(blocks / 4) + b / 4) * 512
+ *           + (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4; bytes of rows and
+ *           blocks past the matrix's are 0 */
+#define BITSMOE_MICRO_E8M0 0
+#define BITSMOE_MICRO_E4M3 1
+typedef struct bitsmoe_microscale {
+  int32_t format, rows, cols;
+  float scale;
+  uint8_t* codes;
+  uint8_t* scales;
+} bitsmoe_microscale;
+
+/* Bytes of the two buffers of such a matrix.  Errors: INVALID_ARG, SHAPE. */
+int bitsmoe_microscale_bytes(int format, int rows, int cols, size_t* codes, size_t* scales);
+
+/* Quantise dense rows into q (weights once, or activations before a product),
+ * asynchronously on `stream`: v = x / q->scale, a = max |v| over a block,
+ *   E8M0: block scale X = 2^clamp(floor(log2 a) - 2, -127, 125)
+ *   E4M3: X = min(a / 6, 448) rounded to E4M3
+ *   element = v / X rounded to E2M1, at most 6 in magnitude (0 where X = 0)
+ * every rounding to nearest, ties to even, of the exact quotient: the result is
+ * deterministic to the bit.  A block that holds a NaN or an infinity gets a NaN
+ * scale and elements 0.
+ *   x     device, q->rows x q->cols of `type` (BITSMOE_F32 or BITSMOE_BF16),
+ *         rows `ld` elements apart (ld >= cols), aligned to its elements (rows
+ *         on 16-byte boundaries are read fastest)
+ *   q     format, rows, cols and scale set by the caller, scale a power of two
+ *         in 2^-100 .. 2^100; codes and scales are written whole, their padding
+ *         with zeros
+ * Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.  Never allocates, never
+ * synchronises; one launch.  rows == 0 is a successful no-op. */
+int bitsmoe_microscale_quantize(const void* x, int type, int64_t ld, const bitsmoe_microscale* q, void* stream);
+
+/* The values of a microscaled matrix, (element * block scale) * scale in fp32,
+ * rounded to `type`: x device, rows x cols, rows `ld` elements apart.  Errors and
+ * the rest as bitsmoe_microscale_quantize (any positive finite scale). */
+int bitsmoe_microscale_dequantize(const bitsmoe_microscale* q, void* x, int type, int64_t ld, void* stream);
+
+/* Product of T dense rows with a microscaled matrix, asynchronously on `stream`:
+ *   y[t][r] = sum_k W[r][k] x[t][k]                          (up NULL)
+ *   y[t][r] = SiLU(sum_k W[r][k] x[t][k]) * sum_k U[r][k] x[t][k]   (up = U)
+ *   w, up   the matrices; up NULL or of w's format, rows and cols
+ *   x, x_ld device, T x w->cols bf16, rows x_ld elements apart (rows on 16-byte
+ *           boundaries are read fastest); NULL when xq is given
+ *   xq      NULL, or the T rows themselves microscaled, in w's format (for
+ *           instance by bitsmoe_microscale_quantize); x is then NULL
+ *   y       device, T x w->rows of y_type, rows y_ld elements apart; written
+ *           (nothing between its rows is touched); must not overlap the inputs
+ *   status  device int or NULL: BITSMOE_ERR_TIMEOUT is written there if a
+ *           bounded wait of the kernel ran out (y is then undefined); not
+ *           cleared by the call
+ * Products and sums are fp32 (the products of two codes, and of a code with a
+ * bf16 value, are exact); y is rounded once.  Errors: INVALID_ARG, SHAPE,
+ * ALIGNMENT, CUDA.  Never allocates, never synchronises; one launch.  T == 0
+ * and rows == 0 are successful no-ops. */
+int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const void* x,
+                               int64_t x_ld, const bitsmoe_microscale* xq, int T, void* y, int y_type,
+                               int64_t y_ld, int* status, void* stream);
+
+/* What stands between a block's output y and the next block's input x, for T
+ * rows of D, in one pass (bitsmoe_rmsnorm_router's norm with gains, after and
+ * before a block; no counterpart in the paper), asynchronously on `stream`:
+ *   n  = y / sqrt(mean_d y^2 + post_eps) * (gain_offset + post_gain)   (post_norm != 0;
+ *        factor 1 where post_gain is NULL), or n = y
+ *   h' = residual_scale * h + branch_scale * channel_scale * gate * n
+ *   x  = h' / sqrt(mean_d h'^2 + pre_eps) * (gain_offset + pre_gain)   (1 where NULL)
+ *   h          device, T x D of h_type: the residual stream
+ *   y          device, T x D of y_type, or NULL (then h' = residual_scale * h)
+ *   gate       BITSMOE_GATE_NONE; _TOKEN: a value per row, gate[t * gate_ld];
+ *              _ELEMENT: T x D, rows gate_ld apart; of gate_type; its sigmoid
+ *              when gate_sigmoid != 0 (a shared expert's gate)
+ *   post_gain, pre_gain, channel_scale  device, D of gain_type, or NULL
+ *   h_out      device, T x D of h_type, written; may be h itself (same h_ld);
+ *              NULL: not stored.  x uses h' before it is rounded to h_type.
+ *   x          device, T x D of x_type, written; NULL: no pre-norm
+ *   *_ld       elements between rows (>= D; gate per token: >= 1)
+ * Types are BITSMOE_F32 or BITSMOE_BF16; every pointer is aligned to its
+ * elements (all rows on 16-byte boundaries with D a multiple of 8 are fastest).
+ * x must not overlap an input, nor h_out one other than h.  fp32 arithmetic.
+ * 1 <= D <= BITSMOE_BLOCK_NORM_MAX_D, T <= 2^24.  Errors: INVALID_ARG, SHAPE,
+ * ALIGNMENT, CUDA.  Never allocates, never synchronises; one launch; T == 0 is
+ * a successful no-op. */
+#define BITSMOE_GATE_NONE    0
+#define BITSMOE_GATE_TOKEN   1
+#define BITSMOE_GATE_ELEMENT 2
+#define BITSMOE_BLOCK_NORM_MAX_D 32768
+typedef struct bitsmoe_block_norm_args {
+  int32_t T, D;
+  int32_t h_type, y_type, gate_type, gain_type, x_type;
+  int32_t post_norm, gate_kind, gate_sigmoid;
+  float post_eps, pre_eps, gain_offset, residual_scale, branch_scale;
+  const void* h;
+  const void* y;
+  const void* gate;
+  const void* post_gain;
+  const void* pre_gain;
+  const void* channel_scale;
+  void* h_out;
+  void* x;
+  int64_t h_ld, y_ld, gate_ld, h_out_ld, x_ld;
+} bitsmoe_block_norm_args;
+int bitsmoe_block_norm(const bitsmoe_block_norm_args* args, void* stream);
+
 /* Where bitsmoe_moe_block_forward(T, top_k) leaves the block's normalised
  * activations x (T x D bf16) and router logits (T x E fp32) in its workspace:
  * byte offsets from the workspace start, valid after the call completes (the

@@ -43,6 +43,20 @@ class _Bytes(ctypes.Structure):
                 ("codes_padded", ctypes.c_uint64), ("meta", ctypes.c_uint64)]
 
 
+class _Microscale(ctypes.Structure):
+    _fields_ = [("format", ctypes.c_int32), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("codes", _P), ("scales", _P)]
+
+
+class _BlockNormArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("T", "D", "h_type", "y_type", "gate_type", "gain_type", "x_type",
+                                               "post_norm", "gate_kind", "gate_sigmoid")]
+                + [(n, ctypes.c_float) for n in ("post_eps", "pre_eps", "gain_offset", "residual_scale",
+                                                 "branch_scale")]
+                + [(n, _P) for n in ("h", "y", "gate", "post_gain", "pre_gain", "channel_scale", "h_out", "x")]
+                + [(n, ctypes.c_int64) for n in ("h_ld", "y_ld", "gate_ld", "h_out_ld", "x_ld")])
+
+
 SIGNATURES = {
     "bitsmoe_pack": (_I, [ctypes.POINTER(_LayerHost), _I, ctypes.POINTER(_P)]),
     "bitsmoe_pack_to_host": (_I, [ctypes.POINTER(_LayerHost), ctypes.POINTER(_P), ctypes.POINTER(_SZ)]),
@@ -79,6 +93,12 @@ SIGNATURES = {
     "bitsmoe_decompose_workspace_bytes": (_SZ, [_I, _I, _I, _I]),
     "bitsmoe_shared_basis": (_I, [_I, _P, _I, _I, _I, _P, _P, _P, _P, _P, _SZ, _I, _P, _P, _P]),
     "bitsmoe_calibration_gram": (_I, [_P, _P, ctypes.c_int64, _I, _P, _P]),
+    "bitsmoe_microscale_bytes": (_I, [_I, _I, _I, ctypes.POINTER(_SZ), ctypes.POINTER(_SZ)]),
+    "bitsmoe_microscale_quantize": (_I, [_P, _I, ctypes.c_int64, ctypes.POINTER(_Microscale), _P]),
+    "bitsmoe_microscale_dequantize": (_I, [ctypes.POINTER(_Microscale), _P, _I, ctypes.c_int64, _P]),
+    "bitsmoe_microscale_product": (_I, [ctypes.POINTER(_Microscale), ctypes.POINTER(_Microscale), _P, ctypes.c_int64,
+                                        ctypes.POINTER(_Microscale), _I, _P, _I, ctypes.c_int64, _P, _P]),
+    "bitsmoe_block_norm": (_I, [ctypes.POINTER(_BlockNormArgs), _P]),
     "bitsmoe_block_norm_outputs": (_I, [_P, _I, _I, ctypes.POINTER(_SZ), ctypes.POINTER(_SZ)]),
     "bitsmoe_last_device_status": (_I, [_P, _P]),
     "bitsmoe_free": (None, [_P]),
@@ -514,6 +534,263 @@ def calibration_gram(x, g=None, stream=None):
     _check(_lib().bitsmoe_calibration_gram(x.data_ptr(), g.data_ptr() if g is not None else None, T, D,
                                            H.data_ptr(), st.cuda_stream), "bitsmoe_calibration_gram")
     return H
+
+
+# --------------------------------------------------------------------------
+# microscaled 4-bit matrices and the norms between blocks (torch tensors)
+# --------------------------------------------------------------------------
+MICRO_FORMATS = {"e8m0": 0, "e4m3": 1}       # BITSMOE_MICRO_*: blocks of 32 and of 16 columns
+_MICRO_BLOCK = {"e8m0": 32, "e4m3": 16}
+BLOCK_NORM_MAX_D = 32768                     # BITSMOE_BLOCK_NORM_MAX_D
+_GATE_NONE, _GATE_TOKEN, _GATE_ELEMENT = 0, 1, 2
+
+
+def _refuse(where: str, why: str, code: str = "INVALID_ARG"):
+    raise BitsMoEError(ERR_CODE[code], f"{where}: {why}")
+
+
+def _dense_type(where: str, name: str, dtype) -> int:
+    import torch
+    if dtype == torch.float32:
+        return 0
+    if dtype == torch.bfloat16:
+        return 1
+    _refuse(where, f"{name} must be float32 or bfloat16, got {dtype}")
+
+
+def _rows(where: str, name: str, x, rows=None, cols=None, device=None, dtype=None):
+    """Checks of a 2-d device tensor whose rows are dense (the pitch between them is free); its pitch."""
+    if x.dim() != 2 or not x.is_cuda:
+        _refuse(where, f"{name} must be a 2-d CUDA tensor")
+    if device is not None and x.device != device:
+        _refuse(where, f"{name} is on {x.device}, expected {device}")
+    if (rows is not None and x.shape[0] != rows) or (cols is not None and x.shape[1] != cols):
+        _refuse(where, f"{name} has shape {tuple(x.shape)}, expected {(rows, cols)}", "SHAPE")
+    if dtype is not None and x.dtype != dtype:
+        _refuse(where, f"{name} must be {dtype}, got {x.dtype}")
+    if x.shape[1] > 1 and x.shape[0] > 0 and x.stride(1) != 1:
+        _refuse(where, f"{name} must have dense rows (stride 1 along them)")
+    if x.shape[0] <= 1:
+        return max(int(x.shape[1]), 1)
+    if x.stride(0) < x.shape[1]:
+        _refuse(where, f"{name}'s rows overlap (stride {x.stride(0)})")
+    return int(x.stride(0))
+
+
+def _vector(where: str, name: str, v, n: int, device, dtype=None):
+    if v is None:
+        return None
+    if v.dim() != 1 or v.shape[0] != n:
+        _refuse(where, f"{name} has shape {tuple(v.shape)}, expected {(n,)}", "SHAPE")
+    if v.device != device or (n > 1 and v.stride(0) != 1):
+        _refuse(where, f"{name} must be a dense vector on {device}")
+    if dtype is not None and v.dtype != dtype:
+        _refuse(where, f"{name} must be {dtype}, got {v.dtype}")
+    return v.data_ptr()
+
+
+class Microscale:
+    """A microscaled 4-bit matrix on the device: `codes` (torch uint8, rows x 16 ceil(cols / 32)) and
+    `scales` (uint8, the stored tile order), see bitsmoe_microscale in include/bitsmoe.h; `fmt` is
+    "e8m0" (blocks of 32 columns) or "e4m3" (16), `scale` the tensor scale."""
+
+    __slots__ = ("codes", "scales", "rows", "cols", "fmt", "scale")
+
+    def __init__(self, codes, scales, rows: int, cols: int, fmt: str = "e8m0", scale: float = 1.0):
+        import torch
+        if fmt not in MICRO_FORMATS:
+            _refuse("Microscale", f"unknown format {fmt!r}")
+        nc, ns = microscale_bytes(fmt, rows, cols)
+        for name, t, n in (("codes", codes, nc), ("scales", scales, ns)):
+            if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() != n:
+                _refuse("Microscale", f"{name} must be {n} contiguous bytes (uint8)", "SHAPE")
+        if codes.device != scales.device:
+            _refuse("Microscale", "codes and scales are on different devices")
+        self.codes, self.scales = codes, scales
+        self.rows, self.cols, self.fmt, self.scale = int(rows), int(cols), fmt, float(scale)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, fmt: str = "e8m0", scale: float = 1.0, device=None) -> "Microscale":
+        import torch
+        nc, ns = microscale_bytes(fmt, rows, cols)
+        dev = device if device is not None else f"cuda:{torch.cuda.current_device()}"
+        return cls(torch.empty(nc, dtype=torch.uint8, device=dev), torch.empty(ns, dtype=torch.uint8, device=dev),
+                   rows, cols, fmt, scale)
+
+    @classmethod
+    def from_rows(cls, codes, block_scales, cols: int, fmt: str = "e8m0", scale: float = 1.0) -> "Microscale":
+        """From a checkpoint's arrays: codes uint8 rows x ceil(cols / 2) (even column in the lower half) and
+        one scale byte per block, uint8 rows x ceil(cols / block)."""
+        import torch
+        import torch.nn.functional as F
+        if fmt not in MICRO_FORMATS:
+            _refuse("Microscale.from_rows", f"unknown format {fmt!r}")
+        rows, nb = int(codes.shape[0]), -(-cols // _MICRO_BLOCK[fmt])
+        if tuple(codes.shape) != (rows, (cols + 1) // 2) or tuple(block_scales.shape) != (rows, nb):
+            _refuse("Microscale.from_rows", f"codes {tuple(codes.shape)}, scales {tuple(block_scales.shape)}", "SHAPE")
+        if codes.dtype != torch.uint8 or block_scales.dtype != torch.uint8:
+            _refuse("Microscale.from_rows", "codes and scales must be uint8")
+        if cols % 2:
+            codes = codes.clone()
+            codes[:, -1] &= 15
+        c = F.pad(codes, (0, 16 * (-(-cols // 32)) - codes.shape[1])).contiguous()
+        s = F.pad(block_scales, (0, -nb % 4, 0, -rows % 128))
+        s = s.view(s.shape[0] // 128, 4, 32, s.shape[1] // 4, 4).permute(0, 3, 2, 1, 4).reshape(-1)
+        return cls(c.view(-1), s.contiguous(), rows, cols, fmt, scale)
+
+    def block_scales(self):
+        """The scale bytes by row and block (uint8, rows x blocks)."""
+        nb = -(-self.cols // _MICRO_BLOCK[self.fmt])
+        rt, ct = -(-self.rows // 128), -(-nb // 4)
+        s = self.scales.view(rt, ct, 32, 4, 4).permute(0, 3, 2, 1, 4).reshape(rt * 128, ct * 4)
+        return s[:self.rows, :nb]
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def _struct(self) -> "_Microscale":
+        return _Microscale(MICRO_FORMATS[self.fmt], self.rows, self.cols, self.scale, self.codes.data_ptr(),
+                           self.scales.data_ptr())
+
+
+def microscale_bytes(fmt: str, rows: int, cols: int):
+    """Bytes of a microscaled matrix's codes and scales."""
+    if fmt not in MICRO_FORMATS:
+        _refuse("microscale_bytes", f"unknown format {fmt!r}")
+    nc, ns = _SZ(0), _SZ(0)
+    _check(_lib().bitsmoe_microscale_bytes(MICRO_FORMATS[fmt], int(rows), int(cols), ctypes.byref(nc),
+                                           ctypes.byref(ns)), "bitsmoe_microscale_bytes")
+    return int(nc.value), int(ns.value)
+
+
+def _on(device, stream):
+    """Context with `device` current and its stream (the given one or the current one): outputs are
+    allocated on the stream that writes them."""
+    import torch
+    return torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device))
+
+
+def microscale_quantize(x, fmt: str = "e8m0", scale: float = 1.0, out: Optional[Microscale] = None,
+                        stream=None) -> Microscale:
+    """Quantise the rows of x (torch fp32 or bf16, 2-d, dense rows, on the device) into a Microscale with
+    tensor scale `scale` (a power of two); `out` reuses an existing one of the same shape and format."""
+    import torch
+    ty = _dense_type("microscale_quantize", "x", x.dtype)
+    ld = _rows("microscale_quantize", "x", x)
+    rows, cols = int(x.shape[0]), int(x.shape[1])
+    with _on(x.device, stream):
+        if out is None:
+            out = Microscale.empty(rows, cols, fmt, scale, x.device)
+        elif (out.rows, out.cols, out.fmt) != (rows, cols, fmt) or out.device != x.device:
+            _refuse("microscale_quantize", "out has another shape, format or device", "SHAPE")
+        out.scale = float(scale)
+        _check(_lib().bitsmoe_microscale_quantize(x.data_ptr(), ty, ld, out._struct(),
+                                                  torch.cuda.current_stream().cuda_stream),
+               "bitsmoe_microscale_quantize")
+    return out
+
+
+def microscale_dequantize(q: Microscale, dtype=None, out=None, stream=None):
+    """The values of a Microscale as a torch tensor rows x cols (float32, or bfloat16)."""
+    import torch
+    with _on(q.device, stream):
+        if out is None:
+            out = torch.empty((q.rows, q.cols), dtype=dtype if dtype is not None else torch.float32, device=q.device)
+        ty = _dense_type("microscale_dequantize", "out", out.dtype)
+        ld = _rows("microscale_dequantize", "out", out, q.rows, q.cols, q.device)
+        _check(_lib().bitsmoe_microscale_dequantize(q._struct(), out.data_ptr(), ty, ld,
+                                                    torch.cuda.current_stream().cuda_stream),
+               "bitsmoe_microscale_dequantize")
+    return out
+
+
+def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=None, y=None, status=None,
+                       stream=None):
+    """y (T x w.rows, fp32 by default, or bf16) = x w^T for x a torch bf16 tensor (T x w.cols, dense rows) or a
+    Microscale of w's format; with `up` (w's shape and format) SiLU(x w^T) * (x up^T).  `status`: an optional
+    int32 tensor of one element that receives a device-side timeout."""
+    import torch
+    where = "microscale_product"
+    coded = isinstance(x, Microscale)
+    if (x.device != w.device) or (up is not None and up.device != w.device):
+        _refuse(where, "the operands are on different devices")
+    if coded:
+        T, x_ptr, x_ld = x.rows, None, 0
+    else:
+        x_ld = _rows(where, "x", x, None, w.cols, w.device, torch.bfloat16)
+        T, x_ptr = int(x.shape[0]), x.data_ptr()
+    if status is not None and (status.dtype != torch.int32 or status.numel() != 1 or status.device != w.device):
+        _refuse(where, "status must be one int32 on the operands' device")
+    with _on(w.device, stream):
+        if y is None:
+            y = torch.empty((T, w.rows), dtype=dtype if dtype is not None else torch.float32, device=w.device)
+        ty = _dense_type(where, "y", y.dtype)
+        y_ld = _rows(where, "y", y, T, w.rows, w.device)
+        _check(_lib().bitsmoe_microscale_product(w._struct(), up._struct() if up is not None else None, x_ptr, x_ld,
+                                                 x._struct() if coded else None, T, y.data_ptr(), ty, y_ld,
+                                                 status.data_ptr() if status is not None else None,
+                                                 torch.cuda.current_stream().cuda_stream),
+               "bitsmoe_microscale_product")
+    return y
+
+
+def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: float = 1e-6, gate=None,
+               gate_sigmoid: bool = False, channel_scale=None, branch_scale: float = 1.0,
+               residual_scale: float = 1.0, pre_norm: bool = True, pre_gain=None, pre_eps: float = 1e-6,
+               gain_offset: float = 0.0, h_out=None, x=None, x_dtype=None, stream=None):
+    """What stands between a block's output y and the next block's input (see bitsmoe_block_norm):
+    returns (h', x), h' = residual_scale h + branch_scale channel_scale gate norm(y) and x = norm(h').
+
+    h (T x D, fp32 or bf16) is the residual stream; y None: h' is not formed (the result's first item is h
+    times residual_scale only when h_out is given, else None); gate is a vector of T (one value per row) or
+    T x D; the gains and channel_scale are vectors of D of one type.  h_out and x are allocated when not
+    given (h_out may be h: in place); pre_norm False returns x None."""
+    import torch
+    where = "block_norm"
+    a = _BlockNormArgs()
+    a.h_type, a.h_ld = _dense_type(where, "h", h.dtype), _rows(where, "h", h)
+    T, D, dev = int(h.shape[0]), int(h.shape[1]), h.device
+    a.T, a.D, a.h = T, D, h.data_ptr()
+    if y is not None:
+        a.y_type, a.y_ld = _dense_type(where, "y", y.dtype), _rows(where, "y", y, T, D, dev)
+        a.y = y.data_ptr()
+    if gate is not None:
+        a.gate_type = _dense_type(where, "gate", gate.dtype)
+        if gate.dim() == 1:
+            if gate.shape[0] != T or gate.device != dev:
+                _refuse(where, f"gate has shape {tuple(gate.shape)} on {gate.device}, expected {(T,)} on {dev}", "SHAPE")
+            a.gate_kind, a.gate_ld = _GATE_TOKEN, max(int(gate.stride(0)), 1)
+            if T > 1 and gate.stride(0) < 1:
+                _refuse(where, "gate's elements overlap")
+        else:
+            a.gate_kind, a.gate_ld = _GATE_ELEMENT, _rows(where, "gate", gate, T, D, dev)
+        a.gate = gate.data_ptr()
+    vecs = [v for v in (post_gain, pre_gain, channel_scale) if v is not None]
+    gt = vecs[0].dtype if vecs else torch.float32
+    a.gain_type = _dense_type(where, "gains", gt)
+    a.post_gain = _vector(where, "post_gain", post_gain, D, dev, gt)
+    a.pre_gain = _vector(where, "pre_gain", pre_gain, D, dev, gt)
+    a.channel_scale = _vector(where, "channel_scale", channel_scale, D, dev, gt)
+    a.post_norm, a.gate_sigmoid = int(bool(post_norm)), int(bool(gate_sigmoid))
+    a.post_eps, a.pre_eps, a.gain_offset = post_eps, pre_eps, gain_offset
+    a.residual_scale, a.branch_scale = residual_scale, branch_scale
+    with _on(dev, stream):
+        if h_out is None and y is not None:
+            h_out = torch.empty((T, D), dtype=h.dtype, device=dev)
+        if h_out is not None:
+            a.h_out_ld = _rows(where, "h_out", h_out, T, D, dev, h.dtype)
+            a.h_out = h_out.data_ptr()
+        if x is None and pre_norm:
+            x = torch.empty((T, D), dtype=x_dtype if x_dtype is not None else torch.bfloat16, device=dev)
+        if x is not None:
+            if not pre_norm:
+                _refuse(where, "x is given but pre_norm is off")
+            a.x_type, a.x_ld = _dense_type(where, "x", x.dtype), _rows(where, "x", x, T, D, dev)
+            a.x = x.data_ptr()
+        _check(_lib().bitsmoe_block_norm(ctypes.byref(a), torch.cuda.current_stream().cuda_stream),
+               "bitsmoe_block_norm")
+    return h_out, x
 
 
 def bitsmoe_debug_single_token_kernel(which: int) -> None:

@@ -1,14 +1,16 @@
 """Build libbitsmoe.so in-tree with nvcc for sm_103a (GB300).
 
-Ten translation units, compiled in parallel: the host packer (pack.cpp,
+Thirteen translation units, compiled in parallel: the host packer (pack.cpp,
 plain C++), the CUDA kernel chain + C ABI (forward.cu), the two fused
 single-token decode kernels (fused.cu, and the clustered one in fused2.cu),
 the tensor-core projections (gemm.cu), the tensor-core expert factors of
 calls with several tokens (expert_mma.cu), the per-unit quantiser from float spectral vectors
 (quantize.cu), the per-projection bit allocation (allocate.cu) and the
 importance beta from calibration tokens that the allocation weighs its losses
-by (importance.cu), and the shared-basis decomposition with the calibration
-Gram (decompose.cu).  The CUDA runtime is linked statically, so the library
+by (importance.cu), the shared-basis decomposition with the calibration
+Gram (decompose.cu), the microscaled 4-bit quantiser and product
+(microscale.cu, microscale_product.cu) and the norms between blocks
+(block_norm.cu).  The CUDA runtime is linked statically, so the library
 loads on a machine without a GPU (the host-only entry points then work; the
 device ones return BITSMOE_ERR_CUDA).
 """
@@ -44,7 +46,8 @@ def _run(cmd):
 
 def sources():
     return [os.path.join(CSRC, f) for f in ("pack.cpp", "forward.cu", "fused.cu", "fused2.cu", "gemm.cu", "expert_mma.cu",
-                                              "quantize.cu", "allocate.cu", "importance.cu", "decompose.cu")]
+                                              "quantize.cu", "allocate.cu", "importance.cu", "decompose.cu",
+                                              "microscale.cu", "microscale_product.cu", "block_norm.cu")]
 
 
 def up_to_date() -> bool:

@@ -1,0 +1,352 @@
+"""GPU parity of the microscaled 4-bit quantiser, its inverse and the product (through the C ABI) against
+the oracle (oracle/microscale.py, fp64).
+
+The quantiser is bit-exact.  Product tolerance, by arithmetic: the products of two codes or of a code with a
+bf16 value are exact in fp32, a sum of K of them in any order is off by at most (K - 1) roundings, each at
+most a step (2^-23, truncation counted) of the sum of magnitudes, and the tensor scale, its application and
+a split of the sum add 4 more: (K + 4) 2^-23 sum |w x|.  A bf16 result adds half a step, 2^-8 |y|.  For
+silu(g) u: |silu'| <= 1.1, so 1.1 eg |u| + |silu(g)| eu + 1.1 eg eu, and 16 roundings (exp, sum, quotient and
+product) of 2^-23 |y|.
+"""
+import numpy as np
+import pytest
+
+from oracle import microscale as om
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -23
+
+
+@pytest.fixture(scope="module")
+def env():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import __graft_entry__
+    __graft_entry__.build()
+    import paper_2606_00079_gb300 as bm
+    torch.cuda.set_device(0)
+    return torch, bm
+
+
+def bf16(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(torch.bfloat16)
+
+
+def check_quantized(q, x, fmt, scale):
+    codes, byte = om.quantize(x, fmt, scale)
+    rows = x.shape[0]
+    np.testing.assert_array_equal(q.scales.cpu().numpy(), om.tile_scales(byte))
+    np.testing.assert_array_equal(q.codes.cpu().numpy().reshape(rows, -1), om.pack_codes(codes))
+    return om.values(codes, byte, fmt, scale)
+
+
+SHAPES = [(1, 1), (1, 31), (3, 33), (2, 16), (5, 1001), (33, 130), (129, 64), (257, 512), (130, 2048), (300, 2050)]
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_quantizer_is_bit_exact(env, fmt, dt, shape):
+    torch, bm = env
+    rng = np.random.default_rng([*shape, len(fmt), len(dt)])
+    x = rng.standard_normal(shape) * np.exp(rng.uniform(-12, 4, (shape[0], 1)))
+    x[:, 0::7] *= 20
+    x[shape[0] // 2] = 0.0
+    t = torch.from_numpy(x.astype(np.float32))
+    if dt == "bf16":
+        t = t.to(torch.bfloat16)
+    scale = 1.0 if fmt == "e8m0" else 2.0 ** -6
+    q = bm.microscale_quantize(t.cuda(), fmt, scale)
+    v = check_quantized(q, t.float().numpy(), fmt, scale)
+    for out in (torch.float32, torch.bfloat16):
+        got = bm.microscale_dequantize(q, out).cpu()
+        assert torch.equal(got, torch.from_numpy(v).to(out))
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+def test_quantizer_at_the_borders(env, fmt):
+    """Ties between codes and between scales with their fp32 neighbours, powers of two and their neighbours,
+    subnormals, the largest values, both zeros."""
+    torch, bm = env
+    blk = om.BLOCK[fmt]
+    rng = np.random.default_rng(11)
+    mids = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0], np.float32)
+    around = np.concatenate([mids, np.nextafter(mids, np.float32(0)), np.nextafter(mids, np.float32(9))])
+    rows = []
+    if fmt == "e8m0":
+        tops = np.float32(2.0) ** np.array([-140, -127, -126, -125, -60, -3, 0, 1, 60, 125, 126], np.float32)
+        tops = np.concatenate([tops, np.nextafter(tops, np.float32(0)), tops * np.float32(1.5),
+                               [np.float32(3.4e38), np.float32(2e-45)]])
+        for top in tops:
+            x = (2.0 ** np.floor(np.log2(np.float64(top))) / 4) * rng.choice(around, 2 * blk).astype(np.float64)
+            x = np.where(np.abs(x) > top, top, x).astype(np.float32)
+            x[0], x[blk], x[3], x[5] = top, -top, 0.0, -0.0
+            rows.append(x * rng.choice([-1, 1], 2 * blk).astype(np.float32))
+    else:
+        s = om.E4M3[:127].astype(np.float64)
+        tops = np.concatenate([6 * s, 3 * (s[1:] + s[:-1])]).astype(np.float32)   # scales and their midpoints
+        tops = np.concatenate([tops, np.nextafter(tops, np.float32(0)), np.nextafter(tops, np.float32(1e9)),
+                               np.float32([1e4, 1e-6, 1e-30, 3e38])])
+        for top in tops:
+            sc = om.E4M3[om.nearest_even(np.minimum(np.float64(top) / 6, 448.0), om.E4M3[:127])]
+            m = rng.choice(mids[:7], 2 * blk) * sc                                # exact in fp32: 7 bits
+            x = m.astype(np.float32)
+            j = rng.integers(0, 3, 2 * blk)
+            x = np.where(j == 1, np.nextafter(x, np.float32(0)), np.where(j == 2, np.nextafter(x, np.float32(1e9)), x))
+            x = np.minimum(x, top)
+            x[0], x[blk] = top, top
+            x = (x * rng.choice([-1, 1], 2 * blk)).astype(np.float32)
+            rows.append(x)
+    x = np.stack(rows)
+    for scale in (1.0, 2.0 ** -40, 2.0 ** 3):
+        with np.errstate(over="ignore"):
+            xs = (x * np.float32(scale)).astype(np.float32)
+        q = bm.microscale_quantize(torch.from_numpy(xs).cuda(), fmt, scale)
+        if scale == 1.0:
+            check_quantized(q, xs, fmt, scale)
+            xb = bf16(xs)
+            check_quantized(bm.microscale_quantize(xb.cuda(), fmt, 1.0), xb.float().numpy(), fmt, 1.0)
+        else:
+            # v = x / scale in fp32: what the definition quantises (x may have lost bits, the quotient may too)
+            with np.errstate(over="ignore", under="ignore"):
+                check_quantized(q, (xs / np.float32(scale)).astype(np.float32), fmt, 1.0)
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+def test_quantizer_blocks_without_a_scale(env, fmt):
+    """A NaN or an infinity makes its own block NaN and no other; the product passes it on to that row only."""
+    torch, bm = env
+    rng = np.random.default_rng(5)
+    x = rng.standard_normal((6, 70)).astype(np.float32)
+    x[1, 40] = np.nan
+    x[2, 3] = np.inf
+    x[3, 69] = -np.inf
+    q = bm.microscale_quantize(torch.from_numpy(x).cuda(), fmt, 1.0)
+    v = check_quantized(q, x, fmt, 1.0)
+    got = bm.microscale_dequantize(q).cpu().numpy()
+    np.testing.assert_array_equal(got, v.astype(np.float32))
+    assert np.isnan(got[1]).sum() in (16, 32) and np.isnan(got).any(axis=1).tolist() == [False, True, True, True, False, False]
+    act = bf16(rng.standard_normal((3, 70)))
+    y = bm.microscale_product(q, act.cuda()).cpu().numpy()
+    assert np.isnan(y).any(axis=0).tolist() == [False, True, True, True, False, False]
+    aq = bm.microscale_quantize(act.cuda(), fmt, 1.0)
+    y = bm.microscale_product(q, aq).cpu().numpy()
+    assert np.isnan(y).any(axis=0).tolist() == [False, True, True, True, False, False]
+    assert np.isnan(y).all(axis=0).tolist() == [False, True, True, True, False, False]
+
+
+@pytest.mark.parametrize("ty", ["f32", "bf16"])
+def test_quantizer_strides_and_alignment(env, ty):
+    """Rows apart and on odd addresses; what lies between the rows is neither read into a block nor written."""
+    torch, bm = env
+    dt = torch.float32 if ty == "f32" else torch.bfloat16
+    g = torch.Generator().manual_seed(1)
+    for ld, off, cols in ((72, 0, 64), (67, 1, 64), (133, 3, 130), (1040, 8, 1024)):
+        base = torch.randn(9 * ld + off, generator=g).to(dt)
+        x = base[off:off + 9 * ld].view(9, ld)[:, :cols]
+        dev = base.cuda()[off:off + 9 * ld].view(9, ld)[:, :cols]
+        q = bm.microscale_quantize(dev, "e4m3", 1.0)
+        check_quantized(q, x.float().numpy(), "e4m3", 1.0)
+        out = torch.full((9 * ld + off,), 7.0, dtype=dt, device="cuda")
+        view = out[off:off + 9 * ld].view(9, ld)[:, :cols]
+        bm.microscale_dequantize(q, out=view)
+        assert torch.equal(view, bm.microscale_dequantize(q, dt))
+        rest = torch.ones_like(out, dtype=torch.bool)
+        rest[off:off + 9 * ld].view(9, ld)[:, :cols] = False
+        assert (out[rest] == 7).all()
+
+
+def test_quantizer_offsets_past_32_bits(env):
+    """More than 2^32 elements and 2^31 code bytes: the last rows equal the same rows quantised alone."""
+    torch, bm = env
+    rows, cols = 70000, 65536
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x[-3:] = torch.randn(3, cols, device="cuda").to(torch.bfloat16)
+    q = bm.microscale_quantize(x, "e8m0")
+    alone = bm.microscale_quantize(x[-3:], "e8m0")
+    assert torch.equal(q.codes.view(rows, -1)[-3:], alone.codes.view(3, -1))
+    assert torch.equal(q.block_scales()[-3:], alone.block_scales())
+    assert int(q.codes.view(rows, -1)[:-3].max()) == 0
+    act = torch.randn(1, cols, device="cuda").to(torch.bfloat16)
+    y = bm.microscale_product(q, act)
+    assert torch.equal(y[:, -3:], bm.microscale_product(alone, act))
+    assert int(torch.count_nonzero(y[:, :-3])) == 0
+
+
+def make(rng, rows, cols, fmt, scale=None):
+    """A random matrix of any codes and varied block scales: (Microscale arrays, fp64 values)."""
+    codes = rng.integers(0, 16, (rows, cols)).astype(np.uint8)
+    nb = -(-cols // om.BLOCK[fmt])
+    byte = rng.integers(110, 130, (rows, nb)) if fmt == "e8m0" else rng.integers(1, 100, (rows, nb))
+    scale = scale or float(np.float32(0.37))
+    return codes, byte.astype(np.uint8), scale, om.values(codes, byte, fmt, float(np.float32(scale)))
+
+
+def upload(env, m, fmt):
+    torch, bm = env
+    codes, byte, scale, _ = m
+    p = np.pad(codes, ((0, 0), (0, codes.shape[1] % 2)))
+    return bm.Microscale.from_rows(torch.from_numpy(p[:, 0::2] | (p[:, 1::2] << 4)).cuda(),
+                                   torch.from_numpy(byte).cuda(), codes.shape[1], fmt, scale)
+
+
+def check_product(env, T, rows, cols, fmt, coded, glu, out, seed=0):
+    torch, bm = env
+    rng = np.random.default_rng([seed, T, rows, cols])
+    w = make(rng, rows, cols, fmt)
+    u = make(rng, rows, cols, fmt, 0.01) if glu else None
+    if coded:
+        a = make(rng, T, cols, fmt, 0.5)
+        x, xv = upload(env, a, fmt), a[3]
+    else:
+        t = bf16(rng.standard_normal((T, cols)) * np.exp(rng.uniform(-3, 3, (T, 1))))
+        x, xv = t.cuda(), t.double().numpy()
+    dt = torch.float32 if out == "f32" else torch.bfloat16
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    y = bm.microscale_product(upload(env, w, fmt), x, up=upload(env, u, fmt) if glu else None, dtype=dt, status=status)
+    got = y.double().cpu().numpy()
+    assert int(status.item()) == 0
+    r = om.product(w[3], xv, u[3] if glu else None)
+    e = (cols + 4) * U * r[1]
+    want = r[0]
+    if glu:
+        eu = (cols + 4) * U * r[3]
+        want = om.silu(r[0]) * r[2]
+        e = 1.1 * e * np.abs(r[2]) + np.abs(om.silu(r[0])) * eu + 1.1 * e * eu + 16 * U * np.abs(want)
+    tol = e + (2.0 ** -8 * (np.abs(want) + e) if out == "bf16" else 0) + 1e-37
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:4].tolist(), int(bad.sum()), float((np.abs(got - want) / tol).max()))
+
+
+PRODUCTS = [   # T, rows, cols
+    (1, 1, 1), (1, 128, 64), (2, 3, 31), (1, 130, 33), (3, 127, 129), (5, 256, 256), (8, 129, 500), (16, 200, 1001),
+    (17, 384, 2048), (33, 65, 255), (64, 300, 320), (100, 257, 640), (128, 128, 512), (129, 140, 257), (255, 128, 96),
+    (256, 256, 1024), (257, 130, 130), (300, 512, 768), (520, 1000, 200),
+]
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+@pytest.mark.parametrize("x", ["bf16", "coded"])
+@pytest.mark.parametrize("shape", PRODUCTS)
+def test_product(env, fmt, x, shape):
+    check_product(env, *shape, fmt, x == "coded", False, "f32")
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+@pytest.mark.parametrize("x", ["bf16", "coded"])
+@pytest.mark.parametrize("shape", PRODUCTS[::2])
+def test_product_swiglu(env, fmt, x, shape):
+    check_product(env, *shape, fmt, x == "coded", True, "bf16")
+    check_product(env, *shape, fmt, x == "coded", True, "f32", seed=1)
+
+
+@pytest.mark.parametrize("x", ["bf16", "coded"])
+@pytest.mark.parametrize("T,rows,cols", [(1, 4096, 14336), (7, 2048, 8192), (40, 1536, 4096), (700, 640, 4096)])
+def test_product_large(env, x, T, rows, cols):
+    check_product(env, T, rows, cols, "e4m3", x == "coded", False, "f32")
+    check_product(env, T, rows, cols, "e8m0", x == "coded", False, "bf16")
+
+
+@pytest.mark.parametrize("coded", [False, True])
+@pytest.mark.parametrize("T", [1, 9, 140])
+def test_product_strides(env, coded, T):
+    """x rows apart and off 16-byte boundaries, y rows apart and off them: the same values as dense ones, and
+    what lies between and behind y's rows stays."""
+    torch, bm = env
+    rng = np.random.default_rng(T)
+    rows, cols = 150, 264
+    w = upload(env, make(rng, rows, cols, "e4m3"), "e4m3")
+    x = bf16(rng.standard_normal((T, cols))).cuda()
+    xq = bm.microscale_quantize(x, "e4m3", 1.0)
+    ref = bm.microscale_product(w, xq if coded else x)
+    for ld, off in ((264, 0), (272, 8), (265, 0), (300, 1), (267, 3)):
+        buf = torch.full((T * ld + 8,), float("nan"), dtype=torch.bfloat16, device="cuda")
+        xv = buf[off:off + T * ld].view(T, ld)[:, :cols]
+        xv.copy_(x)
+        for dt in (torch.float32, torch.bfloat16):
+            out = torch.full(((T + 1) * 161 + 5,), 7.0, dtype=dt, device="cuda")
+            yv = out[off:off + T * 161].view(T, 161)[:, :rows]
+            bm.microscale_product(w, xq if coded else xv, y=yv)
+            assert torch.equal(yv, ref.to(dt)), (ld, off, dt)
+            rest = torch.ones_like(out, dtype=torch.bool)
+            rest[off:off + T * 161].view(T, 161)[:, :rows] = False
+            assert (out[rest] == 7).all()
+
+
+def test_product_with_values_that_are_not_finite(env):
+    """A NaN or infinite activation reaches its own row of y only."""
+    torch, bm = env
+    rng = np.random.default_rng(2)
+    w = upload(env, make(rng, 70, 100, "e8m0"), "e8m0")
+    x = bf16(rng.standard_normal((20, 100)))
+    clean = bm.microscale_product(w, x.cuda())
+    x[3, 50] = float("nan")
+    x[7, 0] = float("inf")
+    y = bm.microscale_product(w, x.cuda())
+    keep = [t for t in range(20) if t not in (3, 7)]
+    assert torch.equal(y[keep], clean[keep])
+    assert not torch.isfinite(y[3]).any() and not torch.isfinite(y[7]).all()
+    q = bm.microscale_product(w, bm.microscale_quantize(x.cuda(), "e8m0"))
+    assert torch.isnan(q[3]).all() and torch.isnan(q[7]).all() and torch.isfinite(q[keep]).all()
+
+
+def test_product_scale_extremes(env):
+    """E8M0 scales far from 1 whose products stay in fp32's range."""
+    torch, bm = env
+    rng = np.random.default_rng(9)
+    for lo, hi, xs in ((0, 4, 2.0 ** 100), (240, 245, 2.0 ** -60)):
+        codes = rng.integers(0, 16, (130, 96)).astype(np.uint8)
+        byte = rng.integers(lo, hi, (130, 3)).astype(np.uint8)
+        v = om.values(codes, byte, "e8m0", 1.0)
+        t = bf16(rng.standard_normal((5, 96)) * xs)
+        y = bm.microscale_product(upload(env, (codes, byte, 1.0, None), "e8m0"), t.cuda()).double().cpu().numpy()
+        want, mag = om.product(v, t.double().numpy())
+        assert (np.abs(y - want) <= 100 * U * mag).all()
+
+
+def test_empty_calls_write_nothing(env):
+    torch, bm = env
+    rng = np.random.default_rng(0)
+    w = upload(env, make(rng, 5, 64, "e8m0"), "e8m0")
+    assert bm.microscale_product(w, torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda")).shape == (0, 5)
+    assert bm.microscale_product(w, bm.Microscale.empty(0, 64)).shape == (0, 5)
+    assert bm.microscale_quantize(torch.zeros(0, 64, device="cuda")).rows == 0
+    assert bm.microscale_dequantize(bm.Microscale.empty(0, 64)).shape == (0, 64)
+    none = bm.Microscale.empty(0, 64)
+    assert bm.microscale_product(none, torch.zeros(3, 64, dtype=torch.bfloat16, device="cuda")).shape == (3, 0)
+
+
+@pytest.mark.parametrize("coded", [False, True])
+def test_product_on_streams_in_graphs_and_again(env, coded):
+    """The same bits on the current stream, on another one, on two at once, captured and replayed with new
+    inputs in the same buffers."""
+    torch, bm = env
+    rng = np.random.default_rng(4)
+    w = upload(env, make(rng, 700, 1024, "e4m3"), "e4m3")
+    u = upload(env, make(rng, 700, 1024, "e4m3", 0.01), "e4m3")
+    xs = [bf16(rng.standard_normal((24, 1024))).cuda() for _ in range(2)]
+    xq = [bm.microscale_quantize(x, "e4m3", 1.0) for x in xs] if coded else xs
+    ref = [bm.microscale_product(w, x, up=u) for x in xq]
+    assert torch.equal(bm.microscale_product(w, xq[0], up=u), ref[0])
+    torch.cuda.synchronize()
+    s = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = [bm.microscale_product(w, xq[i], up=u, stream=s[i]) for i in range(2)]
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+    x = xs[0].clone()
+    y = torch.empty_like(ref[0])
+    q = bm.Microscale.empty(24, 1024, "e4m3", 1.0)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        if coded:
+            bm.microscale_quantize(x, "e4m3", 1.0, out=q)
+        bm.microscale_product(w, q if coded else x, up=u, y=y)
+    for i in (0, 1, 0):
+        x.copy_(xs[i])
+        y.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, ref[i])
