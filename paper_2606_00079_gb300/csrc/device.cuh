@@ -217,6 +217,8 @@ constexpr int kSplitTokens = 64;
 // y = Phi_dn s (mode 1; y += when p.accum) for all T tokens of p.  Mode 0 also
 // clears `zero` and takes max |z| per token into zmax (cleared by the router).
 bool make_basis_map(void* map_out, const void* base, int rows, int cols_pad);
+// TMA map of a row-major matrix of bytes or bf16 for tiles of box_rows rows x 128 bytes (gemm.cu); pitch a multiple of 16.
+bool make_row_map(void* map_out, bool bytes, const void* base, int64_t rows, int64_t cols, int64_t pitch_bytes, int box_rows);
 cudaError_t launch_gemm_tc(int mode, const void* map, const Fwd& p, int sms, cudaStream_t st, bool pdl,
                            void* zero = nullptr, size_t zero_bytes = 0, uint32_t* zmax = nullptr);
 // Multi-token expert factors on mma.sync (expert_mma.cu): sizes for T tokens (false when the layer

@@ -32,13 +32,6 @@ constexpr int kGThreads = 64 + kStagers;     // warp 0 TMA, warp 1 MMA
 constexpr int kKB = 64;                    // K elements per stage (one 128-byte swizzle row of bf16)
 constexpr uint32_t kATile = 128 * kKB * 2; // bytes of an A stage (128 rows)
 
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
-
 // Eight fp32 values -> bf16 hi and lo = bf16(value - hi)
 __device__ __forceinline__ void split_bf16(const float4 (&v)[2], uint4& hi, uint4& lo) {
   const float f[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
@@ -407,18 +400,26 @@ EncodeTiledFn encode_fn() {
 
 namespace bmoe {
 
-// Tensor map of a row-major bf16 matrix [rows][cols_pad] for tiles of box_rows rows and 64
-// columns with 128-byte swizzle.  cols_pad * 2 must be a multiple of 16.
-static bool make_map(CUtensorMap* m, const void* base, int rows, int cols_pad, int box_rows) {
+// Tensor map of a row-major matrix for tiles of box_rows rows and 128 bytes of a row with 128-byte
+// swizzle (what lies outside the matrix is read as zeros).  The pitch must be a multiple of 16 bytes.
+bool make_row_map(void* map_out, bool bytes, const void* base, int64_t rows, int64_t cols, int64_t pitch_bytes, int box_rows) {
   EncodeTiledFn fn = encode_fn();
-  if (!fn || rows < 1 || cols_pad < 8 || (cols_pad * 2) % 16 || (reinterpret_cast<uintptr_t>(base) & 15)) return false;
-  const cuuint64_t dims[2] = {(cuuint64_t)cols_pad, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)cols_pad * 2};
-  const cuuint32_t box[2] = {(cuuint32_t)kKB, (cuuint32_t)box_rows};
+  if (!fn || rows < 1 || cols < 1 || pitch_bytes < 16 || pitch_bytes % 16 || box_rows < 1 || box_rows > 256 ||
+      (reinterpret_cast<uintptr_t>(base) & 15))
+    return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)pitch_bytes};
+  const cuuint32_t box[2] = {(cuuint32_t)(bytes ? 128 : 64), (cuuint32_t)box_rows};
   const cuuint32_t estr[2] = {1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return fn(static_cast<CUtensorMap*>(map_out), bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+            const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Tensor map of a row-major bf16 matrix [rows][cols_pad] for tiles of box_rows rows and 64
+// columns.  cols_pad * 2 must be a multiple of 16.
+static bool make_map(CUtensorMap* m, const void* base, int rows, int cols_pad, int box_rows) {
+  return cols_pad >= 8 && make_row_map(m, false, base, rows, cols_pad, (int64_t)cols_pad * 2, box_rows);
 }
 bool make_basis_map(void* map_out, const void* base, int rows, int cols_pad) {
   return make_map(static_cast<CUtensorMap*>(map_out), base, rows, cols_pad, 128);

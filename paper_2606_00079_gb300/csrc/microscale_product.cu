@@ -4,9 +4,13 @@
 //   or, with a second matrix U of the same shape, SiLU(W x) * (U x)
 //
 // x in bf16, or itself microscaled.
-#include "microscale.cuh"
-
 #include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+
+#include "microscale.cuh"
+#include "tc.cuh"
 
 namespace {
 using namespace bmoe;
@@ -101,6 +105,734 @@ __global__ void __launch_bounds__(kPThreads) k_micro_product(ProductArgs a) {
   }
 }
 
+__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + expf(-g)) * u; }
+
+__device__ __forceinline__ void store_y(void* y, int type, int64_t i, float v) {
+  if (type == BITSMOE_F32) static_cast<float*>(y)[i] = v;
+  else static_cast<__nv_bfloat16*>(y)[i] = __float2bfloat16_rn(v);
+}
+
+// ---------------------------------------------------------------------------
+// Few tokens: the weights' codes pass once through shared memory into warp-level
+// products (mma.sync m16n8k16, 16 weight rows x 8 tokens x 16 columns).
+//
+// A code is exact in fp16, and two of them are converted by one instruction
+// (e2m1x2 -> f16x2: 7 operations for 8 codes with the byte picks; forming bf16
+// bit patterns takes 15).  The activations of a CTA's columns are scaled by a power
+// of two that brings their largest to [2^14, 2^15) and kept in fp16 when all of them
+// are exact there (bf16's 8 bits over 32 binades below the largest); otherwise the
+// CTA takes the bf16 products (the codes as bf16 bit patterns times 2^126).  All 16 columns of a product lie in one block of
+// each row, so the block's scale is applied to the product's fp32 result.
+// ---------------------------------------------------------------------------
+constexpr int kFewWarps = 16;                      // consumers: 8 row tiles x 2 halves of a stage's columns
+constexpr int kFewThreads = 32 * (kFewWarps + 1);  // and the warp that copies
+constexpr int kFewTokens = 16;
+constexpr int kStageK = 256;                       // columns of a stage (128 bytes of codes a row)
+constexpr uint32_t kCodeTile = 128 * 128;          // bytes of 128 rows of a stage's codes
+
+struct FewArgs {
+  int T, rows, cols, tiles;
+  int nst, sps, splits, stages;
+  uint32_t stage;
+  uint32_t x_pitch;      // bytes of a token's activations in shared memory
+  const uint8_t* ws;
+  const uint8_t* us;
+  const __nv_bfloat16* x;
+  int64_t x_ld;
+  int x_vec;             // x's rows can be read 16 bytes at a time
+  MicroMat xq;
+  float sw, su;
+  void* y;
+  int y_type;
+  int64_t y_ld;
+  long long spin;
+  int lose;
+  int* status;
+};
+
+template <bool BF>
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const float (&c)[4]) {
+  if constexpr (BF)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+
+// The codes of byte B of w (columns 2B and 2B + 1) as a pair of fp16, or of bf16.
+template <bool BF, int B>
+__device__ __forceinline__ uint32_t code_pair(uint32_t w) {
+  uint32_t r;
+  if constexpr (!BF) {
+    asm("{\n .reg .b8 t0, t1, t2, t3;\n mov.b32 {t0, t1, t2, t3}, %1;\n cvt.rn.f16x2.e2m1x2 %0, t0;\n}" : "=r"(r) : "r"(w >> (8 * B)));
+  } else {
+    const uint32_t n = ((w >> (8 * B)) & 0xFu) | (((w >> (8 * B + 4)) & 0xFu) << 16);
+    r = ((n & 0x00080008u) << 12) | ((n & 0x00070007u) << 6);            // the values times 2^-126
+    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(r) : "r"(0x7E807E80u));       // 2^126: exact
+  }
+  return r;
+}
+
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint4 lds128a(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+
+// The four block scales of a scale word in fp32, times inv.
+template <int FMT>
+__device__ __forceinline__ void scales4(uint32_t w, float inv, float (&s)[4]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint16_t p = (uint16_t)(w >> (16 * h));
+    uint32_t r;
+    if constexpr (FMT == BITSMOE_MICRO_E8M0) {
+      asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(r) : "h"(p));
+      s[2 * h] = bf16lo(r) * inv;
+      s[2 * h + 1] = bf16hi(r) * inv;
+    } else {
+      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(p));
+      s[2 * h] = f16lo(r) * inv;
+      s[2 * h + 1] = f16hi(r) * inv;
+    }
+  }
+}
+
+// This warp's 16 rows x 128 columns of a stage (half kh) with NT tiles of 8 tokens.
+template <int FMT, int NA, int NT, bool BF>
+__device__ __forceinline__ void few_half(uint32_t code, uint32_t sf, uint32_t xa, uint32_t x_pitch, int T, int rt, int kh,
+                                         int lane, int tiles_left, float inv, float (&acc)[NA][NT][4]) {
+  constexpr bool E8 = FMT == BITSMOE_MICRO_E8M0;
+  constexpr int TPH = E8 ? 1 : 2;   // scale tiles of a half
+  constexpr int CPS = 2 * TPH;
+  const int g = lane >> 2, t = lane & 3;
+  const int r = 16 * rt + g;
+  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int q = 0; q < TPH; ++q) {
+    const int tile = kh * TPH + q;
+    if (tile >= tiles_left) return;   // past the matrix's columns (and its scales)
+    float s[NA][2][4];
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int rr = r + 8 * h;
+        scales4<FMT>(lds32(sf + (uint32_t)(a * CPS + tile) * 512 + (rr & 31) * 16 + (rr >> 5) * 4), inv, s[a][h]);
+      }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int j = E8 ? kh * 4 + b : kh * 4 + q * 2 + (b >> 1);   // 16-byte chunk of the row
+      uint32_t xb[NT][E8 ? 4 : 2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const uint32_t at = xa + (uint32_t)(n * 8 + g) * x_pitch + (uint32_t)j * 64 + (E8 ? t * 16 : (b & 1) * 32 + t * 8);
+        if constexpr (E8) {
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (n * 8 + g < T) v = lds128a(at);
+          xb[n][0] = v.x, xb[n][1] = v.y, xb[n][2] = v.z, xb[n][3] = v.w;
+        } else {
+          uint2 v = make_uint2(0u, 0u);
+          if (n * 8 + g < T) v = lds64(at);
+          xb[n][0] = v.x, xb[n][1] = v.y;
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < NA; ++a) {
+        const uint32_t base = code + (uint32_t)a * kCodeTile + (uint32_t)r * 128 + (uint32_t)((j ^ g) << 4);
+        float d[NT][4];
+        if constexpr (E8) {
+          const uint32_t w0 = lds32(base + t * 4), w1 = lds32(base + 1024 + t * 4);
+          const uint32_t a0[4] = {code_pair<BF, 0>(w0), code_pair<BF, 0>(w1), code_pair<BF, 1>(w0), code_pair<BF, 1>(w1)};
+          const uint32_t a1[4] = {code_pair<BF, 2>(w0), code_pair<BF, 2>(w1), code_pair<BF, 3>(w0), code_pair<BF, 3>(w1)};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            mma16<BF>(d[n], a0, xb[n][0], xb[n][1], zero);
+            mma16<BF>(d[n], a1, xb[n][2], xb[n][3], d[n]);
+          }
+        } else {
+          const uint32_t o = (b & 1) * 8 + t * 2;
+          const uint32_t w0 = lds16(base + o), w1 = lds16(base + 1024 + o);
+          const uint32_t a0[4] = {code_pair<BF, 0>(w0), code_pair<BF, 0>(w1), code_pair<BF, 1>(w0), code_pair<BF, 1>(w1)};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma16<BF>(d[n], a0, xb[n][0], xb[n][1], zero);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          acc[a][n][0] = fmaf(s[a][0][b], d[n][0], acc[a][n][0]);
+          acc[a][n][1] = fmaf(s[a][0][b], d[n][1], acc[a][n][1]);
+          acc[a][n][2] = fmaf(s[a][1][b], d[n][2], acc[a][n][2]);
+          acc[a][n][3] = fmaf(s[a][1][b], d[n][3], acc[a][n][3]);
+        }
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(kFewWarps * 32) : "memory"); }
+
+// Eight activations of token t from column k (a multiple of 8) in fp32, zeros past the columns.
+__device__ __forceinline__ void few_x8(const FewArgs& g, int format, int t, int k, float (&v)[8]) {
+  if (g.xq.codes) {
+    decode8(g.xq, format, t, g.T, k, g.cols, v);
+  } else {
+    const __nv_bfloat16* p = g.x + (int64_t)t * g.x_ld + k;
+    if (g.x_vec && k + 8 <= g.cols) {
+      const uint4 q = *reinterpret_cast<const uint4*>(p);
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = bf16lo(w[i]);
+        v[2 * i + 1] = bf16hi(w[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = k + i < g.cols ? __bfloat162float(p[i]) : 0.f;
+    }
+  }
+}
+
+template <int FMT, bool GLU, int NT>
+__global__ void __launch_bounds__(kFewThreads, 1)
+    k_micro_few(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, FewArgs g) {
+  constexpr bool E8 = FMT == BITSMOE_MICRO_E8M0;
+  constexpr int NA = GLU ? 2 : 1, CPS = E8 ? 2 : 4;
+  extern __shared__ uint8_t raw[];
+  __shared__ uint32_t top;     // the largest finite |activation| of the CTA's columns (fp32 bits)
+  __shared__ int inexact_any;
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int S = g.stages;
+  constexpr uint32_t redb = 2u * NA * NT * 8 * 512;   // [half][matrix][token][128 rows] fp32, reuses the ring
+  const uint32_t ring = (uint32_t)S * g.stage > redb ? (uint32_t)S * g.stage : redb;
+  float* red = reinterpret_cast<float*>(sm);
+  uint8_t* xs = sm + ring;
+  uint64_t* full = reinterpret_cast<uint64_t*>(xs + (size_t)g.T * g.x_pitch);
+  uint64_t* empty = full + S;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int rank = blockIdx.y, mi = blockIdx.x, m0 = mi * 128;
+  const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
+  if (tid == 0) {
+    for (int i = 0; i < S; ++i) {
+      mbar_init_n(full + i, 1);
+      mbar_init_n(empty + i, kFewWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (tid == 0) top = 0u, inexact_any = 0;
+  __syncthreads();
+  bool ok = true;
+  float acc[NA][NT][4] = {};
+  float inv = 1.f;   // undoes the activations' power of two, in the block scales
+
+  if (wid == kFewWarps) {
+    if (lane == 0) {
+      int i = 0;
+      for (int st = 0, u = 0; i < nk; ++i) {
+        if (u > 0) ok = mbar_wait(empty + st, (uint32_t)(u - 1) & 1u, g.spin);
+        if (!ok) break;
+        const int kb = st0 + i, cnt = min(CPS, g.tiles - kb * CPS);
+        uint8_t* base = sm + (size_t)st * g.stage;
+        const uint32_t bar = smem_u32(full + st);
+        mbar_expect_tx(full + st, NA * (kCodeTile + (uint32_t)cnt * 512u));
+        tma_load_2d(smem_u32(base), &wmap, kb * 128, m0, bar);
+        if (GLU) tma_load_2d(smem_u32(base) + kCodeTile, &umap, kb * 128, m0, bar);
+        const size_t at = ((size_t)mi * g.tiles + (size_t)kb * CPS) * 512;
+        bulk_g2s(base + NA * kCodeTile, g.ws + at, (uint32_t)cnt * 512u, full + st);
+        if (GLU) bulk_g2s(base + NA * kCodeTile + CPS * 512, g.us + at, (uint32_t)cnt * 512u, full + st);
+        if (++st == S) {
+          st = 0;
+          ++u;
+        }
+      }
+      for (int j = max(0, i - S); j < i; ++j) mbar_wait(full + j % S, (uint32_t)(j / S) & 1u);   // copies in flight
+    }
+    __syncwarp();
+  } else {
+    // The activations of this CTA's columns, 8 a thread at a time (a warp within one token).
+    const int k0 = st0 * kStageK, n8 = nk * (kStageK / 8), per = (n8 + 31) / 32;
+    float m = 0.f;
+    for (int w = wid; w < g.T * per; w += kFewWarps) {
+      const int t = w / per, c = (w - t * per) * 32 + lane;
+      if (c >= n8) continue;
+      float v[8];
+      few_x8(g, FMT, t, k0 + c * 8, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (fabsf(v[i]) <= 3.402823466e38f) m = fmaxf(m, fabsf(v[i]));
+    }
+    m = warp_max(m);
+    if (lane == 0 && m > 0.f) atomicMax(&top, __float_as_uint(m));
+    bar_consumers();
+    // 2^14 over the power of two at or below the largest; beyond 2^29 or below 2^-86 (and at 0) they stay as they are
+    const int e = (int)(top >> 23) - 127;
+    const bool norm = e >= -86 && e < 29;
+    const float mul = norm ? __uint_as_float((uint32_t)(14 - e + 127) << 23) : 1.f;
+    inv = norm ? __uint_as_float((uint32_t)(e - 14 + 127) << 23) : 1.f;
+    bool inexact = !norm && top != 0u;
+    for (int w = wid; w < g.T * per; w += kFewWarps) {
+      const int t = w / per, c = (w - t * per) * 32 + lane;
+      if (c >= n8) continue;
+      float v[8];
+      few_x8(g, FMT, t, k0 + c * 8, v);
+      uint32_t h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = v[2 * i] * mul, q = v[2 * i + 1] * mul;
+        const __half2 f = __floats2half2_rn(p, q);
+        const float2 back = __half22float2(f);
+        inexact |= (back.x != p && p == p) || (back.y != q && q == q) || (p == 0.f && v[2 * i] != 0.f) ||
+                   (q == 0.f && v[2 * i + 1] != 0.f);
+        h[i] = *reinterpret_cast<const uint32_t*>(&f);
+      }
+      *reinterpret_cast<uint4*>(xs + (size_t)t * g.x_pitch + (size_t)c * 16) = make_uint4(h[0], h[1], h[2], h[3]);
+    }
+    if (inexact) inexact_any = 1;
+    bar_consumers();
+    const bool bf = inexact_any != 0;
+    if (bf) {
+      inv = 1.f;
+      for (int w = wid; w < g.T * per; w += kFewWarps) {
+        const int t = w / per, c = (w - t * per) * 32 + lane;
+        if (c >= n8) continue;
+        float v[8];
+        few_x8(g, FMT, t, k0 + c * 8, v);
+        uint32_t h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __nv_bfloat162 f = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);   // exact
+          h[i] = *reinterpret_cast<const uint32_t*>(&f);
+        }
+        *reinterpret_cast<uint4*>(xs + (size_t)t * g.x_pitch + (size_t)c * 16) = make_uint4(h[0], h[1], h[2], h[3]);
+      }
+      bar_consumers();
+    }
+    const int rt = wid & 7, kh = wid >> 3;
+    const uint32_t xa = smem_u32(xs);
+    for (int i = 0, st = 0, u = 0; i < nk; ++i) {
+      if (lane == 0) ok = mbar_wait(full + st, (uint32_t)u & 1u, g.spin);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      const uint32_t code = smem_u32(sm) + (uint32_t)st * g.stage, sf = code + NA * kCodeTile;
+      const int left = g.tiles - (st0 + i) * CPS;
+      if (bf) few_half<FMT, NA, NT, true>(code, sf, xa + (uint32_t)i * (kStageK * 2), g.x_pitch, g.T, rt, kh, lane, left, inv, acc);
+      else few_half<FMT, NA, NT, false>(code, sf, xa + (uint32_t)i * (kStageK * 2), g.x_pitch, g.T, rt, kh, lane, left, inv, acc);
+      __syncwarp();
+      if (lane == 0 && !(g.lose && i == 0 && wid == 0 && (blockIdx.x | blockIdx.y) == 0)) mbar_arrive(empty + st);
+      if (++st == S) {
+        st = 0;
+        ++u;
+      }
+    }
+  }
+  __syncthreads();   // every stage has been read: the ring is free
+  if (wid < kFewWarps) {
+    const int rt = wid & 7, kh = wid >> 3, r = 16 * rt + (lane >> 2);
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = n * 8 + (lane & 3) * 2 + (j & 1);
+          red[(size_t)((kh * NA + a) * NT * 8 + c) * 128 + r + (j >> 1) * 8] = acc[a][n][j];
+        }
+  }
+  // the partial sums of the two halves and of the cluster's CTAs, in this order; a CTA sums its share of the rows
+  const auto finish = [&](bool cluster) {
+    const int rs = 128 / g.splits, rbeg = rank * rs;
+    const uint32_t lred = smem_u32(red);
+    for (int e = tid; e < rs * g.T; e += kFewThreads) {
+      const int c = e / rs, r = rbeg + (e - c * rs);
+      float sum[NA];
+#pragma unroll
+      for (int a = 0; a < NA; ++a) {
+        const uint32_t l0 = lred + (uint32_t)((a * NT * 8 + c) * 128 + r) * 4u, l1 = l0 + (uint32_t)(NA * NT * 8) * 512u;
+        if (!cluster) {
+          sum[a] = __uint_as_float(lds32(l0)) + __uint_as_float(lds32(l1));
+        } else {
+          float p[16];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            p[2 * q] = p[2 * q + 1] = 0.f;
+            if (q < g.splits) {
+              uint32_t ra;
+              asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(l0), "r"(q));
+              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p[2 * q]) : "r"(ra) : "memory");
+              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p[2 * q + 1]) : "r"(ra + (l1 - l0)) : "memory");
+            }
+          }
+          sum[a] = 0.f;
+#pragma unroll
+          for (int q = 0; q < 8; ++q) sum[a] += p[2 * q] + p[2 * q + 1];
+        }
+      }
+      if (m0 + r >= g.rows) continue;
+      float o = sum[0] * g.sw;
+      if (GLU) o = silu_mul(o, sum[NA - 1] * g.su);
+      store_y(g.y, g.y_type, (int64_t)c * g.y_ld + m0 + r, o);
+    }
+    __syncwarp();
+  };
+  if (g.splits > 1) {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    finish(true);
+    // no CTA leaves while others may still read its shared memory
+    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+  } else {
+    __syncthreads();
+    finish(false);
+  }
+  if (!ok && g.status) atomicCAS(g.status, 0, BITSMOE_ERR_TIMEOUT);
+}
+
+struct FewPlan {
+  int splits, sps, stages;
+  uint32_t stage, x_pitch;
+  size_t smem;
+};
+
+// How T tokens run on the kernel for few of them, or false when their activations do not fit shared memory.
+bool few_plan(int format, bool glu, int T, int rows, int cols, int sms, FewPlan* p) {
+  if (T > kFewTokens) return false;
+  const int NA = glu ? 2 : 1, CPS = format == BITSMOE_MICRO_E8M0 ? 2 : 4;
+  const int nst = (cols + kStageK - 1) / kStageK;
+  const int64_t mt = (rows + 127) / 128;
+  int splits = 1;
+  while (splits < 8 && mt * splits * 2 <= sms && nst >= 2 * splits) splits *= 2;
+  p->stage = (uint32_t)NA * (kCodeTile + (uint32_t)CPS * 512);
+  const size_t red = (size_t)2 * NA * (T > 8 ? 16 : 8) * 512;
+  for (;; splits *= 2) {   // more CTAs per row tile where the activations take too much of the shared memory
+    if (splits > 8) return false;
+    p->sps = (nst + splits - 1) / splits;
+    // 64 (32) bytes beyond a multiple of 128: the 8 tokens of a fragment's 16-byte (8-byte) loads in different banks
+    p->x_pitch = (uint32_t)p->sps * kStageK * 2 + (format == BITSMOE_MICRO_E8M0 ? 64 : 32);
+    const size_t xb = (size_t)T * p->x_pitch;
+    const size_t room = 225 * 1024 - 1024 - 512;
+    if (xb + 3 * (size_t)p->stage > room || xb + red > room) continue;
+    p->stages = (int)std::min<size_t>({(size_t)p->sps, (room - xb) / p->stage, (size_t)16});
+    const size_t ring = std::max((size_t)p->stages * p->stage, red);
+    p->smem = 1024 + ring + xb + (size_t)2 * p->stages * 8;
+    p->splits = splits;
+    return true;
+  }
+}
+
+template <int FMT, bool GLU, int NT>
+cudaError_t launch_few(const FewPlan& p, const bitsmoe_microscale* w, const bitsmoe_microscale* up, FewArgs g, cudaStream_t st) {
+  g.nst = (g.cols + kStageK - 1) / kStageK;
+  g.splits = p.splits;
+  g.sps = p.sps;
+  g.stages = p.stages;
+  g.stage = p.stage;
+  g.x_pitch = p.x_pitch;
+  CUtensorMap wm, um;
+  const int64_t pitch = micro_pitch(g.cols);
+  if (!make_row_map(&wm, true, w->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
+  um = wm;
+  if (GLU && !make_row_map(&um, true, up->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
+  auto kern = k_micro_few<FMT, GLU, NT>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1;
+  attr[0].val.clusterDim.y = (unsigned)p.splits;
+  attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((g.rows + 127) / 128), (unsigned)p.splits, 1);
+  cfg.blockDim = dim3(kFewThreads);
+  cfg.dynamicSmemBytes = p.smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.splits > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, wm, um, g);
+}
+
+template <int FMT, bool GLU>
+cudaError_t launch_few_nt(const FewPlan& p, const bitsmoe_microscale* w, const bitsmoe_microscale* up, const FewArgs& g, cudaStream_t st) {
+  return g.T > 8 ? launch_few<FMT, GLU, 2>(p, w, up, g, st) : launch_few<FMT, GLU, 1>(p, w, up, g, st);
+}
+
+// ---------------------------------------------------------------------------
+// Coded activations: both operands go to the tensor core as they are stored.
+// ---------------------------------------------------------------------------
+constexpr int kCodedThreads = 192;            // warp 0: copies, warp 1: MMA, warps 2-5: epilogue
+
+struct CodedArgs {
+  int T, rows, cols;
+  int N;             // tokens of a tile: the MMA's N
+  int mt;            // 128-row tiles
+  int nst, sps;      // stages of the whole product, of a split
+  int splits;        // CTAs of a cluster, one per range of stages
+  int stages;        // ring depth
+  uint32_t stage;    // bytes of a stage
+  int tiles;         // 512-byte scale tiles across a row
+  const uint8_t* ws;
+  const uint8_t* us;
+  const uint8_t* xs;
+  float sw, su;
+  void* y;
+  int y_type;
+  int64_t y_ld;
+  long long spin;    // bound of the waits, in SM clocks
+  int lose;          // testing hook: the first CTA's ring never reports its first slot free
+  int* status;
+};
+
+// 128 weight rows x N tokens a CTA (with GLU 128 rows of both matrices).  Codes come by TMA, 256 columns a
+// stage, scale tiles by bulk copies; the MMA thread moves a stage's scales into tensor memory (columns of the
+// stage's own, so that the ring's barriers order their reuse) and issues the block-scaled products.  With few
+// tiles the columns are split over a cluster, whose CTAs add their partial tiles through distributed shared
+// memory in rank order.
+template <int FMT, bool GLU>
+__global__ void __launch_bounds__(kCodedThreads, 1)
+    k_micro_coded(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap,
+                  const __grid_constant__ CUtensorMap xmap, CodedArgs g) {
+  constexpr bool E8 = FMT == BITSMOE_MICRO_E8M0;
+  constexpr int NA = GLU ? 2 : 1;
+  constexpr int CPS = E8 ? 2 : 4;   // scale tiles of a stage's 256 columns
+  extern __shared__ uint8_t raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int S = g.stages, N = g.N, G = (N + 127) / 128;
+  const uint32_t ring = (uint32_t)S * g.stage, redb = g.splits > 1 ? (uint32_t)(NA * N) * 512u : 0u;
+  float* red = reinterpret_cast<float*>(sm);   // [NA][N][128], reuses the ring once the MMAs are done
+  uint64_t* full = reinterpret_cast<uint64_t*>(sm + (ring > redb ? ring : redb));
+  uint64_t* empty = full + S;
+  uint64_t* done = empty + S;
+  uint32_t* slot = reinterpret_cast<uint32_t*>(done + 1);
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int rank = blockIdx.y;
+  const int tile = blockIdx.x, mi = tile % g.mt, m0 = mi * 128, t0 = tile / g.mt * N;
+  const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
+  const int nbg = min(G, (g.T + 127) / 128 - t0 / 128);
+  const uint32_t b_bytes = (uint32_t)N * 128, sf_off = NA * kCodeTile + b_bytes;
+  const uint32_t sfa_cols = NA * CPS * 4, sf_cols = sfa_cols + (uint32_t)G * CPS * 4;
+
+  if (tid == 0) {
+    for (int i = 0; i < S; ++i) {
+      mbar_init_n(full + i, 1);
+      mbar_init_n(empty + i, 1);
+    }
+    mbar_init_n(done, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (wid == 1) tmem_alloc(slot, 512);
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = *slot;
+  bool ok = true;
+
+  if (wid == 0) {
+    if (lane == 0) {
+      int i = 0;
+      for (int st = 0, u = 0; i < nk; ++i) {
+        if (u > 0) ok = mbar_wait(empty + st, (uint32_t)(u - 1) & 1u, g.spin);
+        if (!ok) break;
+        const int kb = st0 + i, cnt = min(CPS, g.tiles - kb * CPS);
+        uint8_t* base = sm + (size_t)st * g.stage;
+        const uint32_t bar = smem_u32(full + st);
+        mbar_expect_tx(full + st, NA * kCodeTile + b_bytes + (uint32_t)(cnt * (NA + nbg)) * 512u);
+        tma_load_2d(smem_u32(base), &wmap, kb * 128, m0, bar);
+        if (GLU) tma_load_2d(smem_u32(base) + kCodeTile, &umap, kb * 128, m0, bar);
+        tma_load_2d(smem_u32(base) + NA * kCodeTile, &xmap, kb * 128, t0, bar);
+        uint8_t* sf = base + sf_off;
+        const size_t at = ((size_t)mi * g.tiles + (size_t)kb * CPS) * 512;
+        bulk_g2s(sf, g.ws + at, (uint32_t)cnt * 512u, full + st);
+        if (GLU) bulk_g2s(sf + CPS * 512, g.us + at, (uint32_t)cnt * 512u, full + st);
+        for (int j = 0; j < nbg; ++j)
+          bulk_g2s(sf + (NA + j) * CPS * 512, g.xs + ((size_t)(t0 / 128 + j) * g.tiles + (size_t)kb * CPS) * 512,
+                   (uint32_t)cnt * 512u, full + st);
+        if (++st == S) {
+          st = 0;
+          ++u;
+        }
+      }
+      for (int j = max(0, i - S); j < i; ++j) mbar_wait(full + j % S, (uint32_t)(j / S) & 1u);   // copies in flight
+    }
+    __syncwarp();
+  } else if (wid == 1) {
+    if (lane == 0) {
+      const int nk64 = (g.cols + 63) / 64;
+      const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(sm) + NA * kCodeTile);
+      const uint32_t sstep = g.stage >> 4;
+      for (int i = 0, st = 0, u = 0; i < nk; ++i) {
+        ok = mbar_wait(full + st, (uint32_t)u & 1u, g.spin);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const int kb = st0 + i, cnt = min(CPS, g.tiles - kb * CPS);
+        const uint32_t sf = smem_u32(sm) + (uint32_t)st * g.stage + sf_off;
+        const uint32_t ta = tmem + (uint32_t)(NA * N) + (uint32_t)st * sf_cols, tb = ta + sfa_cols;
+        for (int q = 0; q < cnt; ++q) {
+#pragma unroll
+          for (int a = 0; a < NA; ++a) tmem_copy_scales(ta + (uint32_t)(a * CPS + q) * 4, sf + (uint32_t)(a * CPS + q) * 512);
+          for (int j = 0; j < nbg; ++j)
+            tmem_copy_scales(tb + (uint32_t)(q * G + j) * 4, sf + (uint32_t)((NA + j) * CPS + q) * 512);
+        }
+        const uint64_t a0 = da + (uint64_t)st * sstep, b0 = db + (uint64_t)st * sstep;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (kb * 4 + k >= nk64) break;
+          const int q = E8 ? k >> 1 : k;
+          const uint32_t id = idesc_e2m1(N, E8, E8 ? (uint32_t)(k & 1) * 2u : 0u);
+#pragma unroll
+          for (int a = 0; a < NA; ++a)
+            mma_e2m1<E8>(tmem + (uint32_t)(a * N), a0 + a * (kCodeTile >> 4) + 2 * k, b0 + 2 * k, id,
+                         ta + (uint32_t)(a * CPS + q) * 4, tb + (uint32_t)(q * G) * 4, (i | k) != 0);
+        }
+        if (!(g.lose && i == 0 && (blockIdx.x | blockIdx.y) == 0)) mma_commit(empty + st);
+        if (++st == S) {
+          st = 0;
+          ++u;
+        }
+      }
+      mma_commit(done);
+    }
+    __syncwarp();
+  } else {
+    if (lane == 0) ok = mbar_wait(done, 0, g.spin);
+    __syncwarp();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const int r = 32 * (wid & 3) + lane;
+    const uint32_t tl = tmem + ((uint32_t)(32 * (wid & 3)) << 16);
+    for (int c0 = 0; c0 < N; c0 += 16) {
+      uint32_t v[NA][16];
+#pragma unroll
+      for (int a = 0; a < NA; ++a) {
+        if (nk > 0) {
+          tmem_ld16(tl + (uint32_t)(a * N + c0), v[a]);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 16; ++q) v[a][q] = 0u;
+        }
+      }
+      if (g.splits > 1) {
+#pragma unroll
+        for (int a = 0; a < NA; ++a)
+#pragma unroll
+          for (int q = 0; q < 16; ++q) red[(size_t)(a * N + c0 + q) * 128 + r] = __uint_as_float(v[a][q]);
+      } else if (m0 + r < g.rows) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const int t = t0 + c0 + q;
+          if (t >= g.T) break;
+          float o = __uint_as_float(v[0][q]) * g.sw;
+          if (GLU) o = silu_mul(o, __uint_as_float(v[NA - 1][q]) * g.su);
+          store_y(g.y, g.y_type, (int64_t)t * g.y_ld + m0 + r, o);
+        }
+      }
+    }
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  if (g.splits > 1) {
+    // every CTA of the cluster has its partial tile in shared memory; this CTA's share of the rows is summed
+    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    const int rs = 128 / g.splits, rbeg = rank * rs;
+    const uint32_t lred = smem_u32(red);
+    for (int e = tid; e < rs * N; e += kCodedThreads) {
+      const int c = e / rs, r = rbeg + (e - c * rs);
+      float p[NA][8];
+#pragma unroll
+      for (int a = 0; a < NA; ++a)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          p[a][q] = 0.f;
+          if (q < g.splits) {
+            uint32_t ra;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(lred + (uint32_t)((a * N + c) * 128 + r) * 4u), "r"(q));
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p[a][q]) : "r"(ra) : "memory");
+          }
+        }
+      float sum[NA];
+#pragma unroll
+      for (int a = 0; a < NA; ++a)
+        sum[a] = ((p[a][0] + p[a][1]) + (p[a][2] + p[a][3])) + ((p[a][4] + p[a][5]) + (p[a][6] + p[a][7]));
+      const int t = t0 + c;
+      if (m0 + r >= g.rows || t >= g.T) continue;
+      float o = sum[0] * g.sw;
+      if (GLU) o = silu_mul(o, sum[NA - 1] * g.su);
+      store_y(g.y, g.y_type, (int64_t)t * g.y_ld + m0 + r, o);
+    }
+    // no CTA leaves while others may still read its shared memory
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+  } else {
+    __syncthreads();
+  }
+  if (!ok && g.status) atomicCAS(g.status, 0, BITSMOE_ERR_TIMEOUT);
+  if (wid == 1) {
+    __syncwarp();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int FMT, bool GLU>
+cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const bitsmoe_microscale* xq, CodedArgs g,
+                         int sms, cudaStream_t st) {
+  constexpr int NA = GLU ? 2 : 1, CPS = FMT == BITSMOE_MICRO_E8M0 ? 2 : 4;
+  g.N = std::min((g.T + 15) / 16 * 16, 256 / NA);
+  const int G = (g.N + 127) / 128, tt = (g.T + g.N - 1) / g.N;
+  g.mt = (g.rows + 127) / 128;
+  g.nst = (g.cols + kStageK - 1) / kStageK;
+  int splits = 1;
+  while (splits < 8 && (int64_t)g.mt * tt * splits * 2 <= sms && g.nst >= 2 * splits) splits *= 2;
+  g.splits = splits;
+  g.sps = (g.nst + splits - 1) / splits;
+  g.stage = (NA * kCodeTile + (uint32_t)g.N * 128 + (uint32_t)((NA + G) * CPS) * 512 + 1023) / 1024 * 1024;
+  const int sf_cols = (NA + G) * CPS * 4;
+  g.stages = std::min({g.sps, (int)(216 * 1024 / g.stage), (512 - NA * g.N) / sf_cols});
+  const size_t ring = (size_t)g.stages * g.stage, redb = splits > 1 ? (size_t)NA * g.N * 512 : 0;
+  const size_t smem = 1024 + std::max(ring, redb) + (size_t)(2 * g.stages + 1) * 8 + 16;
+  CUtensorMap wm, um, xm;
+  if (!make_row_map(&wm, true, w->codes, g.rows, micro_pitch(g.cols), micro_pitch(g.cols), 128) ||
+      !make_row_map(&xm, true, xq->codes, g.T, micro_pitch(g.cols), micro_pitch(g.cols), g.N))
+    return cudaErrorInvalidValue;
+  um = wm;
+  if (GLU && !make_row_map(&um, true, up->codes, g.rows, micro_pitch(g.cols), micro_pitch(g.cols), 128))
+    return cudaErrorInvalidValue;
+  auto kern = k_micro_coded<FMT, GLU>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1;
+  attr[0].val.clusterDim.y = (unsigned)splits;
+  attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(g.mt * tt), (unsigned)splits, 1);
+  cfg.blockDim = dim3(kCodedThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = splits > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, wm, um, xm, g);
+}
+
 MicroMat mat_of(const bitsmoe_microscale* m) {
   if (!m) return MicroMat{nullptr, nullptr, 0, 0};
   return MicroMat{m->codes, m->scales, micro_pitch(m->cols), micro_tiles(m->format, m->cols)};
@@ -130,7 +862,65 @@ extern "C" int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bit
   if (T == 0 || w->rows == 0) return BITSMOE_OK;
   if ((!x && !xq) || !y) return BITSMOE_ERR_INVALID_ARG;
   if ((uintptr_t)x % 2 || (uintptr_t)y % dense_size(y_type) || (uintptr_t)status % 4) return BITSMOE_ERR_ALIGNMENT;
+  if ((int64_t)((w->rows + 127) / 128) * ((T + 127) / 128) >= (1ll << 31)) return BITSMOE_ERR_SHAPE;
   const float sx = xq ? xq->scale : 1.f;
+  const long long spin = debug_wait_clocks() > 0 ? debug_wait_clocks() : kWaitClocks;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return record_cuda_error((int)e);
+  const bool e8 = w->format == BITSMOE_MICRO_E8M0;
+  FewPlan fp;
+  if (few_plan(w->format, up != nullptr, T, w->rows, w->cols, sms, &fp)) {
+    FewArgs f;
+    std::memset(&f, 0, sizeof(f));
+    f.T = T;
+    f.rows = w->rows;
+    f.cols = w->cols;
+    f.tiles = micro_tiles(w->format, w->cols);
+    f.ws = w->scales;
+    f.us = up ? up->scales : nullptr;
+    f.x = static_cast<const __nv_bfloat16*>(x);
+    f.x_ld = x_ld;
+    f.x_vec = (uintptr_t)x % 16 == 0 && x_ld % 8 == 0;
+    f.xq = mat_of(xq);
+    f.sw = w->scale * sx;
+    f.su = up ? up->scale * sx : 0.f;
+    f.y = y;
+    f.y_type = y_type;
+    f.y_ld = y_ld;
+    f.spin = spin;
+    f.lose = debug_skip_arrival();
+    f.status = status;
+    if (e8) e = up ? launch_few_nt<BITSMOE_MICRO_E8M0, true>(fp, w, up, f, st) : launch_few_nt<BITSMOE_MICRO_E8M0, false>(fp, w, up, f, st);
+    else e = up ? launch_few_nt<BITSMOE_MICRO_E4M3, true>(fp, w, up, f, st) : launch_few_nt<BITSMOE_MICRO_E4M3, false>(fp, w, up, f, st);
+    return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
+  }
+  if (xq) {
+    CodedArgs c;
+    std::memset(&c, 0, sizeof(c));
+    c.T = T;
+    c.rows = w->rows;
+    c.cols = w->cols;
+    c.tiles = micro_tiles(w->format, w->cols);
+    c.ws = w->scales;
+    c.us = up ? up->scales : nullptr;
+    c.xs = xq->scales;
+    c.sw = w->scale * sx;
+    c.su = up ? up->scale * sx : 0.f;
+    c.y = y;
+    c.y_type = y_type;
+    c.y_ld = y_ld;
+    c.spin = spin;
+    c.lose = debug_skip_arrival();
+    c.status = status;
+    if (e8)
+      e = up ? launch_coded<BITSMOE_MICRO_E8M0, true>(w, up, xq, c, sms, st) : launch_coded<BITSMOE_MICRO_E8M0, false>(w, up, xq, c, sms, st);
+    else
+      e = up ? launch_coded<BITSMOE_MICRO_E4M3, true>(w, up, xq, c, sms, st) : launch_coded<BITSMOE_MICRO_E4M3, false>(w, up, xq, c, sms, st);
+    return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
+  }
   ProductArgs a{mat_of(w), mat_of(up), mat_of(xq), static_cast<const __nv_bfloat16*>(x), x_ld, T, w->rows, w->cols,
                 w->format, w->scale * sx, up ? up->scale * sx : 0.f, y, y_type, y_ld};
   const dim3 g((unsigned)((w->rows + kTR - 1) / kTR), (unsigned)((T + kTT - 1) / kTT < 65535 ? (T + kTT - 1) / kTT : 65535));
