@@ -15,9 +15,6 @@
 namespace {
 using namespace bmoe;
 
-constexpr int kTR = 64, kTT = 64, kTK = 32;   // rows, tokens and columns of a tile
-constexpr int kPThreads = 256;
-
 struct MicroMat {
   const uint8_t* codes;
   const uint8_t* scales;
@@ -25,18 +22,7 @@ struct MicroMat {
   int tiles;
 };
 
-struct ProductArgs {
-  MicroMat w, u, xq;   // u.codes null: plain; xq.codes null: x is bf16
-  const __nv_bfloat16* x;
-  int64_t x_ld;
-  int T, rows, cols, format;
-  float sw, su;        // tensor scales (the coded activations' multiplied in)
-  void* y;
-  int y_type;
-  int64_t y_ld;
-};
-
-// 32 columns of a row from column k (a multiple of 32), a quarter of them per call: 8 values.
+// The 8 values of a coded row from column k (a multiple of 8) without the tensor scale; zeros past the matrix.
 __device__ __forceinline__ void decode8(const MicroMat& m, int format, int r, int rows, int k, int cols, float* dst) {
   if (r < rows && k < cols) {
     const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(m.codes + (int64_t)r * m.pitch + k / 2));
@@ -46,62 +32,6 @@ __device__ __forceinline__ void decode8(const MicroMat& m, int format, int r, in
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) dst[i] = 0.f;
-  }
-}
-
-__global__ void __launch_bounds__(kPThreads) k_micro_product(ProductArgs a) {
-  __shared__ float ws[2][kTR][kTK + 1], xs[kTT][kTK + 1];
-  const int r0 = blockIdx.x * kTR;
-  const bool glu = a.u.codes != nullptr;
-  const int tr = threadIdx.x & 15, tt = threadIdx.x >> 4;
-  const int lr = threadIdx.x >> 2, lk = (threadIdx.x & 3) * 8;
-  for (int t0 = blockIdx.y * kTT; t0 < a.T; t0 += gridDim.y * kTT) {
-    float acc[2][4][4] = {};
-    for (int k0 = 0; k0 < a.cols; k0 += kTK) {
-      __syncthreads();
-      decode8(a.w, a.format, r0 + lr, a.rows, k0 + lk, a.cols, &ws[0][lr][lk]);
-      if (glu) decode8(a.u, a.format, r0 + lr, a.rows, k0 + lk, a.cols, &ws[1][lr][lk]);
-      if (a.xq.codes) {
-        decode8(a.xq, a.format, t0 + lr, a.T, k0 + lk, a.cols, &xs[lr][lk]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int t = t0 + lr, k = k0 + lk + i;
-          xs[lr][lk + i] = t < a.T && k < a.cols ? __bfloat162float(a.x[(int64_t)t * a.x_ld + k]) : 0.f;
-        }
-      }
-      __syncthreads();
-      for (int k = 0; k < kTK; ++k) {
-        float xv[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) xv[j] = xs[tt * 4 + j][k];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float wv = ws[0][tr + 16 * i][k];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[0][i][j] = fmaf(wv, xv[j], acc[0][i][j]);
-        }
-        if (glu) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float uv = ws[1][tr + 16 * i][k];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[1][i][j] = fmaf(uv, xv[j], acc[1][i][j]);
-          }
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int r = r0 + tr + 16 * i, t = t0 + tt * 4 + j;
-        if (r >= a.rows || t >= a.T) continue;
-        float v = acc[0][i][j] * a.sw;
-        if (glu) v = v / (1.f + expf(-v)) * (acc[1][i][j] * a.su);
-        if (a.y_type == BITSMOE_F32) static_cast<float*>(a.y)[(int64_t)t * a.y_ld + r] = v;
-        else static_cast<__nv_bfloat16*>(a.y)[(int64_t)t * a.y_ld + r] = __float2bfloat16_rn(v);
-      }
   }
 }
 
@@ -574,6 +504,39 @@ cudaError_t launch_few_nt(const FewPlan& p, const bitsmoe_microscale* w, const b
   return g.T > 8 ? launch_few<FMT, GLU, 2>(p, w, up, g, st) : launch_few<FMT, GLU, 1>(p, w, up, g, st);
 }
 
+// A CTA's share of the rows of a tile split over a cluster: the partial tiles red [NA][N][128] of the
+// cluster's CTAs added in rank order (all of an element's requested before the first is used), scaled, stored.
+template <int NA, int THREADS>
+__device__ __forceinline__ void sum_splits(const float* red, int N, int splits, int rank, int m0, int rows, int t0, int T,
+                                           float sw, float su, void* y, int y_type, int64_t y_ld) {
+  const int rs = 128 / splits, rbeg = rank * rs;
+  const uint32_t lred = smem_u32(red);
+  for (int e = threadIdx.x; e < rs * N; e += THREADS) {
+    const int c = e / rs, r = rbeg + (e - c * rs);
+    float p[NA][8];
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        p[a][q] = 0.f;
+        if (q < splits) {
+          uint32_t ra;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(lred + (uint32_t)((a * N + c) * 128 + r) * 4u), "r"(q));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p[a][q]) : "r"(ra) : "memory");
+        }
+      }
+    float sum[NA];
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+      sum[a] = ((p[a][0] + p[a][1]) + (p[a][2] + p[a][3])) + ((p[a][4] + p[a][5]) + (p[a][6] + p[a][7]));
+    const int t = t0 + c;
+    if (m0 + r >= rows || t >= T) continue;
+    float o = sum[0] * sw;
+    if (NA == 2) o = silu_mul(o, sum[NA - 1] * su);
+    store_y(y, y_type, (int64_t)t * y_ld + m0 + r, o);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Coded activations: both operands go to the tensor core as they are stored.
 // ---------------------------------------------------------------------------
@@ -750,32 +713,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
     // every CTA of the cluster has its partial tile in shared memory; this CTA's share of the rows is summed
     asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-    const int rs = 128 / g.splits, rbeg = rank * rs;
-    const uint32_t lred = smem_u32(red);
-    for (int e = tid; e < rs * N; e += kCodedThreads) {
-      const int c = e / rs, r = rbeg + (e - c * rs);
-      float p[NA][8];
-#pragma unroll
-      for (int a = 0; a < NA; ++a)
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          p[a][q] = 0.f;
-          if (q < g.splits) {
-            uint32_t ra;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(lred + (uint32_t)((a * N + c) * 128 + r) * 4u), "r"(q));
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p[a][q]) : "r"(ra) : "memory");
-          }
-        }
-      float sum[NA];
-#pragma unroll
-      for (int a = 0; a < NA; ++a)
-        sum[a] = ((p[a][0] + p[a][1]) + (p[a][2] + p[a][3])) + ((p[a][4] + p[a][5]) + (p[a][6] + p[a][7]));
-      const int t = t0 + c;
-      if (m0 + r >= g.rows || t >= g.T) continue;
-      float o = sum[0] * g.sw;
-      if (GLU) o = silu_mul(o, sum[NA - 1] * g.su);
-      store_y(g.y, g.y_type, (int64_t)t * g.y_ld + m0 + r, o);
-    }
+    sum_splits<NA, kCodedThreads>(red, N, g.splits, rank, m0, g.rows, t0, g.T, g.sw, g.su, g.y, g.y_type, g.y_ld);
     // no CTA leaves while others may still read its shared memory
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
@@ -826,6 +764,383 @@ cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* 
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(g.mt * tt), (unsigned)splits, 1);
   cfg.blockDim = dim3(kCodedThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = splits > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, wm, um, xm, g);
+}
+
+// ---------------------------------------------------------------------------
+// Many 16-bit activations: the codes become bf16 tiles in shared memory.
+//
+// A CTA takes 128 weight rows (with GLU of both matrices) x N tokens at a time.
+// Warp 0 brings codes and scale tiles (256 columns a stage) into one ring; eight
+// warps turn them into bf16 tiles of 64 columns, code times block scale (exact:
+// at most 6 significant bits), in a second ring, where warp 2 brings the
+// activations by TMA; warp 1 issues tcgen05.mma (kind::f16) and four warps
+// empty the accumulators, two of them in turn where tensor memory holds two, so
+// that the next tile's products run meanwhile.  CTAs stay for all their tiles.
+// With few tiles the columns are split over a cluster instead.
+// ---------------------------------------------------------------------------
+constexpr int kWideThreads = 512;   // warps: 0 codes, 1 MMA, 2 activations, 4-11 decode, 12-15 epilogue
+constexpr int kDecodeWarps = 8;
+
+struct WideArgs {
+  int T, rows, cols, tiles;
+  int N, mt, ntiles, nbuf;
+  int nst, sps, splits;
+  int P, Q;              // depths of the two rings
+  uint32_t pst, qst;     // bytes of their stages
+  int btma;              // x's rows are on 16-byte boundaries
+  const uint8_t* ws;
+  const uint8_t* us;
+  const __nv_bfloat16* x;
+  int64_t x_ld;
+  float sw, su;
+  void* y;
+  int y_type;
+  int64_t y_ld;
+  long long spin;
+  int lose;
+  int* status;
+};
+
+// 32 codes (four words) of one row times their block scales -> 64 bytes of bf16 in a 128-byte swizzled tile.
+// A code's sign and other three bits, moved to a bf16's sign and lowest exponent and highest mantissa bits, are
+// its value times 2^-126; the factor brings the scale and 2^126 back: E8M0 whole, E4M3 2^119 (448 2^119 is the
+// largest that fits; the result's 2^-7 goes into the tensor scale).
+template <int FMT>
+__device__ __forceinline__ void decode32(const uint4& v, uint32_t sc, uint8_t* row, int half, int r7) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t f[2];
+  bool twice = false;
+  uint32_t f2 = 0;
+  if constexpr (FMT == BITSMOE_MICRO_E8M0) {
+    const uint32_t c = sc & 255u;
+    twice = c > 128u;   // 2^(c - 127) 2^126 is above bf16's largest: in two steps
+    uint32_t b = (min(c, 128u) + 126u) << 7;
+    f[0] = f[1] = b | (b << 16);
+    b = c == 255u ? 0x7FC0u : (c - 1u) << 7;   // 2^(c - 128)
+    f2 = b | (b << 16);
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float s = micro_e4m3((sc >> (8 * h)) & 255u) * 6.646139978924579e35f;   // 2^119
+      const uint32_t b = __float_as_uint(s) >> 16;
+      f[h] = b | (b << 16);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t w4 = w[q] << 4;
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t t = __byte_perm(w4, w[q], ((4u + i) << 12) | ((uint32_t)i << 4));   // codes 2i, 2i + 1 at bits 15..12, 31..28
+      o[i] = ((t >> 6) & 0x01C001C0u) | (t & 0x80008000u);
+      asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(o[i]) : "r"(f[q >> 1]));
+    }
+    if (FMT == BITSMOE_MICRO_E8M0 && twice) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(o[i]) : "r"(f2));
+    }
+    *reinterpret_cast<uint4*>(row + (((half * 4 + q) ^ r7) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+}
+
+template <int FMT, bool GLU>
+__global__ void __launch_bounds__(kWideThreads, 1)
+    k_micro_wide(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap,
+                 const __grid_constant__ CUtensorMap xmap, WideArgs g) {
+  constexpr bool E8 = FMT == BITSMOE_MICRO_E8M0;
+  constexpr int NA = GLU ? 2 : 1, CPS = E8 ? 2 : 4;
+  extern __shared__ uint8_t raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int P = g.P, Q = g.Q, N = g.N;
+  uint8_t* pring = sm + (size_t)Q * g.qst;
+  float* red = reinterpret_cast<float*>(sm);   // split: [NA][N][128], reuses the rings
+  uint64_t* pfull = reinterpret_cast<uint64_t*>(pring + (size_t)P * g.pst);
+  uint64_t* pempty = pfull + P;
+  uint64_t* qfull = pempty + P;
+  uint64_t* qempty = qfull + Q;
+  uint64_t* afull = qempty + Q;
+  uint64_t* aempty = afull + 2;
+  uint32_t* slot = reinterpret_cast<uint32_t*>(aempty + 2);
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int rank = blockIdx.y;
+  const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
+  const int nks = (g.cols + 63) / 64;   // slots of 64 columns in all
+  const int s0 = st0 * 4, ns = max(0, min(nk * 4, nks - s0));   // this CTA's
+  const uint32_t b_bytes = (uint32_t)N * 128;
+
+  if (tid == 0) {
+    for (int i = 0; i < P; ++i) {
+      mbar_init_n(pfull + i, 1);
+      mbar_init_n(pempty + i, kDecodeWarps);
+    }
+    for (int i = 0; i < Q; ++i) {
+      mbar_init_n(qfull + i, kDecodeWarps + (g.btma ? 1 : 0));
+      mbar_init_n(qempty + i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init_n(afull + i, 1);
+      mbar_init_n(aempty + i, 4);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (wid == 1) tmem_alloc(slot, 512);
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = *slot;
+  bool ok = true;
+
+  if (wid == 0) {
+    if (lane == 0) {
+      int st = 0, u = 0, n = 0;
+      for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x) {
+        const int mi = tile % g.mt;
+        for (int i = 0; i < nk; ++i, ++n) {
+          if (u > 0) ok = mbar_wait(pempty + st, (uint32_t)(u - 1) & 1u, g.spin);
+          if (!ok) break;
+          const int kb = st0 + i, cnt = min(CPS, g.tiles - kb * CPS);
+          uint8_t* base = pring + (size_t)st * g.pst;
+          const uint32_t bar = smem_u32(pfull + st);
+          mbar_expect_tx(pfull + st, NA * (kCodeTile + (uint32_t)cnt * 512u));
+          tma_load_2d(smem_u32(base), &wmap, kb * 128, mi * 128, bar);
+          if (GLU) tma_load_2d(smem_u32(base) + kCodeTile, &umap, kb * 128, mi * 128, bar);
+          const size_t at = ((size_t)mi * g.tiles + (size_t)kb * CPS) * 512;
+          bulk_g2s(base + NA * kCodeTile, g.ws + at, (uint32_t)cnt * 512u, pfull + st);
+          if (GLU) bulk_g2s(base + NA * kCodeTile + CPS * 512, g.us + at, (uint32_t)cnt * 512u, pfull + st);
+          if (++st == P) {
+            st = 0;
+            ++u;
+          }
+        }
+      }
+      for (int j = max(0, n - P); j < n; ++j) mbar_wait(pfull + j % P, (uint32_t)(j / P) & 1u);   // copies in flight
+    }
+    __syncwarp();
+  } else if (wid == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = idesc_bf16(N);
+      const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(sm) + NA * kCodeTile);
+      const uint32_t sstep = g.qst >> 4;
+      int st = 0, u = 0, it = 0;
+      for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x, ++it) {
+        const int buf = it % g.nbuf, use = it / g.nbuf;
+        if (use > 0) ok = mbar_wait(aempty + buf, (uint32_t)(use - 1) & 1u, g.spin);
+        if (!ok) break;
+        const uint32_t acc = tmem + (uint32_t)(buf * NA * N);
+        for (int i = 0; i < ns; ++i) {
+          ok = mbar_wait(qfull + st, (uint32_t)u & 1u, g.spin);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint64_t a0 = da + (uint64_t)st * sstep, b0 = db + (uint64_t)st * sstep;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int a = 0; a < NA; ++a)
+              mma_f16(acc + (uint32_t)(a * N), a0 + a * (kCodeTile >> 4) + 2 * k, b0 + 2 * k, idesc, (i | k) != 0);
+          if (!(g.lose && i == 0 && it == 0 && (blockIdx.x | blockIdx.y) == 0)) mma_commit(qempty + st);
+          if (++st == Q) {
+            st = 0;
+            ++u;
+          }
+        }
+        mma_commit(afull + buf);
+      }
+    }
+    __syncwarp();
+  } else if (wid == 2) {
+    if (lane == 0 && g.btma) {
+      int st = 0, u = 0, n = 0;
+      for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x) {
+        const int t0 = tile / g.mt * N;
+        for (int i = 0; i < ns; ++i, ++n) {
+          if (u > 0) ok = mbar_wait(qempty + st, (uint32_t)(u - 1) & 1u, g.spin);
+          if (!ok) break;
+          mbar_expect_tx(qfull + st, b_bytes);
+          tma_load_2d(smem_u32(sm + (size_t)st * g.qst) + NA * kCodeTile, &xmap, (s0 + i) * 64, t0, smem_u32(qfull + st));
+          if (++st == Q) {
+            st = 0;
+            ++u;
+          }
+        }
+      }
+      // copies in flight: their bytes end a phase only with the decoders' arrivals, which may be missing after a timeout
+      for (int j = max(0, n - Q); j < n; ++j) mbar_wait(qfull + j % Q, (uint32_t)(j / Q) & 1u, ok ? kWaitClocks : g.spin);
+    }
+    __syncwarp();
+  } else if (wid >= 4 && wid < 4 + kDecodeWarps) {
+    const int dw = wid - 4, r = 16 * dw + (lane & 15), half = lane >> 4, r7 = r & 7;
+    const int bt = tid - 128;
+    int ps = 0, pu = 0, qs = 0, qu = 0;
+    for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x) {
+      const int t0 = tile / g.mt * N;
+      for (int i = 0; i < ns; ++i) {
+        const int sub = i & 3;
+        if (sub == 0) {
+          if (lane == 0) ok = mbar_wait(pfull + ps, (uint32_t)pu & 1u, g.spin);
+          ok = __all_sync(0xFFFFFFFFu, ok);
+          if (!ok) break;
+        }
+        if (qu > 0) {
+          if (lane == 0) ok = mbar_wait(qempty + qs, (uint32_t)(qu - 1) & 1u, g.spin);
+          ok = __all_sync(0xFFFFFFFFu, ok);
+          if (!ok) break;
+        }
+        const uint8_t* base = pring + (size_t)ps * g.pst;
+        uint8_t* out = sm + (size_t)qs * g.qst;
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
+          const uint4 v = *reinterpret_cast<const uint4*>(base + (size_t)a * kCodeTile + r * 128 + (((2 * sub + half) ^ r7) << 4));
+          const uint8_t* sc = base + NA * kCodeTile + (a * CPS + (E8 ? sub >> 1 : sub)) * 512 + (r & 31) * 16 + (r >> 5) * 4;
+          const uint32_t s = E8 ? (uint32_t)sc[(sub & 1) * 2 + half] : (uint32_t)*reinterpret_cast<const uint16_t*>(sc + half * 2);
+          decode32<FMT>(v, s, out + (size_t)a * kCodeTile + r * 128, half, r7);
+        }
+        if (!g.btma) {   // rows off 16-byte boundaries: 8 columns a thread at a time
+          const int k0 = (s0 + i) * 64;
+          for (int c = bt; c < N * 8; c += kDecodeWarps * 32) {
+            const int t = t0 + (c >> 3), k = k0 + (c & 7) * 8;
+            const uint16_t* xr = reinterpret_cast<const uint16_t*>(g.x) + (int64_t)t * g.x_ld + k;
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t lo = t < g.T && k + 2 * e < g.cols ? xr[2 * e] : 0u;
+              const uint32_t hi = t < g.T && k + 2 * e + 1 < g.cols ? xr[2 * e + 1] : 0u;
+              w[e] = lo | (hi << 16);
+            }
+            const int rr = c >> 3;
+            *reinterpret_cast<uint4*>(out + NA * kCodeTile + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+        fence_proxy_async();   // generic writes -> tensor-core reads
+        __syncwarp();
+        if (lane == 0) mbar_arrive(qfull + qs);
+        if (++qs == Q) {
+          qs = 0;
+          ++qu;
+        }
+        if (sub == 3 || i == ns - 1) {
+          if (lane == 0) mbar_arrive(pempty + ps);
+          if (++ps == P) {
+            ps = 0;
+            ++pu;
+          }
+        }
+      }
+    }
+  } else if (wid >= 4 + kDecodeWarps) {
+    const int r = 32 * (wid & 3) + lane;
+    int it = 0;
+    for (int tile = blockIdx.x; tile < g.ntiles; tile += gridDim.x, ++it) {
+      const int buf = it % g.nbuf, use = it / g.nbuf;
+      if (lane == 0) ok = mbar_wait(afull + buf, (uint32_t)use & 1u, g.spin);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const int m = tile % g.mt * 128 + r, t0 = tile / g.mt * N;
+      const uint32_t tl = tmem + ((uint32_t)(32 * (wid & 3)) << 16) + (uint32_t)(buf * NA * N);
+      for (int c0 = 0; c0 < N; c0 += 16) {
+        uint32_t v[NA][16];
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
+          if (ns > 0) {
+            tmem_ld16(tl + (uint32_t)(a * N + c0), v[a]);
+          } else {
+#pragma unroll
+            for (int q = 0; q < 16; ++q) v[a][q] = 0u;
+          }
+        }
+        if (g.splits > 1) {
+#pragma unroll
+          for (int a = 0; a < NA; ++a)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) red[(size_t)(a * N + c0 + q) * 128 + r] = __uint_as_float(v[a][q]);
+        } else if (m < g.rows) {
+#pragma unroll
+          for (int q = 0; q < 16; ++q) {
+            const int t = t0 + c0 + q;
+            if (t >= g.T) break;
+            float o = __uint_as_float(v[0][q]) * g.sw;
+            if (GLU) o = silu_mul(o, __uint_as_float(v[NA - 1][q]) * g.su);
+            store_y(g.y, g.y_type, (int64_t)t * g.y_ld + m, o);
+          }
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(aempty + buf);
+    }
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  if (g.splits > 1) {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    const int tile = blockIdx.x;
+    sum_splits<NA, kWideThreads>(red, N, g.splits, rank, tile % g.mt * 128, g.rows, tile / g.mt * N, g.T, g.sw, g.su, g.y, g.y_type, g.y_ld);
+    // no CTA leaves while others may still read its shared memory
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+  } else {
+    __syncthreads();
+  }
+  if (!ok && g.status) atomicCAS(g.status, 0, BITSMOE_ERR_TIMEOUT);
+  if (wid == 1) {
+    __syncwarp();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int FMT, bool GLU>
+cudaError_t launch_wide(const bitsmoe_microscale* w, const bitsmoe_microscale* up, WideArgs g, int sms, cudaStream_t st) {
+  constexpr int NA = GLU ? 2 : 1, CPS = FMT == BITSMOE_MICRO_E8M0 ? 2 : 4;
+  constexpr uint32_t kRoom = 216 * 1024;
+  int tt = (g.T + 255) / 256;
+  g.N = ((g.T + tt - 1) / tt + 15) / 16 * 16;
+  tt = (g.T + g.N - 1) / g.N;
+  g.mt = (g.rows + 127) / 128;
+  g.ntiles = g.mt * tt;
+  g.nbuf = 2 * NA * g.N <= 512 ? 2 : 1;
+  g.nst = (g.cols + kStageK - 1) / kStageK;
+  g.pst = (uint32_t)NA * (kCodeTile + CPS * 512);
+  g.qst = (uint32_t)NA * kCodeTile + (uint32_t)g.N * 128;
+  g.Q = std::min<int>(4, (kRoom - 2 * g.pst) / g.qst);
+  g.P = std::min<int>(8, (kRoom - g.Q * g.qst) / g.pst);
+  int splits = 1;
+  while (splits < 8 && (int64_t)g.ntiles * splits * 2 <= sms && g.nst >= 2 * splits &&
+         (uint32_t)(NA * g.N) * 512u <= g.Q * g.qst + g.P * g.pst)
+    splits *= 2;
+  g.splits = splits;
+  g.sps = (g.nst + splits - 1) / splits;
+  if (FMT == BITSMOE_MICRO_E4M3) {
+    g.sw *= 128.f;
+    g.su *= 128.f;
+  }
+  const size_t smem = 1024 + (size_t)g.Q * g.qst + (size_t)g.P * g.pst + (size_t)(2 * g.P + 2 * g.Q + 4) * 8 + 16;
+  const int64_t pitch = micro_pitch(g.cols);
+  CUtensorMap wm, um, xm;
+  if (!make_row_map(&wm, true, w->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
+  um = xm = wm;
+  if (GLU && !make_row_map(&um, true, up->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
+  g.btma = (uintptr_t)g.x % 16 == 0 && (g.x_ld % 8 == 0 || g.T == 1);
+  if (g.btma) g.btma = make_row_map(&xm, false, g.x, g.T, g.cols, g.T == 1 ? (g.cols * 2 + 15) / 16 * 16 : g.x_ld * 2, g.N);
+  auto kern = k_micro_wide<FMT, GLU>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1;
+  attr[0].val.clusterDim.y = (unsigned)splits;
+  attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(splits > 1 ? g.ntiles : std::min(g.ntiles, sms)), (unsigned)splits, 1);
+  cfg.blockDim = dim3(kWideThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
@@ -921,10 +1236,25 @@ extern "C" int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bit
       e = up ? launch_coded<BITSMOE_MICRO_E4M3, true>(w, up, xq, c, sms, st) : launch_coded<BITSMOE_MICRO_E4M3, false>(w, up, xq, c, sms, st);
     return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
   }
-  ProductArgs a{mat_of(w), mat_of(up), mat_of(xq), static_cast<const __nv_bfloat16*>(x), x_ld, T, w->rows, w->cols,
-                w->format, w->scale * sx, up ? up->scale * sx : 0.f, y, y_type, y_ld};
-  const dim3 g((unsigned)((w->rows + kTR - 1) / kTR), (unsigned)((T + kTT - 1) / kTT < 65535 ? (T + kTT - 1) / kTT : 65535));
-  k_micro_product<<<g, kPThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
-  const cudaError_t r = cudaGetLastError();
-  return r == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)r);
+  WideArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.T = T;
+  a.rows = w->rows;
+  a.cols = w->cols;
+  a.tiles = micro_tiles(w->format, w->cols);
+  a.ws = w->scales;
+  a.us = up ? up->scales : nullptr;
+  a.x = static_cast<const __nv_bfloat16*>(x);
+  a.x_ld = x_ld;
+  a.sw = w->scale;
+  a.su = up ? up->scale : 0.f;
+  a.y = y;
+  a.y_type = y_type;
+  a.y_ld = y_ld;
+  a.spin = spin;
+  a.lose = debug_skip_arrival();
+  a.status = status;
+  if (e8) e = up ? launch_wide<BITSMOE_MICRO_E8M0, true>(w, up, a, sms, st) : launch_wide<BITSMOE_MICRO_E8M0, false>(w, up, a, sms, st);
+  else e = up ? launch_wide<BITSMOE_MICRO_E4M3, true>(w, up, a, sms, st) : launch_wide<BITSMOE_MICRO_E4M3, false>(w, up, a, sms, st);
+  return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
 }
