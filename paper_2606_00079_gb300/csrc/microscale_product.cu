@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstring>
 
 #include "microscale.cuh"
@@ -60,8 +61,12 @@ constexpr int kFewTokens = 16;
 constexpr int kStageK = 256;                       // columns of a stage (128 bytes of codes a row)
 constexpr uint32_t kCodeTile = 128 * 128;          // bytes of 128 rows of a stage's codes
 
+// Bytes of a CTA's buffer of partial sums: 2 halves x matrices x tokens x 128 rows (a CTA's share of the rows
+// from every CTA of the cluster).
+__host__ __device__ constexpr uint32_t few_red_bytes(int na, int nt) { return 2u * na * nt * 8 * 512; }
+
 struct FewArgs {
-  int T, rows, cols, tiles;
+  int T, rows, cols, tiles, mt;
   int nst, sps, splits, stages;
   uint32_t stage;
   uint32_t x_pitch;      // bytes of a token's activations in shared memory
@@ -92,18 +97,22 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 
-// The codes of byte B of w (columns 2B and 2B + 1) as a pair of fp16, or of bf16.
-template <bool BF, int B>
-__device__ __forceinline__ uint32_t code_pair(uint32_t w) {
-  uint32_t r;
+// The 8 codes of w as 4 pairs (columns 2i, 2i + 1) of fp16, or of bf16 (the codes' bits as bf16 are the
+// values times 2^-126).
+template <bool BF>
+__device__ __forceinline__ void code_pairs(uint32_t w, uint32_t (&r)[4]) {
   if constexpr (!BF) {
-    asm("{\n .reg .b8 t0, t1, t2, t3;\n mov.b32 {t0, t1, t2, t3}, %1;\n cvt.rn.f16x2.e2m1x2 %0, t0;\n}" : "=r"(r) : "r"(w >> (8 * B)));
+    asm("{\n .reg .b8 t0, t1, t2, t3;\n mov.b32 {t0, t1, t2, t3}, %4;\n cvt.rn.f16x2.e2m1x2 %0, t0;\n cvt.rn.f16x2.e2m1x2 %1, t1;\n"
+        " cvt.rn.f16x2.e2m1x2 %2, t2;\n cvt.rn.f16x2.e2m1x2 %3, t3;\n}"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(w));
   } else {
-    const uint32_t n = ((w >> (8 * B)) & 0xFu) | (((w >> (8 * B + 4)) & 0xFu) << 16);
-    r = ((n & 0x00080008u) << 12) | ((n & 0x00070007u) << 6);            // the values times 2^-126
-    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(r) : "r"(0x7E807E80u));       // 2^126: exact
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const uint32_t n = ((w >> (8 * b)) & 0xFu) | (((w >> (8 * b + 4)) & 0xFu) << 16);
+      r[b] = ((n & 0x00080008u) << 12) | ((n & 0x00070007u) << 6);
+      asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(r[b]) : "r"(0x7E807E80u));   // 2^126: exact
+    }
   }
-  return r;
 }
 
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
@@ -111,106 +120,106 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a) {
   asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
 }
-__device__ __forceinline__ uint32_t lds16(uint32_t a) {
-  uint16_t v;
-  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-  uint2 v;
-  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-  return v;
-}
 __device__ __forceinline__ uint4 lds128a(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
   return v;
 }
-
-// The four block scales of a scale word in fp32, times inv.
-template <int FMT>
-__device__ __forceinline__ void scales4(uint32_t w, float inv, float (&s)[4]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const uint16_t p = (uint16_t)(w >> (16 * h));
-    uint32_t r;
-    if constexpr (FMT == BITSMOE_MICRO_E8M0) {
-      asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(r) : "h"(p));
-      s[2 * h] = bf16lo(r) * inv;
-      s[2 * h + 1] = bf16hi(r) * inv;
-    } else {
-      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(p));
-      s[2 * h] = f16lo(r) * inv;
-      s[2 * h + 1] = f16hi(r) * inv;
-    }
-  }
+__device__ __forceinline__ uint32_t e4m3x2_f16(uint32_t p) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)p));
+  return r;
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (BF) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 
-// This warp's 16 rows x 128 columns of a stage (half kh) with NT tiles of 8 tokens.
+// This warp's 16 rows x 128 columns of a stage (half kh) with NT tiles of 8 tokens.  Lane (g, t) takes the codes
+// of columns 8t .. 8t + 7 of every 32, of rows g and g + 8: two products of 16 columns.
+// E8M0: the 32 columns are a block of each row; its scale (times inv, a pair of bf16) multiplies the products' fp32 sum.
+// E4M3: a lane's 8 columns lie in one block, whose scale multiplies the codes (6 significant bits between 2^-10
+// and 2688: exact in fp16 and bf16).
 template <int FMT, int NA, int NT, bool BF>
-__device__ __forceinline__ void few_half(uint32_t code, uint32_t sf, uint32_t xa, uint32_t x_pitch, int T, int rt, int kh,
-                                         int lane, int tiles_left, float inv, float (&acc)[NA][NT][4]) {
+__device__ __forceinline__ void few_half(uint32_t code, uint32_t sf, const uint32_t (&xo)[NT], int rt, int kh, int lane,
+                                         int tiles_left, uint32_t inv, float (&acc)[NA][NT][4]) {
   constexpr bool E8 = FMT == BITSMOE_MICRO_E8M0;
   constexpr int TPH = E8 ? 1 : 2;   // scale tiles of a half
   constexpr int CPS = 2 * TPH;
   const int g = lane >> 2, t = lane & 3;
   const int r = 16 * rt + g;
-  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+  const uint32_t pick = t >= 2 ? 0x3232u : 0x1010u;   // E4M3: this lane's block of the two of 32 columns
 #pragma unroll
   for (int q = 0; q < TPH; ++q) {
     const int tile = kh * TPH + q;
     if (tile >= tiles_left) return;   // past the matrix's columns (and its scales)
-    float s[NA][2][4];
+    uint32_t sw[NA][2];
 #pragma unroll
     for (int a = 0; a < NA; ++a)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int rr = r + 8 * h;
-        scales4<FMT>(lds32(sf + (uint32_t)(a * CPS + tile) * 512 + (rr & 31) * 16 + (rr >> 5) * 4), inv, s[a][h]);
+        sw[a][h] = lds32(sf + (uint32_t)(a * CPS + tile) * 512 + (rr & 31) * 16 + (rr >> 5) * 4);
       }
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int j = E8 ? kh * 4 + b : kh * 4 + q * 2 + (b >> 1);   // 16-byte chunk of the row
-      uint32_t xb[NT][E8 ? 4 : 2];
+    for (int b = 0; b < 4 / TPH; ++b) {
+      const int j = kh * 4 + q * 2 + b;   // 32 columns: 16-byte chunk of the row
+      uint4 xb[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const uint32_t at = xa + (uint32_t)(n * 8 + g) * x_pitch + (uint32_t)j * 64 + (E8 ? t * 16 : (b & 1) * 32 + t * 8);
-        if constexpr (E8) {
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (n * 8 + g < T) v = lds128a(at);
-          xb[n][0] = v.x, xb[n][1] = v.y, xb[n][2] = v.z, xb[n][3] = v.w;
-        } else {
-          uint2 v = make_uint2(0u, 0u);
-          if (n * 8 + g < T) v = lds64(at);
-          xb[n][0] = v.x, xb[n][1] = v.y;
-        }
+        xb[n] = lds128a(xo[n] + (uint32_t)j * 64);
       }
 #pragma unroll
       for (int a = 0; a < NA; ++a) {
-        const uint32_t base = code + (uint32_t)a * kCodeTile + (uint32_t)r * 128 + (uint32_t)((j ^ g) << 4);
-        float d[NT][4];
+        const uint32_t base = code + (uint32_t)a * kCodeTile + (uint32_t)r * 128 + (uint32_t)((j ^ g) << 4) + t * 4;
+        uint32_t p0[4], p1[4];
+        code_pairs<BF>(lds32(base), p0);
+        code_pairs<BF>(lds32(base + 1024), p1);
         if constexpr (E8) {
-          const uint32_t w0 = lds32(base + t * 4), w1 = lds32(base + 1024 + t * 4);
-          const uint32_t a0[4] = {code_pair<BF, 0>(w0), code_pair<BF, 0>(w1), code_pair<BF, 1>(w0), code_pair<BF, 1>(w1)};
-          const uint32_t a1[4] = {code_pair<BF, 2>(w0), code_pair<BF, 2>(w1), code_pair<BF, 3>(w0), code_pair<BF, 3>(w1)};
+          float s[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t v;
+            asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(v) : "h"((uint16_t)(sw[a][h] >> (16 * (b >> 1)))));
+            v = mul2<true>(v, inv);
+            s[h] = (b & 1) ? bf16hi(v) : bf16lo(v);
+          }
+          const float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            mma16<BF>(d[n], a0, xb[n][0], xb[n][1], zero);
-            mma16<BF>(d[n], a1, xb[n][2], xb[n][3], d[n]);
+            float d[4], e[4];
+            mma16<BF>(d, {p0[0], p1[0], p0[1], p1[1]}, xb[n].x, xb[n].y, zero);
+            mma16<BF>(e, {p0[2], p1[2], p0[3], p1[3]}, xb[n].z, xb[n].w, d);
+            acc[a][n][0] = fmaf(s[0], e[0], acc[a][n][0]);
+            acc[a][n][1] = fmaf(s[0], e[1], acc[a][n][1]);
+            acc[a][n][2] = fmaf(s[1], e[2], acc[a][n][2]);
+            acc[a][n][3] = fmaf(s[1], e[3], acc[a][n][3]);
           }
         } else {
-          const uint32_t o = (b & 1) * 8 + t * 2;
-          const uint32_t w0 = lds16(base + o), w1 = lds16(base + 1024 + o);
-          const uint32_t a0[4] = {code_pair<BF, 0>(w0), code_pair<BF, 0>(w1), code_pair<BF, 1>(w0), code_pair<BF, 1>(w1)};
+          uint32_t m[2];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma16<BF>(d[n], a0, xb[n][0], xb[n][1], zero);
-        }
+          for (int h = 0; h < 2; ++h) {
+            m[h] = e4m3x2_f16(sw[a][h] >> (16 * b));
+            if constexpr (BF) {
+              const __nv_bfloat162 v = __floats2bfloat162_rn(f16lo(m[h]), f16hi(m[h]));   // exact
+              m[h] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+            m[h] = __byte_perm(m[h], 0u, pick);
+          }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          acc[a][n][0] = fmaf(s[a][0][b], d[n][0], acc[a][n][0]);
-          acc[a][n][1] = fmaf(s[a][0][b], d[n][1], acc[a][n][1]);
-          acc[a][n][2] = fmaf(s[a][1][b], d[n][2], acc[a][n][2]);
-          acc[a][n][3] = fmaf(s[a][1][b], d[n][3], acc[a][n][3]);
+          for (int i = 0; i < 4; ++i) {
+            p0[i] = mul2<BF>(p0[i], m[0]);
+            p1[i] = mul2<BF>(p1[i], m[1]);
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float d[4];
+            mma16<BF>(d, {p0[0], p1[0], p0[1], p1[1]}, xb[n].x, xb[n].y, acc[a][n]);
+            mma16<BF>(acc[a][n], {p0[2], p1[2], p0[3], p1[3]}, xb[n].z, xb[n].w, d);
+          }
         }
       }
     }
@@ -240,6 +249,9 @@ __device__ __forceinline__ void few_x8(const FewArgs& g, int format, int t, int 
   }
 }
 
+// A cluster takes row tiles of 128 one after the other; its CTAs split the columns.  Each warp adds its part of a
+// tile to the CTA that stores those rows, by remote stores into that CTA's shared memory, two buffers in turn
+// (a CTA that has all parts of tile i + 1 knows that every CTA is done with its buffer of tile i).
 template <int FMT, bool GLU, int NT>
 __global__ void __launch_bounds__(kFewThreads, 1)
     k_micro_few(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, FewArgs g) {
@@ -250,227 +262,310 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   __shared__ int inexact_any;
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const int S = g.stages;
-  constexpr uint32_t redb = 2u * NA * NT * 8 * 512;   // [half][matrix][token][128 rows] fp32, reuses the ring
-  const uint32_t ring = (uint32_t)S * g.stage > redb ? (uint32_t)S * g.stage : redb;
-  float* red = reinterpret_cast<float*>(sm);
-  uint8_t* xs = sm + ring;
+  constexpr uint32_t kRed = few_red_bytes(NA, NT);   // [rank][half][matrix][token][rows of this CTA] fp32
+  uint8_t* redb = sm + (size_t)S * g.stage;          // two of them
+  uint8_t* xs = redb + 2 * kRed;
   uint64_t* full = reinterpret_cast<uint64_t*>(xs + (size_t)g.T * g.x_pitch);
   uint64_t* empty = full + S;
+  uint64_t* rfull = empty + S;                        // [2] the parts of a tile are there
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int rank = blockIdx.y, mi = blockIdx.x, m0 = mi * 128;
+  const int rank = blockIdx.y;
   const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
+  if (tid == kFewWarps * 32) {
+    prefetch_map(&wmap);
+    if (GLU) prefetch_map(&umap);
+  }
   if (tid == 0) {
     for (int i = 0; i < S; ++i) {
       mbar_init_n(full + i, 1);
-      mbar_init_n(empty + i, kFewWarps);
+      mbar_init_n(empty + i, nk == 1 ? kFewWarps : kFewWarps / 2);
     }
+    for (int i = 0; i < 2; ++i) mbar_init_n(rfull + i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    for (int i = 0; i < 2; ++i) mbar_expect_tx(rfull + i, kRed);
+    top = 0u;
+    inexact_any = 0;
   }
-  if (tid == 0) top = 0u, inexact_any = 0;
   __syncthreads();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
   bool ok = true;
-  float acc[NA][NT][4] = {};
-  float inv = 1.f;   // undoes the activations' power of two, in the block scales
 
   if (wid == kFewWarps) {
     if (lane == 0) {
-      int i = 0;
-      for (int st = 0, u = 0; i < nk; ++i) {
-        if (u > 0) ok = mbar_wait(empty + st, (uint32_t)(u - 1) & 1u, g.spin);
-        if (!ok) break;
-        const int kb = st0 + i, cnt = min(CPS, g.tiles - kb * CPS);
-        uint8_t* base = sm + (size_t)st * g.stage;
-        const uint32_t bar = smem_u32(full + st);
-        mbar_expect_tx(full + st, NA * (kCodeTile + (uint32_t)cnt * 512u));
-        tma_load_2d(smem_u32(base), &wmap, kb * 128, m0, bar);
-        if (GLU) tma_load_2d(smem_u32(base) + kCodeTile, &umap, kb * 128, m0, bar);
-        const size_t at = ((size_t)mi * g.tiles + (size_t)kb * CPS) * 512;
-        bulk_g2s(base + NA * kCodeTile, g.ws + at, (uint32_t)cnt * 512u, full + st);
-        if (GLU) bulk_g2s(base + NA * kCodeTile + CPS * 512, g.us + at, (uint32_t)cnt * 512u, full + st);
-        if (++st == S) {
-          st = 0;
-          ++u;
+      int st = 0, u = 0, n = 0;
+      for (int mi = blockIdx.x; mi < g.mt && ok; mi += gridDim.x) {
+        for (int i = 0; i < nk; ++i, ++n) {
+          if (u > 0) ok = mbar_wait(empty + st, (uint32_t)(u - 1) & 1u, g.spin);
+          if (!ok) break;
+          const int kb = st0 + i, cnt = min(CPS, g.tiles - kb * CPS);
+          uint8_t* base = sm + (size_t)st * g.stage;
+          const uint32_t bar = smem_u32(full + st);
+          mbar_expect_tx(full + st, NA * (kCodeTile + (uint32_t)cnt * 512u));
+          tma_load_2d(smem_u32(base), &wmap, kb * 128, mi * 128, bar);
+          if (GLU) tma_load_2d(smem_u32(base) + kCodeTile, &umap, kb * 128, mi * 128, bar);
+          const size_t at = ((size_t)mi * g.tiles + (size_t)kb * CPS) * 512;
+          bulk_g2s(base + NA * kCodeTile, g.ws + at, (uint32_t)cnt * 512u, full + st);
+          if (GLU) bulk_g2s(base + NA * kCodeTile + CPS * 512, g.us + at, (uint32_t)cnt * 512u, full + st);
+          if (++st == S) {
+            st = 0;
+            ++u;
+          }
         }
       }
-      for (int j = max(0, i - S); j < i; ++j) mbar_wait(full + j % S, (uint32_t)(j / S) & 1u);   // copies in flight
+      for (int j = max(0, n - S); j < n; ++j) mbar_wait(full + j % S, (uint32_t)(j / S) & 1u);   // copies in flight
     }
     __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
   } else {
     // The activations of this CTA's columns, 8 a thread at a time (a warp within one token).
     const int k0 = st0 * kStageK, n8 = nk * (kStageK / 8), per = (n8 + 31) / 32;
-    float m = 0.f;
-    for (int w = wid; w < g.T * per; w += kFewWarps) {
-      const int t = w / per, c = (w - t * per) * 32 + lane;
-      if (c >= n8) continue;
-      float v[8];
-      few_x8(g, FMT, t, k0 + c * 8, v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (fabsf(v[i]) <= 3.402823466e38f) m = fmaxf(m, fabsf(v[i]));
-    }
-    m = warp_max(m);
-    if (lane == 0 && m > 0.f) atomicMax(&top, __float_as_uint(m));
-    bar_consumers();
-    // 2^14 over the power of two at or below the largest; beyond 2^29 or below 2^-86 (and at 0) they stay as they are
-    const int e = (int)(top >> 23) - 127;
-    const bool norm = e >= -86 && e < 29;
-    const float mul = norm ? __uint_as_float((uint32_t)(14 - e + 127) << 23) : 1.f;
-    inv = norm ? __uint_as_float((uint32_t)(e - 14 + 127) << 23) : 1.f;
-    bool inexact = !norm && top != 0u;
-    for (int w = wid; w < g.T * per; w += kFewWarps) {
-      const int t = w / per, c = (w - t * per) * 32 + lane;
-      if (c >= n8) continue;
-      float v[8];
-      few_x8(g, FMT, t, k0 + c * 8, v);
-      uint32_t h[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p = v[2 * i] * mul, q = v[2 * i + 1] * mul;
-        const __half2 f = __floats2half2_rn(p, q);
-        const float2 back = __half22float2(f);
-        inexact |= (back.x != p && p == p) || (back.y != q && q == q) || (p == 0.f && v[2 * i] != 0.f) ||
-                   (q == 0.f && v[2 * i + 1] != 0.f);
-        h[i] = *reinterpret_cast<const uint32_t*>(&f);
-      }
-      *reinterpret_cast<uint4*>(xs + (size_t)t * g.x_pitch + (size_t)c * 16) = make_uint4(h[0], h[1], h[2], h[3]);
-    }
-    if (inexact) inexact_any = 1;
-    bar_consumers();
-    const bool bf = inexact_any != 0;
-    if (bf) {
-      inv = 1.f;
+    float inv = 1.f;   // undoes the activations' power of two
+    bool bf = false;
+    if (!E8 && g.xq.codes) {   // code times E4M3 scale: exact in fp16 as it is
       for (int w = wid; w < g.T * per; w += kFewWarps) {
-        const int t = w / per, c = (w - t * per) * 32 + lane;
+        const int t = w / per, c = (w - t * per) * 32 + lane, k = k0 + c * 8;
         if (c >= n8) continue;
-        float v[8];
-        few_x8(g, FMT, t, k0 + c * 8, v);
-        uint32_t h[4];
+        uint32_t h[4] = {0u, 0u, 0u, 0u};
+        if (k < g.cols) {
+          code_pairs<false>(__ldg(reinterpret_cast<const uint32_t*>(g.xq.codes + (int64_t)t * g.xq.pitch + k / 2)), h);
+          const uint32_t m = __byte_perm(e4m3x2_f16(g.xq.scales[micro_scale_at(g.xq.tiles, t, k / 16)]), 0u, 0x1010u);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const __nv_bfloat162 f = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);   // exact
-          h[i] = *reinterpret_cast<const uint32_t*>(&f);
+          for (int i = 0; i < 4; ++i) h[i] = mul2<false>(h[i], m);
         }
         *reinterpret_cast<uint4*>(xs + (size_t)t * g.x_pitch + (size_t)c * 16) = make_uint4(h[0], h[1], h[2], h[3]);
       }
       bar_consumers();
-    }
-    const int rt = wid & 7, kh = wid >> 3;
-    const uint32_t xa = smem_u32(xs);
-    for (int i = 0, st = 0, u = 0; i < nk; ++i) {
-      if (lane == 0) ok = mbar_wait(full + st, (uint32_t)u & 1u, g.spin);
-      ok = __all_sync(0xFFFFFFFFu, ok);
-      if (!ok) break;
-      const uint32_t code = smem_u32(sm) + (uint32_t)st * g.stage, sf = code + NA * kCodeTile;
-      const int left = g.tiles - (st0 + i) * CPS;
-      if (bf) few_half<FMT, NA, NT, true>(code, sf, xa + (uint32_t)i * (kStageK * 2), g.x_pitch, g.T, rt, kh, lane, left, inv, acc);
-      else few_half<FMT, NA, NT, false>(code, sf, xa + (uint32_t)i * (kStageK * 2), g.x_pitch, g.T, rt, kh, lane, left, inv, acc);
-      __syncwarp();
-      if (lane == 0 && !(g.lose && i == 0 && wid == 0 && (blockIdx.x | blockIdx.y) == 0)) mbar_arrive(empty + st);
-      if (++st == S) {
-        st = 0;
-        ++u;
+    } else {
+      // In fp16 times mul; whether all of them are exact there; the largest finite magnitude.
+      const auto stage = [&](float mul) {
+        bool inexact = false;
+        float m = 0.f;
+        for (int w = wid; w < g.T * per; w += kFewWarps) {
+          const int t = w / per, c = (w - t * per) * 32 + lane;
+          if (c >= n8) continue;
+          float v[8];
+          few_x8(g, FMT, t, k0 + c * 8, v);
+          uint32_t h[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = v[2 * i] * mul, q = v[2 * i + 1] * mul;
+            const __half2 f = __floats2half2_rn(p, q);
+            const float2 back = __half22float2(f);
+            inexact |= (back.x != p && p == p) || (back.y != q && q == q) || (p == 0.f && v[2 * i] != 0.f) ||
+                       (q == 0.f && v[2 * i + 1] != 0.f);
+            h[i] = *reinterpret_cast<const uint32_t*>(&f);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (fabsf(v[i]) <= 3.402823466e38f) m = fmaxf(m, fabsf(v[i]));
+          *reinterpret_cast<uint4*>(xs + (size_t)t * g.x_pitch + (size_t)c * 16) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+        if (inexact) {
+          inexact_any = 1;
+          atomicMax(&top, __float_as_uint(m));
+        } else if (m > 0.f && g.T * per > 0) {
+          const uint32_t b = __float_as_uint(m);
+          if (b > *(volatile uint32_t*)&top) atomicMax(&top, b);
+        }
+        bar_consumers();
+        return inexact_any != 0;
+      };
+      inv = 0.015625f;
+      if (stage(64.f)) {   // not all of them in 2^-23 .. 2^10: the largest to [2^14, 2^15)
+        bar_consumers();
+        if (tid == 0) inexact_any = 0;
+        bar_consumers();
+        const int e = (int)(top >> 23) - 127;
+        const bool norm = e >= -86 && e < 29;   // beyond, the inverse could take block scales out of range
+        inv = norm ? __uint_as_float((uint32_t)(e - 14 + 127) << 23) : 1.f;
+        bf = !norm || stage(__uint_as_float((uint32_t)(14 - e + 127) << 23));
+        if (bf) {
+          inv = 1.f;
+          bar_consumers();
+          for (int w = wid; w < g.T * per; w += kFewWarps) {
+            const int t = w / per, c = (w - t * per) * 32 + lane;
+            if (c >= n8) continue;
+            float v[8];
+            few_x8(g, FMT, t, k0 + c * 8, v);
+            uint32_t h[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const __nv_bfloat162 f = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);   // exact
+              h[i] = *reinterpret_cast<const uint32_t*>(&f);
+            }
+            *reinterpret_cast<uint4*>(xs + (size_t)t * g.x_pitch + (size_t)c * 16) = make_uint4(h[0], h[1], h[2], h[3]);
+          }
+          bar_consumers();
+        }
       }
     }
-  }
-  __syncthreads();   // every stage has been read: the ring is free
-  if (wid < kFewWarps) {
-    const int rt = wid & 7, kh = wid >> 3, r = 16 * rt + (lane >> 2);
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // the cluster's barriers are set up
+    const int rt = wid & 7, kh = wid >> 3;
+    uint32_t xo[NT];   // this lane's activations of column 0 (tokens past T read the last one's; nothing stores their results)
 #pragma unroll
-    for (int a = 0; a < NA; ++a)
+    for (int n = 0; n < NT; ++n)
+      xo[n] = smem_u32(xs) + (uint32_t)min(n * 8 + (lane >> 2), g.T - 1) * g.x_pitch + (uint32_t)(lane & 3) * 16;
+    const uint32_t inv2 = (__float_as_uint(inv) >> 16) * 0x10001u;   // a power of two from 2^-100 to 2^14: exact in bf16
+    // The two groups of eight warps take every other stage; a CTA with a single one, half of its columns each.
+    const bool halves = nk == 1;
+    const int rs = 128 / g.splits;                              // rows that a CTA stores
+    const int owner = 16 * rt / rs, orow = 16 * rt - owner * rs + (lane >> 2);
+    int n = 0, it = 0;   // stages of all tiles so far
+    for (int mi = blockIdx.x; mi < g.mt; mi += gridDim.x, ++it) {
+      float acc[NA][NT][4] = {};
+      for (int i = 0; i < nk && ok; ++i, ++n) {
+        if (!halves && (i & 1) != kh) continue;
+        const int st = n % S;
+        if (lane == 0) ok = mbar_wait(full + st, (uint32_t)(n / S) & 1u, g.spin);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        const uint32_t code = smem_u32(sm) + (uint32_t)st * g.stage, sf = code + NA * kCodeTile;
+        const int left = g.tiles - (st0 + i) * CPS;
+        uint32_t xi[NT];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int c = n * 8 + (lane & 3) * 2 + (j & 1);
-          red[(size_t)((kh * NA + a) * NT * 8 + c) * 128 + r + (j >> 1) * 8] = acc[a][n][j];
-        }
-  }
-  // the partial sums of the two halves and of the cluster's CTAs, in this order; a CTA sums its share of the rows
-  const auto finish = [&](bool cluster) {
-    const int rs = 128 / g.splits, rbeg = rank * rs;
-    const uint32_t lred = smem_u32(red);
-    for (int e = tid; e < rs * g.T; e += kFewThreads) {
-      const int c = e / rs, r = rbeg + (e - c * rs);
-      float sum[NA];
-#pragma unroll
-      for (int a = 0; a < NA; ++a) {
-        const uint32_t l0 = lred + (uint32_t)((a * NT * 8 + c) * 128 + r) * 4u, l1 = l0 + (uint32_t)(NA * NT * 8) * 512u;
-        if (!cluster) {
-          sum[a] = __uint_as_float(lds32(l0)) + __uint_as_float(lds32(l1));
+        for (int q = 0; q < NT; ++q) xi[q] = xo[q] + (uint32_t)i * (kStageK * 2);
+        if (bf) {
+#pragma unroll 1
+          for (int h = halves ? kh : 0; h < (halves ? kh + 1 : 2); ++h)
+            few_half<FMT, NA, NT, true>(code, sf, xi, rt, h, lane, left, inv2, acc);
+        } else if (halves) {
+          few_half<FMT, NA, NT, false>(code, sf, xi, rt, kh, lane, left, inv2, acc);
         } else {
+          few_half<FMT, NA, NT, false>(code, sf, xi, rt, 0, lane, left, inv2, acc);
+          few_half<FMT, NA, NT, false>(code, sf, xi, rt, 1, lane, left, inv2, acc);
+        }
+        __syncwarp();
+        if (lane == 0 && !(g.lose && i == 0 && it == 0 && wid == 0 && (blockIdx.x | blockIdx.y) == 0)) mbar_arrive(empty + st);
+      }
+      // this warp's part to the CTA that stores these rows, counted in bytes on its barrier
+      uint32_t dst, bar;
+      const uint32_t buf = smem_u32(redb) + (uint32_t)(it & 1) * kRed;
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"(buf), "r"(owner));
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(smem_u32(rfull + (it & 1))), "r"(owner));
+      const float unit = E8 ? 1.f : inv;
+#pragma unroll
+      for (int a = 0; a < NA; ++a)
+#pragma unroll
+        for (int q = 0; q < NT; ++q)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int c = q * 8 + (lane & 3) * 2 + (j & 1);
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::
+                             "r"(dst + (uint32_t)((((rank * 2 + kh) * NA + a) * NT * 8 + c) * rs + orow + (j >> 1) * 8) * 4u),
+                         "r"(__float_as_uint(acc[a][q][j] * unit)), "r"(bar) : "memory");
+          }
+      if (mi + (int)gridDim.x >= g.mt) {   // everything sent: the others may leave once they have their parts
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+      }
+      // the parts of this CTA's rows, added in the order of the CTAs and halves
+      // (a warp whose wait ran out sends and stores nothing of use from then on, but keeps every barrier)
+      if (ok && lane == 0) ok = mbar_wait_cluster(rfull + (it & 1), (uint32_t)(it >> 1) & 1u, g.spin);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      for (int e = tid; e < rs * g.T; e += kFewWarps * 32) {
+        const int c = e / rs, r = e - c * rs;
+        float sum[NA];
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
           float p[16];
 #pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            p[2 * q] = p[2 * q + 1] = 0.f;
-            if (q < g.splits) {
-              uint32_t ra;
-              asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(l0), "r"(q));
-              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p[2 * q]) : "r"(ra) : "memory");
-              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p[2 * q + 1]) : "r"(ra + (l1 - l0)) : "memory");
-            }
-          }
+          for (int q = 0; q < 16; ++q)
+            p[q] = q < 2 * g.splits ? __uint_as_float(lds32(buf + (uint32_t)(((q * NA + a) * NT * 8 + c) * rs + r) * 4u)) : 0.f;
           sum[a] = 0.f;
 #pragma unroll
-          for (int q = 0; q < 8; ++q) sum[a] += p[2 * q] + p[2 * q + 1];
+          for (int q = 0; q < 16; ++q) sum[a] += p[q];
         }
+        const int m = mi * 128 + rank * rs + r;
+        if (m >= g.rows) continue;
+        float o = sum[0] * g.sw;
+        if (GLU) o = silu_mul(o, sum[NA - 1] * g.su);
+        store_y(g.y, g.y_type, (int64_t)c * g.y_ld + m, o);
       }
-      if (m0 + r >= g.rows) continue;
-      float o = sum[0] * g.sw;
-      if (GLU) o = silu_mul(o, sum[NA - 1] * g.su);
-      store_y(g.y, g.y_type, (int64_t)c * g.y_ld + m0 + r, o);
+      __syncwarp();
+      bar_consumers();   // the whole CTA is done with this buffer before any of its warps sends tile i + 1
+      if (tid == 0 && ok) mbar_expect_tx(rfull + (it & 1), kRed);   // for tile i + 2
     }
-    __syncwarp();
-  };
-  if (g.splits > 1) {
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-    finish(true);
-    // no CTA leaves while others may still read its shared memory
-    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-  } else {
-    __syncthreads();
-    finish(false);
   }
-  if (!ok && g.status) atomicCAS(g.status, 0, BITSMOE_ERR_TIMEOUT);
+  // No CTA leaves while others may still write to its shared memory: it has all parts that are sent to it, or,
+  // after a wait that ran out, every CTA of the cluster has sent its own and they have had time to arrive.
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+  if (!ok) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 100000) {
+    }
+    if (g.status) atomicCAS(g.status, 0, BITSMOE_ERR_TIMEOUT);
+  }
+}
+
+// Clusters of `splits` CTAs of a kernel (one CTA an SM) that run at once on the current device, asked once for each.
+template <typename K>
+int resident_clusters(K kern, int threads, int splits) {
+  static std::atomic<int> known[64][4];
+  int dev = 0, q = splits == 1 ? 0 : splits == 2 ? 1 : splits == 4 ? 2 : 3;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  if (dev < 64) {
+    const int n = known[dev][q].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+  }
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024) != cudaSuccess) return 0;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1;
+  attr[0].val.clusterDim.y = (unsigned)splits;
+  attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(1, (unsigned)splits, 1);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = 220 * 1024;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) return 0;
+  if (dev < 64) known[dev][q].store(n, std::memory_order_relaxed);
+  return n;
 }
 
 struct FewPlan {
-  int splits, sps, stages;
+  int splits, sps, stages, clusters;
   uint32_t stage, x_pitch;
   size_t smem;
 };
 
 // How T tokens run on the kernel for few of them, or false when their activations do not fit shared memory.
-bool few_plan(int format, bool glu, int T, int rows, int cols, int sms, FewPlan* p) {
+bool few_plan(int format, bool glu, int T, int rows, int cols, int (*resident)(int), FewPlan* p) {
   if (T > kFewTokens) return false;
   const int NA = glu ? 2 : 1, CPS = format == BITSMOE_MICRO_E8M0 ? 2 : 4;
-  const int nst = (cols + kStageK - 1) / kStageK;
-  const int64_t mt = (rows + 127) / 128;
-  int splits = 1;
-  while (splits < 8 && mt * splits * 2 <= sms && nst >= 2 * splits) splits *= 2;
+  const int nst = (cols + kStageK - 1) / kStageK, mt = (rows + 127) / 128;
   p->stage = (uint32_t)NA * (kCodeTile + (uint32_t)CPS * 512);
-  const size_t red = (size_t)2 * NA * (T > 8 ? 16 : 8) * 512;
-  for (;; splits *= 2) {   // more CTAs per row tile where the activations take too much of the shared memory
-    if (splits > 8) return false;
-    p->sps = (nst + splits - 1) / splits;
-    // 64 (32) bytes beyond a multiple of 128: the 8 tokens of a fragment's 16-byte (8-byte) loads in different banks
-    p->x_pitch = (uint32_t)p->sps * kStageK * 2 + (format == BITSMOE_MICRO_E8M0 ? 64 : 32);
-    const size_t xb = (size_t)T * p->x_pitch;
-    const size_t room = 225 * 1024 - 1024 - 512;
-    if (xb + 3 * (size_t)p->stage > room || xb + red > room) continue;
-    p->stages = (int)std::min<size_t>({(size_t)p->sps, (room - xb) / p->stage, (size_t)16});
-    const size_t ring = std::max((size_t)p->stages * p->stage, red);
-    p->smem = 1024 + ring + xb + (size_t)2 * p->stages * 8;
+  const size_t red = 2 * (size_t)few_red_bytes(NA, T > 8 ? 2 : 1), room = 225 * 1024 - 1024 - 512;
+  int64_t best = -1;
+  for (int splits = 1; splits <= 8; splits *= 2) {   // CTAs of a cluster: the fewest of those with the least work a CTA
+    const int sps = (nst + splits - 1) / splits;
+    // 64 bytes beyond a multiple of 128: the tokens of a fragment's 16-byte loads in different banks
+    const uint32_t pitch = (uint32_t)sps * kStageK * 2 + 64;
+    const size_t xb = (size_t)T * pitch;
+    if (xb + red + 2 * (size_t)p->stage > room) continue;
+    const int clusters = std::min(mt, resident(splits));
+    if (clusters < 1) continue;
+    const int64_t work = (int64_t)((mt + clusters - 1) / clusters) * sps;
+    if (best >= 0 && work >= best) continue;
+    best = work;
     p->splits = splits;
-    return true;
+    p->sps = sps;
+    p->clusters = clusters;
+    p->x_pitch = pitch;
+    p->stages = (int)std::min<size_t>((room - xb - red) / p->stage, 16);
+    p->smem = 1024 + (size_t)p->stages * p->stage + red + xb + (size_t)(2 * p->stages + 2) * 8;
   }
+  return best >= 0;
 }
 
 template <int FMT, bool GLU, int NT>
 cudaError_t launch_few(const FewPlan& p, const bitsmoe_microscale* w, const bitsmoe_microscale* up, FewArgs g, cudaStream_t st) {
   g.nst = (g.cols + kStageK - 1) / kStageK;
+  g.mt = (g.rows + 127) / 128;
   g.splits = p.splits;
   g.sps = p.sps;
   g.stages = p.stages;
@@ -490,14 +585,17 @@ cudaError_t launch_few(const FewPlan& p, const bitsmoe_microscale* w, const bits
   attr[0].val.clusterDim.y = (unsigned)p.splits;
   attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((g.rows + 127) / 128), (unsigned)p.splits, 1);
+  cfg.gridDim = dim3((unsigned)p.clusters, (unsigned)p.splits, 1);
   cfg.blockDim = dim3(kFewThreads);
   cfg.dynamicSmemBytes = p.smem;
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = p.splits > 1 ? 1 : 0;
+  cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, wm, um, g);
 }
+
+// (all variants have the same threads and take a whole SM)
+int few_resident(int splits) { return resident_clusters(k_micro_few<BITSMOE_MICRO_E8M0, false, 1>, kFewThreads, splits); }
 
 template <int FMT, bool GLU>
 cudaError_t launch_few_nt(const FewPlan& p, const bitsmoe_microscale* w, const bitsmoe_microscale* up, const FewArgs& g, cudaStream_t st) {
@@ -1187,7 +1285,7 @@ extern "C" int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bit
   if (e != cudaSuccess) return record_cuda_error((int)e);
   const bool e8 = w->format == BITSMOE_MICRO_E8M0;
   FewPlan fp;
-  if (few_plan(w->format, up != nullptr, T, w->rows, w->cols, sms, &fp)) {
+  if (few_plan(w->format, up != nullptr, T, w->rows, w->cols, few_resident, &fp)) {
     FewArgs f;
     std::memset(&f, 0, sizeof(f));
     f.T = T;

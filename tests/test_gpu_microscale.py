@@ -374,3 +374,31 @@ def test_product_on_streams_in_graphs_and_again(env, coded):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, ref[i])
+
+
+@pytest.mark.parametrize("case", ["few", "few_split", "coded", "coded_split", "wide", "wide_split", "wide_swiglu"])
+def test_product_reports_a_wait_that_ran_out(env, case):
+    """A block that never reports a slot of its ring free (testing hook): the bounded waits run out, the status word
+    says so, and the next call is right.  Every case has more stages than its ring."""
+    torch, bm = env
+    rng = np.random.default_rng(6)
+    T = {"few": 3, "few_split": 2}.get(case, 40)
+    rows, cols = {"few": (152 * 128, 8192), "few_split": (130, 65536), "coded": (152 * 128, 8192), "coded_split": (130, 65536),
+                  "wide": (152 * 128, 2048), "wide_split": (130, 16384), "wide_swiglu": (152 * 128, 1024)}[case]
+    w = bm.microscale_quantize(torch.randn(rows, cols, device="cuda"), "e4m3", 1.0)
+    x = bf16(rng.standard_normal((T, cols))).cuda()
+    if case.startswith("coded"):
+        x = bm.microscale_quantize(x, "e4m3", 1.0)
+    up = w if case.endswith("swiglu") else None
+    ref = bm.microscale_product(w, x, up=up)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    bm.bitsmoe_debug_wait_limit(1, 2_000_000)
+    try:
+        bm.microscale_product(w, x, up=up, status=status)
+        torch.cuda.synchronize()
+    finally:
+        bm.bitsmoe_debug_wait_limit(0, 0)
+    assert int(status.item()) == bm.ERR_CODE["TIMEOUT"]
+    status.zero_()
+    assert torch.equal(bm.microscale_product(w, x, up=up, status=status), ref)
+    assert int(status.item()) == 0
