@@ -560,21 +560,24 @@ def _dense_type(where: str, name: str, dtype) -> int:
 
 def _rows(where: str, name: str, x, rows=None, cols=None, device=None, dtype=None):
     """Checks of a 2-d device tensor whose rows are dense (the pitch between them is free); its pitch."""
-    if x.dim() != 2 or not x.is_cuda:
+    shape = x.shape
+    if len(shape) != 2 or not x.is_cuda:
         _refuse(where, f"{name} must be a 2-d CUDA tensor")
     if device is not None and x.device != device:
         _refuse(where, f"{name} is on {x.device}, expected {device}")
-    if (rows is not None and x.shape[0] != rows) or (cols is not None and x.shape[1] != cols):
-        _refuse(where, f"{name} has shape {tuple(x.shape)}, expected {(rows, cols)}", "SHAPE")
+    r, c = shape
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        _refuse(where, f"{name} has shape {tuple(shape)}, expected {(rows, cols)}", "SHAPE")
     if dtype is not None and x.dtype != dtype:
         _refuse(where, f"{name} must be {dtype}, got {x.dtype}")
-    if x.shape[1] > 1 and x.shape[0] > 0 and x.stride(1) != 1:
+    ld, step = x.stride()
+    if step != 1 and c > 1 and r > 0:
         _refuse(where, f"{name} must have dense rows (stride 1 along them)")
-    if x.shape[0] <= 1:
-        return max(int(x.shape[1]), 1)
-    if x.stride(0) < x.shape[1]:
-        _refuse(where, f"{name}'s rows overlap (stride {x.stride(0)})")
-    return int(x.stride(0))
+    if r <= 1:
+        return c if c > 0 else 1
+    if ld < c:
+        _refuse(where, f"{name}'s rows overlap (stride {ld})")
+    return ld
 
 
 def _vector(where: str, name: str, v, n: int, device, dtype=None):
@@ -594,28 +597,51 @@ class Microscale:
     `scales` (uint8, the stored tile order), see bitsmoe_microscale in include/bitsmoe.h; `fmt` is
     "e8m0" (blocks of 32 columns) or "e4m3" (16), `scale` the tensor scale."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "fmt", "scale")
+    __slots__ = ("_codes", "_scales", "_buf", "_ptrs", "device", "rows", "cols", "fmt", "scale")
 
     def __init__(self, codes, scales, rows: int, cols: int, fmt: str = "e8m0", scale: float = 1.0):
         import torch
         if fmt not in MICRO_FORMATS:
             _refuse("Microscale", f"unknown format {fmt!r}")
-        nc, ns = microscale_bytes(fmt, rows, cols)
+        nc, ns = _micro_sizes(fmt, rows, cols)
+        if rows < 0 or cols < 1:
+            _refuse("Microscale", f"{rows} rows, {cols} columns")
         for name, t, n in (("codes", codes, nc), ("scales", scales, ns)):
-            if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() != n:
+            if t.dtype != torch.uint8 or t.numel() != n or not t.is_contiguous():
                 _refuse("Microscale", f"{name} must be {n} contiguous bytes (uint8)", "SHAPE")
         if codes.device != scales.device:
             _refuse("Microscale", "codes and scales are on different devices")
-        self.codes, self.scales = codes, scales
+        self._codes, self._scales, self._buf = codes, scales, None
+        self._ptrs, self.device = (codes.data_ptr(), scales.data_ptr()), codes.device
         self.rows, self.cols, self.fmt, self.scale = int(rows), int(cols), fmt, float(scale)
 
     @classmethod
     def empty(cls, rows: int, cols: int, fmt: str = "e8m0", scale: float = 1.0, device=None) -> "Microscale":
         import torch
-        nc, ns = microscale_bytes(fmt, rows, cols)
-        dev = device if device is not None else f"cuda:{torch.cuda.current_device()}"
-        return cls(torch.empty(nc, dtype=torch.uint8, device=dev), torch.empty(ns, dtype=torch.uint8, device=dev),
-                   rows, cols, fmt, scale)
+        nc, ns = _micro_sizes(fmt, rows, cols) if fmt in MICRO_FORMATS and rows >= 0 and cols > 0 else \
+            microscale_bytes(fmt, rows, cols)
+        self = cls.__new__(cls)   # one allocation for both; the tensors are made when asked for
+        at = (nc + 255) // 256 * 256
+        self._buf = torch.empty(at + ns, dtype=torch.uint8,
+                                device=device if device is not None else f"cuda:{torch.cuda.current_device()}")
+        self._codes = self._scales = None
+        base = self._buf.data_ptr()
+        self._ptrs, self.device = (base, base + at), self._buf.device
+        self.rows, self.cols, self.fmt, self.scale = int(rows), int(cols), fmt, float(scale)
+        return self
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            self._codes = self._buf[:_micro_sizes(self.fmt, self.rows, self.cols)[0]]
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            n = _micro_sizes(self.fmt, self.rows, self.cols)[1]
+            self._scales = self._buf[self._buf.numel() - n:]
+        return self._scales
 
     @classmethod
     def from_rows(cls, codes, block_scales, cols: int, fmt: str = "e8m0", scale: float = 1.0) -> "Microscale":
@@ -645,13 +671,13 @@ class Microscale:
         s = self.scales.view(rt, ct, 32, 4, 4).permute(0, 3, 2, 1, 4).reshape(rt * 128, ct * 4)
         return s[:self.rows, :nb]
 
-    @property
-    def device(self):
-        return self.codes.device
-
     def _struct(self) -> "_Microscale":
-        return _Microscale(MICRO_FORMATS[self.fmt], self.rows, self.cols, self.scale, self.codes.data_ptr(),
-                           self.scales.data_ptr())
+        return _Microscale(MICRO_FORMATS[self.fmt], self.rows, self.cols, self.scale, *self._ptrs)
+
+
+def _micro_sizes(fmt: str, rows: int, cols: int):
+    """The sizes that bitsmoe_microscale_bytes gives, of codes and scales."""
+    return rows * (-(-cols // 32) * 16), -(-rows // 128) * -(-(-(-cols // _MICRO_BLOCK[fmt])) // 4) * 512
 
 
 def microscale_bytes(fmt: str, rows: int, cols: int):
@@ -664,11 +690,18 @@ def microscale_bytes(fmt: str, rows: int, cols: int):
     return int(nc.value), int(ns.value)
 
 
-def _on(device, stream):
-    """Context with `device` current and its stream (the given one or the current one): outputs are
-    allocated on the stream that writes them."""
+def _launch(device, stream, call):
+    """call(raw stream) with `device` current, on the given stream or the device's current one: outputs that
+    the call allocates belong to the stream that writes them."""
     import torch
-    return torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device))
+    if stream is None and torch.cuda.current_device() == device.index:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the public way builds a Stream object (2 us)
+        return call(raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream)
+    with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)) as _:
+        st = torch.cuda.current_stream()
+        if st.device != device:
+            _refuse("stream", f"the stream is of {st.device}, the tensors are on {device}")
+        return call(st.cuda_stream)
 
 
 def microscale_quantize(x, fmt: str = "e8m0", scale: float = 1.0, out: Optional[Microscale] = None,
@@ -676,33 +709,38 @@ def microscale_quantize(x, fmt: str = "e8m0", scale: float = 1.0, out: Optional[
     """Quantise the rows of x (torch fp32 or bf16, 2-d, dense rows, on the device) into a Microscale with
     tensor scale `scale` (a power of two); `out` reuses an existing one of the same shape and format."""
     import torch
-    ty = _dense_type("microscale_quantize", "x", x.dtype)
-    ld = _rows("microscale_quantize", "x", x)
-    rows, cols = int(x.shape[0]), int(x.shape[1])
-    with _on(x.device, stream):
-        if out is None:
-            out = Microscale.empty(rows, cols, fmt, scale, x.device)
-        elif (out.rows, out.cols, out.fmt) != (rows, cols, fmt) or out.device != x.device:
-            _refuse("microscale_quantize", "out has another shape, format or device", "SHAPE")
-        out.scale = float(scale)
-        _check(_lib().bitsmoe_microscale_quantize(x.data_ptr(), ty, ld, out._struct(),
-                                                  torch.cuda.current_stream().cuda_stream),
-               "bitsmoe_microscale_quantize")
-    return out
+    where = "microscale_quantize"
+    ty = _dense_type(where, "x", x.dtype)
+    ld = _rows(where, "x", x)
+    rows, cols = x.shape
+
+    def call(st):
+        q = out
+        if q is None:
+            q = Microscale.empty(rows, cols, fmt, scale, x.device)
+        elif (q.rows, q.cols, q.fmt) != (rows, cols, fmt) or q.device != x.device:
+            _refuse(where, "out has another shape, format or device", "SHAPE")
+        q.scale = float(scale)
+        _check(_lib().bitsmoe_microscale_quantize(x.data_ptr(), ty, ld, q._struct(), st), "bitsmoe_microscale_quantize")
+        return q
+    return _launch(x.device, stream, call)
 
 
 def microscale_dequantize(q: Microscale, dtype=None, out=None, stream=None):
     """The values of a Microscale as a torch tensor rows x cols (float32, or bfloat16)."""
     import torch
-    with _on(q.device, stream):
-        if out is None:
-            out = torch.empty((q.rows, q.cols), dtype=dtype if dtype is not None else torch.float32, device=q.device)
-        ty = _dense_type("microscale_dequantize", "out", out.dtype)
-        ld = _rows("microscale_dequantize", "out", out, q.rows, q.cols, q.device)
-        _check(_lib().bitsmoe_microscale_dequantize(q._struct(), out.data_ptr(), ty, ld,
-                                                    torch.cuda.current_stream().cuda_stream),
-               "bitsmoe_microscale_dequantize")
-    return out
+    where = "microscale_dequantize"
+    dev = q.device
+
+    def call(st):
+        x = out
+        if x is None:
+            x = torch.empty((q.rows, q.cols), dtype=dtype if dtype is not None else torch.float32, device=dev)
+        ty = _dense_type(where, "out", x.dtype)
+        ld = _rows(where, "out", x, q.rows, q.cols, dev)
+        _check(_lib().bitsmoe_microscale_dequantize(q._struct(), x.data_ptr(), ty, ld, st), "bitsmoe_microscale_dequantize")
+        return x
+    return _launch(dev, stream, call)
 
 
 def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=None, y=None, status=None,
@@ -713,26 +751,29 @@ def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=
     import torch
     where = "microscale_product"
     coded = isinstance(x, Microscale)
-    if (x.device != w.device) or (up is not None and up.device != w.device):
+    dev = w.device
+    if x.device != dev or (up is not None and up.device != dev):
         _refuse(where, "the operands are on different devices")
     if coded:
         T, x_ptr, x_ld = x.rows, None, 0
     else:
-        x_ld = _rows(where, "x", x, None, w.cols, w.device, torch.bfloat16)
-        T, x_ptr = int(x.shape[0]), x.data_ptr()
-    if status is not None and (status.dtype != torch.int32 or status.numel() != 1 or status.device != w.device):
+        x_ld = _rows(where, "x", x, None, w.cols, dev, torch.bfloat16)
+        T, x_ptr = x.shape[0], x.data_ptr()
+    if status is not None and (status.dtype != torch.int32 or status.numel() != 1 or status.device != dev):
         _refuse(where, "status must be one int32 on the operands' device")
-    with _on(w.device, stream):
-        if y is None:
-            y = torch.empty((T, w.rows), dtype=dtype if dtype is not None else torch.float32, device=w.device)
-        ty = _dense_type(where, "y", y.dtype)
-        y_ld = _rows(where, "y", y, T, w.rows, w.device)
+
+    def call(st):
+        out = y
+        if out is None:
+            out = torch.empty((T, w.rows), dtype=dtype if dtype is not None else torch.float32, device=dev)
+        ty = _dense_type(where, "y", out.dtype)
+        y_ld = _rows(where, "y", out, T, w.rows, dev)
         _check(_lib().bitsmoe_microscale_product(w._struct(), up._struct() if up is not None else None, x_ptr, x_ld,
-                                                 x._struct() if coded else None, T, y.data_ptr(), ty, y_ld,
-                                                 status.data_ptr() if status is not None else None,
-                                                 torch.cuda.current_stream().cuda_stream),
+                                                 x._struct() if coded else None, T, out.data_ptr(), ty, y_ld,
+                                                 status.data_ptr() if status is not None else None, st),
                "bitsmoe_microscale_product")
-    return y
+        return out
+    return _launch(dev, stream, call)
 
 
 def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: float = 1e-6, gate=None,
@@ -748,49 +789,46 @@ def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: 
     given (h_out may be h: in place); pre_norm False returns x None."""
     import torch
     where = "block_norm"
-    a = _BlockNormArgs()
-    a.h_type, a.h_ld = _dense_type(where, "h", h.dtype), _rows(where, "h", h)
-    T, D, dev = int(h.shape[0]), int(h.shape[1]), h.device
-    a.T, a.D, a.h = T, D, h.data_ptr()
+    dev = h.device
+    h_type, h_ld = _dense_type(where, "h", h.dtype), _rows(where, "h", h)
+    T, D = h.shape
+    y_type = y_ld = gate_type = gate_kind = gate_ld = 0
+    y_ptr = gate_ptr = None
     if y is not None:
-        a.y_type, a.y_ld = _dense_type(where, "y", y.dtype), _rows(where, "y", y, T, D, dev)
-        a.y = y.data_ptr()
+        y_type, y_ld, y_ptr = _dense_type(where, "y", y.dtype), _rows(where, "y", y, T, D, dev), y.data_ptr()
     if gate is not None:
-        a.gate_type = _dense_type(where, "gate", gate.dtype)
+        gate_type, gate_ptr = _dense_type(where, "gate", gate.dtype), gate.data_ptr()
         if gate.dim() == 1:
             if gate.shape[0] != T or gate.device != dev:
                 _refuse(where, f"gate has shape {tuple(gate.shape)} on {gate.device}, expected {(T,)} on {dev}", "SHAPE")
-            a.gate_kind, a.gate_ld = _GATE_TOKEN, max(int(gate.stride(0)), 1)
+            gate_kind, gate_ld = _GATE_TOKEN, max(gate.stride(0), 1)
             if T > 1 and gate.stride(0) < 1:
                 _refuse(where, "gate's elements overlap")
         else:
-            a.gate_kind, a.gate_ld = _GATE_ELEMENT, _rows(where, "gate", gate, T, D, dev)
-        a.gate = gate.data_ptr()
-    vecs = [v for v in (post_gain, pre_gain, channel_scale) if v is not None]
-    gt = vecs[0].dtype if vecs else torch.float32
-    a.gain_type = _dense_type(where, "gains", gt)
-    a.post_gain = _vector(where, "post_gain", post_gain, D, dev, gt)
-    a.pre_gain = _vector(where, "pre_gain", pre_gain, D, dev, gt)
-    a.channel_scale = _vector(where, "channel_scale", channel_scale, D, dev, gt)
-    a.post_norm, a.gate_sigmoid = int(bool(post_norm)), int(bool(gate_sigmoid))
-    a.post_eps, a.pre_eps, a.gain_offset = post_eps, pre_eps, gain_offset
-    a.residual_scale, a.branch_scale = residual_scale, branch_scale
-    with _on(dev, stream):
-        if h_out is None and y is not None:
-            h_out = torch.empty((T, D), dtype=h.dtype, device=dev)
-        if h_out is not None:
-            a.h_out_ld = _rows(where, "h_out", h_out, T, D, dev, h.dtype)
-            a.h_out = h_out.data_ptr()
-        if x is None and pre_norm:
-            x = torch.empty((T, D), dtype=x_dtype if x_dtype is not None else torch.bfloat16, device=dev)
-        if x is not None:
-            if not pre_norm:
-                _refuse(where, "x is given but pre_norm is off")
-            a.x_type, a.x_ld = _dense_type(where, "x", x.dtype), _rows(where, "x", x, T, D, dev)
-            a.x = x.data_ptr()
-        _check(_lib().bitsmoe_block_norm(ctypes.byref(a), torch.cuda.current_stream().cuda_stream),
-               "bitsmoe_block_norm")
-    return h_out, x
+            gate_kind, gate_ld = _GATE_ELEMENT, _rows(where, "gate", gate, T, D, dev)
+    gt = next((v.dtype for v in (post_gain, pre_gain, channel_scale) if v is not None), torch.float32)
+    gain_type = _dense_type(where, "gains", gt)
+    vec = [_vector(where, n, v, D, dev, gt)
+           for n, v in (("post_gain", post_gain), ("pre_gain", pre_gain), ("channel_scale", channel_scale))]
+    if x is not None and not pre_norm:
+        _refuse(where, "x is given but pre_norm is off")
+
+    def call(st):
+        ho, xo = h_out, x
+        if ho is None and y is not None:
+            ho = torch.empty((T, D), dtype=h.dtype, device=dev)
+        if xo is None and pre_norm:
+            xo = torch.empty((T, D), dtype=x_dtype if x_dtype is not None else torch.bfloat16, device=dev)
+        ho_ld = _rows(where, "h_out", ho, T, D, dev, h.dtype) if ho is not None else 0
+        x_type, x_ld = (_dense_type(where, "x", xo.dtype), _rows(where, "x", xo, T, D, dev)) if xo is not None else (0, 0)
+        a = _BlockNormArgs(T, D, h_type, y_type, gate_type, gain_type, x_type, 1 if post_norm else 0, gate_kind,
+                           1 if gate_sigmoid else 0, post_eps, pre_eps, gain_offset, residual_scale, branch_scale,
+                           h.data_ptr(), y_ptr, gate_ptr, vec[0], vec[1], vec[2],
+                           ho.data_ptr() if ho is not None else None, xo.data_ptr() if xo is not None else None,
+                           h_ld, y_ld, gate_ld, ho_ld, x_ld)
+        _check(_lib().bitsmoe_block_norm(ctypes.byref(a), st), "bitsmoe_block_norm")
+        return ho, xo
+    return _launch(dev, stream, call)
 
 
 def bitsmoe_debug_single_token_kernel(which: int) -> None:

@@ -6,6 +6,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "device.cuh"
@@ -22,40 +23,435 @@ __device__ __forceinline__ void store1(void* p, int type, int64_t i, float v) {
   else static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
 }
 
-constexpr int kBThreads = 256;
+// ---------------------------------------------------------------------------
+// A row per group of threads (a warp for rows of up to 256, else a block), the whole
+// row in registers: the block's output, its gate and the residual are requested
+// together and read once.  Two sums over the group (of the output's and of h's
+// squares) are all that it waits for.  VEC elements a load: 8 where every row starts
+// on a 16-byte boundary, 2 or 1 otherwise.  DRAM bounds it from some thousand rows on:
+// 16384 rows of 4096 (fp32, post- and pre-norm) 165 us, 5.7 TB/s; with the rows
+// requested into registers instead of the ring of k_block_norm_rows 198 us, without
+// requesting ahead 259 us.  One row of 2048: 2.8 us.
+// ---------------------------------------------------------------------------
+template <int VEC>
+struct Raw {          // VEC elements as they are stored: fp32 in w[0 .. VEC), bf16 in w[0 .. (VEC + 1) / 2)
+  uint32_t w[VEC];
+};
 
+template <int VEC>
+__device__ __forceinline__ Raw<VEC> load_raw(const void* p, int type, int64_t i) {
+  Raw<VEC> r;
+  if (type == BITSMOE_F32) {
+    const float* q = static_cast<const float*>(p) + i;
+    if constexpr (VEC == 8) {
+      const uint4 a = __ldg(reinterpret_cast<const uint4*>(q)), b = __ldg(reinterpret_cast<const uint4*>(q) + 1);
+      r.w[0] = a.x, r.w[1] = a.y, r.w[2] = a.z, r.w[3] = a.w, r.w[4] = b.x, r.w[5] = b.y, r.w[6] = b.z, r.w[7] = b.w;
+    } else if constexpr (VEC == 2) {
+      const uint2 a = __ldg(reinterpret_cast<const uint2*>(q));
+      r.w[0] = a.x, r.w[1] = a.y;
+    } else {
+      r.w[0] = __ldg(reinterpret_cast<const uint32_t*>(q));
+    }
+  } else {
+    const uint16_t* q = static_cast<const uint16_t*>(p) + i;
+    if constexpr (VEC == 8) {
+      const uint4 a = __ldg(reinterpret_cast<const uint4*>(q));
+      r.w[0] = a.x, r.w[1] = a.y, r.w[2] = a.z, r.w[3] = a.w;
+    } else if constexpr (VEC == 2) {
+      r.w[0] = __ldg(reinterpret_cast<const uint32_t*>(q));
+    } else {
+      r.w[0] = __ldg(q);
+    }
+  }
+  return r;
+}
+// The same of memory that this kernel writes (h, where h_out is h).
+template <int VEC>
+__device__ __forceinline__ Raw<VEC> load_own(const void* p, int type, int64_t i) {
+  Raw<VEC> r;
+  if (type == BITSMOE_F32) {
+    const float* q = static_cast<const float*>(p) + i;
+    if constexpr (VEC == 8) {
+      const uint4 a = __ldcs(reinterpret_cast<const uint4*>(q)), b = __ldcs(reinterpret_cast<const uint4*>(q) + 1);
+      r.w[0] = a.x, r.w[1] = a.y, r.w[2] = a.z, r.w[3] = a.w, r.w[4] = b.x, r.w[5] = b.y, r.w[6] = b.z, r.w[7] = b.w;
+    } else if constexpr (VEC == 2) {
+      const uint2 a = __ldcs(reinterpret_cast<const uint2*>(q));
+      r.w[0] = a.x, r.w[1] = a.y;
+    } else {
+      r.w[0] = __ldcs(reinterpret_cast<const uint32_t*>(q));
+    }
+  } else {
+    const uint16_t* q = static_cast<const uint16_t*>(p) + i;
+    if constexpr (VEC == 8) {
+      const uint4 a = __ldcs(reinterpret_cast<const uint4*>(q));
+      r.w[0] = a.x, r.w[1] = a.y, r.w[2] = a.z, r.w[3] = a.w;
+    } else if constexpr (VEC == 2) {
+      r.w[0] = __ldcs(reinterpret_cast<const uint32_t*>(q));
+    } else {
+      r.w[0] = __ldcs(q);
+    }
+  }
+  return r;
+}
+// Eight elements of a row in shared memory (filled by a bulk copy).
+__device__ __forceinline__ Raw<8> load_shared(const uint8_t* p, int type, int i) {
+  Raw<8> r;
+  const uint4 a = lds128(p + (type == BITSMOE_F32 ? 4 : 2) * i);
+  r.w[0] = a.x, r.w[1] = a.y, r.w[2] = a.z, r.w[3] = a.w;
+  if (type == BITSMOE_F32) {
+    const uint4 b = lds128(p + 4 * i + 16);
+    r.w[4] = b.x, r.w[5] = b.y, r.w[6] = b.z, r.w[7] = b.w;
+  }
+  return r;
+}
+template <int VEC>
+__device__ __forceinline__ void unpack(const Raw<VEC>& r, int type, float (&v)[VEC]) {
+  if (type == BITSMOE_F32) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = __uint_as_float(r.w[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = e & 1 ? bf16hi(r.w[e / 2]) : bf16lo(r.w[e / 2]);
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void store_vec(void* p, int type, int64_t i, const float (&v)[VEC]) {
+  if (type == BITSMOE_F32) {
+    float* q = static_cast<float*>(p) + i;
+    if constexpr (VEC == 8) {
+      __stcs(reinterpret_cast<float4*>(q), make_float4(v[0], v[1], v[2], v[3]));
+      __stcs(reinterpret_cast<float4*>(q) + 1, make_float4(v[4], v[5], v[6], v[7]));
+    } else if constexpr (VEC == 2) {
+      *reinterpret_cast<float2*>(q) = make_float2(v[0], v[1]);
+    } else {
+      *q = v[0];
+    }
+  } else {
+    uint16_t* q = static_cast<uint16_t*>(p) + i;
+    if constexpr (VEC == 1) {
+      *q = __bfloat16_as_ushort(__float2bfloat16_rn(v[0]));
+    } else {
+      uint32_t h[VEC / 2];
+#pragma unroll
+      for (int e = 0; e < VEC / 2; ++e) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+        h[e] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+      if constexpr (VEC == 8) *reinterpret_cast<uint4*>(q) = make_uint4(h[0], h[1], h[2], h[3]);
+      else *reinterpret_cast<uint32_t*>(q) = h[0];
+    }
+  }
+}
+
+constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32;
+
+// Sum over a block of at most 16 warps, in one order whatever their number; `red` holds zeros past them
+// and is this sum's own buffer (the two sums of a row take turns).
 __device__ __forceinline__ float block_sum(float v, float* red) {
   v = warp_sum(v);
-  __syncthreads();   // the previous sum has been read
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
   __syncthreads();
   float s = 0.f;
 #pragma unroll
-  for (int w = 0; w < kBThreads / 32; ++w) s += red[w];
+  for (int q = 0; q < kRowWarps / 4; ++q) {
+    const float4 p = reinterpret_cast<const float4*>(red)[q];
+    s += (p.x + p.y) + (p.z + p.w);
+  }
   return s;
 }
 
-// One block per row; the row's h' stays in shared memory between the two norms.
-__global__ void __launch_bounds__(kBThreads) k_block_norm(bitsmoe_block_norm_args a) {
+__device__ __forceinline__ float sigmoid(float v) { return 1.f / (1.f + expf(-v)); }
+
+// What multiplies a normalised output: branch_scale * channel_scale * (offset + post_gain).
+template <int VEC>
+__device__ __forceinline__ void branch_factor(const bitsmoe_block_norm_args& a, const Raw<VEC>& post, const Raw<VEC>& chan, float (&c)[VEC]) {
+  float v[VEC];
+#pragma unroll
+  for (int q = 0; q < VEC; ++q) c[q] = a.branch_scale;
+  if (a.channel_scale) {
+    unpack<VEC>(chan, a.gain_type, v);
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) c[q] *= v[q];
+  }
+  if (a.post_gain) {
+    unpack<VEC>(post, a.gain_type, v);
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) c[q] *= a.gain_offset + v[q];
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void pre_factor(const bitsmoe_block_norm_args& a, const Raw<VEC>& pre, float (&c)[VEC]) {
+#pragma unroll
+  for (int q = 0; q < VEC; ++q) c[q] = 1.f;
+  if (a.pre_gain) {
+    unpack<VEC>(pre, a.gain_type, c);
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) c[q] += a.gain_offset;
+  }
+}
+
+// Threads at VEC * (k * group + i) hold vector k of a row; k < NV.  ONE: every group has one row, and latency
+// counts: the gains are requested with it.  Otherwise the next row is requested before this one's second sum
+// and the gains are read where they are used (they stay in L1).
+template <int VEC, int NV, bool WARP, bool ONE>
+__global__ void __launch_bounds__(WARP ? 128 : kRowThreads, WARP ? 4 : NV * VEC > 8 ? 1 : 2)
+    k_block_norm(const __grid_constant__ bitsmoe_block_norm_args a) {
+  __shared__ __align__(16) float red[2][kRowWarps];
+  const int gsize = WARP ? 32 : blockDim.x, gi = WARP ? (threadIdx.x & 31) : threadIdx.x;
+  const int64_t step = gridDim.x;
+  int64_t t = WARP ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+  if (t >= a.T) return;   // (whole groups)
+  if (!WARP && threadIdx.x < 2 * kRowWarps) red[threadIdx.x / kRowWarps][threadIdx.x % kRowWarps] = 0.f;
+  const auto sum = [&](float v, int which) { return WARP ? warp_sum(v) : block_sum(v, red[which]); };
+  int at[NV];
+  bool in[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    at[k] = (k * gsize + gi) * VEC;
+    in[k] = at[k] < a.D;   // a vector lies inside the row or outside: D is a multiple of VEC
+  }
+  const bool elem = a.gate_kind == BITSMOE_GATE_ELEMENT;
+  constexpr bool kGate = NV * VEC <= 16;
+  Raw<VEC> y[NV], h[NV], e[NV], post[NV], pre[NV], chan[NV];
+  float tg = 1.f;
+  const auto request = [&](int64_t row) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (in[k]) {
+        if (a.y) y[k] = load_raw<VEC>(a.y, a.y_type, row * a.y_ld + at[k]);
+        h[k] = load_own<VEC>(a.h, a.h_type, row * a.h_ld + at[k]);
+        if (elem && kGate) e[k] = load_raw<VEC>(a.gate, a.gate_type, row * a.gate_ld + at[k]);
+      }
+    if (a.gate_kind == BITSMOE_GATE_TOKEN) tg = load1(a.gate, a.gate_type, row * a.gate_ld);
+  };
+  const auto gain = [&](Raw<VEC>& r, const void* p, int k) {
+    if (p && in[k]) r = load_raw<VEC>(p, a.gain_type, at[k]);
+  };
+  constexpr bool kEarly = ONE && NV * VEC <= 16, kNext = !ONE && NV * VEC <= 8;   // what the registers hold
+  request(t);
+  if (!WARP) __syncthreads();   // red is cleared
+  const float inv_d = 1.f / (float)a.D;
+  for (; t < a.T; t += step) {
+    float inv = 1.f;
+    float v[NV][VEC], c[VEC];
+    if (kEarly)
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        gain(post[k], a.post_gain, k);
+        gain(chan[k], a.channel_scale, k);
+        gain(pre[k], a.pre_gain, k);
+      }
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int q = 0; q < VEC; ++q) v[k][q] = 0.f;
+    if (a.y) {
+      float ss = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (in[k]) {
+          unpack<VEC>(y[k], a.y_type, v[k]);
+#pragma unroll
+          for (int q = 0; q < VEC; ++q) ss = fmaf(v[k][q], v[k][q], ss);
+        }
+      if (a.post_norm) inv = rsqrtf(sum(ss, 0) * inv_d + a.post_eps);
+    }
+    const float g = a.gate_kind == BITSMOE_GATE_TOKEN && a.gate_sigmoid ? sigmoid(tg) : tg;
+    float ss = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (in[k]) {
+        if (a.y) {
+          if (!kEarly) {
+            gain(post[k], a.post_gain, k);
+            gain(chan[k], a.channel_scale, k);
+          }
+          branch_factor<VEC>(a, post[k], chan[k], c);
+#pragma unroll
+          for (int q = 0; q < VEC; ++q) v[k][q] = v[k][q] * inv * c[q];
+          if (elem) {
+            if (!kGate) e[k] = load_raw<VEC>(a.gate, a.gate_type, t * a.gate_ld + at[k]);
+            unpack<VEC>(e[k], a.gate_type, c);
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) v[k][q] *= a.gate_sigmoid ? sigmoid(c[q]) : c[q];
+          } else if (a.gate_kind) {
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) v[k][q] *= g;
+          }
+        }
+        unpack<VEC>(h[k], a.h_type, c);
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) {
+          v[k][q] = fmaf(a.residual_scale, c[q], v[k][q]);
+          ss = fmaf(v[k][q], v[k][q], ss);
+        }
+      }
+    if (kNext && t + step < a.T) request(t + step);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (in[k] && a.h_out) store_vec<VEC>(a.h_out, a.h_type, t * a.h_out_ld + at[k], v[k]);
+    if (a.x) {
+      inv = rsqrtf(sum(ss, 1) * inv_d + a.pre_eps);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (in[k]) {
+          if (!kEarly) gain(pre[k], a.pre_gain, k);
+          pre_factor<VEC>(a, pre[k], c);
+#pragma unroll
+          for (int q = 0; q < VEC; ++q) v[k][q] = v[k][q] * inv * c[q];
+          store_vec<VEC>(a.x, a.x_type, t * a.x_ld + at[k], v[k]);
+        }
+    }
+    if (ONE) return;
+    if (!kNext && t + step < a.T) request(t + step);
+    if (!(a.y && a.post_norm && a.x)) __syncthreads();   // one sum a row: its buffer is read before the next row's
+  }
+}
+
+// Many rows on 16-byte boundaries: blocks that stay, whose rows come ahead by bulk copies into a ring of slots in
+// shared memory; the factors of a thread's columns stay in its registers.  The same operations in the same order as
+// above, so a row's result does not depend on how many there are.
+constexpr int kMaxSlots = 8;
+
+template <int NV, int HT, int YT>
+__global__ void __launch_bounds__(kRowThreads, NV == 1 ? 2 : 1)
+    k_block_norm_rows(const __grid_constant__ bitsmoe_block_norm_args a, int slots) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ __align__(16) float red[2][kRowWarps];
+  __shared__ uint64_t full[kMaxSlots];
+  constexpr uint32_t hs = HT == BITSMOE_F32 ? 4 : 2, ys = YT == BITSMOE_F32 ? 4 : 2;
+  const uint32_t es = a.gate_type == BITSMOE_F32 ? 4 : 2;
+  const bool elem = a.gate_kind == BITSMOE_GATE_ELEMENT;
+  const uint32_t yb = a.y ? a.D * ys : 0u, hb = a.D * hs, eb = elem ? a.D * es : 0u;   // a slot: y's row, h's, the gate's
+  if (threadIdx.x < 2 * kRowWarps) red[threadIdx.x / kRowWarps][threadIdx.x % kRowWarps] = 0.f;
+  const auto fill = [&](int slot, int64_t row) {   // by one thread
+    uint8_t* dst = ring + (size_t)slot * (yb + hb + eb);
+    mbar_expect_tx(full + slot, yb + hb + eb);
+    if (yb) bulk_g2s(dst, static_cast<const uint8_t*>(a.y) + row * a.y_ld * ys, yb, full + slot);
+    bulk_g2s(dst + yb, static_cast<const uint8_t*>(a.h) + row * a.h_ld * hs, hb, full + slot);
+    if (eb) bulk_g2s(dst + yb + hb, static_cast<const uint8_t*>(a.gate) + row * a.gate_ld * es, eb, full + slot);
+  };
+  int64_t t = blockIdx.x;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < slots; ++i) mbar_init(full + i);
+    for (int i = 0; i < slots && t + (int64_t)i * gridDim.x < a.T; ++i) fill(i, t + (int64_t)i * gridDim.x);
+  }
+  int at[NV];
+  bool in[NV];
+  float cb[NV][8], cp[NV][8];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    at[k] = (k * blockDim.x + threadIdx.x) * 8;
+    in[k] = at[k] < a.D;
+    Raw<8> post, chan, pre;
+    if (in[k]) {
+      if (a.post_gain) post = load_raw<8>(a.post_gain, a.gain_type, at[k]);
+      if (a.channel_scale) chan = load_raw<8>(a.channel_scale, a.gain_type, at[k]);
+      if (a.pre_gain) pre = load_raw<8>(a.pre_gain, a.gain_type, at[k]);
+      branch_factor<8>(a, post, chan, cb[k]);
+      pre_factor<8>(a, pre, cp[k]);
+    }
+  }
+  __syncthreads();
+  const float inv_d = 1.f / (float)a.D;
+  int slot = 0, use = 0;
+  for (; t < a.T; t += gridDim.x) {
+    // (a wait that runs out reads the row from global memory)
+    const bool here = mbar_wait(full + slot, (uint32_t)use & 1u);
+    const uint8_t* src = ring + (size_t)slot * (yb + hb + eb);
+    float v[NV][8], c[8];
+    float inv = 1.f, g = 1.f;
+    if (a.gate_kind == BITSMOE_GATE_TOKEN) {
+      g = load1(a.gate, a.gate_type, t * a.gate_ld);
+      if (a.gate_sigmoid) g = sigmoid(g);
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[k][q] = 0.f;
+    if (a.y) {
+      float ss = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (in[k]) {
+          unpack<8>(here ? load_shared(src, YT, at[k]) : load_raw<8>(a.y, YT, t * a.y_ld + at[k]), YT, v[k]);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) ss = fmaf(v[k][q], v[k][q], ss);
+        }
+      if (a.post_norm) inv = rsqrtf(block_sum(ss, red[0]) * inv_d + a.post_eps);
+    }
+    float ss = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (in[k]) {
+        if (a.y) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[k][q] = v[k][q] * inv * cb[k][q];
+          if (elem) {
+            unpack<8>(here ? load_shared(src + yb + hb, a.gate_type, at[k]) : load_raw<8>(a.gate, a.gate_type, t * a.gate_ld + at[k]),
+                      a.gate_type, c);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[k][q] *= a.gate_sigmoid ? sigmoid(c[q]) : c[q];
+          } else if (a.gate_kind) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[k][q] *= g;
+          }
+        }
+        unpack<8>(here ? load_shared(src + yb, HT, at[k]) : load_own<8>(a.h, HT, t * a.h_ld + at[k]), HT, c);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          v[k][q] = fmaf(a.residual_scale, c[q], v[k][q]);
+          ss = fmaf(v[k][q], v[k][q], ss);
+        }
+        if (a.h_out) store_vec<8>(a.h_out, HT, t * a.h_out_ld + at[k], v[k]);
+      }
+    if (a.x) inv = rsqrtf(block_sum(ss, red[1]) * inv_d + a.pre_eps);
+    if (!(a.y && a.post_norm && a.x)) __syncthreads();   // one sum a row: its buffer is read before the next row's
+    if (threadIdx.x == 0 && t + (int64_t)slots * gridDim.x < a.T) fill(slot, t + (int64_t)slots * gridDim.x);   // all have read it
+    if (++slot == slots) {
+      slot = 0;
+      ++use;
+    }
+    if (a.x) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (in[k]) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[k][q] = v[k][q] * inv * cp[k][q];
+          store_vec<8>(a.x, a.x_type, t * a.x_ld + at[k], v[k]);
+        }
+    }
+  }
+}
+
+// Wide rows that registers do not hold: one block per row, h' in shared memory between the two norms.
+constexpr int kWideThreads = 1024;
+__global__ void __launch_bounds__(kWideThreads) k_block_norm_wide(const __grid_constant__ bitsmoe_block_norm_args a) {
   extern __shared__ float row[];   // [D]
-  __shared__ float red[kBThreads / 32];
+  __shared__ float red[2][32];
+  const auto sum = [&](float v, float* r) {
+    v = warp_sum(v);
+    if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = v;
+    __syncthreads();
+    return warp_sum(r[threadIdx.x & 31]);
+  };
   const int64_t t = blockIdx.x;
   float inv = 1.f;
   if (a.y && a.post_norm) {
     float ss = 0.f;
-    for (int d = threadIdx.x; d < a.D; d += kBThreads) {
+    for (int d = threadIdx.x; d < a.D; d += kWideThreads) {
       const float v = load1(a.y, a.y_type, t * a.y_ld + d);
       ss = fmaf(v, v, ss);
     }
-    inv = rsqrtf(block_sum(ss, red) / (float)a.D + a.post_eps);
+    inv = rsqrtf(sum(ss, red[0]) / (float)a.D + a.post_eps);
   }
   float tg = 1.f;
   if (a.gate_kind == BITSMOE_GATE_TOKEN) {
     tg = load1(a.gate, a.gate_type, t * a.gate_ld);
-    if (a.gate_sigmoid) tg = 1.f / (1.f + expf(-tg));
+    if (a.gate_sigmoid) tg = sigmoid(tg);
   }
   float ss = 0.f;
-  for (int d = threadIdx.x; d < a.D; d += kBThreads) {
+  for (int d = threadIdx.x; d < a.D; d += kWideThreads) {
     float v = a.residual_scale * load1(a.h, a.h_type, t * a.h_ld + d);
     if (a.y) {
       float n = load1(a.y, a.y_type, t * a.y_ld + d);
@@ -63,7 +459,7 @@ __global__ void __launch_bounds__(kBThreads) k_block_norm(bitsmoe_block_norm_arg
       float g = tg;
       if (a.gate_kind == BITSMOE_GATE_ELEMENT) {
         g = load1(a.gate, a.gate_type, t * a.gate_ld + d);
-        if (a.gate_sigmoid) g = 1.f / (1.f + expf(-g));
+        if (a.gate_sigmoid) g = sigmoid(g);
       }
       if (a.gate_kind) n *= g;
       if (a.channel_scale) n *= load1(a.channel_scale, a.gain_type, d);
@@ -74,10 +470,60 @@ __global__ void __launch_bounds__(kBThreads) k_block_norm(bitsmoe_block_norm_arg
     ss = fmaf(v, v, ss);
   }
   if (!a.x) return;
-  inv = rsqrtf(block_sum(ss, red) / (float)a.D + a.pre_eps);
-  for (int d = threadIdx.x; d < a.D; d += kBThreads)
+  inv = rsqrtf(sum(ss, red[1]) / (float)a.D + a.pre_eps);
+  for (int d = threadIdx.x; d < a.D; d += kWideThreads)
     store1(a.x, a.x_type, t * a.x_ld + d,
            row[d] * inv * (a.pre_gain ? a.gain_offset + load1(a.pre_gain, a.gain_type, d) : 1.f));
+}
+
+// Rows can be read VEC elements at a time: D a multiple of it and every row on a boundary of their size (16 bytes at most).
+bool rows_of(const bitsmoe_block_norm_args& a, int vec) {
+  if (a.D % vec) return false;
+  const auto ok = [&](const void* p, int type, int64_t ld) {
+    if (!p) return true;
+    const int64_t size = type == BITSMOE_F32 ? 4 : 2, align = size * vec < 16 ? size * vec : 16;
+    return reinterpret_cast<uintptr_t>(p) % align == 0 && (a.T == 1 || ld * size % align == 0);
+  };
+  return ok(a.h, a.h_type, a.h_ld) && ok(a.y, a.y_type, a.y_ld) && ok(a.h_out, a.h_type, a.h_out_ld) && ok(a.x, a.x_type, a.x_ld) &&
+         ok(a.gate_kind == BITSMOE_GATE_ELEMENT ? a.gate : nullptr, a.gate_type, a.gate_ld) &&
+         ok(a.post_gain, a.gain_type, 0) && ok(a.pre_gain, a.gain_type, 0) && ok(a.channel_scale, a.gain_type, 0);
+}
+
+template <int VEC, int NV>
+cudaError_t launch_norm(const bitsmoe_block_norm_args& a, cudaStream_t st) {
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  const int nvec = a.D / VEC, threads = ((nvec + NV - 1) / NV + 31) / 32 * 32;
+  if constexpr (VEC * NV <= 8) {
+    if (threads == 32) {   // rows of up to 256: a warp a row, four rows a block
+      k_block_norm<VEC, NV, true, true><<<(unsigned)(((int64_t)a.T + 3) / 4), 128, 0, st>>>(a);
+      return cudaGetLastError();
+    }
+  }
+  // as many blocks as run at once (64 registers a thread: 1024 threads; 128 with more than 8 elements a thread)
+  const int per_sm = std::max(1, (VEC * NV > 8 ? 512 : 1024) / threads);
+  const int64_t full = (int64_t)sms * per_sm;
+  if (a.T <= full) {
+    k_block_norm<VEC, NV, false, true><<<(unsigned)a.T, threads, 0, st>>>(a);
+  } else if constexpr (VEC == 8) {
+    const auto size = [](int type) { return type == BITSMOE_F32 ? 4 : 2; };
+    const size_t row = (size_t)a.D * ((a.y ? size(a.y_type) : 0) + size(a.h_type) + (a.gate_kind == BITSMOE_GATE_ELEMENT ? size(a.gate_type) : 0));
+    const int slots = (int)std::min<size_t>(kMaxSlots, (size_t)(220 / per_sm - 2) * 1024 / row);   // >= 1: at most 12 x 16384 bytes
+    const bool hf = a.h_type == BITSMOE_F32, yf = a.y_type == BITSMOE_F32;
+    const auto run = [&](auto kern) {
+      const cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+      if (r == cudaSuccess) kern<<<(unsigned)full, threads, slots * row, st>>>(a, slots);
+      return r;
+    };
+    e = hf ? (yf ? run(k_block_norm_rows<NV, BITSMOE_F32, BITSMOE_F32>) : run(k_block_norm_rows<NV, BITSMOE_F32, BITSMOE_BF16>))
+           : (yf ? run(k_block_norm_rows<NV, BITSMOE_BF16, BITSMOE_F32>) : run(k_block_norm_rows<NV, BITSMOE_BF16, BITSMOE_BF16>));
+    if (e != cudaSuccess) return e;
+  } else {
+    k_block_norm<VEC, NV, false, false><<<(unsigned)full, threads, 0, st>>>(a);
+  }
+  return cudaGetLastError();
 }
 
 bool type_ok(int t) { return t == BITSMOE_F32 || t == BITSMOE_BF16; }
@@ -107,13 +553,22 @@ extern "C" int bitsmoe_block_norm(const bitsmoe_block_norm_args* args, void* str
       misaligned(a.post_gain, a.gain_type) || misaligned(a.pre_gain, a.gain_type) ||
       misaligned(a.channel_scale, a.gain_type) || misaligned(a.h_out, a.h_type) || misaligned(a.x, a.x_type))
     return BITSMOE_ERR_ALIGNMENT;
-  const size_t smem = (size_t)a.D * 4;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
-  if (smem > 40 * 1024)   // 48 KB with the static part need no opt-in
-    e = cudaFuncSetAttribute(k_block_norm, cudaFuncAttributeMaxDynamicSharedMemorySize, BITSMOE_BLOCK_NORM_MAX_D * 4);
-  if (e == cudaSuccess) {
-    k_block_norm<<<(unsigned)a.T, kBThreads, smem, static_cast<cudaStream_t>(stream)>>>(a);
-    e = cudaGetLastError();
+  if (a.D <= 16384 && rows_of(a, 8)) {
+    e = a.D <= 4096 ? launch_norm<8, 1>(a, st) : a.D <= 8192 ? launch_norm<8, 2>(a, st) : launch_norm<8, 4>(a, st);
+  } else if (a.D <= 4096 && rows_of(a, 2)) {
+    e = launch_norm<2, 4>(a, st);
+  } else if (a.D <= 4096) {
+    e = launch_norm<1, 8>(a, st);
+  } else {
+    const size_t smem = (size_t)a.D * 4;
+    if (smem > 40 * 1024)   // 48 KB with the static part need no opt-in
+      e = cudaFuncSetAttribute(k_block_norm_wide, cudaFuncAttributeMaxDynamicSharedMemorySize, BITSMOE_BLOCK_NORM_MAX_D * 4);
+    if (e == cudaSuccess) {
+      k_block_norm_wide<<<(unsigned)a.T, kWideThreads, smem, st>>>(a);
+      e = cudaGetLastError();
+    }
   }
   return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
 }
