@@ -542,9 +542,9 @@ extern "C" int bitsmoe_block_norm(const bitsmoe_block_norm_args* args, void* str
   if (!(a.post_eps >= 0.f) || !(a.pre_eps >= 0.f) || !std::isfinite(a.residual_scale) || !std::isfinite(a.branch_scale) ||
       !std::isfinite(a.gain_offset))
     return BITSMOE_ERR_INVALID_ARG;
+  if (a.T == 0) return BITSMOE_OK;   // (pointers of empty rows may be null)
   if ((!a.y && (a.post_norm || a.gate_kind || a.channel_scale)) || (a.post_gain && !a.post_norm)) return BITSMOE_ERR_INVALID_ARG;
   if (!a.x && a.pre_gain) return BITSMOE_ERR_INVALID_ARG;
-  if (a.T == 0) return BITSMOE_OK;
   if (!a.h || (!a.h_out && !a.x) || (a.gate_kind && !a.gate)) return BITSMOE_ERR_INVALID_ARG;
   if (a.h_ld < a.D || (a.y && a.y_ld < a.D) || (a.h_out && a.h_out_ld < a.D) || (a.x && a.x_ld < a.D) ||
       (a.gate_kind == BITSMOE_GATE_TOKEN && a.gate_ld < 1) || (a.gate_kind == BITSMOE_GATE_ELEMENT && a.gate_ld < a.D))

@@ -602,6 +602,19 @@ cudaError_t launch_few_nt(const FewPlan& p, const bitsmoe_microscale* w, const b
   return g.T > 8 ? launch_few<FMT, GLU, 2>(p, w, up, g, st) : launch_few<FMT, GLU, 1>(p, w, up, g, st);
 }
 
+// Sixteen tokens' results of weight row m (a lane's; the warp's lanes hold consecutive rows) from token t on.
+template <int NA>
+__device__ __forceinline__ void store_tokens(const uint32_t (&v)[NA][16], int t, int T, int m, float sw, float su, void* y,
+                                             int y_type, int64_t y_ld) {
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    if (t + q >= T) break;
+    float o = __uint_as_float(v[0][q]) * sw;
+    if (NA == 2) o = silu_mul(o, __uint_as_float(v[NA - 1][q]) * su);
+    store_y(y, y_type, (int64_t)(t + q) * y_ld + m, o);
+  }
+}
+
 // A CTA's share of the rows of a tile split over a cluster: the partial tiles red [NA][N][128] of the
 // cluster's CTAs added in rank order (all of an element's requested before the first is used), scaled, stored.
 template <int NA, int THREADS>
@@ -638,12 +651,13 @@ __device__ __forceinline__ void sum_splits(const float* red, int N, int splits, 
 // ---------------------------------------------------------------------------
 // Coded activations: both operands go to the tensor core as they are stored.
 // ---------------------------------------------------------------------------
-constexpr int kCodedThreads = 192;            // warp 0: copies, warp 1: MMA, warps 2-5: epilogue
+constexpr int kCodedThreads = 320;   // warp 0: copies, warp 1: scales and MMA, warps 2-9: epilogue
 
 struct CodedArgs {
   int T, rows, cols;
   int N;             // tokens of a tile: the MMA's N
-  int mt;            // 128-row tiles
+  int mt, ntiles;    // 128-row tiles, tiles in all
+  int nbuf;          // accumulators in tensor memory
   int nst, sps;      // stages of the whole product, of a split
   int splits;        // CTAs of a cluster, one per range of stages
   int stages;        // ring depth
@@ -661,148 +675,173 @@ struct CodedArgs {
   int* status;
 };
 
-// 128 weight rows x N tokens a CTA (with GLU 128 rows of both matrices).  Codes come by TMA, 256 columns a
-// stage, scale tiles by bulk copies; the MMA thread moves a stage's scales into tensor memory (columns of the
-// stage's own, so that the ring's barriers order their reuse) and issues the block-scaled products.  With few
-// tiles the columns are split over a cluster, whose CTAs add their partial tiles through distributed shared
-// memory in rank order.
-template <int FMT, bool GLU>
+// 128 weight rows x N tokens a CTA at a time (with GLU 128 rows of both matrices).  Codes come by TMA, 256 columns
+// a stage, scale tiles by bulk copies; the MMA warp moves a stage's scales into tensor memory (columns of the
+// stage's own, so that the ring's barriers order their reuse) and issues the block-scaled products.  It runs
+// converged, with one lane's predicate on the instructions, so that their operands stay in uniform registers, and
+// copies whole stages (scale tiles that the matrix does not have are what an earlier stage left: no product reads
+// them): with a loop of one lane over the tiles that exist, a copy of 512 bytes took 74 clocks.  CTAs stay for
+// all their tiles; the ring runs on while eight warps empty the accumulator.  With few tiles the columns are
+// split over a cluster, whose CTAs add their partial tiles through distributed shared memory in rank order.
+// G: groups of 128 tokens of a tile.
+template <int FMT, bool GLU, int G>
 __global__ void __launch_bounds__(kCodedThreads, 1)
     k_micro_coded(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap,
-                  const __grid_constant__ CUtensorMap xmap, CodedArgs g) {
+                  const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CodedArgs g) {
   constexpr bool E8 = FMT == BITSMOE_MICRO_E8M0;
   constexpr int NA = GLU ? 2 : 1;
   constexpr int CPS = E8 ? 2 : 4;   // scale tiles of a stage's 256 columns
+  constexpr uint32_t kSfCols = (NA + G) * CPS * 4;
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  const int S = g.stages, N = g.N, G = (N + 127) / 128;
+  const int S = g.stages, N = g.N;
   const uint32_t ring = (uint32_t)S * g.stage, redb = g.splits > 1 ? (uint32_t)(NA * N) * 512u : 0u;
-  float* red = reinterpret_cast<float*>(sm);   // [NA][N][128], reuses the ring once the MMAs are done
+  float* red = reinterpret_cast<float*>(sm);   // split: [NA][N][128], reuses the ring once the MMAs are done
   uint64_t* full = reinterpret_cast<uint64_t*>(sm + (ring > redb ? ring : redb));
   uint64_t* empty = full + S;
-  uint64_t* done = empty + S;
-  uint32_t* slot = reinterpret_cast<uint32_t*>(done + 1);
+  uint64_t* afull = empty + S;
+  uint64_t* aempty = afull + 2;
+  uint32_t* slot = reinterpret_cast<uint32_t*>(aempty + 2);
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int rank = blockIdx.y;
-  const int tile = blockIdx.x, mi = tile % g.mt, m0 = mi * 128, t0 = tile / g.mt * N;
   const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
-  const int nbg = min(G, (g.T + 127) / 128 - t0 / 128);
   const uint32_t b_bytes = (uint32_t)N * 128, sf_off = NA * kCodeTile + b_bytes;
-  const uint32_t sfa_cols = NA * CPS * 4, sf_cols = sfa_cols + (uint32_t)G * CPS * 4;
 
   if (tid == 0) {
+    prefetch_map(&wmap);
+    prefetch_map(&xmap);
+    if (GLU) prefetch_map(&umap);
     for (int i = 0; i < S; ++i) {
       mbar_init_n(full + i, 1);
       mbar_init_n(empty + i, 1);
     }
-    mbar_init_n(done, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init_n(afull + i, 1);
+      mbar_init_n(aempty + i, 8);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (wid == 1) tmem_alloc(slot, 512);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  const uint32_t tmem = *slot;
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, *slot, 0);
   bool ok = true;
 
   if (wid == 0) {
     if (lane == 0) {
-      int i = 0;
-      for (int st = 0, u = 0; i < nk; ++i) {
-        if (u > 0) ok = mbar_wait(empty + st, (uint32_t)(u - 1) & 1u, g.spin);
-        if (!ok) break;
-        const int kb = st0 + i, cnt = min(CPS, g.tiles - kb * CPS);
-        uint8_t* base = sm + (size_t)st * g.stage;
-        const uint32_t bar = smem_u32(full + st);
-        mbar_expect_tx(full + st, NA * kCodeTile + b_bytes + (uint32_t)(cnt * (NA + nbg)) * 512u);
-        tma_load_2d(smem_u32(base), &wmap, kb * 128, m0, bar);
-        if (GLU) tma_load_2d(smem_u32(base) + kCodeTile, &umap, kb * 128, m0, bar);
-        tma_load_2d(smem_u32(base) + NA * kCodeTile, &xmap, kb * 128, t0, bar);
-        uint8_t* sf = base + sf_off;
-        const size_t at = ((size_t)mi * g.tiles + (size_t)kb * CPS) * 512;
-        bulk_g2s(sf, g.ws + at, (uint32_t)cnt * 512u, full + st);
-        if (GLU) bulk_g2s(sf + CPS * 512, g.us + at, (uint32_t)cnt * 512u, full + st);
-        for (int j = 0; j < nbg; ++j)
-          bulk_g2s(sf + (NA + j) * CPS * 512, g.xs + ((size_t)(t0 / 128 + j) * g.tiles + (size_t)kb * CPS) * 512,
-                   (uint32_t)cnt * 512u, full + st);
-        if (++st == S) {
-          st = 0;
-          ++u;
+      int st = 0, u = 0, n = 0;
+      for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x) {
+        const int mi = tile % g.mt, t0 = tile / g.mt * N;
+        const int nbg = min(G, (g.T + 127) / 128 - t0 / 128);
+        for (int i = 0; i < nk; ++i, ++n) {
+          if (u > 0) ok = mbar_wait(empty + st, (uint32_t)(u - 1) & 1u, g.spin);
+          if (!ok) break;
+          const int kb = st0 + i, cnt = min(CPS, g.tiles - kb * CPS);
+          uint8_t* base = sm + (size_t)st * g.stage;
+          const uint32_t bar = smem_u32(full + st);
+          mbar_expect_tx(full + st, NA * kCodeTile + b_bytes + (uint32_t)(cnt * (NA + nbg)) * 512u);
+          tma_load_2d(smem_u32(base), &wmap, kb * 128, mi * 128, bar);
+          if (GLU) tma_load_2d(smem_u32(base) + kCodeTile, &umap, kb * 128, mi * 128, bar);
+          tma_load_2d(smem_u32(base) + NA * kCodeTile, &xmap, kb * 128, t0, bar);
+          uint8_t* sf = base + sf_off;
+          const size_t at = ((size_t)mi * g.tiles + (size_t)kb * CPS) * 512;
+          bulk_g2s(sf, g.ws + at, (uint32_t)cnt * 512u, full + st);
+          if (GLU) bulk_g2s(sf + CPS * 512, g.us + at, (uint32_t)cnt * 512u, full + st);
+          for (int j = 0; j < nbg; ++j)
+            bulk_g2s(sf + (NA + j) * CPS * 512, g.xs + ((size_t)(t0 / 128 + j) * g.tiles + (size_t)kb * CPS) * 512,
+                     (uint32_t)cnt * 512u, full + st);
+          if (++st == S) {
+            st = 0;
+            ++u;
+          }
         }
       }
-      for (int j = max(0, i - S); j < i; ++j) mbar_wait(full + j % S, (uint32_t)(j / S) & 1u);   // copies in flight
+      for (int j = max(0, n - S); j < n; ++j) mbar_wait(full + j % S, (uint32_t)(j / S) & 1u);   // copies in flight
     }
     __syncwarp();
   } else if (wid == 1) {
-    if (lane == 0) {
-      const int nk64 = (g.cols + 63) / 64;
-      const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(sm) + NA * kCodeTile);
-      const uint32_t sstep = g.stage >> 4;
-      for (int i = 0, st = 0, u = 0; i < nk; ++i) {
+    const uint32_t one = elect_one();
+    const int nk64 = (g.cols + 63) / 64;
+    const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(sm) + NA * kCodeTile);
+    const uint64_t ds = scale_desc(smem_u32(sm) + sf_off);
+    const uint32_t sstep = g.stage >> 4, id0 = idesc_e2m1(N, E8, 0), id2 = idesc_e2m1(N, E8, 2);
+    const uint32_t sf0 = tmem + (uint32_t)(g.nbuf * NA * N);
+    int st = 0, u = 0, it = 0;
+    for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x, ++it) {
+      const int buf = it % g.nbuf, used = it / g.nbuf;
+      if (used > 0) ok = mbar_wait(aempty + buf, (uint32_t)(used - 1) & 1u, g.spin);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      const uint32_t acc = tmem + (uint32_t)(buf * NA * N);
+      for (int i = 0; i < nk; ++i) {
         ok = mbar_wait(full + st, (uint32_t)u & 1u, g.spin);
+        ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const int kb = st0 + i, cnt = min(CPS, g.tiles - kb * CPS);
-        const uint32_t sf = smem_u32(sm) + (uint32_t)st * g.stage + sf_off;
-        const uint32_t ta = tmem + (uint32_t)(NA * N) + (uint32_t)st * sf_cols, tb = ta + sfa_cols;
-        for (int q = 0; q < cnt; ++q) {
+        const uint64_t so = (uint64_t)((uint32_t)st * sstep);
+        const uint64_t a0 = da + so, b0 = db + so, s0 = ds + so;
+        const uint32_t ta = sf0 + (uint32_t)st * kSfCols, tb = ta + NA * CPS * 4;
 #pragma unroll
-          for (int a = 0; a < NA; ++a) tmem_copy_scales(ta + (uint32_t)(a * CPS + q) * 4, sf + (uint32_t)(a * CPS + q) * 512);
-          for (int j = 0; j < nbg; ++j)
-            tmem_copy_scales(tb + (uint32_t)(q * G + j) * 4, sf + (uint32_t)((NA + j) * CPS + q) * 512);
+        for (int q = 0; q < CPS; ++q) {
+#pragma unroll
+          for (int a = 0; a < NA; ++a) tmem_copy_scales(one, ta + (a * CPS + q) * 4, s0 + (a * CPS + q) * 32);
+#pragma unroll
+          for (int j = 0; j < G; ++j) tmem_copy_scales(one, tb + (q * G + j) * 4, s0 + ((NA + j) * CPS + q) * 32);
         }
-        const uint64_t a0 = da + (uint64_t)st * sstep, b0 = db + (uint64_t)st * sstep;
+        const int k64 = nk64 - (st0 + i) * 4;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          if (kb * 4 + k >= nk64) break;
+          if (k >= k64) break;
           const int q = E8 ? k >> 1 : k;
-          const uint32_t id = idesc_e2m1(N, E8, E8 ? (uint32_t)(k & 1) * 2u : 0u);
 #pragma unroll
           for (int a = 0; a < NA; ++a)
-            mma_e2m1<E8>(tmem + (uint32_t)(a * N), a0 + a * (kCodeTile >> 4) + 2 * k, b0 + 2 * k, id,
-                         ta + (uint32_t)(a * CPS + q) * 4, tb + (uint32_t)(q * G) * 4, (i | k) != 0);
+            mma_e2m1<E8>(one, acc + (uint32_t)(a * N), a0 + a * (kCodeTile >> 4) + 2 * k, b0 + 2 * k, E8 && (k & 1) ? id2 : id0,
+                         ta + (a * CPS + q) * 4, tb + (q * G) * 4, (uint32_t)(i | k));
         }
-        if (!(g.lose && i == 0 && (blockIdx.x | blockIdx.y) == 0)) mma_commit(empty + st);
+        if (!(g.lose && i == 0 && it == 0 && (blockIdx.x | blockIdx.y) == 0)) mma_commit(one, empty + st);
         if (++st == S) {
           st = 0;
           ++u;
         }
       }
-      mma_commit(done);
+      mma_commit(one, afull + buf);
     }
-    __syncwarp();
   } else {
-    if (lane == 0) ok = mbar_wait(done, 0, g.spin);
-    __syncwarp();
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const int r = 32 * (wid & 3) + lane;
-    const uint32_t tl = tmem + ((uint32_t)(32 * (wid & 3)) << 16);
-    for (int c0 = 0; c0 < N; c0 += 16) {
-      uint32_t v[NA][16];
+    const int r = 32 * (wid & 3) + lane, half = (wid - 2) >> 2;
+    const int nh = (N / 16 + 1) / 2 * 16;   // columns of the first half
+    int it = 0;
+    for (int tile = blockIdx.x; tile < g.ntiles; tile += gridDim.x, ++it) {
+      const int buf = it % g.nbuf, used = it / g.nbuf;
+      if (lane == 0) ok = mbar_wait(afull + buf, (uint32_t)used & 1u, g.spin);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const int m = tile % g.mt * 128 + r, t0 = tile / g.mt * N;
+      const uint32_t tl = tmem + ((uint32_t)(32 * (wid & 3)) << 16) + (uint32_t)(buf * NA * N);
+      for (int c0 = half ? nh : 0; c0 < (half ? N : nh); c0 += 16) {
+        uint32_t v[NA][16];
 #pragma unroll
-      for (int a = 0; a < NA; ++a) {
-        if (nk > 0) {
-          tmem_ld16(tl + (uint32_t)(a * N + c0), v[a]);
-        } else {
+        for (int a = 0; a < NA; ++a) {
+          if (nk > 0) {
+            tmem_ld16(tl + (uint32_t)(a * N + c0), v[a]);
+          } else {
 #pragma unroll
-          for (int q = 0; q < 16; ++q) v[a][q] = 0u;
+            for (int q = 0; q < 16; ++q) v[a][q] = 0u;
+          }
+        }
+        if (g.splits > 1) {
+#pragma unroll
+          for (int a = 0; a < NA; ++a)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) red[(size_t)(a * N + c0 + q) * 128 + r] = __uint_as_float(v[a][q]);
+        } else if (m < g.rows) {
+          store_tokens<NA>(v, t0 + c0, g.T, m, g.sw, g.su, g.y, g.y_type, g.y_ld);
         }
       }
-      if (g.splits > 1) {
-#pragma unroll
-        for (int a = 0; a < NA; ++a)
-#pragma unroll
-          for (int q = 0; q < 16; ++q) red[(size_t)(a * N + c0 + q) * 128 + r] = __uint_as_float(v[a][q]);
-      } else if (m0 + r < g.rows) {
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          const int t = t0 + c0 + q;
-          if (t >= g.T) break;
-          float o = __uint_as_float(v[0][q]) * g.sw;
-          if (GLU) o = silu_mul(o, __uint_as_float(v[NA - 1][q]) * g.su);
-          store_y(g.y, g.y_type, (int64_t)t * g.y_ld + m0 + r, o);
-        }
-      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(aempty + buf);
     }
   }
   __syncwarp();
@@ -811,7 +850,8 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
     // every CTA of the cluster has its partial tile in shared memory; this CTA's share of the rows is summed
     asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-    sum_splits<NA, kCodedThreads>(red, N, g.splits, rank, m0, g.rows, t0, g.T, g.sw, g.su, g.y, g.y_type, g.y_ld);
+    const int tile = blockIdx.x;
+    sum_splits<NA, kCodedThreads>(red, N, g.splits, rank, tile % g.mt * 128, g.rows, tile / g.mt * N, g.T, g.sw, g.su, g.y, g.y_type, g.y_ld);
     // no CTA leaves while others may still read its shared memory
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
@@ -827,31 +867,33 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
   }
 }
 
-template <int FMT, bool GLU>
-cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const bitsmoe_microscale* xq, CodedArgs g,
-                         int sms, cudaStream_t st) {
+template <int FMT, bool GLU, int G>
+cudaError_t launch_coded_g(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const bitsmoe_microscale* xq, CodedArgs g,
+                           int sms, cudaStream_t st) {
   constexpr int NA = GLU ? 2 : 1, CPS = FMT == BITSMOE_MICRO_E8M0 ? 2 : 4;
-  g.N = std::min((g.T + 15) / 16 * 16, 256 / NA);
-  const int G = (g.N + 127) / 128, tt = (g.T + g.N - 1) / g.N;
+  const int tt = (g.T + g.N - 1) / g.N;
   g.mt = (g.rows + 127) / 128;
+  g.ntiles = g.mt * tt;
   g.nst = (g.cols + kStageK - 1) / kStageK;
   int splits = 1;
-  while (splits < 8 && (int64_t)g.mt * tt * splits * 2 <= sms && g.nst >= 2 * splits) splits *= 2;
+  while (splits < 8 && (int64_t)g.ntiles * splits * 2 <= sms && g.nst >= 2 * splits) splits *= 2;
   g.splits = splits;
   g.sps = (g.nst + splits - 1) / splits;
   g.stage = (NA * kCodeTile + (uint32_t)g.N * 128 + (uint32_t)((NA + G) * CPS) * 512 + 1023) / 1024 * 1024;
   const int sf_cols = (NA + G) * CPS * 4;
-  g.stages = std::min({g.sps, (int)(216 * 1024 / g.stage), (512 - NA * g.N) / sf_cols});
+  const int fit = std::min((int)(216 * 1024 / g.stage), 16);
+  // two accumulators where tensor memory holds them beside the scales of every stage
+  g.nbuf = splits == 1 && 2 * NA * g.N + fit * sf_cols <= 512 ? 2 : 1;
+  g.stages = std::min(fit, (512 - g.nbuf * NA * g.N) / sf_cols);
   const size_t ring = (size_t)g.stages * g.stage, redb = splits > 1 ? (size_t)NA * g.N * 512 : 0;
-  const size_t smem = 1024 + std::max(ring, redb) + (size_t)(2 * g.stages + 1) * 8 + 16;
+  const size_t smem = 1024 + std::max(ring, redb) + (size_t)(2 * g.stages + 4) * 8 + 16;
   CUtensorMap wm, um, xm;
-  if (!make_row_map(&wm, true, w->codes, g.rows, micro_pitch(g.cols), micro_pitch(g.cols), 128) ||
-      !make_row_map(&xm, true, xq->codes, g.T, micro_pitch(g.cols), micro_pitch(g.cols), g.N))
+  const int64_t pitch = micro_pitch(g.cols);
+  if (!make_row_map(&wm, true, w->codes, g.rows, pitch, pitch, 128) || !make_row_map(&xm, true, xq->codes, g.T, pitch, pitch, g.N))
     return cudaErrorInvalidValue;
   um = wm;
-  if (GLU && !make_row_map(&um, true, up->codes, g.rows, micro_pitch(g.cols), micro_pitch(g.cols), 128))
-    return cudaErrorInvalidValue;
-  auto kern = k_micro_coded<FMT, GLU>;
+  if (GLU && !make_row_map(&um, true, up->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
+  auto kern = k_micro_coded<FMT, GLU, G>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
@@ -860,13 +902,23 @@ cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* 
   attr[0].val.clusterDim.y = (unsigned)splits;
   attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(g.mt * tt), (unsigned)splits, 1);
+  cfg.gridDim = dim3((unsigned)(splits > 1 ? g.ntiles : std::min(g.ntiles, sms)), (unsigned)splits, 1);
   cfg.blockDim = dim3(kCodedThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = splits > 1 ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kern, wm, um, xm, g);
+}
+
+template <int FMT, bool GLU>
+cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const bitsmoe_microscale* xq, CodedArgs g,
+                         int sms, cudaStream_t st) {
+  g.N = std::min((g.T + 15) / 16 * 16, GLU ? 128 : 256);   // past one tile a multiple of the scale tiles' 128
+  if constexpr (!GLU) {
+    if (g.N > 128) return launch_coded_g<FMT, GLU, 2>(w, up, xq, g, sms, st);
+  }
+  return launch_coded_g<FMT, GLU, 1>(w, up, xq, g, sms, st);
 }
 
 // ---------------------------------------------------------------------------
@@ -1158,14 +1210,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 #pragma unroll
             for (int q = 0; q < 16; ++q) red[(size_t)(a * N + c0 + q) * 128 + r] = __uint_as_float(v[a][q]);
         } else if (m < g.rows) {
-#pragma unroll
-          for (int q = 0; q < 16; ++q) {
-            const int t = t0 + c0 + q;
-            if (t >= g.T) break;
-            float o = __uint_as_float(v[0][q]) * g.sw;
-            if (GLU) o = silu_mul(o, __uint_as_float(v[NA - 1][q]) * g.su);
-            store_y(g.y, g.y_type, (int64_t)t * g.y_ld + m, o);
-          }
+          store_tokens<NA>(v, t0 + c0, g.T, m, g.sw, g.su, g.y, g.y_type, g.y_ld);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

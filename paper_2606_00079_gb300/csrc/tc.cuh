@@ -56,29 +56,46 @@ __host__ __device__ constexpr uint32_t idesc_e2m1(int n, bool e8m0, uint32_t id)
   return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((e8m0 ? 1u : 0u) << 23) |
          ((uint32_t)(128 >> 4) << 24) | (id << 29);
 }
+// `one`: 1 in the lane that issues it (the warp is converged).
 template <bool E8M0>
-__device__ __forceinline__ void mma_e2m1(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
-                                         uint32_t acc) {
+__device__ __forceinline__ void mma_e2m1(uint32_t one, uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa,
+                                         uint32_t sb, uint32_t acc) {
   if constexpr (E8M0)
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n}\n" ::"r"(d_tmem),
-        "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(sa), "r"(sb)
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %7, 0;\n"
+        " @q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n}\n" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(sa), "r"(sb), "r"(one)
         : "memory");
   else
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%5], [%6], p;\n}\n" ::"r"(d_tmem),
-        "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(sa), "r"(sb)
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %7, 0;\n"
+        " @q tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%5], [%6], p;\n}\n" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(sa), "r"(sb), "r"(one)
         : "memory");
 }
 // 512 bytes of shared memory (32 rows of 16 bytes) into 4 tensor-memory columns of each 32-lane quarter.
-__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint32_t saddr) {
+__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
   uint64_t d = 0;
   d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);   // start address; no swizzle
   d |= (uint64_t)(128 >> 4) << 32;             // stride byte offset: 8 rows x 16 bytes
   d |= (uint64_t)1 << 46;                      // descriptor version
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(d) : "memory");
+  return d;
+}
+__device__ __forceinline__ void tmem_copy_scales(uint32_t one, uint32_t taddr, uint64_t desc) {
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n}\n" ::"r"(taddr),
+               "l"(desc), "r"(one)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void mma_commit(uint32_t one, uint64_t* bar) {
+  asm volatile(
+      "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+      " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(bar)), "r"(one)
+      : "memory");
 }
 
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {

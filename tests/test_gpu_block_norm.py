@@ -178,6 +178,14 @@ def test_strides_and_alignment(env):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+def test_no_rows(env):
+    torch, bm = env
+    h, y = torch.zeros(0, 96, device="cuda"), torch.zeros(0, 96, device="cuda")
+    w = torch.ones(96, device="cuda")
+    ho, x = bm.block_norm(h, y, post_norm=True, post_gain=w, pre_gain=w, gate=torch.zeros(0, device="cuda"))
+    assert ho.shape == x.shape == (0, 96)
+
+
 def test_non_finite_rows_stay_apart(env):
     torch, bm = env
     g = torch.Generator().manual_seed(3)
