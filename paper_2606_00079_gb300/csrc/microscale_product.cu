@@ -933,8 +933,8 @@ cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* 
 // that the next tile's products run meanwhile.  CTAs stay for all their tiles.
 // With few tiles the columns are split over a cluster instead.
 // ---------------------------------------------------------------------------
-constexpr int kWideThreads = 512;   // warps: 0 codes, 1 MMA, 2 activations, 4-11 decode, 12-15 epilogue
-constexpr int kDecodeWarps = 8;
+constexpr int kDecodeWarps = 8, kDecodeGroups = 2;   // groups of eight warps, each of which takes every other slot
+constexpr int kWideThreads = 32 * (4 + kDecodeGroups * kDecodeWarps + 4);   // warps: 0 codes, 1 MMA, 2 activations, 4.. decode, epilogue
 
 struct WideArgs {
   int T, rows, cols, tiles;
@@ -956,44 +956,30 @@ struct WideArgs {
   int* status;
 };
 
-// 32 codes (four words) of one row times their block scales -> 64 bytes of bf16 in a 128-byte swizzled tile.
-// A code's sign and other three bits, moved to a bf16's sign and lowest exponent and highest mantissa bits, are
-// its value times 2^-126; the factor brings the scale and 2^126 back: E8M0 whole, E4M3 2^119 (448 2^119 is the
-// largest that fits; the result's 2^-7 goes into the tensor scale).
+// 32 codes (four words) of one row times their block scales -> 64 bytes of bf16 in a 128-byte swizzled tile.  Codes
+// become fp16 pairs by one conversion each, products in fp32 are exact, and so is their rounding to bf16 (at most 6
+// significant bits; E8M0's largest scales overflow as fp32 does): 8 operations of the integer pipe for 8 codes, where
+// moving the bits into place takes 17.
 template <int FMT>
 __device__ __forceinline__ void decode32(const uint4& v, uint32_t sc, uint8_t* row, int half, int r7) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t f[2];
-  bool twice = false;
-  uint32_t f2 = 0;
+  float f[2];
   if constexpr (FMT == BITSMOE_MICRO_E8M0) {
-    const uint32_t c = sc & 255u;
-    twice = c > 128u;   // 2^(c - 127) 2^126 is above bf16's largest: in two steps
-    uint32_t b = (min(c, 128u) + 126u) << 7;
-    f[0] = f[1] = b | (b << 16);
-    b = c == 255u ? 0x7FC0u : (c - 1u) << 7;   // 2^(c - 128)
-    f2 = b | (b << 16);
+    f[0] = f[1] = micro_e8m0(sc & 255u);
   } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float s = micro_e4m3((sc >> (8 * h)) & 255u) * 6.646139978924579e35f;   // 2^119
-      const uint32_t b = __float_as_uint(s) >> 16;
-      f[h] = b | (b << 16);
-    }
+    const uint32_t p = e4m3x2_f16(sc);
+    f[0] = f16lo(p);
+    f[1] = f16hi(p);
   }
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const uint32_t w4 = w[q] << 4;
-    uint32_t o[4];
+    uint32_t h[4], o[4];
+    code_pairs<false>(w[q], h);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t t = __byte_perm(w4, w[q], ((4u + i) << 12) | ((uint32_t)i << 4));   // codes 2i, 2i + 1 at bits 15..12, 31..28
-      o[i] = ((t >> 6) & 0x01C001C0u) | (t & 0x80008000u);
-      asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(o[i]) : "r"(f[q >> 1]));
-    }
-    if (FMT == BITSMOE_MICRO_E8M0 && twice) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(o[i]) : "r"(f2));
+      const float2 c = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+      const __nv_bfloat162 b = __floats2bfloat162_rn(c.x * f[q >> 1], c.y * f[q >> 1]);
+      o[i] = *reinterpret_cast<const uint32_t*>(&b);
     }
     *reinterpret_cast<uint4*>(row + (((half * 4 + q) ^ r7) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
   }
@@ -1027,7 +1013,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   if (tid == 0) {
     for (int i = 0; i < P; ++i) {
       mbar_init_n(pfull + i, 1);
-      mbar_init_n(pempty + i, kDecodeWarps);
+      mbar_init_n(pempty + i, kDecodeGroups * kDecodeWarps);
     }
     for (int i = 0; i < Q; ++i) {
       mbar_init_n(qfull + i, kDecodeWarps + (g.btma ? 1 : 0));
@@ -1123,19 +1109,22 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       for (int j = max(0, n - Q); j < n; ++j) mbar_wait(qfull + j % Q, (uint32_t)(j / Q) & 1u, ok ? kWaitClocks : g.spin);
     }
     __syncwarp();
-  } else if (wid >= 4 && wid < 4 + kDecodeWarps) {
-    const int dw = wid - 4, r = 16 * dw + (lane & 15), half = lane >> 4, r7 = r & 7;
-    const int bt = tid - 128;
-    int ps = 0, pu = 0, qs = 0, qu = 0;
+  } else if (wid >= 4 && wid < 4 + kDecodeGroups * kDecodeWarps) {
+    const int dw = (wid - 4) % kDecodeWarps, group = (wid - 4) / kDecodeWarps;
+    const int r = 16 * dw + (lane & 15), half = lane >> 4, r7 = r & 7;
+    const int bt = dw * 32 + lane;
+    int ps = 0, pu = 0, n = 0;   // n: slots of all tiles so far
     for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x) {
       const int t0 = tile / g.mt * N;
-      for (int i = 0; i < ns; ++i) {
+      for (int i = 0; i < ns; ++i, ++n) {
         const int sub = i & 3;
         if (sub == 0) {
           if (lane == 0) ok = mbar_wait(pfull + ps, (uint32_t)pu & 1u, g.spin);
           ok = __all_sync(0xFFFFFFFFu, ok);
           if (!ok) break;
         }
+        if (n % kDecodeGroups == group) {
+        const int qs = n % Q, qu = n / Q;
         if (qu > 0) {
           if (lane == 0) ok = mbar_wait(qempty + qs, (uint32_t)(qu - 1) & 1u, g.spin);
           ok = __all_sync(0xFFFFFFFFu, ok);
@@ -1169,9 +1158,6 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         fence_proxy_async();   // generic writes -> tensor-core reads
         __syncwarp();
         if (lane == 0) mbar_arrive(qfull + qs);
-        if (++qs == Q) {
-          qs = 0;
-          ++qu;
         }
         if (sub == 3 || i == ns - 1) {
           if (lane == 0) mbar_arrive(pempty + ps);
@@ -1182,7 +1168,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         }
       }
     }
-  } else if (wid >= 4 + kDecodeWarps) {
+  } else if (wid >= 4 + kDecodeGroups * kDecodeWarps) {
     const int r = 32 * (wid & 3) + lane;
     int it = 0;
     for (int tile = blockIdx.x; tile < g.ntiles; tile += gridDim.x, ++it) {
@@ -1261,10 +1247,6 @@ cudaError_t launch_wide(const bitsmoe_microscale* w, const bitsmoe_microscale* u
     splits *= 2;
   g.splits = splits;
   g.sps = (g.nst + splits - 1) / splits;
-  if (FMT == BITSMOE_MICRO_E4M3) {
-    g.sw *= 128.f;
-    g.su *= 128.f;
-  }
   const size_t smem = 1024 + (size_t)g.Q * g.qst + (size_t)g.P * g.pst + (size_t)(2 * g.P + 2 * g.Q + 4) * 8 + 16;
   const int64_t pitch = micro_pitch(g.cols);
   CUtensorMap wm, um, xm;
