@@ -73,6 +73,14 @@ __device__ __forceinline__ void mma_e2m1(uint32_t one, uint32_t d_tmem, uint64_t
         "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(sa), "r"(sb), "r"(one)
         : "memory");
 }
+// mma_f16 of a converged warp.
+__device__ __forceinline__ void mma_f16(uint32_t one, uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
+      : "memory");
+}
 // 512 bytes of shared memory (32 rows of 16 bytes) into 4 tensor-memory columns of each 32-lane quarter.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
   uint64_t d = 0;
@@ -110,6 +118,16 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
+
+// mbar_wait of a warp that has nothing else to do for long: it leaves the issue slots to the others.
+__device__ __forceinline__ bool mbar_wait_idle(uint64_t* bar, uint32_t parity, long long limit) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity)) {
+    if (clock64() - t0 > limit) return false;
+    __nanosleep(100);
+  }
+  return true;
+}
 
 // Bounded wait on a phase that other CTAs of the cluster complete: their earlier writes are visible after it.
 __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, long long limit) {
