@@ -819,29 +819,37 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const int m = tile % g.mt * 128 + r, t0 = tile / g.mt * N;
       const uint32_t tl = tmem + ((uint32_t)(32 * (wid & 3)) << 16) + (uint32_t)(buf * NA * N);
-      for (int c0 = half ? nh : 0; c0 < (half ? N : nh); c0 += 16) {
-        uint32_t v[NA][16];
+      // the accumulator goes to registers first: the next tile's products run while this one is stored
+      constexpr int kChunks = G * 128 / 32;   // of 16 columns, at most, of a half
+      uint32_t v[kChunks][NA][16];
+      const int first = half ? nh : 0, last = half ? N : nh;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          if (nk > 0) {
-            tmem_ld16(tl + (uint32_t)(a * N + c0), v[a]);
+          if (nk > 0 && first + c * 16 < last) {
+            tmem_ld16(tl + (uint32_t)(a * N + first + c * 16), v[c][a]);
           } else {
 #pragma unroll
-            for (int q = 0; q < 16; ++q) v[a][q] = 0u;
+            for (int q = 0; q < 16; ++q) v[c][a][q] = 0u;
           }
         }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(aempty + buf);
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        const int c0 = first + c * 16;
+        if (c0 >= last) break;
         if (g.splits > 1) {
 #pragma unroll
           for (int a = 0; a < NA; ++a)
 #pragma unroll
-            for (int q = 0; q < 16; ++q) red[(size_t)(a * N + c0 + q) * 128 + r] = __uint_as_float(v[a][q]);
+            for (int q = 0; q < 16; ++q) red[(size_t)(a * N + c0 + q) * 128 + r] = __uint_as_float(v[c][a][q]);
         } else if (m < g.rows) {
-          store_tokens<NA>(v, t0 + c0, g.T, m, g.sw, g.su, g.y, g.y_type, g.y_ld);
+          store_tokens<NA>(v[c], t0 + c0, g.T, m, g.sw, g.su, g.y, g.y_type, g.y_ld);
         }
       }
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(aempty + buf);
     }
   }
   __syncwarp();
