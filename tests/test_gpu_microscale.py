@@ -251,6 +251,17 @@ def test_product_large(env, x, T, rows, cols):
     check_product(env, T, rows, cols, "e8m0", x == "coded", False, "bf16")
 
 
+@pytest.mark.parametrize("x", ["bf16", "coded"])
+@pytest.mark.parametrize("T,rows,cols", [(600, 4900, 1300), (513, 5003, 777), (290, 9900, 600)])
+def test_product_many_tiles(env, x, T, rows, cols):
+    """More tiles than SMs or half as many (no split of the columns), odd numbers of row and token tiles, several
+    stages."""
+    check_product(env, T, rows, cols, "e4m3", x == "coded", False, "f32")
+    check_product(env, T, rows, cols, "e8m0", x == "coded", False, "bf16")
+    check_product(env, T, rows, cols, "e8m0", x == "coded", True, "f32")
+    check_product(env, T, rows, cols, "e4m3", x == "coded", True, "bf16")
+
+
 @pytest.mark.parametrize("coded", [False, True])
 @pytest.mark.parametrize("T", [1, 9, 140])
 def test_product_strides(env, coded, T):
@@ -376,14 +387,15 @@ def test_product_on_streams_in_graphs_and_again(env, coded):
         assert torch.equal(y, ref[i])
 
 
-@pytest.mark.parametrize("case", ["few", "few_split", "coded", "coded_split", "wide", "wide_split", "wide_swiglu"])
+@pytest.mark.parametrize("case", ["few", "few_split", "coded", "coded_split", "coded_pair", "coded_pair_swiglu", "wide", "wide_split", "wide_swiglu"])
 def test_product_reports_a_wait_that_ran_out(env, case):
     """A block that never reports a slot of its ring free (testing hook): the bounded waits run out, the status word
     says so, and the next call is right.  Every case has more stages than its ring."""
     torch, bm = env
     rng = np.random.default_rng(6)
-    T = {"few": 3, "few_split": 2}.get(case, 40)
-    rows, cols = {"few": (152 * 128, 8192), "few_split": (130, 65536), "coded": (152 * 128, 8192), "coded_split": (130, 65536),
+    T = {"few": 3, "few_split": 2, "coded_pair": 256, "coded_pair_swiglu": 256}.get(case, 40)
+    rows, cols = {"few": (152 * 128, 8192), "few_split": (130, 65536), "coded": (152 * 128, 8192), "coded_pair": (152 * 128, 4096),
+                  "coded_pair_swiglu": (80 * 128, 4096), "coded_split": (130, 65536),
                   "wide": (152 * 128, 2048), "wide_split": (130, 16384), "wide_swiglu": (152 * 128, 1024)}[case]
     w = bm.microscale_quantize(torch.randn(rows, cols, device="cuda"), "e4m3", 1.0)
     x = bf16(rng.standard_normal((T, cols))).cuda()
