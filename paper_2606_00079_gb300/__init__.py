@@ -545,17 +545,31 @@ BLOCK_NORM_MAX_D = 32768                     # BITSMOE_BLOCK_NORM_MAX_D
 _GATE_NONE, _GATE_TOKEN, _GATE_ELEMENT = 0, 1, 2
 
 
+_torch = None
+_DENSE = {}          # torch dtype -> BITSMOE_F32 / BITSMOE_BF16
+_raw_stream = None   # device index -> the current stream's handle
+
+
+def _load_torch():
+    global _torch, _DENSE, _raw_stream
+    import torch
+    _DENSE = {torch.float32: 0, torch.bfloat16: 1}
+    # the handle without a Stream object around it, where torch has it (0.1 us instead of 2)
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+        lambda i: torch.cuda.current_stream(i).cuda_stream)
+    _torch = torch
+    return torch
+
+
 def _refuse(where: str, why: str, code: str = "INVALID_ARG"):
     raise BitsMoEError(ERR_CODE[code], f"{where}: {why}")
 
 
 def _dense_type(where: str, name: str, dtype) -> int:
-    import torch
-    if dtype == torch.float32:
-        return 0
-    if dtype == torch.bfloat16:
-        return 1
-    _refuse(where, f"{name} must be float32 or bfloat16, got {dtype}")
+    ty = _DENSE.get(dtype)
+    if ty is None:
+        _refuse(where, f"{name} must be float32 or bfloat16, got {dtype}")
+    return ty
 
 
 def _rows(where: str, name: str, x, rows=None, cols=None, device=None, dtype=None):
@@ -580,16 +594,23 @@ def _rows(where: str, name: str, x, rows=None, cols=None, device=None, dtype=Non
     return ld
 
 
-def _vector(where: str, name: str, v, n: int, device, dtype=None):
-    if v is None:
-        return None
-    if v.dim() != 1 or v.shape[0] != n:
-        _refuse(where, f"{name} has shape {tuple(v.shape)}, expected {(n,)}", "SHAPE")
+def _vector(where: str, name: str, v, n: int, device, dtype):
+    shape = v.shape
+    if len(shape) != 1 or shape[0] != n:
+        _refuse(where, f"{name} has shape {tuple(shape)}, expected {(n,)}", "SHAPE")
     if v.device != device or (n > 1 and v.stride(0) != 1):
         _refuse(where, f"{name} must be a dense vector on {device}")
-    if dtype is not None and v.dtype != dtype:
+    if v.dtype != dtype:
         _refuse(where, f"{name} must be {dtype}, got {v.dtype}")
     return v.data_ptr()
+
+
+def _elsewhere(where: str, device, stream):
+    """Context for a call on another stream than the current one, or on a device that is not current: inside it
+    both are, so that outputs belong to the stream that writes them."""
+    if stream is not None and stream.device != device:
+        _refuse(where, f"the stream is of {stream.device}, the tensors are on {device}")
+    return _torch.cuda.stream(stream if stream is not None else _torch.cuda.current_stream(device))
 
 
 class Microscale:
@@ -600,15 +621,17 @@ class Microscale:
     __slots__ = ("_codes", "_scales", "_buf", "_ptrs", "device", "rows", "cols", "fmt", "scale")
 
     def __init__(self, codes, scales, rows: int, cols: int, fmt: str = "e8m0", scale: float = 1.0):
-        import torch
+        torch = _torch or _load_torch()
         if fmt not in MICRO_FORMATS:
             _refuse("Microscale", f"unknown format {fmt!r}")
-        nc, ns = _micro_sizes(fmt, rows, cols)
         if rows < 0 or cols < 1:
             _refuse("Microscale", f"{rows} rows, {cols} columns")
-        for name, t, n in (("codes", codes, nc), ("scales", scales, ns)):
-            if t.dtype != torch.uint8 or t.numel() != n or not t.is_contiguous():
-                _refuse("Microscale", f"{name} must be {n} contiguous bytes (uint8)", "SHAPE")
+        nc, ns = _micro_sizes(fmt, rows, cols)
+        u8 = torch.uint8
+        if codes.dtype != u8 or codes.numel() != nc or not codes.is_contiguous():
+            _refuse("Microscale", f"codes must be {nc} contiguous bytes (uint8)", "SHAPE")
+        if scales.dtype != u8 or scales.numel() != ns or not scales.is_contiguous():
+            _refuse("Microscale", f"scales must be {ns} contiguous bytes (uint8)", "SHAPE")
         if codes.device != scales.device:
             _refuse("Microscale", "codes and scales are on different devices")
         self._codes, self._scales, self._buf = codes, scales, None
@@ -617,17 +640,18 @@ class Microscale:
 
     @classmethod
     def empty(cls, rows: int, cols: int, fmt: str = "e8m0", scale: float = 1.0, device=None) -> "Microscale":
-        import torch
-        nc, ns = _micro_sizes(fmt, rows, cols) if fmt in MICRO_FORMATS and rows >= 0 and cols > 0 else \
-            microscale_bytes(fmt, rows, cols)
+        torch = _torch or _load_torch()
+        if fmt not in MICRO_FORMATS or rows < 0 or cols < 1:
+            _refuse("Microscale.empty", f"{rows} rows, {cols} columns, format {fmt!r}")
+        nc, ns = _micro_sizes(fmt, rows, cols)
         self = cls.__new__(cls)   # one allocation for both; the tensors are made when asked for
         at = (nc + 255) // 256 * 256
-        self._buf = torch.empty(at + ns, dtype=torch.uint8,
-                                device=device if device is not None else f"cuda:{torch.cuda.current_device()}")
+        self._buf = buf = torch.empty(at + ns, dtype=torch.uint8,
+                                      device=device if device is not None else torch.cuda.current_device())
         self._codes = self._scales = None
-        base = self._buf.data_ptr()
-        self._ptrs, self.device = (base, base + at), self._buf.device
-        self.rows, self.cols, self.fmt, self.scale = int(rows), int(cols), fmt, float(scale)
+        base = buf.data_ptr()
+        self._ptrs, self.device = (base, base + at), buf.device
+        self.rows, self.cols, self.fmt, self.scale = rows, cols, fmt, float(scale)
         return self
 
     @property
@@ -690,57 +714,48 @@ def microscale_bytes(fmt: str, rows: int, cols: int):
     return int(nc.value), int(ns.value)
 
 
-def _launch(device, stream, call):
-    """call(raw stream) with `device` current, on the given stream or the device's current one: outputs that
-    the call allocates belong to the stream that writes them."""
-    import torch
-    if stream is None and torch.cuda.current_device() == device.index:
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the public way builds a Stream object (2 us)
-        return call(raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream)
-    with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)) as _:
-        st = torch.cuda.current_stream()
-        if st.device != device:
-            _refuse("stream", f"the stream is of {st.device}, the tensors are on {device}")
-        return call(st.cuda_stream)
-
-
 def microscale_quantize(x, fmt: str = "e8m0", scale: float = 1.0, out: Optional[Microscale] = None,
                         stream=None) -> Microscale:
     """Quantise the rows of x (torch fp32 or bf16, 2-d, dense rows, on the device) into a Microscale with
     tensor scale `scale` (a power of two); `out` reuses an existing one of the same shape and format."""
     import torch
+    torch = _torch or _load_torch()
     where = "microscale_quantize"
+    dev = x.device
     ty = _dense_type(where, "x", x.dtype)
     ld = _rows(where, "x", x)
+    if stream is not None or torch._C._cuda_getDevice() != dev.index:
+        with _elsewhere(where, dev, stream):
+            return microscale_quantize(x, fmt, scale, out)
     rows, cols = x.shape
-
-    def call(st):
-        q = out
-        if q is None:
-            q = Microscale.empty(rows, cols, fmt, scale, x.device)
-        elif (q.rows, q.cols, q.fmt) != (rows, cols, fmt) or q.device != x.device:
-            _refuse(where, "out has another shape, format or device", "SHAPE")
-        q.scale = float(scale)
-        _check(_lib().bitsmoe_microscale_quantize(x.data_ptr(), ty, ld, q._struct(), st), "bitsmoe_microscale_quantize")
-        return q
-    return _launch(x.device, stream, call)
+    if out is None:
+        out = Microscale.empty(rows, cols, fmt, scale, dev)
+    elif (out.rows, out.cols, out.fmt) != (rows, cols, fmt) or out.device != dev:
+        _refuse(where, "out has another shape, format or device", "SHAPE")
+    else:
+        out.scale = float(scale)
+    _check(_lib().bitsmoe_microscale_quantize(x.data_ptr(), ty, ld, out._struct(), _raw_stream(dev.index)),
+           "bitsmoe_microscale_quantize")
+    return out
 
 
 def microscale_dequantize(q: Microscale, dtype=None, out=None, stream=None):
     """The values of a Microscale as a torch tensor rows x cols (float32, or bfloat16)."""
-    import torch
+    torch = _torch or _load_torch()
     where = "microscale_dequantize"
     dev = q.device
-
-    def call(st):
-        x = out
-        if x is None:
-            x = torch.empty((q.rows, q.cols), dtype=dtype if dtype is not None else torch.float32, device=dev)
-        ty = _dense_type(where, "out", x.dtype)
-        ld = _rows(where, "out", x, q.rows, q.cols, dev)
-        _check(_lib().bitsmoe_microscale_dequantize(q._struct(), x.data_ptr(), ty, ld, st), "bitsmoe_microscale_dequantize")
-        return x
-    return _launch(dev, stream, call)
+    if dev.type != "cuda":
+        _refuse(where, "the matrix must be on a CUDA device")
+    if stream is not None or torch._C._cuda_getDevice() != dev.index:
+        with _elsewhere(where, dev, stream):
+            return microscale_dequantize(q, dtype, out)
+    if out is None:
+        out, ld = torch.empty((q.rows, q.cols), dtype=dtype if dtype is not None else torch.float32, device=dev), q.cols
+    else:
+        ld = _rows(where, "out", out, q.rows, q.cols, dev)
+    _check(_lib().bitsmoe_microscale_dequantize(q._struct(), out.data_ptr(), _dense_type(where, "out", out.dtype), ld,
+                                                _raw_stream(dev.index)), "bitsmoe_microscale_dequantize")
+    return out
 
 
 def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=None, y=None, status=None,
@@ -748,32 +763,32 @@ def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=
     """y (T x w.rows, fp32 by default, or bf16) = x w^T for x a torch bf16 tensor (T x w.cols, dense rows) or a
     Microscale of w's format; with `up` (w's shape and format) SiLU(x w^T) * (x up^T).  `status`: an optional
     int32 tensor of one element that receives a device-side timeout."""
-    import torch
+    torch = _torch or _load_torch()
     where = "microscale_product"
-    coded = isinstance(x, Microscale)
     dev = w.device
-    if x.device != dev or (up is not None and up.device != dev):
-        _refuse(where, "the operands are on different devices")
-    if coded:
-        T, x_ptr, x_ld = x.rows, None, 0
+    if dev.type != "cuda" or x.device != dev or (up is not None and up.device != dev):
+        _refuse(where, "the operands must be on one CUDA device")
+    if stream is not None or torch._C._cuda_getDevice() != dev.index:
+        with _elsewhere(where, dev, stream):
+            return microscale_product(w, x, up, dtype, y, status)
+    if type(x) is Microscale:
+        T, x_ptr, x_ld, xq = x.rows, None, 0, x._struct()
     else:
-        x_ld = _rows(where, "x", x, None, w.cols, dev, torch.bfloat16)
-        T, x_ptr = x.shape[0], x.data_ptr()
-    if status is not None and (status.dtype != torch.int32 or status.numel() != 1 or status.device != dev):
-        _refuse(where, "status must be one int32 on the operands' device")
-
-    def call(st):
-        out = y
-        if out is None:
-            out = torch.empty((T, w.rows), dtype=dtype if dtype is not None else torch.float32, device=dev)
-        ty = _dense_type(where, "y", out.dtype)
-        y_ld = _rows(where, "y", out, T, w.rows, dev)
-        _check(_lib().bitsmoe_microscale_product(w._struct(), up._struct() if up is not None else None, x_ptr, x_ld,
-                                                 x._struct() if coded else None, T, out.data_ptr(), ty, y_ld,
-                                                 status.data_ptr() if status is not None else None, st),
-               "bitsmoe_microscale_product")
-        return out
-    return _launch(dev, stream, call)
+        x_ld = _rows(where, "x", x, None, w.cols, None, torch.bfloat16)
+        T, x_ptr, xq = x.shape[0], x.data_ptr(), None
+    st_ptr = None
+    if status is not None:
+        if status.dtype != torch.int32 or status.numel() != 1 or status.device != dev:
+            _refuse(where, "status must be one int32 on the operands' device")
+        st_ptr = status.data_ptr()
+    if y is None:
+        y, y_ld = torch.empty((T, w.rows), dtype=dtype if dtype is not None else torch.float32, device=dev), w.rows
+    else:
+        y_ld = _rows(where, "y", y, T, w.rows, dev)
+    _check(_lib().bitsmoe_microscale_product(w._struct(), up._struct() if up is not None else None, x_ptr, x_ld, xq, T,
+                                             y.data_ptr(), _dense_type(where, "y", y.dtype), y_ld, st_ptr,
+                                             _raw_stream(dev.index)), "bitsmoe_microscale_product")
+    return y
 
 
 def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: float = 1e-6, gate=None,
@@ -787,13 +802,19 @@ def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: 
     times residual_scale only when h_out is given, else None); gate is a vector of T (one value per row) or
     T x D; the gains and channel_scale are vectors of D of one type.  h_out and x are allocated when not
     given (h_out may be h: in place); pre_norm False returns x None."""
-    import torch
+    torch = _torch or _load_torch()
     where = "block_norm"
     dev = h.device
     h_type, h_ld = _dense_type(where, "h", h.dtype), _rows(where, "h", h)
+    if stream is not None or torch._C._cuda_getDevice() != dev.index:
+        with _elsewhere(where, dev, stream):
+            return block_norm(h, y, post_norm=post_norm, post_gain=post_gain, post_eps=post_eps, gate=gate,
+                              gate_sigmoid=gate_sigmoid, channel_scale=channel_scale, branch_scale=branch_scale,
+                              residual_scale=residual_scale, pre_norm=pre_norm, pre_gain=pre_gain, pre_eps=pre_eps,
+                              gain_offset=gain_offset, h_out=h_out, x=x, x_dtype=x_dtype)
     T, D = h.shape
-    y_type = y_ld = gate_type = gate_kind = gate_ld = 0
-    y_ptr = gate_ptr = None
+    y_type = y_ld = gate_type = gate_kind = gate_ld = gain_type = ho_ld = x_type = x_ld = 0
+    y_ptr = gate_ptr = post_ptr = pre_ptr = chan_ptr = ho_ptr = x_ptr = None
     if y is not None:
         y_type, y_ld, y_ptr = _dense_type(where, "y", y.dtype), _rows(where, "y", y, T, D, dev), y.data_ptr()
     if gate is not None:
@@ -801,34 +822,43 @@ def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: 
         if gate.dim() == 1:
             if gate.shape[0] != T or gate.device != dev:
                 _refuse(where, f"gate has shape {tuple(gate.shape)} on {gate.device}, expected {(T,)} on {dev}", "SHAPE")
-            gate_kind, gate_ld = _GATE_TOKEN, max(gate.stride(0), 1)
-            if T > 1 and gate.stride(0) < 1:
-                _refuse(where, "gate's elements overlap")
+            gate_kind, gate_ld = _GATE_TOKEN, gate.stride(0)
+            if gate_ld < 1:
+                if T > 1:
+                    _refuse(where, "gate's elements overlap")
+                gate_ld = 1
         else:
             gate_kind, gate_ld = _GATE_ELEMENT, _rows(where, "gate", gate, T, D, dev)
-    gt = next((v.dtype for v in (post_gain, pre_gain, channel_scale) if v is not None), torch.float32)
-    gain_type = _dense_type(where, "gains", gt)
-    vec = [_vector(where, n, v, D, dev, gt)
-           for n, v in (("post_gain", post_gain), ("pre_gain", pre_gain), ("channel_scale", channel_scale))]
-    if x is not None and not pre_norm:
-        _refuse(where, "x is given but pre_norm is off")
-
-    def call(st):
-        ho, xo = h_out, x
-        if ho is None and y is not None:
-            ho = torch.empty((T, D), dtype=h.dtype, device=dev)
-        if xo is None and pre_norm:
-            xo = torch.empty((T, D), dtype=x_dtype if x_dtype is not None else torch.bfloat16, device=dev)
-        ho_ld = _rows(where, "h_out", ho, T, D, dev, h.dtype) if ho is not None else 0
-        x_type, x_ld = (_dense_type(where, "x", xo.dtype), _rows(where, "x", xo, T, D, dev)) if xo is not None else (0, 0)
-        a = _BlockNormArgs(T, D, h_type, y_type, gate_type, gain_type, x_type, 1 if post_norm else 0, gate_kind,
-                           1 if gate_sigmoid else 0, post_eps, pre_eps, gain_offset, residual_scale, branch_scale,
-                           h.data_ptr(), y_ptr, gate_ptr, vec[0], vec[1], vec[2],
-                           ho.data_ptr() if ho is not None else None, xo.data_ptr() if xo is not None else None,
-                           h_ld, y_ld, gate_ld, ho_ld, x_ld)
-        _check(_lib().bitsmoe_block_norm(ctypes.byref(a), st), "bitsmoe_block_norm")
-        return ho, xo
-    return _launch(dev, stream, call)
+    gt = None
+    if post_gain is not None:
+        gt = post_gain.dtype
+        post_ptr = _vector(where, "post_gain", post_gain, D, dev, gt)
+    if pre_gain is not None:
+        gt = gt or pre_gain.dtype
+        pre_ptr = _vector(where, "pre_gain", pre_gain, D, dev, gt)
+    if channel_scale is not None:
+        gt = gt or channel_scale.dtype
+        chan_ptr = _vector(where, "channel_scale", channel_scale, D, dev, gt)
+    if gt is not None:
+        gain_type = _dense_type(where, "gains", gt)
+    if h_out is not None:
+        ho_ld, ho_ptr = _rows(where, "h_out", h_out, T, D, dev, h.dtype), h_out.data_ptr()
+    elif y is not None:
+        h_out, ho_ld = torch.empty((T, D), dtype=h.dtype, device=dev), D
+        ho_ptr = h_out.data_ptr()
+    if x is not None:
+        if not pre_norm:
+            _refuse(where, "x is given but pre_norm is off")
+        x_type, x_ld, x_ptr = _dense_type(where, "x", x.dtype), _rows(where, "x", x, T, D, dev), x.data_ptr()
+    elif pre_norm:
+        x = torch.empty((T, D), dtype=x_dtype if x_dtype is not None else torch.bfloat16, device=dev)
+        x_type, x_ld, x_ptr = _dense_type(where, "x", x.dtype), D, x.data_ptr()
+    _check(_lib().bitsmoe_block_norm(
+        _BlockNormArgs(T, D, h_type, y_type, gate_type, gain_type, x_type, 1 if post_norm else 0, gate_kind,
+                       1 if gate_sigmoid else 0, post_eps, pre_eps, gain_offset, residual_scale, branch_scale,
+                       h.data_ptr(), y_ptr, gate_ptr, post_ptr, pre_ptr, chan_ptr, ho_ptr, x_ptr,
+                       h_ld, y_ld, gate_ld, ho_ld, x_ld), _raw_stream(dev.index)), "bitsmoe_block_norm")
+    return h_out, x
 
 
 def bitsmoe_debug_single_token_kernel(which: int) -> None:

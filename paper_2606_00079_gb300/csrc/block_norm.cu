@@ -9,7 +9,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "device.cuh"
+#include "microscale.cuh"
 
 namespace {
 using namespace bmoe;
@@ -489,11 +489,17 @@ bool rows_of(const bitsmoe_block_norm_args& a, int vec) {
          ok(a.post_gain, a.gain_type, 0) && ok(a.pre_gain, a.gain_type, 0) && ok(a.channel_scale, a.gain_type, 0);
 }
 
+template <int NV, int HT, int YT>
+cudaError_t launch_rows(const bitsmoe_block_norm_args& a, int dev, int64_t blocks, int threads, int slots, size_t row, cudaStream_t st) {
+  const cudaError_t e = allow_shared<k_block_norm_rows<NV, HT, YT>>(dev, 220 * 1024);
+  if (e == cudaSuccess) k_block_norm_rows<NV, HT, YT><<<(unsigned)blocks, threads, slots * row, st>>>(a, slots);
+  return e;
+}
+
 template <int VEC, int NV>
 cudaError_t launch_norm(const bitsmoe_block_norm_args& a, cudaStream_t st) {
   int dev = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  cudaError_t e = device_sms(&dev, &sms);
   if (e != cudaSuccess) return e;
   const int nvec = a.D / VEC, threads = ((nvec + NV - 1) / NV + 31) / 32 * 32;
   if constexpr (VEC * NV <= 8) {
@@ -512,13 +518,10 @@ cudaError_t launch_norm(const bitsmoe_block_norm_args& a, cudaStream_t st) {
     const size_t row = (size_t)a.D * ((a.y ? size(a.y_type) : 0) + size(a.h_type) + (a.gate_kind == BITSMOE_GATE_ELEMENT ? size(a.gate_type) : 0));
     const int slots = (int)std::min<size_t>(kMaxSlots, (size_t)(220 / per_sm - 2) * 1024 / row);   // >= 1: at most 12 x 16384 bytes
     const bool hf = a.h_type == BITSMOE_F32, yf = a.y_type == BITSMOE_F32;
-    const auto run = [&](auto kern) {
-      const cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
-      if (r == cudaSuccess) kern<<<(unsigned)full, threads, slots * row, st>>>(a, slots);
-      return r;
-    };
-    e = hf ? (yf ? run(k_block_norm_rows<NV, BITSMOE_F32, BITSMOE_F32>) : run(k_block_norm_rows<NV, BITSMOE_F32, BITSMOE_BF16>))
-           : (yf ? run(k_block_norm_rows<NV, BITSMOE_BF16, BITSMOE_F32>) : run(k_block_norm_rows<NV, BITSMOE_BF16, BITSMOE_BF16>));
+    e = hf ? (yf ? launch_rows<NV, BITSMOE_F32, BITSMOE_F32>(a, dev, full, threads, slots, row, st)
+                 : launch_rows<NV, BITSMOE_F32, BITSMOE_BF16>(a, dev, full, threads, slots, row, st))
+           : (yf ? launch_rows<NV, BITSMOE_BF16, BITSMOE_F32>(a, dev, full, threads, slots, row, st)
+                 : launch_rows<NV, BITSMOE_BF16, BITSMOE_BF16>(a, dev, full, threads, slots, row, st));
     if (e != cudaSuccess) return e;
   } else {
     k_block_norm<VEC, NV, false, false><<<(unsigned)full, threads, 0, st>>>(a);

@@ -13,6 +13,7 @@
 #include <cuda_fp8.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <cmath>
 
 #include "device.cuh"
@@ -47,6 +48,29 @@ inline int micro_check(const bitsmoe_microscale* m) {
   if (reinterpret_cast<uintptr_t>(m->codes) % 16 || reinterpret_cast<uintptr_t>(m->scales) % 16)
     return BITSMOE_ERR_ALIGNMENT;
   return BITSMOE_OK;
+}
+
+// SMs of the current device, asked once for each (a query of the runtime takes as long as a small kernel's launch).
+inline cudaError_t device_sms(int* dev, int* sms) {
+  static std::atomic<int> known[64];
+  const cudaError_t e = cudaGetDevice(dev);
+  if (e != cudaSuccess) return e;
+  const int i = *dev & 63;
+  *sms = *dev < 64 ? known[i].load(std::memory_order_relaxed) : 0;
+  if (*sms > 0) return cudaSuccess;
+  const cudaError_t r = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev);
+  if (r == cudaSuccess && *dev < 64) known[i].store(*sms, std::memory_order_relaxed);
+  return r;
+}
+
+// The dynamic shared memory that a kernel may ask for on device `dev`, set once for each (K: the kernel).
+template <auto K>
+cudaError_t allow_shared(int dev, int bytes) {
+  static std::atomic<uint64_t> done;
+  if (dev < 64 && (done.load(std::memory_order_acquire) >> dev & 1)) return cudaSuccess;
+  const cudaError_t r = cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (r == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_release);
+  return r;
 }
 
 }  // namespace bmoe

@@ -563,7 +563,7 @@ bool few_plan(int format, bool glu, int T, int rows, int cols, int (*resident)(i
 }
 
 template <int FMT, bool GLU, int NT>
-cudaError_t launch_few(const FewPlan& p, const bitsmoe_microscale* w, const bitsmoe_microscale* up, FewArgs g, cudaStream_t st) {
+cudaError_t launch_few(const FewPlan& p, const bitsmoe_microscale* w, const bitsmoe_microscale* up, FewArgs g, int dev, cudaStream_t st) {
   g.nst = (g.cols + kStageK - 1) / kStageK;
   g.mt = (g.rows + 127) / 128;
   g.splits = p.splits;
@@ -577,7 +577,7 @@ cudaError_t launch_few(const FewPlan& p, const bitsmoe_microscale* w, const bits
   um = wm;
   if (GLU && !make_row_map(&um, true, up->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
   auto kern = k_micro_few<FMT, GLU, NT>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
+  cudaError_t e = allow_shared<k_micro_few<FMT, GLU, NT>>(dev, 226 * 1024);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -598,8 +598,8 @@ cudaError_t launch_few(const FewPlan& p, const bitsmoe_microscale* w, const bits
 int few_resident(int splits) { return resident_clusters(k_micro_few<BITSMOE_MICRO_E8M0, false, 1>, kFewThreads, splits); }
 
 template <int FMT, bool GLU>
-cudaError_t launch_few_nt(const FewPlan& p, const bitsmoe_microscale* w, const bitsmoe_microscale* up, const FewArgs& g, cudaStream_t st) {
-  return g.T > 8 ? launch_few<FMT, GLU, 2>(p, w, up, g, st) : launch_few<FMT, GLU, 1>(p, w, up, g, st);
+cudaError_t launch_few_nt(const FewPlan& p, const bitsmoe_microscale* w, const bitsmoe_microscale* up, const FewArgs& g, int dev, cudaStream_t st) {
+  return g.T > 8 ? launch_few<FMT, GLU, 2>(p, w, up, g, dev, st) : launch_few<FMT, GLU, 1>(p, w, up, g, dev, st);
 }
 
 // Sixteen tokens' results of weight row m (a lane's; the warp's lanes hold consecutive rows) from token t on.
@@ -915,7 +915,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
 
 template <int FMT, bool GLU, int G, bool PAIR>
 cudaError_t launch_coded_p(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const bitsmoe_microscale* xq, CodedArgs g,
-                           int sms, cudaStream_t st) {
+                           int dev, int sms, cudaStream_t st) {
   constexpr int NA = GLU ? 2 : 1;
   const size_t ring = (size_t)g.stages * g.stage, redb = g.splits > 1 ? (size_t)NA * g.N * 512 : 0;
   const size_t smem = 1024 + std::max(ring, redb) + (size_t)(2 * g.stages + 4) * 8 + 16;
@@ -927,7 +927,7 @@ cudaError_t launch_coded_p(const bitsmoe_microscale* w, const bitsmoe_microscale
   um = wm;
   if (GLU && !make_row_map(&um, true, up->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
   auto kern = k_micro_coded<FMT, GLU, G, PAIR>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  cudaError_t e = allow_shared<k_micro_coded<FMT, GLU, G, PAIR>>(dev, 227 * 1024);
   if (e != cudaSuccess) return e;
   int grid = g.splits > 1 ? g.ntiles : std::min(g.ntiles, sms);
   if (PAIR) {   // tiles are pairs' from here on
@@ -951,7 +951,7 @@ cudaError_t launch_coded_p(const bitsmoe_microscale* w, const bitsmoe_microscale
 
 template <int FMT, bool GLU, int G>
 cudaError_t launch_coded_g(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const bitsmoe_microscale* xq, CodedArgs g,
-                           int sms, cudaStream_t st) {
+                           int dev, int sms, cudaStream_t st) {
   constexpr int NA = GLU ? 2 : 1, CPS = FMT == BITSMOE_MICRO_E8M0 ? 2 : 4;
   const int tt = (g.T + g.N - 1) / g.N;
   g.mt = (g.rows + 127) / 128;
@@ -969,19 +969,19 @@ cudaError_t launch_coded_g(const bitsmoe_microscale* w, const bitsmoe_microscale
   g.stages = std::min(fit, (512 - g.nbuf * NA * g.N) / sf_cols);
   // pairs where there is something to share: whole halves of 128 tokens, or with GLU two token tiles
   if constexpr (GLU || G == 2) {
-    if (splits == 1 && g.N == 256 / NA && (GLU ? tt : g.mt) >= 2) return launch_coded_p<FMT, GLU, G, true>(w, up, xq, g, sms, st);
+    if (splits == 1 && g.N == 256 / NA && (GLU ? tt : g.mt) >= 2) return launch_coded_p<FMT, GLU, G, true>(w, up, xq, g, dev, sms, st);
   }
-  return launch_coded_p<FMT, GLU, G, false>(w, up, xq, g, sms, st);
+  return launch_coded_p<FMT, GLU, G, false>(w, up, xq, g, dev, sms, st);
 }
 
 template <int FMT, bool GLU>
 cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const bitsmoe_microscale* xq, CodedArgs g,
-                         int sms, cudaStream_t st) {
+                         int dev, int sms, cudaStream_t st) {
   g.N = std::min((g.T + 15) / 16 * 16, GLU ? 128 : 256);   // past one tile a multiple of the scale tiles' 128
   if constexpr (!GLU) {
-    if (g.N > 128) return launch_coded_g<FMT, GLU, 2>(w, up, xq, g, sms, st);
+    if (g.N > 128) return launch_coded_g<FMT, GLU, 2>(w, up, xq, g, dev, sms, st);
   }
-  return launch_coded_g<FMT, GLU, 1>(w, up, xq, g, sms, st);
+  return launch_coded_g<FMT, GLU, 1>(w, up, xq, g, dev, sms, st);
 }
 
 // ---------------------------------------------------------------------------
@@ -1304,7 +1304,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 }
 
 template <int FMT, bool GLU>
-cudaError_t launch_wide(const bitsmoe_microscale* w, const bitsmoe_microscale* up, WideArgs g, int sms, cudaStream_t st) {
+cudaError_t launch_wide(const bitsmoe_microscale* w, const bitsmoe_microscale* up, WideArgs g, int dev, int sms, cudaStream_t st) {
   constexpr int NA = GLU ? 2 : 1, CPS = FMT == BITSMOE_MICRO_E8M0 ? 2 : 4;
   constexpr uint32_t kRoom = 216 * 1024;
   int tt = (g.T + 255) / 256;
@@ -1337,7 +1337,7 @@ cudaError_t launch_wide(const bitsmoe_microscale* w, const bitsmoe_microscale* u
   g.btma = (uintptr_t)g.x % 16 == 0 && (g.x_ld % 8 == 0 || g.T == 1);
   if (g.btma) g.btma = make_row_map(&xm, false, g.x, g.T, g.cols, g.T == 1 ? (g.cols * 2 + 15) / 16 * 16 : g.x_ld * 2, g.N);
   auto kern = k_micro_wide<FMT, GLU>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  cudaError_t e = allow_shared<k_micro_wide<FMT, GLU>>(dev, 227 * 1024);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1388,8 +1388,7 @@ extern "C" int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bit
   const long long spin = debug_wait_clocks() > 0 ? debug_wait_clocks() : kWaitClocks;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int dev = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  cudaError_t e = device_sms(&dev, &sms);
   if (e != cudaSuccess) return record_cuda_error((int)e);
   const bool e8 = w->format == BITSMOE_MICRO_E8M0;
   FewPlan fp;
@@ -1414,8 +1413,8 @@ extern "C" int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bit
     f.spin = spin;
     f.lose = debug_skip_arrival();
     f.status = status;
-    if (e8) e = up ? launch_few_nt<BITSMOE_MICRO_E8M0, true>(fp, w, up, f, st) : launch_few_nt<BITSMOE_MICRO_E8M0, false>(fp, w, up, f, st);
-    else e = up ? launch_few_nt<BITSMOE_MICRO_E4M3, true>(fp, w, up, f, st) : launch_few_nt<BITSMOE_MICRO_E4M3, false>(fp, w, up, f, st);
+    if (e8) e = up ? launch_few_nt<BITSMOE_MICRO_E8M0, true>(fp, w, up, f, dev, st) : launch_few_nt<BITSMOE_MICRO_E8M0, false>(fp, w, up, f, dev, st);
+    else e = up ? launch_few_nt<BITSMOE_MICRO_E4M3, true>(fp, w, up, f, dev, st) : launch_few_nt<BITSMOE_MICRO_E4M3, false>(fp, w, up, f, dev, st);
     return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
   }
   if (xq) {
@@ -1437,9 +1436,9 @@ extern "C" int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bit
     c.lose = debug_skip_arrival();
     c.status = status;
     if (e8)
-      e = up ? launch_coded<BITSMOE_MICRO_E8M0, true>(w, up, xq, c, sms, st) : launch_coded<BITSMOE_MICRO_E8M0, false>(w, up, xq, c, sms, st);
+      e = up ? launch_coded<BITSMOE_MICRO_E8M0, true>(w, up, xq, c, dev, sms, st) : launch_coded<BITSMOE_MICRO_E8M0, false>(w, up, xq, c, dev, sms, st);
     else
-      e = up ? launch_coded<BITSMOE_MICRO_E4M3, true>(w, up, xq, c, sms, st) : launch_coded<BITSMOE_MICRO_E4M3, false>(w, up, xq, c, sms, st);
+      e = up ? launch_coded<BITSMOE_MICRO_E4M3, true>(w, up, xq, c, dev, sms, st) : launch_coded<BITSMOE_MICRO_E4M3, false>(w, up, xq, c, dev, sms, st);
     return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
   }
   WideArgs a;
@@ -1460,7 +1459,7 @@ extern "C" int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bit
   a.spin = spin;
   a.lose = debug_skip_arrival();
   a.status = status;
-  if (e8) e = up ? launch_wide<BITSMOE_MICRO_E8M0, true>(w, up, a, sms, st) : launch_wide<BITSMOE_MICRO_E8M0, false>(w, up, a, sms, st);
-  else e = up ? launch_wide<BITSMOE_MICRO_E4M3, true>(w, up, a, sms, st) : launch_wide<BITSMOE_MICRO_E4M3, false>(w, up, a, sms, st);
+  if (e8) e = up ? launch_wide<BITSMOE_MICRO_E8M0, true>(w, up, a, dev, sms, st) : launch_wide<BITSMOE_MICRO_E8M0, false>(w, up, a, dev, sms, st);
+  else e = up ? launch_wide<BITSMOE_MICRO_E4M3, true>(w, up, a, dev, sms, st) : launch_wide<BITSMOE_MICRO_E4M3, false>(w, up, a, dev, sms, st);
   return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
 }
