@@ -23,19 +23,6 @@ struct MicroMat {
   int tiles;
 };
 
-// The 8 values of a coded row from column k (a multiple of 8) without the tensor scale; zeros past the matrix.
-__device__ __forceinline__ void decode8(const MicroMat& m, int format, int r, int rows, int k, int cols, float* dst) {
-  if (r < rows && k < cols) {
-    const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(m.codes + (int64_t)r * m.pitch + k / 2));
-    const float s = micro_scale(format, m.scales[micro_scale_at(m.tiles, r, k / micro_block(format))]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) dst[i] = micro_value((w >> (4 * i)) & 15u) * s;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) dst[i] = 0.f;
-  }
-}
-
 __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + expf(-g)) * u; }
 
 __device__ __forceinline__ void store_y(void* y, int type, int64_t i, float v) {
@@ -228,23 +215,44 @@ __device__ __forceinline__ void few_half(uint32_t code, uint32_t sf, const uint3
 
 __device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(kFewWarps * 32) : "memory"); }
 
-// Eight activations of token t from column k (a multiple of 8) in fp32, zeros past the columns.
-__device__ __forceinline__ void few_x8(const FewArgs& g, int format, int t, int k, float (&v)[8]) {
+// Eight activations of token t from column k (a multiple of 8) as they are stored, zeros past the columns: 8 bf16, or
+// a word of codes and its scale byte.
+__device__ __forceinline__ uint4 few_raw(const FewArgs& g, int format, int t, int k) {
+  uint4 q = make_uint4(0u, 0u, 0u, 0u);
+  if (k >= g.cols) return q;
   if (g.xq.codes) {
-    decode8(g.xq, format, t, g.T, k, g.cols, v);
+    q.x = __ldg(reinterpret_cast<const uint32_t*>(g.xq.codes + (int64_t)t * g.xq.pitch + k / 2));
+    q.y = g.xq.scales[micro_scale_at(g.xq.tiles, t, k / micro_block(format))];
   } else {
     const __nv_bfloat16* p = g.x + (int64_t)t * g.x_ld + k;
     if (g.x_vec && k + 8 <= g.cols) {
-      const uint4 q = *reinterpret_cast<const uint4*>(p);
-      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = bf16lo(w[i]);
-        v[2 * i + 1] = bf16hi(w[i]);
-      }
+      q = *reinterpret_cast<const uint4*>(p);
     } else {
+      uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = k + i < g.cols ? __bfloat162float(p[i]) : 0.f;
+      for (int i = 0; i < 8; ++i)
+        if (k + i < g.cols) w[i / 2] |= (uint32_t)__bfloat16_as_ushort(p[i]) << (16 * (i & 1));
+      q = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  return q;
+}
+__device__ __forceinline__ void few_values(const FewArgs& g, int format, const uint4& q, float (&v)[8]) {
+  if (g.xq.codes) {
+    const float s = micro_scale(format, q.y);
+    uint32_t h[4];
+    code_pairs<false>(q.x, h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = f16lo(h[i]) * s;
+      v[2 * i + 1] = f16hi(h[i]) * s;
+    }
+  } else {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = bf16lo(w[i]);
+      v[2 * i + 1] = bf16hi(w[i]);
     }
   }
 }
@@ -264,7 +272,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   const int S = g.stages;
   constexpr uint32_t kRed = few_red_bytes(NA, NT);   // [rank][half][matrix][token][rows of this CTA] fp32
   uint8_t* redb = sm + (size_t)S * g.stage;          // two of them
-  uint8_t* xs = redb + 2 * kRed;
+  uint8_t* xs = redb + (g.mt > (int)gridDim.x ? 2 : 1) * kRed;
   uint64_t* full = reinterpret_cast<uint64_t*>(xs + (size_t)g.T * g.x_pitch);
   uint64_t* empty = full + S;
   uint64_t* rfull = empty + S;                        // [2] the parts of a tile are there
@@ -322,30 +330,41 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     const int k0 = st0 * kStageK, n8 = nk * (kStageK / 8), per = (n8 + 31) / 32;
     float inv = 1.f;   // undoes the activations' power of two
     bool bf = false;
-    if (!E8 && g.xq.codes) {   // code times E4M3 scale: exact in fp16 as it is
-      for (int w = wid; w < g.T * per; w += kFewWarps) {
-        const int t = w / per, c = (w - t * per) * 32 + lane, k = k0 + c * 8;
-        if (c >= n8) continue;
-        uint32_t h[4] = {0u, 0u, 0u, 0u};
-        if (k < g.cols) {
-          code_pairs<false>(__ldg(reinterpret_cast<const uint32_t*>(g.xq.codes + (int64_t)t * g.xq.pitch + k / 2)), h);
-          const uint32_t m = __byte_perm(e4m3x2_f16(g.xq.scales[micro_scale_at(g.xq.tiles, t, k / 16)]), 0u, 0x1010u);
+    // each(t, c, raw): place c of token t, four places of a thread requested at a time
+    const auto each = [&](auto&& use) {
+      const int items = g.T * per;
+      for (int w0 = wid; w0 < items; w0 += 4 * kFewWarps) {
+        uint4 q[4];
+        int t[4], c[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) h[i] = mul2<false>(h[i], m);
+        for (int i = 0; i < 4; ++i) {
+          const int w = w0 + i * kFewWarps;
+          t[i] = w / per;
+          c[i] = (w - t[i] * per) * 32 + lane;
+          if (w < items && c[i] < n8) q[i] = few_raw(g, FMT, t[i], k0 + c[i] * 8);
+          else c[i] = -1;
         }
-        *reinterpret_cast<uint4*>(xs + (size_t)t * g.x_pitch + (size_t)c * 16) = make_uint4(h[0], h[1], h[2], h[3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (c[i] >= 0) *reinterpret_cast<uint4*>(xs + (size_t)t[i] * g.x_pitch + (size_t)c[i] * 16) = use(q[i]);
       }
+    };
+    if (!E8 && g.xq.codes) {   // code times E4M3 scale: exact in fp16 as it is
+      each([&](const uint4& q) {
+        uint32_t h[4];
+        code_pairs<false>(q.x, h);
+        const uint32_t m = __byte_perm(e4m3x2_f16(q.y), 0u, 0x1010u);
+        return make_uint4(mul2<false>(h[0], m), mul2<false>(h[1], m), mul2<false>(h[2], m), mul2<false>(h[3], m));
+      });
       bar_consumers();
     } else {
       // In fp16 times mul; whether all of them are exact there; the largest finite magnitude.
       const auto stage = [&](float mul) {
         bool inexact = false;
         float m = 0.f;
-        for (int w = wid; w < g.T * per; w += kFewWarps) {
-          const int t = w / per, c = (w - t * per) * 32 + lane;
-          if (c >= n8) continue;
+        each([&](const uint4& raw) {
           float v[8];
-          few_x8(g, FMT, t, k0 + c * 8, v);
+          few_values(g, FMT, raw, v);
           uint32_t h[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -359,15 +378,10 @@ __global__ void __launch_bounds__(kFewThreads, 1)
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             if (fabsf(v[i]) <= 3.402823466e38f) m = fmaxf(m, fabsf(v[i]));
-          *reinterpret_cast<uint4*>(xs + (size_t)t * g.x_pitch + (size_t)c * 16) = make_uint4(h[0], h[1], h[2], h[3]);
-        }
-        if (inexact) {
-          inexact_any = 1;
-          atomicMax(&top, __float_as_uint(m));
-        } else if (m > 0.f && g.T * per > 0) {
-          const uint32_t b = __float_as_uint(m);
-          if (b > *(volatile uint32_t*)&top) atomicMax(&top, b);
-        }
+          return make_uint4(h[0], h[1], h[2], h[3]);
+        });
+        if (inexact) inexact_any = 1;
+        if (__float_as_uint(m) > *(volatile uint32_t*)&top) atomicMax(&top, __float_as_uint(m));
         bar_consumers();
         return inexact_any != 0;
       };
@@ -383,19 +397,17 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         if (bf) {
           inv = 1.f;
           bar_consumers();
-          for (int w = wid; w < g.T * per; w += kFewWarps) {
-            const int t = w / per, c = (w - t * per) * 32 + lane;
-            if (c >= n8) continue;
+          each([&](const uint4& raw) {
             float v[8];
-            few_x8(g, FMT, t, k0 + c * 8, v);
+            few_values(g, FMT, raw, v);
             uint32_t h[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const __nv_bfloat162 f = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);   // exact
               h[i] = *reinterpret_cast<const uint32_t*>(&f);
             }
-            *reinterpret_cast<uint4*>(xs + (size_t)t * g.x_pitch + (size_t)c * 16) = make_uint4(h[0], h[1], h[2], h[3]);
-          }
+            return make_uint4(h[0], h[1], h[2], h[3]);
+          });
           bar_consumers();
         }
       }
@@ -411,15 +423,16 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     const bool halves = nk == 1;
     const int rs = 128 / g.splits;                              // rows that a CTA stores
     const int owner = 16 * rt / rs, orow = 16 * rt - owner * rs + (lane >> 2);
-    int n = 0, it = 0;   // stages of all tiles so far
+    int st = -1, it = 0;     // slot of the ring and its phase's parity
+    uint32_t ph = 0;
     for (int mi = blockIdx.x; mi < g.mt; mi += gridDim.x, ++it) {
       float acc[NA][NT][4] = {};
-      for (int i = 0; i < nk && ok; ++i, ++n) {
-        if (!halves && (i & 1) != kh) continue;
-        const int st = n % S;
-        if (lane == 0) ok = mbar_wait(full + st, (uint32_t)(n / S) & 1u, g.spin);
+      for (int i = 0; i < nk; ++i) {
+        if (++st == S) st = 0, ph ^= 1u;
+        if (!ok || (!halves && (i & 1) != kh)) continue;
+        if (lane == 0) ok = mbar_wait(full + st, ph, g.spin);
         ok = __all_sync(0xFFFFFFFFu, ok);
-        if (!ok) break;
+        if (!ok) continue;
         const uint32_t code = smem_u32(sm) + (uint32_t)st * g.stage, sf = code + NA * kCodeTile;
         const int left = g.tiles - (st0 + i) * CPS;
         uint32_t xi[NT];
@@ -539,16 +552,17 @@ bool few_plan(int format, bool glu, int T, int rows, int cols, int (*resident)(i
   const int NA = glu ? 2 : 1, CPS = format == BITSMOE_MICRO_E8M0 ? 2 : 4;
   const int nst = (cols + kStageK - 1) / kStageK, mt = (rows + 127) / 128;
   p->stage = (uint32_t)NA * (kCodeTile + (uint32_t)CPS * 512);
-  const size_t red = 2 * (size_t)few_red_bytes(NA, T > 8 ? 2 : 1), room = 225 * 1024 - 1024 - 512;
+  const size_t room = 225 * 1024 - 1024 - 512;
   int64_t best = -1;
   for (int splits = 1; splits <= 8; splits *= 2) {   // CTAs of a cluster: the fewest of those with the least work a CTA
     const int sps = (nst + splits - 1) / splits;
     // 64 bytes beyond a multiple of 128: the tokens of a fragment's 16-byte loads in different banks
     const uint32_t pitch = (uint32_t)sps * kStageK * 2 + 64;
     const size_t xb = (size_t)T * pitch;
-    if (xb + red + 2 * (size_t)p->stage > room) continue;
     const int clusters = std::min(mt, resident(splits));
     if (clusters < 1) continue;
+    const size_t red = (size_t)few_red_bytes(NA, T > 8 ? 2 : 1) * (mt > clusters ? 2 : 1);
+    if (xb + red + 2 * (size_t)p->stage > room) continue;
     const int64_t work = (int64_t)((mt + clusters - 1) / clusters) * sps;
     if (best >= 0 && work >= best) continue;
     best = work;
