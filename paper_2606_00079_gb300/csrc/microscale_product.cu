@@ -48,9 +48,9 @@ constexpr int kFewTokens = 16;
 constexpr int kStageK = 256;                       // columns of a stage (128 bytes of codes a row)
 constexpr uint32_t kCodeTile = 128 * 128;          // bytes of 128 rows of a stage's codes
 
-// Bytes of a CTA's buffer of partial sums: 2 halves x matrices x tokens x 128 rows (a CTA's share of the rows
-// from every CTA of the cluster).
-__host__ __device__ constexpr uint32_t few_red_bytes(int na, int nt) { return 2u * na * nt * 8 * 512; }
+// Bytes of a CTA's buffer of partial sums: 2 groups of warps x tokens x 128 rows (a CTA's share of the rows from
+// every CTA of the cluster).
+__host__ __device__ constexpr uint32_t few_red_bytes(int nt) { return 2u * nt * 8 * 512; }
 
 struct FewArgs {
   int T, rows, cols, tiles, mt;
@@ -130,12 +130,11 @@ __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
 // E8M0: the 32 columns are a block of each row; its scale (times inv, a pair of bf16) multiplies the products' fp32 sum.
 // E4M3: a lane's 8 columns lie in one block, whose scale multiplies the codes (6 significant bits between 2^-10
 // and 2688: exact in fp16 and bf16).
-template <int FMT, int NA, int NT, bool BF>
+template <int FMT, int NT, bool BF>
 __device__ __forceinline__ void few_half(uint32_t code, uint32_t sf, const uint32_t (&xo)[NT], int rt, int kh, int lane,
-                                         int tiles_left, uint32_t inv, float (&acc)[NA][NT][4]) {
+                                         int tiles_left, uint32_t inv, float (&acc)[NT][4]) {
   constexpr bool E8 = FMT == BITSMOE_MICRO_E8M0;
   constexpr int TPH = E8 ? 1 : 2;   // scale tiles of a half
-  constexpr int CPS = 2 * TPH;
   const int g = lane >> 2, t = lane & 3;
   const int r = 16 * rt + g;
   const uint32_t pick = t >= 2 ? 0x3232u : 0x1010u;   // E4M3: this lane's block of the two of 32 columns
@@ -143,70 +142,63 @@ __device__ __forceinline__ void few_half(uint32_t code, uint32_t sf, const uint3
   for (int q = 0; q < TPH; ++q) {
     const int tile = kh * TPH + q;
     if (tile >= tiles_left) return;   // past the matrix's columns (and its scales)
-    uint32_t sw[NA][2];
+    uint32_t sw[2];
 #pragma unroll
-    for (int a = 0; a < NA; ++a)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int rr = r + 8 * h;
-        sw[a][h] = lds32(sf + (uint32_t)(a * CPS + tile) * 512 + (rr & 31) * 16 + (rr >> 5) * 4);
-      }
+    for (int h = 0; h < 2; ++h) {
+      const int rr = r + 8 * h;
+      sw[h] = lds32(sf + (uint32_t)tile * 512 + (rr & 31) * 16 + (rr >> 5) * 4);
+    }
 #pragma unroll
     for (int b = 0; b < 4 / TPH; ++b) {
       const int j = kh * 4 + q * 2 + b;   // 32 columns: 16-byte chunk of the row
       uint4 xb[NT];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        xb[n] = lds128a(xo[n] + (uint32_t)j * 64);
-      }
+      for (int n = 0; n < NT; ++n) xb[n] = lds128a(xo[n] + (uint32_t)j * 64);
+      const uint32_t base = code + (uint32_t)r * 128 + (uint32_t)((j ^ g) << 4) + t * 4;
+      uint32_t p0[4], p1[4];
+      code_pairs<BF>(lds32(base), p0);
+      code_pairs<BF>(lds32(base + 1024), p1);
+      if constexpr (E8) {
+        float s[2];
 #pragma unroll
-      for (int a = 0; a < NA; ++a) {
-        const uint32_t base = code + (uint32_t)a * kCodeTile + (uint32_t)r * 128 + (uint32_t)((j ^ g) << 4) + t * 4;
-        uint32_t p0[4], p1[4];
-        code_pairs<BF>(lds32(base), p0);
-        code_pairs<BF>(lds32(base + 1024), p1);
-        if constexpr (E8) {
-          float s[2];
+        for (int h = 0; h < 2; ++h) {
+          uint32_t v;
+          asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(v) : "h"((uint16_t)(sw[h] >> (16 * (b >> 1)))));
+          v = mul2<true>(v, inv);
+          s[h] = (b & 1) ? bf16hi(v) : bf16lo(v);
+        }
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t v;
-            asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(v) : "h"((uint16_t)(sw[a][h] >> (16 * (b >> 1)))));
-            v = mul2<true>(v, inv);
-            s[h] = (b & 1) ? bf16hi(v) : bf16lo(v);
+        for (int n = 0; n < NT; ++n) {
+          float d[4], e[4];
+          mma16<BF>(d, {p0[0], p1[0], p0[1], p1[1]}, xb[n].x, xb[n].y, zero);
+          mma16<BF>(e, {p0[2], p1[2], p0[3], p1[3]}, xb[n].z, xb[n].w, d);
+          acc[n][0] = fmaf(s[0], e[0], acc[n][0]);
+          acc[n][1] = fmaf(s[0], e[1], acc[n][1]);
+          acc[n][2] = fmaf(s[1], e[2], acc[n][2]);
+          acc[n][3] = fmaf(s[1], e[3], acc[n][3]);
+        }
+      } else {
+        uint32_t m[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          m[h] = e4m3x2_f16(sw[h] >> (16 * b));
+          if constexpr (BF) {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(f16lo(m[h]), f16hi(m[h]));   // exact
+            m[h] = *reinterpret_cast<const uint32_t*>(&v);
           }
-          const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+          m[h] = __byte_perm(m[h], 0u, pick);
+        }
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            float d[4], e[4];
-            mma16<BF>(d, {p0[0], p1[0], p0[1], p1[1]}, xb[n].x, xb[n].y, zero);
-            mma16<BF>(e, {p0[2], p1[2], p0[3], p1[3]}, xb[n].z, xb[n].w, d);
-            acc[a][n][0] = fmaf(s[0], e[0], acc[a][n][0]);
-            acc[a][n][1] = fmaf(s[0], e[1], acc[a][n][1]);
-            acc[a][n][2] = fmaf(s[1], e[2], acc[a][n][2]);
-            acc[a][n][3] = fmaf(s[1], e[3], acc[a][n][3]);
-          }
-        } else {
-          uint32_t m[2];
+        for (int i = 0; i < 4; ++i) {
+          p0[i] = mul2<BF>(p0[i], m[0]);
+          p1[i] = mul2<BF>(p1[i], m[1]);
+        }
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            m[h] = e4m3x2_f16(sw[a][h] >> (16 * b));
-            if constexpr (BF) {
-              const __nv_bfloat162 v = __floats2bfloat162_rn(f16lo(m[h]), f16hi(m[h]));   // exact
-              m[h] = *reinterpret_cast<const uint32_t*>(&v);
-            }
-            m[h] = __byte_perm(m[h], 0u, pick);
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p0[i] = mul2<BF>(p0[i], m[0]);
-            p1[i] = mul2<BF>(p1[i], m[1]);
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            float d[4];
-            mma16<BF>(d, {p0[0], p1[0], p0[1], p1[1]}, xb[n].x, xb[n].y, acc[a][n]);
-            mma16<BF>(acc[a][n], {p0[2], p1[2], p0[3], p1[3]}, xb[n].z, xb[n].w, d);
-          }
+        for (int n = 0; n < NT; ++n) {
+          float d[4];
+          mma16<BF>(d, {p0[0], p1[0], p0[1], p1[1]}, xb[n].x, xb[n].y, acc[n]);
+          mma16<BF>(acc[n], {p0[2], p1[2], p0[3], p1[3]}, xb[n].z, xb[n].w, d);
         }
       }
     }
@@ -270,7 +262,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   __shared__ int inexact_any;
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const int S = g.stages;
-  constexpr uint32_t kRed = few_red_bytes(NA, NT);   // [rank][half][matrix][token][rows of this CTA] fp32
+  constexpr uint32_t kRed = few_red_bytes(NT);   // [rank][group of warps][token][rows of this CTA] fp32
   uint8_t* redb = sm + (size_t)S * g.stage;          // two of them
   uint8_t* xs = redb + (g.mt > (int)gridDim.x ? 2 : 1) * kRed;
   uint64_t* full = reinterpret_cast<uint64_t*>(xs + (size_t)g.T * g.x_pitch);
@@ -286,7 +278,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   if (tid == 0) {
     for (int i = 0; i < S; ++i) {
       mbar_init_n(full + i, 1);
-      mbar_init_n(empty + i, nk == 1 ? kFewWarps : kFewWarps / 2);
+      mbar_init_n(empty + i, !GLU && nk == 1 ? kFewWarps : kFewWarps / 2);
     }
     for (int i = 0; i < 2; ++i) mbar_init_n(rfull + i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -302,18 +294,16 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     if (lane == 0) {
       int st = 0, u = 0, n = 0;
       for (int mi = blockIdx.x; mi < g.mt && ok; mi += gridDim.x) {
-        for (int i = 0; i < nk; ++i, ++n) {
+        for (int i = 0; i < nk * NA; ++i, ++n) {
           if (u > 0) ok = mbar_wait(empty + st, (uint32_t)(u - 1) & 1u, g.spin);
           if (!ok) break;
-          const int kb = st0 + i, cnt = min(CPS, g.tiles - kb * CPS);
+          const bool second = GLU && (i & 1);
+          const int kb = st0 + (GLU ? i >> 1 : i), cnt = min(CPS, g.tiles - kb * CPS);
           uint8_t* base = sm + (size_t)st * g.stage;
-          const uint32_t bar = smem_u32(full + st);
-          mbar_expect_tx(full + st, NA * (kCodeTile + (uint32_t)cnt * 512u));
-          tma_load_2d(smem_u32(base), &wmap, kb * 128, mi * 128, bar);
-          if (GLU) tma_load_2d(smem_u32(base) + kCodeTile, &umap, kb * 128, mi * 128, bar);
-          const size_t at = ((size_t)mi * g.tiles + (size_t)kb * CPS) * 512;
-          bulk_g2s(base + NA * kCodeTile, g.ws + at, (uint32_t)cnt * 512u, full + st);
-          if (GLU) bulk_g2s(base + NA * kCodeTile + CPS * 512, g.us + at, (uint32_t)cnt * 512u, full + st);
+          mbar_expect_tx(full + st, kCodeTile + (uint32_t)cnt * 512u);
+          tma_load_2d(smem_u32(base), second ? &umap : &wmap, kb * 128, mi * 128, smem_u32(full + st));
+          bulk_g2s(base + kCodeTile, (second ? g.us : g.ws) + ((size_t)mi * g.tiles + (size_t)kb * CPS) * 512, (uint32_t)cnt * 512u,
+                   full + st);
           if (++st == S) {
             st = 0;
             ++u;
@@ -419,34 +409,34 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     for (int n = 0; n < NT; ++n)
       xo[n] = smem_u32(xs) + (uint32_t)min(n * 8 + (lane >> 2), g.T - 1) * g.x_pitch + (uint32_t)(lane & 3) * 16;
     const uint32_t inv2 = (__float_as_uint(inv) >> 16) * 0x10001u;   // a power of two from 2^-100 to 2^14: exact in bf16
-    // The two groups of eight warps take every other stage; a CTA with a single one, half of its columns each.
-    const bool halves = nk == 1;
+    // The two groups of eight warps take every other slot (with GLU: one matrix each); of a single one, half of its
+    // columns each.
+    const bool halves = !GLU && nk == 1;
     const int rs = 128 / g.splits;                              // rows that a CTA stores
     const int owner = 16 * rt / rs, orow = 16 * rt - owner * rs + (lane >> 2);
     int st = -1, it = 0;     // slot of the ring and its phase's parity
     uint32_t ph = 0;
     for (int mi = blockIdx.x; mi < g.mt; mi += gridDim.x, ++it) {
-      float acc[NA][NT][4] = {};
-      for (int i = 0; i < nk; ++i) {
+      float acc[NT][4] = {};
+      for (int i = 0; i < nk * NA; ++i) {
         if (++st == S) st = 0, ph ^= 1u;
         if (!ok || (!halves && (i & 1) != kh)) continue;
         if (lane == 0) ok = mbar_wait(full + st, ph, g.spin);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) continue;
-        const uint32_t code = smem_u32(sm) + (uint32_t)st * g.stage, sf = code + NA * kCodeTile;
-        const int left = g.tiles - (st0 + i) * CPS;
+        const uint32_t code = smem_u32(sm) + (uint32_t)st * g.stage, sf = code + kCodeTile;
+        const int ks = GLU ? i >> 1 : i, left = g.tiles - (st0 + ks) * CPS;
         uint32_t xi[NT];
 #pragma unroll
-        for (int q = 0; q < NT; ++q) xi[q] = xo[q] + (uint32_t)i * (kStageK * 2);
+        for (int q = 0; q < NT; ++q) xi[q] = xo[q] + (uint32_t)ks * (kStageK * 2);
+        // one copy of the code for both halves: unrolled, it did not stay in the instruction cache
+        const int h0 = halves ? kh : 0, h1 = halves ? kh + 1 : 2;
         if (bf) {
 #pragma unroll 1
-          for (int h = halves ? kh : 0; h < (halves ? kh + 1 : 2); ++h)
-            few_half<FMT, NA, NT, true>(code, sf, xi, rt, h, lane, left, inv2, acc);
-        } else if (halves) {
-          few_half<FMT, NA, NT, false>(code, sf, xi, rt, kh, lane, left, inv2, acc);
+          for (int h = h0; h < h1; ++h) few_half<FMT, NT, true>(code, sf, xi, rt, h, lane, left, inv2, acc);
         } else {
-          few_half<FMT, NA, NT, false>(code, sf, xi, rt, 0, lane, left, inv2, acc);
-          few_half<FMT, NA, NT, false>(code, sf, xi, rt, 1, lane, left, inv2, acc);
+#pragma unroll 1
+          for (int h = h0; h < h1; ++h) few_half<FMT, NT, false>(code, sf, xi, rt, h, lane, left, inv2, acc);
         }
         __syncwarp();
         if (lane == 0 && !(g.lose && i == 0 && it == 0 && wid == 0 && (blockIdx.x | blockIdx.y) == 0)) mbar_arrive(empty + st);
@@ -458,16 +448,14 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(smem_u32(rfull + (it & 1))), "r"(owner));
       const float unit = E8 ? 1.f : inv;
 #pragma unroll
-      for (int a = 0; a < NA; ++a)
+      for (int q = 0; q < NT; ++q)
 #pragma unroll
-        for (int q = 0; q < NT; ++q)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int c = q * 8 + (lane & 3) * 2 + (j & 1);
-            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::
-                             "r"(dst + (uint32_t)((((rank * 2 + kh) * NA + a) * NT * 8 + c) * rs + orow + (j >> 1) * 8) * 4u),
-                         "r"(__float_as_uint(acc[a][q][j] * unit)), "r"(bar) : "memory");
-          }
+        for (int j = 0; j < 4; ++j) {
+          const int c = q * 8 + (lane & 3) * 2 + (j & 1);
+          asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::
+                           "r"(dst + (uint32_t)(((rank * 2 + kh) * NT * 8 + c) * rs + orow + (j >> 1) * 8) * 4u),
+                       "r"(__float_as_uint(acc[q][j] * unit)), "r"(bar) : "memory");
+        }
       if (mi + (int)gridDim.x >= g.mt) {   // everything sent: the others may leave once they have their parts
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
@@ -478,21 +466,17 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       ok = __all_sync(0xFFFFFFFFu, ok);
       for (int e = tid; e < rs * g.T; e += kFewWarps * 32) {
         const int c = e / rs, r = e - c * rs;
-        float sum[NA];
+        float p[16];   // [CTA][group]
 #pragma unroll
-        for (int a = 0; a < NA; ++a) {
-          float p[16];
+        for (int q = 0; q < 16; ++q)
+          p[q] = q < 2 * g.splits ? __uint_as_float(lds32(buf + (uint32_t)((q * NT * 8 + c) * rs + r) * 4u)) : 0.f;
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-          for (int q = 0; q < 16; ++q)
-            p[q] = q < 2 * g.splits ? __uint_as_float(lds32(buf + (uint32_t)(((q * NA + a) * NT * 8 + c) * rs + r) * 4u)) : 0.f;
-          sum[a] = 0.f;
-#pragma unroll
-          for (int q = 0; q < 16; ++q) sum[a] += p[q];
-        }
+        for (int q = 0; q < 16; ++q) sum[GLU ? q & 1 : 0] += p[q];
         const int m = mi * 128 + rank * rs + r;
         if (m >= g.rows) continue;
         float o = sum[0] * g.sw;
-        if (GLU) o = silu_mul(o, sum[NA - 1] * g.su);
+        if (GLU) o = silu_mul(o, sum[1] * g.su);
         store_y(g.y, g.y_type, (int64_t)c * g.y_ld + m, o);
       }
       __syncwarp();
@@ -547,11 +531,11 @@ struct FewPlan {
 };
 
 // How T tokens run on the kernel for few of them, or false when their activations do not fit shared memory.
-bool few_plan(int format, bool glu, int T, int rows, int cols, int (*resident)(int), FewPlan* p) {
+bool few_plan(int format, int T, int rows, int cols, int (*resident)(int), FewPlan* p) {
   if (T > kFewTokens) return false;
-  const int NA = glu ? 2 : 1, CPS = format == BITSMOE_MICRO_E8M0 ? 2 : 4;
+  const int CPS = format == BITSMOE_MICRO_E8M0 ? 2 : 4;
   const int nst = (cols + kStageK - 1) / kStageK, mt = (rows + 127) / 128;
-  p->stage = (uint32_t)NA * (kCodeTile + (uint32_t)CPS * 512);
+  p->stage = kCodeTile + (uint32_t)CPS * 512;
   const size_t room = 225 * 1024 - 1024 - 512;
   int64_t best = -1;
   for (int splits = 1; splits <= 8; splits *= 2) {   // CTAs of a cluster: the fewest of those with the least work a CTA
@@ -561,8 +545,8 @@ bool few_plan(int format, bool glu, int T, int rows, int cols, int (*resident)(i
     const size_t xb = (size_t)T * pitch;
     const int clusters = std::min(mt, resident(splits));
     if (clusters < 1) continue;
-    const size_t red = (size_t)few_red_bytes(NA, T > 8 ? 2 : 1) * (mt > clusters ? 2 : 1);
-    if (xb + red + 2 * (size_t)p->stage > room) continue;
+    const size_t red = (size_t)few_red_bytes(T > 8 ? 2 : 1) * (mt > clusters ? 2 : 1);
+    if (xb + red + 6 * (size_t)p->stage > room) continue;   // slots enough to cover a copy's latency
     const int64_t work = (int64_t)((mt + clusters - 1) / clusters) * sps;
     if (best >= 0 && work >= best) continue;
     best = work;
@@ -1406,7 +1390,7 @@ extern "C" int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bit
   if (e != cudaSuccess) return record_cuda_error((int)e);
   const bool e8 = w->format == BITSMOE_MICRO_E8M0;
   FewPlan fp;
-  if (few_plan(w->format, up != nullptr, T, w->rows, w->cols, few_resident, &fp)) {
+  if (few_plan(w->format, T, w->rows, w->cols, few_resident, &fp)) {
     FewArgs f;
     std::memset(&f, 0, sizeof(f));
     f.T = T;
