@@ -249,9 +249,9 @@ __device__ __forceinline__ void few_values(const FewArgs& g, int format, const u
   }
 }
 
-// A cluster takes row tiles of 128 one after the other; its CTAs split the columns.  Each warp adds its part of a
-// tile to the CTA that stores those rows, by remote stores into that CTA's shared memory, two buffers in turn
-// (a CTA that has all parts of tile i + 1 knows that every CTA is done with its buffer of tile i).
+// A cluster takes row tiles of 128 one after the other; its CTAs split the columns.  Each warp sends its part of a
+// tile to the CTA that stores those rows, by asynchronous stores into that CTA's shared memory; the next tile's
+// parts wait until every CTA has read this one's.
 template <int FMT, bool GLU, int NT>
 __global__ void __launch_bounds__(kFewThreads, 1)
     k_micro_few(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, FewArgs g) {
@@ -263,11 +263,12 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const int S = g.stages;
   constexpr uint32_t kRed = few_red_bytes(NT);   // [rank][group of warps][token][rows of this CTA] fp32
-  uint8_t* redb = sm + (size_t)S * g.stage;          // two of them
-  uint8_t* xs = redb + (g.mt > (int)gridDim.x ? 2 : 1) * kRed;
+  uint8_t* redb = sm + (size_t)S * g.stage;
+  uint8_t* xs = redb + kRed;
   uint64_t* full = reinterpret_cast<uint64_t*>(xs + (size_t)g.T * g.x_pitch);
   uint64_t* empty = full + S;
-  uint64_t* rfull = empty + S;                        // [2] the parts of a tile are there
+  uint64_t* rfull = empty + S;                        // the parts of a tile are there
+  uint64_t* rfree = rfull + 1;                        // every CTA of the cluster has read them
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int rank = blockIdx.y;
   const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
@@ -280,9 +281,10 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       mbar_init_n(full + i, 1);
       mbar_init_n(empty + i, !GLU && nk == 1 ? kFewWarps : kFewWarps / 2);
     }
-    for (int i = 0; i < 2; ++i) mbar_init_n(rfull + i, 1);
+    mbar_init_n(rfull, 1);
+    mbar_init_n(rfree, (uint32_t)g.splits);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    for (int i = 0; i < 2; ++i) mbar_expect_tx(rfull + i, kRed);
+    mbar_expect_tx(rfull, kRed);
     top = 0u;
     inexact_any = 0;
   }
@@ -442,10 +444,14 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         if (lane == 0 && !(g.lose && i == 0 && it == 0 && wid == 0 && (blockIdx.x | blockIdx.y) == 0)) mbar_arrive(empty + st);
       }
       // this warp's part to the CTA that stores these rows, counted in bytes on its barrier
+      if (it > 0) {
+        if (ok && lane == 0) ok = mbar_wait_cluster(rfree, (uint32_t)(it - 1) & 1u, g.spin);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+      }
       uint32_t dst, bar;
-      const uint32_t buf = smem_u32(redb) + (uint32_t)(it & 1) * kRed;
+      const uint32_t buf = smem_u32(redb);
       asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"(buf), "r"(owner));
-      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(smem_u32(rfull + (it & 1))), "r"(owner));
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(smem_u32(rfull)), "r"(owner));
       const float unit = E8 ? 1.f : inv;
 #pragma unroll
       for (int q = 0; q < NT; ++q)
@@ -462,7 +468,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       }
       // the parts of this CTA's rows, added in the order of the CTAs and halves
       // (a warp whose wait ran out sends and stores nothing of use from then on, but keeps every barrier)
-      if (ok && lane == 0) ok = mbar_wait_cluster(rfull + (it & 1), (uint32_t)(it >> 1) & 1u, g.spin);
+      if (ok && lane == 0) ok = mbar_wait_cluster(rfull, (uint32_t)it & 1u, g.spin);
       ok = __all_sync(0xFFFFFFFFu, ok);
       for (int e = tid; e < rs * g.T; e += kFewWarps * 32) {
         const int c = e / rs, r = e - c * rs;
@@ -480,8 +486,15 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         store_y(g.y, g.y_type, (int64_t)c * g.y_ld + m, o);
       }
       __syncwarp();
-      bar_consumers();   // the whole CTA is done with this buffer before any of its warps sends tile i + 1
-      if (tid == 0 && ok) mbar_expect_tx(rfull + (it & 1), kRed);   // for tile i + 2
+      if (mi + (int)gridDim.x < g.mt) {
+        bar_consumers();   // the whole CTA has read the parts
+        if (tid == 0 && ok) mbar_expect_tx(rfull, kRed);   // for the next tile
+        if (tid < g.splits) {
+          uint32_t to;
+          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_u32(rfree)), "r"(tid));
+          asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(to) : "memory");
+        }
+      }
     }
   }
   // No CTA leaves while others may still write to its shared memory: it has all parts that are sent to it, or,
@@ -531,7 +544,10 @@ struct FewPlan {
 };
 
 // How T tokens run on the kernel for few of them, or false when their activations do not fit shared memory.
-bool few_plan(int format, int T, int rows, int cols, int (*resident)(int), FewPlan* p) {
+// Measured (us): a 16-bit token takes 12.4 here and 29.4 by the decoded tiles (4096 rows x 14336), 16 tokens 23.4 and
+// 29.8, 24 tokens 41.5 and 29.9; for coded tokens the block-scaled MMAs take 10.2 at 1 to 24 tokens, so only small
+// products stay here (2048 x 2048: 5.0 to 6.6 against 9.3 to 10.1).
+bool few_plan(int format, bool glu, bool coded, int T, int rows, int cols, int (*resident)(int), FewPlan* p) {
   if (T > kFewTokens) return false;
   const int CPS = format == BITSMOE_MICRO_E8M0 ? 2 : 4;
   const int nst = (cols + kStageK - 1) / kStageK, mt = (rows + 127) / 128;
@@ -545,8 +561,8 @@ bool few_plan(int format, int T, int rows, int cols, int (*resident)(int), FewPl
     const size_t xb = (size_t)T * pitch;
     const int clusters = std::min(mt, resident(splits));
     if (clusters < 1) continue;
-    const size_t red = (size_t)few_red_bytes(T > 8 ? 2 : 1) * (mt > clusters ? 2 : 1);
-    if (xb + red + 6 * (size_t)p->stage > room) continue;   // slots enough to cover a copy's latency
+    const size_t red = (size_t)few_red_bytes(T > 8 ? 2 : 1);
+    if (xb + red + 5 * (size_t)p->stage > room) continue;   // slots enough to cover a copy's latency
     const int64_t work = (int64_t)((mt + clusters - 1) / clusters) * sps;
     if (best >= 0 && work >= best) continue;
     best = work;
@@ -557,7 +573,7 @@ bool few_plan(int format, int T, int rows, int cols, int (*resident)(int), FewPl
     p->stages = (int)std::min<size_t>((room - xb - red) / p->stage, 16);
     p->smem = 1024 + (size_t)p->stages * p->stage + red + xb + (size_t)(2 * p->stages + 2) * 8;
   }
-  return best >= 0;
+  return best >= 0 && !(coded && best * (glu ? 2 : 1) * (T > 8 ? 2 : 1) > 8);
 }
 
 template <int FMT, bool GLU, int NT>
@@ -1018,19 +1034,22 @@ struct WideArgs {
 };
 
 // 32 codes (four words) of one row times their block scales -> 64 bytes of bf16 in a 128-byte swizzled tile.  Codes
-// become fp16 pairs by one conversion each, products in fp32 are exact, and so is their rounding to bf16 (at most 6
-// significant bits; E8M0's largest scales overflow as fp32 does): 8 operations of the integer pipe for 8 codes, where
-// moving the bits into place takes 17.
+// become fp16 pairs by one conversion each and bf16 pairs by way of fp32; their products with the scales are exact
+// in bf16 (at most 6 significant bits; E8M0's largest scales overflow as fp32 does): 8 operations of the integer
+// pipe for 8 codes, where moving the bits into place takes 17.
 template <int FMT>
 __device__ __forceinline__ void decode32(const uint4& v, uint32_t sc, uint8_t* row, int half, int r7) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  float f[2];
+  uint32_t f[2];
   if constexpr (FMT == BITSMOE_MICRO_E8M0) {
-    f[0] = f[1] = micro_e8m0(sc & 255u);
+    asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(f[0]) : "h"((uint16_t)((sc & 255u) * 0x101u)));
+    f[1] = f[0];
   } else {
     const uint32_t p = e4m3x2_f16(sc);
-    f[0] = f16lo(p);
-    f[1] = f16hi(p);
+    f[0] = __float_as_uint(f16lo(p)) >> 16;   // 4 significant bits: exact
+    f[1] = __float_as_uint(f16hi(p)) >> 16;
+    f[0] |= f[0] << 16;
+    f[1] |= f[1] << 16;
   }
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
@@ -1039,8 +1058,8 @@ __device__ __forceinline__ void decode32(const uint4& v, uint32_t sc, uint8_t* r
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float2 c = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-      const __nv_bfloat162 b = __floats2bfloat162_rn(c.x * f[q >> 1], c.y * f[q >> 1]);
-      o[i] = *reinterpret_cast<const uint32_t*>(&b);
+      const __nv_bfloat162 b = __floats2bfloat162_rn(c.x, c.y);
+      o[i] = mul2<true>(*reinterpret_cast<const uint32_t*>(&b), f[q >> 1]);
     }
     *reinterpret_cast<uint4*>(row + (((half * 4 + q) ^ r7) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
   }
@@ -1390,7 +1409,7 @@ extern "C" int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bit
   if (e != cudaSuccess) return record_cuda_error((int)e);
   const bool e8 = w->format == BITSMOE_MICRO_E8M0;
   FewPlan fp;
-  if (few_plan(w->format, T, w->rows, w->cols, few_resident, &fp)) {
+  if (few_plan(w->format, up != nullptr, xq != nullptr, T, w->rows, w->cols, few_resident, &fp)) {
     FewArgs f;
     std::memset(&f, 0, sizeof(f));
     f.T = T;

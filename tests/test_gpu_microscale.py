@@ -224,7 +224,7 @@ def check_product(env, T, rows, cols, fmt, coded, glu, out, seed=0):
 
 PRODUCTS = [   # T, rows, cols
     (1, 1, 1), (1, 128, 64), (2, 3, 31), (1, 130, 33), (3, 127, 129), (5, 256, 256), (8, 129, 500), (16, 200, 1001),
-    (17, 384, 2048), (33, 65, 255), (64, 300, 320), (100, 257, 640), (128, 128, 512), (129, 140, 257), (255, 128, 96),
+    (17, 384, 2048), (31, 150, 300), (33, 65, 255), (64, 300, 320), (100, 257, 640), (128, 128, 512), (129, 140, 257), (255, 128, 96),
     (256, 256, 1024), (257, 130, 130), (300, 512, 768), (520, 1000, 200),
 ]
 
@@ -245,7 +245,7 @@ def test_product_swiglu(env, fmt, x, shape):
 
 
 @pytest.mark.parametrize("x", ["bf16", "coded"])
-@pytest.mark.parametrize("T,rows,cols", [(1, 4096, 14336), (7, 2048, 8192), (40, 1536, 4096), (700, 640, 4096)])
+@pytest.mark.parametrize("T,rows,cols", [(1, 4096, 14336), (7, 2048, 8192), (24, 6000, 2048), (16, 21000, 1536), (40, 1536, 4096), (700, 640, 4096)])
 def test_product_large(env, x, T, rows, cols):
     check_product(env, T, rows, cols, "e4m3", x == "coded", False, "f32")
     check_product(env, T, rows, cols, "e8m0", x == "coded", False, "bf16")
