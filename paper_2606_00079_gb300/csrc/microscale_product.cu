@@ -1017,7 +1017,7 @@ struct WideArgs {
   int T, rows, cols, tiles;
   int N, mt, ntiles, nbuf;
   int nst, sps, splits;
-  int P, Q, B;           // depths of the rings of codes, of bf16 weight tiles and of activations
+  int P, Q;              // depths of the rings of codes and of tiles
   uint32_t pst;          // bytes of a stage of codes
   int btma;              // x's rows are on 16-byte boundaries
   const uint8_t* ws;
@@ -1065,47 +1065,46 @@ __device__ __forceinline__ void decode32(const uint4& v, uint32_t sc, uint8_t* r
   }
 }
 
-template <int FMT, bool GLU>
+// KS: steps of 64 columns in a slot (two where tokens are few: a slot's barriers cost the MMA warp about 350 clocks,
+// as long as the products of 64 columns with 128 tokens).
+template <int FMT, bool GLU, int KS>
 __global__ void __launch_bounds__(kWideThreads, 1)
     k_micro_wide(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap,
                  const __grid_constant__ CUtensorMap xmap, const __grid_constant__ WideArgs g) {
   constexpr bool E8 = FMT == BITSMOE_MICRO_E8M0;
   constexpr int NA = GLU ? 2 : 1, CPS = E8 ? 2 : 4;
+  constexpr int kSlots = 4 / KS;   // slots of a stage of codes
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  const int P = g.P, Q = g.Q, B = g.B, N = g.N;
-  constexpr uint32_t kATile = NA * kCodeTile;   // a weight tile: 128 rows x 64 bf16, as many bytes as 256 columns of codes
-  const uint32_t b_bytes = (uint32_t)N * 128;
-  uint8_t* bring = sm + (size_t)Q * kATile;
-  uint8_t* pring = bring + (size_t)B * b_bytes;
+  const int P = g.P, Q = g.Q, N = g.N;
+  constexpr uint32_t kATile = NA * kCodeTile;   // 128 rows x 64 bf16, as many bytes as 256 columns of codes
+  const uint32_t b_bytes = (uint32_t)N * 128, step = kATile + b_bytes, qst = KS * step;   // a step: weights, activations
+  uint8_t* pring = sm + (size_t)Q * qst;
   float* red = reinterpret_cast<float*>(sm);   // split: [NA][N][128], reuses the rings
   uint64_t* pfull = reinterpret_cast<uint64_t*>(pring + (size_t)P * g.pst);
   uint64_t* pempty = pfull + P;
   uint64_t* qfull = pempty + P;
   uint64_t* qempty = qfull + Q;
-  uint64_t* bfull = qempty + Q;
-  uint64_t* bempty = bfull + B;
-  uint64_t* afull = bempty + B;
+  uint64_t* afull = qempty + Q;
   uint64_t* aempty = afull + 2;
   uint32_t* slot = reinterpret_cast<uint32_t*>(aempty + 2);
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int rank = blockIdx.y;
   const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
-  const int nks = (g.cols + 63) / 64;   // slots of 64 columns in all
-  const int s0 = st0 * 4, ns = max(0, min(nk * 4, nks - s0));   // this CTA's
+  const int s0 = st0 * 4, n64 = max(0, min(nk * 4, (g.cols + 63) / 64 - s0));   // this CTA's steps of 64 columns
+  const int ns = (n64 + KS - 1) / KS;                                            // and slots
 
   if (tid == 0) {
+    prefetch_map(&wmap);
+    prefetch_map(&xmap);
+    if (GLU) prefetch_map(&umap);
     for (int i = 0; i < P; ++i) {
       mbar_init_n(pfull + i, 1);
       mbar_init_n(pempty + i, kDecodeGroups * kDecodeWarps);
     }
     for (int i = 0; i < Q; ++i) {
-      mbar_init_n(qfull + i, kDecodeWarps);
+      mbar_init_n(qfull + i, kDecodeWarps + (g.btma ? 1 : 0));
       mbar_init_n(qempty + i, 1);
-    }
-    for (int i = 0; i < B; ++i) {
-      mbar_init_n(bfull + i, g.btma ? 1 : kDecodeWarps);
-      mbar_init_n(bempty + i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init_n(afull + i, 1);
@@ -1150,8 +1149,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     // converged, with one lane's predicate on the instructions: their operands stay in uniform registers (issued by
     // one lane of a diverged warp, the four products and the commit of a slot took 490 clocks)
     const uint32_t one = elect_one(), idesc = idesc_bf16(N);
-    const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(bring));
-    int st = 0, u = 0, bs = 0, bu = 0, it = 0;
+    const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(sm) + kATile);
+    int st = 0, u = 0, it = 0;
     for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x, ++it) {
       const int buf = it % g.nbuf, use = it / g.nbuf;
       if (use > 0) ok = mbar_wait(aempty + buf, (uint32_t)(use - 1) & 1u, g.spin);
@@ -1159,27 +1158,25 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       if (!ok) break;
       const uint32_t acc = tmem + (uint32_t)(buf * NA * N);
       for (int i = 0; i < ns; ++i) {
-        ok = mbar_wait(bfull + bs, (uint32_t)bu & 1u, g.spin) && mbar_wait(qfull + st, (uint32_t)u & 1u, g.spin);
+        ok = mbar_try_wait(qfull + st, (uint32_t)u & 1u) || mbar_wait(qfull + st, (uint32_t)u & 1u, g.spin);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint64_t a0 = da + (uint64_t)((uint32_t)st * (kATile >> 4)), b0 = db + (uint64_t)((uint32_t)bs * (b_bytes >> 4));
+        const uint64_t so = (uint64_t)((uint32_t)st * (qst >> 4)), a0 = da + so, b0 = db + so;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int s = 0; s < KS; ++s) {
+          if (s > 0 && i * KS + s >= n64) break;
+          const uint64_t o = (uint64_t)((uint32_t)s * (step >> 4));
 #pragma unroll
-          for (int a = 0; a < NA; ++a)
-            mma_f16(one, acc + (uint32_t)(a * N), a0 + a * (kCodeTile >> 4) + 2 * k, b0 + 2 * k, idesc, (uint32_t)(i | k));
-        if (!(g.lose && i == 0 && it == 0 && (blockIdx.x | blockIdx.y) == 0)) {
-          mma_commit(one, bempty + bs);
-          mma_commit(one, qempty + st);
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int a = 0; a < NA; ++a)
+              mma_f16(one, acc + (uint32_t)(a * N), a0 + o + a * (kCodeTile >> 4) + 2 * k, b0 + o + 2 * k, idesc, (uint32_t)(i | s | k));
         }
+        if (!(g.lose && i == 0 && it == 0 && (blockIdx.x | blockIdx.y) == 0)) mma_commit(one, qempty + st);
         if (++st == Q) {
           st = 0;
           ++u;
-        }
-        if (++bs == B) {
-          bs = 0;
-          ++bu;
         }
       }
       mma_commit(one, afull + buf);
@@ -1190,17 +1187,20 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x) {
         const int t0 = tile / g.mt * N;
         for (int i = 0; i < ns; ++i, ++n) {
-          if (u > 0) ok = mbar_wait(bempty + st, (uint32_t)(u - 1) & 1u, g.spin);
+          if (u > 0) ok = mbar_wait(qempty + st, (uint32_t)(u - 1) & 1u, g.spin);
           if (!ok) break;
-          mbar_expect_tx(bfull + st, b_bytes);
-          tma_load_2d(smem_u32(bring) + (uint32_t)st * b_bytes, &xmap, (s0 + i) * 64, t0, smem_u32(bfull + st));
-          if (++st == B) {
+          const int cnt = min(KS, n64 - i * KS);
+          mbar_expect_tx(qfull + st, (uint32_t)cnt * b_bytes);
+          for (int s = 0; s < cnt; ++s)
+            tma_load_2d(smem_u32(sm) + (uint32_t)st * qst + (uint32_t)s * step + kATile, &xmap, (s0 + i * KS + s) * 64, t0, smem_u32(qfull + st));
+          if (++st == Q) {
             st = 0;
             ++u;
           }
         }
       }
-      for (int j = max(0, n - B); j < n; ++j) mbar_wait(bfull + j % B, (uint32_t)(j / B) & 1u);   // copies in flight
+      // copies in flight: their bytes end a phase only with the decoders' arrivals, which may be missing after a timeout
+      for (int j = max(0, n - Q); j < n; ++j) mbar_wait(qfull + j % Q, (uint32_t)(j / Q) & 1u, ok ? kWaitClocks : g.spin);
     }
     __syncwarp();
   } else if (wid >= 4 && wid < 4 + kDecodeGroups * kDecodeWarps) {
@@ -1209,53 +1209,51 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     const int bt = dw * 32 + lane;
     const uint8_t* code = pring + r * 128;
     const uint8_t* scale = pring + NA * kCodeTile + (r & 31) * 16 + (r >> 5) * 4;
-    uint32_t ps = 0, pp = 0, qs = 0, qp = 0, bs = 0, bp = 0;   // slots of the three rings and their phases' parities
-    const auto next = [&](uint32_t& slot, uint32_t& parity, int depth) {
-      slot += kDecodeGroups;
-      while (slot >= (uint32_t)depth) slot -= depth, parity ^= 1u;
-    };
-    uint32_t n0 = group;   // this group's first slot of the tile
+    uint32_t ps = 0, pp = 0, n0 = group;   // slot of the codes' ring and its phase's parity; this group's first slot of the tile
     for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x, n0 += ns) {
       const int t0 = tile / g.mt * N;
-      qs = n0 % Q, qp = n0 / Q & 1u, bs = n0 % B, bp = n0 / B & 1u;
-      for (int i0 = 0; i0 < ns && ok; i0 += 4) {   // a stage: up to four slots, this group's every other one
+      uint32_t qs = n0 % Q, qp = n0 / Q & 1u;
+      for (int i0 = 0; i0 < ns && ok; i0 += kSlots) {   // a stage of codes: this group's every other slot
         ok = mbar_wait(pfull + ps, pp, g.spin);
-        for (int sub = group; sub < min(4, ns - i0) && ok; sub += kDecodeGroups) {
+        for (int sub = group; sub < min(kSlots, ns - i0) && ok; sub += kDecodeGroups) {
           const int i = i0 + sub;
-          ok = mbar_wait(qempty + qs, qp ^ 1u, g.spin) && (g.btma || mbar_wait(bempty + bs, bp ^ 1u, g.spin));
+          ok = mbar_try_wait(qempty + qs, qp ^ 1u) || mbar_wait(qempty + qs, qp ^ 1u, g.spin);
           if (!ok) break;
-          uint8_t* out = sm + (size_t)qs * kATile + r * 128;
 #pragma unroll
-          for (int a = 0; a < NA; ++a) {
-            const uint4 v = *reinterpret_cast<const uint4*>(code + (size_t)ps * g.pst + (size_t)a * kCodeTile + (((2 * sub + half) ^ r7) << 4));
-            const uint8_t* sc = scale + (size_t)ps * g.pst + (a * CPS + (E8 ? sub >> 1 : sub)) * 512;
-            const uint32_t f = E8 ? (uint32_t)sc[(sub & 1) * 2 + half] : (uint32_t)*reinterpret_cast<const uint16_t*>(sc + half * 2);
-            decode32<FMT>(v, f, out + (size_t)a * kCodeTile, half, r7);
-          }
-          if (!g.btma) {   // rows off 16-byte boundaries: 8 columns a thread at a time
-            const int k0 = (s0 + i) * 64;
-            for (int c = bt; c < N * 8; c += kDecodeWarps * 32) {
-              const int t = t0 + (c >> 3), k = k0 + (c & 7) * 8;
-              const uint16_t* xr = reinterpret_cast<const uint16_t*>(g.x) + (int64_t)t * g.x_ld + k;
-              uint32_t w[4];
+          for (int s = 0; s < KS; ++s) {
+            if (s > 0 && i * KS + s >= n64) break;
+            const int q = sub * KS + s;   // step of the stage
+            uint8_t* out = sm + (size_t)qs * qst + (size_t)s * step + r * 128;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t lo = t < g.T && k + 2 * e < g.cols ? xr[2 * e] : 0u;
-                const uint32_t hi = t < g.T && k + 2 * e + 1 < g.cols ? xr[2 * e + 1] : 0u;
-                w[e] = lo | (hi << 16);
+            for (int a = 0; a < NA; ++a) {
+              const uint4 v = *reinterpret_cast<const uint4*>(code + (size_t)ps * g.pst + (size_t)a * kCodeTile + (((2 * q + half) ^ r7) << 4));
+              const uint8_t* sc = scale + (size_t)ps * g.pst + (a * CPS + (E8 ? q >> 1 : q)) * 512;
+              const uint32_t f = E8 ? (uint32_t)sc[(q & 1) * 2 + half] : (uint32_t)*reinterpret_cast<const uint16_t*>(sc + half * 2);
+              decode32<FMT>(v, f, out + (size_t)a * kCodeTile, half, r7);
+            }
+            if (!g.btma) {   // rows off 16-byte boundaries: 8 columns a thread at a time
+              const int k0 = (s0 + i * KS + s) * 64;
+              for (int c = bt; c < N * 8; c += kDecodeWarps * 32) {
+                const int t = t0 + (c >> 3), k = k0 + (c & 7) * 8;
+                const uint16_t* xr = reinterpret_cast<const uint16_t*>(g.x) + (int64_t)t * g.x_ld + k;
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const uint32_t lo = t < g.T && k + 2 * e < g.cols ? xr[2 * e] : 0u;
+                  const uint32_t hi = t < g.T && k + 2 * e + 1 < g.cols ? xr[2 * e + 1] : 0u;
+                  w[e] = lo | (hi << 16);
+                }
+                const int rr = c >> 3;
+                *reinterpret_cast<uint4*>(sm + (size_t)qs * qst + (size_t)s * step + kATile + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
+                    make_uint4(w[0], w[1], w[2], w[3]);
               }
-              const int rr = c >> 3;
-              *reinterpret_cast<uint4*>(bring + (size_t)bs * b_bytes + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
             }
           }
           fence_proxy_async();   // generic writes -> tensor-core reads
           __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(qfull + qs);
-            if (!g.btma) mbar_arrive(bfull + bs);
-          }
-          next(qs, qp, Q);
-          next(bs, bp, B);
+          if (lane == 0) mbar_arrive(qfull + qs);
+          qs += kDecodeGroups;
+          while (qs >= (uint32_t)Q) qs -= Q, qp ^= 1u;
         }
         __syncwarp();
         if (lane == 0 && ok) mbar_arrive(pempty + ps);
@@ -1277,7 +1275,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         uint32_t v[NA][16];
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          if (ns > 0) {
+          if (n64 > 0) {
             tmem_ld16(tl + (uint32_t)(a * N + c0), v[a]);
           } else {
 #pragma unroll
@@ -1320,32 +1318,25 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   }
 }
 
-template <int FMT, bool GLU>
-cudaError_t launch_wide(const bitsmoe_microscale* w, const bitsmoe_microscale* up, WideArgs g, int dev, int sms, cudaStream_t st) {
+template <int FMT, bool GLU, int KS>
+cudaError_t launch_wide_k(const bitsmoe_microscale* w, const bitsmoe_microscale* up, WideArgs g, int dev, int sms, cudaStream_t st) {
   constexpr int NA = GLU ? 2 : 1, CPS = FMT == BITSMOE_MICRO_E8M0 ? 2 : 4;
   constexpr uint32_t kRoom = 216 * 1024;
-  int tt = (g.T + 255) / 256;
-  g.N = ((g.T + tt - 1) / tt + 15) / 16 * 16;
-  tt = (g.T + g.N - 1) / g.N;
+  const int tt = (g.T + g.N - 1) / g.N;
   g.mt = (g.rows + 127) / 128;
   g.ntiles = g.mt * tt;
   g.nbuf = 2 * NA * g.N <= 512 ? 2 : 1;
   g.nst = (g.cols + kStageK - 1) / kStageK;
   g.pst = (uint32_t)NA * (kCodeTile + CPS * 512);
-  // Activations have the longest way (from L2 after a slot is free), so their ring is the deepest: two stages of codes
-  // (eight slots), three weight tiles (two with GLU), the rest for them; what is left then for more codes.
-  const uint32_t at = (uint32_t)NA * kCodeTile, bt = (uint32_t)g.N * 128;
-  g.Q = GLU ? 2 : 3;
-  g.B = std::min<int>(16, (kRoom - 2 * g.pst - g.Q * at) / bt);
-  g.P = std::min<int>(8, (kRoom - g.Q * at - g.B * bt) / g.pst);
-  const uint32_t rings = g.Q * at + g.B * bt + g.P * g.pst;
+  const uint32_t qst = (uint32_t)KS * (NA * kCodeTile + (uint32_t)g.N * 128);
+  g.Q = std::min<int>(4, (kRoom - 2 * g.pst) / qst);
+  g.P = std::min<int>(8, (kRoom - g.Q * qst) / g.pst);
+  const uint32_t rings = g.Q * qst + g.P * g.pst;
   int splits = 1;
-  while (splits < 8 && (int64_t)g.ntiles * splits * 2 <= sms && g.nst >= 2 * splits &&
-         (uint32_t)(NA * g.N) * 512u <= rings)
-    splits *= 2;
+  while (splits < 8 && (int64_t)g.ntiles * splits * 2 <= sms && g.nst >= 2 * splits && (uint32_t)(NA * g.N) * 512u <= rings) splits *= 2;
   g.splits = splits;
   g.sps = (g.nst + splits - 1) / splits;
-  const size_t smem = 1024 + (size_t)rings + (size_t)(2 * g.P + 2 * g.Q + 2 * g.B + 4) * 8 + 16;
+  const size_t smem = 1024 + (size_t)rings + (size_t)(2 * g.P + 2 * g.Q + 4) * 8 + 16;
   const int64_t pitch = micro_pitch(g.cols);
   CUtensorMap wm, um, xm;
   if (!make_row_map(&wm, true, w->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
@@ -1353,8 +1344,8 @@ cudaError_t launch_wide(const bitsmoe_microscale* w, const bitsmoe_microscale* u
   if (GLU && !make_row_map(&um, true, up->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
   g.btma = (uintptr_t)g.x % 16 == 0 && (g.x_ld % 8 == 0 || g.T == 1);
   if (g.btma) g.btma = make_row_map(&xm, false, g.x, g.T, g.cols, g.T == 1 ? (g.cols * 2 + 15) / 16 * 16 : g.x_ld * 2, g.N);
-  auto kern = k_micro_wide<FMT, GLU>;
-  cudaError_t e = allow_shared<k_micro_wide<FMT, GLU>>(dev, 227 * 1024);
+  auto kern = k_micro_wide<FMT, GLU, KS>;
+  cudaError_t e = allow_shared<k_micro_wide<FMT, GLU, KS>>(dev, 227 * 1024);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1369,6 +1360,15 @@ cudaError_t launch_wide(const bitsmoe_microscale* w, const bitsmoe_microscale* u
   cfg.attrs = attr;
   cfg.numAttrs = splits > 1 ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kern, wm, um, xm, g);
+}
+
+template <int FMT, bool GLU>
+cudaError_t launch_wide(const bitsmoe_microscale* w, const bitsmoe_microscale* up, WideArgs g, int dev, int sms, cudaStream_t st) {
+  const int tt = (g.T + 255) / 256;
+  g.N = ((g.T + tt - 1) / tt + 15) / 16 * 16;
+  // two steps a slot where three such slots fit beside two stages of codes
+  if (g.N <= (GLU ? 16 : 112)) return launch_wide_k<FMT, GLU, 2>(w, up, g, dev, sms, st);
+  return launch_wide_k<FMT, GLU, 1>(w, up, g, dev, sms, st);
 }
 
 MicroMat mat_of(const bitsmoe_microscale* m) {
