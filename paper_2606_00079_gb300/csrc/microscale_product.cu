@@ -418,11 +418,13 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     const int owner = 16 * rt / rs, orow = 16 * rt - owner * rs + (lane >> 2);
     int st = -1, it = 0;     // slot of the ring and its phase's parity
     uint32_t ph = 0;
+    // The ring has an even number of slots, so a slot is always the same group's: a group that waits for a slot's next
+    // use has seen its last one, and a phase's parity cannot stand for the one before.
     for (int mi = blockIdx.x; mi < g.mt; mi += gridDim.x, ++it) {
       float acc[NT][4] = {};
       for (int i = 0; i < nk * NA; ++i) {
         if (++st == S) st = 0, ph ^= 1u;
-        if (!ok || (!halves && (i & 1) != kh)) continue;
+        if (!ok || (!halves && (st & 1) != kh)) continue;
         if (lane == 0) ok = mbar_wait(full + st, ph, g.spin);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) continue;
@@ -562,7 +564,7 @@ bool few_plan(int format, bool glu, bool coded, int T, int rows, int cols, int (
     const int clusters = std::min(mt, resident(splits));
     if (clusters < 1) continue;
     const size_t red = (size_t)few_red_bytes(T > 8 ? 2 : 1);
-    if (xb + red + 5 * (size_t)p->stage > room) continue;   // slots enough to cover a copy's latency
+    if (xb + red + 4 * (size_t)p->stage > room) continue;   // slots enough to cover a copy's latency
     const int64_t work = (int64_t)((mt + clusters - 1) / clusters) * sps;
     if (best >= 0 && work >= best) continue;
     best = work;
@@ -570,7 +572,7 @@ bool few_plan(int format, bool glu, bool coded, int T, int rows, int cols, int (
     p->sps = sps;
     p->clusters = clusters;
     p->x_pitch = pitch;
-    p->stages = (int)std::min<size_t>((room - xb - red) / p->stage, 16);
+    p->stages = (int)std::min<size_t>((room - xb - red) / p->stage, 16) & ~1;   // even: see the kernel
     p->smem = 1024 + (size_t)p->stages * p->stage + red + xb + (size_t)(2 * p->stages + 2) * 8;
   }
   return best >= 0 && !(coded && best * (glu ? 2 : 1) * (T > 8 ? 2 : 1) > 8);
@@ -1010,7 +1012,7 @@ cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* 
 // that the next tile's products run meanwhile.  CTAs stay for all their tiles.
 // With few tiles the columns are split over a cluster instead.
 // ---------------------------------------------------------------------------
-constexpr int kDecodeWarps = 8, kDecodeGroups = 2;   // groups of eight warps, each of which takes every other slot
+constexpr int kDecodeWarps = 8, kDecodeGroups = 3;   // groups of eight warps that take the slots in turn
 constexpr int kWideThreads = 32 * (4 + kDecodeGroups * kDecodeWarps + 4);   // warps: 0 codes, 1 MMA, 2 activations, 4.. decode, epilogue
 
 struct WideArgs {
@@ -1209,15 +1211,18 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     const int bt = dw * 32 + lane;
     const uint8_t* code = pring + r * 128;
     const uint8_t* scale = pring + NA * kCodeTile + (r & 31) * 16 + (r >> 5) * 4;
-    uint32_t ps = 0, pp = 0, n0 = group;   // slot of the codes' ring and its phase's parity; this group's first slot of the tile
-    for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x, n0 += ns) {
+    uint32_t ps = 0, pp = 0;                     // slot of the codes' ring and its phase's parity
+    uint32_t qs = group, qp = 0;                 // and of the tiles' ring (at least as many slots as groups)
+    int i = group;                               // this group's next slot, counted in the tile: every third of all tiles' slots
+    for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x, i -= ns) {
       const int t0 = tile / g.mt * N;
-      uint32_t qs = n0 % Q, qp = n0 / Q & 1u;
-      for (int i0 = 0; i0 < ns && ok; i0 += kSlots) {   // a stage of codes: this group's every other slot
-        ok = mbar_wait(pfull + ps, pp, g.spin);
-        for (int sub = group; sub < min(kSlots, ns - i0) && ok; sub += kDecodeGroups) {
-          const int i = i0 + sub;
+      for (int i0 = 0; i0 < ns && ok; i0 += kSlots) {   // a stage of codes
+        ok = mbar_try_wait(pfull + ps, pp) || mbar_wait(pfull + ps, pp, g.spin);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        for (; i < min(i0 + kSlots, ns) && ok; i += kDecodeGroups) {
+          const int sub = i - i0;
           ok = mbar_try_wait(qempty + qs, qp ^ 1u) || mbar_wait(qempty + qs, qp ^ 1u, g.spin);
+          ok = __all_sync(0xFFFFFFFFu, ok);
           if (!ok) break;
 #pragma unroll
           for (int s = 0; s < KS; ++s) {
@@ -1330,6 +1335,9 @@ cudaError_t launch_wide_k(const bitsmoe_microscale* w, const bitsmoe_microscale*
   g.pst = (uint32_t)NA * (kCodeTile + CPS * 512);
   const uint32_t qst = (uint32_t)KS * (NA * kCodeTile + (uint32_t)g.N * 128);
   g.Q = std::min<int>(4, (kRoom - 2 * g.pst) / qst);
+  // A group of decoders steps by as many slots as there are groups; with fewer slots it would wait for a phase two
+  // ahead of the one in progress, which a wait by parity takes for complete.
+  if (g.Q < kDecodeGroups) return cudaErrorInvalidValue;
   g.P = std::min<int>(8, (kRoom - g.Q * qst) / g.pst);
   const uint32_t rings = g.Q * qst + g.P * g.pst;
   int splits = 1;
@@ -1364,10 +1372,13 @@ cudaError_t launch_wide_k(const bitsmoe_microscale* w, const bitsmoe_microscale*
 
 template <int FMT, bool GLU>
 cudaError_t launch_wide(const bitsmoe_microscale* w, const bitsmoe_microscale* up, WideArgs g, int dev, int sms, cudaStream_t st) {
-  const int tt = (g.T + 255) / 256;
+  // at most 256 tokens a tile, with GLU 128 (two accumulators in turn; three slots fit)
+  const int most = GLU ? 128 : 256, tt = (g.T + most - 1) / most;
   g.N = ((g.T + tt - 1) / tt + 15) / 16 * 16;
   // two steps a slot where three such slots fit beside two stages of codes
-  if (g.N <= (GLU ? 16 : 112)) return launch_wide_k<FMT, GLU, 2>(w, up, g, dev, sms, st);
+  if constexpr (!GLU) {
+    if (g.N <= 96) return launch_wide_k<FMT, GLU, 2>(w, up, g, dev, sms, st);
+  }
   return launch_wide_k<FMT, GLU, 1>(w, up, g, dev, sms, st);
 }
 

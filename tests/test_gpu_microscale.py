@@ -252,7 +252,8 @@ def test_product_large(env, x, T, rows, cols):
 
 
 @pytest.mark.parametrize("x", ["bf16", "coded"])
-@pytest.mark.parametrize("T,rows,cols", [(600, 4900, 1300), (513, 5003, 777), (290, 9900, 600)])
+@pytest.mark.parametrize("T,rows,cols", [(600, 4900, 1300), (513, 5003, 777), (290, 9900, 600), (300, 12900, 700), (90, 20400, 330),
+                                         (20, 20400, 1090), (5, 20400, 2300)])
 def test_product_many_tiles(env, x, T, rows, cols):
     """More tiles than SMs or half as many (no split of the columns), odd numbers of row and token tiles, several
     stages."""
