@@ -1012,7 +1012,7 @@ cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* 
 // that the next tile's products run meanwhile.  CTAs stay for all their tiles.
 // With few tiles the columns are split over a cluster instead.
 // ---------------------------------------------------------------------------
-constexpr int kDecodeWarps = 8, kDecodeGroups = 3;   // groups of eight warps that take the slots in turn
+constexpr int kDecodeWarps = 8, kDecodeGroups = 2;   // groups of eight warps that take the slots in turn
 constexpr int kWideThreads = 32 * (4 + kDecodeGroups * kDecodeWarps + 4);   // warps: 0 codes, 1 MMA, 2 activations, 4.. decode, epilogue
 
 struct WideArgs {
@@ -1213,7 +1213,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     const uint8_t* scale = pring + NA * kCodeTile + (r & 31) * 16 + (r >> 5) * 4;
     uint32_t ps = 0, pp = 0;                     // slot of the codes' ring and its phase's parity
     uint32_t qs = group, qp = 0;                 // and of the tiles' ring (at least as many slots as groups)
-    int i = group;                               // this group's next slot, counted in the tile: every third of all tiles' slots
+    int i = group;                               // this group's next slot, counted in the tile: every other of all tiles' slots
     for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x, i -= ns) {
       const int t0 = tile / g.mt * N;
       for (int i0 = 0; i0 < ns && ok; i0 += kSlots) {   // a stage of codes
