@@ -30,8 +30,28 @@ struct MicroArgs {
   uint8_t* scales;
   int64_t pitch;
   int tiles;           // 512-byte scale tiles across a row
+  int chunks;          // of the columns: quantise 256, dequantise 512 bytes of the result
   int vec;             // dense rows can be read or written 8 elements at a time
 };
+
+// v / x on the right side of every midpoint between codes, from r = 1 / x rounded.  bf16 rows: v has 8 significant
+// bits and midpoint * x at most 7, so a quotient that is not a midpoint is at least 2^-8 of itself away from one, and
+// v r (off by 2^-23) rounded to 16 bits is on its side, and exactly on it for a tie.  fp32 rows: v r is on the wrong
+// side only within 2 units in the last place of a midpoint (whose mantissa's low 21 bits are zero); there the division
+// decides.
+template <typename T>
+__device__ __forceinline__ float quotient(float v, float x, float r) {
+  const float q = v * r;
+  const uint32_t b = __float_as_uint(q);
+  if constexpr (sizeof(T) == 4) return ((b + 4u) & 0x1FFFFFu) <= 8u ? __fdiv_rn(v, x) : q;
+  return __uint_as_float((b + 0x80u) & 0xFFFFFF00u);
+}
+// RNE_E4M3(min(top / 6, 448)): the same for midpoints between scales (the low 19 bits).
+__device__ __forceinline__ uint32_t scale_e4m3(float top) {
+  float t = top * 0.16666667163372040f;
+  if (((__float_as_uint(t) + 4u) & 0x7FFFFu) <= 8u) t = __fdiv_rn(top, 6.f);
+  return __nv_cvt_float_to_fp8(t, __NV_SATFINITE, __NV_E4M3);
+}
 
 // Two floats -> two E2M1 codes, b in the lower half of the byte (nearest, ties to even, saturating).
 __device__ __forceinline__ uint32_t e2m1x2(float hi, float lo) {
@@ -40,129 +60,198 @@ __device__ __forceinline__ uint32_t e2m1x2(float hi, float lo) {
   return r;
 }
 
+// Eight elements of a row from column c as they are stored, zeros past the columns.
 template <typename T>
-__device__ __forceinline__ void load8(const MicroArgs& a, int row, int c, float (&v)[8]) {
-  const T* p = static_cast<const T*>(a.in) + (int64_t)row * a.ld + c;
+struct Eight {
+  uint32_t w[sizeof(T) * 2];
+};
+template <typename T>
+__device__ __forceinline__ Eight<T> load8(const MicroArgs& a, int64_t row, int c) {
+  Eight<T> v;
+  const T* p = static_cast<const T*>(a.in) + row * a.ld + c;
   if (a.vec && c + 8 <= a.cols) {
-    if constexpr (sizeof(T) == 4) {
-      const float4 x = __ldcs(reinterpret_cast<const float4*>(p)), y = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-      v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-      v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-    } else {
-      const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p));
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = bf16lo(w[i]);
-        v[2 * i + 1] = bf16hi(w[i]);
-      }
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+      const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+      v.w[4 * i] = x.x, v.w[4 * i + 1] = x.y, v.w[4 * i + 2] = x.z, v.w[4 * i + 3] = x.w;
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[i] = 0.f;
-      if (c + i < a.cols) {
-        if constexpr (sizeof(T) == 4) v[i] = p[i];
-        else v[i] = __uint_as_float((uint32_t)__bfloat16_as_ushort(p[i]) << 16);
-      }
-    }
+    return v;
   }
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) * 2; ++i) v.w[i] = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (c + i < a.cols) {
+      if constexpr (sizeof(T) == 4) v.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+      else v.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+    }
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ float element(const Eight<T>& v, int i) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(v.w[i]);
+  else return i & 1 ? bf16hi(v.w[i / 2]) : bf16lo(v.w[i / 2]);
 }
 
-// A lane takes 8 columns; 2 (E4M3) or 4 (E8M0) lanes share a block.  Rows and blocks
-// past the matrix's own up to whole scale tiles are written as zeros.
+// A warp takes 256 columns of kRowsOfWarp rows 32 apart (r, r + 32, .. of a scale tile: the words of all four are 16 bytes in a
+// row), their loads in flight together; a lane 8 columns, LPB lanes a block, LPT lanes the four blocks of a scale word.
+// Neighbouring chunks of a row in neighbouring warps.  Rows and blocks past the matrix's own up to whole scale tiles are
+// written as zeros.
+// Rows of a warp: fp32 (32 bytes a lane and row) 2, bf16 4.  14336 x 4096, us with 1, 2, 4 rows: fp32 47.8, 47.5, 56.7
+// (E8M0: 5.6 TB/s) and 64.5, 64.8, 85.1 (E4M3), bf16 46.4, 35.9, 34.8 and 54.7, 48.6, 43.6.
+template <typename T>
+constexpr int kRowsOfWarp = sizeof(T) == 4 ? 2 : 4;
+
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kMThreads) k_micro_quantize(MicroArgs a) {
-  constexpr int LPB = FMT == BITSMOE_MICRO_E8M0 ? 4 : 2;   // lanes of a block
-  const int row = blockIdx.y + blockIdx.z * gridDim.y;
-  const int c = (blockIdx.x * kMThreads + threadIdx.x) * 8;   // first column of this lane
-  if (row >= (a.rows + 127) / 128 * 128) return;
-  float v[8];
-  float top = 0.f;
-  bool bad = false;
-  if (row < a.rows) {
-    load8<T>(a, row, c, v);
+  constexpr int V = 8, LPB = FMT == BITSMOE_MICRO_E8M0 ? 4 : 2, LPT = 4 * LPB, R = kRowsOfWarp<T>;
+  const int lane = threadIdx.x & 31;
+  const int64_t task = (int64_t)blockIdx.x * (kMThreads / 32) + (threadIdx.x >> 5);   // (rows, chunk of 256 columns)
+  const int64_t q = task / a.chunks;
+  const int chunk = (int)(task - q * a.chunks);
+  // q: row tile, R-th part of its four rows of a lane, lane
+  const int64_t rt = q / (128 / R);
+  const int rl = (int)(q - rt * (128 / R)), j0 = rl >> 5 << (R == 1 ? 0 : R == 2 ? 1 : 2);
+  const int64_t r0 = rt * 128 + (rl & 31) + 32 * j0;
+  const int c = (chunk * 32 + lane) * V;
+  if (r0 >= (a.rows + 127) / 128 * 128) return;
+  Eight<T> in[R];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[i] *= a.inv;
-      bad |= !(fabsf(v[i]) <= 3.402823466e38f);
-      top = fmaxf(top, fabsf(v[i]));
-    }
-  } else {
+  for (int j = 0; j < R; ++j) {
+    if (r0 + 32 * j < a.rows) {
+      in[j] = load8<T>(a, r0 + 32 * j, c);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.f;
-  }
-#pragma unroll
-  for (int o = 1; o < LPB; o <<= 1) {
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    bad |= __shfl_xor_sync(0xFFFFFFFFu, (int)bad, o) != 0;
-  }
-  uint32_t byte, code = 0;
-  if (FMT == BITSMOE_MICRO_E8M0) {
-    // exponent of a: the fp32 field (subnormal a: field 0, below every usable exponent)
-    const int e = max((int)(__float_as_uint(top) >> 23) - 2, 0);
-    byte = (uint32_t)e;
-    const float r = __uint_as_float((uint32_t)(254 - e) << 23);   // 1 / 2^(e - 127), e in [0, 252]
-#pragma unroll
-    for (int i = 0; i < 4; ++i) code |= e2m1x2(v[2 * i + 1] * r, v[2 * i] * r) << (8 * i);
-  } else {
-    byte = __nv_cvt_float_to_fp8(__fdiv_rn(top, 6.f), __NV_SATFINITE, __NV_E4M3);
-    const float x = micro_e4m3(byte);
-    if (x > 0.f) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) code |= e2m1x2(__fdiv_rn(v[2 * i + 1], x), __fdiv_rn(v[2 * i], x)) << (8 * i);
+      for (int i = 0; i < (int)sizeof(T) * 2; ++i) in[j].w[i] = 0u;
     }
   }
-  if (bad) {
-    byte = FMT == BITSMOE_MICRO_E8M0 ? 255u : 127u;
-    code = 0u;
+  uint32_t words[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    float v[V];
+    uint32_t most = 0u;   // the largest magnitude's bits; a NaN's or an infinity's are above every finite one's
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      v[i] = element<T>(in[j], i) * a.inv;
+      most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    }
+#pragma unroll
+    for (int o = 1; o < LPB; o <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+    const bool bad = most >= 0x7F800000u;
+    uint32_t byte, code = 0;
+    if (FMT == BITSMOE_MICRO_E8M0) {
+      // exponent of a: the fp32 field (subnormal a: field 0, below every usable exponent)
+      byte = bad ? 0u : (uint32_t)max((int)(most >> 23) - 2, 0);
+      const float r = __uint_as_float((254u - byte) << 23);   // 1 / 2^(byte - 127), byte in [0, 252]
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) code |= e2m1x2(v[2 * i + 1] * r, v[2 * i] * r) << (8 * i);
+    } else {
+      byte = scale_e4m3(__uint_as_float(most));
+      const float x = micro_e4m3(byte), r = __frcp_rn(x);
+      if (x > 0.f) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) code |= e2m1x2(quotient<T>(v[2 * i + 1], x, r), quotient<T>(v[2 * i], x, r)) << (8 * i);
+      }
+    }
+    if (bad) {
+      byte = FMT == BITSMOE_MICRO_E8M0 ? 255u : 127u;
+      code = 0u;
+    }
+    if (r0 + 32 * j >= a.rows || c >= a.cols) byte = 0u;
+    if (LPB > 1) byte = __shfl_sync(0xFFFFFFFFu, byte, lane / LPB * LPB);   // (its first lane's: the later ones may be past the columns)
+    if (r0 + 32 * j < a.rows && c < a.pitch * 2) {
+      *reinterpret_cast<uint32_t*>(a.codes + (r0 + 32 * j) * a.pitch + c / 2) = code;
+    }
+    // the four blocks' bytes of a scale word
+    uint32_t word = byte << (8 * (lane / LPB & 3));
+#pragma unroll
+    for (int o = LPB; o < LPT; o <<= 1) word |= __shfl_xor_sync(0xFFFFFFFFu, word, o);
+    words[j] = word;
   }
-  if (row >= a.rows) byte = 0u;
-  if (row < a.rows && c < a.pitch * 2) *reinterpret_cast<uint32_t*>(a.codes + (int64_t)row * a.pitch + c / 2) = code;
-  const int b = c / (8 * LPB);
-  if (threadIdx.x % LPB == 0 && b < a.tiles * 4)
-    a.scales[micro_scale_at(a.tiles, row, b)] = (uint8_t)(c < a.cols ? byte : 0u);
+  const int tile = chunk * (32 / LPT) + lane / LPT;
+  if (lane % LPT == 0 && tile < a.tiles)
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+      *reinterpret_cast<uint32_t*>(a.scales + (rt * a.tiles + tile) * 512 + (rl & 31) * 16 + (j0 + j) * 4) = words[j];
 }
 
+// Four rows 32 apart a warp, V columns a lane in 16 bytes of the result, so that a store writes whole sectors (rows off
+// 16-byte boundaries: column by column, so that neighbouring lanes still write neighbouring elements); the rows' scale
+// words are one 16-byte load.  14336 x 4096 to fp32: 40 us, 6.6 TB/s; with 32 bytes a lane in two stores 56 us.
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kMThreads) k_micro_dequantize(MicroArgs a) {
-  constexpr int LPB = FMT == BITSMOE_MICRO_E8M0 ? 4 : 2;
-  const int row = blockIdx.y + blockIdx.z * gridDim.y;
-  const int c = (blockIdx.x * kMThreads + threadIdx.x) * 8;
-  if (row >= a.rows || c >= a.cols) return;
-  const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(a.codes + (int64_t)row * a.pitch + c / 2));
-  const float x = micro_scale(FMT, a.scales[micro_scale_at(a.tiles, row, c / (8 * LPB))]);
-  float v[8];
+  constexpr int V = 16 / sizeof(T), LPB = (FMT == BITSMOE_MICRO_E8M0 ? 32 : 16) / V, LPT = 4 * LPB;
+  const int lane = threadIdx.x & 31;
+  const int64_t task = (int64_t)blockIdx.x * (kMThreads / 32) + (threadIdx.x >> 5);
+  const int64_t q = task / a.chunks;
+  const int chunk = (int)(task - q * a.chunks);
+  const int64_t r0 = (q >> 5) * 128 + (q & 31);
+  if (r0 >= a.rows) return;
+  const uint8_t* scales = a.scales + (q >> 5) * a.tiles * 512 + (q & 31) * 16;
+  if (!a.vec) {
+    for (int i = 0; i < V; ++i) {
+      const int c = chunk * 32 * V + i * 32 + lane, b = c / (V * LPB);
+      if (c >= a.cols) continue;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = micro_value((w >> (4 * i)) & 15u) * x * a.s;
-  T* p = static_cast<T*>(a.out) + (int64_t)row * a.ld + c;
-  if (a.vec && c + 8 <= a.cols) {
-    if constexpr (sizeof(T) == 4) {
-      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      uint32_t h[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        h[i] = *reinterpret_cast<const uint32_t*>(&t);
+      for (int j = 0; j < 4; ++j) {
+        if (r0 + 32 * j >= a.rows) break;
+        const uint32_t code = __ldg(a.codes + (r0 + 32 * j) * a.pitch + c / 2) >> (4 * (c & 1)) & 15u;
+        const float v = micro_value(code) * micro_scale(FMT, __ldg(scales + (size_t)(b >> 2) * 512 + j * 4 + (b & 3))) * a.s;
+        T* p = static_cast<T*>(a.out) + (r0 + 32 * j) * a.ld + c;
+        if constexpr (sizeof(T) == 4) *p = v;
+        else *p = __float2bfloat16_rn(v);
       }
-      *reinterpret_cast<uint4*>(p) = make_uint4(h[0], h[1], h[2], h[3]);
     }
-  } else {
+    return;
+  }
+  const int c = (chunk * 32 + lane) * V;
+  if (c >= a.cols) return;
+  const uint4 sc = __ldg(reinterpret_cast<const uint4*>(scales + (size_t)(chunk * (32 / LPT) + lane / LPT) * 512));
+  const uint32_t words[4] = {sc.x, sc.y, sc.z, sc.w};
+  uint32_t code[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (c + i < a.cols) {
-        if constexpr (sizeof(T) == 4) p[i] = v[i];
-        else p[i] = __float2bfloat16_rn(v[i]);
+  for (int j = 0; j < 4; ++j) {
+    code[j] = 0u;
+    if (r0 + 32 * j < a.rows) {
+      const uint8_t* src = a.codes + (r0 + 32 * j) * a.pitch + c / 2;
+      if constexpr (V == 8) code[j] = __ldg(reinterpret_cast<const uint32_t*>(src));
+      else code[j] = __ldg(reinterpret_cast<const uint16_t*>(src));
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (r0 + 32 * j >= a.rows) break;
+    const float x = micro_scale(FMT, words[j] >> (8 * (lane / LPB & 3)) & 255u);
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = micro_value(code[j] >> (4 * i) & 15u) * x * a.s;
+    T* p = static_cast<T*>(a.out) + (r0 + 32 * j) * a.ld + c;
+    if (c + V <= a.cols) {
+      if constexpr (sizeof(T) == 4) {
+        __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+      } else {
+        uint32_t h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+          h[i] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+        __stcs(reinterpret_cast<uint4*>(p), make_uint4(h[0], h[1], h[2], h[3]));
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (c + i < a.cols) {
+          if constexpr (sizeof(T) == 4) p[i] = v[i];
+          else p[i] = __float2bfloat16_rn(v[i]);
+        }
+    }
   }
 }
 
-// Grid: columns in x, rows in y and z (y alone holds 65535 rows).
-dim3 row_grid(int64_t cols, int64_t rows) {
-  const int64_t y = rows < 32768 ? rows : 32768;
-  return dim3((unsigned)((cols + kMThreads * 8 - 1) / (kMThreads * 8)), (unsigned)y, (unsigned)((rows + y - 1) / y));
+// Blocks for a warp per `rows` rows of a row tile and chunk of the columns, neighbouring chunks in neighbouring warps.
+int64_t micro_grid(const MicroArgs& a, int rows) {
+  return (((int64_t)a.rows + 127) / 128 * (128 / rows) * a.chunks + kMThreads / 32 - 1) / (kMThreads / 32);
 }
 
 bool rows_aligned(const void* p, int64_t ld, int type) {
@@ -197,8 +286,10 @@ int bitsmoe_microscale_quantize(const void* x, int type, int64_t ld, const bitsm
   if ((rc = dense_check(x, type, ld, q->rows, q->cols))) return rc;
   if (q->rows == 0) return BITSMOE_OK;
   MicroArgs a{x, nullptr, ld, q->rows, q->cols, q->scale, 1.f / q->scale, q->codes, q->scales, micro_pitch(q->cols),
-              micro_tiles(q->format, q->cols), rows_aligned(x, ld, type)};
-  const dim3 g = row_grid((int64_t)a.tiles * 4 * micro_block(q->format), (a.rows + 127) / 128 * 128);
+              micro_tiles(q->format, q->cols), (q->cols + 255) / 256, rows_aligned(x, ld, type)};
+  const int64_t grid = micro_grid(a, type == BITSMOE_F32 ? kRowsOfWarp<float> : kRowsOfWarp<__nv_bfloat16>);
+  if (grid >= (1ll << 31)) return BITSMOE_ERR_SHAPE;
+  const unsigned g = (unsigned)grid;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool e8 = q->format == BITSMOE_MICRO_E8M0;
   if (type == BITSMOE_F32) {
@@ -218,8 +309,10 @@ int bitsmoe_microscale_dequantize(const bitsmoe_microscale* q, void* x, int type
   if ((rc = dense_check(x, type, ld, q->rows, q->cols))) return rc;
   if (q->rows == 0) return BITSMOE_OK;
   MicroArgs a{nullptr, x, ld, q->rows, q->cols, q->scale, 0.f, q->codes, q->scales, micro_pitch(q->cols),
-              micro_tiles(q->format, q->cols), rows_aligned(x, ld, type)};
-  const dim3 g = row_grid(a.cols, a.rows);
+              micro_tiles(q->format, q->cols), (q->cols + 512 / dense_size(type) - 1) / (512 / dense_size(type)), rows_aligned(x, ld, type)};
+  const int64_t grid = micro_grid(a, 4);
+  if (grid >= (1ll << 31)) return BITSMOE_ERR_SHAPE;
+  const unsigned g = (unsigned)grid;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool e8 = q->format == BITSMOE_MICRO_E8M0;
   if (type == BITSMOE_F32) {
