@@ -174,7 +174,8 @@ int bitsmoe_forward_plan(const bitsmoe_layer* layer, int T, int top_k);
 
 /* Testing hook (no counterpart in the paper): bound every wait of the fused
  * single-token kernels, and the waits inside a block of the tensor-core
- * projections and the expert kernels of several tokens, to `spin_clocks` SM
+ * projections, of the expert kernels of several tokens and of the microscaled
+ * product (whose own status word then says so), to `spin_clocks` SM
  * clocks (<= 0: the default, about one second), and when skip_arrival is 1 let
  * block 0 skip an arrival (the former: at their first grid barrier, the latter:
  * at a stage in shared memory), so that the bounded waits for it run out.  The
@@ -518,7 +519,8 @@ int bitsmoe_shared_basis(int side, const float* W, int E, int d, int D, float* p
  * T == 0 writes zeros.  Never allocates, never synchronises; one launch. */
 int bitsmoe_calibration_gram(const void* x, const float* g, int64_t T, int D, float* H, void* stream);
 
-/* Element types of dense rows in the calls below. */
+/* Element types of dense rows in the calls below, whose device pointers are of
+ * the current device. */
 #define BITSMOE_F32  0
 #define BITSMOE_BF16 1
 

@@ -667,6 +667,11 @@ __device__ __forceinline__ void sum_splits(const float* red, int N, int splits, 
 // ---------------------------------------------------------------------------
 // Coded activations: both operands go to the tensor core as they are stored.
 // ---------------------------------------------------------------------------
+// The kernels that allocate tensor memory ask for all of an SM's shared memory, whatever their rings need: two CTAs on
+// one SM, each of a cluster (of this kernel or of another stream's) whose CTAs wait for one another, could otherwise
+// hold the tensor memory that the other's cluster waits for.
+constexpr int kAllShared = 227 * 1024;
+
 constexpr int kCodedThreads = 320;   // warp 0: copies, warp 1: scales and MMA, warps 2-9: epilogue
 
 struct CodedArgs {
@@ -934,7 +939,7 @@ cudaError_t launch_coded_p(const bitsmoe_microscale* w, const bitsmoe_microscale
                            int dev, int sms, cudaStream_t st) {
   constexpr int NA = GLU ? 2 : 1;
   const size_t ring = (size_t)g.stages * g.stage, redb = g.splits > 1 ? (size_t)NA * g.N * 512 : 0;
-  const size_t smem = 1024 + std::max(ring, redb) + (size_t)(2 * g.stages + 4) * 8 + 16;
+  if (1024 + std::max(ring, redb) + (size_t)(2 * g.stages + 4) * 8 + 16 > kAllShared) return cudaErrorInvalidValue;
   CUtensorMap wm, um, xm;
   const int64_t pitch = micro_pitch(g.cols);
   if (!make_row_map(&wm, true, w->codes, g.rows, pitch, pitch, 128) ||
@@ -943,7 +948,7 @@ cudaError_t launch_coded_p(const bitsmoe_microscale* w, const bitsmoe_microscale
   um = wm;
   if (GLU && !make_row_map(&um, true, up->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
   auto kern = k_micro_coded<FMT, GLU, G, PAIR>;
-  cudaError_t e = allow_shared<k_micro_coded<FMT, GLU, G, PAIR>>(dev, 227 * 1024);
+  cudaError_t e = allow_shared<k_micro_coded<FMT, GLU, G, PAIR>>(dev, kAllShared);
   if (e != cudaSuccess) return e;
   int grid = g.splits > 1 ? g.ntiles : std::min(g.ntiles, sms);
   if (PAIR) {   // tiles are pairs' from here on
@@ -958,7 +963,7 @@ cudaError_t launch_coded_p(const bitsmoe_microscale* w, const bitsmoe_microscale
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid, (unsigned)g.splits, 1);
   cfg.blockDim = dim3(kCodedThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = kAllShared;
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = PAIR || g.splits > 1 ? 1 : 0;
@@ -1344,7 +1349,7 @@ cudaError_t launch_wide_k(const bitsmoe_microscale* w, const bitsmoe_microscale*
   while (splits < 8 && (int64_t)g.ntiles * splits * 2 <= sms && g.nst >= 2 * splits && (uint32_t)(NA * g.N) * 512u <= rings) splits *= 2;
   g.splits = splits;
   g.sps = (g.nst + splits - 1) / splits;
-  const size_t smem = 1024 + (size_t)rings + (size_t)(2 * g.P + 2 * g.Q + 4) * 8 + 16;
+  if (1024 + (size_t)rings + (size_t)(2 * g.P + 2 * g.Q + 4) * 8 + 16 > kAllShared) return cudaErrorInvalidValue;
   const int64_t pitch = micro_pitch(g.cols);
   CUtensorMap wm, um, xm;
   if (!make_row_map(&wm, true, w->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
@@ -1353,7 +1358,7 @@ cudaError_t launch_wide_k(const bitsmoe_microscale* w, const bitsmoe_microscale*
   g.btma = (uintptr_t)g.x % 16 == 0 && (g.x_ld % 8 == 0 || g.T == 1);
   if (g.btma) g.btma = make_row_map(&xm, false, g.x, g.T, g.cols, g.T == 1 ? (g.cols * 2 + 15) / 16 * 16 : g.x_ld * 2, g.N);
   auto kern = k_micro_wide<FMT, GLU, KS>;
-  cudaError_t e = allow_shared<k_micro_wide<FMT, GLU, KS>>(dev, 227 * 1024);
+  cudaError_t e = allow_shared<k_micro_wide<FMT, GLU, KS>>(dev, kAllShared);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1363,7 +1368,7 @@ cudaError_t launch_wide_k(const bitsmoe_microscale* w, const bitsmoe_microscale*
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(splits > 1 ? g.ntiles : std::min(g.ntiles, sms)), (unsigned)splits, 1);
   cfg.blockDim = dim3(kWideThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = kAllShared;
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = splits > 1 ? 1 : 0;

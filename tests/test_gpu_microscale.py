@@ -415,3 +415,77 @@ def test_product_reports_a_wait_that_ran_out(env, case):
     status.zero_()
     assert torch.equal(bm.microscale_product(w, x, up=up, status=status), ref)
     assert int(status.item()) == 0
+
+
+def test_products_beside_the_forward_on_another_stream(env):
+    """Both allocate tensor memory and wait inside clusters: split and paired products on one stream, forwards of the
+    tensor-core projections on another, many at a time; every result as alone."""
+    import synth
+    torch, bm = env
+    rng = np.random.default_rng(12)
+    spec = synth.scaled_spec(synth.WORKLOADS["tiny"], D=256, E=8, I=256, n=128, group=128, top_k=2)
+    L = bm.bitsmoe_pack(synth.make_layer(spec, seed=5, bits_dist={0: .1, 1: .2, 2: .4, 3: .2, 4: .1}), device=0)
+    x, logits = synth.make_inputs(spec, 40, seed=5)
+    xd, ld = torch.from_numpy(x.view(np.int16)).cuda(), torch.from_numpy(logits).cuda()
+    ws = bm.Workspace(L, 40, spec.top_k)
+    y_ref = bm.moe_forward(L, xd, ld, spec.top_k, ws)
+    cases = []
+    for T, rows, cols in ((40, 300, 4096), (256, 1500, 1024), (3, 400, 2048)):
+        w = upload(env, make(rng, rows, cols, "e4m3"), "e4m3")
+        a = bf16(rng.standard_normal((T, cols))).cuda()
+        for v in (a, bm.microscale_quantize(a, "e4m3", 1.0)):
+            cases.append((w, v, bm.microscale_product(w, v)))
+    torch.cuda.synchronize()
+    s = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        y = torch.empty_like(y_ref)
+        with torch.cuda.stream(s[0]):
+            for _ in range(3):
+                bm.moe_forward(L, xd, ld, spec.top_k, ws, y=y)
+        got = [bm.microscale_product(w, v, stream=s[1]) for w, v, _ in cases]
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, r) for g, (_, _, r) in zip(got, cases))
+        assert bm.bitsmoe_last_device_status(ws.ptr) == 0
+        torch.testing.assert_close(y, y_ref, rtol=1e-5, atol=1e-6)
+
+
+_FIRST_IN_CAPTURE = r"""
+import sys
+import torch
+sys.path.insert(0, sys.argv[1])
+import paper_2606_00079_gb300 as bm
+torch.manual_seed(0)
+w, x = torch.randn(300, 512, device="cuda"), torch.randn(40, 512, device="cuda").bfloat16()
+q, xq = bm.Microscale.empty(300, 512, "e4m3", 1.0), bm.Microscale.empty(40, 512, "e4m3", 1.0)
+o = [torch.zeros(n, 300, device="cuda") for n in (40, 40, 3, 3)]
+d, hx = torch.zeros(300, 512, device="cuda"), torch.zeros(40, 512, dtype=torch.bfloat16, device="cuda")
+torch.cuda.synchronize()
+def calls():
+    bm.microscale_quantize(w, "e4m3", 1.0, out=q)
+    bm.microscale_quantize(x, "e4m3", 1.0, out=xq)
+    bm.microscale_dequantize(q, out=d)
+    bm.microscale_product(q, x, y=o[0])
+    bm.microscale_product(q, xq, y=o[1])
+    bm.microscale_product(q, x[:3], y=o[2])
+    bm.microscale_product(q, x[:3], up=q, y=o[3])
+    bm.block_norm(x, x=hx)
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    calls()
+g.replay()
+torch.cuda.synchronize()
+first = [t.clone() for t in (*o, d, hx)]
+calls()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(first, (*o, d, hx))) and float(o[0].abs().max()) > 0
+print("CAPTURED")
+"""
+
+
+def test_first_calls_of_a_process_inside_a_capture(env):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", _FIRST_IN_CAPTURE, root], capture_output=True, text=True, timeout=300)
+    assert "CAPTURED" in r.stdout, (r.stdout, r.stderr[-2000:])
