@@ -622,20 +622,19 @@ class Microscale:
 
     def __init__(self, codes, scales, rows: int, cols: int, fmt: str = "e8m0", scale: float = 1.0):
         torch = _torch or _load_torch()
-        if fmt not in MICRO_FORMATS:
-            _refuse("Microscale", f"unknown format {fmt!r}")
-        if rows < 0 or cols < 1:
-            _refuse("Microscale", f"{rows} rows, {cols} columns")
+        if fmt not in MICRO_FORMATS or rows < 0 or cols < 1:
+            _refuse("Microscale", f"{rows} rows, {cols} columns, format {fmt!r}")
         nc, ns = _micro_sizes(fmt, rows, cols)
         u8 = torch.uint8
         if codes.dtype != u8 or codes.numel() != nc or not codes.is_contiguous():
             _refuse("Microscale", f"codes must be {nc} contiguous bytes (uint8)", "SHAPE")
         if scales.dtype != u8 or scales.numel() != ns or not scales.is_contiguous():
             _refuse("Microscale", f"scales must be {ns} contiguous bytes (uint8)", "SHAPE")
-        if codes.device != scales.device:
+        self.device = dev = codes.device
+        if scales.device != dev:
             _refuse("Microscale", "codes and scales are on different devices")
         self._codes, self._scales, self._buf = codes, scales, None
-        self._ptrs, self.device = (codes.data_ptr(), scales.data_ptr()), codes.device
+        self._ptrs = (codes.data_ptr(), scales.data_ptr())
         self.rows, self.cols, self.fmt, self.scale = int(rows), int(cols), fmt, float(scale)
 
     @classmethod
@@ -701,7 +700,8 @@ class Microscale:
 
 def _micro_sizes(fmt: str, rows: int, cols: int):
     """The sizes that bitsmoe_microscale_bytes gives, of codes and scales."""
-    return rows * (-(-cols // 32) * 16), -(-rows // 128) * -(-(-(-cols // _MICRO_BLOCK[fmt])) // 4) * 512
+    tile = 4 * _MICRO_BLOCK[fmt]   # columns of a 512-byte scale tile
+    return rows * ((cols + 31) // 32 * 16), (rows + 127) // 128 * ((cols + tile - 1) // tile * 512)
 
 
 def microscale_bytes(fmt: str, rows: int, cols: int):

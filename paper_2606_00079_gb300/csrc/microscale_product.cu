@@ -127,12 +127,12 @@ __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
 
 // This warp's 16 rows x 128 columns of a stage (half kh) with NT tiles of 8 tokens.  Lane (g, t) takes the codes
 // of columns 8t .. 8t + 7 of every 32, of rows g and g + 8: two products of 16 columns.
-// E8M0: the 32 columns are a block of each row; its scale (times inv, a pair of bf16) multiplies the products' fp32 sum.
+// E8M0: the 32 columns are a block of each row; its scale (times inv, in fp32) multiplies the products' fp32 sum.
 // E4M3: a lane's 8 columns lie in one block, whose scale multiplies the codes (6 significant bits between 2^-10
 // and 2688: exact in fp16 and bf16).
 template <int FMT, int NT, bool BF>
 __device__ __forceinline__ void few_half(uint32_t code, uint32_t sf, const uint32_t (&xo)[NT], int rt, int kh, int lane,
-                                         int tiles_left, uint32_t inv, float (&acc)[NT][4]) {
+                                         int tiles_left, float inv, float (&acc)[NT][4]) {
   constexpr bool E8 = FMT == BITSMOE_MICRO_E8M0;
   constexpr int TPH = E8 ? 1 : 2;   // scale tiles of a half
   const int g = lane >> 2, t = lane & 3;
@@ -164,8 +164,7 @@ __device__ __forceinline__ void few_half(uint32_t code, uint32_t sf, const uint3
         for (int h = 0; h < 2; ++h) {
           uint32_t v;
           asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(v) : "h"((uint16_t)(sw[h] >> (16 * (b >> 1)))));
-          v = mul2<true>(v, inv);
-          s[h] = (b & 1) ? bf16hi(v) : bf16lo(v);
+          s[h] = ((b & 1) ? bf16hi(v) : bf16lo(v)) * inv;
         }
         const float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -383,7 +382,9 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         if (tid == 0) inexact_any = 0;
         bar_consumers();
         const int e = (int)(top >> 23) - 127;
-        const bool norm = e >= -86 && e < 29;   // beyond, the inverse could take block scales out of range
+        // The inverse only makes scales smaller (none of another block overflows), and those that leave fp32's range
+        // are of sums below 2^-127.
+        const bool norm = e >= -86 && e <= 14;
         inv = norm ? __uint_as_float((uint32_t)(e - 14 + 127) << 23) : 1.f;
         bf = !norm || stage(__uint_as_float((uint32_t)(14 - e + 127) << 23));
         if (bf) {
@@ -410,7 +411,6 @@ __global__ void __launch_bounds__(kFewThreads, 1)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
       xo[n] = smem_u32(xs) + (uint32_t)min(n * 8 + (lane >> 2), g.T - 1) * g.x_pitch + (uint32_t)(lane & 3) * 16;
-    const uint32_t inv2 = (__float_as_uint(inv) >> 16) * 0x10001u;   // a power of two from 2^-100 to 2^14: exact in bf16
     // The two groups of eight warps take every other slot (with GLU: one matrix each); of a single one, half of its
     // columns each.
     const bool halves = !GLU && nk == 1;
@@ -437,10 +437,10 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         const int h0 = halves ? kh : 0, h1 = halves ? kh + 1 : 2;
         if (bf) {
 #pragma unroll 1
-          for (int h = h0; h < h1; ++h) few_half<FMT, NT, true>(code, sf, xi, rt, h, lane, left, inv2, acc);
+          for (int h = h0; h < h1; ++h) few_half<FMT, NT, true>(code, sf, xi, rt, h, lane, left, inv, acc);
         } else {
 #pragma unroll 1
-          for (int h = h0; h < h1; ++h) few_half<FMT, NT, false>(code, sf, xi, rt, h, lane, left, inv2, acc);
+          for (int h = h0; h < h1; ++h) few_half<FMT, NT, false>(code, sf, xi, rt, h, lane, left, inv, acc);
         }
         __syncwarp();
         if (lane == 0 && !(g.lose && i == 0 && it == 0 && wid == 0 && (blockIdx.x | blockIdx.y) == 0)) mbar_arrive(empty + st);

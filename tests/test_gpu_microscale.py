@@ -320,6 +320,23 @@ def test_product_scale_extremes(env):
         assert (np.abs(y - want) <= 100 * U * mag).all()
 
 
+@pytest.mark.parametrize("T", [3, 12, 30])
+def test_product_scale_extremes_with_a_range_of_activations(env, T):
+    """Activations that are not all exact in fp16 as they are: small ones on small scales (sums of 2^-110 and
+    less), and small ones on a block of large scales beside large ones on a block of small scales."""
+    torch, bm = env
+    rng = np.random.default_rng(T)
+    codes = rng.integers(0, 16, (130, 96)).astype(np.uint8)
+    for scales, xs in (((1, 8, 12), (0.5, 0.125, 2.0 ** -30)), ((80, 83, 86), (2.0 ** -80, 2.0 ** -83, 2.0 ** -85)),
+                       ((247, 127, 100), (0.125, 2.0 ** 27, 1.0)), ((250, 127, 120), (2.0 ** -16, 2.0 ** 14, 2.0 ** 13))):
+        byte = np.tile(np.array(scales, np.uint8), (130, 1))
+        v = om.values(codes, byte, "e8m0", 1.0)
+        t = bf16(rng.uniform(0.5, 1, (T, 96)) * rng.choice([-1, 1], (T, 96)) * np.repeat(xs, 32))
+        y = bm.microscale_product(upload(env, (codes, byte, 1.0, None), "e8m0"), t.cuda()).double().cpu().numpy()
+        want, mag = om.product(v, t.double().numpy())
+        assert (np.abs(y - want) <= 100 * U * mag).all(), (scales, xs)
+
+
 @pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
 @pytest.mark.parametrize("T", [1, 7, 16, 40])
 def test_product_activation_range(env, fmt, T):
