@@ -36,11 +36,18 @@ __device__ __forceinline__ void store_y(void* y, int type, int64_t i, float v) {
 //
 // A code is exact in fp16, and two of them are converted by one instruction
 // (e2m1x2 -> f16x2: 7 operations for 8 codes with the byte picks; forming bf16
-// bit patterns takes 15).  The activations of a CTA's columns are scaled by a power
-// of two that brings their largest to [2^14, 2^15) and kept in fp16 when all of them
-// are exact there (bf16's 8 bits over 32 binades below the largest); otherwise the
-// CTA takes the bf16 products (the codes as bf16 bit patterns times 2^126).  All 16 columns of a product lie in one block of
-// each row, so the block's scale is applied to the product's fp32 result.
+// bit patterns takes 15).  The activations of a CTA's columns are kept in fp16 where
+// all of them are exact there: times 2^6 (bf16's 8 bits from 2^-23 to 2^10), or else
+// times the power of two that brings their largest to [2^14, 2^15) (32 binades below
+// it).  Otherwise the CTA takes the bf16 products (the codes as bf16 bit patterns
+// times 2^126).  So nothing is rounded but the fp32 sums.
+//
+// The matrix's bytes are the floor, streamed once: 4096 rows x 14336, one token, 31 MB
+// in 12.2 us (2.6 TB/s; 4.6 us at the copy bandwidth), 19456 x 8192, 85 MB in 23 us
+// (3.7 TB/s; the copies alone 16.3).  Above the copies lies what the decode issues,
+// and on small matrices the fixed 5 us of a launch, a cluster's start, the
+// first copies' latency and the sum over the cluster (2048 x 2048: 5.5 us in all).  16
+// tokens with SwiGLU, 14336 rows x 4096 of both matrices: 37.7 us.
 // ---------------------------------------------------------------------------
 constexpr int kFewWarps = 16;                      // consumers: 8 row tiles x 2 halves of a stage's columns
 constexpr int kFewThreads = 32 * (kFewWarps + 1);  // and the warp that copies
@@ -696,6 +703,11 @@ struct CodedArgs {
   int* status;
 };
 
+// The product's floor is the MMAs': 128 rows x 256 tokens x 64 columns take 128 clocks of the tensor core (9.8 PFLOP/s
+// on all SMs).  14336 rows x 4096, 8192 tokens to bf16: 177 us, 5.4 PFLOP/s; 512 tokens 22.5 us.  What bounds it is the
+// tiles' way from L2 to the SMs, about 72 bytes a clock and SM: loads alone 145 us, with the stores of y 165, MMAs 100.
+// Few tokens: 4096 x 14336, 8 tokens 9.7 us (floor 4.9: the codes' bytes; a launch and a cluster's sum are 5 us of it).
+//
 // 128 weight rows x N tokens a CTA at a time (with GLU 128 rows of both matrices).  Codes come by TMA, 256 columns
 // a stage, scale tiles by bulk copies; the MMA warp moves a stage's scales into tensor memory (columns of the
 // stage's own, so that the ring's barriers order their reuse) and issues the block-scaled products.  It runs
@@ -1009,13 +1021,20 @@ cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* 
 // Many 16-bit activations: the codes become bf16 tiles in shared memory.
 //
 // A CTA takes 128 weight rows (with GLU of both matrices) x N tokens at a time.
-// Warp 0 brings codes and scale tiles (256 columns a stage) into one ring; eight
-// warps turn them into bf16 tiles of 64 columns, code times block scale (exact:
-// at most 6 significant bits), in a second ring, where warp 2 brings the
-// activations by TMA; warp 1 issues tcgen05.mma (kind::f16) and four warps
+// Warp 0 brings codes and scale tiles (256 columns a stage) into one ring.  Two
+// groups of eight warps, which take the slots of a second ring in turn, turn them
+// into bf16 tiles of 64 columns, code times block scale (exact: at most 6
+// significant bits); warp 2 brings the activations of the same columns into the
+// same slots by TMA.  Warp 1 issues tcgen05.mma (kind::f16), and four warps
 // empty the accumulators, two of them in turn where tensor memory holds two, so
 // that the next tile's products run meanwhile.  CTAs stay for all their tiles.
 // With few tiles the columns are split over a cluster instead.
+//
+// 14336 rows x 4096, 4096 tokens: 310 us, 1.55 PFLOP/s (floor 244 at the library's
+// measured bf16 rate); 2048 tokens with SwiGLU 388 us; 64 tokens 25 us.  A slot
+// of 64 columns x 256 tokens takes 650 to 770 clocks, its MMAs 512: shared memory
+// serves the tiles' writes beside the MMAs' reads (253 us without the writes,
+// 193 without decoding; the conversions alone need 200 clocks of a slot).
 // ---------------------------------------------------------------------------
 constexpr int kDecodeWarps = 8, kDecodeGroups = 2;   // groups of eight warps that take the slots in turn
 constexpr int kWideThreads = 32 * (4 + kDecodeGroups * kDecodeWarps + 4);   // warps: 0 codes, 1 MMA, 2 activations, 4.. decode, epilogue
