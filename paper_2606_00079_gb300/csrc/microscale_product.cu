@@ -43,11 +43,12 @@ __device__ __forceinline__ void store_y(void* y, int type, int64_t i, float v) {
 // times 2^126).  So nothing is rounded but the fp32 sums.
 //
 // The matrix's bytes are the floor, streamed once: 4096 rows x 14336, one token, 31 MB
-// in 12.2 us (2.6 TB/s; 4.6 us at the copy bandwidth), 19456 x 8192, 85 MB in 23 us
-// (3.7 TB/s; the copies alone 16.3).  Above the copies lies what the decode issues,
+// in 11.2 us (2.8 TB/s; 4.6 us at the copy bandwidth), 19456 x 8192, 85 MB in 21 us
+// (4.0 TB/s; the copies alone 16.3).  Above the copies lies what the decode issues,
 // and on small matrices the fixed 5 us of a launch, a cluster's start, the
-// first copies' latency and the sum over the cluster (2048 x 2048: 5.5 us in all).  16
-// tokens with SwiGLU, 14336 rows x 4096 of both matrices: 37.7 us.
+// first copies' latency and the sum over the cluster (2048 x 2048: 5.2 us in all); more
+// tokens add their conversion and its reads from shared memory (8 tokens of the first
+// 15.7 us).
 // ---------------------------------------------------------------------------
 constexpr int kFewWarps = 16;                      // consumers: 8 row tiles x 2 halves of a stage's columns
 constexpr int kFewThreads = 32 * (kFewWarps + 1);  // and the warp that copies
@@ -555,9 +556,11 @@ struct FewPlan {
 };
 
 // How T tokens run on the kernel for few of them, or false when their activations do not fit shared memory.
-// Measured (us): a 16-bit token takes 12.4 here and 29.4 by the decoded tiles (4096 rows x 14336), 16 tokens 23.4 and
-// 29.8, 24 tokens 41.5 and 29.9; for coded tokens the block-scaled MMAs take 10.2 at 1 to 24 tokens, so only small
-// products stay here (2048 x 2048: 5.0 to 6.6 against 9.3 to 10.1).
+// Measured, us here and by the decoded tiles: 1, 8, 12, 16 tokens of 14336 rows x 4096 (16 slots a CTA) 12.0, 16.9,
+// 22.2, 25.5 and 21.6, 22.1, 22.3, 22.3, with SwiGLU 19.9, 25.1, 32.7, 36.1 and 32.9, 34.0, 34.4, 34.7; of 4096 x 14336
+// (14 slots) 11.6, 15.7, 20.2, 22.6 and 21.3, 21.4, 21.6, 21.6; 16 of 2048 x 2048 (2 slots) 6.9 and 11.8.  For
+// coded tokens the block-scaled MMAs take 10.2 at 1 to 24 tokens, so only small products stay here (2048 x 2048: 5.0
+// to 6.6 against 9.3 to 10.1).
 bool few_plan(int format, bool glu, bool coded, int T, int rows, int cols, int (*resident)(int), FewPlan* p) {
   if (T > kFewTokens) return false;
   const int CPS = format == BITSMOE_MICRO_E8M0 ? 2 : 4;
@@ -584,7 +587,8 @@ bool few_plan(int format, bool glu, bool coded, int T, int rows, int cols, int (
     p->stages = (int)std::min<size_t>((room - xb - red) / p->stage, 16) & ~1;   // even: see the kernel
     p->smem = 1024 + (size_t)p->stages * p->stage + red + xb + (size_t)(2 * p->stages + 2) * 8;
   }
-  return best >= 0 && !(coded && best * (glu ? 2 : 1) * (T > 8 ? 2 : 1) > 8);
+  if (coded) return best >= 0 && best * (glu ? 2 : 1) * (T > 8 ? 2 : 1) <= 8;
+  return best >= 0 && (T <= 12 || best <= 12);
 }
 
 template <int FMT, bool GLU, int NT>
@@ -706,8 +710,9 @@ struct CodedArgs {
 };
 
 // The product's floor is the MMAs': 128 rows x 256 tokens x 64 columns take 128 clocks of the tensor core (9.8 PFLOP/s
-// on all SMs).  14336 rows x 4096, 8192 tokens to bf16: 177 us, 5.4 PFLOP/s; 512 tokens 22.5 us.  What bounds it is the
-// tiles' way from L2 to the SMs, about 72 bytes a clock and SM: loads alone 145 us, with the stores of y 165, MMAs 100.
+// on all SMs).  14336 rows x 4096, 8192 tokens to bf16: 168 us, 5.7 PFLOP/s; 512 tokens 22 us.  What bounds it is the
+// tiles' way from L2 to the SMs together with y's: loads alone 139 to 145 us, without the stores 159, MMAs alone 125
+// (100, and the turn of the accumulator: one of 256 tokens leaves no room for a second beside the scales).
 // Few tokens: 4096 x 14336, 8 tokens 9.7 us (floor 4.9: the codes' bytes; a launch and a cluster's sum are 5 us of it).
 //
 // 128 weight rows x N tokens a CTA at a time (with GLU 128 rows of both matrices).  Codes come by TMA, 256 columns
@@ -1032,8 +1037,8 @@ cudaError_t launch_coded(const bitsmoe_microscale* w, const bitsmoe_microscale* 
 // that the next tile's products run meanwhile.  CTAs stay for all their tiles.
 // With few tiles the columns are split over a cluster instead.
 //
-// 14336 rows x 4096, 4096 tokens: 310 us, 1.55 PFLOP/s (floor 244 at the library's
-// measured bf16 rate); 2048 tokens with SwiGLU 388 us; 64 tokens 25 us.  A slot
+// 14336 rows x 4096, 4096 tokens: 307 us, 1.56 PFLOP/s (floor 244 at the library's
+// measured bf16 rate); 2048 tokens with SwiGLU 385 us; 64 tokens 25 us.  A slot
 // of 64 columns x 256 tokens takes 650 to 770 clocks, its MMAs 512: shared memory
 // serves the tiles' writes beside the MMAs' reads (253 us without the writes,
 // 193 without decoding; the conversions alone need 200 clocks of a slot).
