@@ -550,6 +550,9 @@ _DENSE = {}          # torch dtype -> BITSMOE_F32 / BITSMOE_BF16
 _raw_stream = None   # device index -> the current stream's handle
 
 
+_MAX_ROWS = 1 << 24   # the library's limit of rows; beyond 32 bits a size would be cut on its way there
+
+
 def _load_torch():
     global _torch, _DENSE, _raw_stream
     import torch
@@ -580,6 +583,8 @@ def _rows(where: str, name: str, x, rows=None, cols=None, device=None, dtype=Non
     if device is not None and x.device != device:
         _refuse(where, f"{name} is on {x.device}, expected {device}")
     r, c = shape
+    if r > _MAX_ROWS or c > _MAX_ROWS:
+        _refuse(where, f"{name} has shape {tuple(shape)}", "SHAPE")
     if (rows is not None and r != rows) or (cols is not None and c != cols):
         _refuse(where, f"{name} has shape {tuple(shape)}, expected {(rows, cols)}", "SHAPE")
     if dtype is not None and x.dtype != dtype:
@@ -618,30 +623,34 @@ class Microscale:
     `scales` (uint8, the stored tile order), see bitsmoe_microscale in include/bitsmoe.h; `fmt` is
     "e8m0" (blocks of 32 columns) or "e4m3" (16), `scale` the tensor scale."""
 
-    __slots__ = ("_codes", "_scales", "_buf", "_ptrs", "device", "rows", "cols", "fmt", "scale")
+    __slots__ = ("_codes", "_scales", "_buf", "_c", "device", "rows", "cols", "fmt")   # _c: what the library reads
 
     def __init__(self, codes, scales, rows: int, cols: int, fmt: str = "e8m0", scale: float = 1.0):
         torch = _torch or _load_torch()
         if fmt not in MICRO_FORMATS or rows < 0 or cols < 1:
             _refuse("Microscale", f"{rows} rows, {cols} columns, format {fmt!r}")
+        if rows > _MAX_ROWS or cols > _MAX_ROWS:
+            _refuse("Microscale", f"{rows} rows, {cols} columns", "SHAPE")
         nc, ns = _micro_sizes(fmt, rows, cols)
         u8 = torch.uint8
-        if codes.dtype != u8 or codes.numel() != nc or not codes.is_contiguous():
+        if codes.dtype is not u8 or codes.numel() != nc or not codes.is_contiguous():
             _refuse("Microscale", f"codes must be {nc} contiguous bytes (uint8)", "SHAPE")
-        if scales.dtype != u8 or scales.numel() != ns or not scales.is_contiguous():
+        if scales.dtype is not u8 or scales.numel() != ns or not scales.is_contiguous():
             _refuse("Microscale", f"scales must be {ns} contiguous bytes (uint8)", "SHAPE")
         self.device = dev = codes.device
         if scales.device != dev:
             _refuse("Microscale", "codes and scales are on different devices")
         self._codes, self._scales, self._buf = codes, scales, None
-        self._ptrs = (codes.data_ptr(), scales.data_ptr())
-        self.rows, self.cols, self.fmt, self.scale = int(rows), int(cols), fmt, float(scale)
+        self.rows, self.cols, self.fmt = rows, cols, fmt
+        self._c = _Microscale(MICRO_FORMATS[fmt], rows, cols, scale, codes.data_ptr(), scales.data_ptr())
 
     @classmethod
     def empty(cls, rows: int, cols: int, fmt: str = "e8m0", scale: float = 1.0, device=None) -> "Microscale":
         torch = _torch or _load_torch()
         if fmt not in MICRO_FORMATS or rows < 0 or cols < 1:
             _refuse("Microscale.empty", f"{rows} rows, {cols} columns, format {fmt!r}")
+        if rows > _MAX_ROWS or cols > _MAX_ROWS:
+            _refuse("Microscale.empty", f"{rows} rows, {cols} columns", "SHAPE")
         nc, ns = _micro_sizes(fmt, rows, cols)
         self = cls.__new__(cls)   # one allocation for both; the tensors are made when asked for
         at = (nc + 255) // 256 * 256
@@ -649,9 +658,18 @@ class Microscale:
                                       device=device if device is not None else torch.cuda.current_device())
         self._codes = self._scales = None
         base = buf.data_ptr()
-        self._ptrs, self.device = (base, base + at), buf.device
-        self.rows, self.cols, self.fmt, self.scale = rows, cols, fmt, float(scale)
+        self.device = buf.device
+        self.rows, self.cols, self.fmt = rows, cols, fmt
+        self._c = _Microscale(MICRO_FORMATS[fmt], rows, cols, scale, base, base + at)
         return self
+
+    @property
+    def scale(self) -> float:
+        return self._c.scale   # (as the library has it: fp32)
+
+    @scale.setter
+    def scale(self, value: float):
+        self._c.scale = value
 
     @property
     def codes(self):
@@ -694,9 +712,6 @@ class Microscale:
         s = self.scales.view(rt, ct, 32, 4, 4).permute(0, 3, 2, 1, 4).reshape(rt * 128, ct * 4)
         return s[:self.rows, :nb]
 
-    def _struct(self) -> "_Microscale":
-        return _Microscale(MICRO_FORMATS[self.fmt], self.rows, self.cols, self.scale, *self._ptrs)
-
 
 def _micro_sizes(fmt: str, rows: int, cols: int):
     """The sizes that bitsmoe_microscale_bytes gives, of codes and scales."""
@@ -718,7 +733,6 @@ def microscale_quantize(x, fmt: str = "e8m0", scale: float = 1.0, out: Optional[
                         stream=None) -> Microscale:
     """Quantise the rows of x (torch fp32 or bf16, 2-d, dense rows, on the device) into a Microscale with
     tensor scale `scale` (a power of two); `out` reuses an existing one of the same shape and format."""
-    import torch
     torch = _torch or _load_torch()
     where = "microscale_quantize"
     dev = x.device
@@ -733,8 +747,8 @@ def microscale_quantize(x, fmt: str = "e8m0", scale: float = 1.0, out: Optional[
     elif (out.rows, out.cols, out.fmt) != (rows, cols, fmt) or out.device != dev:
         _refuse(where, "out has another shape, format or device", "SHAPE")
     else:
-        out.scale = float(scale)
-    _check(_lib().bitsmoe_microscale_quantize(x.data_ptr(), ty, ld, out._struct(), _raw_stream(dev.index)),
+        out.scale = scale
+    _check(_lib().bitsmoe_microscale_quantize(x.data_ptr(), ty, ld, out._c, _raw_stream(dev.index)),
            "bitsmoe_microscale_quantize")
     return out
 
@@ -753,7 +767,7 @@ def microscale_dequantize(q: Microscale, dtype=None, out=None, stream=None):
         out, ld = torch.empty((q.rows, q.cols), dtype=dtype if dtype is not None else torch.float32, device=dev), q.cols
     else:
         ld = _rows(where, "out", out, q.rows, q.cols, dev)
-    _check(_lib().bitsmoe_microscale_dequantize(q._struct(), out.data_ptr(), _dense_type(where, "out", out.dtype), ld,
+    _check(_lib().bitsmoe_microscale_dequantize(q._c, out.data_ptr(), _dense_type(where, "out", out.dtype), ld,
                                                 _raw_stream(dev.index)), "bitsmoe_microscale_dequantize")
     return out
 
@@ -772,7 +786,7 @@ def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=
         with _elsewhere(where, dev, stream):
             return microscale_product(w, x, up, dtype, y, status)
     if type(x) is Microscale:
-        T, x_ptr, x_ld, xq = x.rows, None, 0, x._struct()
+        T, x_ptr, x_ld, xq = x.rows, None, 0, x._c
     else:
         x_ld = _rows(where, "x", x, None, w.cols, None, torch.bfloat16)
         T, x_ptr, xq = x.shape[0], x.data_ptr(), None
@@ -785,7 +799,7 @@ def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=
         y, y_ld = torch.empty((T, w.rows), dtype=dtype if dtype is not None else torch.float32, device=dev), w.rows
     else:
         y_ld = _rows(where, "y", y, T, w.rows, dev)
-    _check(_lib().bitsmoe_microscale_product(w._struct(), up._struct() if up is not None else None, x_ptr, x_ld, xq, T,
+    _check(_lib().bitsmoe_microscale_product(w._c, up._c if up is not None else None, x_ptr, x_ld, xq, T,
                                              y.data_ptr(), _dense_type(where, "y", y.dtype), y_ld, st_ptr,
                                              _raw_stream(dev.index)), "bitsmoe_microscale_product")
     return y

@@ -359,6 +359,19 @@ def test_product_activation_range(env, fmt, T):
         assert (np.abs(y - want) <= (cols + 4) * U * mag).all(), (lo, hi)
 
 
+def test_sizes_past_32_bits_are_refused(env):
+    """2^32 + 5 rows or columns are not cut to 5 on their way to the library."""
+    torch, bm = env
+    n = 2 ** 32 + 5
+    x = torch.empty(n, dtype=torch.bfloat16, device="cuda")
+    w = bm.microscale_quantize(torch.ones(4, 1, device="cuda"))
+    for call in (lambda: bm.microscale_quantize(x.view(n, 1)), lambda: bm.microscale_quantize(x.view(1, n)),
+                 lambda: bm.microscale_product(w, x.view(n, 1)), lambda: bm.block_norm(x.view(n, 1)),
+                 lambda: bm.block_norm(x.view(1, n)), lambda: bm.Microscale.empty(n, 1), lambda: bm.Microscale.empty(1, n)):
+        with pytest.raises(bm.BitsMoEError):
+            call()
+
+
 def test_empty_calls_write_nothing(env):
     torch, bm = env
     rng = np.random.default_rng(0)
