@@ -616,7 +616,8 @@ int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bitsmoe_micros
  *   x          device, T x D of x_type, written; NULL: no pre-norm
  *   *_ld       elements between rows (>= D; gate per token: >= 1)
  * Types are BITSMOE_F32 or BITSMOE_BF16; every pointer is aligned to its
- * elements (all rows on 16-byte boundaries with D a multiple of 8 are fastest).
+ * elements (all rows on 16-byte boundaries with D a multiple of 8 are fastest;
+ * of others the aligned 16 bytes at a row's two ends are read whole).
  * x must not overlap an input, nor h_out one other than h.  fp32 arithmetic.
  * 1 <= D <= BITSMOE_BLOCK_NORM_MAX_D, T <= 2^24.  Errors: INVALID_ARG, SHAPE,
  * ALIGNMENT, CUDA.  Never allocates, never synchronises; one launch; T == 0 is

@@ -92,6 +92,23 @@ def test_rows(env, T):
     run_case(env, T, 520, h="bf16", channel=True, a=0.5, b=-2.0)
 
 
+@pytest.mark.parametrize("T,D", [(700, 5001), (400, 8191), (5000, 515), (2500, 1030), (1300, 4095), (20000, 259)])
+def test_many_rows_off_boundaries(env, T, D):
+    """Several rows a block, whose ends share 16 bytes with their neighbours'; in place, and the same rows alone."""
+    torch, bm = env
+    run_case(env, T, D, channel=True)
+    run_case(env, T, D, h="bf16", y="f32", gate="element", sigmoid=True, seed=1)
+    run_case(env, T, D, h="bf16", y="bf16", gains="bf16", x="f32", post=False, gate="token", seed=2)
+    g = torch.Generator().manual_seed(D)
+    h, y = torch.randn(T, D, generator=g).cuda(), torch.randn(T, D, generator=g).bfloat16().cuda()
+    ho, x = bm.block_norm(h, y, post_norm=True)
+    for i in (0, 1, T - 1):
+        ah, ax = bm.block_norm(h[i:i + 1], y[i:i + 1], post_norm=True)
+        assert torch.equal(ho[i:i + 1], ah) and torch.equal(x[i:i + 1], ax)
+    _, x2 = bm.block_norm(h, y, post_norm=True, h_out=h)
+    assert torch.equal(h, ho) and torch.equal(x2, x)
+
+
 @pytest.mark.parametrize("h", ["f32", "bf16"])
 @pytest.mark.parametrize("y", ["f32", "bf16"])
 @pytest.mark.parametrize("gains", ["f32", "bf16"])
