@@ -577,12 +577,21 @@ int bitsmoe_microscale_quantize(const void* x, int type, int64_t ld, const bitsm
  * the rest as bitsmoe_microscale_quantize (any positive finite scale). */
 int bitsmoe_microscale_dequantize(const bitsmoe_microscale* q, void* x, int type, int64_t ld, void* stream);
 
+/* bf16 rows on any pitch and alignment into rows on 16-byte boundaries (out 16-byte
+ * aligned, out_ld a multiple of 8, >= cols): what a product of many rows reads five
+ * times as fast (4096 rows of 4095: the copy 16 us, the product 1560 -> 310).  The
+ * columns up to the next multiple of 8 are written as zeros.  x and out must not
+ * overlap; of x the aligned 16 bytes at a row's two ends are read whole.  T 0 .. 2^24,
+ * cols 1 .. 2^20.  Errors and the rest as bitsmoe_microscale_quantize. */
+int bitsmoe_microscale_align(const void* x, int64_t x_ld, int T, int cols, void* out, int64_t out_ld, void* stream);
+
 /* Product of T dense rows with a microscaled matrix, asynchronously on `stream`:
  *   y[t][r] = sum_k W[r][k] x[t][k]                          (up NULL)
  *   y[t][r] = SiLU(sum_k W[r][k] x[t][k]) * sum_k U[r][k] x[t][k]   (up = U)
  *   w, up   the matrices; up NULL or of w's format, rows and cols
  *   x, x_ld device, T x w->cols bf16, rows x_ld elements apart (rows on 16-byte
- *           boundaries are read fastest); NULL when xq is given
+ *           boundaries are read fastest, see bitsmoe_microscale_align); NULL when
+ *           xq is given
  *   xq      NULL, or the T rows themselves microscaled, in w's format (for
  *           instance by bitsmoe_microscale_quantize); x is then NULL
  *   y       device, T x w->rows of y_type, rows y_ld elements apart; written

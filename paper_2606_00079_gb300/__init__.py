@@ -96,6 +96,7 @@ SIGNATURES = {
     "bitsmoe_microscale_bytes": (_I, [_I, _I, _I, ctypes.POINTER(_SZ), ctypes.POINTER(_SZ)]),
     "bitsmoe_microscale_quantize": (_I, [_P, _I, ctypes.c_int64, ctypes.POINTER(_Microscale), _P]),
     "bitsmoe_microscale_dequantize": (_I, [ctypes.POINTER(_Microscale), _P, _I, ctypes.c_int64, _P]),
+    "bitsmoe_microscale_align": (_I, [_P, ctypes.c_int64, _I, _I, _P, ctypes.c_int64, _P]),
     "bitsmoe_microscale_product": (_I, [ctypes.POINTER(_Microscale), ctypes.POINTER(_Microscale), _P, ctypes.c_int64,
                                         ctypes.POINTER(_Microscale), _I, _P, _I, ctypes.c_int64, _P, _P]),
     "bitsmoe_block_norm": (_I, [ctypes.POINTER(_BlockNormArgs), _P]),
@@ -790,6 +791,14 @@ def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=
     else:
         x_ld = _rows(where, "x", x, None, w.cols, None, torch.bfloat16)
         T, x_ptr, xq = x.shape[0], x.data_ptr(), None
+        # Many rows off 16-byte boundaries are brought onto them first (us with and without: 60 x 4999 by 7000 rows
+        # 26 and 38, 500 55 and 228; 37 x 2041 by 1001 rows 9 and 8, and 6 more on the host).
+        if T > 16 and (x_ptr % 16 or x_ld % 8) and T * w.rows * w.cols > 1 << 29:
+            ld = (w.cols + 7) // 8 * 8
+            rows = torch.empty((T, ld), dtype=torch.bfloat16, device=dev)
+            _check(_lib().bitsmoe_microscale_align(x_ptr, x_ld, T, w.cols, rows.data_ptr(), ld, _raw_stream(dev.index)),
+                   "bitsmoe_microscale_align")
+            x_ptr, x_ld = rows.data_ptr(), ld
     st_ptr = None
     if status is not None:
         if status.dtype != torch.int32 or status.numel() != 1 or status.device != dev:

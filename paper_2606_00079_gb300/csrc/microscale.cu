@@ -266,6 +266,38 @@ int dense_check(const void* p, int type, int64_t ld, int rows, int cols) {
   return BITSMOE_OK;
 }
 
+// Rows of bf16 at any address to rows on 16-byte boundaries: a lane reads the two aligned 16 bytes that hold its
+// eight columns (neighbours share them in L1) and shifts.  A warp takes kAlignColumns / 8 of them of a row.
+constexpr int kAlignColumns = 1024;
+__global__ void __launch_bounds__(256) k_align_rows(const uint8_t* x, int64_t pitch, int T, int cols, uint4* out, int64_t out_pitch) {
+  const int c0 = blockIdx.y * (kAlignColumns / 8), nc = min((cols + 7) / 8, c0 + kAlignColumns / 8);
+  for (int64_t t = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; t < T; t += (int64_t)gridDim.x * 8) {
+    const uint8_t* row = x + t * pitch;
+    uint4* to = out + t * out_pitch;
+    const uint32_t a = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15);   // of every 16 bytes of the row
+#pragma unroll 4
+    for (int c = c0 + threadIdx.x % 32; c < nc; c += 32) {
+      const uint4* p = reinterpret_cast<const uint4*>(row - a) + c;
+      const uint4 lo = __ldg(p);
+      const int n = cols - 8 * c;                                                // its columns (8 at most count)
+      const uint4 hi = a && 16 - (int)a < 2 * n ? __ldg(p + 1) : make_uint4(0u, 0u, 0u, 0u);   // holds one of them
+      uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      if (a & 8)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+      if (a & 4)
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+      if (a & 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] &= n >= 2 * i + 2 ? 0xFFFFFFFFu : n == 2 * i + 1 ? 0xFFFFu : 0u;
+      to[c] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
 }  // namespace
 
 extern "C" {
@@ -327,3 +359,19 @@ int bitsmoe_microscale_dequantize(const bitsmoe_microscale* q, void* x, int type
 }
 
 }  // extern "C"
+
+extern "C" int bitsmoe_microscale_align(const void* x, int64_t x_ld, int T, int cols, void* out, int64_t out_ld, void* stream) {
+  if (T < 0 || cols < 1 || x_ld < cols || out_ld < cols || out_ld % 8) return BITSMOE_ERR_INVALID_ARG;
+  if (T > kMaxMicroRows || cols > kMaxMicroCols) return BITSMOE_ERR_SHAPE;
+  if (T == 0) return BITSMOE_OK;
+  if (!x || !out) return BITSMOE_ERR_INVALID_ARG;
+  if ((uintptr_t)x % 2 || (uintptr_t)out % 16) return BITSMOE_ERR_ALIGNMENT;
+  int dev = 0, sms = 0;
+  cudaError_t e = device_sms(&dev, &sms);
+  if (e != cudaSuccess) return record_cuda_error((int)e);
+  const dim3 grid((unsigned)std::min<int64_t>(((int64_t)T + 7) / 8, 8ll * sms), (unsigned)((cols + kAlignColumns - 1) / kAlignColumns));
+  k_align_rows<<<grid, 256, 0, static_cast<cudaStream_t>(stream)>>>(
+      static_cast<const uint8_t*>(x), x_ld * 2, T, cols, static_cast<uint4*>(out), out_ld / 8);
+  e = cudaGetLastError();
+  return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
+}

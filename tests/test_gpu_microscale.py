@@ -289,6 +289,38 @@ def test_product_strides(env, coded, T):
             assert (out[rest] == 7).all()
 
 
+@pytest.mark.parametrize("cols", [1, 7, 8, 9, 64, 255, 777, 2041])
+def test_rows_brought_onto_16_byte_boundaries(env, cols):
+    """Every offset and odd pitches: the columns as they were, zeros up to the next eight, nothing behind."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(cols)
+    for T, ld, off in ((1, cols, 0), (1, cols, 5), (9, cols, 1), (9, cols + 1, 2), (40, cols + 3, 3), (40, cols + 8, 4), (17, cols + 5, 7)):
+        buf = torch.full((T * ld + off,), float("nan"), dtype=torch.bfloat16, device="cuda")
+        x = buf[off:off + T * ld].view(T, ld)[:, :cols]
+        x.copy_(torch.randn(T, cols, generator=g).bfloat16())
+        pad = (cols + 7) // 8 * 8
+        out = torch.full((T + 1, pad + 8), 3.0, dtype=torch.bfloat16, device="cuda")
+        rc = bm._lib().bitsmoe_microscale_align(x.data_ptr(), ld, T, cols, out.data_ptr(), pad + 8, bm._raw_stream(0))
+        assert rc == 0
+        assert torch.equal(out[:T, :cols], x) and int(torch.count_nonzero(out[:T, cols:pad])) == 0
+        assert (out[:T, pad:] == 3).all() and (out[T] == 3).all()
+
+
+@pytest.mark.parametrize("T,rows,cols", [(20, 300, 777), (70, 140, 2041), (300, 260, 515)])
+def test_product_reads_rows_off_boundaries_itself(env, T, rows, cols):
+    """The C entry takes such rows as they are; the binding brings many of them onto boundaries: the same values."""
+    torch, bm = env
+    rng = np.random.default_rng(T)
+    w, u = (upload(env, make(rng, rows, cols, "e4m3"), "e4m3") for _ in range(2))
+    x = bf16(rng.standard_normal((T, cols))).cuda()
+    for up in (None, u):
+        y = torch.empty(T, rows, device="cuda")
+        rc = bm._lib().bitsmoe_microscale_product(w._c, up._c if up else None, x.data_ptr(), cols, None, T, y.data_ptr(), 0, rows, None,
+                                                  bm._raw_stream(0))
+        assert rc == 0
+        assert torch.equal(y, bm.microscale_product(w, x, up=up))
+
+
 def test_product_with_values_that_are_not_finite(env):
     """A NaN or infinite activation reaches its own row of y only."""
     torch, bm = env

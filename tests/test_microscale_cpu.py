@@ -118,6 +118,17 @@ def test_block_norm_refusals(bm):
         assert f(**kw) == E["ALIGNMENT"], kw
 
 
+def test_align_refusals(bm):
+    E, A, f = bm.ERR_CODE, 1 << 20, bm._lib().bitsmoe_microscale_align
+    for args in ((A, 8, -1, 8, A, 8, None), (A, 8, 1, 0, A, 8, None), (A, 7, 1, 8, A, 8, None), (A, 9, 1, 9, A, 8, None),
+                 (A, 9, 1, 9, A, 12, None), (None, 8, 1, 8, A, 8, None), (A, 8, 1, 8, None, 8, None)):
+        assert f(*args) == E["INVALID_ARG"], args
+    assert f(A, 8, (1 << 24) + 1, 8, A, 8, None) == E["SHAPE"]
+    assert f(A, 1 << 21, 1, (1 << 20) + 1, A, 1 << 21, None) == E["SHAPE"]
+    assert f(A + 1, 8, 1, 8, A, 8, None) == E["ALIGNMENT"] and f(A, 8, 1, 8, A + 8, 8, None) == E["ALIGNMENT"]
+    assert f(None, 8, 0, 8, None, 8, None) == bm.OK
+
+
 def test_torch_wrappers_refuse_before_the_library(bm):
     torch = pytest.importorskip("torch")
     codes = torch.zeros(4, 32, dtype=torch.uint8)
