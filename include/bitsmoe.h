@@ -564,7 +564,8 @@ int bitsmoe_microscale_bytes(int format, int rows, int cols, size_t* codes, size
  * scale and elements 0.
  *   x     device, q->rows x q->cols of `type` (BITSMOE_F32 or BITSMOE_BF16),
  *         rows `ld` elements apart (ld >= cols), aligned to its elements (rows
- *         on 16-byte boundaries are read fastest)
+ *         on 16-byte boundaries are read fastest; of others the aligned 16
+ *         bytes at a row's two ends are read whole)
  *   q     format, rows, cols and scale set by the caller, scale a power of two
  *         in 2^-100 .. 2^100; codes and scales are written whole, their padding
  *         with zeros

@@ -65,11 +65,11 @@ template <typename T>
 struct Eight {
   uint32_t w[sizeof(T) * 2];
 };
-template <typename T>
+template <typename T, bool VEC>   // VEC: rows on 16-byte boundaries
 __device__ __forceinline__ Eight<T> load8(const MicroArgs& a, int64_t row, int c) {
   Eight<T> v;
   const T* p = static_cast<const T*>(a.in) + row * a.ld + c;
-  if (a.vec && c + 8 <= a.cols) {
+  if (VEC && c + 8 <= a.cols) {
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
       const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p) + i);
@@ -77,14 +77,45 @@ __device__ __forceinline__ Eight<T> load8(const MicroArgs& a, int64_t row, int c
     }
     return v;
   }
+  if constexpr (VEC) {   // the last columns
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) * 2; ++i) v.w[i] = 0u;
+    for (int i = 0; i < (int)sizeof(T) * 2; ++i) v.w[i] = 0u;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (c + i < a.cols) {
-      if constexpr (sizeof(T) == 4) v.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
-      else v.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
-    }
+    for (int i = 0; i < 8; ++i)
+      if (c + i < a.cols) {
+        if constexpr (sizeof(T) == 4) v.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+        else v.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+      }
+    return v;
+  }
+  // the aligned 16 bytes that hold one of the columns, shifted
+  constexpr int G = sizeof(T) / 2 + 1, W = 2 * sizeof(T);
+  const int n = a.cols - c;   // its columns (8 at most count)
+  uint32_t w[4 * G];
+  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15);
+  const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(p) - off);
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    uint4 x = make_uint4(0u, 0u, 0u, 0u);
+    if (16 * i < (int)off + (int)sizeof(T) * min(n, 8) && n > 0) x = __ldg(q + i);
+    w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
+  }
+  if (off & 8)
+#pragma unroll
+    for (int i = 0; i < 4 * G - 2; ++i) w[i] = w[i + 2];
+  if (off & 4)
+#pragma unroll
+    for (int i = 0; i < 4 * G - 1; ++i) w[i] = w[i + 1];
+  if constexpr (sizeof(T) == 2) {
+    if (off & 2)
+#pragma unroll
+      for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    if constexpr (sizeof(T) == 4) v.w[i] = i < n ? w[i] : 0u;
+    else v.w[i] = 2 * i + 2 <= n ? w[i] : 2 * i + 1 == n ? w[i] & 0xFFFFu : 0u;
+  }
   return v;
 }
 template <typename T>
@@ -99,10 +130,12 @@ __device__ __forceinline__ float element(const Eight<T>& v, int i) {
 // written as zeros.
 // Rows of a warp: fp32 (32 bytes a lane and row) 2, bf16 4.  14336 x 4096, us with 1, 2, 4 rows: fp32 47.8, 47.5, 56.7
 // (E8M0: 5.6 TB/s) and 64.5, 64.8, 85.1 (E4M3), bf16 46.4, 35.9, 34.8 and 54.7, 48.6, 43.6.
+// Rows off 16-byte boundaries (VEC false): a lane reads the aligned 16 bytes that hold its columns and shifts; there and
+// back 14336 x 4095 fp32 takes 102 us (140 element by element; 85 for 4096 columns).
 template <typename T>
 constexpr int kRowsOfWarp = sizeof(T) == 4 ? 2 : 4;
 
-template <typename T, int FMT>
+template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(kMThreads) k_micro_quantize(MicroArgs a) {
   constexpr int V = 8, LPB = FMT == BITSMOE_MICRO_E8M0 ? 4 : 2, LPT = 4 * LPB, R = kRowsOfWarp<T>;
   const int lane = threadIdx.x & 31;
@@ -119,7 +152,7 @@ __global__ void __launch_bounds__(kMThreads) k_micro_quantize(MicroArgs a) {
 #pragma unroll
   for (int j = 0; j < R; ++j) {
     if (r0 + 32 * j < a.rows) {
-      in[j] = load8<T>(a, r0 + 32 * j, c);
+      in[j] = load8<T, VEC>(a, r0 + 32 * j, c);
     } else {
 #pragma unroll
       for (int i = 0; i < (int)sizeof(T) * 2; ++i) in[j].w[i] = 0u;
@@ -176,11 +209,12 @@ __global__ void __launch_bounds__(kMThreads) k_micro_quantize(MicroArgs a) {
 }
 
 // Four rows 32 apart a warp, V columns a lane in 16 bytes of the result, so that a store writes whole sectors (rows off
-// 16-byte boundaries: column by column, so that neighbouring lanes still write neighbouring elements); the rows' scale
+// 16-byte boundaries: turned in shared memory, so that neighbouring lanes still write neighbouring elements); the rows' scale
 // words are one 16-byte load.  14336 x 4096 to fp32: 40 us, 6.6 TB/s; with 32 bytes a lane in two stores 56 us.
-template <typename T, int FMT>
+template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(kMThreads) k_micro_dequantize(MicroArgs a) {
   constexpr int V = 16 / sizeof(T), LPB = (FMT == BITSMOE_MICRO_E8M0 ? 32 : 16) / V, LPT = 4 * LPB;
+  __shared__ uint4 turn[kMThreads / 32][32];
   const int lane = threadIdx.x & 31;
   const int64_t task = (int64_t)blockIdx.x * (kMThreads / 32) + (threadIdx.x >> 5);
   const int64_t q = task / a.chunks;
@@ -188,31 +222,17 @@ __global__ void __launch_bounds__(kMThreads) k_micro_dequantize(MicroArgs a) {
   const int64_t r0 = (q >> 5) * 128 + (q & 31);
   if (r0 >= a.rows) return;
   const uint8_t* scales = a.scales + (q >> 5) * a.tiles * 512 + (q & 31) * 16;
-  if (!a.vec) {
-    for (int i = 0; i < V; ++i) {
-      const int c = chunk * 32 * V + i * 32 + lane, b = c / (V * LPB);
-      if (c >= a.cols) continue;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (r0 + 32 * j >= a.rows) break;
-        const uint32_t code = __ldg(a.codes + (r0 + 32 * j) * a.pitch + c / 2) >> (4 * (c & 1)) & 15u;
-        const float v = micro_value(code) * micro_scale(FMT, __ldg(scales + (size_t)(b >> 2) * 512 + j * 4 + (b & 3))) * a.s;
-        T* p = static_cast<T*>(a.out) + (r0 + 32 * j) * a.ld + c;
-        if constexpr (sizeof(T) == 4) *p = v;
-        else *p = __float2bfloat16_rn(v);
-      }
-    }
-    return;
-  }
   const int c = (chunk * 32 + lane) * V;
-  if (c >= a.cols) return;
-  const uint4 sc = __ldg(reinterpret_cast<const uint4*>(scales + (size_t)(chunk * (32 / LPT) + lane / LPT) * 512));
+  if (VEC && c >= a.cols) return;
+  const bool in = VEC || c < a.cols;   // (off the boundaries lanes past the columns help to store)
+  uint4 sc = make_uint4(0u, 0u, 0u, 0u);
+  if (in) sc = __ldg(reinterpret_cast<const uint4*>(scales + (size_t)(chunk * (32 / LPT) + lane / LPT) * 512));
   const uint32_t words[4] = {sc.x, sc.y, sc.z, sc.w};
   uint32_t code[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     code[j] = 0u;
-    if (r0 + 32 * j < a.rows) {
+    if (in && r0 + 32 * j < a.rows) {
       const uint8_t* src = a.codes + (r0 + 32 * j) * a.pitch + c / 2;
       if constexpr (V == 8) code[j] = __ldg(reinterpret_cast<const uint32_t*>(src));
       else code[j] = __ldg(reinterpret_cast<const uint16_t*>(src));
@@ -226,7 +246,28 @@ __global__ void __launch_bounds__(kMThreads) k_micro_dequantize(MicroArgs a) {
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = micro_value(code[j] >> (4 * i) & 15u) * x * a.s;
     T* p = static_cast<T*>(a.out) + (r0 + 32 * j) * a.ld + c;
-    if (c + V <= a.cols) {
+    if constexpr (!VEC) {   // neighbouring lanes store neighbouring columns, by way of shared memory
+      uint4 x;
+      if constexpr (sizeof(T) == 4) {
+        x = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+      } else {
+        uint32_t h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+          h[i] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+        x = make_uint4(h[0], h[1], h[2], h[3]);
+      }
+      __syncwarp();
+      turn[threadIdx.x >> 5][lane] = x;
+      __syncwarp();
+      const T* t = reinterpret_cast<const T*>(turn[threadIdx.x >> 5]);
+      T* first = static_cast<T*>(a.out) + (r0 + 32 * j) * a.ld + chunk * 32 * V;
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (chunk * 32 * V + i * 32 + lane < a.cols) first[i * 32 + lane] = t[i * 32 + lane];
+    } else if (c + V <= a.cols) {
       if constexpr (sizeof(T) == 4) {
         __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
       } else {
@@ -252,6 +293,17 @@ __global__ void __launch_bounds__(kMThreads) k_micro_dequantize(MicroArgs a) {
 // Blocks for a warp per `rows` rows of a row tile and chunk of the columns, neighbouring chunks in neighbouring warps.
 int64_t micro_grid(const MicroArgs& a, int rows) {
   return (((int64_t)a.rows + 127) / 128 * (128 / rows) * a.chunks + kMThreads / 32 - 1) / (kMThreads / 32);
+}
+
+template <typename T, int FMT>
+void launch_quantize(const MicroArgs& a, unsigned grid, cudaStream_t st) {
+  if (a.vec) k_micro_quantize<T, FMT, true><<<grid, kMThreads, 0, st>>>(a);
+  else k_micro_quantize<T, FMT, false><<<grid, kMThreads, 0, st>>>(a);
+}
+template <typename T, int FMT>
+void launch_dequantize(const MicroArgs& a, unsigned grid, cudaStream_t st) {
+  if (a.vec) k_micro_dequantize<T, FMT, true><<<grid, kMThreads, 0, st>>>(a);
+  else k_micro_dequantize<T, FMT, false><<<grid, kMThreads, 0, st>>>(a);
 }
 
 bool rows_aligned(const void* p, int64_t ld, int type) {
@@ -325,11 +377,11 @@ int bitsmoe_microscale_quantize(const void* x, int type, int64_t ld, const bitsm
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool e8 = q->format == BITSMOE_MICRO_E8M0;
   if (type == BITSMOE_F32) {
-    if (e8) k_micro_quantize<float, BITSMOE_MICRO_E8M0><<<g, kMThreads, 0, st>>>(a);
-    else k_micro_quantize<float, BITSMOE_MICRO_E4M3><<<g, kMThreads, 0, st>>>(a);
+    if (e8) launch_quantize<float, BITSMOE_MICRO_E8M0>(a, g, st);
+    else launch_quantize<float, BITSMOE_MICRO_E4M3>(a, g, st);
   } else {
-    if (e8) k_micro_quantize<__nv_bfloat16, BITSMOE_MICRO_E8M0><<<g, kMThreads, 0, st>>>(a);
-    else k_micro_quantize<__nv_bfloat16, BITSMOE_MICRO_E4M3><<<g, kMThreads, 0, st>>>(a);
+    if (e8) launch_quantize<__nv_bfloat16, BITSMOE_MICRO_E8M0>(a, g, st);
+    else launch_quantize<__nv_bfloat16, BITSMOE_MICRO_E4M3>(a, g, st);
   }
   const cudaError_t r = cudaGetLastError();
   return r == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)r);
@@ -348,11 +400,11 @@ int bitsmoe_microscale_dequantize(const bitsmoe_microscale* q, void* x, int type
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool e8 = q->format == BITSMOE_MICRO_E8M0;
   if (type == BITSMOE_F32) {
-    if (e8) k_micro_dequantize<float, BITSMOE_MICRO_E8M0><<<g, kMThreads, 0, st>>>(a);
-    else k_micro_dequantize<float, BITSMOE_MICRO_E4M3><<<g, kMThreads, 0, st>>>(a);
+    if (e8) launch_dequantize<float, BITSMOE_MICRO_E8M0>(a, g, st);
+    else launch_dequantize<float, BITSMOE_MICRO_E4M3>(a, g, st);
   } else {
-    if (e8) k_micro_dequantize<__nv_bfloat16, BITSMOE_MICRO_E8M0><<<g, kMThreads, 0, st>>>(a);
-    else k_micro_dequantize<__nv_bfloat16, BITSMOE_MICRO_E4M3><<<g, kMThreads, 0, st>>>(a);
+    if (e8) launch_dequantize<__nv_bfloat16, BITSMOE_MICRO_E8M0>(a, g, st);
+    else launch_dequantize<__nv_bfloat16, BITSMOE_MICRO_E4M3>(a, g, st);
   }
   const cudaError_t r = cudaGetLastError();
   return r == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)r);
