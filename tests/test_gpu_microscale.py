@@ -321,6 +321,32 @@ def test_product_reads_rows_off_boundaries_itself(env, T, rows, cols):
         assert torch.equal(y, bm.microscale_product(w, x, up=up))
 
 
+def test_large_product_of_rows_off_boundaries_in_a_graph_and_on_a_stream(env):
+    torch, bm = env
+    T, rows, cols = 300, 1500, 1301
+    rng = np.random.default_rng(8)
+    w = upload(env, make(rng, rows, cols, "e8m0"), "e8m0")
+    xs = [bf16(rng.standard_normal((T, cols))).cuda() for _ in range(3)]
+    pad = [torch.nn.functional.pad(x, (0, 3)).contiguous()[:, :cols] for x in xs]   # the same rows on boundaries
+    want = [bm.microscale_product(w, x) for x in pad]
+    for x, v in zip(xs, want):
+        assert torch.equal(bm.microscale_product(w, x), v)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = bm.microscale_product(w, xs[1], stream=s)
+    s.synchronize()
+    assert torch.equal(got, want[1])
+    x, y = xs[0].clone(), torch.empty(T, rows, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bm.microscale_product(w, x, y=y)
+    for k in (2, 1):
+        x.copy_(xs[k])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[k])
+
+
 def test_product_with_values_that_are_not_finite(env):
     """A NaN or infinite activation reaches its own row of y only."""
     torch, bm = env
