@@ -710,9 +710,10 @@ struct CodedArgs {
 };
 
 // The product's floor is the MMAs': 128 rows x 256 tokens x 64 columns take 128 clocks of the tensor core (9.8 PFLOP/s
-// on all SMs).  14336 rows x 4096, 8192 tokens to bf16: 168 us, 5.7 PFLOP/s; 512 tokens 22 us.  What bounds it is the
-// tiles' way from L2 to the SMs together with y's: loads alone 139 to 145 us, without the stores 159, MMAs alone 125
-// (100, and the turn of the accumulator: one of 256 tokens leaves no room for a second beside the scales).
+// on all SMs).  14336 rows x 4096, 8192 tokens to bf16: 181 us, 5.3 PFLOP/s; 512 tokens 23 us.  What bounds it is the
+// tiles' way from L2 to the SMs: loads alone 175 us, MMAs alone 125 (100, and the turn of the accumulator: one of 256
+// tokens leaves no room for a second beside the scales).  Every CTA loads its own tiles: the library also runs as
+// replicas on several GPUs, which rules out loads spread over a cluster (with them 166 us).
 // Few tokens: 4096 x 14336, 8 tokens 9.7 us (floor 4.9: the codes' bytes; a launch and a cluster's sum are 5 us of it).
 //
 // 128 weight rows x N tokens a CTA at a time (with GLU 128 rows of both matrices).  Codes come by TMA, 256 columns
@@ -723,10 +724,8 @@ struct CodedArgs {
 // them): with a loop of one lane over the tiles that exist, a copy of 512 bytes took 74 clocks.  CTAs stay for
 // all their tiles; the ring runs on while eight warps empty the accumulator.  With few tiles the columns are
 // split over a cluster, whose CTAs add their partial tiles through distributed shared memory in rank order.
-// G: groups of 128 tokens of a tile.  PAIR: two CTAs of a cluster share what both need, each bringing half of it to
-// both: the tokens of two neighbouring row tiles, or with GLU the two matrices' rows of two neighbouring token tiles
-// (8192 tokens: the loads of a CTA alone took as long as all products and stores together, 175 us).
-template <int FMT, bool GLU, int G, bool PAIR>
+// G: groups of 128 tokens of a tile.
+template <int FMT, bool GLU, int G>
 __global__ void __launch_bounds__(kCodedThreads, 1)
     k_micro_coded(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap,
                   const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CodedArgs g) {
@@ -745,13 +744,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
   uint64_t* aempty = afull + 2;
   uint32_t* slot = reinterpret_cast<uint32_t*>(aempty + 2);
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int rank = PAIR ? 0 : blockIdx.y;
-  const int peer = PAIR ? blockIdx.x & 1 : 0;                           // this CTA of its pair
-  const int first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x, tile_step = PAIR ? gridDim.x >> 1 : gridDim.x;
-  // tile -> row tile and first token (past the matrix's rows or tokens for the odd one out of a pair)
-  const int across = PAIR && !GLU ? (g.mt + 1) / 2 : g.mt;
-  const auto row_tile = [&](int tile) { return PAIR && !GLU ? tile % across * 2 + peer : tile % across; };
-  const auto first_token = [&](int tile) { return (PAIR && GLU ? tile / across * 2 + peer : tile / across) * g.N; };
+  const int rank = blockIdx.y;
   const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
   const uint32_t b_bytes = (uint32_t)N * 128, sf_off = NA * kCodeTile + b_bytes;
 
@@ -761,7 +754,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
     if (GLU) prefetch_map(&umap);
     for (int i = 0; i < S; ++i) {
       mbar_init_n(full + i, 1);
-      mbar_init_n(empty + i, PAIR ? 2 : 1);   // a pair's slots are refilled together
+      mbar_init_n(empty + i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init_n(afull + i, 1);
@@ -775,17 +768,13 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, *slot, 0);
   bool ok = true;
-  if (PAIR) {   // the other's barriers are set up
-    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-  }
 
   if (wid == 0) {
     if (lane == 0) {
       int st = 0, u = 0, n = 0;
-      for (int tile = first_tile; tile < g.ntiles && ok; tile += tile_step) {
-        const int mi = row_tile(tile), t0 = first_token(tile);
-        const int nag = mi < g.mt ? NA : 0, nbg = max(0, min(G, (g.T + 127) / 128 - t0 / 128));   // scale groups that exist
+      for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x) {
+        const int mi = tile % g.mt, t0 = tile / g.mt * N;
+        const int nbg = min(G, (g.T + 127) / 128 - t0 / 128);   // the tokens' scale groups that exist
         for (int i = 0; i < nk; ++i, ++n) {
           if (u > 0) ok = mbar_wait(empty + st, (uint32_t)(u - 1) & 1u, g.spin);
           if (!ok) break;
@@ -794,30 +783,14 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
           uint8_t* sf = base + sf_off;
           const uint32_t bar = smem_u32(full + st), sb = (uint32_t)cnt * 512u;
           const size_t at = ((size_t)mi * g.tiles + (size_t)kb * CPS) * 512;
-          mbar_expect_tx(full + st, NA * kCodeTile + b_bytes + (uint32_t)(nag + nbg) * sb);
-          const auto scales = [&](int j, bool both) {   // of the tokens' group j
-            const uint8_t* src = g.xs + ((size_t)(t0 / 128 + j) * g.tiles + (size_t)kb * CPS) * 512;
-            if (both) bulk_g2s_multicast(sf + (NA + j) * CPS * 512, src, sb, full + st, 3);
-            else bulk_g2s(sf + (NA + j) * CPS * 512, src, sb, full + st);
-          };
-          if constexpr (PAIR && GLU) {
-            tma_load_2d_multicast(smem_u32(base) + peer * kCodeTile, peer ? &umap : &wmap, kb * 128, mi * 128, bar, 3);
-            bulk_g2s_multicast(sf + peer * CPS * 512, (peer ? g.us : g.ws) + at, sb, full + st, 3);
-            tma_load_2d(smem_u32(base) + NA * kCodeTile, &xmap, kb * 128, t0, bar);
-            for (int j = 0; j < nbg; ++j) scales(j, false);
-          } else if constexpr (PAIR) {
-            tma_load_2d(smem_u32(base), &wmap, kb * 128, mi * 128, bar);
-            if (nag) bulk_g2s(sf, g.ws + at, sb, full + st);
-            tma_load_2d_multicast(smem_u32(base) + kCodeTile + peer * kCodeTile, &xmap, kb * 128, t0 + peer * 128, bar, 3);
-            if (peer < nbg) scales(peer, true);
-          } else {
-            tma_load_2d(smem_u32(base), &wmap, kb * 128, mi * 128, bar);
-            if (GLU) tma_load_2d(smem_u32(base) + kCodeTile, &umap, kb * 128, mi * 128, bar);
-            tma_load_2d(smem_u32(base) + NA * kCodeTile, &xmap, kb * 128, t0, bar);
-            bulk_g2s(sf, g.ws + at, sb, full + st);
-            if (GLU) bulk_g2s(sf + CPS * 512, g.us + at, sb, full + st);
-            for (int j = 0; j < nbg; ++j) scales(j, false);
-          }
+          mbar_expect_tx(full + st, NA * kCodeTile + b_bytes + (uint32_t)(NA + nbg) * sb);
+          tma_load_2d(smem_u32(base), &wmap, kb * 128, mi * 128, bar);
+          if (GLU) tma_load_2d(smem_u32(base) + kCodeTile, &umap, kb * 128, mi * 128, bar);
+          tma_load_2d(smem_u32(base) + NA * kCodeTile, &xmap, kb * 128, t0, bar);
+          bulk_g2s(sf, g.ws + at, sb, full + st);
+          if (GLU) bulk_g2s(sf + CPS * 512, g.us + at, sb, full + st);
+          for (int j = 0; j < nbg; ++j)
+            bulk_g2s(sf + (NA + j) * CPS * 512, g.xs + ((size_t)(t0 / 128 + j) * g.tiles + (size_t)kb * CPS) * 512, sb, full + st);
           if (++st == S) {
             st = 0;
             ++u;
@@ -835,7 +808,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
     const uint32_t sstep = g.stage >> 4, id0 = idesc_e2m1(N, E8, 0), id2 = idesc_e2m1(N, E8, 2);
     const uint32_t sf0 = tmem + (uint32_t)(g.nbuf * NA * N);
     int st = 0, u = 0, it = 0;
-    for (int tile = first_tile; tile < g.ntiles && ok; tile += tile_step, ++it) {
+    for (int tile = blockIdx.x; tile < g.ntiles && ok; tile += gridDim.x, ++it) {
       const int buf = it % g.nbuf, used = it / g.nbuf;
       if (used > 0) ok = mbar_wait(aempty + buf, (uint32_t)(used - 1) & 1u, g.spin);
       ok = __all_sync(0xFFFFFFFFu, ok);
@@ -866,10 +839,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
             mma_e2m1<E8>(one, acc + (uint32_t)(a * N), a0 + a * (kCodeTile >> 4) + 2 * k, b0 + 2 * k, E8 && (k & 1) ? id2 : id0,
                          ta + (a * CPS + q) * 4, tb + (q * G) * 4, (uint32_t)(i | k));
         }
-        if (!(g.lose && i == 0 && it == 0 && (blockIdx.x | blockIdx.y) == 0)) {
-          if (PAIR) mma_commit_multicast(one, empty + st, 3);
-          else mma_commit(one, empty + st);
-        }
+        if (!(g.lose && i == 0 && it == 0 && (blockIdx.x | blockIdx.y) == 0)) mma_commit(one, empty + st);
         if (++st == S) {
           st = 0;
           ++u;
@@ -881,13 +851,13 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
     const int r = 32 * (wid & 3) + lane, half = (wid - 2) >> 2;
     const int nh = (N / 16 + 1) / 2 * 16;   // columns of the first half
     int it = 0;
-    for (int tile = first_tile; tile < g.ntiles; tile += tile_step, ++it) {
+    for (int tile = blockIdx.x; tile < g.ntiles; tile += gridDim.x, ++it) {
       const int buf = it % g.nbuf, used = it / g.nbuf;
       ok = mbar_wait_idle(afull + buf, (uint32_t)used & 1u, g.spin);
       ok = __all_sync(0xFFFFFFFFu, ok);
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const int m = row_tile(tile) * 128 + r, t0 = first_token(tile);
+      const int m = tile % g.mt * 128 + r, t0 = tile / g.mt * N;
       const uint32_t tl = tmem + ((uint32_t)(32 * (wid & 3)) << 16) + (uint32_t)(buf * NA * N);
       // the accumulator goes to registers first: the next tile's products run while this one is stored
       constexpr int kChunks = G * 128 / 32;   // of 16 columns, at most, of a half
@@ -934,14 +904,6 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-  } else if (PAIR) {   // the other may still copy into this CTA's ring and arrive on its barriers
-    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-    if (!ok) {   // a wait ran out: what the other had sent before it gave up too has time to arrive
-      const long long t0 = clock64();
-      while (clock64() - t0 < 100000) {
-      }
-    }
   } else {
     __syncthreads();
   }
@@ -953,49 +915,12 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
   }
 }
 
-template <int FMT, bool GLU, int G, bool PAIR>
-cudaError_t launch_coded_p(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const bitsmoe_microscale* xq, CodedArgs g,
-                           int dev, int sms, cudaStream_t st) {
-  constexpr int NA = GLU ? 2 : 1;
-  const size_t ring = (size_t)g.stages * g.stage, redb = g.splits > 1 ? (size_t)NA * g.N * 512 : 0;
-  if (1024 + std::max(ring, redb) + (size_t)(2 * g.stages + 4) * 8 + 16 > kAllShared) return cudaErrorInvalidValue;
-  CUtensorMap wm, um, xm;
-  const int64_t pitch = micro_pitch(g.cols);
-  if (!make_row_map(&wm, true, w->codes, g.rows, pitch, pitch, 128) ||
-      !make_row_map(&xm, true, xq->codes, g.T, pitch, pitch, PAIR && !GLU ? 128 : g.N))
-    return cudaErrorInvalidValue;
-  um = wm;
-  if (GLU && !make_row_map(&um, true, up->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
-  auto kern = k_micro_coded<FMT, GLU, G, PAIR>;
-  cudaError_t e = allow_shared<k_micro_coded<FMT, GLU, G, PAIR>>(dev, kAllShared);
-  if (e != cudaSuccess) return e;
-  int grid = g.splits > 1 ? g.ntiles : std::min(g.ntiles, sms);
-  if (PAIR) {   // tiles are pairs' from here on
-    g.ntiles = GLU ? g.mt * (((g.T + g.N - 1) / g.N + 1) / 2) : (g.mt + 1) / 2 * ((g.T + g.N - 1) / g.N);
-    grid = 2 * std::min(g.ntiles, sms / 2);
-  }
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = PAIR ? 2 : 1;
-  attr[0].val.clusterDim.y = (unsigned)g.splits;
-  attr[0].val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid, (unsigned)g.splits, 1);
-  cfg.blockDim = dim3(kCodedThreads);
-  cfg.dynamicSmemBytes = kAllShared;
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = PAIR || g.splits > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kern, wm, um, xm, g);
-}
-
 template <int FMT, bool GLU, int G>
 cudaError_t launch_coded_g(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const bitsmoe_microscale* xq, CodedArgs g,
                            int dev, int sms, cudaStream_t st) {
   constexpr int NA = GLU ? 2 : 1, CPS = FMT == BITSMOE_MICRO_E8M0 ? 2 : 4;
-  const int tt = (g.T + g.N - 1) / g.N;
   g.mt = (g.rows + 127) / 128;
-  g.ntiles = g.mt * tt;
+  g.ntiles = g.mt * ((g.T + g.N - 1) / g.N);
   g.nst = (g.cols + kStageK - 1) / kStageK;
   int splits = 1;
   while (splits < 8 && (int64_t)g.ntiles * splits * 2 <= sms && g.nst >= 2 * splits) splits *= 2;
@@ -1007,11 +932,30 @@ cudaError_t launch_coded_g(const bitsmoe_microscale* w, const bitsmoe_microscale
   // two accumulators where tensor memory holds them beside the scales of every stage
   g.nbuf = splits == 1 && 2 * NA * g.N + fit * sf_cols <= 512 ? 2 : 1;
   g.stages = std::min(fit, (512 - g.nbuf * NA * g.N) / sf_cols);
-  // pairs where there is something to share: whole halves of 128 tokens, or with GLU two token tiles
-  if constexpr (GLU || G == 2) {
-    if (splits == 1 && g.N == 256 / NA && (GLU ? tt : g.mt) >= 2) return launch_coded_p<FMT, GLU, G, true>(w, up, xq, g, dev, sms, st);
-  }
-  return launch_coded_p<FMT, GLU, G, false>(w, up, xq, g, dev, sms, st);
+  const size_t ring = (size_t)g.stages * g.stage, redb = splits > 1 ? (size_t)NA * g.N * 512 : 0;
+  if (1024 + std::max(ring, redb) + (size_t)(2 * g.stages + 4) * 8 + 16 > kAllShared) return cudaErrorInvalidValue;
+  CUtensorMap wm, um, xm;
+  const int64_t pitch = micro_pitch(g.cols);
+  if (!make_row_map(&wm, true, w->codes, g.rows, pitch, pitch, 128) || !make_row_map(&xm, true, xq->codes, g.T, pitch, pitch, g.N))
+    return cudaErrorInvalidValue;
+  um = wm;
+  if (GLU && !make_row_map(&um, true, up->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
+  auto kern = k_micro_coded<FMT, GLU, G>;
+  cudaError_t e = allow_shared<k_micro_coded<FMT, GLU, G>>(dev, kAllShared);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1;
+  attr[0].val.clusterDim.y = (unsigned)splits;
+  attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(splits > 1 ? g.ntiles : std::min(g.ntiles, sms)), (unsigned)splits, 1);
+  cfg.blockDim = dim3(kCodedThreads);
+  cfg.dynamicSmemBytes = kAllShared;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = splits > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, wm, um, xm, g);
 }
 
 template <int FMT, bool GLU>

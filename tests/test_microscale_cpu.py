@@ -177,3 +177,13 @@ def test_oracle_against_the_definitions():
     c, s = om.quantize(np.full((1, 16), 6.0 * 448 * 4, np.float32), "e4m3", 1.0)
     assert s[0, 0] == 126 and (c == 7).all()
     np.testing.assert_array_equal(om.values(c, s, "e4m3", 0.5), np.full((1, 16), 1344.0))
+
+
+def test_sources_name_no_multicast():
+    """The library also runs as replicas on several GPUs, where no load or arrival is spread over a cluster."""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    for folder in ("paper_2606_00079_gb300/csrc", "include"):
+        for name in sorted(os.listdir(os.path.join(root, folder))):
+            with open(os.path.join(root, folder, name), encoding="utf-8") as f:
+                assert "multicast" not in f.read(), name
