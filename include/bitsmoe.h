@@ -598,8 +598,8 @@ int bitsmoe_microscale_align(const void* x, int64_t x_ld, int T, int cols, void*
  *   y       device, T x w->rows of y_type, rows y_ld elements apart; written
  *           (nothing between its rows is touched); must not overlap the inputs
  *   status  device int or NULL: BITSMOE_ERR_TIMEOUT is written there if a
- *           bounded wait of the kernel ran out (y is then undefined); not
- *           cleared by the call
+ *           bounded wait of the kernel ran out; not cleared by the call.  The
+ *           results that such a wait has lost are NaN, with and without it
  * Products and sums are fp32 (the products of two codes, and of a code with a
  * bf16 value, are exact); y is rounded once.  Errors: INVALID_ARG, SHAPE,
  * ALIGNMENT, CUDA.  Never allocates, never synchronises; one launch.  T == 0

@@ -777,8 +777,8 @@ def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=
                        stream=None):
     """y (T x w.rows, fp32 by default, or bf16) = x w^T for x a torch bf16 tensor (T x w.cols, dense rows) or a
     Microscale of w's format; with `up` (w's shape and format) SiLU(x w^T) * (x up^T).  `status`: an optional
-    int32 tensor of one element that receives a device-side timeout.  Of large products, x's rows off 16-byte
-    boundaries are copied to a temporary first."""
+    int32 tensor of one element that receives a device-side timeout (the results that it cost are NaN, with and
+    without it).  Of large products, x's rows off 16-byte boundaries are copied to a temporary first."""
     torch = _torch or _load_torch()
     where = "microscale_product"
     dev = w.device

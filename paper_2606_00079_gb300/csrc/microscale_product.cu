@@ -30,6 +30,10 @@ __device__ __forceinline__ void store_y(void* y, int type, int64_t i, float v) {
   else static_cast<__nv_bfloat16*>(y)[i] = __float2bfloat16_rn(v);
 }
 
+// What is stored (NaN) for results that a wait that ran out has lost, so that a call without a status word shows it too.  A
+// warp whose wait ran out passes nothing on: who waits for it runs out as well, up to the warps that store.
+constexpr uint32_t kLost = 0x7FC00000u;
+
 // ---------------------------------------------------------------------------
 // Few tokens: the weights' codes pass once through shared memory into warp-level
 // products (mma.sync m16n8k16, 16 weight rows x 8 tokens x 16 columns).
@@ -465,21 +469,22 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"(buf), "r"(owner));
       asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(smem_u32(rfull)), "r"(owner));
       const float unit = E8 ? 1.f : inv;
+      if (ok)
 #pragma unroll
-      for (int q = 0; q < NT; ++q)
+        for (int q = 0; q < NT; ++q)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int c = q * 8 + (lane & 3) * 2 + (j & 1);
-          asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::
-                           "r"(dst + (uint32_t)(((rank * 2 + kh) * NT * 8 + c) * rs + orow + (j >> 1) * 8) * 4u),
-                       "r"(__float_as_uint(acc[q][j] * unit)), "r"(bar) : "memory");
-        }
+          for (int j = 0; j < 4; ++j) {
+            const int c = q * 8 + (lane & 3) * 2 + (j & 1);
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::
+                             "r"(dst + (uint32_t)(((rank * 2 + kh) * NT * 8 + c) * rs + orow + (j >> 1) * 8) * 4u),
+                         "r"(__float_as_uint(acc[q][j] * unit)), "r"(bar) : "memory");
+          }
       if (mi + (int)gridDim.x >= g.mt) {   // everything sent: the others may leave once they have their parts
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
       }
       // the parts of this CTA's rows, added in the order of the CTAs and halves
-      // (a warp whose wait ran out sends and stores nothing of use from then on, but keeps every barrier)
+      // (a warp whose wait ran out sends nothing and stores NaN from then on, but keeps every barrier)
       if (ok) ok = mbar_wait_cluster(rfull, (uint32_t)it & 1u, g.spin);
       ok = __all_sync(0xFFFFFFFFu, ok);
       for (int e = tid; e < rs * g.T; e += kFewWarps * 32) {
@@ -495,7 +500,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         if (m >= g.rows) continue;
         float o = sum[0] * g.sw;
         if (GLU) o = silu_mul(o, sum[1] * g.su);
-        store_y(g.y, g.y_type, (int64_t)c * g.y_ld + m, o);
+        store_y(g.y, g.y_type, (int64_t)c * g.y_ld + m, ok ? o : __uint_as_float(kLost));
       }
       __syncwarp();
       if (mi + (int)gridDim.x < g.mt) {
@@ -644,6 +649,18 @@ __device__ __forceinline__ void store_tokens(const uint32_t (&v)[NA][16], int t,
   }
 }
 
+// NaN for tokens [c, end) of a tile at weight row m: in the cluster's partial tile (red: this row of [na][N][128]) or in y.
+__device__ __noinline__ void lost_tokens(int c, int end, float* red, int N, int na, int t0, int T, int m, int rows, void* y, int y_type,
+                                         int64_t y_ld) {
+  for (; c < end; ++c) {
+    if (red) {
+      for (int a = 0; a < na; ++a) red[(size_t)(a * N + c) * 128] = __uint_as_float(kLost);
+    } else if (m < rows && t0 + c < T) {
+      store_y(y, y_type, (int64_t)(t0 + c) * y_ld + m, __uint_as_float(kLost));
+    }
+  }
+}
+
 // A CTA's share of the rows of a tile split over a cluster: the partial tiles red [NA][N][128] of the
 // cluster's CTAs added in rank order (all of an element's requested before the first is used), scaled, stored.
 template <int NA, int THREADS>
@@ -742,7 +759,8 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
   uint64_t* empty = full + S;
   uint64_t* afull = empty + S;
   uint64_t* aempty = afull + 2;
-  uint32_t* slot = reinterpret_cast<uint32_t*>(aempty + 2);
+  uint64_t* drained = aempty + 2;   // after a wait of the MMA warp that ran out: the MMAs that it had issued
+  uint32_t* slot = reinterpret_cast<uint32_t*>(drained + 1);
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int rank = blockIdx.y;
   const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
@@ -760,6 +778,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
       mbar_init_n(afull + i, 1);
       mbar_init_n(aempty + i, 8);
     }
+    mbar_init_n(drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (wid == 1) tmem_alloc(slot, 512);
@@ -845,7 +864,12 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
           ++u;
         }
       }
+      if (!ok) break;
       mma_commit(one, afull + buf);
+    }
+    if (!ok) {
+      mma_commit(one, drained);
+      mbar_wait(drained, 0u);
     }
   } else {
     const int r = 32 * (wid & 3) + lane, half = (wid - 2) >> 2;
@@ -853,11 +877,14 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
     int it = 0;
     for (int tile = blockIdx.x; tile < g.ntiles; tile += gridDim.x, ++it) {
       const int buf = it % g.nbuf, used = it / g.nbuf;
-      ok = mbar_wait_idle(afull + buf, (uint32_t)used & 1u, g.spin);
+      if (ok) ok = mbar_wait_idle(afull + buf, (uint32_t)used & 1u, g.spin);
       ok = __all_sync(0xFFFFFFFFu, ok);
-      if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const int m = tile % g.mt * 128 + r, t0 = tile / g.mt * N;
+      if (!ok) {
+        lost_tokens(half ? nh : 0, half ? N : nh, g.splits > 1 ? red + r : nullptr, N, NA, t0, g.T, m, g.rows, g.y, g.y_type, g.y_ld);
+        continue;
+      }
       const uint32_t tl = tmem + ((uint32_t)(32 * (wid & 3)) << 16) + (uint32_t)(buf * NA * N);
       // the accumulator goes to registers first: the next tile's products run while this one is stored
       constexpr int kChunks = G * 128 / 32;   // of 16 columns, at most, of a half
@@ -1064,7 +1091,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   uint64_t* qempty = qfull + Q;
   uint64_t* afull = qempty + Q;
   uint64_t* aempty = afull + 2;
-  uint32_t* slot = reinterpret_cast<uint32_t*>(aempty + 2);
+  uint64_t* drained = aempty + 2;   // after a wait of the MMA warp that ran out: the MMAs that it had issued
+  uint32_t* slot = reinterpret_cast<uint32_t*>(drained + 1);
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int rank = blockIdx.y;
   const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
@@ -1087,6 +1115,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       mbar_init_n(afull + i, 1);
       mbar_init_n(aempty + i, 4);
     }
+    mbar_init_n(drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (wid == 1) tmem_alloc(slot, 512);
@@ -1156,7 +1185,12 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           ++u;
         }
       }
+      if (!ok) break;
       mma_commit(one, afull + buf);
+    }
+    if (!ok) {
+      mma_commit(one, drained);
+      mbar_wait(drained, 0u);
     }
   } else if (wid == 2) {
     if (lane == 0 && g.btma) {
@@ -1245,11 +1279,14 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     int it = 0;
     for (int tile = blockIdx.x; tile < g.ntiles; tile += gridDim.x, ++it) {
       const int buf = it % g.nbuf, use = it / g.nbuf;
-      ok = mbar_wait_idle(afull + buf, (uint32_t)use & 1u, g.spin);
+      if (ok) ok = mbar_wait_idle(afull + buf, (uint32_t)use & 1u, g.spin);
       ok = __all_sync(0xFFFFFFFFu, ok);
-      if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const int m = tile % g.mt * 128 + r, t0 = tile / g.mt * N;
+      if (!ok) {
+        lost_tokens(0, N, g.splits > 1 ? red + r : nullptr, N, NA, t0, g.T, m, g.rows, g.y, g.y_type, g.y_ld);
+        continue;
+      }
       const uint32_t tl = tmem + ((uint32_t)(32 * (wid & 3)) << 16) + (uint32_t)(buf * NA * N);
       for (int c0 = 0; c0 < N; c0 += 16) {
         uint32_t v[NA][16];

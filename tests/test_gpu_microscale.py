@@ -577,3 +577,44 @@ def test_first_calls_of_a_process_inside_a_capture(env):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", _FIRST_IN_CAPTURE, root], capture_output=True, text=True, timeout=300)
     assert "CAPTURED" in r.stdout, (r.stdout, r.stderr[-2000:])
+
+
+WAITS = {"few": (3, 152 * 128, 8192), "few_split": (2, 130, 65536), "few_tiles": (3, 300 * 128, 4096), "few_swiglu": (3, 152 * 128, 4096),
+         "few_split_tiles": (3, 200 * 128, 2304), "few_split_tiles_swiglu": (3, 200 * 128, 1280),
+         "coded": (40, 152 * 128, 8192), "coded_tiles": (256, 152 * 128, 4096), "coded_swiglu": (256, 80 * 128, 4096),
+         "coded_split": (40, 130, 65536), "wide": (40, 152 * 128, 2048), "wide_split": (40, 130, 16384), "wide_swiglu": (40, 152 * 128, 1024)}
+
+
+@pytest.mark.parametrize("case", list(WAITS))
+def test_a_wait_that_ran_out_leaves_nan(env, case):
+    """The ordinary call, without a status word: what a block that gave up has lost is NaN (its first tile, where that has
+    more stages than its ring), every other value is right, nothing between the rows is touched, and the next call is
+    right."""
+    torch, bm = env
+    T, rows, cols = WAITS[case]
+    g = torch.Generator().manual_seed(6)
+    w = bm.microscale_quantize(torch.randn(rows, cols, device="cuda"), "e4m3", 1.0)
+    x = torch.randn(T, cols, generator=g).bfloat16().cuda()
+    if case.startswith("coded"):
+        x = bm.microscale_quantize(x, "e4m3", 1.0)
+    up = w if case.endswith("swiglu") else None
+    ref = bm.microscale_product(w, x, up=up)
+    for dt in (torch.float32, torch.bfloat16):
+        buf = torch.full((T, rows + 5), 7.0, dtype=dt, device="cuda")
+        y = buf[:, :rows]
+        bm.bitsmoe_debug_wait_limit(1, 2_000_000)
+        try:
+            bm.microscale_product(w, x, up=up, y=y)
+            torch.cuda.synchronize()
+        finally:
+            bm.bitsmoe_debug_wait_limit(0, 0)
+        lost = torch.isnan(y)
+        assert bool(lost.any())
+        if "split_tiles" not in case:
+            assert bool(lost[:min(T, 128), :min(rows, 128)].all())
+        assert torch.equal(y[~lost], ref.to(dt)[~lost])
+        assert (buf[:, rows:] == 7).all()
+        if not case.endswith("split"):
+            assert not bool(lost.all())
+        bm.microscale_product(w, x, up=up, y=y)
+        assert torch.equal(y, ref.to(dt))
