@@ -733,7 +733,8 @@ def microscale_bytes(fmt: str, rows: int, cols: int):
 def microscale_quantize(x, fmt: str = "e8m0", scale: float = 1.0, out: Optional[Microscale] = None,
                         stream=None) -> Microscale:
     """Quantise the rows of x (torch fp32 or bf16, 2-d, dense rows, on the device) into a Microscale with
-    tensor scale `scale` (a power of two); `out` reuses an existing one of the same shape and format."""
+    tensor scale `scale` (a power of two); `out` reuses an existing one of the same shape and format (a call that is
+    refused leaves it as it was)."""
     torch = _torch or _load_torch()
     where = "microscale_quantize"
     dev = x.device
@@ -747,10 +748,11 @@ def microscale_quantize(x, fmt: str = "e8m0", scale: float = 1.0, out: Optional[
         out = Microscale.empty(rows, cols, fmt, scale, dev)
     elif (out.rows, out.cols, out.fmt) != (rows, cols, fmt) or out.device != dev:
         _refuse(where, "out has another shape, format or device", "SHAPE")
-    else:
-        out.scale = scale
-    _check(_lib().bitsmoe_microscale_quantize(x.data_ptr(), ty, ld, out._c, _raw_stream(dev.index)),
-           "bitsmoe_microscale_quantize")
+    before, out.scale = out.scale, scale
+    rc = _lib().bitsmoe_microscale_quantize(x.data_ptr(), ty, ld, out._c, _raw_stream(dev.index))
+    if rc:
+        out.scale = before   # its codes are the old ones
+    _check(rc, "bitsmoe_microscale_quantize")
     return out
 
 

@@ -618,3 +618,21 @@ def test_a_wait_that_ran_out_leaves_nan(env, case):
             assert not bool(lost.all())
         bm.microscale_product(w, x, up=up, y=y)
         assert torch.equal(y, ref.to(dt))
+
+
+def test_a_refused_quantisation_leaves_out_as_it_was(env):
+    """A tensor scale that the library does not take: `out` keeps its codes and its own scale."""
+    torch, bm = env
+    x = torch.randn(9, 70, device="cuda")
+    q = bm.microscale_quantize(x, "e4m3", 0.5)
+    before = bm.microscale_dequantize(q)
+    s = torch.cuda.Stream()
+    for scale in (3.0, 2.0 ** 101, 0.0, float("nan")):
+        for kw in ({}, {"stream": s}):
+            with pytest.raises(bm.BitsMoEError):
+                bm.microscale_quantize(x, "e4m3", scale, out=q, **kw)
+            assert q.scale == 0.5
+    torch.cuda.synchronize()
+    assert torch.equal(bm.microscale_dequantize(q), before)
+    bm.microscale_quantize(x, "e4m3", 2.0, out=q)
+    assert q.scale == 2.0 and torch.equal(bm.microscale_dequantize(q), bm.microscale_dequantize(bm.microscale_quantize(x, "e4m3", 2.0)))
