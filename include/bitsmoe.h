@@ -560,8 +560,8 @@ int bitsmoe_microscale_bytes(int format, int rows, int cols, size_t* codes, size
  *   E4M3: X = min(a / 6, 448) rounded to E4M3
  *   element = v / X rounded to E2M1, at most 6 in magnitude (0 where X = 0)
  * every rounding to nearest, ties to even, of the exact quotient: the result is
- * deterministic to the bit.  A block that holds a NaN or an infinity gets a NaN
- * scale and elements 0.
+ * deterministic to the bit.  A block that holds a NaN or an infinity, or a v past
+ * fp32's range, gets a NaN scale and elements 0.
  *   x     device, q->rows x q->cols of `type` (BITSMOE_F32 or BITSMOE_BF16),
  *         rows `ld` elements apart (ld >= cols), aligned to its elements (rows
  *         on 16-byte boundaries are read fastest; of others the aligned 16

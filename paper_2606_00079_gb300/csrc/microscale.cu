@@ -5,12 +5,13 @@
 //   E4M3 (block 16):  X = RNE_E4M3(min(a / 6, 448))
 //   code = RNE_E2M1(v / X), saturated at +-6 (0 where X = 0)
 //
-// s is a power of two, so v is exact, and every rounding is the nearest one of
-// the real quotient: the midpoints between codes times X have at most 7
-// significant bits (those between scales times 6 at most 6), and a quotient
-// v / X rounded to fp32 can only equal such a midpoint when v / X does: the
-// nearest other fp32 v is at least 2^-24 |v| away from midpoint * X, more than
-// the half ulp of a quotient next to the midpoint.
+// s is a power of two, so v is exact where it is a normal number.  (Below that
+// E4M3's codes are 0, and E8M0's come from x / X / s, never rounded where it
+// counts.)  Every rounding is the nearest one of the real quotient: the midpoints
+// between codes times X have at most 7 significant bits (those between scales
+// times 6 at most 6), and a quotient v / X rounded to fp32 can only equal such a
+// midpoint when v / X does: the nearest other fp32 v is at least 2^-24 |v| away
+// from midpoint * X, more than the half ulp of a quotient next to the midpoint.
 #include "microscale.cuh"
 
 #include <cuda_runtime.h>
@@ -128,8 +129,9 @@ __device__ __forceinline__ float element(const Eight<T>& v, int i) {
 // row), their loads in flight together; a lane 8 columns, LPB lanes a block, LPT lanes the four blocks of a scale word.
 // Neighbouring chunks of a row in neighbouring warps.  Rows and blocks past the matrix's own up to whole scale tiles are
 // written as zeros.
-// Rows of a warp: fp32 (32 bytes a lane and row) 2, bf16 4.  14336 x 4096, us with 1, 2, 4 rows: fp32 47.8, 47.5, 56.7
-// (E8M0: 5.6 TB/s) and 64.5, 64.8, 85.1 (E4M3), bf16 46.4, 35.9, 34.8 and 54.7, 48.6, 43.6.
+// Rows of a warp: fp32 (32 bytes a lane and row) 2, bf16 4.  14336 x 4096, us with 1, 2, 4 rows: fp32 46.4, 41.6, 41.4
+// (E8M0: 6.4 TB/s) and 65.0, 57.4, 66.0 (E4M3), off 16-byte boundaries 55, 54, 60 and 72, 73, 83; bf16 46.9, 36.2, 35.3
+// and 55.2, 48.3, 44.2.  What bounds all but the first is what they issue an element.
 // Rows off 16-byte boundaries (VEC false): a lane reads the aligned 16 bytes that hold its columns and shifts; there and
 // back 14336 x 4095 fp32 takes 102 us (140 element by element; 85 for 4096 columns).
 template <typename T>
@@ -165,25 +167,29 @@ __global__ void __launch_bounds__(kMThreads) k_micro_quantize(MicroArgs a) {
     uint32_t most = 0u;   // the largest magnitude's bits; a NaN's or an infinity's are above every finite one's
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      v[i] = element<T>(in[j], i) * a.inv;
+      v[i] = element<T>(in[j], i);
       most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
     }
 #pragma unroll
     for (int o = 1; o < LPB; o <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+    most = __float_as_uint(__uint_as_float(most) * a.inv);   // of x / s
     const bool bad = most >= 0x7F800000u;
     uint32_t byte, code = 0;
     if (FMT == BITSMOE_MICRO_E8M0) {
       // exponent of a: the fp32 field (subnormal a: field 0, below every usable exponent)
       byte = bad ? 0u : (uint32_t)max((int)(most >> 23) - 2, 0);
-      const float r = __uint_as_float((254u - byte) << 23);   // 1 / 2^(byte - 127), byte in [0, 252]
+      // 1 / X = 2^(127 - byte), byte in [0, 252].  x / X is below 8 s, and normal unless x / X / s is below 2^-26, so
+      // the only rounding that counts is the code's (x / s first would lose bits of subnormals that a midpoint decides by).
+      const float r = __uint_as_float((254u - byte) << 23);
 #pragma unroll
-      for (int i = 0; i < V / 2; ++i) code |= e2m1x2(v[2 * i + 1] * r, v[2 * i] * r) << (8 * i);
+      for (int i = 0; i < V / 2; ++i) code |= e2m1x2(v[2 * i + 1] * r * a.inv, v[2 * i] * r * a.inv) << (8 * i);
     } else {
       byte = scale_e4m3(__uint_as_float(most));
       const float x = micro_e4m3(byte), r = __frcp_rn(x);
       if (x > 0.f) {
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) code |= e2m1x2(quotient<T>(v[2 * i + 1], x, r), quotient<T>(v[2 * i], x, r)) << (8 * i);
+        for (int i = 0; i < V / 2; ++i)
+          code |= e2m1x2(quotient<T>(v[2 * i + 1] * a.inv, x, r), quotient<T>(v[2 * i] * a.inv, x, r)) << (8 * i);
       }
     }
     if (bad) {

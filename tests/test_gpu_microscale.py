@@ -636,3 +636,40 @@ def test_a_refused_quantisation_leaves_out_as_it_was(env):
     assert torch.equal(bm.microscale_dequantize(q), before)
     bm.microscale_quantize(x, "e4m3", 2.0, out=q)
     assert q.scale == 2.0 and torch.equal(bm.microscale_dequantize(q), bm.microscale_dequantize(bm.microscale_quantize(x, "e4m3", 2.0)))
+
+
+def test_quantizer_where_the_quotient_is_subnormal(env):
+    """x / scale below fp32's normal range: its lost bits would move values next to a midpoint between codes onto it
+    (E8M0's smallest block scale is 2^-127, the midpoints 2^-129 and up)."""
+    torch, bm = env
+    rng = np.random.default_rng(21)
+    mids = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.5], np.float64)
+    for k in (1, 3, 10, 24, 60, 100):
+        x = rng.choice(mids, (40, 64)) * 2.0 ** -127 * 2.0 ** k
+        x[20:] *= 2.0 ** rng.integers(0, 4, (20, 1))
+        with np.errstate(under="ignore"):
+            x = x.astype(np.float32)
+            j = rng.integers(0, 3, x.shape)
+            x = np.where(j == 1, np.nextafter(x, np.float32(0)), np.where(j == 2, np.nextafter(x, np.float32(1)), x))
+        x *= rng.choice([-1, 1], x.shape).astype(np.float32)
+        for fmt in ("e8m0", "e4m3"):
+            check_quantized(bm.microscale_quantize(torch.from_numpy(x).cuda(), fmt, 2.0 ** k), x, fmt, 2.0 ** k)
+            xb = bf16(x)
+            check_quantized(bm.microscale_quantize(xb.cuda(), fmt, 2.0 ** k), xb.float().numpy(), fmt, 2.0 ** k)
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+def test_quantizer_tensor_scales_far_from_one(env, fmt):
+    """Every block scale and quotient that the extremes of the tensor scale reach, normal and subnormal, and quotients
+    past fp32's range (a block without a scale)."""
+    torch, bm = env
+    rng = np.random.default_rng(22)
+    for k in (-100, -37, 37, 100):
+        e = rng.uniform(-149, 127.9, (64, 1)) if k > 0 else rng.uniform(-149, 127.9 + k / 2, (64, 1))
+        with np.errstate(under="ignore", over="ignore"):
+            x = (rng.standard_normal((64, 96)) * 2.0 ** e).astype(np.float32)
+        x = np.where(np.isfinite(x), x, np.float32(1.0))
+        check_quantized(bm.microscale_quantize(torch.from_numpy(x).cuda(), fmt, 2.0 ** k), x, fmt, 2.0 ** k)
+        xb = bf16(x)
+        xb = torch.where(torch.isfinite(xb), xb, torch.ones_like(xb))
+        check_quantized(bm.microscale_quantize(xb.cuda(), fmt, 2.0 ** k), xb.float().numpy(), fmt, 2.0 ** k)
