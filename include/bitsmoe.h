@@ -601,7 +601,10 @@ int bitsmoe_microscale_align(const void* x, int64_t x_ld, int T, int cols, void*
  *           bounded wait of the kernel ran out; not cleared by the call.  The
  *           results that such a wait has lost are NaN, with and without it
  * Products and sums are fp32 (the products of two codes, and of a code with a
- * bf16 value, are exact); y is rounded once.  Errors: INVALID_ARG, SHAPE,
+ * bf16 value, are exact); y is rounded once.  The tensor scale (with xq the product
+ * of both, which must be a normal fp32 number) multiplies the finished sum, and an
+ * E8M0 block scale may multiply its block's sum: the sums before these
+ * multiplications have to stay in fp32's range.  Errors: INVALID_ARG, SHAPE,
  * ALIGNMENT, CUDA.  Never allocates, never synchronises; one launch.  T == 0
  * and rows == 0 are successful no-ops. */
 int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bitsmoe_microscale* up, const void* x,

@@ -8,6 +8,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstring>
 
 #include "microscale.cuh"
@@ -1417,6 +1418,8 @@ extern "C" int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bit
     if ((rc = micro_check(xq))) return rc;
     if (xq->format != w->format) return BITSMOE_ERR_INVALID_ARG;
     if (xq->rows != T || xq->cols != w->cols) return BITSMOE_ERR_SHAPE;
+    // the sums are multiplied by the two tensor scales' product
+    if (!std::isnormal(w->scale * xq->scale) || (up && !std::isnormal(up->scale * xq->scale))) return BITSMOE_ERR_INVALID_ARG;
   } else if (x_ld < w->cols) {
     return BITSMOE_ERR_INVALID_ARG;
   }

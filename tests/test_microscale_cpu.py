@@ -187,3 +187,16 @@ def test_sources_name_no_multicast():
         for name in sorted(os.listdir(os.path.join(root, folder))):
             with open(os.path.join(root, folder, name), encoding="utf-8") as f:
                 assert "multicast" not in f.read(), name
+
+
+def test_product_refuses_tensor_scales_whose_product_leaves_the_range(bm):
+    """Both scales alone are in the quantiser's range; the sums times their product would be 0 inf or lost."""
+    E = bm.ERR_CODE
+
+    def f(sw, su, sx, T=3):
+        w, u = micro(bm, scale=sw), micro(bm, scale=su)
+        return bm._lib().bitsmoe_microscale_product(w, u, 0, 0, micro(bm, rows=T, scale=sx), T, A, 0, 4, 0, 0)
+    for bad in ((2.0 ** 100, 1.0, 2.0 ** 100), (1.0, 2.0 ** 64, 2.0 ** 64), (2.0 ** -100, 1.0, 2.0 ** -100), (1.0, 2.0 ** -27, 2.0 ** -100)):
+        assert f(*bad) == E["INVALID_ARG"], bad
+    for good in ((2.0 ** 100, 2.0 ** -100, 2.0 ** 27), (2.0 ** -26, 1.0, 2.0 ** -100), (3e38, 1e-37, 1.0)):
+        assert f(*good, T=0) == 0, good
