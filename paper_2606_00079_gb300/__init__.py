@@ -789,7 +789,7 @@ def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=
     if stream is not None or torch._C._cuda_getDevice() != dev.index:
         with _elsewhere(where, dev, stream):
             return microscale_product(w, x, up, dtype, y, status)
-    if type(x) is Microscale:
+    if isinstance(x, Microscale):
         T, x_ptr, x_ld, xq = x.rows, None, 0, x._c
     else:
         x_ld = _rows(where, "x", x, None, w.cols, None, torch.bfloat16)

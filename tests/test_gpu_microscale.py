@@ -673,3 +673,16 @@ def test_quantizer_tensor_scales_far_from_one(env, fmt):
         xb = bf16(x)
         xb = torch.where(torch.isfinite(xb), xb, torch.ones_like(xb))
         check_quantized(bm.microscale_quantize(xb.cuda(), fmt, 2.0 ** k), xb.float().numpy(), fmt, 2.0 ** k)
+
+
+def test_product_takes_subclasses_of_microscale(env):
+    torch, bm = env
+
+    class Mine(bm.Microscale):
+        pass
+
+    rng = np.random.default_rng(3)
+    w = upload(env, make(rng, 40, 96, "e4m3"), "e4m3")
+    a = bm.microscale_quantize(torch.randn(5, 96, device="cuda"), "e4m3")
+    mine = Mine(a.codes, a.scales, 5, 96, "e4m3", a.scale)
+    assert torch.equal(bm.microscale_product(w, mine), bm.microscale_product(w, a))
