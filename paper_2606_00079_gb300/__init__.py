@@ -549,18 +549,20 @@ _GATE_NONE, _GATE_TOKEN, _GATE_ELEMENT = 0, 1, 2
 _torch = None
 _DENSE = {}          # torch dtype -> BITSMOE_F32 / BITSMOE_BF16
 _raw_stream = None   # device index -> the current stream's handle
+_current = None      # the current device's index
 
 
 _MAX_ROWS = 1 << 24   # the library's limit of rows; beyond 32 bits a size would be cut on its way there
 
 
 def _load_torch():
-    global _torch, _DENSE, _raw_stream
+    global _torch, _DENSE, _raw_stream, _current
     import torch
     _DENSE = {torch.float32: 0, torch.bfloat16: 1}
     # the handle without a Stream object around it, where torch has it (0.1 us instead of 2)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
         lambda i: torch.cuda.current_stream(i).cuda_stream)
+    _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _torch = torch
     return torch
 
@@ -740,7 +742,7 @@ def microscale_quantize(x, fmt: str = "e8m0", scale: float = 1.0, out: Optional[
     dev = x.device
     ty = _dense_type(where, "x", x.dtype)
     ld = _rows(where, "x", x)
-    if stream is not None or torch._C._cuda_getDevice() != dev.index:
+    if stream is not None or _current() != dev.index:
         with _elsewhere(where, dev, stream):
             return microscale_quantize(x, fmt, scale, out)
     rows, cols = x.shape
@@ -763,7 +765,7 @@ def microscale_dequantize(q: Microscale, dtype=None, out=None, stream=None):
     dev = q.device
     if dev.type != "cuda":
         _refuse(where, "the matrix must be on a CUDA device")
-    if stream is not None or torch._C._cuda_getDevice() != dev.index:
+    if stream is not None or _current() != dev.index:
         with _elsewhere(where, dev, stream):
             return microscale_dequantize(q, dtype, out)
     if out is None:
@@ -786,7 +788,7 @@ def microscale_product(w: Microscale, x, up: Optional[Microscale] = None, dtype=
     dev = w.device
     if dev.type != "cuda" or x.device != dev or (up is not None and up.device != dev):
         _refuse(where, "the operands must be on one CUDA device")
-    if stream is not None or torch._C._cuda_getDevice() != dev.index:
+    if stream is not None or _current() != dev.index:
         with _elsewhere(where, dev, stream):
             return microscale_product(w, x, up, dtype, y, status)
     if isinstance(x, Microscale):
@@ -832,7 +834,7 @@ def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: 
     where = "block_norm"
     dev = h.device
     h_type, h_ld = _dense_type(where, "h", h.dtype), _rows(where, "h", h)
-    if stream is not None or torch._C._cuda_getDevice() != dev.index:
+    if stream is not None or _current() != dev.index:
         with _elsewhere(where, dev, stream):
             return block_norm(h, y, post_norm=post_norm, post_gain=post_gain, post_eps=post_eps, gate=gate,
                               gate_sigmoid=gate_sigmoid, channel_scale=channel_scale, branch_scale=branch_scale,

@@ -200,3 +200,16 @@ def test_product_refuses_tensor_scales_whose_product_leaves_the_range(bm):
         assert f(*bad) == E["INVALID_ARG"], bad
     for good in ((2.0 ** 100, 2.0 ** -100, 2.0 ** 27), (2.0 ** -26, 1.0, 2.0 ** -100), (3e38, 1e-37, 1.0)):
         assert f(*good, T=0) == 0, good
+
+
+def test_wrappers_do_without_torch_internals(bm, monkeypatch):
+    """Where torch lacks the fast forms of the current device and stream, its public ones are used."""
+    torch = pytest.importorskip("torch")
+    for name in ("_torch", "_DENSE", "_raw_stream", "_current"):
+        monkeypatch.setattr(bm, name, getattr(bm, name))
+    for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+        monkeypatch.delattr(torch._C, name, raising=False)
+    bm._load_torch()
+    assert bm._current is torch.cuda.current_device
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda i: type("S", (), {"cuda_stream": 40 + i}))
+    assert bm._raw_stream(2) == 42
