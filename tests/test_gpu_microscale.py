@@ -686,3 +686,24 @@ def test_product_takes_subclasses_of_microscale(env):
     a = bm.microscale_quantize(torch.randn(5, 96, device="cuda"), "e4m3")
     mine = Mine(a.codes, a.scales, 5, 96, "e4m3", a.scale)
     assert torch.equal(bm.microscale_product(w, mine), bm.microscale_product(w, a))
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+@pytest.mark.parametrize("T,rows,cols", [(3, 130, 777), (14, 300, 1301), (20, 300, 777), (70, 140, 2041), (300, 260, 515), (300, 1500, 1301)])
+def test_rows_off_boundaries_against_rows_on_them(env, fmt, T, rows, cols):
+    """What the kernels read element by element, what the binding copies first (the last case) and what comes by TMA:
+    the same values, with and without the second matrix."""
+    torch, bm = env
+    rng = np.random.default_rng([T, cols])
+    w, u = (upload(env, make(rng, rows, cols, fmt), fmt) for _ in range(2))
+    x = bf16(rng.standard_normal((T, cols))).cuda()
+    on = torch.nn.functional.pad(x, (0, -cols % 8)).contiguous()[:, :cols]
+    assert on.stride(0) % 8 == 0 and on.data_ptr() % 16 == 0 and x.stride(0) % 8
+    for up in (None, u):
+        want = bm.microscale_product(w, on, up=up)
+        y = torch.empty(T, rows, device="cuda")
+        rc = bm._lib().bitsmoe_microscale_product(w._c, up._c if up else None, x.data_ptr(), cols, None, T, y.data_ptr(), 0, rows, None,
+                                                  bm._raw_stream(0))
+        assert rc == 0
+        assert torch.equal(y, want)
+        assert torch.equal(bm.microscale_product(w, x, up=up), want)
