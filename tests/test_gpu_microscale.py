@@ -707,3 +707,33 @@ def test_rows_off_boundaries_against_rows_on_them(env, fmt, T, rows, cols):
         assert rc == 0
         assert torch.equal(y, want)
         assert torch.equal(bm.microscale_product(w, x, up=up), want)
+
+
+@pytest.mark.parametrize("x", ["bf16", "coded"])
+@pytest.mark.parametrize("T,rows,cols", [(13, 14336, 4096), (16, 130, 40000), (1, 5, 1 << 20), (3, 7, (1 << 20) - 37)])
+def test_product_where_few_tokens_take_the_other_kernels(env, x, T, rows, cols):
+    """More slots a CTA than the kernel of few tokens gains with, and activations that its shared memory does not hold."""
+    check_product(env, T, rows, cols, "e4m3", x == "coded", False, "f32")
+    check_product(env, T, rows, cols, "e8m0", x == "coded", True, "bf16")
+
+
+def test_largest_numbers_of_rows_and_tokens(env):
+    """2^24 rows or tokens: the last ones equal the same ones alone."""
+    torch, bm = env
+    n = 1 << 24
+    g = torch.Generator().manual_seed(1)
+    big = torch.zeros(n, 32, dtype=torch.bfloat16, device="cuda")
+    big[-200:] = torch.randn(200, 32, generator=g).bfloat16().cuda()
+    small = torch.randn(3, 32, generator=g).bfloat16().cuda()
+    q, last, few = bm.microscale_quantize(big), bm.microscale_quantize(big[-200:]), bm.microscale_quantize(small)
+    for a in (small, few):
+        y = bm.microscale_product(q, a)
+        assert torch.equal(y[:, -200:], bm.microscale_product(last, a)) and int(torch.count_nonzero(y[:, :-200])) == 0
+        del y
+    for a, b in ((big, big[-200:]), (q, last)):
+        y = bm.microscale_product(few, a)
+        assert torch.equal(y[-200:], bm.microscale_product(few, b)) and int(torch.count_nonzero(y[:-200])) == 0
+    y = bm.microscale_dequantize(q, torch.bfloat16)
+    assert torch.equal(y[-200:], bm.microscale_dequantize(last, torch.bfloat16)) and int(torch.count_nonzero(y[:-200])) == 0
+    _, x = bm.block_norm(big)
+    assert torch.equal(x[-200:], bm.block_norm(big[-200:])[1]) and int(torch.count_nonzero(x[:-200])) == 0
