@@ -311,10 +311,12 @@ __device__ __forceinline__ void copy1(uint8_t* dst, const uint8_t* src, uint32_t
 
 // Blocks that stay, whose rows come ahead by bulk copies into a ring of slots in shared memory; the factors of a
 // thread's columns stay in its registers.  VEC 8: many rows on 16-byte boundaries; the same operations in the same
-// order as above, so a row's result does not depend on how many there are.  VEC 1: rows of more than 256 elements off
-// those boundaries, however many.  The copies take the aligned 16 bytes at both ends whole (they hold
-// elements of the row, so they can be read; the others are not used).  16384 rows of 4095: fp32 162 us (5.8
-// TB/s), bf16 169 (bound by what it issues, an element at a time); element by element from global memory 737 and 691.
+// order as above, so a row's result does not depend on how many there are that are read so.  (A row alone has no pitch:
+// at an aligned address it is read by eights also where its batch is not, and its sums then take another order.)
+// VEC 1: rows of more than 256 elements off those boundaries, however many.  The copies take the aligned 16 bytes at
+// both ends whole (they hold elements of the row, so they can be read; the others are not used).  16384 rows of 4095:
+// fp32 162 us (5.8 TB/s), bf16 169 (bound by what it issues, an element at a time); element by element from global
+// memory 737 and 691.
 constexpr int kMaxSlots = 8;
 
 template <int VEC, int NV, int TH, int HT, int YT>   // TH: threads at most

@@ -302,3 +302,39 @@ def test_a_block_with_routed_experts_and_a_shared_expert(env, T, act):
     r = 1 / np.sqrt((w2 * w2).mean(axis=1, keepdims=True) + 1e-6)
     rel = np.linalg.norm(eh, axis=1, keepdims=True) / np.linalg.norm(w2, axis=1, keepdims=True)
     check(xn, wx, np.abs(f(gain[2])) * r * eh + ((D / 2 + 9) * u + rel) * np.abs(wx), "bf16", "x")
+
+
+@pytest.mark.parametrize("T,D", [(2600, 512), (700, 2048), (500, 4096), (300, 4104), (300, 8192), (200, 12288), (200, 16384)])
+def test_many_rows_on_boundaries(env, T, D):
+    """More rows than run at once: they come through the ring of the 8-wide kernel.  The formula, with the gate per
+    element and per token, in place, and the same rows alone (one block a row, in registers) to the bit."""
+    torch, bm = env
+    run_case(env, T, D, gate="element", sigmoid=True, channel=True)
+    run_case(env, T, D, h="bf16", y="f32", gate="element", seed=1)
+    run_case(env, T, D, h="bf16", y="bf16", x="f32", post=False, gate="token", sigmoid=True, seed=2)
+    g = torch.Generator().manual_seed(D)
+    h, y = torch.randn(T, D, generator=g).cuda(), torch.randn(T, D, generator=g).bfloat16().cuda()
+    e, w = torch.randn(T, D, generator=g).bfloat16().cuda(), torch.rand(D, generator=g).cuda()
+    f = lambda a, b, c, **kw: bm.block_norm(a, b, post_norm=True, post_gain=w, gate=c, gate_sigmoid=True, pre_gain=w, **kw)  # noqa: E731
+    ho, x = f(h, y, e)
+    for i in (0, 1, T // 2, T - 1):
+        ah, ax = f(h[i:i + 1], y[i:i + 1], e[i:i + 1])
+        assert torch.equal(ho[i:i + 1], ah) and torch.equal(x[i:i + 1], ax)
+    _, x2 = f(h, y, e, h_out=h)
+    assert torch.equal(h, ho) and torch.equal(x2, x)
+
+
+@pytest.mark.parametrize("D", [96, 512, 4096])
+def test_an_aligned_row_of_an_odd_pitch_alone(env, D):
+    """One row has no pitch and is read eight elements at a time; in its batch it is not.  The sums take different orders,
+    both near the formula."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(D)
+    buf = torch.randn(9 * (D + 1), generator=g).cuda()
+    h = buf.view(9, D + 1)[:, :D]
+    w = torch.rand(D, generator=g).cuda()
+    _, _, want = om.block_norm(h.double().cpu().numpy(), pre=w.double().cpu().numpy())
+    _, many = bm.block_norm(h, pre_gain=w, x_dtype=torch.float32)
+    _, one = bm.block_norm(h[8:], pre_gain=w, x_dtype=torch.float32)   # (it starts on a 16-byte boundary)
+    check(many, want, (D / 2 + 12) * u * np.abs(want), "f32", "many")
+    check(one, want[8:], (D / 2 + 12) * u * np.abs(want[8:]), "f32", "one")
