@@ -631,7 +631,8 @@ int bitsmoe_microscale_product(const bitsmoe_microscale* w, const bitsmoe_micros
  * Types are BITSMOE_F32 or BITSMOE_BF16; every pointer is aligned to its
  * elements (all rows on 16-byte boundaries with D a multiple of 8 are fastest;
  * of others the aligned 16 bytes at a row's two ends are read whole).
- * x must not overlap an input, nor h_out one other than h.  fp32 arithmetic.
+ * x must not overlap an input, nor h_out one other than h.  fp32 arithmetic (a
+ * row's sum of squares has to stay in its range).
  * 1 <= D <= BITSMOE_BLOCK_NORM_MAX_D, T <= 2^24.  Errors: INVALID_ARG, SHAPE,
  * ALIGNMENT, CUDA.  Never allocates, never synchronises; one launch; T == 0 is
  * a successful no-op. */

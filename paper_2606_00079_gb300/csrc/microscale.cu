@@ -133,7 +133,7 @@ __device__ __forceinline__ float element(const Eight<T>& v, int i) {
 // (E8M0: 6.4 TB/s) and 65.0, 57.4, 66.0 (E4M3), off 16-byte boundaries 55, 54, 60 and 72, 73, 83; bf16 46.9, 36.2, 35.3
 // and 55.2, 48.3, 44.2.  What bounds all but the first is what they issue an element.
 // Rows off 16-byte boundaries (VEC false): a lane reads the aligned 16 bytes that hold its columns and shifts; there and
-// back 14336 x 4095 fp32 takes 102 us (140 element by element; 85 for 4096 columns).
+// back 14336 x 4095 fp32 takes 98 us (140 element by element; 82 for 4096 columns).
 template <typename T>
 constexpr int kRowsOfWarp = sizeof(T) == 4 ? 2 : 4;
 
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kMThreads) k_micro_quantize(MicroArgs a) {
 
 // Four rows 32 apart a warp, V columns a lane in 16 bytes of the result, so that a store writes whole sectors (rows off
 // 16-byte boundaries: turned in shared memory, so that neighbouring lanes still write neighbouring elements); the rows' scale
-// words are one 16-byte load.  14336 x 4096 to fp32: 40 us, 6.6 TB/s; with 32 bytes a lane in two stores 56 us.
+// words are one 16-byte load.  14336 x 4096 to fp32: 40 us, 6.6 TB/s (to bf16 27 to 28); with 32 bytes a lane in two stores 56 us.
 template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(kMThreads) k_micro_dequantize(MicroArgs a) {
   constexpr int V = 16 / sizeof(T), LPB = (FMT == BITSMOE_MICRO_E8M0 ? 32 : 16) / V, LPT = 4 * LPB;

@@ -565,8 +565,8 @@ struct FewPlan {
 // Measured, us here and by the decoded tiles: 1, 8, 12, 16 tokens of 14336 rows x 4096 (16 slots a CTA) 12.0, 16.9,
 // 22.2, 25.5 and 21.6, 22.1, 22.3, 22.3, with SwiGLU 19.9, 25.1, 32.7, 36.1 and 32.9, 34.0, 34.4, 34.7; of 4096 x 14336
 // (14 slots) 11.6, 15.7, 20.2, 22.6 and 21.3, 21.4, 21.6, 21.6; 16 of 2048 x 2048 (2 slots) 6.9 and 11.8.  For
-// coded tokens the block-scaled MMAs take 10.2 at 1 to 24 tokens, so only small products stay here (2048 x 2048: 5.0
-// to 6.6 against 9.3 to 10.1).
+// coded tokens the block-scaled MMAs take 9.5 at 1 to 24 tokens, so only small products stay here (2048 x 2048: 5.0
+// to 6.6 against 9.1 to 10.1).
 bool few_plan(int format, bool glu, bool coded, int T, int rows, int cols, int (*resident)(int), FewPlan* p) {
   if (T > kFewTokens) return false;
   const int CPS = format == BITSMOE_MICRO_E8M0 ? 2 : 4;
@@ -732,7 +732,8 @@ struct CodedArgs {
 // tiles' way from L2 to the SMs: loads alone 175 us, MMAs alone 125 (100, and the turn of the accumulator: one of 256
 // tokens leaves no room for a second beside the scales).  Every CTA loads its own tiles: the library also runs as
 // replicas on several GPUs, which rules out loads spread over a cluster (with them 166 us).
-// Few tokens: 4096 x 14336, 8 tokens 9.7 us (floor 4.9: the codes' bytes; a launch and a cluster's sum are 5 us of it).
+// Few tokens: 4096 x 14336, 1 token 9.9 us, 14336 x 4096, 8 tokens 9.3 (floor 4.9: the codes' bytes; 112 of 152 SMs have
+// a row tile).
 //
 // 128 weight rows x N tokens a CTA at a time (with GLU 128 rows of both matrices).  Codes come by TMA, 256 columns
 // a stage, scale tiles by bulk copies; the MMA warp moves a stage's scales into tensor memory (columns of the
