@@ -762,7 +762,8 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
   uint64_t* afull = empty + S;
   uint64_t* aempty = afull + 2;
   uint64_t* drained = aempty + 2;   // after a wait of the MMA warp that ran out: the MMAs that it had issued
-  uint32_t* slot = reinterpret_cast<uint32_t*>(drained + 1);
+  uint64_t* quiet = drained + 1;    // nothing more is written to the rings
+  uint32_t* slot = reinterpret_cast<uint32_t*>(quiet + 1);
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int rank = blockIdx.y;
   const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
@@ -781,6 +782,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
       mbar_init_n(aempty + i, 8);
     }
     mbar_init_n(drained, 1);
+    mbar_init_n(quiet, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (wid == 1) tmem_alloc(slot, 512);
@@ -819,6 +821,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
         }
       }
       for (int j = max(0, n - S); j < n; ++j) mbar_wait(full + j % S, (uint32_t)(j / S) & 1u);   // copies in flight
+      mbar_arrive(quiet);
     }
     __syncwarp();
   } else if (wid == 1) {
@@ -884,6 +887,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1)
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const int m = tile % g.mt * 128 + r, t0 = tile / g.mt * N;
       if (!ok) {
+        if (g.splits > 1) mbar_wait_idle(quiet, 0u, 4 * (g.spin + kWaitClocks));   // (the partial tile lies in the rings)
         lost_tokens(half ? nh : 0, half ? N : nh, g.splits > 1 ? red + r : nullptr, N, NA, t0, g.T, m, g.rows, g.y, g.y_type, g.y_ld);
         continue;
       }
@@ -962,7 +966,7 @@ cudaError_t launch_coded_g(const bitsmoe_microscale* w, const bitsmoe_microscale
   g.nbuf = splits == 1 && 2 * NA * g.N + fit * sf_cols <= 512 ? 2 : 1;
   g.stages = std::min(fit, (512 - g.nbuf * NA * g.N) / sf_cols);
   const size_t ring = (size_t)g.stages * g.stage, redb = splits > 1 ? (size_t)NA * g.N * 512 : 0;
-  if (1024 + std::max(ring, redb) + (size_t)(2 * g.stages + 4) * 8 + 16 > kAllShared) return cudaErrorInvalidValue;
+  if (1024 + std::max(ring, redb) + (size_t)(2 * g.stages + 6) * 8 + 4 > kAllShared) return cudaErrorInvalidValue;
   CUtensorMap wm, um, xm;
   const int64_t pitch = micro_pitch(g.cols);
   if (!make_row_map(&wm, true, w->codes, g.rows, pitch, pitch, 128) || !make_row_map(&xm, true, xq->codes, g.T, pitch, pitch, g.N))
@@ -1094,7 +1098,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   uint64_t* afull = qempty + Q;
   uint64_t* aempty = afull + 2;
   uint64_t* drained = aempty + 2;   // after a wait of the MMA warp that ran out: the MMAs that it had issued
-  uint32_t* slot = reinterpret_cast<uint32_t*>(drained + 1);
+  uint64_t* quiet = drained + 1;    // nothing more is written to the rings
+  uint32_t* slot = reinterpret_cast<uint32_t*>(quiet + 1);
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int rank = blockIdx.y;
   const int st0 = rank * g.sps, nk = max(0, min(g.sps, g.nst - st0));
@@ -1118,6 +1123,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       mbar_init_n(aempty + i, 4);
     }
     mbar_init_n(drained, 1);
+    mbar_init_n(quiet, 2 + kDecodeGroups * kDecodeWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (wid == 1) tmem_alloc(slot, 512);
@@ -1151,6 +1157,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         }
       }
       for (int j = max(0, n - P); j < n; ++j) mbar_wait(pfull + j % P, (uint32_t)(j / P) & 1u);   // copies in flight
+      mbar_arrive(quiet);
     }
     __syncwarp();
   } else if (wid == 1) {
@@ -1215,6 +1222,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       // copies in flight: their bytes end a phase only with the decoders' arrivals, which may be missing after a timeout
       for (int j = max(0, n - Q); j < n; ++j) mbar_wait(qfull + j % Q, (uint32_t)(j / Q) & 1u, ok ? kWaitClocks : g.spin);
     }
+    mbar_arrive(lane == 0, quiet);
     __syncwarp();
   } else if (wid >= 4 && wid < 4 + kDecodeGroups * kDecodeWarps) {
     const int dw = (wid - 4) % kDecodeWarps, group = (wid - 4) / kDecodeWarps;
@@ -1276,6 +1284,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         if (++ps == (uint32_t)P) ps = 0, pp ^= 1u;
       }
     }
+    __syncwarp();
+    mbar_arrive(lane == 0, quiet);
   } else if (wid >= 4 + kDecodeGroups * kDecodeWarps) {
     const int r = 32 * (wid & 3) + lane;
     int it = 0;
@@ -1286,6 +1296,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const int m = tile % g.mt * 128 + r, t0 = tile / g.mt * N;
       if (!ok) {
+        if (g.splits > 1) mbar_wait_idle(quiet, 0u, 4 * (g.spin + kWaitClocks));
         lost_tokens(0, N, g.splits > 1 ? red + r : nullptr, N, NA, t0, g.T, m, g.rows, g.y, g.y_type, g.y_ld);
         continue;
       }
@@ -1358,7 +1369,7 @@ cudaError_t launch_wide_k(const bitsmoe_microscale* w, const bitsmoe_microscale*
   while (splits < 8 && (int64_t)g.ntiles * splits * 2 <= sms && g.nst >= 2 * splits && (uint32_t)(NA * g.N) * 512u <= rings) splits *= 2;
   g.splits = splits;
   g.sps = (g.nst + splits - 1) / splits;
-  if (1024 + (size_t)rings + (size_t)(2 * g.P + 2 * g.Q + 4) * 8 + 16 > kAllShared) return cudaErrorInvalidValue;
+  if (1024 + (size_t)rings + (size_t)(2 * g.P + 2 * g.Q + 6) * 8 + 4 > kAllShared) return cudaErrorInvalidValue;
   const int64_t pitch = micro_pitch(g.cols);
   CUtensorMap wm, um, xm;
   if (!make_row_map(&wm, true, w->codes, g.rows, pitch, pitch, 128)) return cudaErrorInvalidValue;
