@@ -564,7 +564,9 @@ struct FewPlan {
 // How T tokens run on the kernel for few of them, or false when their activations do not fit shared memory.
 // Measured, us here and by the decoded tiles: 1, 8, 12, 16 tokens of 14336 rows x 4096 (16 slots a CTA) 12.0, 16.9,
 // 22.2, 25.5 and 21.6, 22.1, 22.3, 22.3, with SwiGLU 19.9, 25.1, 32.7, 36.1 and 32.9, 34.0, 34.4, 34.7; of 4096 x 14336
-// (14 slots) 11.6, 15.7, 20.2, 22.6 and 21.3, 21.4, 21.6, 21.6; 16 of 2048 x 2048 (2 slots) 6.9 and 11.8.  For
+// (14 slots) 11.6, 15.7, 20.2, 22.6 and 21.3, 21.4, 21.6, 21.6; 16 of 2048 x 2048 (2 slots) 6.9 and 11.8.  Longer
+// ones: 9, 12 tokens of 14336 x 8192 (32 slots) 32.9, 34.5 and 40.0, 40.1, with SwiGLU 54.9, 56.5 and 62.1, 62.5; of
+// 8192 x 28672 (56 slots) 52.4, 61.0 and 66.8, 66.8.  For
 // coded tokens the block-scaled MMAs take 9.5 at 1 to 24 tokens, so only small products stay here (2048 x 2048: 5.0
 // to 6.6 against 9.1 to 10.1).
 bool few_plan(int format, bool glu, bool coded, int T, int rows, int cols, int (*resident)(int), FewPlan* p) {
