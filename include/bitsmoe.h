@@ -657,6 +657,147 @@ typedef struct bitsmoe_block_norm_args {
 } bitsmoe_block_norm_args;
 int bitsmoe_block_norm(const bitsmoe_block_norm_args* args, void* stream);
 
+/* Rows in 8 bits (no counterpart in the paper): E4M3 codes (1 sign, 4 exponent, 3
+ * mantissa bits; 448 at most) with a fp32 scale for each row,
+ *     value[r][k] = code * scales[r].
+ *   rows, cols  0 .. 2^24, 1 .. 2^20
+ *   codes   device, rows `ld` bytes apart (ld >= cols; rows on 16-byte boundaries
+ *           are read and written fastest, and bitsmoe_expert_product's tensor-core
+ *           kernels want them); what lies between the rows is not touched
+ *   scales  device, rows fp32 */
+#define BITSMOE_E4M3 2
+typedef struct bitsmoe_rowscale {
+  int32_t rows, cols;
+  int64_t ld;
+  uint8_t* codes;
+  float* scales;
+} bitsmoe_rowscale;
+
+/* Code dense rows (weights once, or activations before a product), asynchronously
+ * on `stream`: a = max_k |x[r][k]|,
+ *   scale = 2^max(-100, ceil(log2(a / 448)))    (the smallest power of two with a / scale <= 448; 2^-100 for zeros)
+ *   code  = E4M3 of x / scale, to nearest, ties to even
+ * A power of two, so that the quotient is exact and the code's rounding the only
+ * one (and the values exact in bf16): the result is deterministic to the bit.
+ * A row that holds a NaN or an infinity gets a NaN scale and codes 0.
+ *   x     device, q->rows x q->cols of `type` (BITSMOE_F32 or BITSMOE_BF16), rows `ld`
+ *         elements apart, aligned to its elements (rows on 16-byte boundaries are
+ *         read fastest; of others the aligned 16 bytes at a row's two ends are read whole)
+ * Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.  Never allocates, never
+ * synchronises; one launch.  rows == 0 is a successful no-op. */
+int bitsmoe_rowscale_quantize(const void* x, int type, int64_t ld, const bitsmoe_rowscale* q, void* stream);
+
+/* The values of such rows, code * scale in fp32 (any scale), rounded to `type`: x
+ * device, rows x cols, rows `ld` elements apart.  Errors and the rest as
+ * bitsmoe_rowscale_quantize. */
+int bitsmoe_rowscale_dequantize(const bitsmoe_rowscale* q, void* x, int type, int64_t ld, void* stream);
+
+/* bitsmoe_block_norm with x in 8 bits: args->x_type is BITSMOE_E4M3, args->x the codes
+ * (T x D bytes, rows args->x_ld bytes apart; not NULL unless T is 0) and x_scale
+ * (device, T fp32, written) the rows' scales, as bitsmoe_rowscale_quantize forms them
+ * from the fp32 x (a row whose x is not finite: NaN scale, codes 0).  Errors and the
+ * rest as bitsmoe_block_norm. */
+int bitsmoe_block_norm_rowscale(const bitsmoe_block_norm_args* args, float* x_scale, void* stream);
+
+/* Routing of T tokens among E experts as lists of its own, for
+ * bitsmoe_expert_product and bitsmoe_expert_combine (bitsmoe_moe_forward routes
+ * inside), asynchronously on `stream`:
+ *   logits   device, T x E fp32, rows ld elements apart (ld >= E)
+ *   top_k    1 .. min(E, 32); E <= 1024; T * top_k <= 2^24
+ *   experts  device, T x top_k int32: each token's experts by descending logit (ties
+ *            to the lower expert; -0 and +0 tie).  A NaN or -infinity is never
+ *            selected: where fewer than top_k logits are left (a padded token's are
+ *            all -infinity) the rest of the row is -1
+ *   weights  device, T x top_k fp32: the softmax over the selected logits
+ *            (renormalize != 0) or over all that are not NaN; 0 at expert -1.  (A
+ *            +infinity among them gives NaN weights, as the formula does.)
+ *   offsets  device, E + 1 int32: the pairs of expert e are offsets[e] .. offsets[e + 1]
+ *   pairs    device, T * top_k int32: the pairs' numbers t * top_k + j in the order of
+ *            their experts, by number within one; -1 from offsets[E] on
+ *   places   device, T x top_k int32: where pairs holds that number; -1 at expert -1
+ *   ws       device workspace of >= bitsmoe_route_workspace_bytes(T, E, top_k) bytes,
+ *            16-byte aligned, not used by another call in flight (no initialisation
+ *            needed); may be NULL where that is 0
+ * The result is deterministic to the bit.  Errors: INVALID_ARG, SHAPE, ALIGNMENT,
+ * WORKSPACE_TOO_SMALL, CUDA.  Never allocates, never synchronises; one launch, or two.
+ * T == 0 writes the offsets (zeros).  bitsmoe_route_workspace_bytes is 0 for invalid
+ * arguments. */
+size_t bitsmoe_route_workspace_bytes(int T, int E, int top_k);
+int bitsmoe_route(const float* logits, int64_t ld, int T, int E, int top_k, int renormalize, int32_t* experts,
+                  float* weights, int32_t* offsets, int32_t* pairs, int32_t* places, void* ws, size_t ws_bytes,
+                  void* stream);
+
+/* Dense matrices of E experts (no counterpart in the paper, whose experts are
+ * spectral: the float original that a layer is compared with, layers that stay
+ * unquantised, shared experts), each rows x cols:
+ *   type    BITSMOE_BF16, or BITSMOE_E4M3 with a scale for each row
+ *   data    device; element (e, r, c) at e * expert_ld + r * ld + c
+ *   scales  device, fp32, that of row r of expert e at e * scale_ld + r; not read for bf16 */
+typedef struct bitsmoe_expert_matrices {
+  int32_t type, experts, rows, cols;
+  int64_t ld, expert_ld, scale_ld;
+  const void* data;
+  const float* scales;
+} bitsmoe_expert_matrices;
+
+/* Products grouped by expert with ragged sizes, asynchronously on `stream`: for
+ * offsets[e] <= p < offsets[e + 1]
+ *   y[p][r] = sum_k W_e[r][k] x[q][k]                                   (up NULL)
+ *   y[p][r] = SiLU(sum_k W_e[r][k] x[q][k]) * sum_k U_e[r][k] x[q][k]   (up = U)
+ * with q = p (index NULL) or index[p] / fan (the pairs of bitsmoe_route with fan =
+ * top_k pick the token of each pair).
+ *   w, up      the experts' matrices (experts 1 .. 1024, rows 0 .. 2^20, cols 1 .. 2^20);
+ *              up NULL or of w's type and sizes
+ *   x          device, x_rows x w->cols of w->type, rows x_ld elements apart;
+ *              x_scales: its rows' scales (fp32, device) where w is coded, else not read
+ *   offsets    device, experts + 1 int32, ascending, between 0 and P (others are taken
+ *              as the nearest such value)
+ *   index      device, P int32, or NULL; an entry between offsets[0] and
+ *              offsets[experts] whose q is not a row of x gives a row of NaN
+ *   P          rows of y (0 .. 2^24); those that no expert has are not touched
+ *   y          device, P x w->rows of y_type (BITSMOE_F32 or BITSMOE_BF16), rows y_ld elements
+ *              apart (nothing between its rows is touched); must not overlap the inputs
+ *   status     device int or NULL: BITSMOE_ERR_TIMEOUT is written there if a bounded wait
+ *              of the kernel ran out; not cleared by the call.  The results that such a
+ *              wait has lost are NaN, with and without it
+ * Products are exact and sums fp32; scales multiply the finished sums (which have to
+ * stay in fp32's range before and after it); y is rounded once.  w, up and x whose rows
+ * (and matrices) all start on 16-byte boundaries go through the tensor cores; others are
+ * multiplied by fp32 instructions, many times slower.  Errors: INVALID_ARG, SHAPE,
+ * ALIGNMENT, CUDA.  Never allocates, never synchronises; one launch.  P == 0 and rows == 0
+ * are successful no-ops. */
+typedef struct bitsmoe_expert_product_args {
+  const bitsmoe_expert_matrices* w;
+  const bitsmoe_expert_matrices* up;
+  const void* x;
+  const float* x_scales;
+  int64_t x_ld;
+  int32_t x_rows, P;
+  const int32_t* offsets;
+  const int32_t* index;
+  int32_t fan, y_type;
+  void* y;
+  int64_t y_ld;
+  int* status;
+} bitsmoe_expert_product_args;
+int bitsmoe_expert_product(const bitsmoe_expert_product_args* args, void* stream);
+
+/* The weighted sum that ends a layer of experts, asynchronously on `stream`:
+ *   out[t][d] = base[t][d] + sum_j weights[t][j] y[places[t][j]][d]
+ * in fp32, j ascending, base last, rounded once; a place outside 0 .. P - 1 (-1: the
+ * token has no such expert) adds nothing.
+ *   y        device, P x D of y_type, rows y_ld elements apart
+ *   places, weights  device, T x top_k int32 and fp32 (of bitsmoe_route); top_k 1 .. 32
+ *   base     device, T x D of out_type, rows base_ld apart, or NULL (0); may be out itself
+ *            (same pitch)
+ *   out      device, T x D of out_type, rows out_ld apart, written; must not overlap y
+ * 1 <= D <= 2^20; T, P 0 .. 2^24.  Types are BITSMOE_F32 or BITSMOE_BF16.  Errors: INVALID_ARG,
+ * SHAPE, ALIGNMENT, CUDA.  Never allocates, never synchronises; one launch.  T == 0 is a
+ * successful no-op. */
+int bitsmoe_expert_combine(const void* y, int y_type, int64_t y_ld, int P, const int32_t* places, const float* weights,
+                           int T, int top_k, int D, const void* base, int64_t base_ld, void* out, int out_type,
+                           int64_t out_ld, void* stream);
+
 /* Where bitsmoe_moe_block_forward(T, top_k) leaves the block's normalised
  * activations x (T x D bf16) and router logits (T x E fp32) in its workspace:
  * byte offsets from the workspace start, valid after the call completes (the

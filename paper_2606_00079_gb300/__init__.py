@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Dict, Optional
+from typing import Dict, NamedTuple, Optional
 
 import numpy as np
 
@@ -57,6 +57,23 @@ class _BlockNormArgs(ctypes.Structure):
                 + [(n, ctypes.c_int64) for n in ("h_ld", "y_ld", "gate_ld", "h_out_ld", "x_ld")])
 
 
+class _Rowscale(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("ld", ctypes.c_int64), ("codes", _P),
+                ("scales", _P)]
+
+
+class _ExpertMatrices(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("type", "experts", "rows", "cols")]
+                + [(n, ctypes.c_int64) for n in ("ld", "expert_ld", "scale_ld")] + [("data", _P), ("scales", _P)])
+
+
+class _ExpertProductArgs(ctypes.Structure):
+    _fields_ = [("w", ctypes.POINTER(_ExpertMatrices)), ("up", ctypes.POINTER(_ExpertMatrices)), ("x", _P),
+                ("x_scales", _P), ("x_ld", ctypes.c_int64), ("x_rows", ctypes.c_int32), ("P", ctypes.c_int32),
+                ("offsets", _P), ("index", _P), ("fan", ctypes.c_int32), ("y_type", ctypes.c_int32), ("y", _P),
+                ("y_ld", ctypes.c_int64), ("status", _P)]
+
+
 SIGNATURES = {
     "bitsmoe_pack": (_I, [ctypes.POINTER(_LayerHost), _I, ctypes.POINTER(_P)]),
     "bitsmoe_pack_to_host": (_I, [ctypes.POINTER(_LayerHost), ctypes.POINTER(_P), ctypes.POINTER(_SZ)]),
@@ -100,6 +117,14 @@ SIGNATURES = {
     "bitsmoe_microscale_product": (_I, [ctypes.POINTER(_Microscale), ctypes.POINTER(_Microscale), _P, ctypes.c_int64,
                                         ctypes.POINTER(_Microscale), _I, _P, _I, ctypes.c_int64, _P, _P]),
     "bitsmoe_block_norm": (_I, [ctypes.POINTER(_BlockNormArgs), _P]),
+    "bitsmoe_rowscale_quantize": (_I, [_P, _I, ctypes.c_int64, ctypes.POINTER(_Rowscale), _P]),
+    "bitsmoe_rowscale_dequantize": (_I, [ctypes.POINTER(_Rowscale), _P, _I, ctypes.c_int64, _P]),
+    "bitsmoe_block_norm_rowscale": (_I, [ctypes.POINTER(_BlockNormArgs), _P, _P]),
+    "bitsmoe_route_workspace_bytes": (_SZ, [_I, _I, _I]),
+    "bitsmoe_route": (_I, [_P, ctypes.c_int64, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "bitsmoe_expert_product": (_I, [ctypes.POINTER(_ExpertProductArgs), _P]),
+    "bitsmoe_expert_combine": (_I, [_P, _I, ctypes.c_int64, _I, _P, _P, _I, _I, _I, _P, ctypes.c_int64, _P, _I,
+                                    ctypes.c_int64, _P]),
     "bitsmoe_block_norm_outputs": (_I, [_P, _I, _I, ctypes.POINTER(_SZ), ctypes.POINTER(_SZ)]),
     "bitsmoe_last_device_status": (_I, [_P, _P]),
     "bitsmoe_free": (None, [_P]),
@@ -548,6 +573,7 @@ _GATE_NONE, _GATE_TOKEN, _GATE_ELEMENT = 0, 1, 2
 
 _torch = None
 _DENSE = {}          # torch dtype -> BITSMOE_F32 / BITSMOE_BF16
+_E4M3 = 2            # BITSMOE_E4M3
 _raw_stream = None   # device index -> the current stream's handle
 _current = None      # the current device's index
 
@@ -829,7 +855,8 @@ def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: 
     h (T x D, fp32 or bf16) is the residual stream; y None: h' is not formed (the result's first item is h
     times residual_scale only when h_out is given, else None); gate is a vector of T (one value per row) or
     T x D; the gains and channel_scale are vectors of D of one type.  h_out and x are allocated when not
-    given (h_out may be h: in place); pre_norm False returns x None."""
+    given (h_out may be h: in place); pre_norm False returns x None.  x_dtype torch.float8_e4m3fn, or x a Rowscale:
+    x in 8 bits with a scale a row (see bitsmoe_block_norm_rowscale), returned as a Rowscale."""
     torch = _torch or _load_torch()
     where = "block_norm"
     dev = h.device
@@ -874,19 +901,303 @@ def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: 
     elif y is not None:
         h_out, ho_ld = torch.empty((T, D), dtype=h.dtype, device=dev), D
         ho_ptr = h_out.data_ptr()
-    if x is not None:
+    if isinstance(x, Rowscale) or (x is None and x_dtype is torch.float8_e4m3fn):
+        if not pre_norm:
+            _refuse(where, "x in 8 bits is asked for but pre_norm is off")
+        if x is None:
+            x = Rowscale.empty((T, D), dev)
+        x_type, x_ld, x_ptr = _E4M3, _rowscale_rows(where, "x", x, T, D, dev), x.codes.data_ptr()
+    elif x is not None:
         if not pre_norm:
             _refuse(where, "x is given but pre_norm is off")
         x_type, x_ld, x_ptr = _dense_type(where, "x", x.dtype), _rows(where, "x", x, T, D, dev), x.data_ptr()
     elif pre_norm:
         x = torch.empty((T, D), dtype=x_dtype if x_dtype is not None else torch.bfloat16, device=dev)
         x_type, x_ld, x_ptr = _dense_type(where, "x", x.dtype), D, x.data_ptr()
-    _check(_lib().bitsmoe_block_norm(
-        _BlockNormArgs(T, D, h_type, y_type, gate_type, gain_type, x_type, 1 if post_norm else 0, gate_kind,
-                       1 if gate_sigmoid else 0, post_eps, pre_eps, gain_offset, residual_scale, branch_scale,
-                       h.data_ptr(), y_ptr, gate_ptr, post_ptr, pre_ptr, chan_ptr, ho_ptr, x_ptr,
-                       h_ld, y_ld, gate_ld, ho_ld, x_ld), _raw_stream(dev.index)), "bitsmoe_block_norm")
+    args = _BlockNormArgs(T, D, h_type, y_type, gate_type, gain_type, x_type, 1 if post_norm else 0, gate_kind,
+                          1 if gate_sigmoid else 0, post_eps, pre_eps, gain_offset, residual_scale, branch_scale,
+                          h.data_ptr(), y_ptr, gate_ptr, post_ptr, pre_ptr, chan_ptr, ho_ptr, x_ptr,
+                          h_ld, y_ld, gate_ld, ho_ld, x_ld)
+    if x_type == _E4M3:
+        _check(_lib().bitsmoe_block_norm_rowscale(args, x.scales.data_ptr(), _raw_stream(dev.index)),
+               "bitsmoe_block_norm_rowscale")
+    else:
+        _check(_lib().bitsmoe_block_norm(args, _raw_stream(dev.index)), "bitsmoe_block_norm")
     return h_out, x
+
+
+# --------------------------------------------------------------------------
+# rows in 8 bits, routing and experts that are dense matrices (torch tensors)
+# --------------------------------------------------------------------------
+class Rowscale:
+    """Rows in 8 bits on the device: `codes` (torch.float8_e4m3fn, rows x cols, or experts x rows x cols with dense
+    rows) and `scales` (float32, one for each row); value = code * scale, see bitsmoe_rowscale in include/bitsmoe.h."""
+
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes, scales):
+        torch = _torch or _load_torch()
+        if codes.dtype is not torch.float8_e4m3fn or codes.dim() not in (2, 3):
+            _refuse("Rowscale", f"codes must be 2-d or 3-d float8_e4m3fn, got {codes.dim()}-d {codes.dtype}")
+        if scales.dtype is not torch.float32 or scales.device != codes.device:
+            _refuse("Rowscale", f"scales must be float32 on {codes.device}")
+        if scales.shape != codes.shape[:-1]:
+            _refuse("Rowscale", f"scales have shape {tuple(scales.shape)}, codes {tuple(codes.shape)}", "SHAPE")
+        if scales.dim() and scales.shape[-1] > 1 and scales.stride(-1) != 1:
+            _refuse("Rowscale", "scales must be dense along the rows")
+        self.codes, self.scales = codes, scales
+
+    @classmethod
+    def empty(cls, shape, device=None) -> "Rowscale":
+        """Uninitialised rows on a pitch of a multiple of 16 bytes."""
+        torch = _torch or _load_torch()
+        *rows, cols = shape
+        dev = device if device is not None else torch.cuda.current_device()
+        pitch = (cols + 15) // 16 * 16
+        codes = torch.empty((*rows, pitch), dtype=torch.float8_e4m3fn, device=dev)
+        self = cls.__new__(cls)
+        self.codes = codes if pitch == cols else codes[..., :cols]
+        self.scales = torch.empty(rows, dtype=torch.float32, device=dev)
+        return self
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @property
+    def device(self):
+        return self.codes.device
+
+
+def _flat(where: str, name: str, x):
+    """x as a matrix: its experts' rows one after the other."""
+    if x.dim() == 2:
+        return x
+    if x.dim() != 3:
+        _refuse(where, f"{name} must be 2-d or 3-d")
+    try:
+        return x.view(-1, x.shape[-1]) if x.shape[-1] else x.flatten(0, 1)
+    except RuntimeError:
+        _refuse(where, f"{name}'s matrices must lie one after the other")
+
+
+def _rowscale_rows(where: str, name: str, q: Rowscale, rows=None, cols=None, device=None):
+    """Checks of a 2-d Rowscale; its pitch in bytes."""
+    ld = _rows(where, name, q.codes, rows, cols, device)
+    if q.scales.shape[0] > 1 and q.scales.stride(0) != 1:
+        _refuse(where, f"{name}'s scales must be dense")
+    return ld
+
+
+def _rowscale_c(where: str, q: Rowscale):
+    """The library's view of a Rowscale (experts' rows one after the other)."""
+    codes = _flat(where, "codes", q.codes)
+    ld = _rows(where, "codes", codes)
+    if not q.scales.is_contiguous():
+        _refuse(where, "scales must be dense")
+    return _Rowscale(codes.shape[0], codes.shape[1], ld, codes.data_ptr(), q.scales.data_ptr())
+
+
+def rowscale_quantize(x, out: Optional[Rowscale] = None, stream=None) -> Rowscale:
+    """Code the rows of x (torch fp32 or bf16, 2-d, or 3-d matrices one after the other, dense rows, on the device) as
+    a Rowscale with power-of-two scales; `out` reuses an existing one of the same shape."""
+    _torch or _load_torch()
+    where = "rowscale_quantize"
+    dev = x.device
+    ty = _dense_type(where, "x", x.dtype)
+    flat = _flat(where, "x", x)
+    ld = _rows(where, "x", flat)
+    if stream is not None or _current() != dev.index:
+        with _elsewhere(where, dev, stream):
+            return rowscale_quantize(x, out)
+    if out is None:
+        out = Rowscale.empty(x.shape, dev)
+    elif out.shape != x.shape or out.device != dev:
+        _refuse(where, "out has another shape or device", "SHAPE")
+    _check(_lib().bitsmoe_rowscale_quantize(flat.data_ptr(), ty, ld, _rowscale_c(where, out), _raw_stream(dev.index)),
+           "bitsmoe_rowscale_quantize")
+    return out
+
+
+def rowscale_dequantize(q: Rowscale, dtype=None, out=None, stream=None):
+    """The values of a Rowscale as a torch tensor of its shape (float32, or bfloat16)."""
+    torch = _torch or _load_torch()
+    where = "rowscale_dequantize"
+    dev = q.device
+    if dev.type != "cuda":
+        _refuse(where, "the rows must be on a CUDA device")
+    if stream is not None or _current() != dev.index:
+        with _elsewhere(where, dev, stream):
+            return rowscale_dequantize(q, dtype, out)
+    if out is None:
+        out = torch.empty(q.shape, dtype=dtype if dtype is not None else torch.float32, device=dev)
+    elif out.shape != q.shape:
+        _refuse(where, f"out has shape {tuple(out.shape)}, expected {tuple(q.shape)}", "SHAPE")
+    flat = _flat(where, "out", out)
+    ld = _rows(where, "out", flat, None, None, dev)
+    _check(_lib().bitsmoe_rowscale_dequantize(_rowscale_c(where, q), flat.data_ptr(), _dense_type(where, "out", out.dtype),
+                                              ld, _raw_stream(dev.index)), "bitsmoe_rowscale_dequantize")
+    return out
+
+
+class Routing(NamedTuple):
+    """What `route` returns (see bitsmoe_route): the tokens' experts and weights (T x top_k), where each expert's pairs
+    begin (experts + 1), the pairs t * top_k + j in the order of their experts, and each pair's place there."""
+    experts: object
+    weights: object
+    offsets: object
+    pairs: object
+    places: object
+
+
+def route(logits, top_k: int, renormalize: bool = True, stream=None) -> Routing:
+    """Routing of the rows of logits (torch fp32, T x experts, on the device): the top_k largest (ties to the lower
+    expert), weighted by the softmax over them (renormalize) or over all; a logit of -inf or NaN is never selected, and
+    a token that has fewer others gets expert -1, weight 0 and place -1 for the rest."""
+    torch = _torch or _load_torch()
+    where = "route"
+    dev = logits.device
+    ld = _rows(where, "logits", logits, dtype=torch.float32)
+    if stream is not None or _current() != dev.index:
+        with _elsewhere(where, dev, stream):
+            return route(logits, top_k, renormalize)
+    T, E = logits.shape
+    if not 1 <= top_k <= E:
+        _refuse(where, f"top_k is {top_k} of {E} experts")
+    nws = int(_lib().bitsmoe_route_workspace_bytes(T, E, top_k))
+    i32 = torch.int32
+    experts = torch.empty((T, top_k), dtype=i32, device=dev)
+    places = torch.empty((T, top_k), dtype=i32, device=dev)
+    pairs = torch.empty(T * top_k, dtype=i32, device=dev)
+    offsets = torch.empty(E + 1, dtype=i32, device=dev)
+    weights = torch.empty((T, top_k), dtype=torch.float32, device=dev)
+    ws = torch.empty(nws, dtype=torch.uint8, device=dev) if nws else None
+    _check(_lib().bitsmoe_route(logits.data_ptr(), ld, T, E, top_k, 1 if renormalize else 0, experts.data_ptr(),
+                                weights.data_ptr(), offsets.data_ptr(), pairs.data_ptr(), places.data_ptr(),
+                                ws.data_ptr() if nws else None, nws, _raw_stream(dev.index)), "bitsmoe_route")
+    return Routing(experts, weights, offsets, pairs, places)
+
+
+def _matrices(where: str, name: str, w, device=None):
+    """The library's view of the experts' matrices: a 3-d bf16 tensor or a Rowscale of 3-d codes."""
+    if isinstance(w, Rowscale):
+        data, ty, scales = w.codes, _E4M3, w.scales
+    else:
+        data, ty, scales = w, 1, None
+        if w.dtype is not _torch.bfloat16:
+            _refuse(where, f"{name} must be bfloat16 or a Rowscale, got {w.dtype}")
+    if data.dim() != 3 or not data.is_cuda:
+        _refuse(where, f"{name} must be a 3-d CUDA tensor (experts x rows x cols)")
+    if device is not None and data.device != device:
+        _refuse(where, f"{name} is on {data.device}, expected {device}")
+    E, R, C = data.shape
+    if R > _MAX_ROWS or C > _MAX_ROWS or E > _MAX_ROWS:
+        _refuse(where, f"{name} has shape {tuple(data.shape)}", "SHAPE")
+    eld, ld, step = data.stride()
+    if step != 1 and C > 1:
+        _refuse(where, f"{name} must have dense rows (stride 1 along them)")
+    if R <= 1:
+        ld = C
+    elif ld < C:
+        _refuse(where, f"{name}'s rows overlap (stride {ld})")
+    return _ExpertMatrices(ty, E, R, C, ld, eld, scales.stride(0) if scales is not None else 0, data.data_ptr(),
+                           scales.data_ptr() if scales is not None else None)
+
+
+def _ints(where: str, name: str, v, n, device):
+    if v.dim() != 1 or (n is not None and v.shape[0] != n):
+        _refuse(where, f"{name} has shape {tuple(v.shape)}, expected {(n,)}", "SHAPE")
+    if v.dtype is not _torch.int32 or v.device != device or (v.shape[0] > 1 and v.stride(0) != 1):
+        _refuse(where, f"{name} must be a dense int32 vector on {device}")
+    return v.data_ptr()
+
+
+def expert_product(w, x, offsets, index=None, fan: int = 1, up=None, dtype=None, y=None, status=None, stream=None):
+    """Products grouped by expert, ragged: y[p] = W_e x[q] for offsets[e] <= p < offsets[e + 1], with q = p, or
+    index[p] // fan (see bitsmoe_expert_product); with `up` SiLU(W_e x) * (U_e x).
+
+    w, up: the experts' matrices (torch bf16, experts x rows x cols, or a Rowscale of such codes); x: rows x cols of the
+    same kind; offsets, index: int32 vectors (`route`'s offsets and pairs, with fan = top_k).  y (P x w's rows, P the
+    length of index, or x's rows; float32 unless `dtype` or y says bfloat16): rows that no expert has are not written.
+    `status`: an optional int32 tensor of one element that receives a device-side timeout.  Rows (and matrices) on
+    16-byte boundaries go through the tensor cores."""
+    torch = _torch or _load_torch()
+    where = "expert_product"
+    coded = isinstance(w, Rowscale)
+    if isinstance(x, Rowscale) != coded or (up is not None and isinstance(up, Rowscale) != coded):
+        _refuse(where, "w, up and x must be of one kind, bf16 or Rowscale")
+    dev = w.device
+    if dev.type != "cuda":
+        _refuse(where, "w must be on a CUDA device")
+    if stream is not None or _current() != dev.index:
+        with _elsewhere(where, dev, stream):
+            return expert_product(w, x, offsets, index, fan, up, dtype, y, status)
+    wc = _matrices(where, "w", w, dev)
+    uc = _matrices(where, "up", up, dev) if up is not None else None
+    if coded:
+        x_ld = _rowscale_rows(where, "x", x, None, wc.cols, dev)
+        x_rows, x_ptr, xs_ptr = x.codes.shape[0], x.codes.data_ptr(), x.scales.data_ptr()
+    else:
+        x_ld = _rows(where, "x", x, None, wc.cols, dev, torch.bfloat16)
+        x_rows, x_ptr, xs_ptr = x.shape[0], x.data_ptr(), None
+    off_ptr = _ints(where, "offsets", offsets, wc.experts + 1, dev)
+    P, idx_ptr = x_rows, None
+    if index is not None:
+        idx_ptr = _ints(where, "index", index, None, dev)
+        P = index.shape[0]
+        if P > _MAX_ROWS:
+            _refuse(where, f"index has {P} entries", "SHAPE")
+    if not 1 <= fan <= _MAX_ROWS:
+        _refuse(where, f"fan is {fan}")
+    st_ptr = None
+    if status is not None:
+        if status.dtype != torch.int32 or status.numel() != 1 or status.device != dev:
+            _refuse(where, "status must be one int32 on the operands' device")
+        st_ptr = status.data_ptr()
+    if y is None:
+        y, y_ld = torch.empty((P, wc.rows), dtype=dtype if dtype is not None else torch.float32, device=dev), max(wc.rows, 1)
+    else:
+        y_ld = _rows(where, "y", y, P, wc.rows, dev)
+    args = _ExpertProductArgs(ctypes.pointer(wc), ctypes.pointer(uc) if uc is not None else None, x_ptr, xs_ptr, x_ld,
+                              x_rows, P, off_ptr, idx_ptr, fan, _dense_type(where, "y", y.dtype), y.data_ptr(), y_ld, st_ptr)
+    _check(_lib().bitsmoe_expert_product(args, _raw_stream(dev.index)), "bitsmoe_expert_product")
+    return y
+
+
+def expert_combine(y, places, weights, base=None, dtype=None, out=None, stream=None):
+    """The weighted sum that ends a layer of experts: out[t] = base[t] + sum_j weights[t][j] y[places[t][j]] (places as
+    `route` gives them: a place outside y's rows adds nothing).  y: rows x D (fp32 or bf16); places int32 and weights
+    fp32, T x top_k; base: T x D of out's type (it may be out itself); out: fp32 unless `dtype`, base or out says bf16."""
+    torch = _torch or _load_torch()
+    where = "expert_combine"
+    dev = y.device
+    y_ld = _rows(where, "y", y)
+    if stream is not None or _current() != dev.index:
+        with _elsewhere(where, dev, stream):
+            return expert_combine(y, places, weights, base, dtype, out)
+    P, D = y.shape
+    if places.dim() != 2 or places.shape != weights.shape:
+        _refuse(where, f"places have shape {tuple(places.shape)}, weights {tuple(weights.shape)}", "SHAPE")
+    if places.dtype is not torch.int32 or weights.dtype is not torch.float32:
+        _refuse(where, "places must be int32, weights float32")
+    if places.device != dev or weights.device != dev or not places.is_contiguous() or not weights.is_contiguous():
+        _refuse(where, f"places and weights must be dense on {dev}")
+    T, k = places.shape
+    if T > _MAX_ROWS:
+        _refuse(where, f"{T} tokens", "SHAPE")
+    if out is None:
+        want = dtype if dtype is not None else base.dtype if base is not None else torch.float32
+        out, out_ld = torch.empty((T, D), dtype=want, device=dev), D
+    else:
+        out_ld = _rows(where, "out", out, T, D, dev)
+    base_ptr, base_ld = None, 0
+    if base is not None:
+        base_ld, base_ptr = _rows(where, "base", base, T, D, dev, out.dtype), base.data_ptr()
+    _check(_lib().bitsmoe_expert_combine(y.data_ptr(), _dense_type(where, "y", y.dtype), y_ld, P, places.data_ptr(),
+                                         weights.data_ptr(), T, k, D, base_ptr, base_ld, out.data_ptr(),
+                                         _dense_type(where, "out", out.dtype), out_ld, _raw_stream(dev.index)),
+           "bitsmoe_expert_combine")
+    return out
 
 
 def bitsmoe_debug_single_token_kernel(which: int) -> None:

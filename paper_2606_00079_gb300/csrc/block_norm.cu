@@ -2,7 +2,7 @@
 //
 //   n  = y rsqrt(mean(y^2) + eps_post) (o + g_post)     (or n = y: no post-norm)
 //   h' = a h + b c[d] gate n                            (gate per token or per element, or its sigmoid)
-//   x  = h' rsqrt(mean(h'^2) + eps_pre) (o + g_pre)     (the next block's input)
+//   x  = h' rsqrt(mean(h'^2) + eps_pre) (o + g_pre)     (the next block's input; in 8 bits: its codes and a scale a row)
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -10,6 +10,7 @@
 #include <cmath>
 
 #include "microscale.cuh"
+#include "rows.cuh"
 
 namespace {
 using namespace bmoe;
@@ -169,6 +170,41 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
   return s;
 }
 
+// The largest of a block's values (bits of magnitudes), as block_sum.
+template <int WARPS = kRowWarps>
+__device__ __forceinline__ uint32_t block_most(uint32_t v, uint32_t* red) {
+  v = __reduce_max_sync(0xFFFFFFFFu, v);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+  __syncthreads();
+  uint32_t m = 0u;
+#pragma unroll
+  for (int q = 0; q < WARPS / 4; ++q) {
+    const uint4 p = reinterpret_cast<const uint4*>(red)[q];
+    m = max(m, max(max(p.x, p.y), max(p.z, p.w)));
+  }
+  return m;
+}
+template <int VEC>
+__device__ __forceinline__ uint32_t most_of(const float (&v)[VEC]) {
+  uint32_t m = 0u;
+#pragma unroll
+  for (int q = 0; q < VEC; ++q) m = max(m, __float_as_uint(v[q]) & 0x7FFFFFFFu);
+  return m;
+}
+// Codes of elements i .. of a row in 8 bits.
+template <int VEC>
+__device__ __forceinline__ void store_codes(void* x, int64_t i, const float (&v)[VEC], float inv, bool bad) {
+  uint8_t* p = static_cast<uint8_t*>(x) + i;
+  if constexpr (VEC == 8) {
+    const uint2 w = make_uint2(e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv), e4m3x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
+    *reinterpret_cast<uint2*>(p) = bad ? make_uint2(0u, 0u) : w;
+  } else if constexpr (VEC == 2) {
+    *reinterpret_cast<uint16_t*>(p) = bad ? (uint16_t)0 : (uint16_t)e4m3x2(v[0] * inv, v[1] * inv);
+  } else {
+    *p = bad ? (uint8_t)0 : (uint8_t)e4m3x2(v[0] * inv, 0.f);
+  }
+}
+
 __device__ __forceinline__ float sigmoid(float v) { return 1.f / (1.f + expf(-v)); }
 
 // What multiplies a normalised output: branch_scale * channel_scale * (offset + post_gain).
@@ -200,15 +236,17 @@ __device__ __forceinline__ void pre_factor(const bitsmoe_block_norm_args& a, con
 }
 
 // One row a group.  Threads at VEC * (k * group + i) hold vector k of a row; k < NV.  Latency counts: the gains are
-// requested with the row where the registers hold them.
-template <int VEC, int NV, bool WARP>
+// requested with the row where the registers hold them.  Q: x in 8 bits, its scale from one more maximum over the group.
+template <int VEC, int NV, bool WARP, bool Q>
 __global__ void __launch_bounds__(WARP ? 128 : kRowThreads, WARP ? 4 : NV * VEC > 8 ? 1 : 2)
-    k_block_norm(const __grid_constant__ bitsmoe_block_norm_args a) {
+    k_block_norm(const __grid_constant__ bitsmoe_block_norm_args a, float* x_scale) {
   __shared__ __align__(16) float red[2][kRowWarps];
+  __shared__ __align__(16) uint32_t redm[kRowWarps];
   const int gsize = WARP ? 32 : blockDim.x, gi = WARP ? (threadIdx.x & 31) : threadIdx.x;
   const int64_t t = WARP ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
   if (t >= a.T) return;   // (whole groups)
   if (!WARP && threadIdx.x < 2 * kRowWarps) red[threadIdx.x / kRowWarps][threadIdx.x % kRowWarps] = 0.f;
+  if (Q && !WARP && threadIdx.x < kRowWarps) redm[threadIdx.x] = 0u;
   const auto sum = [&](float v, int which) { return WARP ? warp_sum(v) : block_sum(v, red[which]); };
   int at[NV];
   bool in[NV];
@@ -293,6 +331,7 @@ __global__ void __launch_bounds__(WARP ? 128 : kRowThreads, WARP ? 4 : NV * VEC 
     if (in[k] && a.h_out) store_vec<VEC>(a.h_out, a.h_type, t * a.h_out_ld + at[k], v[k]);
   if (!a.x) return;
   inv = rsqrtf(sum(ss, 1) * inv_d + a.pre_eps);
+  uint32_t most = 0u;
 #pragma unroll
   for (int k = 0; k < NV; ++k)
     if (in[k]) {
@@ -300,8 +339,16 @@ __global__ void __launch_bounds__(WARP ? 128 : kRowThreads, WARP ? 4 : NV * VEC 
       pre_factor<VEC>(a, pre[k], c);
 #pragma unroll
       for (int q = 0; q < VEC; ++q) v[k][q] = v[k][q] * inv * c[q];
-      store_vec<VEC>(a.x, a.x_type, t * a.x_ld + at[k], v[k]);
+      if constexpr (Q) most = max(most, most_of<VEC>(v[k]));
+      else store_vec<VEC>(a.x, a.x_type, t * a.x_ld + at[k], v[k]);
     }
+  if constexpr (Q) {
+    most = WARP ? __reduce_max_sync(0xFFFFFFFFu, most) : block_most(most, redm);
+    if (gi == 0) x_scale[t] = rowscale_of(most);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (in[k]) store_codes<VEC>(a.x, t * a.x_ld + at[k], v[k], rowscale_inverse(most), rowscale_bad(most));
+  }
 }
 
 __device__ __forceinline__ void copy1(uint8_t* dst, const uint8_t* src, uint32_t size) {   // an element
@@ -319,12 +366,13 @@ __device__ __forceinline__ void copy1(uint8_t* dst, const uint8_t* src, uint32_t
 // memory 737 and 691.
 constexpr int kMaxSlots = 8;
 
-template <int VEC, int NV, int TH, int HT, int YT>   // TH: threads at most
+template <int VEC, int NV, int TH, int HT, int YT, bool Q>   // TH: threads at most; Q: x in 8 bits
 __global__ void __launch_bounds__(TH, VEC * NV * TH <= 8 * kRowThreads ? 2 : 1)
-    k_block_norm_rows(const __grid_constant__ bitsmoe_block_norm_args a, int slots) {
+    k_block_norm_rows(const __grid_constant__ bitsmoe_block_norm_args a, int slots, float* x_scale) {
   extern __shared__ __align__(128) uint8_t ring[];
   constexpr int kW = TH / 32;
   __shared__ __align__(16) float red[2][kW];
+  __shared__ __align__(16) uint32_t redm[kW];   // (read behind a barrier, and written again behind the next row's sum)
   __shared__ uint64_t full[kMaxSlots];
   constexpr uint32_t hs = HT == BITSMOE_F32 ? 4 : 2, ys = YT == BITSMOE_F32 ? 4 : 2;
   const uint32_t es = a.gate_type == BITSMOE_F32 ? 4 : 2;
@@ -335,6 +383,7 @@ __global__ void __launch_bounds__(TH, VEC * NV * TH <= 8 * kRowThreads ? 2 : 1)
   const auto row_at = [](const void* p, int64_t element, uint32_t size) { return static_cast<const uint8_t*>(p) + element * size; };
   const auto off = [](const uint8_t* p) { return VEC == 8 ? 0u : (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15); };
   if (threadIdx.x < 2 * kW) red[threadIdx.x / kW][threadIdx.x % kW] = 0.f;
+  if (Q && threadIdx.x < kW) redm[threadIdx.x] = 0u;
   const auto fill = [&](int slot, int64_t row) {   // by one thread
     uint8_t* dst = ring + (size_t)slot * (yb + hb + eb);
     const uint8_t *py = row_at(a.y, row * a.y_ld, ys), *ph = row_at(a.h, row * a.h_ld, hs), *pe = row_at(a.gate, row * a.gate_ld, es);
@@ -475,7 +524,21 @@ __global__ void __launch_bounds__(TH, VEC * NV * TH <= 8 * kRowThreads ? 2 : 1)
         if (in[k]) store_vec<VEC>(a.x, type, t * a.x_ld + at[k], v[k]);
       });
     };
-    if (a.x) {
+    if constexpr (Q) {
+      uint32_t most = 0u;
+      all([&](int k) {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) v[k][q] = v[k][q] * inv * cp[k][q];
+        if (in[k]) most = max(most, most_of<VEC>(v[k]));
+      });
+      most = block_most<kW>(most, redm);
+      const float to = rowscale_inverse(most);
+      const bool bad = rowscale_bad(most);
+      if (threadIdx.x == 0) x_scale[t] = rowscale_of(most);
+      all([&](int k) {
+        if (in[k]) store_codes<VEC>(a.x, t * a.x_ld + at[k], v[k], to, bad);
+      });
+    } else if (a.x) {
       if (a.x_type == BITSMOE_F32) put(BITSMOE_F32);
       else put(BITSMOE_BF16);
     }
@@ -484,9 +547,10 @@ __global__ void __launch_bounds__(TH, VEC * NV * TH <= 8 * kRowThreads ? 2 : 1)
 
 // Wide rows that registers do not hold: one block per row, h' in shared memory between the two norms.
 constexpr int kWideThreads = 1024;
-__global__ void __launch_bounds__(kWideThreads) k_block_norm_wide(const __grid_constant__ bitsmoe_block_norm_args a) {
+__global__ void __launch_bounds__(kWideThreads) k_block_norm_wide(const __grid_constant__ bitsmoe_block_norm_args a, float* x_scale) {
   extern __shared__ float row[];   // [D]
   __shared__ float red[2][32];
+  __shared__ uint32_t redm[32];
   const auto sum = [&](float v, float* r) {
     v = warp_sum(v);
     if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = v;
@@ -529,9 +593,25 @@ __global__ void __launch_bounds__(kWideThreads) k_block_norm_wide(const __grid_c
   }
   if (!a.x) return;
   inv = rsqrtf(sum(ss, red[1]) / (float)a.D + a.pre_eps);
-  for (int d = threadIdx.x; d < a.D; d += kWideThreads)
-    store1(a.x, a.x_type, t * a.x_ld + d,
-           row[d] * inv * (a.pre_gain ? a.gain_offset + load1(a.pre_gain, a.gain_type, d) : 1.f));
+  const auto x_of = [&](int d) { return row[d] * inv * (a.pre_gain ? a.gain_offset + load1(a.pre_gain, a.gain_type, d) : 1.f); };
+  if (!x_scale) {
+    for (int d = threadIdx.x; d < a.D; d += kWideThreads) store1(a.x, a.x_type, t * a.x_ld + d, x_of(d));
+    return;
+  }
+  uint32_t most = 0u;   // x in 8 bits (a thread reads the elements of row that it wrote)
+  for (int d = threadIdx.x; d < a.D; d += kWideThreads) {
+    row[d] = x_of(d);
+    most = max(most, __float_as_uint(row[d]) & 0x7FFFFFFFu);
+  }
+  most = __reduce_max_sync(0xFFFFFFFFu, most);
+  if ((threadIdx.x & 31) == 0) redm[threadIdx.x >> 5] = most;
+  __syncthreads();
+  most = __reduce_max_sync(0xFFFFFFFFu, redm[threadIdx.x & 31]);
+  if (threadIdx.x == 0) x_scale[t] = rowscale_of(most);
+  for (int d = threadIdx.x; d < a.D; d += kWideThreads) {
+    const float v[1] = {row[d]};
+    store_codes<1>(a.x, t * a.x_ld + d, v, rowscale_inverse(most), rowscale_bad(most));
+  }
 }
 
 // Rows can be read VEC elements at a time: D a multiple of it and every row on a boundary of their size (16 bytes at most).
@@ -539,7 +619,7 @@ bool rows_of(const bitsmoe_block_norm_args& a, int vec) {
   if (a.D % vec) return false;
   const auto ok = [&](const void* p, int type, int64_t ld) {
     if (!p) return true;
-    const int64_t size = type == BITSMOE_F32 ? 4 : 2, align = size * vec < 16 ? size * vec : 16;
+    const int64_t size = type == BITSMOE_F32 ? 4 : type == BITSMOE_BF16 ? 2 : 1, align = size * vec < 16 ? size * vec : 16;
     return reinterpret_cast<uintptr_t>(p) % align == 0 && (a.T == 1 || ld * size % align == 0);
   };
   return ok(a.h, a.h_type, a.h_ld) && ok(a.y, a.y_type, a.y_ld) && ok(a.h_out, a.h_type, a.h_out_ld) && ok(a.x, a.x_type, a.x_ld) &&
@@ -547,8 +627,8 @@ bool rows_of(const bitsmoe_block_norm_args& a, int vec) {
          ok(a.post_gain, a.gain_type, 0) && ok(a.pre_gain, a.gain_type, 0) && ok(a.channel_scale, a.gain_type, 0);
 }
 
-template <int VEC, int NV, int TH>
-cudaError_t launch_rows(const bitsmoe_block_norm_args& a, int dev, int64_t blocks, int per_sm, int threads, cudaStream_t st) {
+template <int VEC, int NV, int TH, bool Q>
+cudaError_t launch_rows(const bitsmoe_block_norm_args& a, float* x_scale, int dev, int64_t blocks, int per_sm, int threads, cudaStream_t st) {
   const bool hf = a.h_type == BITSMOE_F32, yf = a.y_type == BITSMOE_F32;
   const auto room = [&](int type) {
     const size_t bytes = (size_t)a.D * (type == BITSMOE_F32 ? 4 : 2);
@@ -558,27 +638,27 @@ cudaError_t launch_rows(const bitsmoe_block_norm_args& a, int dev, int64_t block
   const int slots = (int)std::min<size_t>(kMaxSlots, (size_t)(220 / per_sm - 2) * 1024 / row);
   if (slots < 1) return cudaErrorInvalidValue;   // (VEC 8: at most 12 x 16384 bytes a row; VEC 1: half of it)
   const auto go = [&](auto kern, cudaError_t e) {
-    if (e == cudaSuccess) kern<<<(unsigned)blocks, threads, slots * row, st>>>(a, slots);
+    if (e == cudaSuccess) kern<<<(unsigned)blocks, threads, slots * row, st>>>(a, slots, x_scale);
     return e;
   };
   constexpr int F = BITSMOE_F32, B = BITSMOE_BF16, kRing = 220 * 1024;
   const cudaError_t e =
-      hf ? (yf ? go(k_block_norm_rows<VEC, NV, TH, F, F>, allow_shared<k_block_norm_rows<VEC, NV, TH, F, F>>(dev, kRing))
-               : go(k_block_norm_rows<VEC, NV, TH, F, B>, allow_shared<k_block_norm_rows<VEC, NV, TH, F, B>>(dev, kRing)))
-         : (yf ? go(k_block_norm_rows<VEC, NV, TH, B, F>, allow_shared<k_block_norm_rows<VEC, NV, TH, B, F>>(dev, kRing))
-               : go(k_block_norm_rows<VEC, NV, TH, B, B>, allow_shared<k_block_norm_rows<VEC, NV, TH, B, B>>(dev, kRing)));
+      hf ? (yf ? go(k_block_norm_rows<VEC, NV, TH, F, F, Q>, allow_shared<k_block_norm_rows<VEC, NV, TH, F, F, Q>>(dev, kRing))
+               : go(k_block_norm_rows<VEC, NV, TH, F, B, Q>, allow_shared<k_block_norm_rows<VEC, NV, TH, F, B, Q>>(dev, kRing)))
+         : (yf ? go(k_block_norm_rows<VEC, NV, TH, B, F, Q>, allow_shared<k_block_norm_rows<VEC, NV, TH, B, F, Q>>(dev, kRing))
+               : go(k_block_norm_rows<VEC, NV, TH, B, B, Q>, allow_shared<k_block_norm_rows<VEC, NV, TH, B, B, Q>>(dev, kRing)));
   return e == cudaSuccess ? cudaGetLastError() : e;
 }
 
 // Rows of up to 256: a warp a row, four rows a block.
-template <int VEC, int NV>
-cudaError_t launch_warps(const bitsmoe_block_norm_args& a, cudaStream_t st) {
-  k_block_norm<VEC, NV, true><<<(unsigned)(((int64_t)a.T + 3) / 4), 128, 0, st>>>(a);
+template <int VEC, int NV, bool Q>
+cudaError_t launch_warps(const bitsmoe_block_norm_args& a, float* x_scale, cudaStream_t st) {
+  k_block_norm<VEC, NV, true, Q><<<(unsigned)(((int64_t)a.T + 3) / 4), 128, 0, st>>>(a, x_scale);
   return cudaGetLastError();
 }
 
-template <int VEC, int NV, int TH = kRowThreads>
-cudaError_t launch_norm(const bitsmoe_block_norm_args& a, cudaStream_t st) {
+template <bool Q, int VEC, int NV, int TH = kRowThreads>
+cudaError_t launch_norm(const bitsmoe_block_norm_args& a, float* x_scale, cudaStream_t st) {
   int dev = 0, sms = 0;
   cudaError_t e = device_sms(&dev, &sms);
   if (e != cudaSuccess) return e;
@@ -588,24 +668,44 @@ cudaError_t launch_norm(const bitsmoe_block_norm_args& a, cudaStream_t st) {
   const int64_t full = (int64_t)sms * per_sm;
   if constexpr (VEC == 8) {
     if (a.T <= full) {
-      k_block_norm<VEC, NV, false><<<(unsigned)a.T, threads, 0, st>>>(a);
+      k_block_norm<VEC, NV, false, Q><<<(unsigned)a.T, threads, 0, st>>>(a, x_scale);
       return cudaGetLastError();
     }
   }
-  return launch_rows<VEC, NV, TH>(a, dev, std::min<int64_t>(a.T, full), per_sm, threads, st);
+  return launch_rows<VEC, NV, TH, Q>(a, x_scale, dev, std::min<int64_t>(a.T, full), per_sm, threads, st);
 }
 
 bool type_ok(int t) { return t == BITSMOE_F32 || t == BITSMOE_BF16; }
 bool misaligned(const void* p, int type) { return reinterpret_cast<uintptr_t>(p) % (type == BITSMOE_F32 ? 4 : 2) != 0; }
 
-}  // namespace
+template <bool Q>
+cudaError_t launch_block_norm(const bitsmoe_block_norm_args& a, float* x_scale, cudaStream_t st) {
+  if (a.D <= 256)
+    return rows_of(a, 8)   ? launch_warps<8, 1, Q>(a, x_scale, st)
+           : rows_of(a, 2) ? launch_warps<2, 4, Q>(a, x_scale, st)
+                           : launch_warps<1, 8, Q>(a, x_scale, st);
+  if (a.D <= 16384 && rows_of(a, 8))
+    return a.D <= 4096   ? launch_norm<Q, 8, 1>(a, x_scale, st)
+           : a.D <= 8192 ? launch_norm<Q, 8, 2>(a, x_scale, st)
+                         : launch_norm<Q, 8, 4>(a, x_scale, st);
+  if (a.D <= 8192) return a.D <= 4096 ? launch_norm<Q, 1, 8>(a, x_scale, st) : launch_norm<Q, 1, 8, 1024>(a, x_scale, st);
+  const size_t smem = (size_t)a.D * 4;
+  if (smem > 40 * 1024) {   // 48 KB with the static part need no opt-in
+    const cudaError_t e = cudaFuncSetAttribute(k_block_norm_wide, cudaFuncAttributeMaxDynamicSharedMemorySize, BITSMOE_BLOCK_NORM_MAX_D * 4);
+    if (e != cudaSuccess) return e;
+  }
+  k_block_norm_wide<<<(unsigned)a.T, kWideThreads, smem, st>>>(a, x_scale);
+  return cudaGetLastError();
+}
 
-extern "C" int bitsmoe_block_norm(const bitsmoe_block_norm_args* args, void* stream) {
+// x_scale NULL and `coded` false: x of a dense type.
+int block_norm(const bitsmoe_block_norm_args* args, bool coded, float* x_scale, void* stream) {
   if (!args) return BITSMOE_ERR_INVALID_ARG;
   const bitsmoe_block_norm_args a = *args;
   if (a.T < 0 || a.D < 1) return BITSMOE_ERR_INVALID_ARG;
   if (a.D > BITSMOE_BLOCK_NORM_MAX_D || a.T > (1 << 24)) return BITSMOE_ERR_SHAPE;
-  if (!type_ok(a.h_type) || !type_ok(a.y_type) || !type_ok(a.gate_type) || !type_ok(a.gain_type) || !type_ok(a.x_type))
+  if (!type_ok(a.h_type) || !type_ok(a.y_type) || !type_ok(a.gate_type) || !type_ok(a.gain_type) ||
+      (coded ? a.x_type != BITSMOE_E4M3 : !type_ok(a.x_type)))
     return BITSMOE_ERR_INVALID_ARG;
   if (a.gate_kind < BITSMOE_GATE_NONE || a.gate_kind > BITSMOE_GATE_ELEMENT) return BITSMOE_ERR_INVALID_ARG;
   if (!(a.post_eps >= 0.f) || !(a.pre_eps >= 0.f) || !std::isfinite(a.residual_scale) || !std::isfinite(a.branch_scale) ||
@@ -613,6 +713,7 @@ extern "C" int bitsmoe_block_norm(const bitsmoe_block_norm_args* args, void* str
     return BITSMOE_ERR_INVALID_ARG;
   if (a.T == 0) return BITSMOE_OK;   // (pointers of empty rows may be null)
   if ((!a.y && (a.post_norm || a.gate_kind || a.channel_scale)) || (a.post_gain && !a.post_norm)) return BITSMOE_ERR_INVALID_ARG;
+  if (coded && (!a.x || !x_scale)) return BITSMOE_ERR_INVALID_ARG;
   if (!a.x && a.pre_gain) return BITSMOE_ERR_INVALID_ARG;
   if (!a.h || (!a.h_out && !a.x) || (a.gate_kind && !a.gate)) return BITSMOE_ERR_INVALID_ARG;
   if (a.h_ld < a.D || (a.y && a.y_ld < a.D) || (a.h_out && a.h_out_ld < a.D) || (a.x && a.x_ld < a.D) ||
@@ -620,24 +721,19 @@ extern "C" int bitsmoe_block_norm(const bitsmoe_block_norm_args* args, void* str
     return BITSMOE_ERR_INVALID_ARG;
   if (misaligned(a.h, a.h_type) || misaligned(a.y, a.y_type) || misaligned(a.gate, a.gate_type) ||
       misaligned(a.post_gain, a.gain_type) || misaligned(a.pre_gain, a.gain_type) ||
-      misaligned(a.channel_scale, a.gain_type) || misaligned(a.h_out, a.h_type) || misaligned(a.x, a.x_type))
+      misaligned(a.channel_scale, a.gain_type) || misaligned(a.h_out, a.h_type) || (coded ? reinterpret_cast<uintptr_t>(x_scale) % 4 != 0 : misaligned(a.x, a.x_type)))
     return BITSMOE_ERR_ALIGNMENT;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = cudaSuccess;
-  if (a.D <= 256) {
-    e = rows_of(a, 8) ? launch_warps<8, 1>(a, st) : rows_of(a, 2) ? launch_warps<2, 4>(a, st) : launch_warps<1, 8>(a, st);
-  } else if (a.D <= 16384 && rows_of(a, 8)) {
-    e = a.D <= 4096 ? launch_norm<8, 1>(a, st) : a.D <= 8192 ? launch_norm<8, 2>(a, st) : launch_norm<8, 4>(a, st);
-  } else if (a.D <= 8192) {
-    e = a.D <= 4096 ? launch_norm<1, 8>(a, st) : launch_norm<1, 8, 1024>(a, st);
-  } else {
-    const size_t smem = (size_t)a.D * 4;
-    if (smem > 40 * 1024)   // 48 KB with the static part need no opt-in
-      e = cudaFuncSetAttribute(k_block_norm_wide, cudaFuncAttributeMaxDynamicSharedMemorySize, BITSMOE_BLOCK_NORM_MAX_D * 4);
-    if (e == cudaSuccess) {
-      k_block_norm_wide<<<(unsigned)a.T, kWideThreads, smem, st>>>(a);
-      e = cudaGetLastError();
-    }
-  }
+  const cudaError_t e = coded ? launch_block_norm<true>(a, x_scale, st) : launch_block_norm<false>(a, nullptr, st);
   return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
+}
+
+}  // namespace
+
+extern "C" int bitsmoe_block_norm(const bitsmoe_block_norm_args* args, void* stream) {
+  return block_norm(args, false, nullptr, stream);
+}
+
+extern "C" int bitsmoe_block_norm_rowscale(const bitsmoe_block_norm_args* args, float* x_scale, void* stream) {
+  return block_norm(args, true, x_scale, stream);
 }

@@ -12,9 +12,10 @@
 // times 6 at most 6), and a quotient v / X rounded to fp32 can only equal such a
 // midpoint when v / X does: the nearest other fp32 v is at least 2^-24 |v| away
 // from midpoint * X, more than the half ulp of a quotient next to the midpoint.
-#include "microscale.cuh"
-
 #include <cuda_runtime.h>
+
+#include "microscale.cuh"
+#include "rows.cuh"
 
 namespace {
 using namespace bmoe;
@@ -61,70 +62,6 @@ __device__ __forceinline__ uint32_t e2m1x2(float hi, float lo) {
   return r;
 }
 
-// Eight elements of a row from column c as they are stored, zeros past the columns.
-template <typename T>
-struct Eight {
-  uint32_t w[sizeof(T) * 2];
-};
-template <typename T, bool VEC>   // VEC: rows on 16-byte boundaries
-__device__ __forceinline__ Eight<T> load8(const MicroArgs& a, int64_t row, int c) {
-  Eight<T> v;
-  const T* p = static_cast<const T*>(a.in) + row * a.ld + c;
-  if (VEC && c + 8 <= a.cols) {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-      const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-      v.w[4 * i] = x.x, v.w[4 * i + 1] = x.y, v.w[4 * i + 2] = x.z, v.w[4 * i + 3] = x.w;
-    }
-    return v;
-  }
-  if constexpr (VEC) {   // the last columns
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) * 2; ++i) v.w[i] = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (c + i < a.cols) {
-        if constexpr (sizeof(T) == 4) v.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
-        else v.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
-      }
-    return v;
-  }
-  // the aligned 16 bytes that hold one of the columns, shifted
-  constexpr int G = sizeof(T) / 2 + 1, W = 2 * sizeof(T);
-  const int n = a.cols - c;   // its columns (8 at most count)
-  uint32_t w[4 * G];
-  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15);
-  const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(p) - off);
-#pragma unroll
-  for (int i = 0; i < G; ++i) {
-    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-    if (16 * i < (int)off + (int)sizeof(T) * min(n, 8) && n > 0) x = __ldg(q + i);
-    w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
-  }
-  if (off & 8)
-#pragma unroll
-    for (int i = 0; i < 4 * G - 2; ++i) w[i] = w[i + 2];
-  if (off & 4)
-#pragma unroll
-    for (int i = 0; i < 4 * G - 1; ++i) w[i] = w[i + 1];
-  if constexpr (sizeof(T) == 2) {
-    if (off & 2)
-#pragma unroll
-      for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-  }
-#pragma unroll
-  for (int i = 0; i < W; ++i) {
-    if constexpr (sizeof(T) == 4) v.w[i] = i < n ? w[i] : 0u;
-    else v.w[i] = 2 * i + 2 <= n ? w[i] : 2 * i + 1 == n ? w[i] & 0xFFFFu : 0u;
-  }
-  return v;
-}
-template <typename T>
-__device__ __forceinline__ float element(const Eight<T>& v, int i) {
-  if constexpr (sizeof(T) == 4) return __uint_as_float(v.w[i]);
-  else return i & 1 ? bf16hi(v.w[i / 2]) : bf16lo(v.w[i / 2]);
-}
-
 // A warp takes 256 columns of kRowsOfWarp rows 32 apart (r, r + 32, .. of a scale tile: the words of all four are 16 bytes in a
 // row), their loads in flight together; a lane 8 columns, LPB lanes a block, LPT lanes the four blocks of a scale word.
 // Neighbouring chunks of a row in neighbouring warps.  Rows and blocks past the matrix's own up to whole scale tiles are
@@ -154,7 +91,7 @@ __global__ void __launch_bounds__(kMThreads) k_micro_quantize(MicroArgs a) {
 #pragma unroll
   for (int j = 0; j < R; ++j) {
     if (r0 + 32 * j < a.rows) {
-      in[j] = load8<T, VEC>(a, r0 + 32 * j, c);
+      in[j] = load8<T, VEC>(a.in, a.ld, a.cols, r0 + 32 * j, c);
     } else {
 #pragma unroll
       for (int i = 0; i < (int)sizeof(T) * 2; ++i) in[j].w[i] = 0u;

@@ -1,0 +1,348 @@
+// Routing as lists of its own, and the weighted sum that ends a layer of experts.
+//
+//   experts[t] = the top_k largest logits of a token (ties to the lower expert; NaN and -inf never)
+//   weights[t] = exp(l - l_max) / sum over the selected, or over all, of exp(l - l_max)
+//   pairs      = the pairs t * top_k + j sorted by (expert, number), offsets where each expert's begin,
+//                places the inverse
+//   out[t]     = base[t] + sum_j weights[t][j] y[places[t][j]]
+//
+// The sort is by counting, and no result depends on the order of atomics: 32 tokens at a time set their bits in a word
+// for each expert (a token picks an expert once), and a pair's rank in its expert is the count of the bits below its
+// token's, plus those of the words before.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "microscale.cuh"
+
+namespace {
+using namespace bmoe;
+
+constexpr int kMaxExperts = 1024, kMaxTopK = 32;
+constexpr int kRouteThreads = 1024, kRouteWarps = kRouteThreads / 32;   // 32 tokens at a time, a warp each
+constexpr int kAloneTokens = 64;                                        // one block does all of at most so many
+
+struct RouteArgs {
+  const float* logits;
+  int64_t ld;
+  int T, E, k, renormalize;
+  int per;               // tokens of a block (a multiple of 32)
+  int32_t* experts;
+  float* weights;
+  int32_t* offsets;
+  int32_t* pairs;
+  int32_t* places;
+  int32_t* counts;       // [blocks][E]
+};
+
+__device__ __forceinline__ float logit_of(uint32_t key) {   // order_key's inverse
+  return __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
+}
+
+// One token's selection by a warp: lane j < k gets the j-th expert (-1: none) and its weight.  NE: logits a lane holds.
+template <int NE>
+__device__ __forceinline__ void select_token(const RouteArgs& a, int64_t t, int lane, int& expert, float& weight) {
+  constexpr uint32_t kNone = 0x007FFFFFu;   // -infinity's key, above NaN's
+  uint32_t key[NE];
+  const float* row = a.logits + t * a.ld;
+#pragma unroll
+  for (int i = 0; i < NE; ++i) {
+    const int e = lane + 32 * i;
+    key[i] = e < a.E ? order_key(__ldg(row + e)) : 0u;
+    if (key[i] <= kNone) key[i] = 0u;
+  }
+  expert = -1;
+  weight = 0.f;
+  float top = 0.f, sum = 0.f;
+  for (int j = 0; j < a.k; ++j) {
+    uint32_t m = key[0];
+#pragma unroll
+    for (int i = 1; i < NE; ++i) m = max(m, key[i]);
+    const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, m);
+    if (best == 0u) break;
+    uint32_t at = 0xFFFFFFFFu;
+#pragma unroll
+    for (int i = NE - 1; i >= 0; --i)
+      if (key[i] == best) at = lane + 32 * i;
+    at = __reduce_min_sync(0xFFFFFFFFu, at);
+    const float v = logit_of(best);
+    if (j == 0) {
+      top = v;
+      if (!a.renormalize) {
+#pragma unroll
+        for (int i = 0; i < NE; ++i)
+          if (key[i]) sum += expf(logit_of(key[i]) - top);
+        sum = warp_sum(sum);
+      }
+    }
+    if (lane == j) {
+      expert = (int)at;
+      weight = expf(v - top);
+    }
+#pragma unroll
+    for (int i = 0; i < NE; ++i)
+      if ((int)at == lane + 32 * i) key[i] = 0u;
+  }
+  if (a.renormalize) sum = warp_sum(weight);
+  if (expert >= 0) weight /= sum;
+}
+
+// Exclusive sums of v[0 .. n) in place (n <= 1024, one block of 1024 threads); the whole sum is returned.
+__device__ __forceinline__ int block_scan(int* v, int n, int* part) {
+  const int i = threadIdx.x, lane = i & 31;
+  const int x = i < n ? v[i] : 0;
+  int s = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xFFFFFFFFu, s, o);
+    if (lane >= o) s += y;
+  }
+  if (lane == 31) part[i >> 5] = s;
+  __syncthreads();
+  if (i < 32) {
+    const int q = part[i];
+    int p = q;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xFFFFFFFFu, p, o);
+      if (lane >= o) p += y;
+    }
+    part[i] = p - q;
+    if (i == 31) part[32] = p;
+  }
+  __syncthreads();
+  if (i < n) v[i] = part[i >> 5] + s - x;
+  return part[32];
+}
+
+// Tokens [first, last) of a block, 32 at a time: selection, and each pair's rank among the block's pairs of its expert
+// (into places, for now).  count[e]: the block's pairs of expert e.
+template <int NE>
+__device__ __forceinline__ void select_block(const RouteArgs& a, int first, int last, uint32_t* mask, int* count) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
+    mask[e] = 0u;
+    count[e] = 0;
+  }
+  __syncthreads();
+  for (int t0 = first; t0 < last; t0 += kRouteWarps) {
+    const int t = t0 + w;
+    int expert = -1;
+    float weight = 0.f;
+    if (t < last) {
+      select_token<NE>(a, t, lane, expert, weight);
+      if (expert >= 0) atomicOr(mask + expert, 1u << w);
+    }
+    __syncthreads();
+    if (t < last && lane < a.k) {
+      const int64_t p = (int64_t)t * a.k + lane;
+      a.experts[p] = expert;
+      a.weights[p] = weight;
+      a.places[p] = expert < 0 ? -1 : count[expert] + __popc(mask[expert] & ((1u << w) - 1u));
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
+      count[e] += __popc(mask[e]);
+      mask[e] = 0u;
+    }
+    __syncthreads();
+  }
+}
+
+// Places and pairs of a block's tokens once base[e] is where its first pair of expert e goes.
+__device__ __forceinline__ void place_block(const RouteArgs& a, int first, int last, const int* base) {
+  for (int64_t p = (int64_t)first * a.k + threadIdx.x; p < (int64_t)last * a.k; p += kRouteThreads) {
+    const int e = a.experts[p];
+    if (e < 0) continue;
+    const int at = base[e] + a.places[p];
+    a.places[p] = at;
+    a.pairs[at] = (int)p;
+  }
+}
+
+template <int NE>
+__global__ void __launch_bounds__(kRouteThreads) k_route_alone(const __grid_constant__ RouteArgs a) {
+  __shared__ uint32_t mask[kMaxExperts];
+  __shared__ int count[kMaxExperts];
+  __shared__ int part[33];
+  select_block<NE>(a, 0, a.T, mask, count);
+  const int total = block_scan(count, a.E, part);
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) a.offsets[e] = count[e];
+  if (threadIdx.x == 0) a.offsets[a.E] = total;
+  for (int p = total + threadIdx.x; p < a.T * a.k; p += kRouteThreads) a.pairs[p] = -1;
+  place_block(a, 0, a.T, count);
+}
+
+template <int NE>
+__global__ void __launch_bounds__(kRouteThreads) k_route_select(const __grid_constant__ RouteArgs a) {
+  __shared__ uint32_t mask[kMaxExperts];
+  __shared__ int count[kMaxExperts];
+  const int first = blockIdx.x * a.per;
+  select_block<NE>(a, first, min(first + a.per, a.T), mask, count);
+  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) a.counts[(int64_t)blockIdx.x * a.E + e] = count[e];
+}
+
+// Every block sums the counts itself: of the blocks before it, and of all.
+__global__ void __launch_bounds__(kRouteThreads) k_route_place(const __grid_constant__ RouteArgs a) {
+  __shared__ int base[kMaxExperts], start[kMaxExperts];
+  __shared__ int part[33];
+  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) base[e] = start[e] = 0;
+  __syncthreads();
+  // threads take (expert, slice of the blocks)
+  const int ex = (a.E + 31) / 32 * 32, slices = max(1, kRouteThreads / ex);
+  const int slice = threadIdx.x / ex, e0 = threadIdx.x % ex;
+  if (slice < slices && e0 < a.E) {
+    int before = 0, all = 0;
+#pragma unroll 4
+    for (int b = slice; b < (int)gridDim.x; b += slices) {
+      const int c = __ldg(a.counts + (int64_t)b * a.E + e0);
+      all += c;
+      before += b < (int)blockIdx.x ? c : 0;
+    }
+    atomicAdd(base + e0, before);
+    atomicAdd(start + e0, all);
+  }
+  __syncthreads();
+  const int total = block_scan(start, a.E, part);
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
+    base[e] += start[e];
+    if (blockIdx.x == 0) a.offsets[e] = start[e];
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.offsets[a.E] = total;
+  for (int64_t p = total + (int64_t)blockIdx.x * kRouteThreads + threadIdx.x; p < (int64_t)a.T * a.k; p += (int64_t)gridDim.x * kRouteThreads)
+    a.pairs[p] = -1;
+  __syncthreads();
+  const int first = blockIdx.x * a.per;
+  place_block(a, first, min(first + a.per, a.T), base);
+}
+
+__global__ void k_route_none(int32_t* offsets, int E) {
+  for (int e = threadIdx.x; e <= E; e += blockDim.x) offsets[e] = 0;
+}
+
+template <int NE>
+cudaError_t launch_route(const RouteArgs& a, int blocks, cudaStream_t st) {
+  if (blocks == 1) {
+    k_route_alone<NE><<<1, kRouteThreads, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+  k_route_select<NE><<<blocks, kRouteThreads, 0, st>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  k_route_place<<<blocks, kRouteThreads, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+// Tokens of a block, and blocks of a call: each block of the second launch reads blocks x E counts.
+int route_per(int T, int E) {
+  const int most = std::min(152, std::max(16, 65536 / E));
+  return T <= kAloneTokens ? T : ((T + most - 1) / most + kRouteWarps - 1) / kRouteWarps * kRouteWarps;
+}
+int route_blocks(int T, int E) { return T <= kAloneTokens ? 1 : (T + route_per(T, E) - 1) / route_per(T, E); }
+bool route_sizes_ok(int T, int E, int k) {
+  return T >= 0 && E >= 1 && E <= kMaxExperts && k >= 1 && k <= std::min(E, kMaxTopK) && (int64_t)T * k <= (1 << 24);
+}
+
+// ---------------------------------------------------------------------------
+struct CombineArgs {
+  const void* y;
+  int64_t y_ld;
+  int P, k, D;
+  const int32_t* places;
+  const float* weights;
+  const void* base;
+  int64_t base_ld;
+  void* out;
+  int64_t out_ld;
+};
+
+template <typename T>
+__device__ __forceinline__ float value(const T* p) {
+  if constexpr (sizeof(T) == 4) return *p;
+  else return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
+}
+template <typename T>
+__device__ __forceinline__ void keep(T* p, float v) {
+  if constexpr (sizeof(T) == 4) *p = v;
+  else *p = __float2bfloat16_rn(v);
+}
+
+// An element a thread.
+template <typename TY, typename TO>
+__global__ void __launch_bounds__(256) k_combine_plain(const __grid_constant__ CombineArgs a) {
+  const int64_t t = blockIdx.x;
+  for (int d = blockIdx.y * 256 + threadIdx.x; d < a.D; d += gridDim.y * 256) {
+    float s = 0.f;
+    for (int j = 0; j < a.k; ++j) {
+      const int p = __ldg(a.places + t * a.k + j);
+      if ((unsigned)p < (unsigned)a.P) s = fmaf(__ldg(a.weights + t * a.k + j), value(static_cast<const TY*>(a.y) + (int64_t)p * a.y_ld + d), s);
+    }
+    if (a.base) s = value(static_cast<const TO*>(a.base) + t * a.base_ld + d) + s;
+    keep(static_cast<TO*>(a.out) + t * a.out_ld + d, s);
+  }
+}
+
+}  // namespace
+
+extern "C" size_t bitsmoe_route_workspace_bytes(int T, int E, int top_k) {
+  if (!route_sizes_ok(T, E, top_k) || route_blocks(T, E) == 1) return 0;
+  return (size_t)route_blocks(T, E) * E * 4;
+}
+
+extern "C" int bitsmoe_route(const float* logits, int64_t ld, int T, int E, int top_k, int renormalize, int32_t* experts,
+                             float* weights, int32_t* offsets, int32_t* pairs, int32_t* places, void* ws, size_t ws_bytes,
+                             void* stream) {
+  if (T < 0 || E < 1 || top_k < 1 || top_k > std::min(E, kMaxTopK) || ld < E) return BITSMOE_ERR_INVALID_ARG;
+  if (!route_sizes_ok(T, E, top_k)) return BITSMOE_ERR_SHAPE;
+  if (!offsets || (T > 0 && (!logits || !experts || !weights || !pairs || !places))) return BITSMOE_ERR_INVALID_ARG;
+  const auto odd = [](const void* p, int to) { return reinterpret_cast<uintptr_t>(p) % to != 0; };
+  if (odd(logits, 4) || odd(experts, 4) || odd(weights, 4) || odd(offsets, 4) || odd(pairs, 4) || odd(places, 4) || odd(ws, 16))
+    return BITSMOE_ERR_ALIGNMENT;
+  const size_t need = bitsmoe_route_workspace_bytes(T, E, top_k);
+  if (ws_bytes < need || (need && !ws)) return BITSMOE_ERR_WORKSPACE_TOO_SMALL;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (T == 0) {
+    k_route_none<<<1, 256, 0, st>>>(offsets, E);
+    e = cudaGetLastError();
+  } else {
+    const int blocks = route_blocks(T, E);
+    const RouteArgs a{logits, ld, T, E, top_k, renormalize, route_per(T, E), experts, weights, offsets, pairs, places, static_cast<int32_t*>(ws)};
+    e = E <= 32    ? launch_route<1>(a, blocks, st)
+        : E <= 64  ? launch_route<2>(a, blocks, st)
+        : E <= 128 ? launch_route<4>(a, blocks, st)
+        : E <= 256 ? launch_route<8>(a, blocks, st)
+        : E <= 512 ? launch_route<16>(a, blocks, st)
+                   : launch_route<32>(a, blocks, st);
+  }
+  return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
+}
+
+extern "C" int bitsmoe_expert_combine(const void* y, int y_type, int64_t y_ld, int P, const int32_t* places, const float* weights,
+                                      int T, int top_k, int D, const void* base, int64_t base_ld, void* out, int out_type,
+                                      int64_t out_ld, void* stream) {
+  if (T < 0 || P < 0 || top_k < 1 || top_k > kMaxTopK || D < 1 || !dense_type_ok(y_type) || !dense_type_ok(out_type))
+    return BITSMOE_ERR_INVALID_ARG;
+  if (T > kMaxMicroRows || P > kMaxMicroRows || D > kMaxMicroCols) return BITSMOE_ERR_SHAPE;
+  if (y_ld < D || out_ld < D || (base && base_ld < D)) return BITSMOE_ERR_INVALID_ARG;
+  if (T == 0) return BITSMOE_OK;
+  if ((!y && P > 0) || !places || !weights || !out) return BITSMOE_ERR_INVALID_ARG;
+  if (base == out && base_ld != out_ld && T > 1) return BITSMOE_ERR_INVALID_ARG;
+  const auto odd = [](const void* p, int to) { return reinterpret_cast<uintptr_t>(p) % to != 0; };
+  if (odd(y, dense_size(y_type)) || odd(out, dense_size(out_type)) || odd(base, dense_size(out_type)) || odd(places, 4) || odd(weights, 4))
+    return BITSMOE_ERR_ALIGNMENT;
+  CombineArgs a{y, y_ld, P, top_k, D, places, weights, base, base_ld, out, out_ld};
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const dim3 grid((unsigned)T, (unsigned)std::min(64, (D + 255) / 256));
+  const bool yf = y_type == BITSMOE_F32, of = out_type == BITSMOE_F32;
+  if (yf && of) k_combine_plain<float, float><<<grid, 256, 0, st>>>(a);
+  else if (yf) k_combine_plain<float, __nv_bfloat16><<<grid, 256, 0, st>>>(a);
+  else if (of) k_combine_plain<__nv_bfloat16, float><<<grid, 256, 0, st>>>(a);
+  else k_combine_plain<__nv_bfloat16, __nv_bfloat16><<<grid, 256, 0, st>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
+}

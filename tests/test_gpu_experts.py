@@ -1,0 +1,470 @@
+"""GPU checks of the routing, the products grouped by expert and their weighted sum against float64.
+
+Tolerances, by arithmetic (u = 2^-24).  A sum of K exact products in fp32, in any order and with the tensor core's
+truncating additions (an addition loses less than 2^-23 of the largest operand, and every partial sum is at most the sum M of
+the products' magnitudes): (K + 8) 2^-23 M; its scales add 2 u each of the sum.  SiLU(g) u: |SiLU'| <= 1.1, expf and
+the division at most 8 u (and |g| u through the exponent's argument).  A bf16 result adds half a step, 2^-8 relative.
+Softmax weights: the exponent's argument is off by u |l - l_max|, expf by 2 units in the last place, the sum of n by n u,
+the division by u."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import experts as oe
+
+pytestmark = pytest.mark.gpu
+u = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def env():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import __graft_entry__
+    __graft_entry__.build()
+    import paper_2606_00079_gb300 as bm
+    torch.cuda.set_device(0)
+    return torch, bm
+
+
+# ---------------------------------------------------------------------------
+# routing
+# ---------------------------------------------------------------------------
+def logits_of(rng, T, E):
+    v = rng.standard_normal((T, E)) * 2
+    v = np.where(rng.random((T, 1)) < 0.5, np.round(v * 2) / 2, v).astype(np.float32)   # many ties in half of the rows
+    kinds = rng.integers(0, 12, T)
+    v[kinds == 0] = -np.inf
+    v[kinds == 1] = np.nan
+    v[kinds == 2, E // 2:] = -np.inf
+    v[kinds == 3, :E // 3] = np.nan
+    v[kinds == 4] *= 0.0    # signed zeros
+    v[kinds == 5] = 1e30 * v[kinds == 5]
+    return v
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 128, 8), (3, 7, 7), (31, 33, 4), (32, 64, 8), (64, 128, 8), (65, 128, 8),
+                                   (70, 1024, 32), (200, 300, 5), (1000, 2, 2), (4999, 61, 6), (6000, 1000, 3), (20000, 16, 4)])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_route(env, T, E, k, renorm):
+    torch, bm = env
+    v = logits_of(np.random.default_rng([T, E, k]), T, E)
+    wide = torch.full((T, E + 3), 99.0, device="cuda")
+    wide[:, 1:1 + E] = torch.from_numpy(v).cuda()
+    r = bm.route(wide[:, 1:1 + E], k, renormalize=renorm)
+    experts, weights, offsets, pairs, places = oe.route(v, k, renorm)
+    for name, want in (("experts", experts), ("offsets", offsets), ("pairs", pairs), ("places", places)):
+        np.testing.assert_array_equal(getattr(r, name).cpu().numpy(), want, err_msg=name)
+    got = r.weights.double().cpu().numpy()
+    none = experts < 0
+    assert (got[none] == 0).all()
+    with np.errstate(invalid="ignore", divide="ignore"):
+        span = np.where(weights > 0, np.abs(np.log(weights / np.maximum(weights.max(1, keepdims=True), 1e-300))), 0)
+        # (over all: the largest argument that counts is below 104, where expf underflows)
+        tol = (2 * np.maximum(span, 0 if renorm else 104) + (k if renorm else E) + 16) * u * weights + 1e-40
+    assert (np.abs(got - weights) <= tol).all()
+    again = bm.route(torch.from_numpy(v).cuda(), k, renormalize=renorm)
+    for a, b in zip(r, again):
+        assert torch.equal(a, b)
+
+
+def test_route_no_tokens_infinity_and_refusals(env):
+    torch, bm = env
+    r = bm.route(torch.empty(0, 16, device="cuda"), 4)
+    assert r.offsets.tolist() == [0] * 17 and r.pairs.numel() == 0 and r.experts.shape == (0, 4)
+    r = bm.route(torch.tensor([[0.0, float("inf"), 1.0]], device="cuda"), 2)
+    assert r.experts.tolist() == [[1, 2]] and torch.isnan(r.weights).all()
+    for bad in (0, 17, 33):
+        with pytest.raises(bm.BitsMoEError):
+            bm.route(torch.zeros(4, 16, device="cuda"), bad)
+    with pytest.raises(bm.BitsMoEError):
+        bm.route(torch.zeros(4, 16, device="cuda", dtype=torch.bfloat16), 2)
+
+
+def test_route_in_two_graphs_and_on_a_stream(env):
+    torch, bm = env
+    rng = np.random.default_rng(5)
+    data = [torch.from_numpy(logits_of(rng, 500, 64)).cuda() for _ in range(3)]
+    buf = [torch.zeros(500, 64, device="cuda") for _ in range(2)]
+    graphs, outs = [], []
+    for b in buf:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(bm.route(b, 6))
+        graphs.append(g)
+    for i in range(2):
+        buf[0].copy_(data[i])
+        buf[1].copy_(data[i + 1])
+        graphs[1].replay()
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        for o, d in zip(outs, (data[i], data[i + 1])):
+            for a, b in zip(o, bm.route(d, 6)):
+                assert torch.equal(a, b)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    r = bm.route(data[0], 6, stream=st)
+    st.synchronize()
+    for a, b in zip(r, bm.route(data[0], 6)):
+        assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------------------
+# products
+# ---------------------------------------------------------------------------
+def pitched(torch, x, ty, shift=0):
+    """bf16 rows, or codes with odd scales, on 16-byte boundaries (shift 0) or off them; and their float64 values."""
+    n = 8 if ty == "bf16" else 16
+    if ty == "bf16":
+        t, scale = x.to(torch.bfloat16), None
+        vals = t.double()
+    else:
+        scale = x.abs().amax(-1) / 300 + 1e-3
+        t = (x / scale[..., None]).to(torch.float8_e4m3fn)
+        vals = t.double() * scale.double()[..., None]
+    C = x.shape[-1]
+    pitch = (C + n - 1) // n * n if not shift else C + 1 + (C % 2)
+    flat = torch.zeros(*x.shape[:-1], pitch + (2 if shift else 0), dtype=torch.float32).to(t.dtype).cuda()[..., shift:shift + C]
+    (flat.view(torch.uint8) if ty == "e4m3" else flat).copy_((t.view(torch.uint8) if ty == "e4m3" else t).cuda())
+    return flat, scale.cuda() if scale is not None else None, vals.numpy()
+
+
+def wrap(bm, t, s):
+    return t if s is None else bm.Rowscale(t, s)
+
+
+def run_product(env, counts, R, C, ty="bf16", glu=False, fan=0, out="bf16", shift=0, lead=0, tail=0, seed=0, tokens=None):
+    """counts: rows of each expert; fan: 0 (rows in order) or the index's divisor."""
+    torch, bm = env
+    E = len(counts)
+    off = lead + np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    P = int(off[-1]) + tail
+    g = torch.Generator().manual_seed(1000 * seed + 7 * R + C + P)
+    w, ws, wv = pitched(torch, torch.randn(E, R, C, generator=g) * (0.5 + torch.rand(E, R, 1, generator=g)) / C ** 0.5, ty, shift)
+    up, us, uv = pitched(torch, torch.randn(E, R, C, generator=g) / C ** 0.5, ty, shift) if glu else (None, None, None)
+    rows = P if not fan else tokens or max(1, P // fan)
+    x, xs, xv = pitched(torch, torch.randn(rows, C, generator=g) * 3, ty, shift)
+    idx = torch.randint(0, rows * fan, (P,), generator=g, dtype=torch.int32) if fan else None
+    dt = torch.float32 if out == "f32" else torch.bfloat16
+    ybuf = torch.full((P, R + 3), 77.0, dtype=dt, device="cuda")
+    y = ybuf[:, 1:1 + R]
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), torch.from_numpy(off).cuda(), index=idx.cuda() if fan else None,
+                            fan=max(fan, 1), up=wrap(bm, up, us) if glu else None, y=y, status=status)
+    assert got is y
+    ybuf = ybuf.double().cpu().numpy()
+    assert int(status.item()) == 0
+    assert (ybuf[:, 0] == 77).all() and (ybuf[:, 1 + R:] == 77).all()
+    # float64, expert by expert
+    q = idx.numpy() // fan if fan else np.arange(P)
+    for e in range(E):
+        a, b = off[e], off[e + 1]
+        if a == b:
+            continue
+        xr = xv[q[a:b]]
+        gs, gm = xr @ wv[e].T, np.abs(xr) @ np.abs(wv[e]).T
+        eg = (C + 8) * 2.0 ** -23 * gm + 8 * u * np.abs(gs)
+        if glu:
+            us_, um = xr @ uv[e].T, np.abs(xr) @ np.abs(uv[e]).T
+            eu = (C + 8) * 2.0 ** -23 * um + 8 * u * np.abs(us_)
+            silu = gs / (1 + np.exp(-gs))
+            want = silu * us_
+            tol = 1.1 * eg * (np.abs(us_) + eu) + np.abs(silu) * eu + (16 + np.abs(gs)) * u * np.abs(want)
+        else:
+            want, tol = gs, eg
+        tol = tol + (2.0 ** -8 * (np.abs(want) + tol) if out == "bf16" else 2 * u * np.abs(want)) + 1e-37
+        d = np.abs(ybuf[a:b, 1:1 + R] - want)
+        assert (d <= tol).all(), (e, np.argwhere(~(d <= tol))[:4].tolist(), float(np.nanmax(d / tol)))
+    assert (ybuf[:off[0]] == 77).all() and (ybuf[off[-1]:] == 77).all()
+
+
+def ragged(rng, E, most, empty=0.3):
+    c = rng.integers(0, most + 1, E)
+    c[rng.random(E) < empty] = 0
+    return c
+
+
+PRODUCTS = [
+    # counts of each expert, rows, cols
+    ([1], 1, 1), ([1], 64, 64), ([3], 17, 40), ([0, 5, 0, 1], 100, 72), ([0, 0, 0], 64, 64), ([16, 17, 15, 1], 128, 128),
+    ([33, 0, 2], 200, 264), ([1, 1, 1, 1, 1, 1, 1, 1], 96, 512), ([255, 256, 257], 130, 136), ([513, 1, 70], 64, 200),
+    ([40, 3], 1001, 2041), ([700], 65, 33),
+]
+
+
+@pytest.mark.parametrize("case", range(len(PRODUCTS)))
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("fan", [0, 1, 3])
+def test_expert_product(env, case, ty, glu, fan):
+    counts, R, C = PRODUCTS[case]
+    run_product(env, counts, R, C, ty, glu, fan, out="f32" if case % 2 else "bf16", lead=case % 3, tail=2 * (case % 2), seed=case)
+
+
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("fan", [0, 2])
+def test_expert_product_off_the_boundaries(env, ty, glu, fan):
+    run_product(env, [5, 0, 70, 1], 67, 129, ty, glu, fan, out="f32", shift=1, lead=1, tail=1)
+
+
+@pytest.mark.parametrize("E,most,R,C,ty,glu", [(128, 6, 96, 256, "bf16", True), (300, 3, 40, 128, "e4m3", False), (1024, 2, 16, 64, "bf16", False),
+                                               (60, 40, 320, 512, "e4m3", True), (7, 400, 384, 256, "bf16", True), (5, 600, 520, 384, "e4m3", False)])
+def test_expert_product_many_experts_and_tiles(env, E, most, R, C, ty, glu):
+    rng = np.random.default_rng([E, most])
+    run_product(env, ragged(rng, E, most), R, C, ty, glu, fan=4, out="f32", lead=3, tail=5)
+    run_product(env, ragged(rng, E, most), R, C, ty, glu, fan=0, out="bf16")
+
+
+def test_expert_product_deep(env):
+    run_product(env, [9, 40], 64, 14336, "bf16", False, 0, "f32")
+    run_product(env, [9, 40], 64, 14336, "e4m3", True, 2, "bf16")
+
+
+def test_expert_product_strided_and_shared_matrices(env):
+    """Gate and up as halves of one tensor, an expert's pitch that is not rows * pitch, one matrix for all experts."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(3)
+    both = torch.randn(4, 96, 128, generator=g).to(torch.bfloat16).cuda()
+    x = torch.randn(20, 128, generator=g).to(torch.bfloat16).cuda()
+    off = torch.tensor([0, 4, 4, 15, 20], dtype=torch.int32).cuda()
+    a = bm.expert_product(both[:, :48], x, off, up=both[:, 48:])
+    b = bm.expert_product(both[:, :48].contiguous(), x, off, up=both[:, 48:].contiguous())
+    assert torch.equal(a, b)
+    a = bm.expert_product(both[::2, :48], x, off[:3])
+    b = bm.expert_product(both[::2, :48].contiguous(), x, off[:3])
+    assert torch.equal(a[:4], b[:4])
+    one = both[:1].expand(4, 96, 128)
+    a = bm.expert_product(one, x, off)
+    b = bm.expert_product(both[:1], x, torch.tensor([0, 20], dtype=torch.int32).cuda())
+    # (the sums' order may depend on a tile's size)
+    tol = (128 + 8) * 2.0 ** -22 * (x.double().abs() @ both[0].double().abs().T)
+    assert ((a.double() - b.double()).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_expert_product_rows_that_are_not_there(env, ty, shift):
+    """Indices that are no row of x give NaN rows and nothing else; offsets outside 0 .. P are held there."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(4)
+    w, ws, _ = pitched(torch, torch.randn(3, 80, 96, generator=g), ty, shift)
+    x, xs, _ = pitched(torch, torch.randn(10, 96, generator=g), ty, shift)
+    w, x = wrap(bm, w, ws), wrap(bm, x, xs)
+    idx = torch.randint(0, 20, (40,), generator=g, dtype=torch.int32)
+    bad = idx.clone()
+    for p, v in ((0, -1), (5, 20), (17, 2 ** 31 - 1), (18, -2 ** 31), (39, 21)):
+        bad[p] = v
+    off = torch.tensor([0, 18, 18, 40], dtype=torch.int32).cuda()
+    good = bm.expert_product(w, x, off, index=idx.cuda(), fan=2)
+    y = bm.expert_product(w, x, off, index=bad.cuda(), fan=2)
+    lost = torch.tensor([0, 5, 17, 18, 39])
+    keep = torch.ones(40, dtype=torch.bool)
+    keep[lost] = False
+    assert torch.isnan(y[lost.cuda()]).all() and torch.equal(y[keep.cuda()], good[keep.cuda()])
+    y = torch.zeros(40, 80, device="cuda")
+    bm.expert_product(w, x, torch.tensor([-5, 18, 18, 4000], dtype=torch.int32).cuda(), index=idx.cuda(), fan=2, y=y)
+    assert torch.equal(y, good)
+    y.zero_()
+    bm.expert_product(w, x, torch.tensor([30, 18, 50, 18], dtype=torch.int32).cuda(), index=idx.cuda(), fan=2, y=y)
+    assert (y[:18] == 0).all()
+    # rows in order: past x's last row
+    y = bm.expert_product(w, x, torch.tensor([0, 4, 4, 10], dtype=torch.int32).cuda())
+    assert torch.isfinite(y).all()
+
+
+def test_expert_product_nothing_to_do(env):
+    torch, bm = env
+    w = torch.randn(2, 8, 16, device="cuda").to(torch.bfloat16)
+    x = torch.randn(4, 16, device="cuda").to(torch.bfloat16)
+    off = torch.zeros(3, dtype=torch.int32, device="cuda")
+    y = torch.full((4, 8), 5.0, device="cuda")
+    assert (bm.expert_product(w, x, off, y=y) == 5).all()
+    assert bm.expert_product(w, x[:0], off).shape == (0, 8)
+    assert bm.expert_product(w[:, :0], x, off).shape == (4, 0)
+    # no rows of x at all, all of them asked for
+    y = bm.expert_product(w, x[:0], torch.tensor([0, 2, 3], dtype=torch.int32).cuda(), index=torch.zeros(3, dtype=torch.int32).cuda())
+    assert torch.isnan(y).all()
+
+
+def test_expert_product_not_finite_stays_in_its_row(env):
+    torch, bm = env
+    w = torch.randn(2, 64, 128, device="cuda").to(torch.bfloat16)
+    x = torch.randn(40, 128, device="cuda").to(torch.bfloat16)
+    off = torch.tensor([0, 17, 40], dtype=torch.int32).cuda()
+    good = bm.expert_product(w, x, off)
+    x[16, 3], x[17, 9] = float("nan"), float("inf")
+    y = bm.expert_product(w, x, off)
+    keep = torch.ones(40, dtype=torch.bool, device="cuda")
+    keep[16:18] = False
+    assert torch.equal(y[keep], good[keep]) and torch.isnan(y[16]).all() and not torch.isfinite(y[17]).any()
+    w[0, 5, 7] = float("nan")
+    y = bm.expert_product(w, x, off)
+    rows = torch.ones(64, dtype=torch.bool, device="cuda")
+    rows[5] = False
+    assert torch.equal(y[:16, rows], good[:16, rows]) and torch.isnan(y[:16, 5]).all()
+
+
+def test_expert_product_in_a_graph_and_on_a_stream(env):
+    torch, bm = env
+    rng = np.random.default_rng(9)
+    E, k, T = 16, 3, 50
+    w = torch.randn(E, 96, 128, device="cuda").to(torch.bfloat16)
+    up = torch.randn(E, 96, 128, device="cuda").to(torch.bfloat16)
+    x = torch.randn(T, 128, device="cuda").to(torch.bfloat16)
+    data = [torch.from_numpy(logits_of(rng, T, E)).cuda() for _ in range(3)]
+    logits = data[0].clone()
+    y = torch.zeros(T * k, 96, device="cuda")
+
+    def step():
+        r = bm.route(logits, k)
+        return bm.expert_product(w, x, r.offsets, index=r.pairs, fan=k, up=up, y=y)
+    step()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for d in data[1:]:
+        logits.copy_(d)
+        y.zero_()
+        g.replay()
+        got = y.clone()
+        y.zero_()
+        assert torch.equal(got, step())
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    r = bm.route(logits, k)
+    st.wait_stream(torch.cuda.current_stream())
+    a = bm.expert_product(w, x, r.offsets, index=r.pairs, fan=k, up=up, stream=st)
+    st.synchronize()
+    n = int(r.offsets[-1])
+    assert torch.equal(a[:n], y[:n])
+
+
+# ---------------------------------------------------------------------------
+# the weighted sum
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("T,k,D,P", [(1, 1, 1, 1), (1, 8, 2048, 8), (5, 3, 100, 20), (37, 8, 2050, 296), (70, 32, 64, 2000), (9, 2, 8200, 18),
+                                     (600, 8, 256, 4800), (3, 4, 1, 0)])
+@pytest.mark.parametrize("ty,out", [("bf16", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("base", [None, "own", "place"])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_expert_combine(env, T, k, D, P, ty, out, base, shift):
+    torch, bm = env
+    g = torch.Generator().manual_seed(T + k + D + P)
+    dts = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+    def rows(n, dt):
+        buf = torch.randn(n, D + 9 if shift else (D + 7) // 8 * 8, generator=g).to(dts[dt]).cuda()
+        return buf[:, shift:shift + D]
+    y = rows(P, ty)
+    places = torch.randint(-2, P + 3, (T, k), generator=g, dtype=torch.int32)
+    places[0, 0] = -1
+    weights = torch.rand(T, k, generator=g)
+    obuf = torch.full((T, D + 9 if shift else (D + 7) // 8 * 8 + 8), 77.0, dtype=dts[out], device="cuda")
+    o = obuf[:, shift:shift + D]
+    b = None
+    if base:
+        b = rows(T, out)
+        if base == "place":
+            o.copy_(b)
+            b = o
+    bv = b.double().cpu().numpy() if base else None
+    got = bm.expert_combine(y, places.cuda(), weights.cuda(), base=b, out=o)
+    assert got is o
+    yv, wv = y.double().cpu().numpy(), weights.double().numpy()
+    want = oe.combine(yv, places.numpy(), wv, bv)
+    mag = oe.combine(np.abs(yv), places.numpy(), wv, np.abs(bv) if base else None)
+    tol = (k + 2) * u * mag
+    tol = tol + (2.0 ** -8 * (np.abs(want) + tol) if out == "bf16" else u * np.abs(want))
+    assert (np.abs(o.double().cpu().numpy() - want) <= tol).all()
+    rest = obuf.clone()
+    rest[:, shift:shift + D] = 77.0
+    assert (rest == 77).all()
+
+
+def test_expert_combine_of_experts_that_do_not_count(env):
+    """A place outside the rows adds nothing, whatever its weight and whatever lies in the rows."""
+    torch, bm = env
+    y = torch.full((4, 64), float("nan"), device="cuda")
+    y[2] = 3.0
+    places = torch.tensor([[-1, 2, 4], [-1, -1, -1]], dtype=torch.int32).cuda()
+    w = torch.tensor([[float("inf"), 2.0, float("nan")], [1.0, 1.0, 1.0]]).cuda()
+    out = bm.expert_combine(y, places, w)
+    assert (out[0] == 6).all() and (out[1] == 0).all()
+    assert bm.expert_combine(y, places[:0], w[:0]).shape == (0, 64)
+    with pytest.raises(bm.BitsMoEError):
+        bm.expert_combine(y, places, w[:, :2])
+    with pytest.raises(bm.BitsMoEError):
+        bm.expert_combine(y, places, w, base=torch.zeros(2, 64, device="cuda", dtype=torch.bfloat16), dtype=torch.float32)
+
+
+# ---------------------------------------------------------------------------
+# together
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("T", [1, 6, 90, 400])
+def test_a_block_of_coded_experts(env, T):
+    """Norm in 8 bits, routing, gate and up, SwiGLU's rows in 8 bits, down, weighted sum onto the shared branch, the next
+    norm: as a decoder block runs them, against float64 on the values that each step was given."""
+    torch, bm = env
+    E, k, D, I = 12, 3, 192, 160
+    g = torch.Generator().manual_seed(T)
+    mats = {n: bm.rowscale_quantize((torch.randn(E, *s, generator=g) / s[1] ** 0.5).cuda())
+            for n, s in (("gate", (I, D)), ("up", (I, D)), ("down", (D, I)))}
+    router = (torch.randn(E, D, generator=g) / D ** 0.5).cuda()
+    h = torch.randn(T, D, generator=g).cuda()
+    gain = (1 + 0.1 * torch.randn(D, generator=g)).cuda()
+    shared = torch.randn(T, D, generator=g).cuda()
+    _, x = bm.block_norm(h, pre_gain=gain, x_dtype=torch.float8_e4m3fn)
+    xv = bm.rowscale_dequantize(x)
+    logits = xv @ router.T
+    if T > 2:
+        logits[-1] = float("-inf")
+    r = bm.route(logits, k)
+    hid = bm.expert_product(mats["gate"], x, r.offsets, index=r.pairs, fan=k, up=mats["up"], dtype=torch.bfloat16)
+    n = int(r.offsets[-1])
+    hid[n:] = 0
+    hq = bm.rowscale_quantize(hid)
+    yd = bm.expert_product(mats["down"], hq, r.offsets, dtype=torch.float32)
+    out = bm.expert_combine(yd, r.places, r.weights, base=shared)
+    h2, x2 = bm.block_norm(h, out, x_dtype=torch.float8_e4m3fn)
+    vals = {n_: bm.rowscale_dequantize(m).double().cpu().numpy() for n_, m in mats.items()}
+    off, pairs = r.offsets.cpu().numpy(), r.pairs.cpu().numpy()
+    want, parts = oe.product(vals["gate"], xv.double().cpu().numpy(), off, pairs, k, vals["up"])
+    got = hid.double().cpu().numpy()
+    for p in range(n):
+        gs, gm, us, um = parts[p]
+        eg, eu = (D + 16) * 2.0 ** -23 * gm, (D + 16) * 2.0 ** -23 * um
+        silu = gs / (1 + np.exp(-gs))
+        tol = 1.1 * eg * (np.abs(us) + eu) + np.abs(silu) * eu + (16 + np.abs(gs)) * u * np.abs(want[p])
+        assert (np.abs(got[p] - want[p]) <= tol + 2.0 ** -8 * (np.abs(want[p]) + tol)).all()
+    hv = bm.rowscale_dequantize(hq).double().cpu().numpy()
+    down, parts = oe.product(vals["down"], hv, off)
+    got = yd.double().cpu().numpy()
+    for p in range(n):
+        assert (np.abs(got[p] - down[p]) <= (I + 16) * 2.0 ** -23 * parts[p][1] + 4 * u * np.abs(down[p])).all()
+    wt, pl = r.weights.double().cpu().numpy(), r.places.cpu().numpy()
+    sv = shared.double().cpu().numpy()
+    want = oe.combine(got, pl, wt, sv)
+    mag = oe.combine(np.abs(np.nan_to_num(got)), pl, wt, np.abs(sv))
+    assert (np.abs(out.double().cpu().numpy() - want) <= (k + 3) * u * mag).all()
+    if T > 2:
+        assert torch.equal(out[-1], shared[-1])
+    want_h = h.double().cpu().numpy() + out.double().cpu().numpy()
+    assert (np.abs(h2.double().cpu().numpy() - want_h) <= 2 * u * (np.abs(want_h) + np.abs(h.double().cpu().numpy()))).all()
+    assert torch.isfinite(bm.rowscale_dequantize(x2)).all()
+
+
+def test_refusals_of_the_binding(env):
+    torch, bm = env
+    w = torch.randn(2, 8, 16, device="cuda").to(torch.bfloat16)
+    x = torch.randn(4, 16, device="cuda").to(torch.bfloat16)
+    off = torch.zeros(3, dtype=torch.int32, device="cuda")
+    ok = dict(w=w, x=x, offsets=off)
+    for kw in (dict(w=w.float()), dict(w=w[0]), dict(x=x[:, :8]), dict(x=x.float()), dict(offsets=off[:2]), dict(offsets=off.long()),
+               dict(offsets=off.cpu()), dict(index=off.float()), dict(fan=0), dict(up=w[:, :4]), dict(up=w[:1]), dict(y=torch.zeros(4, 7, device="cuda")),
+               dict(y=torch.zeros(4, 8, device="cuda", dtype=torch.float16)), dict(status=torch.zeros(2, dtype=torch.int32, device="cuda")),
+               dict(w=w.transpose(1, 2)), dict(x=x.cpu())):
+        with pytest.raises(bm.BitsMoEError):
+            bm.expert_product(**{**ok, **kw})
