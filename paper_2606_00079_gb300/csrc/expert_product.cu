@@ -13,6 +13,7 @@
 
 #include "microscale.cuh"
 #include "rows.cuh"
+#include "tc.cuh"
 
 namespace {
 using namespace bmoe;
@@ -35,6 +36,8 @@ struct ExpertArgs {
   void* y;
   int y_type;
   int64_t y_ld;
+  int nk, stages;        // tensor cores: steps of 128 bytes of the columns, depth of the ring
+  int w_next, u_next;    // 1: an expert has matrices of its own (0: one stands for all)
   long long spin;
   int lose;
   int* status;
@@ -208,6 +211,281 @@ cudaError_t launch_plain(ExpertArgs a, int sms, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+// ---------------------------------------------------------------------------
+// Rows on 16-byte boundaries: tcgen05, 128 rows of an expert's matrix (with U 64 of both) x N rows of y a tile, the matrix
+// as the operand of 128 rows, so that an expert's few rows cost an MMA of few columns.
+//
+// A ring of stages of 128 bytes of the columns: warp 0 brings the matrices' tiles by TMA, warp 2 the rows of x, where there
+// is an index four at a time from wherever they are (TMA's gather).  With U, 16 rows of each take turns in the tile, so
+// that a warp's 32 lanes of the accumulator hold 16 rows of both products and one exchange between lanes brings them
+// together.  Warp 1 issues the MMAs; eight warps empty one accumulator while the other fills.
+// ---------------------------------------------------------------------------
+constexpr int kTcThreads = 384;          // warps: 0 matrices, 1 MMA, 2 rows of x, 4.. results
+constexpr int kOutWarps = 8, kOutThreads = 32 * kOutWarps;
+constexpr uint32_t kATile = 128 * 128;   // bytes of a stage's tile of the matrices
+constexpr int kTcShared = 227 * 1024;    // (all of an SM's, as of every kernel that allocates tensor memory)
+
+struct TcShared {
+  Groups groups;
+  alignas(16) float factor[2][256];      // of the rows of y: x's scale, NaN for a row that is not there
+  uint64_t full[16], empty[16], afull[2], aempty[2], drained;
+  uint32_t slot;
+};
+
+// What is stored for results that a wait that ran out has lost.  A warp whose wait ran out passes nothing on: who waits for
+// it runs out as well, up to the warps that store.
+constexpr uint32_t kLost = 0x7FC00000u;
+
+template <bool F8, bool GLU>
+__global__ void __launch_bounds__(kTcThreads, 1)
+    k_expert_tc(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap,
+                const __grid_constant__ CUtensorMap xmap, const __grid_constant__ ExpertArgs a) {
+  constexpr int kCols = F8 ? 128 : 64;   // columns of a stage
+  constexpr int kRows = GLU ? 64 : 128;  // rows of y's width that a tile covers
+  extern __shared__ uint8_t raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t stage = kATile + (uint32_t)a.N * 128;
+  TcShared& s = *reinterpret_cast<TcShared*>(sm + (size_t)a.stages * stage);
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  if (tid == 0) {
+    prefetch_map(&wmap);
+    prefetch_map(&xmap);
+    if (GLU) prefetch_map(&umap);
+    for (int i = 0; i < a.stages; ++i) {
+      mbar_init_n(s.full + i, 2);
+      mbar_init_n(s.empty + i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init_n(s.afull + i, 1);
+      mbar_init_n(s.aempty + i, kOutWarps);
+    }
+    mbar_init_n(&s.drained, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (wid == 1) tmem_alloc(&s.slot, 512);
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  read_groups<kTcThreads>(a, s.groups);   // (with block barriers)
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, s.slot, 0);
+  const int ntiles = s.groups.tiles[a.E] * a.mt;
+  bool ok = true;
+
+  if (wid == 0) {
+    if (lane == 0) {
+      int st = 0, u = 0, n = 0;
+      for (int tile = blockIdx.x; tile < ntiles && ok; tile += gridDim.x) {
+        const Tile t = tile_of(a, s.groups, tile, 16);
+        for (int i = 0; i < a.nk; ++i, ++n) {
+          if (u > 0) ok = mbar_wait(s.empty + st, (uint32_t)(u - 1) & 1u, a.spin);
+          if (!ok) break;
+          const uint32_t bar = smem_u32(s.full + st), dst = smem_u32(sm) + (uint32_t)st * stage;
+          mbar_expect_tx(s.full + st, kATile);
+          if constexpr (GLU) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              tma_load_3d(dst + q * 4096, &wmap, i * kCols, t.m * kRows + 16 * q, t.e * a.w_next, bar);
+              tma_load_3d(dst + q * 4096 + 2048, &umap, i * kCols, t.m * kRows + 16 * q, t.e * a.u_next, bar);
+            }
+          } else {
+            tma_load_3d(dst, &wmap, i * kCols, t.m * kRows, t.e * a.w_next, bar);
+          }
+          if (++st == a.stages) {
+            st = 0;
+            ++u;
+          }
+        }
+      }
+      // copies in flight: a phase ends with the other warp's arrival too, which may be missing after a timeout
+      for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok ? kWaitClocks : a.spin);
+    }
+    __syncwarp();
+  } else if (wid == 1) {
+    const uint32_t one = elect_one();
+    const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(sm) + kATile);
+    int st = 0, u = 0, it = 0;
+    for (int tile = blockIdx.x; tile < ntiles && ok; tile += gridDim.x, ++it) {
+      const int n16 = (tile_of(a, s.groups, tile, 16).n + 15) / 16 * 16;
+      const uint32_t idesc = F8 ? idesc_e4m3(n16) : idesc_bf16(n16);
+      const int buf = it & 1, use = it >> 1;
+      if (use > 0) ok = mbar_wait(s.aempty + buf, (uint32_t)(use - 1) & 1u, a.spin);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t acc = tmem + (uint32_t)(buf * 256);
+      for (int i = 0; i < a.nk; ++i) {
+        ok = mbar_try_wait(s.full + st, (uint32_t)u & 1u) || mbar_wait(s.full + st, (uint32_t)u & 1u, a.spin);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t o = (uint64_t)((uint32_t)st * (stage >> 4));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if constexpr (F8) mma_f8(one, acc, da + o + 2 * k, db + o + 2 * k, idesc, (uint32_t)(i | k));
+          else mma_f16(one, acc, da + o + 2 * k, db + o + 2 * k, idesc, (uint32_t)(i | k));
+        }
+        if (!(a.lose && (i | it | (int)blockIdx.x) == 0)) mma_commit(one, s.empty + st);
+        if (++st == a.stages) {
+          st = 0;
+          ++u;
+        }
+      }
+      if (!ok) break;
+      mma_commit(one, s.afull + buf);
+    }
+    if (!ok) {
+      mma_commit(one, &s.drained);
+      mbar_wait(&s.drained, 0u);
+    }
+    __syncwarp();
+  } else if (wid == 2) {
+    int st = 0, u = 0, n = 0;
+    for (int tile = blockIdx.x; tile < ntiles && ok; tile += gridDim.x) {
+      const Tile t = tile_of(a, s.groups, tile, 16);
+      const int n16 = (t.n + 15) / 16 * 16;
+      int row[2][4];   // with an index: rows 4 (lane + 32 j) .. of the tile (any row of x where there is none)
+      if (a.index) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int r = 4 * (lane + 32 * j) + q;
+            row[j][q] = r < t.n ? max(row_of(a, t.p0 + r), 0) : 0;
+          }
+      }
+      for (int i = 0; i < a.nk; ++i, ++n) {
+        if (u > 0) ok = mbar_try_wait(s.empty + st, (uint32_t)(u - 1) & 1u) || mbar_wait(s.empty + st, (uint32_t)(u - 1) & 1u, a.spin);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        const uint32_t bar = smem_u32(s.full + st), dst = smem_u32(sm) + (uint32_t)st * stage + kATile;
+        if (lane == 0) mbar_expect_tx(s.full + st, (uint32_t)n16 * 128u);
+        __syncwarp();
+        if (a.index) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            if (4 * (lane + 32 * j) < n16) tma_gather4(dst + (uint32_t)(lane + 32 * j) * 512u, &xmap, i * kCols, row[j], bar);
+        } else if (16 * lane < n16) {
+          tma_load_2d(dst + (uint32_t)lane * 2048u, &xmap, i * kCols, t.p0 + 16 * lane, bar);
+        }
+        if (++st == a.stages) {
+          st = 0;
+          ++u;
+        }
+      }
+    }
+    for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok ? kWaitClocks : a.spin);
+    __syncwarp();
+  } else if (wid >= 4) {
+    const int quarter = wid & 3, half = (wid - 4) >> 2;
+    const bool low = !GLU || lane < 16;   // with U: lanes of W's rows, and of U's
+    int it = 0;
+    for (int tile = blockIdx.x; tile < ntiles; tile += gridDim.x, ++it) {
+      const Tile t = tile_of(a, s.groups, tile, 16);
+      const int buf = it & 1, use = it >> 1;
+      float* factor = s.factor[buf];
+      {
+        const int r = tid - 128;
+        float f = 0.f;
+        if (r < t.n) {
+          const int row = row_of(a, t.p0 + r);
+          f = row < 0 ? __uint_as_float(kLost) : F8 ? __ldg(a.xs + row) : 1.f;
+        }
+        factor[r] = f;
+      }
+      const int m = t.m * kRows + (GLU ? 16 * quarter + (lane & 15) : 32 * quarter + lane);
+      float sw = 1.f;
+      if (F8 && m < a.rows) sw = low ? __ldg(a.ws + t.e * a.w_sld + m) : __ldg(a.us + t.e * a.u_sld + m);
+      asm volatile("bar.sync 1, %0;" ::"n"(kOutThreads) : "memory");   // (a warp that passes has read the factors of two tiles ago)
+      if (ok) ok = mbar_wait_idle(s.afull + buf, (uint32_t)use & 1u, a.spin);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t tl = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(buf * 256);
+      for (int c0 = 16 * half; c0 < t.n; c0 += 32) {
+        uint32_t v[16];
+        if (ok) {
+          tmem_ld16(tl + (uint32_t)c0, v);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 16; ++q) v[q] = kLost;
+        }
+        float f[16];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(f + 4 * q) = *reinterpret_cast<const float4*>(factor + c0 + 4 * q);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) f[q] *= F8 ? __uint_as_float(v[q]) * sw : __uint_as_float(v[q]);
+        const int64_t at = (int64_t)(t.p0 + c0) * a.y_ld + m;
+        if constexpr (GLU) {
+#pragma unroll
+          for (int q = 0; q < 16; q += 2) {   // lanes of W's rows take the even columns, those of U's the odd ones
+            const float r = __shfl_xor_sync(0xFFFFFFFFu, low ? f[q + 1] : f[q], 16);
+            const float g = low ? f[q] : r, w = low ? r : f[q + 1];
+            const int c = low ? q : q + 1;
+            if (m < a.rows && c0 + c < t.n) store_y(a.y, a.y_type, at + c * a.y_ld, silu_mul(g, w));
+          }
+        } else if (m < a.rows) {
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            if (c0 + q < t.n) store_y(a.y, a.y_type, at + q * a.y_ld, f[q]);
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      mbar_arrive(lane == 0, s.aempty + buf);
+    }
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (!ok && a.status) atomicCAS(a.status, 0, BITSMOE_ERR_TIMEOUT);
+  if (wid == 1) {
+    __syncwarp();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// Rows of y of a tile: twice an expert's on average, so that few experts have more than one tile, each of which reads
+// the expert's matrix again; a stage of more rows leaves room for fewer stages.
+int tile_rows(int P, int E) {
+  const int most = (P + 15) / 16 * 16;
+  return std::min({256, most, std::max(32, ((int)(2ll * P / E) + 15) / 16 * 16)});
+}
+
+bool on_boundaries(const void* p, int64_t ld, int64_t size, int64_t rows) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || ld * size % 16 == 0);
+}
+int64_t pitch_of(int64_t ld, int64_t cols, int64_t size, int64_t rows) {   // (of one row: any)
+  return rows <= 1 ? (cols * size + 15) / 16 * 16 : ld * size;
+}
+
+// Whether the tensor-core kernel takes these rows; its maps.
+bool tc_maps(const ExpertArgs& a, bool f8, CUtensorMap* wm, CUtensorMap* um, CUtensorMap* xm) {
+  const int64_t es = f8 ? 1 : 2;
+  if (a.x_rows < 1 || !on_boundaries(a.x, a.x_ld, es, a.x_rows)) return false;
+  const int box = a.up ? 16 : 128;
+  const auto matrices = [&](CUtensorMap* m, const void* p, int64_t ld, int64_t eld) {
+    return on_boundaries(p, ld, es, a.rows) && make_matrices_map(m, f8, p, a.E, a.rows, a.cols, pitch_of(ld, a.cols, es, a.rows), eld * es, box);
+  };
+  if (!matrices(wm, a.w, a.w_ld, a.w_eld)) return false;
+  if (a.up && !matrices(um, a.up, a.u_ld, a.u_eld)) return false;
+  return make_row_map(xm, f8, a.x, a.x_rows, a.cols, pitch_of(a.x_ld, a.cols, es, a.x_rows), a.index ? 1 : 16);
+}
+
+template <bool F8, bool GLU>
+cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um, const CUtensorMap& xm, int dev, int sms, cudaStream_t st) {
+  a.N = tile_rows(a.P, a.E);
+  a.mt = (a.rows + (GLU ? 63 : 127)) / (GLU ? 64 : 128);
+  a.nk = (a.cols + (F8 ? 127 : 63)) / (F8 ? 128 : 64);
+  a.w_next = a.w_eld != 0;
+  a.u_next = a.u_eld != 0;
+  a.stages = std::min(16, (int)((kTcShared - 1024 - sizeof(TcShared)) / (kATile + (size_t)a.N * 128)));
+  const int64_t most = std::min<int64_t>(a.P, (int64_t)a.P / a.N + a.E) * a.mt;
+  auto kern = k_expert_tc<F8, GLU>;
+  const cudaError_t e = allow_shared<k_expert_tc<F8, GLU>>(dev, kTcShared);
+  if (e != cudaSuccess) return e;
+  kern<<<(unsigned)std::min<int64_t>(most, sms), kTcThreads, kTcShared, st>>>(wm, um, xm, a);
+  return cudaGetLastError();
+}
+
 int matrices_check(const bitsmoe_expert_matrices* m) {
   if (!m || (m->type != BITSMOE_BF16 && m->type != BITSMOE_E4M3) || m->experts < 1 || m->rows < 0 || m->cols < 1) return BITSMOE_ERR_INVALID_ARG;
   if (m->experts > kMaxExperts || m->rows > kMaxMicroCols || m->cols > kMaxMicroCols) return BITSMOE_ERR_SHAPE;
@@ -277,6 +555,13 @@ extern "C" int bitsmoe_expert_product(const bitsmoe_expert_product_args* args, v
   a.lose = debug_skip_arrival();
   a.status = g.status;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  e = f8 ? launch_plain<true>(a, sms, st) : launch_plain<false>(a, sms, st);
+  CUtensorMap wm, um, xm;
+  if (tc_maps(a, f8, &wm, &um, &xm)) {
+    if (!a.up) um = wm;
+    e = f8 ? (a.up ? launch_tc<true, true>(a, wm, um, xm, dev, sms, st) : launch_tc<true, false>(a, wm, um, xm, dev, sms, st))
+           : (a.up ? launch_tc<false, true>(a, wm, um, xm, dev, sms, st) : launch_tc<false, false>(a, wm, um, xm, dev, sms, st));
+  } else {
+    e = f8 ? launch_plain<true>(a, sms, st) : launch_plain<false>(a, sms, st);
+  }
   return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
 }

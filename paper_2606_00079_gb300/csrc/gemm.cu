@@ -416,6 +416,23 @@ bool make_row_map(void* map_out, bool bytes, const void* base, int64_t rows, int
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same of `count` such matrices `next_bytes` apart (a multiple of 16; a matrix that stands for all of them: 0).
+bool make_matrices_map(void* map_out, bool bytes, const void* base, int64_t count, int64_t rows, int64_t cols, int64_t pitch_bytes,
+                       int64_t next_bytes, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (next_bytes == 0 || count == 1) count = 1, next_bytes = 16;
+  if (!fn || count < 1 || rows < 1 || cols < 1 || pitch_bytes < 16 || pitch_bytes % 16 || next_bytes < 16 || next_bytes % 16 ||
+      box_rows < 1 || box_rows > 256 || (reinterpret_cast<uintptr_t>(base) & 15))
+    return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count};
+  const cuuint64_t strides[2] = {(cuuint64_t)pitch_bytes, (cuuint64_t)next_bytes};
+  const cuuint32_t box[3] = {(cuuint32_t)(bytes ? 128 : 64), (cuuint32_t)box_rows, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(static_cast<CUtensorMap*>(map_out), bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+            const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Tensor map of a row-major bf16 matrix [rows][cols_pad] for tiles of box_rows rows and 64
 // columns.  cols_pad * 2 must be a multiple of 16.
 static bool make_map(CUtensorMap* m, const void* base, int rows, int cols_pad, int box_rows) {

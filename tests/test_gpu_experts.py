@@ -342,6 +342,44 @@ def test_expert_product_in_a_graph_and_on_a_stream(env):
     assert torch.equal(a[:n], y[:n])
 
 
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("fan", [0, 2])
+def test_expert_product_lost_waits(env, ty, glu, fan):
+    """An arrival of block 0 is left out, so that its waits run out: the call reports it, what it lost is NaN, every other
+    result stands, and the next call is as ever."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(8)
+    E, R, C, P = 12, 192, 4096, 240
+    w, ws, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
+    up, us, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty) if glu else (None, None, None)
+    x, xs, _ = pitched(torch, torch.randn(P, C, generator=g), ty)
+    w, x = wrap(bm, w, ws), wrap(bm, x, xs)
+    up = wrap(bm, up, us) if glu else None
+    off = torch.arange(0, P + 1, P // E, dtype=torch.int32).cuda()
+    idx = torch.randint(0, 2 * P, (P,), generator=g, dtype=torch.int32).cuda() if fan else None
+    kw = dict(index=idx, fan=max(fan, 1), up=up)
+    ref = bm.expert_product(w, x, off, **kw)
+    for dt in (torch.float32, torch.bfloat16):
+        for with_status in (True, False):
+            buf = torch.full((P, R + 5), 7.0, dtype=dt, device="cuda")
+            y, status = buf[:, :R], torch.zeros(1, dtype=torch.int32, device="cuda")
+            bm.bitsmoe_debug_wait_limit(1, 2_000_000)
+            try:
+                bm.expert_product(w, x, off, y=y, status=status if with_status else None, **kw)
+                torch.cuda.synchronize()
+            finally:
+                bm.bitsmoe_debug_wait_limit(0, 0)
+            assert int(status.item()) == (bm.ERR_CODE["TIMEOUT"] if with_status else 0)
+            lost = torch.isnan(y)
+            assert bool(lost.any()) and not bool(lost.all())
+            assert torch.equal(y[~lost], ref.to(dt)[~lost])
+            assert (buf[:, R:] == 7).all()
+            status.zero_()
+            assert torch.equal(bm.expert_product(w, x, off, y=y, status=status, **kw), ref.to(dt))
+            assert int(status.item()) == 0
+
+
 # ---------------------------------------------------------------------------
 # the weighted sum
 # ---------------------------------------------------------------------------
