@@ -212,23 +212,27 @@ cudaError_t launch_plain(ExpertArgs a, int sms, cudaStream_t st) {
 }
 
 // ---------------------------------------------------------------------------
-// Rows on 16-byte boundaries: tcgen05, 128 rows of an expert's matrix (with U 64 of both) x N rows of y a tile, the matrix
-// as the operand of 128 rows, so that an expert's few rows cost an MMA of few columns.
+// Rows on 16-byte boundaries: tcgen05, a pair of CTAs a tile of 256 rows of an expert's matrix (with U 128 of both) x N
+// rows of y: the matrix is the operand of many rows, so that an expert's few rows cost an MMA of few columns.  Each CTA
+// has half of both operands and the results of its 128 rows.
 //
-// A ring of stages of 128 bytes of the columns: warp 0 brings the matrices' tiles by TMA, warp 2 the rows of x, where there
-// is an index four at a time from wherever they are (TMA's gather).  With U, 16 rows of each take turns in the tile, so
-// that a warp's 32 lanes of the accumulator hold 16 rows of both products and one exchange between lanes brings them
-// together.  Warp 1 issues the MMAs; eight warps empty one accumulator while the other fills.
+// A ring of stages of 128 bytes of the columns: warp 0 brings the matrix's tile by TMA, four warps the rows of x, wherever
+// they are, 16 bytes a thread at a time (cp.async; TMA's gather of four rows took 63 clocks for 512 bytes); their copies arrive
+// on a barrier by themselves, and warp 2 hands the stage on.  With U, 16 rows of
+// each take turns in the tile, so that a warp's 32 lanes of the accumulator hold 16 rows of both products and one exchange
+// between lanes brings them together.  The first CTA's warp 1 issues the MMAs; eight warps of each CTA empty one
+// accumulator while the other fills.
 // ---------------------------------------------------------------------------
-constexpr int kTcThreads = 384;          // warps: 0 matrices, 1 MMA, 2 rows of x, 4.. results
-constexpr int kOutWarps = 8, kOutThreads = 32 * kOutWarps;
+constexpr int kTcThreads = 512;          // warps: 0 matrices, 1 MMA, 2 rows of x that are there, 4.. rows of x, 8.. results
+constexpr int kXWarps = 4, kOutWarps = 8, kOutThreads = 32 * kOutWarps;
+constexpr int kStagesMost = 12;
 constexpr uint32_t kATile = 128 * 128;   // bytes of a stage's tile of the matrices
 constexpr int kTcShared = 227 * 1024;    // (all of an SM's, as of every kernel that allocates tensor memory)
 
 struct TcShared {
   Groups groups;
   alignas(16) float factor[2][256];      // of the rows of y: x's scale, NaN for a row that is not there
-  uint64_t full[16], empty[16], afull[2], aempty[2], drained;
+  uint64_t full[kStagesMost], empty[kStagesMost], xfull[kStagesMost], afull[2], aempty[2], drained;
   uint32_t slot;
 };
 
@@ -236,35 +240,46 @@ struct TcShared {
 // it runs out as well, up to the warps that store.
 constexpr uint32_t kLost = 0x7FC00000u;
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {   // the rest of the 16 are zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// An arrival of this thread once its copies so far are there.
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
 template <bool F8, bool GLU>
 __global__ void __launch_bounds__(kTcThreads, 1)
-    k_expert_tc(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap,
-                const __grid_constant__ CUtensorMap xmap, const __grid_constant__ ExpertArgs a) {
+    k_expert_tc(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ ExpertArgs a) {
   constexpr int kCols = F8 ? 128 : 64;   // columns of a stage
-  constexpr int kRows = GLU ? 64 : 128;  // rows of y's width that a tile covers
+  constexpr int kRows = GLU ? 64 : 128;  // rows of y's width that a CTA covers
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t stage = kATile + (uint32_t)a.N * 128;
+  const uint32_t stage = kATile + (uint32_t)a.N * 64;
   TcShared& s = *reinterpret_cast<TcShared*>(sm + (size_t)a.stages * stage);
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   if (tid == 0) {
     prefetch_map(&wmap);
-    prefetch_map(&xmap);
     if (GLU) prefetch_map(&umap);
     for (int i = 0; i < a.stages; ++i) {
-      mbar_init_n(s.full + i, 2);
+      mbar_init_n(s.full + i, 3);   // (the first CTA's: the matrices' bytes of both, x's rows of each)
+      mbar_init_n(s.xfull + i, 32 * kXWarps);
       mbar_init_n(s.empty + i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init_n(s.afull + i, 1);
-      mbar_init_n(s.aempty + i, kOutWarps);
+      mbar_init_n(s.aempty + i, 2 * kOutWarps);
     }
     mbar_init_n(&s.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (wid == 1) tmem_alloc(&s.slot, 512);
+  if (wid == 1) tmem_alloc_pair(&s.slot, 512);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  read_groups<kTcThreads>(a, s.groups);   // (with block barriers)
+  read_groups<kTcThreads>(a, s.groups);
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, s.slot, 0);
   const int ntiles = s.groups.tiles[a.E] * a.mt;
@@ -272,22 +287,24 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 
   if (wid == 0) {
     if (lane == 0) {
+      const uint32_t full0 = cluster_address(smem_u32(s.full), 0);
       int st = 0, u = 0, n = 0;
-      for (int tile = blockIdx.x; tile < ntiles && ok; tile += gridDim.x) {
-        const Tile t = tile_of(a, s.groups, tile, 16);
+      for (int tile = pair; tile < ntiles && ok; tile += pairs) {
+        const Tile t = tile_of(a, s.groups, tile, 32);
+        const int m0 = (2 * t.m + rank) * kRows;
         for (int i = 0; i < a.nk; ++i, ++n) {
           if (u > 0) ok = mbar_wait(s.empty + st, (uint32_t)(u - 1) & 1u, a.spin);
           if (!ok) break;
-          const uint32_t bar = smem_u32(s.full + st), dst = smem_u32(sm) + (uint32_t)st * stage;
-          mbar_expect_tx(s.full + st, kATile);
+          const uint32_t bar = full0 + 8u * (uint32_t)st, dst = smem_u32(sm) + (uint32_t)st * stage;
+          if (rank == 0) mbar_expect_tx(s.full + st, 2 * kATile);   // both CTAs' tiles
           if constexpr (GLU) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              tma_load_3d(dst + q * 4096, &wmap, i * kCols, t.m * kRows + 16 * q, t.e * a.w_next, bar);
-              tma_load_3d(dst + q * 4096 + 2048, &umap, i * kCols, t.m * kRows + 16 * q, t.e * a.u_next, bar);
+              tma_load_3d_pair(dst + q * 4096, &wmap, i * kCols, m0 + 16 * q, t.e * a.w_next, bar);
+              tma_load_3d_pair(dst + q * 4096 + 2048, &umap, i * kCols, m0 + 16 * q, t.e * a.u_next, bar);
             }
           } else {
-            tma_load_3d(dst, &wmap, i * kCols, t.m * kRows, t.e * a.w_next, bar);
+            tma_load_3d_pair(dst, &wmap, i * kCols, m0, t.e * a.w_next, bar);
           }
           if (++st == a.stages) {
             st = 0;
@@ -295,17 +312,23 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           }
         }
       }
-      // copies in flight: a phase ends with the other warp's arrival too, which may be missing after a timeout
-      for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok ? kWaitClocks : a.spin);
+      // both CTAs' copies in flight (after a timeout an arrival of the phase may be missing)
+      if (rank == 0)
+        for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok ? kWaitClocks : a.spin);
     }
     __syncwarp();
-  } else if (wid == 1) {
+  } else if (wid == 1 && rank == 0) {
     const uint32_t one = elect_one();
     const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(sm) + kATile);
+    uint32_t empty[2], afull[2];   // both CTAs'
+    for (uint32_t r = 0; r < 2; ++r) {
+      empty[r] = cluster_address(smem_u32(s.empty), r);
+      afull[r] = cluster_address(smem_u32(s.afull), r);
+    }
     int st = 0, u = 0, it = 0;
-    for (int tile = blockIdx.x; tile < ntiles && ok; tile += gridDim.x, ++it) {
-      const int n16 = (tile_of(a, s.groups, tile, 16).n + 15) / 16 * 16;
-      const uint32_t idesc = F8 ? idesc_e4m3(n16) : idesc_bf16(n16);
+    for (int tile = pair; tile < ntiles && ok; tile += pairs, ++it) {
+      const int n32 = (tile_of(a, s.groups, tile, 32).n + 31) / 32 * 32;
+      const uint32_t idesc = idesc_pair<F8>(n32);
       const int buf = it & 1, use = it >> 1;
       if (use > 0) ok = mbar_wait(s.aempty + buf, (uint32_t)(use - 1) & 1u, a.spin);
       ok = __all_sync(0xFFFFFFFFu, ok);
@@ -319,71 +342,89 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint64_t o = (uint64_t)((uint32_t)st * (stage >> 4));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if constexpr (F8) mma_f8(one, acc, da + o + 2 * k, db + o + 2 * k, idesc, (uint32_t)(i | k));
-          else mma_f16(one, acc, da + o + 2 * k, db + o + 2 * k, idesc, (uint32_t)(i | k));
+        for (int k = 0; k < 4; ++k) mma_pair<F8>(one, acc, da + o + 2 * k, db + o + 2 * k, idesc, (uint32_t)(i | k));
+        if (!(a.lose && (i | it | pair) == 0)) {
+          mma_commit_pair(one, empty[0] + 8u * (uint32_t)st);
+          mma_commit_pair(one, empty[1] + 8u * (uint32_t)st);
         }
-        if (!(a.lose && (i | it | (int)blockIdx.x) == 0)) mma_commit(one, s.empty + st);
         if (++st == a.stages) {
           st = 0;
           ++u;
         }
       }
       if (!ok) break;
-      mma_commit(one, s.afull + buf);
+      mma_commit_pair(one, afull[0] + 8u * (uint32_t)buf);
+      mma_commit_pair(one, afull[1] + 8u * (uint32_t)buf);
     }
     if (!ok) {
-      mma_commit(one, &s.drained);
+      mma_commit_pair(one, cluster_address(smem_u32(&s.drained), 0));
       mbar_wait(&s.drained, 0u);
     }
     __syncwarp();
   } else if (wid == 2) {
-    int st = 0, u = 0, n = 0;
-    for (int tile = blockIdx.x; tile < ntiles && ok; tile += gridDim.x) {
-      const Tile t = tile_of(a, s.groups, tile, 16);
-      const int n16 = (t.n + 15) / 16 * 16;
-      int row[2][4];   // with an index: rows 4 (lane + 32 j) .. of the tile (any row of x where there is none)
-      if (a.index) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int r = 4 * (lane + 32 * j) + q;
-            row[j][q] = r < t.n ? max(row_of(a, t.p0 + r), 0) : 0;
+    if (lane == 0) {
+      const uint32_t full0 = cluster_address(smem_u32(s.full), 0);
+      int st = 0, u = 0;
+      for (int tile = pair; tile < ntiles && ok; tile += pairs)
+        for (int i = 0; i < a.nk; ++i) {
+          ok = mbar_wait(s.xfull + st, (uint32_t)u & 1u, a.spin);
+          if (!ok) break;
+          fence_proxy_async();   // generic writes -> tensor-core reads
+          mbar_arrive_cluster(full0 + 8u * (uint32_t)st);
+          if (++st == a.stages) {
+            st = 0;
+            ++u;
           }
+        }
+    }
+    __syncwarp();
+  } else if (wid >= 4 && wid < 4 + kXWarps) {
+    const int g = tid - 128, chunk = g & 7, r0 = g >> 3;   // 16 bytes of rows r0 + 16 j
+    const uint32_t at = (uint32_t)r0 * 128u + (uint32_t)((chunk ^ (r0 & 7)) << 4);
+    const int width = a.cols * (F8 ? 1 : 2);
+    int st = 0, u = 0;
+    for (int tile = pair; tile < ntiles && ok; tile += pairs) {
+      const Tile t = tile_of(a, s.groups, tile, 32);
+      const int half = (t.n + 31) / 32 * 16;   // rows of this CTA
+      const uint8_t* src[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int r = rank * half + r0 + 16 * j;
+        const int row = 16 * j < half && r < t.n ? row_of(a, t.p0 + r) : -1;
+        src[j] = row < 0 ? nullptr : static_cast<const uint8_t*>(a.x) + (int64_t)row * a.x_ld * (F8 ? 1 : 2) + chunk * 16;
       }
-      for (int i = 0; i < a.nk; ++i, ++n) {
+      for (int i = 0; i < a.nk; ++i) {
         if (u > 0) ok = mbar_try_wait(s.empty + st, (uint32_t)(u - 1) & 1u) || mbar_wait(s.empty + st, (uint32_t)(u - 1) & 1u, a.spin);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
-        const uint32_t bar = smem_u32(s.full + st), dst = smem_u32(sm) + (uint32_t)st * stage + kATile;
-        if (lane == 0) mbar_expect_tx(s.full + st, (uint32_t)n16 * 128u);
-        __syncwarp();
-        if (a.index) {
+        const uint32_t dst = smem_u32(sm) + (uint32_t)st * stage + kATile + at;
+        const int left = min(max(width - i * 128 - chunk * 16, 0), 16);
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            if (4 * (lane + 32 * j) < n16) tma_gather4(dst + (uint32_t)(lane + 32 * j) * 512u, &xmap, i * kCols, row[j], bar);
-        } else if (16 * lane < n16) {
-          tma_load_2d(dst + (uint32_t)lane * 2048u, &xmap, i * kCols, t.p0 + 16 * lane, bar);
-        }
+        for (int j = 0; j < 8; ++j)
+          if (16 * j < half) {
+            const int bytes = src[j] ? left : 0;
+            cp_async16(dst + (uint32_t)j * 2048u, bytes ? src[j] + i * 128 : static_cast<const uint8_t*>(a.x), bytes);
+          }
+        cp_async_arrive(s.xfull + st);
         if (++st == a.stages) {
           st = 0;
           ++u;
         }
       }
     }
-    for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok ? kWaitClocks : a.spin);
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncwarp();
-  } else if (wid >= 4) {
-    const int quarter = wid & 3, half = (wid - 4) >> 2;
+  } else if (wid >= 4 + kXWarps) {
+    const int quarter = wid & 3, half = (wid - 4 - kXWarps) >> 2;
     const bool low = !GLU || lane < 16;   // with U: lanes of W's rows, and of U's
+    const uint32_t aempty0 = cluster_address(smem_u32(s.aempty), 0);
     int it = 0;
-    for (int tile = blockIdx.x; tile < ntiles; tile += gridDim.x, ++it) {
-      const Tile t = tile_of(a, s.groups, tile, 16);
+    for (int tile = pair; tile < ntiles; tile += pairs, ++it) {
+      const Tile t = tile_of(a, s.groups, tile, 32);
       const int buf = it & 1, use = it >> 1;
       float* factor = s.factor[buf];
       {
-        const int r = tid - 128;
+        const int r = tid - 32 * (4 + kXWarps);
         float f = 0.f;
         if (r < t.n) {
           const int row = row_of(a, t.p0 + r);
@@ -391,7 +432,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         }
         factor[r] = f;
       }
-      const int m = t.m * kRows + (GLU ? 16 * quarter + (lane & 15) : 32 * quarter + lane);
+      const int m = (2 * t.m + rank) * kRows + (GLU ? 16 * quarter + (lane & 15) : 32 * quarter + lane);
       float sw = 1.f;
       if (F8 && m < a.rows) sw = low ? __ldg(a.ws + t.e * a.w_sld + m) : __ldg(a.us + t.e * a.u_sld + m);
       asm volatile("bar.sync 1, %0;" ::"n"(kOutThreads) : "memory");   // (a warp that passes has read the factors of two tiles ago)
@@ -429,25 +470,27 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      mbar_arrive(lane == 0, s.aempty + buf);
+      if (lane == 0) mbar_arrive_cluster(aempty0 + 8u * (uint32_t)buf);
     }
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  __syncthreads();
+  // no CTA leaves while the other may still reach its shared or tensor memory
+  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
   if (!ok && a.status) atomicCAS(a.status, 0, BITSMOE_ERR_TIMEOUT);
   if (wid == 1) {
     __syncwarp();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc_pair(tmem, 512);
   }
 }
 
 // Rows of y of a tile: twice an expert's on average, so that few experts have more than one tile, each of which reads
 // the expert's matrix again; a stage of more rows leaves room for fewer stages.
 int tile_rows(int P, int E) {
-  const int most = (P + 15) / 16 * 16;
-  return std::min({256, most, std::max(32, ((int)(2ll * P / E) + 15) / 16 * 16)});
+  const int most = (int)std::min<int64_t>(256, ((int64_t)P + 31) / 32 * 32);
+  return std::min(most, (int)std::min<int64_t>(256, (2ll * P / E + 31) / 32 * 32 + 32));
 }
 
 bool on_boundaries(const void* p, int64_t ld, int64_t size, int64_t rows) {
@@ -458,32 +501,40 @@ int64_t pitch_of(int64_t ld, int64_t cols, int64_t size, int64_t rows) {   // (o
 }
 
 // Whether the tensor-core kernel takes these rows; its maps.
-bool tc_maps(const ExpertArgs& a, bool f8, CUtensorMap* wm, CUtensorMap* um, CUtensorMap* xm) {
+bool tc_maps(const ExpertArgs& a, bool f8, CUtensorMap* wm, CUtensorMap* um) {
   const int64_t es = f8 ? 1 : 2;
   if (a.x_rows < 1 || !on_boundaries(a.x, a.x_ld, es, a.x_rows)) return false;
   const int box = a.up ? 16 : 128;
   const auto matrices = [&](CUtensorMap* m, const void* p, int64_t ld, int64_t eld) {
     return on_boundaries(p, ld, es, a.rows) && make_matrices_map(m, f8, p, a.E, a.rows, a.cols, pitch_of(ld, a.cols, es, a.rows), eld * es, box);
   };
-  if (!matrices(wm, a.w, a.w_ld, a.w_eld)) return false;
-  if (a.up && !matrices(um, a.up, a.u_ld, a.u_eld)) return false;
-  return make_row_map(xm, f8, a.x, a.x_rows, a.cols, pitch_of(a.x_ld, a.cols, es, a.x_rows), a.index ? 1 : 16);
+  return matrices(wm, a.w, a.w_ld, a.w_eld) && (!a.up || matrices(um, a.up, a.u_ld, a.u_eld));
 }
 
 template <bool F8, bool GLU>
-cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um, const CUtensorMap& xm, int dev, int sms, cudaStream_t st) {
+cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um, int dev, int sms, cudaStream_t st) {
   a.N = tile_rows(a.P, a.E);
-  a.mt = (a.rows + (GLU ? 63 : 127)) / (GLU ? 64 : 128);
+  a.mt = (a.rows + (GLU ? 127 : 255)) / (GLU ? 128 : 256);
   a.nk = (a.cols + (F8 ? 127 : 63)) / (F8 ? 128 : 64);
   a.w_next = a.w_eld != 0;
   a.u_next = a.u_eld != 0;
-  a.stages = std::min(16, (int)((kTcShared - 1024 - sizeof(TcShared)) / (kATile + (size_t)a.N * 128)));
+  a.stages = std::min(kStagesMost, (int)((kTcShared - 1024 - sizeof(TcShared)) / (kATile + (size_t)a.N * 64)));
   const int64_t most = std::min<int64_t>(a.P, (int64_t)a.P / a.N + a.E) * a.mt;
   auto kern = k_expert_tc<F8, GLU>;
   const cudaError_t e = allow_shared<k_expert_tc<F8, GLU>>(dev, kTcShared);
   if (e != cudaSuccess) return e;
-  kern<<<(unsigned)std::min<int64_t>(most, sms), kTcThreads, kTcShared, st>>>(wm, um, xm, a);
-  return cudaGetLastError();
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2u * (unsigned)std::min<int64_t>(most, sms / 2));
+  cfg.blockDim = dim3(kTcThreads);
+  cfg.dynamicSmemBytes = kTcShared;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, wm, um, a);
 }
 
 int matrices_check(const bitsmoe_expert_matrices* m) {
@@ -555,11 +606,11 @@ extern "C" int bitsmoe_expert_product(const bitsmoe_expert_product_args* args, v
   a.lose = debug_skip_arrival();
   a.status = g.status;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  CUtensorMap wm, um, xm;
-  if (tc_maps(a, f8, &wm, &um, &xm)) {
+  CUtensorMap wm, um;
+  if (tc_maps(a, f8, &wm, &um)) {
     if (!a.up) um = wm;
-    e = f8 ? (a.up ? launch_tc<true, true>(a, wm, um, xm, dev, sms, st) : launch_tc<true, false>(a, wm, um, xm, dev, sms, st))
-           : (a.up ? launch_tc<false, true>(a, wm, um, xm, dev, sms, st) : launch_tc<false, false>(a, wm, um, xm, dev, sms, st));
+    e = f8 ? (a.up ? launch_tc<true, true>(a, wm, um, dev, sms, st) : launch_tc<true, false>(a, wm, um, dev, sms, st))
+           : (a.up ? launch_tc<false, true>(a, wm, um, dev, sms, st) : launch_tc<false, false>(a, wm, um, dev, sms, st));
   } else {
     e = f8 ? launch_plain<true>(a, sms, st) : launch_plain<false>(a, sms, st);
   }

@@ -30,18 +30,11 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
       : "memory");
 }
 
-// The same of a box of a row of matrices.
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+// The same of a box of a row of matrices, by a CTA of a pair (cta_group::2): `bar` may be the other's.
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
-      : "memory");
-}
-// Four rows of a matrix, wherever they are, one after the other (the map's box is one row high).
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, int x, const int (&row)[4], uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3]), "r"(bar)
       : "memory");
 }
 
@@ -54,9 +47,11 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int n) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
-// kind::f8f6f4: e4m3 x e4m3 -> f32, the rest as above (K = 32 a product).
-__host__ __device__ constexpr uint32_t idesc_e4m3(int n) {
-  return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+// The same for a pair of CTAs (M = 256: 128 rows in each one's shared and tensor memory; N columns, half of B's rows in
+// each one's shared memory), and for kind::f8f6f4, e4m3 x e4m3 -> f32 (K = 32 a product).
+template <bool F8>
+__host__ __device__ constexpr uint32_t idesc_pair(int n) {
+  return (1u << 4) | (F8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
 }
 
 // One tcgen05.mma of kind::f16 (f16 or bf16 operands, as the instruction descriptor says).
@@ -101,13 +96,45 @@ __device__ __forceinline__ void mma_f16(uint32_t one, uint32_t d_tmem, uint64_t 
       "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
       : "memory");
 }
-// The same of kind::f8f6f4.
-__device__ __forceinline__ void mma_f8(uint32_t one, uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+// The MMA of a pair of CTAs, by a converged warp of its first one.
+template <bool F8>
+__device__ __forceinline__ void mma_pair(uint32_t one, uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  if constexpr (F8)
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+        " @q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+        " @q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
+        : "memory");
+}
+// An arrival on `bar` (a cluster address: this CTA's or the other's) once the pair's MMAs issued by then are done.
+__device__ __forceinline__ void mma_commit_pair(uint32_t one, uint32_t bar) {
   asm volatile(
-      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
-      "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
+      "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+      " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar), "r"(one)
       : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_address(uint32_t saddr, uint32_t rank) {   // of the same place in CTA `rank`
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
+  return r;
+}
+// One arrival on a barrier of any CTA of the cluster.  It orders nothing for other CTAs' threads (a release at cluster scope took
+// about 1 us): what it stands for is in shared memory behind a proxy fence, or in tensor memory behind tcgen05's.
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t ncols) {   // one full warp of each CTA
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(ncols) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t tmem, uint32_t ncols) {   // one full warp of each CTA
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(ncols) : "memory");
 }
 // 512 bytes of shared memory (32 rows of 16 bytes) into 4 tensor-memory columns of each 32-lane quarter.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
