@@ -36,7 +36,8 @@ struct ExpertArgs {
   void* y;
   int y_type;
   int64_t y_ld;
-  int nk, stages;        // tensor cores: steps of 128 bytes of the columns, depth of the ring
+  int nk, stages, nbuf;  // tensor cores: steps of 128 bytes of the columns, depth of the ring, accumulators in turn
+  int splits, sps;       // CTAs that share the columns of a tile, steps of each
   int w_next, u_next;    // 1: an expert has matrices of its own (0: one stands for all)
   long long spin;
   int lose;
@@ -212,22 +213,23 @@ cudaError_t launch_plain(ExpertArgs a, int sms, cudaStream_t st) {
 }
 
 // ---------------------------------------------------------------------------
-// Rows on 16-byte boundaries: tcgen05, a pair of CTAs a tile of 256 rows of an expert's matrix (with U 128 of both) x N
-// rows of y: the matrix is the operand of many rows, so that an expert's few rows cost an MMA of few columns.  Each CTA
-// has half of both operands and the results of its 128 rows.
+// Rows on 16-byte boundaries: tcgen05.  A CTA has two tiles of 128 rows of an expert's matrix (with U 128 of each, so that
+// both products of a result are in one lane) and up to 256 rows of y: the matrix is the operand of many rows, so that an
+// expert's few rows cost an MMA of few columns.  With many rows two CTAs are a pair (cta_group::2): each brings half of the
+// rows of x for both.
 //
-// A ring of stages of 128 bytes of the columns: warp 0 brings the matrix's tile by TMA, four warps the rows of x, wherever
+// A ring of stages of 128 bytes of the columns: warp 0 brings the matrices' tiles by TMA, eight warps the rows of x, wherever
 // they are, 16 bytes a thread at a time (cp.async; TMA's gather of four rows took 63 clocks for 512 bytes); their copies arrive
-// on a barrier by themselves, and warp 2 hands the stage on.  With U, 16 rows of
-// each take turns in the tile, so that a warp's 32 lanes of the accumulator hold 16 rows of both products and one exchange
-// between lanes brings them together.  The first CTA's warp 1 issues the MMAs; eight warps of each CTA empty one
-// accumulator while the other fills.
+// on a barrier by themselves, and warp 2 hands the stage on.  Warp 1 (of a pair's first CTA) issues the MMAs; eight warps empty
+// the accumulators, two of them in turn where tensor memory holds two.  CTAs stay for all their tiles.  With few tiles the
+// columns are split over a cluster, whose CTAs add their partial tiles through distributed shared memory in rank order.
 // ---------------------------------------------------------------------------
-constexpr int kTcThreads = 512;          // warps: 0 matrices, 1 MMA, 2 rows of x that are there, 4.. rows of x, 8.. results
-constexpr int kXWarps = 4, kOutWarps = 8, kOutThreads = 32 * kOutWarps;
-constexpr int kStagesMost = 12;
-constexpr uint32_t kATile = 128 * 128;   // bytes of a stage's tile of the matrices
-constexpr int kTcShared = 227 * 1024;    // (all of an SM's, as of every kernel that allocates tensor memory)
+constexpr int kXWarps = 8, kOutWarps = 8, kOutThreads = 32 * kOutWarps;
+constexpr int kTcThreads = 32 * (4 + kXWarps + kOutWarps);   // warps: 0 matrices, 1 MMA, 2 rows of x that are there, 4.. rows of x, results
+constexpr int kStagesMost = 8;
+constexpr uint32_t kATile = 2 * 128 * 128;   // bytes of a stage's tiles of the matrices
+constexpr int kTcShared = 227 * 1024;        // (all of an SM's, as of every kernel that allocates tensor memory)
+constexpr int kXRows = 4 * kXWarps;          // rows that one pass of x's warps brings
 
 struct TcShared {
   Groups groups;
@@ -247,126 +249,150 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int by
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+__device__ __forceinline__ void cluster_sync() {   // converged warps
+  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
 
-template <bool F8, bool GLU>
+// SiLU(g) u with the fast exponential and quotient (2 units in the last place each).
+__device__ __forceinline__ float silu_fast(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
+
+template <bool F8, bool GLU, bool PAIR>
 __global__ void __launch_bounds__(kTcThreads, 1)
     k_expert_tc(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ ExpertArgs a) {
-  constexpr int kCols = F8 ? 128 : 64;   // columns of a stage
-  constexpr int kRows = GLU ? 64 : 128;  // rows of y's width that a CTA covers
+  constexpr int kCols = F8 ? 128 : 64;         // columns of a stage
+  constexpr int kRows = GLU ? 128 : 256;       // rows of y's width that a CTA covers
+  constexpr int kUnit = PAIR ? 32 : 16;        // rows of y of a tile are a multiple of it, as the MMA takes them
+  constexpr int kBoth = PAIR ? 2 : 1;          // CTAs that share a tile
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t stage = kATile + (uint32_t)a.N * 64;
-  TcShared& s = *reinterpret_cast<TcShared*>(sm + (size_t)a.stages * stage);
+  const uint32_t stage = kATile + (uint32_t)(a.N / kBoth) * 128;
+  float* red = reinterpret_cast<float*>(sm + (size_t)a.stages * stage);   // split: [2][N][128]
+  TcShared& s = *reinterpret_cast<TcShared*>(reinterpret_cast<uint8_t*>(red) + (a.splits > 1 ? (size_t)a.N * 1024 : 0));
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  // CTAs of a tile: a pair, or the splits of the columns
+  const int group = PAIR ? 2 : a.splits, rank = (int)(blockIdx.x % (unsigned)group), first = (int)(blockIdx.x / (unsigned)group);
+  const int step = (int)(gridDim.x / (unsigned)group), half = PAIR ? rank : 0;
+  const int k0 = PAIR ? 0 : rank * a.sps, nk = max(0, min(a.sps, a.nk - k0));
   if (tid == 0) {
     prefetch_map(&wmap);
     if (GLU) prefetch_map(&umap);
     for (int i = 0; i < a.stages; ++i) {
-      mbar_init_n(s.full + i, 3);   // (the first CTA's: the matrices' bytes of both, x's rows of each)
+      mbar_init_n(s.full + i, 1 + kBoth);   // (a pair's first CTA's, for both: the matrices' bytes, x's rows of each)
       mbar_init_n(s.xfull + i, 32 * kXWarps);
       mbar_init_n(s.empty + i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init_n(s.afull + i, 1);
-      mbar_init_n(s.aempty + i, 2 * kOutWarps);
+      mbar_init_n(s.aempty + i, kBoth * kOutWarps);
     }
     mbar_init_n(&s.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (wid == 1) tmem_alloc_pair(&s.slot, 512);
+  if (wid == 1) {
+    if constexpr (PAIR) tmem_alloc_pair(&s.slot, 512);
+    else tmem_alloc(&s.slot, 512);
+  }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  read_groups<kTcThreads>(a, s.groups);
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+  read_groups<kTcThreads>(a, s.groups);   // (with barriers of the block)
+  if constexpr (PAIR) {
+    __syncwarp();
+    cluster_sync();
+  }
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, s.slot, 0);
   const int ntiles = s.groups.tiles[a.E] * a.mt;
+  const auto at0 = [&](const void* p) {   // the same place in a pair's first CTA, else here
+    return PAIR ? cluster_address(smem_u32(p), 0) : smem_u32(p);
+  };
   bool ok = true;
 
   if (wid == 0) {
     if (lane == 0) {
-      const uint32_t full0 = cluster_address(smem_u32(s.full), 0);
+      const uint32_t full0 = at0(s.full);
       int st = 0, u = 0, n = 0;
-      for (int tile = pair; tile < ntiles && ok; tile += pairs) {
-        const Tile t = tile_of(a, s.groups, tile, 32);
-        const int m0 = (2 * t.m + rank) * kRows;
-        for (int i = 0; i < a.nk; ++i, ++n) {
+      for (int tile = first; tile < ntiles && ok; tile += step) {
+        const Tile t = tile_of(a, s.groups, tile, kUnit);
+        const int m0 = (kBoth * t.m + half) * kRows;
+        for (int i = 0; i < nk; ++i, ++n) {
           if (u > 0) ok = mbar_wait(s.empty + st, (uint32_t)(u - 1) & 1u, a.spin);
           if (!ok) break;
           const uint32_t bar = full0 + 8u * (uint32_t)st, dst = smem_u32(sm) + (uint32_t)st * stage;
-          if (rank == 0) mbar_expect_tx(s.full + st, 2 * kATile);   // both CTAs' tiles
-          if constexpr (GLU) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              tma_load_3d_pair(dst + q * 4096, &wmap, i * kCols, m0 + 16 * q, t.e * a.w_next, bar);
-              tma_load_3d_pair(dst + q * 4096 + 2048, &umap, i * kCols, m0 + 16 * q, t.e * a.u_next, bar);
-            }
-          } else {
-            tma_load_3d_pair(dst, &wmap, i * kCols, m0, t.e * a.w_next, bar);
-          }
+          if (half == 0) mbar_expect_tx(s.full + st, kBoth * kATile);   // of both CTAs
+          tma_load_3d<PAIR>(dst, &wmap, (k0 + i) * kCols, m0, t.e * a.w_next, bar);   // 256 rows, with U 128
+          if (GLU) tma_load_3d<PAIR>(dst + kATile / 2, &umap, (k0 + i) * kCols, m0, t.e * a.u_next, bar);
           if (++st == a.stages) {
             st = 0;
             ++u;
           }
         }
       }
-      // both CTAs' copies in flight (after a timeout an arrival of the phase may be missing)
-      if (rank == 0)
+      // copies in flight, of both CTAs (after a timeout an arrival of the phase may be missing)
+      if (half == 0)
         for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok ? kWaitClocks : a.spin);
     }
     __syncwarp();
-  } else if (wid == 1 && rank == 0) {
+  } else if (wid == 1 && half == 0) {
     const uint32_t one = elect_one();
     const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(sm) + kATile);
-    uint32_t empty[2], afull[2];   // both CTAs'
-    for (uint32_t r = 0; r < 2; ++r) {
-      empty[r] = cluster_address(smem_u32(s.empty), r);
-      afull[r] = cluster_address(smem_u32(s.afull), r);
+    uint32_t empty[kBoth], afull[kBoth];
+#pragma unroll
+    for (int r = 0; r < kBoth; ++r) {
+      empty[r] = PAIR ? cluster_address(smem_u32(s.empty), (uint32_t)r) : smem_u32(s.empty);
+      afull[r] = PAIR ? cluster_address(smem_u32(s.afull), (uint32_t)r) : smem_u32(s.afull);
     }
-    int st = 0, u = 0, it = 0;
-    for (int tile = pair; tile < ntiles && ok; tile += pairs, ++it) {
-      const int n32 = (tile_of(a, s.groups, tile, 32).n + 31) / 32 * 32;
-      const uint32_t idesc = idesc_pair<F8>(n32);
-      const int buf = it & 1, use = it >> 1;
+    int st = 0, u = 0, buf = 0, use = 0, it = 0;
+    for (int tile = first; tile < ntiles && ok; tile += step, ++it) {
+      const int n = (tile_of(a, s.groups, tile, kUnit).n + kUnit - 1) / kUnit * kUnit;
+      const uint32_t idesc = idesc_of<F8, PAIR>(n);
       if (use > 0) ok = mbar_wait(s.aempty + buf, (uint32_t)(use - 1) & 1u, a.spin);
       ok = __all_sync(0xFFFFFFFFu, ok);
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t acc = tmem + (uint32_t)(buf * 256);
-      for (int i = 0; i < a.nk; ++i) {
+      const uint32_t acc = tmem + (uint32_t)(buf * 2 * a.N);
+      for (int i = 0; i < nk; ++i) {
         ok = mbar_try_wait(s.full + st, (uint32_t)u & 1u) || mbar_wait(s.full + st, (uint32_t)u & 1u, a.spin);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint64_t o = (uint64_t)((uint32_t)st * (stage >> 4));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mma_pair<F8>(one, acc, da + o + 2 * k, db + o + 2 * k, idesc, (uint32_t)(i | k));
-        if (!(a.lose && (i | it | pair) == 0)) {
-          mma_commit_pair(one, empty[0] + 8u * (uint32_t)st);
-          mma_commit_pair(one, empty[1] + 8u * (uint32_t)st);
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            mma_of<F8, PAIR>(one, acc + (uint32_t)(h * a.N), da + o + h * (kATile >> 5) + 2 * k, db + o + 2 * k, idesc, (uint32_t)(i | k));
+        if (!(a.lose && (i | it | (int)blockIdx.x) == 0))
+#pragma unroll
+          for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, empty[r] + 8u * (uint32_t)st);
         if (++st == a.stages) {
           st = 0;
           ++u;
         }
       }
       if (!ok) break;
-      mma_commit_pair(one, afull[0] + 8u * (uint32_t)buf);
-      mma_commit_pair(one, afull[1] + 8u * (uint32_t)buf);
+#pragma unroll
+      for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, afull[r] + 8u * (uint32_t)buf);
+      if (++buf == a.nbuf) {
+        buf = 0;
+        ++use;
+      }
     }
     if (!ok) {
-      mma_commit_pair(one, cluster_address(smem_u32(&s.drained), 0));
+      mma_commit_at<PAIR>(one, smem_u32(&s.drained));
       mbar_wait(&s.drained, 0u);
     }
     __syncwarp();
   } else if (wid == 2) {
     if (lane == 0) {
-      const uint32_t full0 = cluster_address(smem_u32(s.full), 0);
+      const uint32_t full0 = at0(s.full);
       int st = 0, u = 0;
-      for (int tile = pair; tile < ntiles && ok; tile += pairs)
-        for (int i = 0; i < a.nk; ++i) {
+      for (int tile = first; tile < ntiles && ok; tile += step)
+        for (int i = 0; i < nk; ++i) {
           ok = mbar_wait(s.xfull + st, (uint32_t)u & 1u, a.spin);
           if (!ok) break;
           fence_proxy_async();   // generic writes -> tensor-core reads
@@ -379,31 +405,32 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     }
     __syncwarp();
   } else if (wid >= 4 && wid < 4 + kXWarps) {
-    const int g = tid - 128, chunk = g & 7, r0 = g >> 3;   // 16 bytes of rows r0 + 16 j
+    const int g = tid - 128, chunk = g & 7, r0 = g >> 3;   // 16 bytes of rows r0 + kXRows j
     const uint32_t at = (uint32_t)r0 * 128u + (uint32_t)((chunk ^ (r0 & 7)) << 4);
     const int width = a.cols * (F8 ? 1 : 2);
+    constexpr int kPasses = 256 / kBoth / kXRows;
     int st = 0, u = 0;
-    for (int tile = pair; tile < ntiles && ok; tile += pairs) {
-      const Tile t = tile_of(a, s.groups, tile, 32);
-      const int half = (t.n + 31) / 32 * 16;   // rows of this CTA
-      const uint8_t* src[8];
+    for (int tile = first; tile < ntiles && ok; tile += step) {
+      const Tile t = tile_of(a, s.groups, tile, kUnit);
+      const int mine = (t.n + kUnit - 1) / kUnit * kUnit / kBoth;   // rows of this CTA
+      const uint8_t* src[kPasses];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int r = rank * half + r0 + 16 * j;
-        const int row = 16 * j < half && r < t.n ? row_of(a, t.p0 + r) : -1;
+      for (int j = 0; j < kPasses; ++j) {
+        const int r = r0 + kXRows * j, q = half * mine + r;
+        const int row = r < mine && q < t.n ? row_of(a, t.p0 + q) : -1;
         src[j] = row < 0 ? nullptr : static_cast<const uint8_t*>(a.x) + (int64_t)row * a.x_ld * (F8 ? 1 : 2) + chunk * 16;
       }
-      for (int i = 0; i < a.nk; ++i) {
+      for (int i = 0; i < nk; ++i) {
         if (u > 0) ok = mbar_try_wait(s.empty + st, (uint32_t)(u - 1) & 1u) || mbar_wait(s.empty + st, (uint32_t)(u - 1) & 1u, a.spin);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
         const uint32_t dst = smem_u32(sm) + (uint32_t)st * stage + kATile + at;
-        const int left = min(max(width - i * 128 - chunk * 16, 0), 16);
+        const int b = (k0 + i) * 128, left = min(max(width - b - chunk * 16, 0), 16);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (16 * j < half) {
+        for (int j = 0; j < kPasses; ++j)
+          if (r0 + kXRows * j < mine) {
             const int bytes = src[j] ? left : 0;
-            cp_async16(dst + (uint32_t)j * 2048u, bytes ? src[j] + i * 128 : static_cast<const uint8_t*>(a.x), bytes);
+            cp_async16(dst + (uint32_t)j * (kXRows * 128u), bytes ? src[j] + b : static_cast<const uint8_t*>(a.x), bytes);
           }
         cp_async_arrive(s.xfull + st);
         if (++st == a.stages) {
@@ -415,14 +442,12 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncwarp();
   } else if (wid >= 4 + kXWarps) {
-    const int quarter = wid & 3, half = (wid - 4 - kXWarps) >> 2;
-    const bool low = !GLU || lane < 16;   // with U: lanes of W's rows, and of U's
-    const uint32_t aempty0 = cluster_address(smem_u32(s.aempty), 0);
-    int it = 0;
-    for (int tile = pair; tile < ntiles; tile += pairs, ++it) {
-      const Tile t = tile_of(a, s.groups, tile, 32);
-      const int buf = it & 1, use = it >> 1;
-      float* factor = s.factor[buf];
+    const int quarter = wid & 3, side = (wid - 4 - kXWarps) >> 2;
+    const uint32_t aempty0 = at0(s.aempty);
+    int buf = 0, use = 0, it = 0;
+    for (int tile = first; tile < ntiles; tile += step, ++it) {
+      const Tile t = tile_of(a, s.groups, tile, kUnit);
+      float* factor = s.factor[it & 1];
       {
         const int r = tid - 32 * (4 + kXWarps);
         float f = 0.f;
@@ -432,57 +457,102 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         }
         factor[r] = f;
       }
-      const int m = (2 * t.m + rank) * kRows + (GLU ? 16 * quarter + (lane & 15) : 32 * quarter + lane);
-      float sw = 1.f;
-      if (F8 && m < a.rows) sw = low ? __ldg(a.ws + t.e * a.w_sld + m) : __ldg(a.us + t.e * a.u_sld + m);
+      const int r = 32 * quarter + lane, m = (kBoth * t.m + half) * kRows + r;   // and, without U, row m + 128
+      const bool in0 = m < a.rows, in1 = GLU ? in0 : m + 128 < a.rows;
+      float s0 = 1.f, s1 = 1.f;
+      if (F8) {
+        if (in0) s0 = __ldg(a.ws + t.e * a.w_sld + m);
+        if (in1) s1 = GLU ? __ldg(a.us + t.e * a.u_sld + m) : __ldg(a.ws + t.e * a.w_sld + m + 128);
+      }
       asm volatile("bar.sync 1, %0;" ::"n"(kOutThreads) : "memory");   // (a warp that passes has read the factors of two tiles ago)
       if (ok) ok = mbar_wait_idle(s.afull + buf, (uint32_t)use & 1u, a.spin);
       ok = __all_sync(0xFFFFFFFFu, ok);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t tl = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(buf * 256);
-      for (int c0 = 16 * half; c0 < t.n; c0 += 32) {
-        uint32_t v[16];
-        if (ok) {
-          tmem_ld16(tl + (uint32_t)c0, v);
+      const uint32_t tl = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(buf * 2 * a.N);
+      for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
+        uint32_t v[2][16];
+        if (!ok) {
+#pragma unroll
+          for (int q = 0; q < 16; ++q) v[0][q] = v[1][q] = kLost;
+        } else if (nk > 0) {
+          tmem_ld16(tl + (uint32_t)c0, v[0]);
+          tmem_ld16(tl + (uint32_t)(a.N + c0), v[1]);
         } else {
 #pragma unroll
-          for (int q = 0; q < 16; ++q) v[q] = kLost;
+          for (int q = 0; q < 16; ++q) v[0][q] = v[1][q] = 0u;
+        }
+        if (!PAIR && a.splits > 1) {
+#pragma unroll
+          for (int q = 0; q < 16; ++q) {
+            red[(c0 + q) * 128 + r] = __uint_as_float(v[0][q]);
+            red[(a.N + c0 + q) * 128 + r] = __uint_as_float(v[1][q]);
+          }
+          continue;
         }
         float f[16];
 #pragma unroll
         for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(f + 4 * q) = *reinterpret_cast<const float4*>(factor + c0 + 4 * q);
-#pragma unroll
-        for (int q = 0; q < 16; ++q) f[q] *= F8 ? __uint_as_float(v[q]) * sw : __uint_as_float(v[q]);
         const int64_t at = (int64_t)(t.p0 + c0) * a.y_ld + m;
-        if constexpr (GLU) {
 #pragma unroll
-          for (int q = 0; q < 16; q += 2) {   // lanes of W's rows take the even columns, those of U's the odd ones
-            const float r = __shfl_xor_sync(0xFFFFFFFFu, low ? f[q + 1] : f[q], 16);
-            const float g = low ? f[q] : r, w = low ? r : f[q + 1];
-            const int c = low ? q : q + 1;
-            if (m < a.rows && c0 + c < t.n) store_y(a.y, a.y_type, at + c * a.y_ld, silu_mul(g, w));
+        for (int q = 0; q < 16; ++q) {
+          const float v0 = __uint_as_float(v[0][q]) * (F8 ? s0 * f[q] : f[q]), v1 = __uint_as_float(v[1][q]) * (F8 ? s1 * f[q] : f[q]);
+          if (c0 + q >= t.n) continue;
+          if constexpr (GLU) {
+            if (in0) store_y(a.y, a.y_type, at + q * a.y_ld, silu_fast(v0, v1));
+          } else {
+            if (in0) store_y(a.y, a.y_type, at + q * a.y_ld, v0);
+            if (in1) store_y(a.y, a.y_type, at + q * a.y_ld + 128, v1);
           }
-        } else if (m < a.rows) {
-#pragma unroll
-          for (int q = 0; q < 16; ++q)
-            if (c0 + q < t.n) store_y(a.y, a.y_type, at + q * a.y_ld, f[q]);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(aempty0 + 8u * (uint32_t)buf);
+      if (++buf == a.nbuf) {
+        buf = 0;
+        ++use;
+      }
     }
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  // no CTA leaves while the other may still reach its shared or tensor memory
-  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+  // no CTA leaves while another may still reach its shared or tensor memory
+  if (PAIR || a.splits > 1) cluster_sync();
+  else __syncthreads();
+  if (!PAIR && a.splits > 1) {
+    if (first < ntiles) {
+      // every CTA has its part of the tile in shared memory; each sums and stores its share of the results
+      const Tile t = tile_of(a, s.groups, first, kUnit);
+      for (int i = rank * kTcThreads + tid; i < t.n * 128; i += a.splits * kTcThreads) {
+        const int c = i >> 7, r = i & 127, m = t.m * kRows + r;
+        float v[2] = {0.f, 0.f};
+        for (int q = 0; q < a.splits; ++q)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) v[h] += ld_cluster(cluster_address(smem_u32(red + (h * a.N + c) * 128 + r), (uint32_t)q));
+        const float f = s.factor[0][c];
+        const int64_t at = (int64_t)(t.p0 + c) * a.y_ld + m;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int mh = GLU ? m : m + 128 * h;
+          if (mh < a.rows) v[h] *= F8 ? f * __ldg((GLU && h ? a.us + t.e * a.u_sld : a.ws + t.e * a.w_sld) + mh) : f;
+        }
+        if constexpr (GLU) {
+          if (m < a.rows) store_y(a.y, a.y_type, at, silu_fast(v[0], v[1]));
+        } else {
+          if (m < a.rows) store_y(a.y, a.y_type, at, v[0]);
+          if (m + 128 < a.rows) store_y(a.y, a.y_type, at + 128, v[1]);
+        }
+      }
+    }
+    __syncwarp();
+    cluster_sync();
+  }
   if (!ok && a.status) atomicCAS(a.status, 0, BITSMOE_ERR_TIMEOUT);
   if (wid == 1) {
     __syncwarp();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    tmem_dealloc_pair(tmem, 512);
+    if constexpr (PAIR) tmem_dealloc_pair(tmem, 512);
+    else tmem_dealloc(tmem, 512);
   }
 }
 
@@ -504,37 +574,50 @@ int64_t pitch_of(int64_t ld, int64_t cols, int64_t size, int64_t rows) {   // (o
 bool tc_maps(const ExpertArgs& a, bool f8, CUtensorMap* wm, CUtensorMap* um) {
   const int64_t es = f8 ? 1 : 2;
   if (a.x_rows < 1 || !on_boundaries(a.x, a.x_ld, es, a.x_rows)) return false;
-  const int box = a.up ? 16 : 128;
+  const int box = a.up ? 128 : 256;
   const auto matrices = [&](CUtensorMap* m, const void* p, int64_t ld, int64_t eld) {
     return on_boundaries(p, ld, es, a.rows) && make_matrices_map(m, f8, p, a.E, a.rows, a.cols, pitch_of(ld, a.cols, es, a.rows), eld * es, box);
   };
   return matrices(wm, a.w, a.w_ld, a.w_eld) && (!a.up || matrices(um, a.up, a.u_ld, a.u_eld));
 }
 
-template <bool F8, bool GLU>
-cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um, int dev, int sms, cudaStream_t st) {
-  a.N = tile_rows(a.P, a.E);
-  a.mt = (a.rows + (GLU ? 127 : 255)) / (GLU ? 128 : 256);
-  a.nk = (a.cols + (F8 ? 127 : 63)) / (F8 ? 128 : 64);
-  a.w_next = a.w_eld != 0;
-  a.u_next = a.u_eld != 0;
-  a.stages = std::min(kStagesMost, (int)((kTcShared - 1024 - sizeof(TcShared)) / (kATile + (size_t)a.N * 64)));
-  const int64_t most = std::min<int64_t>(a.P, (int64_t)a.P / a.N + a.E) * a.mt;
-  auto kern = k_expert_tc<F8, GLU>;
-  const cudaError_t e = allow_shared<k_expert_tc<F8, GLU>>(dev, kTcShared);
+template <bool F8, bool GLU, bool PAIR>
+cudaError_t launch_tc_as(const ExpertArgs& a, const CUtensorMap& wm, const CUtensorMap& um, int64_t groups, int dev, cudaStream_t st) {
+  auto kern = k_expert_tc<F8, GLU, PAIR>;
+  const cudaError_t e = allow_shared<k_expert_tc<F8, GLU, PAIR>>(dev, kTcShared);
   if (e != cudaSuccess) return e;
+  const unsigned size = PAIR ? 2u : (unsigned)a.splits;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.x = size;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2u * (unsigned)std::min<int64_t>(most, sms / 2));
+  cfg.gridDim = dim3(size * (unsigned)groups);
   cfg.blockDim = dim3(kTcThreads);
   cfg.dynamicSmemBytes = kTcShared;
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = size > 1 ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kern, wm, um, a);
+}
+
+template <bool F8, bool GLU>
+cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um, int dev, int sms, cudaStream_t st) {
+  a.N = tile_rows(a.P, a.E);
+  const bool pair = a.N > 64;
+  const int rows = (GLU ? 128 : 256) * (pair ? 2 : 1);
+  a.mt = (a.rows + rows - 1) / rows;
+  a.nk = (a.cols + (F8 ? 127 : 63)) / (F8 ? 128 : 64);
+  a.w_next = a.w_eld != 0;
+  a.u_next = a.u_eld != 0;
+  a.nbuf = 4 * a.N <= 512 ? 2 : 1;
+  const int64_t most = std::min<int64_t>(a.P, (int64_t)a.P / a.N + a.E) * a.mt;   // tiles at most
+  a.splits = pair ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({8, sms / most, a.nk / 2}));
+  a.sps = (a.nk + a.splits - 1) / a.splits;
+  const size_t room = kTcShared - 1024 - sizeof(TcShared) - (a.splits > 1 ? (size_t)a.N * 1024 : 0);
+  a.stages = std::min(kStagesMost, (int)(room / (kATile + (size_t)a.N * (pair ? 64 : 128))));
+  if (pair) return launch_tc_as<F8, GLU, true>(a, wm, um, std::min<int64_t>(most, sms / 2), dev, st);
+  return launch_tc_as<F8, GLU, false>(a, wm, um, std::min<int64_t>(most, sms / a.splits), dev, st);
 }
 
 int matrices_check(const bitsmoe_expert_matrices* m) {

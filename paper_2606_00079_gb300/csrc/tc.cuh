@@ -30,12 +30,19 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
       : "memory");
 }
 
-// The same of a box of a row of matrices, by a CTA of a pair (cta_group::2): `bar` may be the other's.
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
-      : "memory");
+// The same of a box of a row of matrices; PAIR: by a CTA of a pair (cta_group::2), `bar` may be the other's.
+template <bool PAIR>
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  if constexpr (PAIR)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
 }
 
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
@@ -47,11 +54,11 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int n) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
-// The same for a pair of CTAs (M = 256: 128 rows in each one's shared and tensor memory; N columns, half of B's rows in
-// each one's shared memory), and for kind::f8f6f4, e4m3 x e4m3 -> f32 (K = 32 a product).
-template <bool F8>
-__host__ __device__ constexpr uint32_t idesc_pair(int n) {
-  return (1u << 4) | (F8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
+// The same for kind::f8f6f4 (F8: e4m3 x e4m3 -> f32, K = 32 a product), and for a pair of CTAs (PAIR: M = 256, 128 rows in each
+// one's shared and tensor memory; N columns, half of B's rows in each one's shared memory).
+template <bool F8, bool PAIR>
+__host__ __device__ constexpr uint32_t idesc_of(int n) {
+  return (1u << 4) | (F8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
 }
 
 // One tcgen05.mma of kind::f16 (f16 or bf16 operands, as the instruction descriptor says).
@@ -96,28 +103,47 @@ __device__ __forceinline__ void mma_f16(uint32_t one, uint32_t d_tmem, uint64_t 
       "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
       : "memory");
 }
-// The MMA of a pair of CTAs, by a converged warp of its first one.
-template <bool F8>
-__device__ __forceinline__ void mma_pair(uint32_t one, uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  if constexpr (F8)
+// The same of either kind and of a pair of CTAs (by a warp of its first one).
+template <bool F8, bool PAIR>
+__device__ __forceinline__ void mma_of(uint32_t one, uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  if constexpr (F8 && PAIR)
     asm volatile(
         "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
         " @q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
         "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
         : "memory");
-  else
+  else if constexpr (F8)
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+        " @q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
+        : "memory");
+  else if constexpr (PAIR)
     asm volatile(
         "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
         " @q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
         "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
         : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
+        : "memory");
 }
-// An arrival on `bar` (a cluster address: this CTA's or the other's) once the pair's MMAs issued by then are done.
-__device__ __forceinline__ void mma_commit_pair(uint32_t one, uint32_t bar) {
-  asm volatile(
-      "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
-      " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar), "r"(one)
-      : "memory");
+// An arrival on `bar` (a cluster address: this CTA's or, of a pair, the other's) once the MMAs issued by then are done.
+template <bool PAIR>
+__device__ __forceinline__ void mma_commit_at(uint32_t one, uint32_t bar) {
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+        " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar), "r"(one)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+        " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar), "r"(one)
+        : "memory");
 }
 __device__ __forceinline__ uint32_t cluster_address(uint32_t saddr, uint32_t rank) {   // of the same place in CTA `rank`
   uint32_t r;
