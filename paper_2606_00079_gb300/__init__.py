@@ -29,6 +29,7 @@ ERR_CODE = {v: k for k, v in ERR.items()}
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _SZ = ctypes.c_size_t
+_addressof = ctypes.addressof
 
 
 class _LayerHost(ctypes.Structure):
@@ -68,7 +69,7 @@ class _ExpertMatrices(ctypes.Structure):
 
 
 class _ExpertProductArgs(ctypes.Structure):
-    _fields_ = [("w", ctypes.POINTER(_ExpertMatrices)), ("up", ctypes.POINTER(_ExpertMatrices)), ("x", _P),
+    _fields_ = [("w", _P), ("up", _P), ("x", _P),
                 ("x_scales", _P), ("x_ld", ctypes.c_int64), ("x_rows", ctypes.c_int32), ("P", ctypes.c_int32),
                 ("offsets", _P), ("index", _P), ("fan", ctypes.c_int32), ("y_type", ctypes.c_int32), ("y", _P),
                 ("y_ld", ctypes.c_int64), ("status", _P)]
@@ -906,7 +907,10 @@ def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: 
             _refuse(where, "x in 8 bits is asked for but pre_norm is off")
         if x is None:
             x = Rowscale.empty((T, D), dev)
-        x_type, x_ld, x_ptr = _E4M3, _rowscale_rows(where, "x", x, T, D, dev), x.codes.data_ptr()
+            x_ld = x._c.ld
+        else:
+            x_ld = _rowscale_rows(where, "x", x, T, D, dev)
+        x_type, x_ptr = _E4M3, x.codes.data_ptr()
     elif x is not None:
         if not pre_norm:
             _refuse(where, "x is given but pre_norm is off")
@@ -933,7 +937,7 @@ class Rowscale:
     """Rows in 8 bits on the device: `codes` (torch.float8_e4m3fn, rows x cols, or experts x rows x cols with dense
     rows) and `scales` (float32, one for each row); value = code * scale, see bitsmoe_rowscale in include/bitsmoe.h."""
 
-    __slots__ = ("codes", "scales")
+    __slots__ = ("_codes", "_scales", "_c")   # _c: what the library reads, formed when it is first needed
 
     def __init__(self, codes, scales):
         torch = _torch or _load_torch()
@@ -943,30 +947,42 @@ class Rowscale:
             _refuse("Rowscale", f"scales must be float32 on {codes.device}")
         if scales.shape != codes.shape[:-1]:
             _refuse("Rowscale", f"scales have shape {tuple(scales.shape)}, codes {tuple(codes.shape)}", "SHAPE")
-        if scales.dim() and scales.shape[-1] > 1 and scales.stride(-1) != 1:
+        if scales.shape[-1] > 1 and scales.stride(-1) != 1:
             _refuse("Rowscale", "scales must be dense along the rows")
-        self.codes, self.scales = codes, scales
+        self._codes, self._scales, self._c = codes, scales, None
 
     @classmethod
     def empty(cls, shape, device=None) -> "Rowscale":
         """Uninitialised rows on a pitch of a multiple of 16 bytes."""
         torch = _torch or _load_torch()
         *rows, cols = shape
+        if len(rows) not in (1, 2) or cols < 1 or min(rows) < 0:
+            _refuse("Rowscale.empty", f"shape {tuple(shape)}")
         dev = device if device is not None else torch.cuda.current_device()
-        pitch = (cols + 15) // 16 * 16
+        pitch = (cols + 15) & ~15
         codes = torch.empty((*rows, pitch), dtype=torch.float8_e4m3fn, device=dev)
         self = cls.__new__(cls)
-        self.codes = codes if pitch == cols else codes[..., :cols]
-        self.scales = torch.empty(rows, dtype=torch.float32, device=dev)
+        self._codes = codes if pitch == cols else codes[..., :cols]
+        self._scales = scales = torch.empty(rows, dtype=torch.float32, device=dev)
+        n = rows[0] if len(rows) == 1 else rows[0] * rows[1]
+        self._c = _Rowscale(n, cols, pitch, codes.data_ptr(), scales.data_ptr()) if n <= _MAX_ROWS >= cols else None
         return self
 
     @property
+    def codes(self):
+        return self._codes
+
+    @property
+    def scales(self):
+        return self._scales
+
+    @property
     def shape(self):
-        return self.codes.shape
+        return self._codes.shape
 
     @property
     def device(self):
-        return self.codes.device
+        return self._codes.device
 
 
 def _flat(where: str, name: str, x):
@@ -991,11 +1007,13 @@ def _rowscale_rows(where: str, name: str, q: Rowscale, rows=None, cols=None, dev
 
 def _rowscale_c(where: str, q: Rowscale):
     """The library's view of a Rowscale (experts' rows one after the other)."""
-    codes = _flat(where, "codes", q.codes)
-    ld = _rows(where, "codes", codes)
-    if not q.scales.is_contiguous():
-        _refuse(where, "scales must be dense")
-    return _Rowscale(codes.shape[0], codes.shape[1], ld, codes.data_ptr(), q.scales.data_ptr())
+    if q._c is None:
+        codes = _flat(where, "codes", q.codes)
+        ld = _rows(where, "codes", codes)
+        if not q.scales.is_contiguous():
+            _refuse(where, "scales must be dense")
+        q._c = _Rowscale(codes.shape[0], codes.shape[1], ld, codes.data_ptr(), q.scales.data_ptr())
+    return q._c
 
 
 def rowscale_quantize(x, out: Optional[Rowscale] = None, stream=None) -> Rowscale:
@@ -1005,7 +1023,7 @@ def rowscale_quantize(x, out: Optional[Rowscale] = None, stream=None) -> Rowscal
     where = "rowscale_quantize"
     dev = x.device
     ty = _dense_type(where, "x", x.dtype)
-    flat = _flat(where, "x", x)
+    flat = x if x.dim() == 2 else _flat(where, "x", x)
     ld = _rows(where, "x", flat)
     if stream is not None or _current() != dev.index:
         with _elsewhere(where, dev, stream):
@@ -1014,8 +1032,9 @@ def rowscale_quantize(x, out: Optional[Rowscale] = None, stream=None) -> Rowscal
         out = Rowscale.empty(x.shape, dev)
     elif out.shape != x.shape or out.device != dev:
         _refuse(where, "out has another shape or device", "SHAPE")
-    _check(_lib().bitsmoe_rowscale_quantize(flat.data_ptr(), ty, ld, _rowscale_c(where, out), _raw_stream(dev.index)),
-           "bitsmoe_rowscale_quantize")
+    rc = _lib().bitsmoe_rowscale_quantize(flat.data_ptr(), ty, ld, out._c or _rowscale_c(where, out), _raw_stream(dev.index))
+    if rc:
+        _check(rc, "bitsmoe_rowscale_quantize")
     return out
 
 
@@ -1029,14 +1048,18 @@ def rowscale_dequantize(q: Rowscale, dtype=None, out=None, stream=None):
     if stream is not None or _current() != dev.index:
         with _elsewhere(where, dev, stream):
             return rowscale_dequantize(q, dtype, out)
+    c = q._c or _rowscale_c(where, q)
     if out is None:
-        out = torch.empty(q.shape, dtype=dtype if dtype is not None else torch.float32, device=dev)
+        out, ld = torch.empty(q.codes.shape, dtype=dtype if dtype is not None else torch.float32, device=dev), c.cols
+        ptr = out.data_ptr()
     elif out.shape != q.shape:
         _refuse(where, f"out has shape {tuple(out.shape)}, expected {tuple(q.shape)}", "SHAPE")
-    flat = _flat(where, "out", out)
-    ld = _rows(where, "out", flat, None, None, dev)
-    _check(_lib().bitsmoe_rowscale_dequantize(_rowscale_c(where, q), flat.data_ptr(), _dense_type(where, "out", out.dtype),
-                                              ld, _raw_stream(dev.index)), "bitsmoe_rowscale_dequantize")
+    else:
+        flat = _flat(where, "out", out)
+        ld, ptr = _rows(where, "out", flat, None, None, dev), flat.data_ptr()
+    rc = _lib().bitsmoe_rowscale_dequantize(c, ptr, _dense_type(where, "out", out.dtype), ld, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "bitsmoe_rowscale_dequantize")
     return out
 
 
@@ -1048,6 +1071,9 @@ class Routing(NamedTuple):
     offsets: object
     pairs: object
     places: object
+
+
+_ROUTE_WS = {}   # (T, experts, top_k) -> bytes of the workspace
 
 
 def route(logits, top_k: int, renormalize: bool = True, stream=None) -> Routing:
@@ -1064,7 +1090,11 @@ def route(logits, top_k: int, renormalize: bool = True, stream=None) -> Routing:
     T, E = logits.shape
     if not 1 <= top_k <= E:
         _refuse(where, f"top_k is {top_k} of {E} experts")
-    nws = int(_lib().bitsmoe_route_workspace_bytes(T, E, top_k))
+    nws = _ROUTE_WS.get((T, E, top_k))
+    if nws is None:
+        if len(_ROUTE_WS) > 4096:
+            _ROUTE_WS.clear()
+        nws = _ROUTE_WS[T, E, top_k] = int(_lib().bitsmoe_route_workspace_bytes(T, E, top_k))
     i32 = torch.int32
     experts = torch.empty((T, top_k), dtype=i32, device=dev)
     places = torch.empty((T, top_k), dtype=i32, device=dev)
@@ -1072,9 +1102,11 @@ def route(logits, top_k: int, renormalize: bool = True, stream=None) -> Routing:
     offsets = torch.empty(E + 1, dtype=i32, device=dev)
     weights = torch.empty((T, top_k), dtype=torch.float32, device=dev)
     ws = torch.empty(nws, dtype=torch.uint8, device=dev) if nws else None
-    _check(_lib().bitsmoe_route(logits.data_ptr(), ld, T, E, top_k, 1 if renormalize else 0, experts.data_ptr(),
-                                weights.data_ptr(), offsets.data_ptr(), pairs.data_ptr(), places.data_ptr(),
-                                ws.data_ptr() if nws else None, nws, _raw_stream(dev.index)), "bitsmoe_route")
+    rc = _lib().bitsmoe_route(logits.data_ptr(), ld, T, E, top_k, 1 if renormalize else 0, experts.data_ptr(),
+                              weights.data_ptr(), offsets.data_ptr(), pairs.data_ptr(), places.data_ptr(),
+                              ws.data_ptr() if nws else None, nws, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "bitsmoe_route")
     return Routing(experts, weights, offsets, pairs, places)
 
 
@@ -1158,9 +1190,11 @@ def expert_product(w, x, offsets, index=None, fan: int = 1, up=None, dtype=None,
         y, y_ld = torch.empty((P, wc.rows), dtype=dtype if dtype is not None else torch.float32, device=dev), max(wc.rows, 1)
     else:
         y_ld = _rows(where, "y", y, P, wc.rows, dev)
-    args = _ExpertProductArgs(ctypes.pointer(wc), ctypes.pointer(uc) if uc is not None else None, x_ptr, xs_ptr, x_ld,
-                              x_rows, P, off_ptr, idx_ptr, fan, _dense_type(where, "y", y.dtype), y.data_ptr(), y_ld, st_ptr)
-    _check(_lib().bitsmoe_expert_product(args, _raw_stream(dev.index)), "bitsmoe_expert_product")
+    args = _ExpertProductArgs(_addressof(wc), _addressof(uc) if uc is not None else None, x_ptr, xs_ptr, x_ld, x_rows, P,
+                              off_ptr, idx_ptr, fan, _dense_type(where, "y", y.dtype), y.data_ptr(), y_ld, st_ptr)
+    rc = _lib().bitsmoe_expert_product(args, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "bitsmoe_expert_product")
     return y
 
 
@@ -1193,10 +1227,11 @@ def expert_combine(y, places, weights, base=None, dtype=None, out=None, stream=N
     base_ptr, base_ld = None, 0
     if base is not None:
         base_ld, base_ptr = _rows(where, "base", base, T, D, dev, out.dtype), base.data_ptr()
-    _check(_lib().bitsmoe_expert_combine(y.data_ptr(), _dense_type(where, "y", y.dtype), y_ld, P, places.data_ptr(),
-                                         weights.data_ptr(), T, k, D, base_ptr, base_ld, out.data_ptr(),
-                                         _dense_type(where, "out", out.dtype), out_ld, _raw_stream(dev.index)),
-           "bitsmoe_expert_combine")
+    rc = _lib().bitsmoe_expert_combine(y.data_ptr(), _dense_type(where, "y", y.dtype), y_ld, P, places.data_ptr(),
+                                       weights.data_ptr(), T, k, D, base_ptr, base_ld, out.data_ptr(),
+                                       _dense_type(where, "out", out.dtype), out_ld, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "bitsmoe_expert_combine")
     return out
 
 

@@ -8,6 +8,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -34,7 +35,7 @@ struct ExpertArgs {
   const float* xs;
   int64_t x_ld;
   void* y;
-  int y_type;
+  int y_type, y_vec;     // y_vec: bf16 rows on 16-byte boundaries
   int64_t y_ld;
   int nk, stages, nbuf;  // tensor cores: steps of 128 bytes of the columns, depth of the ring, accumulators in turn
   int splits, sps;       // CTAs that share the columns of a tile, steps of each
@@ -229,6 +230,7 @@ constexpr int kTcThreads = 32 * (4 + kXWarps + kOutWarps);   // warps: 0 matrice
 constexpr int kStagesMost = 8;
 constexpr uint32_t kATile = 2 * 128 * 128;   // bytes of a stage's tiles of the matrices
 constexpr int kTcShared = 227 * 1024;        // (all of an SM's, as of every kernel that allocates tensor memory)
+constexpr int kTurnPitch = 80;               // (64 bytes and 16, so that no two of eight rows meet in a bank)
 constexpr int kXRows = 4 * kXWarps;          // rows that one pass of x's warps brings
 
 struct TcShared {
@@ -236,6 +238,7 @@ struct TcShared {
   alignas(16) float factor[2][256];      // of the rows of y: x's scale, NaN for a row that is not there
   uint64_t full[kStagesMost], empty[kStagesMost], xfull[kStagesMost], afull[2], aempty[2], drained;
   uint32_t slot;
+  alignas(16) uint8_t turn[kOutWarps][16 * kTurnPitch];   // 16 rows of y of a warp's 32 results each, on their way out
 };
 
 // What is stored for results that a wait that ran out has lost.  A warp whose wait ran out passes nothing on: who waits for
@@ -469,39 +472,104 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       ok = __all_sync(0xFFFFFFFFu, ok);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t tl = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(buf * 2 * a.N);
-      for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
-        uint32_t v[2][16];
-        if (!ok) {
+      if (!PAIR && a.splits > 1) {   // the part of the columns: all that is left of it is summed below
+        for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
 #pragma unroll
-          for (int q = 0; q < 16; ++q) v[0][q] = v[1][q] = kLost;
-        } else if (nk > 0) {
+          for (int h = 0; h < 2; ++h) {
+            uint32_t v[16];
+            if (ok && nk > 0) tmem_ld16(tl + (uint32_t)(h * a.N + c0), v);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) red[(h * a.N + c0 + q) * 128 + r] = !ok ? __uint_as_float(kLost) : nk > 0 ? __uint_as_float(v[q]) : 0.f;
+          }
+        }
+      } else if (!ok) {
+        for (int c = side; c < t.n; c += 2) {
+          const int64_t at = (int64_t)(t.p0 + c) * a.y_ld + m;
+          if (in0) store_y(a.y, a.y_type, at, __uint_as_float(kLost));
+          if (!GLU && in1) store_y(a.y, a.y_type, at + 128, __uint_as_float(kLost));
+        }
+      } else if (a.y_vec) {
+        // bf16 rows on 16-byte boundaries: rows lie along the lanes of tensor memory; turned by way of shared memory a row of y
+        // goes out 16 bytes a lane
+        const int mw = m - lane;   // the warp's first row
+        uint8_t* turn = s.turn[wid - 4 - kXWarps];
+        const uint32_t put = smem_u32(turn) + (uint32_t)((lane >> 4) * 8 + (lane & 7)) * kTurnPitch + (uint32_t)(lane >> 3 & 1) * 16u;
+        float sr[2][2][2];   // scales of the lane's rows 16 h + 8 i + l / 4 of both tiles
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            sr[0][h][i] = F8 ? __shfl_sync(0xFFFFFFFFu, s0, 16 * h + 8 * i + (lane >> 2)) : 1.f;
+            sr[1][h][i] = F8 ? __shfl_sync(0xFFFFFFFFu, s1, 16 * h + 8 * i + (lane >> 2)) : 1.f;
+          }
+        for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
+          uint32_t d[2][2][8];
+          tmem_ld_fragments(tl + (uint32_t)c0, d[0]);
+          tmem_ld_fragments(tl + (uint32_t)(a.N + c0), d[1]);
+          float2 f[2];
+          f[0] = *reinterpret_cast<const float2*>(factor + c0 + 2 * (lane & 3));
+          f[1] = *reinterpret_cast<const float2*>(factor + c0 + 8 + 2 * (lane & 3));
+          tmem_wait(d[0]);
+          tmem_wait(d[1]);
+          const auto value = [&](int b, int h, int q) {   // element q of 8: columns 8 (q / 4) + q % 2, rows 8 (q / 2 % 2)
+            const float g = q & 1 ? f[q >> 2].y : f[q >> 2].x;
+            return __uint_as_float(d[b][h][q]) * (F8 ? g * sr[b][h][q >> 1 & 1] : g);
+          };
+#pragma unroll
+          for (int b = 0; b < (GLU ? 1 : 2); ++b) {
+            if (b) __syncwarp();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t o[4];
+#pragma unroll
+              for (int q = 0; q < 8; q += 2) {
+                float x = value(b, h, q), y = value(b, h, q + 1);
+                if constexpr (GLU) {
+                  x = silu_fast(x, value(1, h, q));
+                  y = silu_fast(y, value(1, h, q + 1));
+                }
+                const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
+                o[q >> 1] = *reinterpret_cast<const uint32_t*>(&p);
+              }
+              store_transposed(put + (uint32_t)h * 32u, o[0], o[1], o[2], o[3]);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int c = 8 * i + (lane >> 2), col = mw + 128 * b + 8 * (lane & 3);
+              const uint4 p = lds128(turn + c * kTurnPitch + 16 * (lane & 3));
+              if (c0 + c < t.n && col < a.rows) {
+                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y) + (int64_t)(t.p0 + c0 + c) * a.y_ld + col;
+                if (col + 8 <= a.rows) {
+                  *reinterpret_cast<uint4*>(y) = p;
+                } else {
+                  const uint32_t e[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+                  for (int n = 0; n < 7; ++n)
+                    if (col + n < a.rows) reinterpret_cast<uint16_t*>(y)[n] = (uint16_t)(e[n >> 1] >> (16 * (n & 1)));
+                }
+              }
+            }
+          }
+          __syncwarp();
+        }
+      } else {
+        for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
+          uint32_t v[2][16];
           tmem_ld16(tl + (uint32_t)c0, v[0]);
           tmem_ld16(tl + (uint32_t)(a.N + c0), v[1]);
-        } else {
-#pragma unroll
-          for (int q = 0; q < 16; ++q) v[0][q] = v[1][q] = 0u;
-        }
-        if (!PAIR && a.splits > 1) {
+          const int64_t at = (int64_t)(t.p0 + c0) * a.y_ld + m;
 #pragma unroll
           for (int q = 0; q < 16; ++q) {
-            red[(c0 + q) * 128 + r] = __uint_as_float(v[0][q]);
-            red[(a.N + c0 + q) * 128 + r] = __uint_as_float(v[1][q]);
-          }
-          continue;
-        }
-        float f[16];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(f + 4 * q) = *reinterpret_cast<const float4*>(factor + c0 + 4 * q);
-        const int64_t at = (int64_t)(t.p0 + c0) * a.y_ld + m;
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          const float v0 = __uint_as_float(v[0][q]) * (F8 ? s0 * f[q] : f[q]), v1 = __uint_as_float(v[1][q]) * (F8 ? s1 * f[q] : f[q]);
-          if (c0 + q >= t.n) continue;
-          if constexpr (GLU) {
-            if (in0) store_y(a.y, a.y_type, at + q * a.y_ld, silu_fast(v0, v1));
-          } else {
-            if (in0) store_y(a.y, a.y_type, at + q * a.y_ld, v0);
-            if (in1) store_y(a.y, a.y_type, at + q * a.y_ld + 128, v1);
+            const float f = factor[c0 + q];
+            const float v0 = __uint_as_float(v[0][q]) * (F8 ? s0 * f : f), v1 = __uint_as_float(v[1][q]) * (F8 ? s1 * f : f);
+            if (c0 + q >= t.n) continue;
+            if constexpr (GLU) {
+              if (in0) store_y(a.y, a.y_type, at + q * a.y_ld, silu_fast(v0, v1));
+            } else {
+              if (in0) store_y(a.y, a.y_type, at + q * a.y_ld, v0);
+              if (in1) store_y(a.y, a.y_type, at + q * a.y_ld + 128, v1);
+            }
           }
         }
       }
@@ -581,6 +649,32 @@ bool tc_maps(const ExpertArgs& a, bool f8, CUtensorMap* wm, CUtensorMap* um) {
   return matrices(wm, a.w, a.w_ld, a.w_eld) && (!a.up || matrices(um, a.up, a.u_ld, a.u_eld));
 }
 
+// Clusters of n CTAs of a kernel (one CTA an SM) that run at once on device `dev`, asked once for each.
+template <auto K>
+int clusters_at_once(int dev, int n) {
+  static std::atomic<int> known[64][4];
+  const int q = n == 1 ? 0 : n == 2 ? 1 : n == 4 ? 2 : 3;
+  if (dev < 64) {
+    const int c = known[dev][q].load(std::memory_order_relaxed);
+    if (c > 0) return c;
+  }
+  if (allow_shared<K>(dev, kTcShared) != cudaSuccess) return 0;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)n;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)n);
+  cfg.blockDim = dim3(kTcThreads);
+  cfg.dynamicSmemBytes = kTcShared;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int c = 0;
+  if (cudaOccupancyMaxActiveClusters(&c, K, &cfg) != cudaSuccess) return 0;
+  if (dev < 64) known[dev][q].store(c, std::memory_order_relaxed);
+  return c;
+}
+
 template <bool F8, bool GLU, bool PAIR>
 cudaError_t launch_tc_as(const ExpertArgs& a, const CUtensorMap& wm, const CUtensorMap& um, int64_t groups, int dev, cudaStream_t st) {
   auto kern = k_expert_tc<F8, GLU, PAIR>;
@@ -612,7 +706,10 @@ cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um
   a.u_next = a.u_eld != 0;
   a.nbuf = 4 * a.N <= 512 ? 2 : 1;
   const int64_t most = std::min<int64_t>(a.P, (int64_t)a.P / a.N + a.E) * a.mt;   // tiles at most
-  a.splits = pair ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({8, sms / most, a.nk / 2}));
+  a.splits = 1;
+  if (!pair)   // (clusters that do not all run at once would take a second turn)
+    for (int n = 8; n > 1 && a.splits == 1; n /= 2)
+      if (most * n <= sms && a.nk >= 2 * n && most <= clusters_at_once<k_expert_tc<F8, GLU, false>>(dev, n)) a.splits = n;
   a.sps = (a.nk + a.splits - 1) / a.splits;
   const size_t room = kTcShared - 1024 - sizeof(TcShared) - (a.splits > 1 ? (size_t)a.N * 1024 : 0);
   a.stages = std::min(kStagesMost, (int)(room / (kATile + (size_t)a.N * (pair ? 64 : 128))));
@@ -685,6 +782,7 @@ extern "C" int bitsmoe_expert_product(const bitsmoe_expert_product_args* args, v
   a.y = g.y;
   a.y_type = g.y_type;
   a.y_ld = g.y_ld;
+  a.y_vec = g.y_type == BITSMOE_BF16 && on_boundaries(g.y, g.y_ld, 2, g.P);
   a.spin = debug_wait_clocks() > 0 ? debug_wait_clocks() : kWaitClocks;
   a.lose = debug_skip_arrival();
   a.status = g.status;

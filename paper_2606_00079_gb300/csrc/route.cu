@@ -6,9 +6,9 @@
 //                places the inverse
 //   out[t]     = base[t] + sum_j weights[t][j] y[places[t][j]]
 //
-// The sort is by counting, and no result depends on the order of atomics: 32 tokens at a time set their bits in a word
-// for each expert (a token picks an expert once), and a pair's rank in its expert is the count of the bits below its
-// token's, plus those of the words before.
+// The sort is by counting, and no result depends on the order of atomics: each 32 tokens set their bits in a word for
+// each expert (a token picks an expert once), and a pair's rank in its expert is the count of the bits below its
+// token's, plus those of the words before.  The chain of launches and dependent reads bounds it, not the logits' bytes.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -21,8 +21,9 @@ namespace {
 using namespace bmoe;
 
 constexpr int kMaxExperts = 1024, kMaxTopK = 32;
-constexpr int kRouteThreads = 1024, kRouteWarps = kRouteThreads / 32;   // 32 tokens at a time, a warp each
-constexpr int kAloneTokens = 64;                                        // one block does all of at most so many
+constexpr int kRouteThreads = 1024;
+constexpr int kWords = 4, kChunk = 32 * kWords;   // tokens of a block at a time: a bit of a warp's in each word
+constexpr int kAloneTokens = kChunk;              // one block does all of at most so many
 
 struct RouteArgs {
   const float* logits;
@@ -41,16 +42,23 @@ __device__ __forceinline__ float logit_of(uint32_t key) {   // order_key's inver
   return __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
 }
 
-// One token's selection by a warp: lane j < k gets the j-th expert (-1: none) and its weight.  NE: logits a lane holds.
+// A token's logits as keys, of lane l those of experts l + 32 i: 0 where one cannot be selected.
 template <int NE>
-__device__ __forceinline__ void select_token(const RouteArgs& a, int64_t t, int lane, int& expert, float& weight) {
-  constexpr uint32_t kNone = 0x007FFFFFu;   // -infinity's key, above NaN's
-  uint32_t key[NE];
+__device__ __forceinline__ void load_keys(const RouteArgs& a, int64_t t, int lane, uint32_t (&key)[NE]) {
   const float* row = a.logits + t * a.ld;
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
     const int e = lane + 32 * i;
-    key[i] = e < a.E ? order_key(__ldg(row + e)) : 0u;
+    key[i] = e < a.E ? __float_as_uint(__ldg(row + e)) : 0xFF800000u;
+  }
+}
+// One token's selection by a warp: lane j < k gets the j-th expert (-1: none) and its weight.  NE: logits a lane holds.
+template <int NE>
+__device__ __forceinline__ void select_token(const RouteArgs& a, int lane, uint32_t (&key)[NE], int& expert, float& weight) {
+  constexpr uint32_t kNone = 0x007FFFFFu;   // -infinity's key, above NaN's
+#pragma unroll
+  for (int i = 0; i < NE; ++i) {
+    key[i] = order_key(__uint_as_float(key[i]));
     if (key[i] <= kNone) key[i] = 0u;
   }
   expert = -1;
@@ -117,38 +125,70 @@ __device__ __forceinline__ int block_scan(int* v, int n, int* part) {
   return part[32];
 }
 
-// Tokens [first, last) of a block, 32 at a time: selection, and each pair's rank among the block's pairs of its expert
-// (into places, for now).  count[e]: the block's pairs of expert e.
+struct RouteShared {
+  uint32_t mask[kWords][kMaxExperts];
+  int count[kMaxExperts];
+  uint16_t pick[kChunk * kMaxTopK];
+  int part[33];
+};
+
+// Tokens [first, last) of a block: selection, and each pair's rank among the block's pairs of its expert (into places, for
+// now).  s.count[e]: the block's pairs of expert e.
 template <int NE>
-__device__ __forceinline__ void select_block(const RouteArgs& a, int first, int last, uint32_t* mask, int* count) {
+__device__ __forceinline__ void select_block(const RouteArgs& a, int first, int last, RouteShared& s) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  constexpr bool kAhead = NE <= 8;   // the next token's logits are requested before this one's are used
   for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
-    mask[e] = 0u;
-    count[e] = 0;
+#pragma unroll
+    for (int q = 0; q < kWords; ++q) s.mask[q][e] = 0u;
+    s.count[e] = 0;
+  }
+  for (int t0 = first; t0 < last; t0 += kChunk) {
+    const int n = min(last - t0, kChunk);
+    uint32_t key[NE], next[kAhead ? NE : 1];
+    if (kAhead && w < n) load_keys<NE>(a, t0 + w, lane, key);
+    __syncthreads();
+    for (int q = 0; w + 32 * q < n; ++q) {
+      const int t = w + 32 * q;
+      int expert;
+      float weight;
+      if constexpr (kAhead) {
+        if (t + 32 < n) load_keys<NE>(a, t0 + t + 32, lane, next);
+      } else {
+        load_keys<NE>(a, t0 + t, lane, key);
+      }
+      select_token<NE>(a, lane, key, expert, weight);
+      if (lane < a.k) {
+        a.weights[(int64_t)(t0 + t) * a.k + lane] = weight;
+        s.pick[t * a.k + lane] = (uint16_t)expert;
+        if (expert >= 0) atomicOr(s.mask[q] + expert, 1u << w);
+      }
+      if constexpr (kAhead) {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) key[i] = next[i];
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n * a.k; i += kRouteThreads) {
+      const int t = i / a.k, e = (int16_t)s.pick[i];
+      int rank = -1;
+      if (e >= 0) {
+        rank = s.count[e] + __popc(s.mask[t >> 5][e] & ((1u << (t & 31)) - 1u));
+        for (int q = 0; q < t >> 5; ++q) rank += __popc(s.mask[q][e]);
+      }
+      const int64_t p = (int64_t)t0 * a.k + i;
+      a.experts[p] = e;
+      a.places[p] = rank;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.E; e += kRouteThreads)
+#pragma unroll
+      for (int q = 0; q < kWords; ++q) {
+        s.count[e] += __popc(s.mask[q][e]);
+        s.mask[q][e] = 0u;
+      }
   }
   __syncthreads();
-  for (int t0 = first; t0 < last; t0 += kRouteWarps) {
-    const int t = t0 + w;
-    int expert = -1;
-    float weight = 0.f;
-    if (t < last) {
-      select_token<NE>(a, t, lane, expert, weight);
-      if (expert >= 0) atomicOr(mask + expert, 1u << w);
-    }
-    __syncthreads();
-    if (t < last && lane < a.k) {
-      const int64_t p = (int64_t)t * a.k + lane;
-      a.experts[p] = expert;
-      a.weights[p] = weight;
-      a.places[p] = expert < 0 ? -1 : count[expert] + __popc(mask[expert] & ((1u << w) - 1u));
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
-      count[e] += __popc(mask[e]);
-      mask[e] = 0u;
-    }
-    __syncthreads();
-  }
 }
 
 // Places and pairs of a block's tokens once base[e] is where its first pair of expert e goes.
@@ -164,33 +204,32 @@ __device__ __forceinline__ void place_block(const RouteArgs& a, int first, int l
 
 template <int NE>
 __global__ void __launch_bounds__(kRouteThreads) k_route_alone(const __grid_constant__ RouteArgs a) {
-  __shared__ uint32_t mask[kMaxExperts];
-  __shared__ int count[kMaxExperts];
-  __shared__ int part[33];
-  select_block<NE>(a, 0, a.T, mask, count);
-  const int total = block_scan(count, a.E, part);
+  __shared__ RouteShared s;
+  select_block<NE>(a, 0, a.T, s);
+  const int total = block_scan(s.count, a.E, s.part);
   __syncthreads();
-  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) a.offsets[e] = count[e];
+  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) a.offsets[e] = s.count[e];
   if (threadIdx.x == 0) a.offsets[a.E] = total;
   for (int p = total + threadIdx.x; p < a.T * a.k; p += kRouteThreads) a.pairs[p] = -1;
-  place_block(a, 0, a.T, count);
+  place_block(a, 0, a.T, s.count);
 }
 
 template <int NE>
 __global__ void __launch_bounds__(kRouteThreads) k_route_select(const __grid_constant__ RouteArgs a) {
-  __shared__ uint32_t mask[kMaxExperts];
-  __shared__ int count[kMaxExperts];
+  __shared__ RouteShared s;
+  pdl_trigger();
   const int first = blockIdx.x * a.per;
-  select_block<NE>(a, first, min(first + a.per, a.T), mask, count);
-  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) a.counts[(int64_t)blockIdx.x * a.E + e] = count[e];
+  select_block<NE>(a, first, min(first + a.per, a.T), s);
+  for (int e = threadIdx.x; e < a.E; e += kRouteThreads) a.counts[(int64_t)blockIdx.x * a.E + e] = s.count[e];
 }
 
-// Every block sums the counts itself: of the blocks before it, and of all.
+// Every block sums the counts itself: of the blocks before it, and of all.  (Launched while the selection runs.)
 __global__ void __launch_bounds__(kRouteThreads) k_route_place(const __grid_constant__ RouteArgs a) {
   __shared__ int base[kMaxExperts], start[kMaxExperts];
   __shared__ int part[33];
   for (int e = threadIdx.x; e < a.E; e += kRouteThreads) base[e] = start[e] = 0;
   __syncthreads();
+  pdl_wait();
   // threads take (expert, slice of the blocks)
   const int ex = (a.E + 31) / 32 * 32, slices = max(1, kRouteThreads / ex);
   const int slice = threadIdx.x / ex, e0 = threadIdx.x % ex;
@@ -198,7 +237,7 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_place(const __grid_cons
     int before = 0, all = 0;
 #pragma unroll 4
     for (int b = slice; b < (int)gridDim.x; b += slices) {
-      const int c = __ldg(a.counts + (int64_t)b * a.E + e0);
+      const int c = a.counts[(int64_t)b * a.E + e0];
       all += c;
       before += b < (int)blockIdx.x ? c : 0;
     }
@@ -233,14 +272,22 @@ cudaError_t launch_route(const RouteArgs& a, int blocks, cudaStream_t st) {
   k_route_select<NE><<<blocks, kRouteThreads, 0, st>>>(a);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  k_route_place<<<blocks, kRouteThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(kRouteThreads);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_route_place, a);
 }
 
 // Tokens of a block, and blocks of a call: each block of the second launch reads blocks x E counts.
 int route_per(int T, int E) {
   const int most = std::min(152, std::max(16, 65536 / E));
-  return T <= kAloneTokens ? T : ((T + most - 1) / most + kRouteWarps - 1) / kRouteWarps * kRouteWarps;
+  return T <= kAloneTokens ? T : ((T + most - 1) / most + 31) / 32 * 32;
 }
 int route_blocks(int T, int E) { return T <= kAloneTokens ? 1 : (T + route_per(T, E) - 1) / route_per(T, E); }
 bool route_sizes_ok(int T, int E, int k) {
@@ -260,30 +307,117 @@ struct CombineArgs {
   int64_t out_ld;
 };
 
-template <typename T>
-__device__ __forceinline__ float value(const T* p) {
-  if constexpr (sizeof(T) == 4) return *p;
-  else return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
+// V elements of a row: 16 bytes or what the rows' boundaries allow.
+template <typename T, int V>
+struct Piece {
+  uint32_t w[(V * sizeof(T) + 3) / 4];
+};
+template <typename T, int V>
+__device__ __forceinline__ Piece<T, V> load_piece(const T* p) {
+  Piece<T, V> r;
+  if constexpr (V * sizeof(T) >= 16) {
+#pragma unroll
+    for (int i = 0; i < (int)(V * sizeof(T)) / 16; ++i) {
+      const uint4 x = reinterpret_cast<const uint4*>(p)[i];
+      r.w[4 * i] = x.x, r.w[4 * i + 1] = x.y, r.w[4 * i + 2] = x.z, r.w[4 * i + 3] = x.w;
+    }
+  } else if constexpr (V * sizeof(T) == 8) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    r.w[0] = x.x, r.w[1] = x.y;
+  } else if constexpr (V * sizeof(T) == 4) {
+    r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else {
+    r.w[0] = *reinterpret_cast<const uint16_t*>(p);
+  }
+  return r;
 }
-template <typename T>
-__device__ __forceinline__ void keep(T* p, float v) {
-  if constexpr (sizeof(T) == 4) *p = v;
-  else *p = __float2bfloat16_rn(v);
+template <typename T, int V>
+__device__ __forceinline__ float piece_at(const Piece<T, V>& r, int i) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(r.w[i]);
+  else return i & 1 ? bf16hi(r.w[i / 2]) : bf16lo(r.w[i / 2]);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_piece(T* p, const float (&v)[V]) {
+  Piece<T, V> r = {};
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.w[i] = __float_as_uint(v[i]);
+  } else if constexpr (V == 1) {
+    *p = __float2bfloat16_rn(v[0]);
+    return;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[i], v[i + 1]);
+      r.w[i / 2] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+  }
+  if constexpr (V * sizeof(T) >= 16) {
+#pragma unroll
+    for (int i = 0; i < (int)(V * sizeof(T)) / 16; ++i)
+      reinterpret_cast<uint4*>(p)[i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
+  } else if constexpr (V * sizeof(T) == 8) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(r.w[0], r.w[1]);
+  } else {
+    *reinterpret_cast<uint32_t*>(p) = r.w[0];
+  }
 }
 
-// An element a thread.
-template <typename TY, typename TO>
-__global__ void __launch_bounds__(256) k_combine_plain(const __grid_constant__ CombineArgs a) {
+// V columns of a token a thread; the pieces of eight rows are requested before the first is used.  The rows' bytes bound it.
+template <typename TY, typename TO, int V>
+__global__ void __launch_bounds__(256) k_combine(const __grid_constant__ CombineArgs a) {
+  constexpr int kAhead = 8;
   const int64_t t = blockIdx.x;
-  for (int d = blockIdx.y * 256 + threadIdx.x; d < a.D; d += gridDim.y * 256) {
-    float s = 0.f;
-    for (int j = 0; j < a.k; ++j) {
-      const int p = __ldg(a.places + t * a.k + j);
-      if ((unsigned)p < (unsigned)a.P) s = fmaf(__ldg(a.weights + t * a.k + j), value(static_cast<const TY*>(a.y) + (int64_t)p * a.y_ld + d), s);
-    }
-    if (a.base) s = value(static_cast<const TO*>(a.base) + t * a.base_ld + d) + s;
-    keep(static_cast<TO*>(a.out) + t * a.out_ld + d, s);
+  const int d = (blockIdx.y * 256 + threadIdx.x) * V;
+  if (d >= a.D) return;   // (D is a multiple of V)
+  float s[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) s[i] = 0.f;
+  Piece<TO, V> base;
+  if (a.base) base = load_piece<TO, V>(static_cast<const TO*>(a.base) + t * a.base_ld + d);
+  for (int j0 = 0; j0 < a.k; j0 += kAhead) {
+    Piece<TY, V> y[kAhead];
+    float w[kAhead];
+    int p[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) p[j] = j0 + j < a.k ? __ldg(a.places + t * a.k + j0 + j) : -1;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if ((unsigned)p[j] < (unsigned)a.P) {
+        y[j] = load_piece<TY, V>(static_cast<const TY*>(a.y) + (int64_t)p[j] * a.y_ld + d);
+        w[j] = __ldg(a.weights + t * a.k + j0 + j);
+      }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if ((unsigned)p[j] < (unsigned)a.P) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] = fmaf(w[j], piece_at<TY, V>(y[j], i), s[i]);
+      }
   }
+  if (a.base) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] = piece_at<TO, V>(base, i) + s[i];
+  }
+  store_piece<TO, V>(static_cast<TO*>(a.out) + t * a.out_ld + d, s);
+}
+
+template <typename TY, typename TO>
+cudaError_t launch_combine(const CombineArgs& a, int T, cudaStream_t st) {
+  const auto fits = [&](int v) {
+    const auto on = [&](const void* p, int64_t ld, int size) {
+      const int64_t to = std::min(16, v * size);
+      return reinterpret_cast<uintptr_t>(p) % to == 0 && (ld * size) % to == 0;
+    };
+    return a.D % v == 0 && on(a.y, a.y_ld, sizeof(TY)) && on(a.out, a.out_ld, sizeof(TO)) && (!a.base || on(a.base, a.base_ld, sizeof(TO)));
+  };
+  const auto go = [&](auto kern, int v) {
+    kern<<<dim3((unsigned)T, (unsigned)((a.D / v + 255) / 256)), 256, 0, st>>>(a);
+    return cudaGetLastError();
+  };
+  constexpr int kWide = sizeof(TY) == 4 ? 4 : 8;
+  if (fits(kWide)) return go(k_combine<TY, TO, kWide>, kWide);
+  if (fits(2)) return go(k_combine<TY, TO, 2>, 2);
+  return go(k_combine<TY, TO, 1>, 1);
 }
 
 }  // namespace
@@ -337,12 +471,8 @@ extern "C" int bitsmoe_expert_combine(const void* y, int y_type, int64_t y_ld, i
     return BITSMOE_ERR_ALIGNMENT;
   CombineArgs a{y, y_ld, P, top_k, D, places, weights, base, base_ld, out, out_ld};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const dim3 grid((unsigned)T, (unsigned)std::min(64, (D + 255) / 256));
   const bool yf = y_type == BITSMOE_F32, of = out_type == BITSMOE_F32;
-  if (yf && of) k_combine_plain<float, float><<<grid, 256, 0, st>>>(a);
-  else if (yf) k_combine_plain<float, __nv_bfloat16><<<grid, 256, 0, st>>>(a);
-  else if (of) k_combine_plain<__nv_bfloat16, float><<<grid, 256, 0, st>>>(a);
-  else k_combine_plain<__nv_bfloat16, __nv_bfloat16><<<grid, 256, 0, st>>>(a);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = yf ? (of ? launch_combine<float, float>(a, T, st) : launch_combine<float, __nv_bfloat16>(a, T, st))
+                           : (of ? launch_combine<__nv_bfloat16, float>(a, T, st) : launch_combine<__nv_bfloat16, __nv_bfloat16>(a, T, st));
   return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
 }

@@ -253,4 +253,27 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "memory");
 }
 
+// 16 columns of 32 lanes as two halves of 16 lanes, asynchronous (tmem_wait): v[h][4 j ..] of lane l are columns 8 j + 2 (l % 4), + 1
+// of rows 16 h + l / 4 and, in the last two, + 8: the fragments that store_transposed takes.
+__device__ __forceinline__ void tmem_ld_fragments(uint32_t taddr, uint32_t (&v)[2][8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[h][0]), "=r"(v[h][1]), "=r"(v[h][2]), "=r"(v[h][3]), "=r"(v[h][4]), "=r"(v[h][5]), "=r"(v[h][6]), "=r"(v[h][7])
+                 : "r"(taddr + ((uint32_t)(16 * h) << 16)));
+}
+// (The registers go through it, so that nothing reads them before.)
+__device__ __forceinline__ void tmem_wait(uint32_t (&v)[2][8]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0][0]), "+r"(v[0][1]), "+r"(v[0][2]), "+r"(v[0][3]), "+r"(v[0][4]), "+r"(v[0][5]), "+r"(v[0][6]), "+r"(v[0][7]), "+r"(v[1][0]), "+r"(v[1][1]), "+r"(v[1][2]), "+r"(v[1][3]), "+r"(v[1][4]), "+r"(v[1][5]), "+r"(v[1][6]), "+r"(v[1][7])
+               :
+               : "memory");
+}
+// Four 8 x 8 matrices of 16 bits, lane l holding columns 2 (l % 4), + 1 of row l / 4 of each: lanes 8 i .. 8 i + 7 say where the
+// columns of matrix i go (16 bytes each).
+__device__ __forceinline__ void store_transposed(uint32_t saddr, uint32_t m0, uint32_t m1, uint32_t m2, uint32_t m3) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared::cta.b16 [%0], {%1,%2,%3,%4};" ::"r"(saddr), "r"(m0), "r"(m1), "r"(m2), "r"(m3)
+               : "memory");
+}
+
 }  // namespace

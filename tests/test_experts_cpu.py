@@ -93,8 +93,9 @@ def test_expert_product_refusals(bm):
     m = lambda **kw: matrices(bm, **kw)
 
     def f(w=None, up=None, **kw):
-        a = bm._ExpertProductArgs(ctypes.pointer(w if w is not None else m()), ctypes.pointer(up) if up is not None else None,
-                                  A, A, 16, 5, 7, A, A, 2, 1, A, 8, 0)
+        w = w if w is not None else m()
+        a = bm._ExpertProductArgs(ctypes.addressof(w), ctypes.addressof(up) if up is not None else None, A, A, 16, 5, 7, A, A, 2, 1,
+                                  A, 8, 0)
         for k, v in kw.items():
             setattr(a, k, v)
         return bm._lib().bitsmoe_expert_product(ctypes.byref(a), 0)
