@@ -907,10 +907,8 @@ def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: 
             _refuse(where, "x in 8 bits is asked for but pre_norm is off")
         if x is None:
             x = Rowscale.empty((T, D), dev)
-            x_ld = x._c.ld
-        else:
-            x_ld = _rowscale_rows(where, "x", x, T, D, dev)
-        x_type, x_ptr = _E4M3, x.codes.data_ptr()
+        xc = _rowscale_rows(where, "x", x, T, D, dev)
+        x_type, x_ld, x_ptr = _E4M3, xc.ld, xc.codes
     elif x is not None:
         if not pre_norm:
             _refuse(where, "x is given but pre_norm is off")
@@ -923,7 +921,7 @@ def block_norm(h, y=None, *, post_norm: bool = False, post_gain=None, post_eps: 
                           h.data_ptr(), y_ptr, gate_ptr, post_ptr, pre_ptr, chan_ptr, ho_ptr, x_ptr,
                           h_ld, y_ld, gate_ld, ho_ld, x_ld)
     if x_type == _E4M3:
-        _check(_lib().bitsmoe_block_norm_rowscale(args, x.scales.data_ptr(), _raw_stream(dev.index)),
+        _check(_lib().bitsmoe_block_norm_rowscale(args, xc.scales, _raw_stream(dev.index)),
                "bitsmoe_block_norm_rowscale")
     else:
         _check(_lib().bitsmoe_block_norm(args, _raw_stream(dev.index)), "bitsmoe_block_norm")
@@ -937,7 +935,7 @@ class Rowscale:
     """Rows in 8 bits on the device: `codes` (torch.float8_e4m3fn, rows x cols, or experts x rows x cols with dense
     rows) and `scales` (float32, one for each row); value = code * scale, see bitsmoe_rowscale in include/bitsmoe.h."""
 
-    __slots__ = ("_codes", "_scales", "_c")   # _c: what the library reads, formed when it is first needed
+    __slots__ = ("_codes", "_scales", "_buf", "_c", "shape", "device")   # _c: what the library reads, formed when first needed
 
     def __init__(self, codes, scales):
         torch = _torch or _load_torch()
@@ -949,40 +947,43 @@ class Rowscale:
             _refuse("Rowscale", f"scales have shape {tuple(scales.shape)}, codes {tuple(codes.shape)}", "SHAPE")
         if scales.shape[-1] > 1 and scales.stride(-1) != 1:
             _refuse("Rowscale", "scales must be dense along the rows")
-        self._codes, self._scales, self._c = codes, scales, None
+        self._codes, self._scales, self._buf, self._c = codes, scales, None, None
+        self.shape, self.device = codes.shape, codes.device
 
     @classmethod
     def empty(cls, shape, device=None) -> "Rowscale":
         """Uninitialised rows on a pitch of a multiple of 16 bytes."""
         torch = _torch or _load_torch()
-        *rows, cols = shape
-        if len(rows) not in (1, 2) or cols < 1 or min(rows) < 0:
+        dims = len(shape)
+        if dims not in (2, 3) or min(shape) < 0 or shape[-1] < 1:
             _refuse("Rowscale.empty", f"shape {tuple(shape)}")
-        dev = device if device is not None else torch.cuda.current_device()
+        n, cols = (shape[0] if dims == 2 else shape[0] * shape[1]), shape[-1]
+        if n > _MAX_ROWS or cols > _MAX_ROWS:
+            _refuse("Rowscale.empty", f"shape {tuple(shape)}", "SHAPE")
         pitch = (cols + 15) & ~15
-        codes = torch.empty((*rows, pitch), dtype=torch.float8_e4m3fn, device=dev)
-        self = cls.__new__(cls)
-        self._codes = codes if pitch == cols else codes[..., :cols]
-        self._scales = scales = torch.empty(rows, dtype=torch.float32, device=dev)
-        n = rows[0] if len(rows) == 1 else rows[0] * rows[1]
-        self._c = _Rowscale(n, cols, pitch, codes.data_ptr(), scales.data_ptr()) if n <= _MAX_ROWS >= cols else None
+        self = cls.__new__(cls)   # one allocation for both; the tensors are made when asked for
+        self._buf = buf = torch.empty(n * pitch + 4 * n, dtype=torch.uint8,
+                                      device=device if device is not None else torch.cuda.current_device())
+        self._codes = self._scales = None
+        self.shape, self.device = shape, buf.device
+        base = buf.data_ptr()
+        self._c = _Rowscale(n, cols, pitch, base, base + n * pitch)
         return self
 
     @property
     def codes(self):
+        if self._codes is None:
+            c = self._c
+            flat = self._buf[:c.rows * c.ld].view(_torch.float8_e4m3fn)
+            self._codes = flat.view(*self.shape[:-1], c.ld)[..., :c.cols]
         return self._codes
 
     @property
     def scales(self):
+        if self._scales is None:
+            c = self._c
+            self._scales = self._buf[c.rows * c.ld:].view(_torch.float32).view(self.shape[:-1])
         return self._scales
-
-    @property
-    def shape(self):
-        return self._codes.shape
-
-    @property
-    def device(self):
-        return self._codes.device
 
 
 def _flat(where: str, name: str, x):
@@ -997,14 +998,6 @@ def _flat(where: str, name: str, x):
         _refuse(where, f"{name}'s matrices must lie one after the other")
 
 
-def _rowscale_rows(where: str, name: str, q: Rowscale, rows=None, cols=None, device=None):
-    """Checks of a 2-d Rowscale; its pitch in bytes."""
-    ld = _rows(where, name, q.codes, rows, cols, device)
-    if q.scales.shape[0] > 1 and q.scales.stride(0) != 1:
-        _refuse(where, f"{name}'s scales must be dense")
-    return ld
-
-
 def _rowscale_c(where: str, q: Rowscale):
     """The library's view of a Rowscale (experts' rows one after the other)."""
     if q._c is None:
@@ -1014,6 +1007,16 @@ def _rowscale_c(where: str, q: Rowscale):
             _refuse(where, "scales must be dense")
         q._c = _Rowscale(codes.shape[0], codes.shape[1], ld, codes.data_ptr(), q.scales.data_ptr())
     return q._c
+
+
+def _rowscale_rows(where: str, name: str, q: Rowscale, rows, cols: int, device):
+    """Checks of a 2-d Rowscale; the library's view of it."""
+    if len(q.shape) != 2 or q.device != device or device.type != "cuda":
+        _refuse(where, f"{name} must be 2-d on {device}, got {len(q.shape)}-d on {q.device}")
+    c = q._c or _rowscale_c(where, q)
+    if c.cols != cols or (rows is not None and c.rows != rows):
+        _refuse(where, f"{name} has shape {tuple(q.shape)}, expected {(rows, cols)}", "SHAPE")
+    return c
 
 
 def rowscale_quantize(x, out: Optional[Rowscale] = None, stream=None) -> Rowscale:
@@ -1095,6 +1098,7 @@ def route(logits, top_k: int, renormalize: bool = True, stream=None) -> Routing:
         if len(_ROUTE_WS) > 4096:
             _ROUTE_WS.clear()
         nws = _ROUTE_WS[T, E, top_k] = int(_lib().bitsmoe_route_workspace_bytes(T, E, top_k))
+    # (an allocation each: parts of one cost the host more)
     i32 = torch.int32
     experts = torch.empty((T, top_k), dtype=i32, device=dev)
     places = torch.empty((T, top_k), dtype=i32, device=dev)
@@ -1113,7 +1117,7 @@ def route(logits, top_k: int, renormalize: bool = True, stream=None) -> Routing:
 def _matrices(where: str, name: str, w, device=None):
     """The library's view of the experts' matrices: a 3-d bf16 tensor or a Rowscale of 3-d codes."""
     if isinstance(w, Rowscale):
-        data, ty, scales = w.codes, _E4M3, w.scales
+        data, ty, scales = w.codes, _E4M3, w.scales   # (kept: matrices are used for long)
     else:
         data, ty, scales = w, 1, None
         if w.dtype is not _torch.bfloat16:
@@ -1167,8 +1171,8 @@ def expert_product(w, x, offsets, index=None, fan: int = 1, up=None, dtype=None,
     wc = _matrices(where, "w", w, dev)
     uc = _matrices(where, "up", up, dev) if up is not None else None
     if coded:
-        x_ld = _rowscale_rows(where, "x", x, None, wc.cols, dev)
-        x_rows, x_ptr, xs_ptr = x.codes.shape[0], x.codes.data_ptr(), x.scales.data_ptr()
+        xc = _rowscale_rows(where, "x", x, None, wc.cols, dev)
+        x_rows, x_ld, x_ptr, xs_ptr = xc.rows, xc.ld, xc.codes, xc.scales
     else:
         x_ld = _rows(where, "x", x, None, wc.cols, dev, torch.bfloat16)
         x_rows, x_ptr, xs_ptr = x.shape[0], x.data_ptr(), None

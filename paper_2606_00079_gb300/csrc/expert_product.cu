@@ -221,7 +221,7 @@ cudaError_t launch_plain(ExpertArgs a, int sms, cudaStream_t st) {
 //
 // A ring of stages of 128 bytes of the columns: warp 0 brings the matrices' tiles by TMA, eight warps the rows of x, wherever
 // they are, 16 bytes a thread at a time (cp.async; TMA's gather of four rows took 63 clocks for 512 bytes); their copies arrive
-// on a barrier by themselves, and warp 2 hands the stage on.  Warp 1 (of a pair's first CTA) issues the MMAs; eight warps empty
+// on a barrier by themselves (of a pair warp 2 hands that on to the first CTA).  Warp 1 (of a pair's first CTA) issues the MMAs; eight warps empty
 // the accumulators, two of them in turn where tensor memory holds two.  CTAs stay for all their tiles.  With few tiles the
 // columns are split over a cluster, whose CTAs add their partial tiles through distributed shared memory in rank order.
 // ---------------------------------------------------------------------------
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     prefetch_map(&wmap);
     if (GLU) prefetch_map(&umap);
     for (int i = 0; i < a.stages; ++i) {
-      mbar_init_n(s.full + i, 1 + kBoth);   // (a pair's first CTA's, for both: the matrices' bytes, x's rows of each)
+      mbar_init_n(s.full + i, 1 + (PAIR ? 2 : 32 * kXWarps));   // the matrices' bytes, x's rows (a pair's first CTA's: of both)
       mbar_init_n(s.xfull + i, 32 * kXWarps);
       mbar_init_n(s.empty + i, 1);
     }
@@ -362,6 +362,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         ok = mbar_try_wait(s.full + st, (uint32_t)u & 1u) || mbar_wait(s.full + st, (uint32_t)u & 1u, a.spin);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
+        if (!PAIR) fence_proxy_async();   // x's rows: generic writes -> tensor-core reads
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint64_t o = (uint64_t)((uint32_t)st * (stage >> 4));
 #pragma unroll
@@ -390,7 +391,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       mbar_wait(&s.drained, 0u);
     }
     __syncwarp();
-  } else if (wid == 2) {
+  } else if (PAIR && wid == 2) {
     if (lane == 0) {
       const uint32_t full0 = at0(s.full);
       int st = 0, u = 0;
@@ -435,7 +436,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             const int bytes = src[j] ? left : 0;
             cp_async16(dst + (uint32_t)j * (kXRows * 128u), bytes ? src[j] + b : static_cast<const uint8_t*>(a.x), bytes);
           }
-        cp_async_arrive(s.xfull + st);
+        cp_async_arrive((PAIR ? s.xfull : s.full) + st);
         if (++st == a.stages) {
           st = 0;
           ++u;
