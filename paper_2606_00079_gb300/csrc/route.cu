@@ -42,39 +42,38 @@ __device__ __forceinline__ float logit_of(uint32_t key) {   // order_key's inver
   return __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
 }
 
-// A token's logits as keys, of lane l those of experts l + 32 i: 0 where one cannot be selected.
+// A token's logits: lane l holds those of experts NE l + i.
 template <int NE>
-__device__ __forceinline__ void load_keys(const RouteArgs& a, int64_t t, int lane, uint32_t (&key)[NE]) {
-  const float* row = a.logits + t * a.ld;
+__device__ __forceinline__ void load_logits(const RouteArgs& a, int64_t t, int lane, uint32_t (&key)[NE]) {
+  const float* row = a.logits + t * a.ld + lane * NE;
 #pragma unroll
-  for (int i = 0; i < NE; ++i) {
-    const int e = lane + 32 * i;
-    key[i] = e < a.E ? __float_as_uint(__ldg(row + e)) : 0xFF800000u;
-  }
+  for (int i = 0; i < NE; ++i) key[i] = lane * NE + i < a.E ? __float_as_uint(__ldg(row + i)) : 0xFF800000u;
 }
-// One token's selection by a warp: lane j < k gets the j-th expert (-1: none) and its weight.  NE: logits a lane holds.
+// One token's selection by a warp: lane j < k gets the j-th expert (-1: none) and its weight.  Each lane offers its largest
+// logit (the first of equal ones); the largest offer of the lowest lane is the lowest expert's.
 template <int NE>
 __device__ __forceinline__ void select_token(const RouteArgs& a, int lane, uint32_t (&key)[NE], int& expert, float& weight) {
   constexpr uint32_t kNone = 0x007FFFFFu;   // -infinity's key, above NaN's
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
-    key[i] = order_key(__uint_as_float(key[i]));
+    key[i] = order_key(__uint_as_float(key[i]));   // 0 where one cannot be selected
     if (key[i] <= kNone) key[i] = 0u;
   }
   expert = -1;
-  weight = 0.f;
-  float top = 0.f, sum = 0.f;
+  float mine = 0.f, top = 0.f, sum = 0.f;
   for (int j = 0; j < a.k; ++j) {
-    uint32_t m = key[0];
+    uint32_t offer = key[0];
+    int at = 0;
 #pragma unroll
-    for (int i = 1; i < NE; ++i) m = max(m, key[i]);
-    const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, m);
+    for (int i = 1; i < NE; ++i)
+      if (key[i] > offer) {
+        offer = key[i];
+        at = i;
+      }
+    const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, offer);
     if (best == 0u) break;
-    uint32_t at = 0xFFFFFFFFu;
-#pragma unroll
-    for (int i = NE - 1; i >= 0; --i)
-      if (key[i] == best) at = lane + 32 * i;
-    at = __reduce_min_sync(0xFFFFFFFFu, at);
+    const int from = __ffs(__ballot_sync(0xFFFFFFFFu, offer == best)) - 1;
+    const int e = from * NE + __shfl_sync(0xFFFFFFFFu, at, from);
     const float v = logit_of(best);
     if (j == 0) {
       top = v;
@@ -86,13 +85,14 @@ __device__ __forceinline__ void select_token(const RouteArgs& a, int lane, uint3
       }
     }
     if (lane == j) {
-      expert = (int)at;
-      weight = expf(v - top);
+      expert = e;
+      mine = v;
     }
 #pragma unroll
     for (int i = 0; i < NE; ++i)
-      if ((int)at == lane + 32 * i) key[i] = 0u;
+      if (e == lane * NE + i) key[i] = 0u;
   }
+  weight = expert >= 0 ? expf(mine - top) : 0.f;
   if (a.renormalize) sum = warp_sum(weight);
   if (expert >= 0) weight /= sum;
 }
@@ -146,16 +146,16 @@ __device__ __forceinline__ void select_block(const RouteArgs& a, int first, int 
   for (int t0 = first; t0 < last; t0 += kChunk) {
     const int n = min(last - t0, kChunk);
     uint32_t key[NE], next[kAhead ? NE : 1];
-    if (kAhead && w < n) load_keys<NE>(a, t0 + w, lane, key);
+    if (kAhead && w < n) load_logits<NE>(a, t0 + w, lane, key);
     __syncthreads();
     for (int q = 0; w + 32 * q < n; ++q) {
       const int t = w + 32 * q;
       int expert;
       float weight;
       if constexpr (kAhead) {
-        if (t + 32 < n) load_keys<NE>(a, t0 + t + 32, lane, next);
+        if (t + 32 < n) load_logits<NE>(a, t0 + t + 32, lane, next);
       } else {
-        load_keys<NE>(a, t0 + t, lane, key);
+        load_logits<NE>(a, t0 + t, lane, key);
       }
       select_token<NE>(a, lane, key, expert, weight);
       if (lane < a.k) {
@@ -191,15 +191,12 @@ __device__ __forceinline__ void select_block(const RouteArgs& a, int first, int 
   __syncthreads();
 }
 
-// Places and pairs of a block's tokens once base[e] is where its first pair of expert e goes.
-__device__ __forceinline__ void place_block(const RouteArgs& a, int first, int last, const int* base) {
-  for (int64_t p = (int64_t)first * a.k + threadIdx.x; p < (int64_t)last * a.k; p += kRouteThreads) {
-    const int e = a.experts[p];
-    if (e < 0) continue;
-    const int at = base[e] + a.places[p];
-    a.places[p] = at;
-    a.pairs[at] = (int)p;
-  }
+// Place of pair p, of rank r among the block's of expert e, once base[e] is where the block's first one goes.
+__device__ __forceinline__ void place_pair(const RouteArgs& a, int64_t p, int e, int r, const int* base) {
+  if (e < 0) return;
+  const int at = base[e] + r;
+  a.places[p] = at;
+  a.pairs[at] = (int)p;
 }
 
 template <int NE>
@@ -211,7 +208,7 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_alone(const __grid_cons
   for (int e = threadIdx.x; e < a.E; e += kRouteThreads) a.offsets[e] = s.count[e];
   if (threadIdx.x == 0) a.offsets[a.E] = total;
   for (int p = total + threadIdx.x; p < a.T * a.k; p += kRouteThreads) a.pairs[p] = -1;
-  place_block(a, 0, a.T, s.count);
+  for (int p = threadIdx.x; p < a.T * a.k; p += kRouteThreads) place_pair(a, p, a.experts[p], a.places[p], s.count);
 }
 
 template <int NE>
@@ -230,16 +227,24 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_place(const __grid_cons
   for (int e = threadIdx.x; e < a.E; e += kRouteThreads) base[e] = start[e] = 0;
   __syncthreads();
   pdl_wait();
-  // threads take (expert, slice of the blocks)
+  const int64_t first = (int64_t)blockIdx.x * a.per * a.k, last = min(first + (int64_t)a.per * a.k, (int64_t)a.T * a.k);
+  // this thread's first pair, requested with the counts
+  const int64_t p0 = first + threadIdx.x;
+  const int e1 = p0 < last ? a.experts[p0] : -1, r1 = p0 < last ? a.places[p0] : 0;
+  // threads take (expert, slice of the blocks), their counts requested sixteen at a time
   const int ex = (a.E + 31) / 32 * 32, slices = max(1, kRouteThreads / ex);
   const int slice = threadIdx.x / ex, e0 = threadIdx.x % ex;
   if (slice < slices && e0 < a.E) {
     int before = 0, all = 0;
-#pragma unroll 4
-    for (int b = slice; b < (int)gridDim.x; b += slices) {
-      const int c = a.counts[(int64_t)b * a.E + e0];
-      all += c;
-      before += b < (int)blockIdx.x ? c : 0;
+    for (int b0 = slice; b0 < (int)gridDim.x; b0 += 16 * slices) {
+      int c[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c[i] = b0 + i * slices < (int)gridDim.x ? a.counts[(int64_t)(b0 + i * slices) * a.E + e0] : 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        all += c[i];
+        before += b0 + i * slices < (int)blockIdx.x ? c[i] : 0;
+      }
     }
     atomicAdd(base + e0, before);
     atomicAdd(start + e0, all);
@@ -255,8 +260,8 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_place(const __grid_cons
   for (int64_t p = total + (int64_t)blockIdx.x * kRouteThreads + threadIdx.x; p < (int64_t)a.T * a.k; p += (int64_t)gridDim.x * kRouteThreads)
     a.pairs[p] = -1;
   __syncthreads();
-  const int first = blockIdx.x * a.per;
-  place_block(a, first, min(first + a.per, a.T), base);
+  place_pair(a, p0, e1, r1, base);
+  for (int64_t p = p0 + kRouteThreads; p < last; p += kRouteThreads) place_pair(a, p, a.experts[p], a.places[p], base);
 }
 
 __global__ void k_route_none(int32_t* offsets, int E) {
