@@ -230,7 +230,6 @@ constexpr int kTcThreads = 32 * (4 + kXWarps + kOutWarps);   // warps: 0 matrice
 constexpr int kStagesMost = 8;
 constexpr uint32_t kATile = 2 * 128 * 128;   // bytes of a stage's tiles of the matrices
 constexpr int kTcShared = 227 * 1024;        // (all of an SM's, as of every kernel that allocates tensor memory)
-constexpr int kTurnPitch = 80;               // (64 bytes and 16, so that no two of eight rows meet in a bank)
 constexpr int kXRows = 4 * kXWarps;          // rows that one pass of x's warps brings
 
 struct TcShared {
@@ -238,7 +237,7 @@ struct TcShared {
   alignas(16) float factor[2][256];      // of the rows of y: x's scale, NaN for a row that is not there
   uint64_t full[kStagesMost], empty[kStagesMost], xfull[kStagesMost], afull[2], aempty[2], drained;
   uint32_t slot;
-  alignas(16) uint8_t turn[kOutWarps][16 * kTurnPitch];   // 16 rows of y of a warp's 32 results each, on their way out
+  alignas(16) uint8_t turn[kOutWarps][2][1024];   // 16 rows of y of a warp's 32 results each (of both tiles), on their way out
 };
 
 // What is stored for results that a wait that ran out has lost.  A warp whose wait ran out passes nothing on: who waits for
@@ -492,9 +491,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       } else if (a.y_vec) {
         // bf16 rows on 16-byte boundaries: rows lie along the lanes of tensor memory; turned by way of shared memory a row of y
         // goes out 16 bytes a lane
+        // (a row is 64 bytes; its 16-byte pieces are turned by its number, so that no two of eight rows meet in a bank)
         const int mw = m - lane;   // the warp's first row
-        uint8_t* turn = s.turn[wid - 4 - kXWarps];
-        const uint32_t put = smem_u32(turn) + (uint32_t)((lane >> 4) * 8 + (lane & 7)) * kTurnPitch + (uint32_t)(lane >> 3 & 1) * 16u;
+        uint8_t(*turn)[1024] = s.turn[wid - 4 - kXWarps];
+        const int pr = (lane >> 4) * 8 + (lane & 7);   // the row that this lane says the place of
+        const auto piece = [](int row, int i) { return row * 64 + ((i ^ (row >> 1 & 3)) << 4); };
         float sr[2][2][2];   // scales of the lane's rows 16 h + 8 i + l / 4 of both tiles
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -503,10 +504,13 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             sr[0][h][i] = F8 ? __shfl_sync(0xFFFFFFFFu, s0, 16 * h + 8 * i + (lane >> 2)) : 1.f;
             sr[1][h][i] = F8 ? __shfl_sync(0xFFFFFFFFu, s1, 16 * h + 8 * i + (lane >> 2)) : 1.f;
           }
-        for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
-          uint32_t d[2][2][8];
+        uint32_t d[2][2][8];
+        const auto load = [&](int c0) {
           tmem_ld_fragments(tl + (uint32_t)c0, d[0]);
           tmem_ld_fragments(tl + (uint32_t)(a.N + c0), d[1]);
+        };
+        if (16 * side < t.n) load(16 * side);
+        for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
           float2 f[2];
           f[0] = *reinterpret_cast<const float2*>(factor + c0 + 2 * (lane & 3));
           f[1] = *reinterpret_cast<const float2*>(factor + c0 + 8 + 2 * (lane & 3));
@@ -517,8 +521,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             return __uint_as_float(d[b][h][q]) * (F8 ? g * sr[b][h][q >> 1 & 1] : g);
           };
 #pragma unroll
-          for (int b = 0; b < (GLU ? 1 : 2); ++b) {
-            if (b) __syncwarp();
+          for (int b = 0; b < (GLU ? 1 : 2); ++b)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               uint32_t o[4];
@@ -532,13 +535,16 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
                 o[q >> 1] = *reinterpret_cast<const uint32_t*>(&p);
               }
-              store_transposed(put + (uint32_t)h * 32u, o[0], o[1], o[2], o[3]);
+              store_transposed(smem_u32(turn[b]) + (uint32_t)piece(pr, 2 * h + (lane >> 3 & 1)), o[0], o[1], o[2], o[3]);
             }
-            __syncwarp();
+          if (c0 + 32 < t.n) load(c0 + 32);   // (in flight while this one goes out)
+          __syncwarp();
+#pragma unroll
+          for (int b = 0; b < (GLU ? 1 : 2); ++b)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               const int c = 8 * i + (lane >> 2), col = mw + 128 * b + 8 * (lane & 3);
-              const uint4 p = lds128(turn + c * kTurnPitch + 16 * (lane & 3));
+              const uint4 p = lds128(turn[b] + piece(c, lane & 3));
               if (c0 + c < t.n && col < a.rows) {
                 __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y) + (int64_t)(t.p0 + c0 + c) * a.y_ld + col;
                 if (col + 8 <= a.rows) {
@@ -551,7 +557,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 }
               }
             }
-          }
           __syncwarp();
         }
       } else {
