@@ -232,8 +232,19 @@ constexpr uint32_t kATile = 2 * 128 * 128;   // bytes of a stage's tiles of the 
 constexpr int kTcShared = 227 * 1024;        // (all of an SM's, as of every kernel that allocates tensor memory)
 constexpr int kXRows = 4 * kXWarps;          // rows that one pass of x's warps brings
 
+// Pairs take the tiles in waves, a tile each.  Tiles differ (an expert's rows, shared among its tiles): in turn, the pair with
+// the most work had 10 to 15 % more than the average.  So warp 3 gives the largest tiles of a wave to the pairs that have had the
+// least so far.  Every CTA works that out for itself, for all pairs, ahead of its tiles.
+constexpr int kPairsMost = 96, kAhead = 4;   // waves whose tiles are known ahead
+struct Waves {
+  int keys[kPairsMost], loads[kPairsMost], by_rank[kPairsMost];   // of the tiles of a wave; of the pairs; work by the tiles' rank
+  int tile[kAhead];
+  uint64_t known[kAhead], done[kAhead];
+};
+
 struct TcShared {
   Groups groups;
+  Waves waves;
   alignas(16) float factor[2][256];      // of the rows of y: x's scale, NaN for a row that is not there
   uint64_t full[kStagesMost], empty[kStagesMost], xfull[kStagesMost], afull[2], aempty[2], drained;
   uint32_t slot;
@@ -259,6 +270,73 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
   return v;
+}
+
+// By one warp: this pair's tile of every wave (the first: its own number).
+__device__ __forceinline__ void plan_waves(const ExpertArgs& a, const Groups& g, Waves& s, int ntiles, int pairs, int pair, int unit) {
+  constexpr int kEach = kPairsMost / 32;
+  const int lane = threadIdx.x & 31;
+  const auto work = [&](int tile) {   // of a tile: its rows, and what a tile costs whatever they are
+    const int n = tile_of(a, g, tile, unit).n;
+    return max((n + unit - 1) / unit * unit, 96) + 16;
+  };
+  mbar_arrive(lane == 0, s.known);   // (the first wave's phase)
+  int load[kEach];   // of pairs lane + 32 i
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int p = lane + 32 * i;
+    load[i] = p < pairs && p < ntiles ? work(p) : 0;
+  }
+  for (int wave = 1; (int64_t)wave * pairs < ntiles; ++wave) {
+    if (wave >= kAhead && !mbar_wait_idle(s.done + wave % kAhead, (uint32_t)(wave / kAhead - 1) & 1u, 4 * (a.spin + kWaitClocks))) return;
+    const int t0 = wave * pairs, n = min(pairs, ntiles - t0);
+    int w[kEach], key[kEach], low = 0x7FFFFFFF;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (lane + 32 * i < pairs) low = min(low, load[i]);
+    low = __reduce_min_sync(0xFFFFFFFFu, low);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int p = lane + 32 * i;
+      load[i] -= low;
+      w[i] = p < n ? work(t0 + p) : 0;   // (a pair without a tile: last)
+      key[i] = w[i] * 128 + 127 - p;     // no two alike
+      if (p < pairs) {
+        s.keys[p] = key[i];
+        s.loads[p] = load[i] * 128 + p;
+      }
+    }
+    __syncwarp();
+    int tile_rank[kEach] = {}, load_rank[kEach] = {};
+    for (int q = 0; q < pairs; ++q) {
+      const int k = s.keys[q], l = s.loads[q];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        tile_rank[i] += k > key[i];
+        load_rank[i] += l < load[i] * 128 + lane + 32 * i;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (lane + 32 * i < pairs) s.by_rank[tile_rank[i]] = w[i];
+    __syncwarp();
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int p = lane + 32 * i;
+      if (p == pair) mine = load_rank[i];
+      if (p < pairs) load[i] += s.by_rank[load_rank[i]];
+    }
+    mine = __shfl_sync(0xFFFFFFFFu, mine, pair & 31);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int p = lane + 32 * i;
+      if (p < pairs && tile_rank[i] == mine) s.tile[wave % kAhead] = p < n ? t0 + p : ntiles;
+    }
+    __syncwarp();
+    mbar_arrive(lane == 0, s.known + wave % kAhead);
+  }
 }
 
 // SiLU(g) u with the fast exponential and quotient (2 units in the last place each).
@@ -293,6 +371,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       mbar_init_n(s.afull + i, 1);
       mbar_init_n(s.aempty + i, kBoth * kOutWarps);
     }
+    for (int i = 0; i < kAhead; ++i) {
+      mbar_init_n(s.waves.known + i, 1);
+      mbar_init_n(s.waves.done + i, kOutWarps);
+    }
     mbar_init_n(&s.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -312,13 +394,19 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const auto at0 = [&](const void* p) {   // the same place in a pair's first CTA, else here
     return PAIR ? cluster_address(smem_u32(p), 0) : smem_u32(p);
   };
+  // The tile after `tile`, this group's of wave `wave` (ntiles: none).
+  const auto next_tile = [&](int tile, int wave) {
+    if (!PAIR) return tile + step;
+    if ((int64_t)wave * step >= ntiles || !mbar_wait(s.waves.known + wave % kAhead, (uint32_t)(wave / kAhead) & 1u, a.spin)) return ntiles;
+    return *reinterpret_cast<volatile int*>(s.waves.tile + wave % kAhead);
+  };
   bool ok = true;
 
   if (wid == 0) {
     if (lane == 0) {
       const uint32_t full0 = at0(s.full);
       int st = 0, u = 0, n = 0;
-      for (int tile = first; tile < ntiles && ok; tile += step) {
+      for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
         const Tile t = tile_of(a, s.groups, tile, kUnit);
         const int m0 = (kBoth * t.m + half) * kRows;
         for (int i = 0; i < nk; ++i, ++n) {
@@ -348,8 +436,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       empty[r] = PAIR ? cluster_address(smem_u32(s.empty), (uint32_t)r) : smem_u32(s.empty);
       afull[r] = PAIR ? cluster_address(smem_u32(s.afull), (uint32_t)r) : smem_u32(s.afull);
     }
-    int st = 0, u = 0, buf = 0, use = 0, it = 0;
-    for (int tile = first; tile < ntiles && ok; tile += step, ++it) {
+    int st = 0, u = 0, buf = 0, use = 0;
+    for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
       const int n = (tile_of(a, s.groups, tile, kUnit).n + kUnit - 1) / kUnit * kUnit;
       const uint32_t idesc = idesc_of<F8, PAIR>(n);
       if (use > 0) ok = mbar_wait(s.aempty + buf, (uint32_t)(use - 1) & 1u, a.spin);
@@ -394,7 +482,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     if (lane == 0) {
       const uint32_t full0 = at0(s.full);
       int st = 0, u = 0;
-      for (int tile = first; tile < ntiles && ok; tile += step)
+      for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it))
         for (int i = 0; i < nk; ++i) {
           ok = mbar_wait(s.xfull + st, (uint32_t)u & 1u, a.spin);
           if (!ok) break;
@@ -407,13 +495,15 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         }
     }
     __syncwarp();
+  } else if (PAIR && wid == 3) {
+    plan_waves(a, s.groups, s.waves, ntiles, step, first, kUnit);
   } else if (wid >= 4 && wid < 4 + kXWarps) {
     const int g = tid - 128, chunk = g & 7, r0 = g >> 3;   // 16 bytes of rows r0 + kXRows j
     const uint32_t at = (uint32_t)r0 * 128u + (uint32_t)((chunk ^ (r0 & 7)) << 4);
     const int width = a.cols * (F8 ? 1 : 2);
     constexpr int kPasses = 256 / kBoth / kXRows;
     int st = 0, u = 0;
-    for (int tile = first; tile < ntiles && ok; tile += step) {
+    for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
       const Tile t = tile_of(a, s.groups, tile, kUnit);
       const int mine = (t.n + kUnit - 1) / kUnit * kUnit / kBoth;   // rows of this CTA
       const uint8_t* src[kPasses];
@@ -447,8 +537,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   } else if (wid >= 4 + kXWarps) {
     const int quarter = wid & 3, side = (wid - 4 - kXWarps) >> 2;
     const uint32_t aempty0 = at0(s.aempty);
-    int buf = 0, use = 0, it = 0;
-    for (int tile = first; tile < ntiles; tile += step, ++it) {
+    int buf = 0, use = 0;
+    for (int tile = first, it = 0; tile < ntiles; tile = next_tile(tile, ++it)) {
       const Tile t = tile_of(a, s.groups, tile, kUnit);
       float* factor = s.factor[it & 1];
       {
@@ -582,6 +672,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(aempty0 + 8u * (uint32_t)buf);
+      if (PAIR) mbar_arrive(lane == 0, s.waves.done + it % kAhead);   // (everyone else is past this tile, or has given up)
       if (++buf == a.nbuf) {
         buf = 0;
         ++use;
@@ -719,7 +810,7 @@ cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um
   a.sps = (a.nk + a.splits - 1) / a.splits;
   const size_t room = kTcShared - 1024 - sizeof(TcShared) - (a.splits > 1 ? (size_t)a.N * 1024 : 0);
   a.stages = std::min(kStagesMost, (int)(room / (kATile + (size_t)a.N * (pair ? 64 : 128))));
-  if (pair) return launch_tc_as<F8, GLU, true>(a, wm, um, std::min<int64_t>(most, sms / 2), dev, st);
+  if (pair) return launch_tc_as<F8, GLU, true>(a, wm, um, std::min<int64_t>({most, sms / 2, kPairsMost}), dev, st);
   return launch_tc_as<F8, GLU, false>(a, wm, um, std::min<int64_t>(most, sms / a.splits), dev, st);
 }
 
