@@ -47,9 +47,11 @@ struct ExpertArgs {
 
 __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + expf(-g)) * u; }
 
+__device__ __forceinline__ void keep(float* y, float v) { *y = v; }
+__device__ __forceinline__ void keep(__nv_bfloat16* y, float v) { *y = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void store_y(void* y, int type, int64_t i, float v) {
-  if (type == BITSMOE_F32) static_cast<float*>(y)[i] = v;
-  else static_cast<__nv_bfloat16*>(y)[i] = __float2bfloat16_rn(v);
+  if (type == BITSMOE_F32) keep(static_cast<float*>(y) + i, v);
+  else keep(static_cast<__nv_bfloat16*>(y) + i, v);
 }
 
 // ---------------------------------------------------------------------------
@@ -219,14 +221,19 @@ cudaError_t launch_plain(ExpertArgs a, int sms, cudaStream_t st) {
 // expert's few rows cost an MMA of few columns.  With many rows two CTAs are a pair (cta_group::2): each brings half of the
 // rows of x for both.
 //
-// A ring of stages of 128 bytes of the columns: warp 0 brings the matrices' tiles by TMA, eight warps the rows of x, wherever
+// A ring of stages of 128 bytes of the columns: warp 0 brings the matrices' tiles by TMA, four warps the rows of x, wherever
 // they are, 16 bytes a thread at a time (cp.async; TMA's gather of four rows took 63 clocks for 512 bytes); their copies arrive
 // on a barrier by themselves (of a pair warp 2 hands that on to the first CTA).  Warp 1 (of a pair's first CTA) issues the MMAs; eight warps empty
 // the accumulators, two of them in turn where tensor memory holds two.  CTAs stay for all their tiles.  With few tiles the
 // columns are split over a cluster, whose CTAs add their partial tiles through distributed shared memory in rank order.
 // ---------------------------------------------------------------------------
-constexpr int kXWarps = 8, kOutWarps = 8, kOutThreads = 32 * kOutWarps;
-constexpr int kTcThreads = 32 * (4 + kXWarps + kOutWarps);   // warps: 0 matrices, 1 MMA, 2 rows of x that are there, 4.. rows of x, results
+// Warps: 0 matrices, 1 MMA, 2 rows of x that are there (of a pair), 3 the tiles to come (of a pair), four of rows of x, eight of
+// results.  (Eight of x's fill a stage faster, 685 clocks in place of 780 of the MMAs' 1024, but many large products are bound
+// by the card's power, and warps that wait draw it: 4096 rows of y of 14336 x 4096 in 8 bits at a stretch 386 us with eight, 380
+// with four.)
+constexpr int kXWarps = 4, kOutWarps = 8, kOutThreads = 32 * kOutWarps;
+constexpr int kTcThreads = 32 * (4 + kXWarps + kOutWarps);
+constexpr int kFewRows = 64;                 // rows of y of a tile from which on pairs take it
 constexpr int kStagesMost = 8;
 constexpr uint32_t kATile = 2 * 128 * 128;   // bytes of a stage's tiles of the matrices
 constexpr int kTcShared = 227 * 1024;        // (all of an SM's, as of every kernel that allocates tensor memory)
@@ -501,7 +508,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const int g = tid - 128, chunk = g & 7, r0 = g >> 3;   // 16 bytes of rows r0 + kXRows j
     const uint32_t at = (uint32_t)r0 * 128u + (uint32_t)((chunk ^ (r0 & 7)) << 4);
     const int width = a.cols * (F8 ? 1 : 2);
-    constexpr int kPasses = 256 / kBoth / kXRows;
+    constexpr int kPasses = (PAIR ? 128 : kFewRows) / kXRows;
     int st = 0, u = 0;
     for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
       const Tile t = tile_of(a, s.groups, tile, kUnit);
@@ -650,24 +657,28 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           __syncwarp();
         }
       } else {
-        for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
-          uint32_t v[2][16];
-          tmem_ld16(tl + (uint32_t)c0, v[0]);
-          tmem_ld16(tl + (uint32_t)(a.N + c0), v[1]);
-          const int64_t at = (int64_t)(t.p0 + c0) * a.y_ld + m;
+        const auto go_out = [&](auto* y) {   // a row of the matrix a lane
+          for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
+            uint32_t v[2][16];
+            tmem_ld16(tl + (uint32_t)c0, v[0]);
+            tmem_ld16(tl + (uint32_t)(a.N + c0), v[1]);
 #pragma unroll
-          for (int q = 0; q < 16; ++q) {
-            const float f = factor[c0 + q];
-            const float v0 = __uint_as_float(v[0][q]) * (F8 ? s0 * f : f), v1 = __uint_as_float(v[1][q]) * (F8 ? s1 * f : f);
-            if (c0 + q >= t.n) continue;
-            if constexpr (GLU) {
-              if (in0) store_y(a.y, a.y_type, at + q * a.y_ld, silu_fast(v0, v1));
-            } else {
-              if (in0) store_y(a.y, a.y_type, at + q * a.y_ld, v0);
-              if (in1) store_y(a.y, a.y_type, at + q * a.y_ld + 128, v1);
+            for (int q = 0; q < 16; ++q) {
+              const float f = factor[c0 + q];
+              const float v0 = __uint_as_float(v[0][q]) * (F8 ? s0 * f : f), v1 = __uint_as_float(v[1][q]) * (F8 ? s1 * f : f);
+              if (c0 + q >= t.n) continue;
+              auto* at = y + (int64_t)(t.p0 + c0 + q) * a.y_ld + m;
+              if constexpr (GLU) {
+                if (in0) keep(at, silu_fast(v0, v1));
+              } else {
+                if (in0) keep(at, v0);
+                if (in1) keep(at + 128, v1);
+              }
             }
           }
-        }
+        };
+        if (a.y_type == BITSMOE_F32) go_out(static_cast<float*>(a.y));
+        else go_out(static_cast<__nv_bfloat16*>(a.y));
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
@@ -795,7 +806,7 @@ cudaError_t launch_tc_as(const ExpertArgs& a, const CUtensorMap& wm, const CUten
 template <bool F8, bool GLU>
 cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um, int dev, int sms, cudaStream_t st) {
   a.N = tile_rows(a.P, a.E);
-  const bool pair = a.N > 64;
+  const bool pair = a.N > kFewRows;
   const int rows = (GLU ? 128 : 256) * (pair ? 2 : 1);
   a.mt = (a.rows + rows - 1) / rows;
   a.nk = (a.cols + (F8 ? 127 : 63)) / (F8 ? 128 : 64);
