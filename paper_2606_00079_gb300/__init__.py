@@ -935,7 +935,7 @@ class Rowscale:
     """Rows in 8 bits on the device: `codes` (torch.float8_e4m3fn, rows x cols, or experts x rows x cols with dense
     rows) and `scales` (float32, one for each row); value = code * scale, see bitsmoe_rowscale in include/bitsmoe.h."""
 
-    __slots__ = ("_codes", "_scales", "_buf", "_c", "shape", "device")   # _c: what the library reads, formed when first needed
+    __slots__ = ("codes", "scales", "_c", "shape", "device")   # _c: what the library reads, formed when first needed
 
     def __init__(self, codes, scales):
         torch = _torch or _load_torch()
@@ -947,7 +947,7 @@ class Rowscale:
             _refuse("Rowscale", f"scales have shape {tuple(scales.shape)}, codes {tuple(codes.shape)}", "SHAPE")
         if scales.shape[-1] > 1 and scales.stride(-1) != 1:
             _refuse("Rowscale", "scales must be dense along the rows")
-        self._codes, self._scales, self._buf, self._c = codes, scales, None, None
+        self.codes, self.scales, self._c = codes, scales, None
         self.shape, self.device = codes.shape, codes.device
 
     @classmethod
@@ -961,29 +961,14 @@ class Rowscale:
         if n > _MAX_ROWS or cols > _MAX_ROWS:
             _refuse("Rowscale.empty", f"shape {tuple(shape)}", "SHAPE")
         pitch = (cols + 15) & ~15
-        self = cls.__new__(cls)   # one allocation for both; the tensors are made when asked for
-        self._buf = buf = torch.empty(n * pitch + 4 * n, dtype=torch.uint8,
-                                      device=device if device is not None else torch.cuda.current_device())
-        self._codes = self._scales = None
-        self.shape, self.device = shape, buf.device
-        base = buf.data_ptr()
-        self._c = _Rowscale(n, cols, pitch, base, base + n * pitch)
+        dev = device if device is not None else torch.cuda.current_device()
+        self = cls.__new__(cls)   # (an allocation each: parts of one cost the host more)
+        codes = torch.empty((*shape[:-1], pitch), dtype=torch.float8_e4m3fn, device=dev)
+        self.codes = codes if pitch == cols else codes[..., :cols]
+        self.scales = scales = torch.empty(shape[:-1], dtype=torch.float32, device=dev)
+        self.shape, self.device = shape, codes.device
+        self._c = _Rowscale(n, cols, pitch, codes.data_ptr(), scales.data_ptr())
         return self
-
-    @property
-    def codes(self):
-        if self._codes is None:
-            c = self._c
-            flat = self._buf[:c.rows * c.ld].view(_torch.float8_e4m3fn)
-            self._codes = flat.view(*self.shape[:-1], c.ld)[..., :c.cols]
-        return self._codes
-
-    @property
-    def scales(self):
-        if self._scales is None:
-            c = self._c
-            self._scales = self._buf[c.rows * c.ld:].view(_torch.float32).view(self.shape[:-1])
-        return self._scales
 
 
 def _flat(where: str, name: str, x):
