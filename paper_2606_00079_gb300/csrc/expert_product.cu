@@ -390,6 +390,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     else tmem_alloc(&s.slot, 512);
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  pdl_trigger();   // (the next such kernel may get ready on SMs that are free)
+  pdl_wait();      // nothing above reads or writes global memory: the kernel before may still run
   read_groups<kTcThreads>(a, s.groups);   // (with barriers of the block)
   if constexpr (PAIR) {
     __syncwarp();
@@ -789,17 +791,19 @@ cudaError_t launch_tc_as(const ExpertArgs& a, const CUtensorMap& wm, const CUten
   const cudaError_t e = allow_shared<k_expert_tc<F8, GLU, PAIR>>(dev, kTcShared);
   if (e != cudaSuccess) return e;
   const unsigned size = PAIR ? 2u : (unsigned)a.splits;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = size;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = size;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(size * (unsigned)groups);
   cfg.blockDim = dim3(kTcThreads);
   cfg.dynamicSmemBytes = kTcShared;
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = size > 1 ? 1 : 0;
+  cfg.numAttrs = size > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, wm, um, a);
 }
 

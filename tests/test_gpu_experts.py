@@ -342,15 +342,21 @@ def test_expert_product_in_a_graph_and_on_a_stream(env):
     assert torch.equal(a[:n], y[:n])
 
 
+# experts, rows of a matrix, columns, rows of y, first rows of y and of the matrices that are lost with block 0's first tile:
+# pairs (many rows an expert), single CTAs (few), columns split over a cluster (few tiles: all of the tile is lost)
+LOST = {"pairs": (12, 700, 4096, 1200, 64, 128), "single": (80, 520, 4096, 400, 5, 128), "split": (3, 520, 8192, 15, 5, 128)}
+
+
+@pytest.mark.parametrize("kind", sorted(LOST))
 @pytest.mark.parametrize("ty", ["bf16", "e4m3"])
 @pytest.mark.parametrize("glu", [False, True])
 @pytest.mark.parametrize("fan", [0, 2])
-def test_expert_product_lost_waits(env, ty, glu, fan):
+def test_expert_product_lost_waits(env, kind, ty, glu, fan):
     """An arrival of block 0 is left out, so that its waits run out: the call reports it, what it lost is NaN, every other
     result stands, and the next call is as ever."""
     torch, bm = env
     g = torch.Generator().manual_seed(8)
-    E, R, C, P = 12, 192, 4096, 240
+    E, R, C, P, rows, cols = LOST[kind]
     w, ws, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
     up, us, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty) if glu else (None, None, None)
     x, xs, _ = pitched(torch, torch.randn(P, C, generator=g), ty)
@@ -362,7 +368,7 @@ def test_expert_product_lost_waits(env, ty, glu, fan):
     ref = bm.expert_product(w, x, off, **kw)
     for dt in (torch.float32, torch.bfloat16):
         for with_status in (True, False):
-            buf = torch.full((P, R + 5), 7.0, dtype=dt, device="cuda")
+            buf = torch.full((P, R + 8), 7.0, dtype=dt, device="cuda")
             y, status = buf[:, :R], torch.zeros(1, dtype=torch.int32, device="cuda")
             bm.bitsmoe_debug_wait_limit(1, 2_000_000)
             try:
@@ -372,12 +378,102 @@ def test_expert_product_lost_waits(env, ty, glu, fan):
                 bm.bitsmoe_debug_wait_limit(0, 0)
             assert int(status.item()) == (bm.ERR_CODE["TIMEOUT"] if with_status else 0)
             lost = torch.isnan(y)
-            assert bool(lost.any()) and not bool(lost.all())
+            assert bool(lost[:rows, :cols].all()) and not bool(lost.all())
             assert torch.equal(y[~lost], ref.to(dt)[~lost])
             assert (buf[:, R:] == 7).all()
             status.zero_()
             assert torch.equal(bm.expert_product(w, x, off, y=y, status=status, **kw), ref.to(dt))
             assert int(status.item()) == 0
+
+
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("R", [64, 250, 256, 300, 1000])
+@pytest.mark.parametrize("shift", [0, 1, 8])
+def test_expert_product_16_bit_results(env, ty, R, shift):
+    """bf16 rows of y on 16-byte boundaries (turned on their way out) and off them: the same bits, and the fp32 results
+    rounded once; nothing beside them is touched."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(R)
+    C = 320
+    w, ws, _ = pitched(torch, torch.randn(4, R, C, generator=g), ty)
+    up, us, _ = pitched(torch, torch.randn(4, R, C, generator=g), ty)
+    x, xs, _ = pitched(torch, torch.randn(700, C, generator=g), ty)
+    off = torch.tensor([1, 3, 300, 300, 698], dtype=torch.int32).cuda()
+    for u_ in (None, wrap(bm, up, us)):
+        f = torch.full((700, R), 7.0, device="cuda")
+        bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, up=u_, y=f)
+        buf = torch.full((700, (R + 24) // 8 * 8 + (1 if shift == 1 else 0)), 7.0, dtype=torch.bfloat16, device="cuda")
+        y = buf[:, shift:shift + R]
+        bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, up=u_, y=y)
+        assert torch.equal(y, f.bfloat16())
+        rest = buf.clone()
+        rest[:, shift:shift + R] = 7.0
+        assert (rest == 7).all() and (y[0] == 7).all() and (y[698:] == 7).all()
+
+
+def test_expert_product_waves_of_unequal_tiles(env):
+    """Many waves of tiles of all sizes: every row's result, whoever had it."""
+    torch, bm = env
+    rng = np.random.default_rng(11)
+    counts = rng.integers(0, 900, 40)
+    counts[rng.random(40) < 0.2] = 0
+    E, R, C = 40, 1300, 64
+    off = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).cuda()
+    P = int(off[-1])
+    w = torch.randn(E, R, C, device="cuda").to(torch.bfloat16)
+    x = torch.randn(P, C, device="cuda").to(torch.bfloat16)
+    for up in (None, torch.randn(E, R, C, device="cuda").to(torch.bfloat16)):
+        y = bm.expert_product(w, x, off, up=up)
+        o = off.tolist()
+        for e in range(E):
+            if o[e] == o[e + 1]:
+                continue
+            xr = x[o[e]:o[e + 1]].float()
+            a = xr @ w[e].float().T
+            m = xr.abs() @ w[e].float().abs().T
+            if up is not None:
+                b = xr @ up[e].float().T
+                want = a / (1 + torch.exp(-a)) * b
+                tol = (C + 16) * 2.0 ** -22 * (1.1 * m * b.abs() + a.abs() * (xr.abs() @ up[e].float().abs().T)) + 1e-5 * want.abs()
+            else:
+                want, tol = a, (C + 16) * 2.0 ** -22 * m
+            assert ((y[o[e]:o[e + 1]] - want).abs() <= tol).all(), e
+
+
+def test_expert_products_beside_the_forward_on_another_stream(env):
+    """Kernels of one stream wait inside pairs and clusters and hold whole SMs; forwards of the tensor-core projections and
+    microscaled products run on another: every result as alone."""
+    import synth
+    torch, bm = env
+    spec = synth.scaled_spec(synth.WORKLOADS["tiny"], D=256, E=8, I=256, n=128, group=128, top_k=2)
+    L = bm.bitsmoe_pack(synth.make_layer(spec, seed=5, bits_dist={0: .1, 1: .2, 2: .4, 3: .2, 4: .1}), device=0)
+    xf, logits = synth.make_inputs(spec, 40, seed=5)
+    xd, ld = torch.from_numpy(xf.view(np.int16)).cuda(), torch.from_numpy(logits).cuda()
+    ws = bm.Workspace(L, 40, spec.top_k)
+    y_ref = bm.moe_forward(L, xd, ld, spec.top_k, ws).clone()
+    mw = bm.microscale_quantize(torch.randn(300, 4096, device="cuda"))
+    mx = torch.randn(40, 4096, device="cuda").to(torch.bfloat16)
+    m_ref = bm.microscale_product(mw, mx)
+    cases = []
+    for E, R, C, P in ((3, 520, 2048, 15), (40, 520, 512, 200), (6, 700, 512, 1500)):
+        w = torch.randn(E, R, C, device="cuda").to(torch.bfloat16)
+        x = torch.randn(P, C, device="cuda").to(torch.bfloat16)
+        off = torch.arange(0, P + 1, P // E, dtype=torch.int32).cuda()
+        cases.append((w, x, off, bm.expert_product(w, x, off, up=w)))
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    got, other = [], []
+    for _ in range(30):
+        with torch.cuda.stream(st):
+            for w, x, off, ref in cases:
+                got.append((bm.expert_product(w, x, off, up=w), ref))
+        other.append((bm.moe_forward(L, xd, ld, spec.top_k, ws).clone(), y_ref))
+        other.append((bm.microscale_product(mw, mx), m_ref))
+    torch.cuda.synchronize()
+    for a, b in got:
+        assert torch.equal(a, b)
+    for a, b in other:
+        torch.testing.assert_close(a, b, rtol=1e-4, atol=1e-5)
 
 
 # ---------------------------------------------------------------------------
