@@ -34,6 +34,7 @@ struct ExpertArgs {
   const void* x;
   const float* xs;
   int64_t x_ld;
+  int x_vec;             // rows of x start on 16-byte boundaries
   void* y;
   int y_type, y_vec;     // y_vec: bf16 rows on 16-byte boundaries
   int64_t y_ld;
@@ -268,6 +269,30 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int by
 // An arrival of this thread once its copies so far are there.
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// Bytes [0, n) from any address as 16, the rest zeros: the aligned 16 bytes that hold them (each holds one of them, so it
+// can be read), shifted.
+__device__ __forceinline__ uint4 load16_anywhere(const uint8_t* p, int n) {
+  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15);
+  const uint4* q = reinterpret_cast<const uint4*>(p - off);
+  uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+  if (n > 0) a = __ldg(q);
+  if ((int)off + n > 16) b = __ldg(q + 1);
+  uint32_t w[9] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, 0u};
+  if (off & 8)
+#pragma unroll
+    for (int i = 0; i < 7; ++i) w[i] = i + 2 < 9 ? w[i + 2] : 0u;
+  if (off & 4)
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 1];
+  const uint32_t sh = (off & 3) * 8;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = __funnelshift_r(w[i], w[i + 1], sh);
+    const int left = n - 4 * i;   // bytes of this word that count
+    if (left < 4) w[i] &= left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ void cluster_sync() {   // converged warps
   asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
@@ -528,13 +553,24 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (!ok) break;
         const uint32_t dst = smem_u32(sm) + (uint32_t)st * stage + kATile + at;
         const int b = (k0 + i) * 128, left = min(max(width - b - chunk * 16, 0), 16);
+        uint64_t* there = (PAIR ? s.xfull : s.full) + st;
+        if (a.x_vec) {
 #pragma unroll
-        for (int j = 0; j < kPasses; ++j)
-          if (r0 + kXRows * j < mine) {
-            const int bytes = src[j] ? left : 0;
-            cp_async16(dst + (uint32_t)j * (kXRows * 128u), bytes ? src[j] + b : static_cast<const uint8_t*>(a.x), bytes);
-          }
-        cp_async_arrive((PAIR ? s.xfull : s.full) + st);
+          for (int j = 0; j < kPasses; ++j)
+            if (r0 + kXRows * j < mine) {
+              const int bytes = src[j] ? left : 0;
+              cp_async16(dst + (uint32_t)j * (kXRows * 128u), bytes ? src[j] + b : static_cast<const uint8_t*>(a.x), bytes);
+            }
+          cp_async_arrive(there);
+        } else {   // rows off 16-byte boundaries
+#pragma unroll
+          for (int j = 0; j < kPasses; ++j)
+            if (r0 + kXRows * j < mine) {
+              const uint4 v = load16_anywhere(src[j] ? src[j] + b : static_cast<const uint8_t*>(a.x), src[j] ? left : 0);
+              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst + (uint32_t)j * (kXRows * 128u)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+            }
+          mbar_arrive(there);
+        }
         if (++st == a.stages) {
           st = 0;
           ++u;
@@ -751,7 +787,7 @@ int64_t pitch_of(int64_t ld, int64_t cols, int64_t size, int64_t rows) {   // (o
 // Whether the tensor-core kernel takes these rows; its maps.
 bool tc_maps(const ExpertArgs& a, bool f8, CUtensorMap* wm, CUtensorMap* um) {
   const int64_t es = f8 ? 1 : 2;
-  if (a.x_rows < 1 || !on_boundaries(a.x, a.x_ld, es, a.x_rows)) return false;
+  if (a.x_rows < 1) return false;
   const int box = a.up ? 128 : 256;
   const auto matrices = [&](CUtensorMap* m, const void* p, int64_t ld, int64_t eld) {
     return on_boundaries(p, ld, es, a.rows) && make_matrices_map(m, f8, p, a.E, a.rows, a.cols, pitch_of(ld, a.cols, es, a.rows), eld * es, box);
@@ -899,6 +935,7 @@ extern "C" int bitsmoe_expert_product(const bitsmoe_expert_product_args* args, v
   a.lose = debug_skip_arrival();
   a.status = g.status;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  a.x_vec = on_boundaries(g.x, g.x_ld, f8 ? 1 : 2, g.x_rows);
   CUtensorMap wm, um;
   if (tc_maps(a, f8, &wm, &um)) {
     if (!a.up) um = wm;

@@ -210,6 +210,29 @@ def test_expert_product_off_the_boundaries(env, ty, glu, fan):
     run_product(env, [5, 0, 70, 1], 67, 129, ty, glu, fan, out="f32", shift=1, lead=1, tail=1)
 
 
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("counts,R,C", [([1], 64, 64), ([5, 0, 70, 1], 67, 129), ([300, 2], 300, 517), ([3, 9], 40, 4095), ([2], 33, 1)])
+@pytest.mark.parametrize("shift", [1, 3, 8, 15])
+def test_expert_product_rows_of_x_off_the_boundaries(env, ty, counts, R, C, shift):
+    """Matrices on 16-byte boundaries, rows of x anywhere: the bits of the same rows on boundaries."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(C)
+    E, P = len(counts), sum(counts)
+    w, ws, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
+    up, us, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
+    x, xs, _ = pitched(torch, torch.randn(P, C, generator=g), ty)
+    raw = torch.full((P, C + 17), 127, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) if ty == "e4m3" else torch.full(
+        (P, C + 17), float("nan"), dtype=torch.bfloat16, device="cuda")   # (NaN between the rows)
+    off_x = raw[:, shift:shift + C]
+    (off_x.view(torch.uint8) if ty == "e4m3" else off_x).copy_(x.view(torch.uint8) if ty == "e4m3" else x)
+    off = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).cuda()
+    idx = torch.randint(0, 2 * P, (P,), generator=g, dtype=torch.int32).cuda()
+    for kw in (dict(), dict(index=idx, fan=2, up=wrap(bm, up, us))):
+        a = bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, **kw)
+        b = bm.expert_product(wrap(bm, w, ws), wrap(bm, off_x, xs), off, **kw)
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("E,most,R,C,ty,glu", [(128, 6, 96, 256, "bf16", True), (300, 3, 40, 128, "e4m3", False), (1024, 2, 16, 64, "bf16", False),
                                                (60, 40, 320, 512, "e4m3", True), (7, 400, 384, 256, "bf16", True), (5, 600, 520, 384, "e4m3", False)])
 def test_expert_product_many_experts_and_tiles(env, E, most, R, C, ty, glu):
@@ -602,3 +625,40 @@ def test_refusals_of_the_binding(env):
                dict(w=w.transpose(1, 2)), dict(x=x.cpu())):
         with pytest.raises(bm.BitsMoEError):
             bm.expert_product(**{**ok, **kw})
+
+
+FIRST = """
+import sys, torch
+sys.path.insert(0, sys.argv[1])
+import paper_2606_00079_gb300 as bm
+torch.cuda.set_device(0)
+T, E, k, D, I = int(sys.argv[2]), 8, 2, 256, 192
+w, up = (torch.randn(E, I, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+logits, h = torch.randn(T, E, device="cuda"), torch.randn(T, D, device="cuda")
+dn = torch.randn(E, D, I, device="cuda")
+def step():
+    _, x = bm.block_norm(h, x_dtype=torch.float8_e4m3fn)
+    xd = bm.rowscale_dequantize(x, torch.bfloat16)
+    r = bm.route(logits, k)
+    a = bm.expert_product(w, xd, r.offsets, index=r.pairs, fan=k, up=up)
+    y = bm.expert_product(bm.rowscale_quantize(dn), bm.rowscale_quantize(a), r.offsets)
+    return bm.expert_combine(y, r.places, r.weights, base=h)
+g = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(g):
+    out = step()
+g.replay()
+torch.cuda.synchronize()
+assert torch.equal(out, step()) and bool(torch.isfinite(out).all())
+print("same")
+"""
+
+
+@pytest.mark.parametrize("T", [3, 400])
+def test_first_calls_inside_a_capture(env, T):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST, root, str(T)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
