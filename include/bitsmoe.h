@@ -761,11 +761,9 @@ typedef struct bitsmoe_expert_matrices {
  *              of the kernel ran out; not cleared by the call.  The results that such a
  *              wait has lost are NaN, with and without it
  * Products are exact and sums fp32; scales multiply the finished sums (which have to
- * stay in fp32's range before and after it); y is rounded once.  w and up whose rows (and
- * matrices) all start on 16-byte boundaries go through the tensor cores; others are
- * multiplied by fp32 instructions, many times slower.  x's rows may start anywhere (on
- * 16-byte boundaries they are read fastest; of others the aligned 16 bytes at a row's two
- * ends are read whole).  Errors: INVALID_ARG, SHAPE,
+ * stay in fp32's range before and after it); y is rounded once.  w, up and x may start
+ * anywhere (all rows, and matrices, on 16-byte boundaries are read fastest; of others the
+ * aligned 16 bytes at a row's two ends are read whole).  Errors: INVALID_ARG, SHAPE,
  * ALIGNMENT, CUDA.  Never allocates, never synchronises; one launch.  P == 0 and rows == 0
  * are successful no-ops. */
 typedef struct bitsmoe_expert_product_args {

@@ -34,7 +34,7 @@ struct ExpertArgs {
   const void* x;
   const float* xs;
   int64_t x_ld;
-  int x_vec;             // rows of x start on 16-byte boundaries
+  int w_vec, x_vec;      // rows of the matrices, rows of x start on 16-byte boundaries
   void* y;
   int y_type, y_vec;     // y_vec: bf16 rows on 16-byte boundaries
   int64_t y_ld;
@@ -45,8 +45,6 @@ struct ExpertArgs {
   int lose;
   int* status;
 };
-
-__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + expf(-g)) * u; }
 
 __device__ __forceinline__ void keep(float* y, float v) { *y = v; }
 __device__ __forceinline__ void keep(__nv_bfloat16* y, float v) { *y = __float2bfloat16_rn(v); }
@@ -132,92 +130,7 @@ __device__ __forceinline__ int row_of(const ExpertArgs& a, int p) {
 }
 
 // ---------------------------------------------------------------------------
-// Rows on any boundary: tiles of 64 x 64 by fp32 instructions.
-// ---------------------------------------------------------------------------
-constexpr int kPlainThreads = 256, kPlainTile = 64, kPlainK = 16;
-
-template <bool F8>
-__device__ __forceinline__ float element_at(const void* p, int64_t i) {
-  if constexpr (F8) return e4m3_values((uint32_t)__ldg(static_cast<const uint8_t*>(p) + i)).x;
-  else return __uint_as_float((uint32_t)__ldg(static_cast<const uint16_t*>(p) + i) << 16);
-}
-
-template <bool F8, bool GLU>
-__global__ void __launch_bounds__(kPlainThreads) k_expert_plain(const __grid_constant__ ExpertArgs a) {
-  constexpr int NA = GLU ? 2 : 1;
-  __shared__ Groups s;
-  __shared__ __align__(16) float xt[kPlainK][kPlainTile + 4], wt[NA][kPlainK][kPlainTile + 4];
-  read_groups<kPlainThreads>(a, s);
-  const int tid = threadIdx.x, lr = tid >> 2, lk = (tid & 3) * 4;   // what a thread brings: 4 columns of a row
-  const int tr = (tid & 15) * 4, tp = (tid >> 4) * 4;               // what it sums: 4 rows of the matrix x 4 of y
-  const int ntiles = s.tiles[a.E] * a.mt;
-  for (int tile = blockIdx.x; tile < ntiles; tile += gridDim.x) {
-    const Tile t = tile_of(a, s, tile, 1);
-    const int m = t.m * kPlainTile + lr, q = lr < t.n ? row_of(a, t.p0 + lr) : -1;
-    float acc[NA][4][4];
-#pragma unroll
-    for (int i = 0; i < NA * 16; ++i) (&acc[0][0][0])[i] = 0.f;
-    for (int k0 = 0; k0 < a.cols; k0 += kPlainK) {
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int k = k0 + lk + i;
-        xt[lk + i][lr] = q >= 0 && k < a.cols ? element_at<F8>(a.x, q * a.x_ld + k) : 0.f;
-        wt[0][lk + i][lr] = m < a.rows && k < a.cols ? element_at<F8>(a.w, t.e * a.w_eld + m * a.w_ld + k) : 0.f;
-        if constexpr (GLU) wt[NA - 1][lk + i][lr] = m < a.rows && k < a.cols ? element_at<F8>(a.up, t.e * a.u_eld + m * a.u_ld + k) : 0.f;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < kPlainK; ++k) {
-        const float4 xv = *reinterpret_cast<const float4*>(&xt[k][tp]);
-        const float xa[4] = {xv.x, xv.y, xv.z, xv.w};
-#pragma unroll
-        for (int b = 0; b < NA; ++b) {
-          const float4 wv = *reinterpret_cast<const float4*>(&wt[b][k][tr]);
-          const float wa[4] = {wv.x, wv.y, wv.z, wv.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[b][i][j] = fmaf(xa[i], wa[j], acc[b][i][j]);
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (tp + i >= t.n) continue;
-      const int64_t p = t.p0 + tp + i;
-      const int row = row_of(a, (int)p);
-      const float f = row < 0 ? __uint_as_float(0x7FC00000u) : F8 ? __ldg(a.xs + row) : 1.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int r = t.m * kPlainTile + tr + j;
-        if (r >= a.rows) continue;
-        float v = acc[0][i][j] * f;
-        if (F8) v *= __ldg(a.ws + t.e * a.w_sld + r);
-        if constexpr (GLU) {
-          float u = acc[NA - 1][i][j] * f;
-          if (F8) u *= __ldg(a.us + t.e * a.u_sld + r);
-          v = silu_mul(v, u);
-        }
-        store_y(a.y, a.y_type, p * a.y_ld + r, v);
-      }
-    }
-  }
-}
-
-template <bool F8>
-cudaError_t launch_plain(ExpertArgs a, int sms, cudaStream_t st) {
-  a.N = kPlainTile;
-  a.mt = (a.rows + kPlainTile - 1) / kPlainTile;
-  const int64_t most = (int64_t)std::min<int64_t>(a.P, (int64_t)a.P / a.N + a.E) * a.mt;
-  const unsigned blocks = (unsigned)std::min<int64_t>(most, (int64_t)sms * 4);
-  if (a.up) k_expert_plain<F8, true><<<blocks, kPlainThreads, 0, st>>>(a);
-  else k_expert_plain<F8, false><<<blocks, kPlainThreads, 0, st>>>(a);
-  return cudaGetLastError();
-}
-
-// ---------------------------------------------------------------------------
-// Rows on 16-byte boundaries: tcgen05.  A CTA has two tiles of 128 rows of an expert's matrix (with U 128 of each, so that
+// A CTA has two tiles of 128 rows of an expert's matrix (with U 128 of each, so that
 // both products of a result are in one lane) and up to 256 rows of y: the matrix is the operand of many rows, so that an
 // expert's few rows cost an MMA of few columns.  With many rows two CTAs are a pair (cta_group::2): each brings half of the
 // rows of x for both.
@@ -392,10 +305,13 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const int step = (int)(gridDim.x / (unsigned)group), half = PAIR ? rank : 0;
   const int k0 = PAIR ? 0 : rank * a.sps, nk = max(0, min(a.sps, a.nk - k0));
   if (tid == 0) {
-    prefetch_map(&wmap);
-    if (GLU) prefetch_map(&umap);
+    if (a.w_vec) {
+      prefetch_map(&wmap);
+      if (GLU) prefetch_map(&umap);
+    }
     for (int i = 0; i < a.stages; ++i) {
-      mbar_init_n(s.full + i, 1 + (PAIR ? 2 : 32 * kXWarps));   // the matrices' bytes, x's rows (a pair's first CTA's: of both)
+      // the matrices' bytes (if by TMA), x's rows (a pair's first CTA's: of both)
+      mbar_init_n(s.full + i, (a.w_vec ? 1 : 0) + (PAIR ? 2 : 32 * kXWarps));
       mbar_init_n(s.xfull + i, 32 * kXWarps);
       mbar_init_n(s.empty + i, 1);
     }
@@ -437,7 +353,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   bool ok = true;
 
   if (wid == 0) {
-    if (lane == 0) {
+    if (lane == 0 && a.w_vec) {
       const uint32_t full0 = at0(s.full);
       int st = 0, u = 0, n = 0;
       for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
@@ -554,6 +470,21 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         const uint32_t dst = smem_u32(sm) + (uint32_t)st * stage + kATile + at;
         const int b = (k0 + i) * 128, left = min(max(width - b - chunk * 16, 0), 16);
         uint64_t* there = (PAIR ? s.xfull : s.full) + st;
+        const auto put = [&](uint32_t to, const uint4& v) {
+          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+        };
+        if (!a.w_vec) {   // the matrices too: rows r0 + kXRows j of the two tiles
+          const int m0 = (kBoth * t.m + half) * kRows;
+#pragma unroll 4
+          for (int j = 0; j < 256 / kXRows; ++j) {
+            const int r = r0 + kXRows * j;
+            const bool up = GLU && r >= 128;
+            const int m = m0 + (up ? r - 128 : r);
+            const uint8_t* row = static_cast<const uint8_t*>(up ? a.up : a.w) +
+                                 ((int64_t)t.e * (up ? a.u_eld : a.w_eld) + (int64_t)m * (up ? a.u_ld : a.w_ld)) * (F8 ? 1 : 2);
+            put(dst - kATile + (uint32_t)j * (kXRows * 128u), load16_anywhere(row + b + chunk * 16, m < a.rows ? left : 0));
+          }
+        }
         if (a.x_vec) {
 #pragma unroll
           for (int j = 0; j < kPasses; ++j)
@@ -566,8 +497,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
           for (int j = 0; j < kPasses; ++j)
             if (r0 + kXRows * j < mine) {
-              const uint4 v = load16_anywhere(src[j] ? src[j] + b : static_cast<const uint8_t*>(a.x), src[j] ? left : 0);
-              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst + (uint32_t)j * (kXRows * 128u)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+              put(dst + (uint32_t)j * (kXRows * 128u), load16_anywhere(src[j] ? src[j] + b : static_cast<const uint8_t*>(a.x), src[j] ? left : 0));
             }
           mbar_arrive(there);
         }
@@ -784,10 +714,9 @@ int64_t pitch_of(int64_t ld, int64_t cols, int64_t size, int64_t rows) {   // (o
   return rows <= 1 ? (cols * size + 15) / 16 * 16 : ld * size;
 }
 
-// Whether the tensor-core kernel takes these rows; its maps.
+// The maps of matrices whose rows start on 16-byte boundaries (false: they are read another way).
 bool tc_maps(const ExpertArgs& a, bool f8, CUtensorMap* wm, CUtensorMap* um) {
   const int64_t es = f8 ? 1 : 2;
-  if (a.x_rows < 1) return false;
   const int box = a.up ? 128 : 256;
   const auto matrices = [&](CUtensorMap* m, const void* p, int64_t ld, int64_t eld) {
     return on_boundaries(p, ld, es, a.rows) && make_matrices_map(m, f8, p, a.E, a.rows, a.cols, pitch_of(ld, a.cols, es, a.rows), eld * es, box);
@@ -935,14 +864,12 @@ extern "C" int bitsmoe_expert_product(const bitsmoe_expert_product_args* args, v
   a.lose = debug_skip_arrival();
   a.status = g.status;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  a.x_vec = on_boundaries(g.x, g.x_ld, f8 ? 1 : 2, g.x_rows);
+  a.x_vec = g.x_rows > 0 && on_boundaries(g.x, g.x_ld, f8 ? 1 : 2, g.x_rows);
   CUtensorMap wm, um;
-  if (tc_maps(a, f8, &wm, &um)) {
-    if (!a.up) um = wm;
-    e = f8 ? (a.up ? launch_tc<true, true>(a, wm, um, dev, sms, st) : launch_tc<true, false>(a, wm, um, dev, sms, st))
-           : (a.up ? launch_tc<false, true>(a, wm, um, dev, sms, st) : launch_tc<false, false>(a, wm, um, dev, sms, st));
-  } else {
-    e = f8 ? launch_plain<true>(a, sms, st) : launch_plain<false>(a, sms, st);
-  }
+  std::memset(&wm, 0, sizeof(wm));
+  std::memset(&um, 0, sizeof(um));
+  a.w_vec = tc_maps(a, f8, &wm, &um);
+  e = f8 ? (a.up ? launch_tc<true, true>(a, wm, um, dev, sms, st) : launch_tc<true, false>(a, wm, um, dev, sms, st))
+         : (a.up ? launch_tc<false, true>(a, wm, um, dev, sms, st) : launch_tc<false, false>(a, wm, um, dev, sms, st));
   return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
 }

@@ -211,7 +211,8 @@ def test_expert_product_off_the_boundaries(env, ty, glu, fan):
 
 
 @pytest.mark.parametrize("ty", ["bf16", "e4m3"])
-@pytest.mark.parametrize("counts,R,C", [([1], 64, 64), ([5, 0, 70, 1], 67, 129), ([300, 2], 300, 517), ([3, 9], 40, 4095), ([2], 33, 1)])
+@pytest.mark.parametrize("counts,R,C", [([1], 64, 64), ([5, 0, 70, 1], 67, 129), ([300, 2], 300, 517), ([3, 9], 40, 4095), ([2], 33, 1),
+                                          ([700, 900], 700, 2041)])
 @pytest.mark.parametrize("shift", [1, 3, 8, 15])
 def test_expert_product_rows_of_x_off_the_boundaries(env, ty, counts, R, C, shift):
     """Matrices on 16-byte boundaries, rows of x anywhere: the bits of the same rows on boundaries."""
@@ -231,6 +232,32 @@ def test_expert_product_rows_of_x_off_the_boundaries(env, ty, counts, R, C, shif
         a = bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, **kw)
         b = bm.expert_product(wrap(bm, w, ws), wrap(bm, off_x, xs), off, **kw)
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("counts,R,C", [([1], 64, 64), ([5, 0, 70, 1], 67, 129), ([300, 2], 300, 517), ([3, 9], 40, 4095), ([2], 33, 1)])
+@pytest.mark.parametrize("shift", [1, 6])
+def test_expert_product_matrices_off_the_boundaries(env, ty, counts, R, C, shift):
+    """Matrices anywhere (with or without U, x on boundaries or off them): the bits of the same matrices on boundaries."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(C)
+    E, P = len(counts), sum(counts)
+    w, ws, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
+    up, us, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
+    x, xs, _ = pitched(torch, torch.randn(P, C, generator=g), ty)
+
+    def moved(t):
+        raw = torch.full((*t.shape[:-1], C + 9), 127, dtype=torch.uint8, device="cuda").view(t.dtype) if ty == "e4m3" else torch.full(
+            (*t.shape[:-1], C + 9), float("nan"), dtype=t.dtype, device="cuda")
+        v = raw[..., shift:shift + C]
+        (v.view(torch.uint8) if ty == "e4m3" else v).copy_(t.view(torch.uint8) if ty == "e4m3" else t)
+        return v
+    off = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).cuda()
+    for u_ in (None, up):
+        a = bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, up=None if u_ is None else wrap(bm, u_, us))
+        for xx in (x, moved(x)):
+            b = bm.expert_product(wrap(bm, moved(w), ws), wrap(bm, xx, xs), off, up=None if u_ is None else wrap(bm, moved(u_), us))
+            assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("E,most,R,C,ty,glu", [(128, 6, 96, 256, "bf16", True), (300, 3, 40, 128, "e4m3", False), (1024, 2, 16, 64, "bf16", False),
@@ -259,6 +286,9 @@ def test_expert_product_strided_and_shared_matrices(env):
     a = bm.expert_product(both[::2, :48], x, off[:3])
     b = bm.expert_product(both[::2, :48].contiguous(), x, off[:3])
     assert torch.equal(a[:4], b[:4])
+    turned = both.transpose(0, 1).contiguous().transpose(0, 1)   # experts between the rows
+    assert turned.stride() == (128, 512, 1)
+    assert torch.equal(bm.expert_product(turned, x, off), bm.expert_product(both, x, off))
     one = both[:1].expand(4, 96, 128)
     a = bm.expert_product(one, x, off)
     b = bm.expert_product(both[:1], x, torch.tensor([0, 20], dtype=torch.int32).cuda())
