@@ -1171,7 +1171,7 @@ def expert_product(w, x, offsets, index=None, fan: int = 1, up=None, dtype=None,
     if not 1 <= fan <= _MAX_ROWS:
         _refuse(where, f"fan is {fan}")
     # Large products: rows of x off 16-byte boundaries are brought onto them first (us with and without, 16 experts of 1001
-    # x 2041, 64 rows 16 and 16, 4800 41 and 122, 64000 290 and 1180).
+    # x 2041, 64 rows 16 and 16, 4800 38 and 122, 64000 296 and 1180).
     if not coded and x_rows > 0 and (x_ptr % 16 or (x_ld % 8 and x_rows > 1)) and P * wc.rows * wc.cols > 1 << 31:
         ld = (wc.cols + 7) & ~7
         rows = torch.empty((x_rows, ld), dtype=torch.bfloat16, device=dev)

@@ -16,6 +16,7 @@
 #include <cmath>
 
 #include "microscale.cuh"
+#include "rows.cuh"
 
 namespace {
 using namespace bmoe;
@@ -42,17 +43,16 @@ __device__ __forceinline__ float logit_of(uint32_t key) {   // order_key's inver
   return __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
 }
 
-// A token's logits: lane l holds those of experts NE l + i.
+// A token's logits: lane l holds those of experts l + 32 i.
 template <int NE>
 __device__ __forceinline__ void load_logits(const RouteArgs& a, int64_t t, int lane, uint32_t (&key)[NE]) {
-  const float* row = a.logits + t * a.ld + lane * NE;
+  const float* row = a.logits + t * a.ld + lane;
 #pragma unroll
-  for (int i = 0; i < NE; ++i) key[i] = lane * NE + i < a.E ? __float_as_uint(__ldg(row + i)) : 0xFF800000u;
+  for (int i = 0; i < NE; ++i) key[i] = lane + 32 * i < a.E ? __float_as_uint(__ldg(row + 32 * i)) : 0xFF800000u;
 }
-// One token's selection by a warp: lane j < k gets the j-th expert (-1: none) and its weight.  Each lane offers its largest
-// logit (the first of equal ones); the largest offer of the lowest lane is the lowest expert's.
+// One token's selection by a warp: lane j < k gets the j-th expert (-1: none) and its weight.  list: the warp's own.
 template <int NE>
-__device__ __forceinline__ void select_token(const RouteArgs& a, int lane, uint32_t (&key)[NE], int& expert, float& weight) {
+__device__ __forceinline__ void select_token(const RouteArgs& a, int lane, uint32_t (&key)[NE], uint2* list, int& expert, float& weight) {
   constexpr uint32_t kNone = 0x007FFFFFu;   // -infinity's key, above NaN's
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
@@ -61,36 +61,82 @@ __device__ __forceinline__ void select_token(const RouteArgs& a, int lane, uint3
   }
   expert = -1;
   float mine = 0.f, top = 0.f, sum = 0.f;
-  for (int j = 0; j < a.k; ++j) {
-    uint32_t offer = key[0];
-    int at = 0;
+  // The top_k-th largest of the lanes' largest logits is not above the token's top_k-th largest: what is not below it are
+  // the candidates, few more than top_k.  Where a lane each holds them, a candidate's rank is the count of better ones.
+  uint32_t most = key[0];
 #pragma unroll
-    for (int i = 1; i < NE; ++i)
-      if (key[i] > offer) {
-        offer = key[i];
-        at = i;
-      }
-    const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, offer);
-    if (best == 0u) break;
-    const int from = __ffs(__ballot_sync(0xFFFFFFFFu, offer == best)) - 1;
-    const int e = from * NE + __shfl_sync(0xFFFFFFFFu, at, from);
-    const float v = logit_of(best);
-    if (j == 0) {
-      top = v;
-      if (!a.renormalize) {
+  for (int i = 1; i < NE; ++i) most = max(most, key[i]);
+  uint32_t sorted = most;   // by lane, descending
 #pragma unroll
-        for (int i = 0; i < NE; ++i)
-          if (key[i]) sum += expf(logit_of(key[i]) - top);
-        sum = warp_sum(sum);
-      }
+  for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+    for (int o = size / 2; o; o /= 2) {
+      const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, sorted, o);
+      const bool larger = ((lane & o) == 0) == ((lane & size) == 0);
+      sorted = larger ? max(sorted, other) : min(sorted, other);
     }
-    if (lane == j) {
-      expert = e;
-      mine = v;
-    }
+  const uint32_t border = max(__shfl_sync(0xFFFFFFFFu, sorted, a.k - 1), 1u);
+  const uint32_t first = __shfl_sync(0xFFFFFFFFu, sorted, 0);
+  if (first == 0u) {
+    weight = 0.f;
+    return;
+  }
+  top = logit_of(first);
+  if (!a.renormalize) {
 #pragma unroll
     for (int i = 0; i < NE; ++i)
-      if (e == lane * NE + i) key[i] = 0u;
+      if (key[i]) sum += expf(logit_of(key[i]) - top);
+    sum = warp_sum(sum);
+  }
+  int n = 0;   // candidates
+#pragma unroll
+  for (int i = 0; i < NE; ++i) {
+    const uint32_t who = __ballot_sync(0xFFFFFFFFu, key[i] >= border);
+    const int at = n + __popc(who & ((1u << lane) - 1u));
+    if (key[i] >= border && at < 32) list[at] = make_uint2(key[i], (uint32_t)(lane + 32 * i));
+    n += __popc(who);
+  }
+  __syncwarp();
+  if (n <= 32) {
+    uint2 c = make_uint2(0u, 0xFFFFFFFFu);
+    if (lane < n) c = list[lane];
+    int rank = 0;
+    for (int q = 0; q < n; ++q) {
+      const uint2 d = list[q];
+      rank += d.x > c.x || (d.x == c.x && d.y < c.y);
+    }
+    __syncwarp();
+    if (lane < n && rank < a.k) list[rank] = c;
+    __syncwarp();
+    if (lane < min(n, a.k)) {
+      expert = (int)list[lane].y;
+      mine = logit_of(list[lane].x);
+    }
+    __syncwarp();   // (the list is the next token's)
+  } else {
+    // (many equal ones) each lane offers its largest logit, the first of equal ones; of the largest offers the lowest
+    // expert's is taken
+    for (int j = 0; j < a.k; ++j) {
+      uint32_t offer = key[0];
+      int at = lane;
+#pragma unroll
+      for (int i = 1; i < NE; ++i)
+        if (key[i] > offer) {
+          offer = key[i];
+          at = lane + 32 * i;
+        }
+      const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, offer);
+      if (best == 0u) break;
+      const int e = (int)__reduce_min_sync(0xFFFFFFFFu, offer == best ? (uint32_t)at : 0xFFFFFFFFu);
+      if (lane == j) {
+        expert = e;
+        mine = logit_of(best);
+      }
+#pragma unroll
+      for (int i = 0; i < NE; ++i)
+        if (e == lane + 32 * i) key[i] = 0u;
+    }
+    __syncwarp();
   }
   weight = expert >= 0 ? expf(mine - top) : 0.f;
   if (a.renormalize) sum = warp_sum(weight);
@@ -129,6 +175,7 @@ struct RouteShared {
   uint32_t mask[kWords][kMaxExperts];
   int count[kMaxExperts];
   uint16_t pick[kChunk * kMaxTopK];
+  uint2 list[kRouteThreads / 32][32];
   int part[33];
 };
 
@@ -157,7 +204,7 @@ __device__ __forceinline__ void select_block(const RouteArgs& a, int first, int 
       } else {
         load_logits<NE>(a, t0 + t, lane, key);
       }
-      select_token<NE>(a, lane, key, expert, weight);
+      select_token<NE>(a, lane, key, s.list[w], expert, weight);
       if (lane < a.k) {
         a.weights[(int64_t)(t0 + t) * a.k + lane] = weight;
         s.pick[t * a.k + lane] = (uint16_t)expert;
@@ -290,11 +337,11 @@ cudaError_t launch_route(const RouteArgs& a, int blocks, cudaStream_t st) {
 }
 
 // Tokens of a block, and blocks of a call: each block of the second launch reads blocks x E counts.
-int route_per(int T, int E) {
-  const int most = std::min(152, std::max(16, 65536 / E));
+int route_per(int T) {
+  const int most = 152;
   return T <= kAloneTokens ? T : ((T + most - 1) / most + 31) / 32 * 32;
 }
-int route_blocks(int T, int E) { return T <= kAloneTokens ? 1 : (T + route_per(T, E) - 1) / route_per(T, E); }
+int route_blocks(int T) { return T <= kAloneTokens ? 1 : (T + route_per(T) - 1) / route_per(T); }
 bool route_sizes_ok(int T, int E, int k) {
   return T >= 0 && E >= 1 && E <= kMaxExperts && k >= 1 && k <= std::min(E, kMaxTopK) && (int64_t)T * k <= (1 << 24);
 }
@@ -303,7 +350,8 @@ bool route_sizes_ok(int T, int E, int k) {
 struct CombineArgs {
   const void* y;
   int64_t y_ld;
-  int P, k, D;
+  int T, P, k, D;
+  int shift;             // log2 of a token's threads
   const int32_t* places;
   const float* weights;
   const void* base;
@@ -312,10 +360,10 @@ struct CombineArgs {
   int64_t out_ld;
 };
 
-// V elements of a row: 16 bytes or what the rows' boundaries allow.
+// V elements of a row on 16-byte boundaries (V: 16 bytes of y's type; 8, 16 or 32 of the other's).
 template <typename T, int V>
 struct Piece {
-  uint32_t w[(V * sizeof(T) + 3) / 4];
+  uint32_t w[V * sizeof(T) / 4];
 };
 template <typename T, int V>
 __device__ __forceinline__ Piece<T, V> load_piece(const T* p) {
@@ -326,13 +374,9 @@ __device__ __forceinline__ Piece<T, V> load_piece(const T* p) {
       const uint4 x = reinterpret_cast<const uint4*>(p)[i];
       r.w[4 * i] = x.x, r.w[4 * i + 1] = x.y, r.w[4 * i + 2] = x.z, r.w[4 * i + 3] = x.w;
     }
-  } else if constexpr (V * sizeof(T) == 8) {
+  } else {
     const uint2 x = *reinterpret_cast<const uint2*>(p);
     r.w[0] = x.x, r.w[1] = x.y;
-  } else if constexpr (V * sizeof(T) == 4) {
-    r.w[0] = *reinterpret_cast<const uint32_t*>(p);
-  } else {
-    r.w[0] = *reinterpret_cast<const uint16_t*>(p);
   }
   return r;
 }
@@ -343,57 +387,55 @@ __device__ __forceinline__ float piece_at(const Piece<T, V>& r, int i) {
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_piece(T* p, const float (&v)[V]) {
-  Piece<T, V> r = {};
+  uint32_t w[V * sizeof(T) / 4];
   if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) r.w[i] = __float_as_uint(v[i]);
-  } else if constexpr (V == 1) {
-    *p = __float2bfloat16_rn(v[0]);
-    return;
+    for (int i = 0; i < V; ++i) w[i] = __float_as_uint(v[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
       const __nv_bfloat162 b = __floats2bfloat162_rn(v[i], v[i + 1]);
-      r.w[i / 2] = *reinterpret_cast<const uint32_t*>(&b);
+      w[i / 2] = *reinterpret_cast<const uint32_t*>(&b);
     }
   }
   if constexpr (V * sizeof(T) >= 16) {
 #pragma unroll
     for (int i = 0; i < (int)(V * sizeof(T)) / 16; ++i)
-      reinterpret_cast<uint4*>(p)[i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
-  } else if constexpr (V * sizeof(T) == 8) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(r.w[0], r.w[1]);
+      reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
   } else {
-    *reinterpret_cast<uint32_t*>(p) = r.w[0];
+    *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
   }
 }
 
-// V columns of a token a thread; the pieces of eight rows are requested before the first is used.  The rows' bytes bound it.
-template <typename TY, typename TO, int V>
-__global__ void __launch_bounds__(256) k_combine(const __grid_constant__ CombineArgs a) {
-  constexpr int kAhead = 8;
-  const int64_t t = blockIdx.x;
-  const int d = (blockIdx.y * 256 + threadIdx.x) * V;
-  if (d >= a.D) return;   // (D is a multiple of V)
+// A group of threads a token (2^shift of the block's 256), V columns a thread; the pieces of R rows are requested before the
+// first is used (of one or two rows R is 2, and the registers leave room for twice the warps).  The rows' bytes bound it: 8192
+// tokens of 8 rows of 2048 bf16 57 us, 5.9 TB/s.
+constexpr int kCombineThreads = 256;
+template <typename TY, typename TO, int V, int R, bool ONE>   // ONE: a block's threads have one token (its places are uniform)
+__global__ void __launch_bounds__(kCombineThreads, R == 2 ? 6 : 3) k_combine(const __grid_constant__ CombineArgs a) {
+  const int64_t t = ONE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (kCombineThreads >> a.shift) + (threadIdx.x >> a.shift);
+  const int d = ONE ? (int)(blockIdx.y * kCombineThreads + threadIdx.x) * V
+                    : (int)((blockIdx.y << a.shift) + (threadIdx.x & ((1 << a.shift) - 1))) * V;
+  if (t >= a.T || d >= a.D) return;   // (D is a multiple of V)
   float s[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) s[i] = 0.f;
   Piece<TO, V> base;
   if (a.base) base = load_piece<TO, V>(static_cast<const TO*>(a.base) + t * a.base_ld + d);
-  for (int j0 = 0; j0 < a.k; j0 += kAhead) {
-    Piece<TY, V> y[kAhead];
-    float w[kAhead];
-    int p[kAhead];
+  for (int j0 = 0; j0 < a.k; j0 += R) {
+    Piece<TY, V> y[R];
+    float w[R];
+    int p[R];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) p[j] = j0 + j < a.k ? __ldg(a.places + t * a.k + j0 + j) : -1;
+    for (int j = 0; j < R; ++j) p[j] = j0 + j < a.k ? __ldg(a.places + t * a.k + j0 + j) : -1;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
+    for (int j = 0; j < R; ++j)
       if ((unsigned)p[j] < (unsigned)a.P) {
         y[j] = load_piece<TY, V>(static_cast<const TY*>(a.y) + (int64_t)p[j] * a.y_ld + d);
         w[j] = __ldg(a.weights + t * a.k + j0 + j);
       }
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
+    for (int j = 0; j < R; ++j)
       if ((unsigned)p[j] < (unsigned)a.P) {
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] = fmaf(w[j], piece_at<TY, V>(y[j], i), s[i]);
@@ -406,30 +448,132 @@ __global__ void __launch_bounds__(256) k_combine(const __grid_constant__ Combine
   store_piece<TO, V>(static_cast<TO*>(a.out) + t * a.out_ld + d, s);
 }
 
+// Rows on any boundary: a warp 32 V columns of a token (V: 16 bytes of y's type), a lane's as the two aligned 16 bytes that hold
+// them, of four rows requested before the first is shifted into place; the sums are turned in shared memory, so that
+// neighbouring lanes store neighbouring elements.  8192 tokens of 8 rows of 2050 bf16, with a base, 110 us (an element a lane at a time 128).
 template <typename TY, typename TO>
-cudaError_t launch_combine(const CombineArgs& a, int T, cudaStream_t st) {
-  const auto fits = [&](int v) {
-    const auto on = [&](const void* p, int64_t ld, int size) {
-      const int64_t to = std::min(16, v * size);
-      return reinterpret_cast<uintptr_t>(p) % to == 0 && (ld * size) % to == 0;
-    };
-    return a.D % v == 0 && on(a.y, a.y_ld, sizeof(TY)) && on(a.out, a.out_ld, sizeof(TO)) && (!a.base || on(a.base, a.base_ld, sizeof(TO)));
+__global__ void __launch_bounds__(kCombineThreads) k_combine_any(const __grid_constant__ CombineArgs a) {
+  constexpr int R = 4, V = 16 / sizeof(TY), kCols = 32 * V;
+  __shared__ float turn[kCombineThreads / 32][kCols];
+  const int lane = threadIdx.x & 31;
+  const int chunks = (a.D + kCols - 1) / kCols;
+  const int64_t task = (int64_t)blockIdx.x * (kCombineThreads / 32) + (threadIdx.x >> 5);
+  const int64_t t = task / chunks;
+  if (t >= a.T) return;   // (whole warps)
+  const int d0 = (int)(task - t * chunks) * kCols, d = d0 + lane * V;
+  const int bytes = min(a.D - d, V) * (int)sizeof(TY);   // (not above 0: nothing)
+  float s[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) s[i] = 0.f;
+  const TO* base = static_cast<const TO*>(a.base) + t * a.base_ld;
+  TO* out = static_cast<TO*>(a.out) + t * a.out_ld;
+  float held[V];   // base, of the elements that the lane stores
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    held[i] = 0.f;
+    if (a.base && d0 + 32 * i + lane < a.D) {
+      if constexpr (sizeof(TO) == 4) held[i] = base[d0 + 32 * i + lane];
+      else held[i] = __bfloat162float(base[d0 + 32 * i + lane]);
+    }
+  }
+  int pn[R];   // of the next four rows, requested while these are on their way
+  float wn[R];
+  const auto take = [&](int j0) {
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      pn[j] = j0 + j < a.k ? __ldg(a.places + t * a.k + j0 + j) : -1;
+      wn[j] = j0 + j < a.k ? __ldg(a.weights + t * a.k + j0 + j) : 0.f;
+    }
   };
-  const auto go = [&](auto kern, int v) {
-    kern<<<dim3((unsigned)T, (unsigned)((a.D / v + 255) / 256)), 256, 0, st>>>(a);
+  take(0);
+  for (int j0 = 0; j0 < a.k; j0 += R) {
+    uint4 lo[R], hi[R];
+    int p[R];
+    float w[R];
+    uint32_t off[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      p[j] = (unsigned)pn[j] < (unsigned)a.P ? pn[j] : -1;
+      w[j] = wn[j];
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      lo[j] = hi[j] = make_uint4(0u, 0u, 0u, 0u);
+      const uint8_t* at = reinterpret_cast<const uint8_t*>(static_cast<const TY*>(a.y) + (int64_t)max(p[j], 0) * a.y_ld + d);
+      off[j] = (uint32_t)(reinterpret_cast<uintptr_t>(at) & 15);
+      const uint4* q = reinterpret_cast<const uint4*>(at - off[j]);
+      if (p[j] >= 0 && bytes > 0) lo[j] = __ldg(q);
+      if (p[j] >= 0 && (int)off[j] + bytes > 16) hi[j] = __ldg(q + 1);
+    }
+    if (j0 + R < a.k) take(j0 + R);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      if (p[j] < 0) continue;
+      uint32_t v[8] = {lo[j].x, lo[j].y, lo[j].z, lo[j].w, hi[j].x, hi[j].y, hi[j].z, hi[j].w};
+      if (off[j] & 8)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) v[i] = v[i + 2];
+      if (off[j] & 4)
+#pragma unroll
+        for (int i = 0; i < 5; ++i) v[i] = v[i + 1];
+      if constexpr (sizeof(TY) == 2) {
+        const uint32_t sh = (off[j] & 2) * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(v[i], v[i + 1], sh);
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float e;
+        if constexpr (sizeof(TY) == 4) e = __uint_as_float(v[i]);
+        else e = i & 1 ? bf16hi(v[i / 2]) : bf16lo(v[i / 2]);
+        s[i] = fmaf(w[j], e, s[i]);   // (what lies past the columns is not stored)
+      }
+    }
+  }
+  float* mine = turn[threadIdx.x >> 5];
+#pragma unroll
+  for (int i = 0; i < V / 4; ++i) reinterpret_cast<float4*>(mine)[V / 4 * lane + i] = make_float4(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int c = 32 * i + lane;
+    if (d0 + c >= a.D) break;
+    const float v = a.base ? held[i] + mine[c] : mine[c];
+    if constexpr (sizeof(TO) == 4) out[d0 + c] = v;
+    else out[d0 + c] = __float2bfloat16_rn(v);
+  }
+}
+
+template <typename TY, typename TO>
+cudaError_t launch_combine(CombineArgs a, cudaStream_t st) {
+  constexpr int V = sizeof(TY) == 4 ? 4 : 8;
+  const auto on = [&](const void* p, int64_t ld, int size) {
+    const int64_t to = std::min(16, V * size);
+    return reinterpret_cast<uintptr_t>(p) % to == 0 && (ld * size) % to == 0;
+  };
+  if (a.D % V || !on(a.y, a.y_ld, sizeof(TY)) || !on(a.out, a.T == 1 ? 0 : a.out_ld, sizeof(TO)) || !on(a.base, a.T == 1 ? 0 : a.base_ld, sizeof(TO))) {
+    const int64_t warps = (int64_t)a.T * ((a.D + 32 * V - 1) / (32 * V)), per = kCombineThreads / 32;
+    if ((warps + per - 1) / per >= (1ll << 31)) return cudaErrorInvalidValue;
+    k_combine_any<TY, TO><<<(unsigned)((warps + per - 1) / per), kCombineThreads, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+  const int pieces = a.D / V;
+  a.shift = 0;
+  while (a.shift < 8 && 1 << a.shift < pieces) ++a.shift;
+  const int per = kCombineThreads >> a.shift;
+  const auto go = [&](auto kern) {
+    kern<<<dim3((unsigned)((a.T + per - 1) / per), (unsigned)((pieces + (1 << a.shift) - 1) >> a.shift)), kCombineThreads, 0, st>>>(a);
     return cudaGetLastError();
   };
-  constexpr int kWide = sizeof(TY) == 4 ? 4 : 8;
-  if (fits(kWide)) return go(k_combine<TY, TO, kWide>, kWide);
-  if (fits(2)) return go(k_combine<TY, TO, 2>, 2);
-  return go(k_combine<TY, TO, 1>, 1);
+  if (per == 1) return a.k <= 2 ? go(k_combine<TY, TO, V, 2, true>) : go(k_combine<TY, TO, V, 8, true>);
+  return a.k <= 2 ? go(k_combine<TY, TO, V, 2, false>) : go(k_combine<TY, TO, V, 8, false>);
 }
 
 }  // namespace
 
 extern "C" size_t bitsmoe_route_workspace_bytes(int T, int E, int top_k) {
-  if (!route_sizes_ok(T, E, top_k) || route_blocks(T, E) == 1) return 0;
-  return (size_t)route_blocks(T, E) * E * 4;
+  if (!route_sizes_ok(T, E, top_k) || route_blocks(T) == 1) return 0;
+  return (size_t)route_blocks(T) * E * 4;
 }
 
 extern "C" int bitsmoe_route(const float* logits, int64_t ld, int T, int E, int top_k, int renormalize, int32_t* experts,
@@ -449,8 +593,8 @@ extern "C" int bitsmoe_route(const float* logits, int64_t ld, int T, int E, int 
     k_route_none<<<1, 256, 0, st>>>(offsets, E);
     e = cudaGetLastError();
   } else {
-    const int blocks = route_blocks(T, E);
-    const RouteArgs a{logits, ld, T, E, top_k, renormalize, route_per(T, E), experts, weights, offsets, pairs, places, static_cast<int32_t*>(ws)};
+    const int blocks = route_blocks(T);
+    const RouteArgs a{logits, ld, T, E, top_k, renormalize, route_per(T), experts, weights, offsets, pairs, places, static_cast<int32_t*>(ws)};
     e = E <= 32    ? launch_route<1>(a, blocks, st)
         : E <= 64  ? launch_route<2>(a, blocks, st)
         : E <= 128 ? launch_route<4>(a, blocks, st)
@@ -474,10 +618,10 @@ extern "C" int bitsmoe_expert_combine(const void* y, int y_type, int64_t y_ld, i
   const auto odd = [](const void* p, int to) { return reinterpret_cast<uintptr_t>(p) % to != 0; };
   if (odd(y, dense_size(y_type)) || odd(out, dense_size(out_type)) || odd(base, dense_size(out_type)) || odd(places, 4) || odd(weights, 4))
     return BITSMOE_ERR_ALIGNMENT;
-  CombineArgs a{y, y_ld, P, top_k, D, places, weights, base, base_ld, out, out_ld};
+  CombineArgs a{y, y_ld, T, P, top_k, D, 0, places, weights, base, base_ld, out, out_ld};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool yf = y_type == BITSMOE_F32, of = out_type == BITSMOE_F32;
-  const cudaError_t e = yf ? (of ? launch_combine<float, float>(a, T, st) : launch_combine<float, __nv_bfloat16>(a, T, st))
-                           : (of ? launch_combine<__nv_bfloat16, float>(a, T, st) : launch_combine<__nv_bfloat16, __nv_bfloat16>(a, T, st));
+  const cudaError_t e = yf ? (of ? launch_combine<float, float>(a, st) : launch_combine<float, __nv_bfloat16>(a, st))
+                           : (of ? launch_combine<__nv_bfloat16, float>(a, st) : launch_combine<__nv_bfloat16, __nv_bfloat16>(a, st));
   return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
 }

@@ -24,7 +24,7 @@ struct RowscaleArgs {
   int64_t pitch;       // of the codes, bytes
   float* scales;
   int vec;             // codes can be read and written 8 at a time
-  int chunks;          // dequantise: chunks of a row
+  int chunks, shift;   // dequantise: chunks of a row; log2 of the lanes that take one
 };
 
 // The codes of columns c .. c + 7 of a row.
@@ -61,13 +61,13 @@ __global__ void __launch_bounds__(G < 128 ? 128 : G) k_rowscale_quantize(const _
   __shared__ uint32_t red[kThreads / 32];
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G;
   const int gi = threadIdx.x % G;
-  if (row >= a.rows) return;   // (whole groups)
+  if (G >= 32 && row >= a.rows) return;   // (whole warps; smaller groups help their warp's exchange)
   Eight<T> v[NV];
   uint32_t most = 0u;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = (k * G + gi) * 8;
-    if (c < a.cols) {
+    if (c < a.cols && (G >= 32 || row < a.rows)) {
       v[k] = load8<T, VEC>(a.in, a.ld, a.cols, row, c);
     } else {
 #pragma unroll
@@ -76,13 +76,19 @@ __global__ void __launch_bounds__(G < 128 ? 128 : G) k_rowscale_quantize(const _
   }
 #pragma unroll
   for (int k = 0; k < NV; ++k) most = max(most, most8<T>(v[k]));
-  most = __reduce_max_sync(0xFFFFFFFFu, most);
+  if constexpr (G < 32) {
+#pragma unroll
+    for (int o = 1; o < G; o <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+  } else {
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+  }
   if constexpr (G > 32) {
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = most;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kThreads / 32; ++i) most = max(most, red[i]);
   }
+  if (G < 32 && row >= a.rows) return;
   const float inv = rowscale_inverse(most);
   const bool bad = rowscale_bad(most);
   if (gi == 0) a.scales[row] = rowscale_of(most);
@@ -114,42 +120,76 @@ __global__ void __launch_bounds__(kLongThreads) k_rowscale_quantize_long(const _
   for (int c = threadIdx.x * 8; c < a.cols; c += kLongThreads * 8) put8<T>(a, row, c, load8<T, VEC>(a.in, a.ld, a.cols, row, c), inv, bad);
 }
 
-// A warp a chunk of a row: 16 bytes of the result a lane where the rows allow it, else neighbouring elements in
-// neighbouring lanes.
-constexpr int kBackThreads = 256;
-template <typename T, bool VEC>
+// A warp (for short rows a part of one) a chunk of a row, V columns of the result a lane at a time: 16 bytes where the rows
+// allow it, else 2 or 1.
+constexpr int kBackThreads = 256, kBackPieces = 4;
+template <typename T, int V>
 __global__ void __launch_bounds__(kBackThreads) k_rowscale_dequantize(const __grid_constant__ RowscaleArgs a) {
-  constexpr int V = 16 / sizeof(T);
   const int lane = threadIdx.x & 31;
-  const int64_t task = (int64_t)blockIdx.x * (kBackThreads / 32) + (threadIdx.x >> 5);
+  const int64_t task = (int64_t)blockIdx.x * (kBackThreads >> a.shift) + (threadIdx.x >> a.shift);
   const int64_t row = task / a.chunks;
   if (row >= a.rows) return;
-  const int c0 = (int)(task - row * a.chunks) * 32 * V;
+  const int piece = V << a.shift, c0 = (int)(task - row * a.chunks) * piece * kBackPieces + (lane & ((1 << a.shift) - 1)) * V;
   const uint8_t* src = a.codes + row * a.pitch;
   T* dst = static_cast<T*>(a.out) + row * a.ld;
   const float s = __ldg(a.scales + row);
-  const auto put = [&](int c, float v) {
-    if constexpr (sizeof(T) == 4) dst[c] = v;
-    else dst[c] = __float2bfloat16_rn(v);
-  };
-  if (VEC && c0 + 32 * V <= a.cols) {
-    const int c = c0 + lane * V;
-    if constexpr (V == 4) {
-      const float4 v = e4m3_values(__ldg(reinterpret_cast<const uint32_t*>(src + c)));
-      __stcs(reinterpret_cast<float4*>(dst + c), make_float4(v.x * s, v.y * s, v.z * s, v.w * s));
-    } else {
-      const uint2 w = __ldg(reinterpret_cast<const uint2*>(src + c));
-      const float4 p = e4m3_values(w.x), q = e4m3_values(w.y);
-      const __nv_bfloat162 h[4] = {__floats2bfloat162_rn(p.x * s, p.y * s), __floats2bfloat162_rn(p.z * s, p.w * s),
-                                   __floats2bfloat162_rn(q.x * s, q.y * s), __floats2bfloat162_rn(q.z * s, q.w * s)};
-      __stcs(reinterpret_cast<uint4*>(dst + c), *reinterpret_cast<const uint4*>(h));
+  uint32_t w[kBackPieces][(V + 3) / 4];
+#pragma unroll
+  for (int u = 0; u < kBackPieces; ++u) {   // (the last piece of a row may go past its columns where V is above 2)
+    const int c = c0 + u * piece;
+#pragma unroll
+    for (int i = 0; i < (V + 3) / 4; ++i) w[u][i] = 0u;
+    if (c + V <= a.cols) {
+      if constexpr (V == 8) {
+        const uint2 x = __ldg(reinterpret_cast<const uint2*>(src + c));
+        w[u][0] = x.x, w[u][1] = x.y;
+      } else if constexpr (V == 4) {
+        w[u][0] = __ldg(reinterpret_cast<const uint32_t*>(src + c));
+      } else if constexpr (V == 2) {
+        w[u][0] = __ldg(reinterpret_cast<const uint16_t*>(src + c));
+      } else {
+        w[u][0] = __ldg(src + c);
+      }
+    } else if (V > 1) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (c + i < a.cols) w[u][i / 4] |= (uint32_t)__ldg(src + c + i) << (8 * (i & 3));
     }
-    return;
   }
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int c = c0 + i * 32 + lane;
-    if (c < a.cols) put(c, e4m3_values((uint32_t)src[c]).x * s);
+  for (int u = 0; u < kBackPieces; ++u) {
+    const int c = c0 + u * piece;
+    if (c >= a.cols) break;
+    float v[(V + 3) / 4 * 4];
+#pragma unroll
+    for (int i = 0; i < (V + 3) / 4; ++i) {
+      const float4 f = e4m3_values(w[u][i]);
+      v[4 * i] = f.x * s, v[4 * i + 1] = f.y * s, v[4 * i + 2] = f.z * s, v[4 * i + 3] = f.w * s;
+    }
+    uint32_t h[4];
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4 && i < V; ++i) h[i] = __float_as_uint(v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < (V + 1) / 2; ++i) {
+        const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        h[i] = *reinterpret_cast<const uint32_t*>(&t);
+      }
+    }
+    if (c + V <= a.cols) {
+      if constexpr (V * sizeof(T) == 16) __stcs(reinterpret_cast<uint4*>(dst + c), make_uint4(h[0], h[1], h[2], h[3]));
+      else if constexpr (V * sizeof(T) == 8) __stcs(reinterpret_cast<uint2*>(dst + c), make_uint2(h[0], h[1]));
+      else if constexpr (V * sizeof(T) == 4) __stcs(reinterpret_cast<uint32_t*>(dst + c), h[0]);
+      else *reinterpret_cast<uint16_t*>(dst + c) = (uint16_t)h[0];
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (c + i < a.cols) {
+          if constexpr (sizeof(T) == 4) dst[c + i] = v[i];
+          else dst[c + i] = __float2bfloat16_rn(v[i]);
+        }
+    }
   }
 }
 
@@ -164,9 +204,12 @@ cudaError_t launch_quantize(const RowscaleArgs& a, cudaStream_t st) {
     kern<<<(unsigned)((a.rows + rows - 1) / rows), threads, 0, st>>>(a);
     return cudaGetLastError();
   };
+  if (n <= 8) return go(k_rowscale_quantize<T, VEC, 8, 1>, 128, 16);
+  if (n <= 16) return go(k_rowscale_quantize<T, VEC, 16, 1>, 128, 8);
   if (n <= 32) return go(k_rowscale_quantize<T, VEC, 32, 1>, 128, 4);
-  if (n <= 128) return go(k_rowscale_quantize<T, VEC, 128, 1>, 128, 1);
+  if (n <= 128) return go(k_rowscale_quantize<T, VEC, 32, 4>, 128, 4);
   if (n <= 512) return go(k_rowscale_quantize<T, VEC, 128, 4>, 128, 1);
+  if (n <= 1024) return go(k_rowscale_quantize<T, VEC, 256, 4>, 256, 1);
   if (n <= 2048) return go(k_rowscale_quantize<T, VEC, 512, 4>, 512, 1);
   return go(k_rowscale_quantize_long<T, VEC>, kLongThreads, 1);
 }
@@ -189,7 +232,7 @@ extern "C" int bitsmoe_rowscale_quantize(const void* x, int type, int64_t ld, co
   int rc = rowscale_check(q, type, ld);
   if (rc || q->rows == 0) return rc;
   if ((rc = rowscale_pointers(q, x, type))) return rc;
-  RowscaleArgs a{x, nullptr, ld, q->rows, q->cols, q->codes, q->ld, q->scales, aligned_rows(q->codes, q->ld, q->rows, 8), 0};
+  RowscaleArgs a{x, nullptr, ld, q->rows, q->cols, q->codes, q->ld, q->scales, aligned_rows(q->codes, q->ld, q->rows, 8), 0, 0};
   const bool vec = aligned_rows(x, ld * dense_size(type), q->rows, 16);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
@@ -202,11 +245,16 @@ extern "C" int bitsmoe_rowscale_dequantize(const bitsmoe_rowscale* q, void* x, i
   int rc = rowscale_check(q, type, ld);
   if (rc || q->rows == 0) return rc;
   if ((rc = rowscale_pointers(q, x, type))) return rc;
-  RowscaleArgs a{nullptr, x, ld, q->rows, q->cols, q->codes, q->ld, q->scales, 0, 0};
-  const int per = 32 * 16 / dense_size(type);
+  RowscaleArgs a{nullptr, x, ld, q->rows, q->cols, q->codes, q->ld, q->scales, 0, 0, 0};
+  // columns of a piece: 16 bytes of the result, or 2, where the rows of both start on such boundaries
+  const int size = dense_size(type);
+  const auto fits = [&](int v) { return aligned_rows(x, ld * size, q->rows, v * size) && aligned_rows(q->codes, q->ld, q->rows, v); };
+  const int v = fits(16 / size) ? 16 / size : fits(2) ? 2 : 1;
+  a.shift = 2;
+  while (a.shift < 5 && (v << a.shift) * kBackPieces < q->cols) ++a.shift;
+  const int per = (v << a.shift) * kBackPieces, tasks = kBackThreads >> a.shift;   // columns of a chunk, chunks of a block
   a.chunks = (q->cols + per - 1) / per;
-  const bool vec = aligned_rows(x, ld * dense_size(type), q->rows, 16) && aligned_rows(q->codes, q->ld, q->rows, 8);
-  const int64_t blocks = ((int64_t)q->rows * a.chunks + kBackThreads / 32 - 1) / (kBackThreads / 32);
+  const int64_t blocks = ((int64_t)q->rows * a.chunks + tasks - 1) / tasks;
   if (blocks >= (1ll << 31)) return BITSMOE_ERR_SHAPE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const auto go = [&](auto kern) {
@@ -214,7 +262,10 @@ extern "C" int bitsmoe_rowscale_dequantize(const bitsmoe_rowscale* q, void* x, i
     return cudaGetLastError();
   };
   cudaError_t e;
-  if (type == BITSMOE_F32) e = vec ? go(k_rowscale_dequantize<float, true>) : go(k_rowscale_dequantize<float, false>);
-  else e = vec ? go(k_rowscale_dequantize<__nv_bfloat16, true>) : go(k_rowscale_dequantize<__nv_bfloat16, false>);
+  if (type == BITSMOE_F32) e = v == 4 ? go(k_rowscale_dequantize<float, 4>) : v == 2 ? go(k_rowscale_dequantize<float, 2>) : go(k_rowscale_dequantize<float, 1>);
+  else
+    e = v == 8   ? go(k_rowscale_dequantize<__nv_bfloat16, 8>)
+        : v == 2 ? go(k_rowscale_dequantize<__nv_bfloat16, 2>)
+                 : go(k_rowscale_dequantize<__nv_bfloat16, 1>);
   return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
 }
