@@ -450,17 +450,18 @@ __global__ void __launch_bounds__(kCombineThreads, R == 2 ? 6 : 3) k_combine(con
 
 // Rows on any boundary: a warp 32 V columns of a token (V: 16 bytes of y's type), a lane's as the two aligned 16 bytes that hold
 // them, of four rows requested before the first is shifted into place; the sums are turned in shared memory, so that
-// neighbouring lanes store neighbouring elements.  8192 tokens of 8 rows of 2050 bf16, with a base, 110 us (an element a lane at a time 128).
-template <typename TY, typename TO>
+// neighbouring lanes store neighbouring elements.  8192 tokens of 8 rows of 2050 bf16, with a base, 92 us (an element a lane at a time 128).
+template <typename TY, typename TO, bool ONE>   // ONE: a block's warps have one token
 __global__ void __launch_bounds__(kCombineThreads) k_combine_any(const __grid_constant__ CombineArgs a) {
   constexpr int R = 4, V = 16 / sizeof(TY), kCols = 32 * V;
   __shared__ float turn[kCombineThreads / 32][kCols];
   const int lane = threadIdx.x & 31;
   const int chunks = (a.D + kCols - 1) / kCols;
   const int64_t task = (int64_t)blockIdx.x * (kCombineThreads / 32) + (threadIdx.x >> 5);
-  const int64_t t = task / chunks;
-  if (t >= a.T) return;   // (whole warps)
-  const int d0 = (int)(task - t * chunks) * kCols, d = d0 + lane * V;
+  const int64_t t = ONE ? (int64_t)blockIdx.x : task / chunks;
+  const int chunk = ONE ? (int)(blockIdx.y * (kCombineThreads / 32) + (threadIdx.x >> 5)) : (int)(task - t * chunks);
+  if (t >= a.T || chunk >= chunks) return;   // (whole warps)
+  const int d0 = chunk * kCols, d = d0 + lane * V;
   const int bytes = min(a.D - d, V) * (int)sizeof(TY);   // (not above 0: nothing)
   float s[V];
 #pragma unroll
@@ -552,9 +553,9 @@ cudaError_t launch_combine(CombineArgs a, cudaStream_t st) {
     return reinterpret_cast<uintptr_t>(p) % to == 0 && (ld * size) % to == 0;
   };
   if (a.D % V || !on(a.y, a.y_ld, sizeof(TY)) || !on(a.out, a.T == 1 ? 0 : a.out_ld, sizeof(TO)) || !on(a.base, a.T == 1 ? 0 : a.base_ld, sizeof(TO))) {
-    const int64_t warps = (int64_t)a.T * ((a.D + 32 * V - 1) / (32 * V)), per = kCombineThreads / 32;
-    if ((warps + per - 1) / per >= (1ll << 31)) return cudaErrorInvalidValue;
-    k_combine_any<TY, TO><<<(unsigned)((warps + per - 1) / per), kCombineThreads, 0, st>>>(a);
+    const int chunks = (a.D + 32 * V - 1) / (32 * V), per = kCombineThreads / 32;
+    if (chunks > per / 2) k_combine_any<TY, TO, true><<<dim3((unsigned)a.T, (unsigned)((chunks + per - 1) / per)), kCombineThreads, 0, st>>>(a);
+    else k_combine_any<TY, TO, false><<<(unsigned)(((int64_t)a.T * chunks + per - 1) / per), kCombineThreads, 0, st>>>(a);
     return cudaGetLastError();
   }
   const int pieces = a.D / V;
