@@ -700,8 +700,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
 }
 
-// Rows of y of a tile: twice an expert's on average, so that few experts have more than one tile, each of which reads
-// the expert's matrix again; a stage of more rows leaves room for fewer stages.
+// Rows of y of a tile: twice an expert's on average and 32 more, so that few experts have more than one tile, each of which
+// reads the expert's matrix again; a stage of more rows leaves room for fewer stages.  Without the 32, gate and up of 128
+// experts of 768 x 2048 (us): 25 rows an expert 126 in place of 117, 10 rows 117 and 114, 3 rows 87 and 89.
 int tile_rows(int P, int E) {
   const int most = (int)std::min<int64_t>(256, ((int64_t)P + 31) / 32 * 32);
   return std::min(most, (int)std::min<int64_t>(256, (2ll * P / E + 31) / 32 * 32 + 32));
@@ -775,7 +776,18 @@ cudaError_t launch_tc_as(const ExpertArgs& a, const CUtensorMap& wm, const CUten
 template <bool F8, bool GLU>
 cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um, int dev, int sms, cudaStream_t st) {
   a.N = tile_rows(a.P, a.E);
-  const bool pair = a.N > kFewRows;
+  bool pair = a.N > kFewRows;
+  if (pair) {
+    // Pairs where a third of them have a tile; else smaller tiles of single CTAs, over which the columns can be split too.  One
+    // matrix of 4096 x 4096 (us, pairs and single): 100 rows of y (8 tiles of pairs) 30 and 13, 300 (16) 31 and 26; two of
+    // them with SwiGLU, 512 (32) 44 and 51.
+    const int64_t experts = std::min(a.P, a.E), tall = GLU ? 256 : 512;
+    const int64_t tiles = experts * ((a.P / experts + a.N - 1) / a.N) * ((a.rows + tall - 1) / tall);
+    if (6 * tiles < sms) {
+      pair = false;
+      a.N = kFewRows;
+    }
+  }
   const int rows = (GLU ? 128 : 256) * (pair ? 2 : 1);
   a.mt = (a.rows + rows - 1) / rows;
   a.nk = (a.cols + (F8 ? 127 : 63)) / (F8 ? 128 : 64);
@@ -783,6 +795,8 @@ cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um
   a.u_next = a.u_eld != 0;
   a.nbuf = 4 * a.N <= 512 ? 2 : 1;
   const int64_t most = std::min<int64_t>(a.P, (int64_t)a.P / a.N + a.E) * a.mt;   // tiles at most
+  // Few tiles: the columns over clusters of as many CTAs as the SMs hold (one token by 4096 x 4096 9.8 us, unsplit 24.0; through
+  // gate and up of eight experts of 768 x 2048 11.6 and 14.8).
   a.splits = 1;
   if (!pair)   // (clusters that do not all run at once would take a second turn)
     for (int n = 8; n > 1 && a.splits == 1; n /= 2)
