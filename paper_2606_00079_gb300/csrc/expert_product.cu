@@ -13,7 +13,6 @@
 #include <cstring>
 
 #include "microscale.cuh"
-#include "rows.cuh"
 #include "tc.cuh"
 
 namespace {
@@ -284,8 +283,13 @@ __device__ __forceinline__ void plan_waves(const ExpertArgs& a, const Groups& g,
   }
 }
 
-// SiLU(g) u with the fast exponential and quotient (2 units in the last place each).
-__device__ __forceinline__ float silu_fast(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
+// SiLU(g) u.  The quotient's denominator is 1 .. 2, so that the fast one (2 units in the last place) holds for every g.  Gate
+// and up of 128 experts of 768 x 2048, 8192 tokens 294 us; with an exact division 340, with the fast exponential (which loses
+// 1.2 |g| units) 288.
+__device__ __forceinline__ float silu(float g, float u) {
+  const float e = expf(-fabsf(g));
+  return g * __fdividef(g < 0.f ? e : 1.f, 1.f + e) * u;
+}
 
 template <bool F8, bool GLU, bool PAIR>
 __global__ void __launch_bounds__(kTcThreads, 1)
@@ -594,8 +598,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
               for (int q = 0; q < 8; q += 2) {
                 float x = value(b, h, q), y = value(b, h, q + 1);
                 if constexpr (GLU) {
-                  x = silu_fast(x, value(1, h, q));
-                  y = silu_fast(y, value(1, h, q + 1));
+                  x = silu(x, value(1, h, q));
+                  y = silu(y, value(1, h, q + 1));
                 }
                 const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
                 o[q >> 1] = *reinterpret_cast<const uint32_t*>(&p);
@@ -637,7 +641,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
               if (c0 + q >= t.n) continue;
               auto* at = y + (int64_t)(t.p0 + c0 + q) * a.y_ld + m;
               if constexpr (GLU) {
-                if (in0) keep(at, silu_fast(v0, v1));
+                if (in0) keep(at, silu(v0, v1));
               } else {
                 if (in0) keep(at, v0);
                 if (in1) keep(at + 128, v1);
@@ -681,7 +685,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           if (mh < a.rows) v[h] *= F8 ? f * __ldg((GLU && h ? a.us + t.e * a.u_sld : a.ws + t.e * a.w_sld) + mh) : f;
         }
         if constexpr (GLU) {
-          if (m < a.rows) store_y(a.y, a.y_type, at, silu_fast(v[0], v[1]));
+          if (m < a.rows) store_y(a.y, a.y_type, at, silu(v[0], v[1]));
         } else {
           if (m < a.rows) store_y(a.y, a.y_type, at, v[0]);
           if (m + 128 < a.rows) store_y(a.y, a.y_type, at + 128, v[1]);

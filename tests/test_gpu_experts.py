@@ -692,3 +692,23 @@ def test_first_calls_inside_a_capture(env, T):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST, root, str(T)], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("T,E,R", [(1, 1, 200), (40, 2, 130), (900, 3, 300), (3000, 40, 161)])   # split columns, single CTAs, pairs
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_swiglu_of_large_gates(env, T, E, R, out):
+    """Sums of one product, so exact: y is SiLU's own error.  expf and a quotient of 2 units in the last place each are 4 u
+    each, the sum below the quotient u, two products u each; bf16 adds half a step."""
+    torch, bm = env
+    C = 1024   # (columns to split; all but one of x are 0)
+    g = torch.linspace(-80, 80, E * R, device="cuda").view(E, R).bfloat16()
+    w, up = (torch.randn(E, R, C, device="cuda").bfloat16() for _ in range(2))
+    w[:, :, 5], up[:, :, 5] = g, 1.5
+    x = torch.zeros(T, C, dtype=torch.bfloat16, device="cuda")
+    x[:, 5] = 1
+    off = torch.linspace(0, T, E + 1, device="cuda").int()
+    y = bm.expert_product(w, x, off, up=up, dtype=torch.float32 if out == "f32" else torch.bfloat16).double()
+    o, gd = off.tolist(), g.double()
+    want = torch.cat([(gd[e] / (1 + torch.exp(-gd[e])) * 1.5).expand(o[e + 1] - o[e], R) for e in range(E)])
+    rel = 12 * u if out == "f32" else 2.0 ** -8 + 13 * u
+    assert ((y - want).abs() <= rel * want.abs()).all()
