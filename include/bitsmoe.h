@@ -174,8 +174,8 @@ int bitsmoe_forward_plan(const bitsmoe_layer* layer, int T, int top_k);
 
 /* Testing hook (no counterpart in the paper): bound every wait of the fused
  * single-token kernels, and the waits inside a block of the tensor-core
- * projections, of the expert kernels of several tokens and of the microscaled
- * product (whose own status word then says so), to `spin_clocks` SM
+ * projections, of the expert kernels of several tokens, of the microscaled
+ * product and of the products grouped by expert (whose own status words then say so), to `spin_clocks` SM
  * clocks (<= 0: the default, about one second), and when skip_arrival is 1 let
  * block 0 skip an arrival (the former: at their first grid barrier, the latter:
  * at a stage in shared memory), so that the bounded waits for it run out.  The
@@ -662,8 +662,7 @@ int bitsmoe_block_norm(const bitsmoe_block_norm_args* args, void* stream);
  *     value[r][k] = code * scales[r].
  *   rows, cols  0 .. 2^24, 1 .. 2^20
  *   codes   device, rows `ld` bytes apart (ld >= cols; rows on 16-byte boundaries
- *           are read and written fastest, and bitsmoe_expert_product's tensor-core
- *           kernels want them); what lies between the rows is not touched
+ *           are read and written fastest); what lies between the rows is not touched
  *   scales  device, rows fp32 */
 #define BITSMOE_E4M3 2
 typedef struct bitsmoe_rowscale {

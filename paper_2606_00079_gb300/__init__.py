@@ -935,7 +935,7 @@ class Rowscale:
     """Rows in 8 bits on the device: `codes` (torch.float8_e4m3fn, rows x cols, or experts x rows x cols with dense
     rows) and `scales` (float32, one for each row); value = code * scale, see bitsmoe_rowscale in include/bitsmoe.h."""
 
-    __slots__ = ("codes", "scales", "_c", "shape", "device")   # _c: what the library reads, formed when first needed
+    __slots__ = ("_codes", "_scales", "_c", "shape", "device")   # _c: what the library reads, formed when first needed
 
     def __init__(self, codes, scales):
         torch = _torch or _load_torch()
@@ -947,8 +947,16 @@ class Rowscale:
             _refuse("Rowscale", f"scales have shape {tuple(scales.shape)}, codes {tuple(codes.shape)}", "SHAPE")
         if scales.shape[-1] > 1 and scales.stride(-1) != 1:
             _refuse("Rowscale", "scales must be dense along the rows")
-        self.codes, self.scales, self._c = codes, scales, None
+        self._codes, self._scales, self._c = codes, scales, None
         self.shape, self.device = codes.shape, codes.device
+
+    @property
+    def codes(self):
+        return self._codes
+
+    @property
+    def scales(self):
+        return self._scales
 
     @classmethod
     def empty(cls, shape, device=None) -> "Rowscale":
@@ -964,9 +972,9 @@ class Rowscale:
         dev = device if device is not None else torch.cuda.current_device()
         self = cls.__new__(cls)   # (an allocation each: parts of one cost the host more)
         codes = torch.empty((*shape[:-1], pitch), dtype=torch.float8_e4m3fn, device=dev)
-        self.codes = codes if pitch == cols else codes[..., :cols]
-        self.scales = scales = torch.empty(shape[:-1], dtype=torch.float32, device=dev)
-        self.shape, self.device = shape, codes.device
+        self._codes = codes if pitch == cols else codes[..., :cols]
+        self._scales = scales = torch.empty(shape[:-1], dtype=torch.float32, device=dev)
+        self.shape, self.device = shape if isinstance(shape, tuple) else tuple(shape), codes.device
         self._c = _Rowscale(n, cols, pitch, codes.data_ptr(), scales.data_ptr())
         return self
 
@@ -1076,8 +1084,8 @@ def route(logits, top_k: int, renormalize: bool = True, stream=None) -> Routing:
         with _elsewhere(where, dev, stream):
             return route(logits, top_k, renormalize)
     T, E = logits.shape
-    if not 1 <= top_k <= E:
-        _refuse(where, f"top_k is {top_k} of {E} experts")
+    if not 1 <= top_k <= min(E, 32):
+        _refuse(where, f"top_k is {top_k} of {E} experts (32 at most)")
     nws = _ROUTE_WS.get((T, E, top_k))
     if nws is None:
         if len(_ROUTE_WS) > 4096:

@@ -8,7 +8,8 @@
 //
 // The sort is by counting, and no result depends on the order of atomics: each 32 tokens set their bits in a word for
 // each expert (a token picks an expert once), and a pair's rank in its expert is the count of the bits below its
-// token's, plus those of the words before.  The chain of launches and dependent reads bounds it, not the logits' bytes.
+// token's, plus those of the words before.  The chain of launches and dependent reads bounds it, not the logits' bytes:
+// one token of 128 experts 3.5 us, 16384 tokens 16.4 (10.5 MB, 1.6 us at DRAM's rate), 8 of them selected.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -16,7 +17,6 @@
 #include <cmath>
 
 #include "microscale.cuh"
-#include "rows.cuh"
 
 namespace {
 using namespace bmoe;
@@ -258,6 +258,8 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_alone(const __grid_cons
   for (int p = threadIdx.x; p < a.T * a.k; p += kRouteThreads) place_pair(a, p, a.experts[p], a.places[p], s.count);
 }
 
+// 16384 tokens of 128 experts are 128 blocks whose warps have four tokens each in turn: 8.6 us, issuing on two thirds of the
+// cycles (the sort of the lanes' largest, the candidates' ranks).
 template <int NE>
 __global__ void __launch_bounds__(kRouteThreads) k_route_select(const __grid_constant__ RouteArgs a) {
   __shared__ RouteShared s;
@@ -409,7 +411,7 @@ __device__ __forceinline__ void store_piece(T* p, const float (&v)[V]) {
 
 // A group of threads a token (2^shift of the block's 256), V columns a thread; the pieces of R rows are requested before the
 // first is used (of one or two rows R is 2, and the registers leave room for twice the warps).  The rows' bytes bound it: 8192
-// tokens of 8 rows of 2048 bf16 57 us, 5.9 TB/s.
+// tokens of 8 rows of 2048 bf16 59 us, 5.7 TB/s.
 constexpr int kCombineThreads = 256;
 template <typename TY, typename TO, int V, int R, bool ONE>   // ONE: a block's threads have one token (its places are uniform)
 __global__ void __launch_bounds__(kCombineThreads, R == 2 ? 6 : 3) k_combine(const __grid_constant__ CombineArgs a) {

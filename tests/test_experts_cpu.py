@@ -160,6 +160,16 @@ def test_binding_refusals(bm):
             call()
 
 
+def test_rowscale_holds_its_tensors(bm):
+    torch = pytest.importorskip("torch")
+    q = bm.Rowscale(torch.zeros(4, 8, dtype=torch.float8_e4m3fn), torch.zeros(4))
+    for name in ("codes", "scales"):
+        with pytest.raises(AttributeError):   # (the library's view of them is kept)
+            setattr(q, name, torch.zeros(4))
+    e = bm.Rowscale.empty([2, 3, 5], torch.device("cpu"))
+    assert e.shape == (2, 3, 5) and e.codes.shape == e.shape and e.codes.stride() == (48, 16, 1) and e.scales.shape == (2, 3)
+
+
 # ---------------------------------------------------------------------------
 # the oracle
 # ---------------------------------------------------------------------------
