@@ -971,8 +971,12 @@ class Rowscale:
         pitch = (cols + 15) & ~15
         dev = device if device is not None else torch.cuda.current_device()
         self = cls.__new__(cls)   # (an allocation each: parts of one cost the host more)
-        codes = torch.empty((*shape[:-1], pitch), dtype=torch.float8_e4m3fn, device=dev)
-        self._codes = codes if pitch == cols else codes[..., :cols]
+        if pitch == cols:
+            codes = torch.empty(shape, dtype=torch.float8_e4m3fn, device=dev)
+        else:
+            codes = torch.empty_strided(shape, (pitch, 1) if dims == 2 else (shape[1] * pitch, pitch, 1),
+                                        dtype=torch.float8_e4m3fn, device=dev)
+        self._codes = codes
         self._scales = scales = torch.empty(shape[:-1], dtype=torch.float32, device=dev)
         self.shape, self.device = shape if isinstance(shape, tuple) else tuple(shape), codes.device
         self._c = _Rowscale(n, cols, pitch, codes.data_ptr(), scales.data_ptr())
