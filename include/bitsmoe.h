@@ -759,8 +759,10 @@ typedef struct bitsmoe_expert_matrices {
  *   status     device int or NULL: BITSMOE_ERR_TIMEOUT is written there if a bounded wait
  *              of the kernel ran out; not cleared by the call.  The results that such a
  *              wait has lost are NaN, with and without it
- * Products are exact and sums fp32; scales multiply the finished sums (which have to
- * stay in fp32's range before and after it); y is rounded once.  w, up and x may start
+ * Products are exact and sums fp32 (for y in bf16 as the tensor core adds, which cuts
+ * off; for y in fp32 rounded to nearest after every few of its additions); scales
+ * multiply the finished sums (which have to stay in fp32's range before and after it);
+ * y is rounded once.  w, up and x may start
  * anywhere (all rows, and matrices, on 16-byte boundaries are read fastest; of others the
  * aligned 16 bytes at a row's two ends are read whole).  Errors: INVALID_ARG, SHAPE,
  * ALIGNMENT, CUDA.  Never allocates, never synchronises; one launch.  P == 0 and rows == 0

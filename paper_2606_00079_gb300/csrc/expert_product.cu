@@ -11,6 +11,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "microscale.cuh"
 #include "tc.cuh"
@@ -35,10 +36,11 @@ struct ExpertArgs {
   int64_t x_ld;
   int w_vec, x_vec;      // rows of the matrices, rows of x start on 16-byte boundaries
   void* y;
-  int y_type, y_vec;     // y_vec: bf16 rows on 16-byte boundaries
+  int y_vec;             // bf16 rows on 16-byte boundaries
   int64_t y_ld;
   int nk, stages, nbuf;  // tensor cores: steps of 128 bytes of the columns, depth of the ring, accumulators in turn
   int splits, sps;       // CTAs that share the columns of a tile, steps of each
+  int chain;             // steps that an accumulator takes (fp32 results: a few)
   int w_next, u_next;    // 1: an expert has matrices of its own (0: one stands for all)
   long long spin;
   int lose;
@@ -47,10 +49,6 @@ struct ExpertArgs {
 
 __device__ __forceinline__ void keep(float* y, float v) { *y = v; }
 __device__ __forceinline__ void keep(__nv_bfloat16* y, float v) { *y = __float2bfloat16_rn(v); }
-__device__ __forceinline__ void store_y(void* y, int type, int64_t i, float v) {
-  if (type == BITSMOE_F32) keep(static_cast<float*>(y) + i, v);
-  else keep(static_cast<__nv_bfloat16*>(y) + i, v);
-}
 
 // ---------------------------------------------------------------------------
 // The groups in shared memory: first[e] the first row of expert e (of y), tiles[e] the tiles of N rows before it, and
@@ -147,7 +145,7 @@ __device__ __forceinline__ int row_of(const ExpertArgs& a, int p) {
 constexpr int kXWarps = 4, kOutWarps = 8, kOutThreads = 32 * kOutWarps;
 constexpr int kTcThreads = 32 * (4 + kXWarps + kOutWarps);
 constexpr int kFewRows = 64;                 // rows of y of a tile from which on pairs take it
-constexpr int kStagesMost = 8;
+constexpr int kStagesMost = 8, kAccumulators = 4;
 constexpr uint32_t kATile = 2 * 128 * 128;   // bytes of a stage's tiles of the matrices
 constexpr int kTcShared = 227 * 1024;        // (all of an SM's, as of every kernel that allocates tensor memory)
 constexpr int kXRows = 4 * kXWarps;          // rows that one pass of x's warps brings
@@ -166,7 +164,7 @@ struct TcShared {
   Groups groups;
   Waves waves;
   alignas(16) float factor[2][256];      // of the rows of y: x's scale, NaN for a row that is not there
-  uint64_t full[kStagesMost], empty[kStagesMost], xfull[kStagesMost], afull[2], aempty[2], drained;
+  uint64_t full[kStagesMost], empty[kStagesMost], xfull[kStagesMost], afull[kAccumulators], aempty[kAccumulators], drained;
   uint32_t slot;
   alignas(16) uint8_t turn[kOutWarps][2][1024];   // 16 rows of y of a warp's 32 results each (of both tiles), on their way out
 };
@@ -291,13 +289,20 @@ __device__ __forceinline__ float silu(float g, float u) {
   return g * __fdividef(g < 0.f ? e : 1.f, 1.f + e) * u;
 }
 
-template <bool F8, bool GLU, bool PAIR>
+// SUMS: fp32 results.  The tensor core cuts off what an addition has below fp32: 500 of them (8000 columns of bf16) lose 7e-6
+// of a sum, of SiLU of it twice that; nothing beside the half step of a result in bf16, but 8 times what sums in fp32 lose.  So
+// an accumulator takes a few steps, and registers add those up to nearest: 2e-7, and 3e-7.  They hold the sums of 64 rows of y;
+// larger products read the matrices more often for it and L2 bounds them (gate and up of 128 experts of 768 x 2048, us, fp32
+// and bf16: 1 token 13.5 and 12.4, 256 124 and 119, 8192 748 and 297).
+template <bool F8, bool GLU, bool PAIR, bool SUMS>
 __global__ void __launch_bounds__(kTcThreads, 1)
     k_expert_tc(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ ExpertArgs a) {
   constexpr int kCols = F8 ? 128 : 64;         // columns of a stage
   constexpr int kRows = GLU ? 128 : 256;       // rows of y's width that a CTA covers
   constexpr int kUnit = PAIR ? 32 : 16;        // rows of y of a tile are a multiple of it, as the MMA takes them
   constexpr int kBoth = PAIR ? 2 : 1;          // CTAs that share a tile
+  using Y = std::conditional_t<SUMS, float, __nv_bfloat16>;
+  static_assert(!(SUMS && PAIR), "");
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t stage = kATile + (uint32_t)(a.N / kBoth) * 128;
@@ -319,7 +324,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       mbar_init_n(s.xfull + i, 32 * kXWarps);
       mbar_init_n(s.empty + i, 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kAccumulators; ++i) {
       mbar_init_n(s.afull + i, 1);
       mbar_init_n(s.aempty + i, kBoth * kOutWarps);
     }
@@ -394,38 +399,44 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
       const int n = (tile_of(a, s.groups, tile, kUnit).n + kUnit - 1) / kUnit * kUnit;
       const uint32_t idesc = idesc_of<F8, PAIR>(n);
-      if (use > 0) ok = mbar_wait(s.aempty + buf, (uint32_t)(use - 1) & 1u, a.spin);
-      ok = __all_sync(0xFFFFFFFFu, ok);
-      if (!ok) break;
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t acc = tmem + (uint32_t)(buf * 2 * a.N);
-      for (int i = 0; i < nk; ++i) {
-        ok = mbar_try_wait(s.full + st, (uint32_t)u & 1u) || mbar_wait(s.full + st, (uint32_t)u & 1u, a.spin);
+      int i0 = 0;
+      do {   // (once, but of fp32 results)
+        if (use > 0) ok = mbar_wait(s.aempty + buf, (uint32_t)(use - 1) & 1u, a.spin);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
-        if (!PAIR) fence_proxy_async();   // x's rows: generic writes -> tensor-core reads
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint64_t o = (uint64_t)((uint32_t)st * (stage >> 4));
+        const uint32_t acc = tmem + (uint32_t)(buf * 2 * a.N);
+        const int last = SUMS ? min(i0 + a.chain, nk) : nk;
+        for (int i = i0; i < last; ++i) {
+          ok = mbar_try_wait(s.full + st, (uint32_t)u & 1u) || mbar_wait(s.full + st, (uint32_t)u & 1u, a.spin);
+          ok = __all_sync(0xFFFFFFFFu, ok);
+          if (!ok) break;
+          if (!PAIR) fence_proxy_async();   // x's rows: generic writes -> tensor-core reads
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint64_t o = (uint64_t)((uint32_t)st * (stage >> 4));
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            mma_of<F8, PAIR>(one, acc + (uint32_t)(h * a.N), da + o + h * (kATile >> 5) + 2 * k, db + o + 2 * k, idesc, (uint32_t)(i | k));
-        if (!(a.lose && (i | it | (int)blockIdx.x) == 0))
+            for (int k = 0; k < 4; ++k)
+              mma_of<F8, PAIR>(one, acc + (uint32_t)(h * a.N), da + o + h * (kATile >> 5) + 2 * k, db + o + 2 * k, idesc, (uint32_t)((i - i0) | k));
+          if (!(a.lose && (i | it | (int)blockIdx.x) == 0))
 #pragma unroll
-          for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, empty[r] + 8u * (uint32_t)st);
-        if (++st == a.stages) {
-          st = 0;
-          ++u;
+            for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, empty[r] + 8u * (uint32_t)st);
+          if (++st == a.stages) {
+            st = 0;
+            ++u;
+          }
         }
-      }
-      if (!ok) break;
+        if (!ok) break;
 #pragma unroll
-      for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, afull[r] + 8u * (uint32_t)buf);
-      if (++buf == a.nbuf) {
-        buf = 0;
-        ++use;
-      }
+        for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, afull[r] + 8u * (uint32_t)buf);
+        if (++buf == a.nbuf) {
+          buf = 0;
+          ++use;
+        }
+        i0 = last;
+      } while (SUMS && i0 < nk);
+      if (!ok) break;
     }
     if (!ok) {
       mma_commit_at<PAIR>(one, smem_u32(&s.drained));
@@ -537,27 +548,73 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (in1) s1 = GLU ? __ldg(a.us + t.e * a.u_sld + m) : __ldg(a.ws + t.e * a.w_sld + m + 128);
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kOutThreads) : "memory");   // (a warp that passes has read the factors of two tiles ago)
-      if (ok) ok = mbar_wait_idle(s.afull + buf, (uint32_t)use & 1u, a.spin);
-      ok = __all_sync(0xFFFFFFFFu, ok);
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      float sum[SUMS ? 2 : 1][2][16];   // columns 16 side + 32 i + q of both tiles
+      if constexpr (SUMS) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) sum[i][h][q] = 0.f;
+        for (int i0 = 0;; ) {
+          if (ok) ok = mbar_wait_idle(s.afull + buf, (uint32_t)use & 1u, a.spin);
+          ok = __all_sync(0xFFFFFFFFu, ok);
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t tl = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(buf * 2 * a.N + 16 * side);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (ok && nk > 0 && 16 * side + 32 * i < t.n) {
+              uint32_t v[2][16];
+              tmem_ld16_two(tl + (uint32_t)(32 * i), tl + (uint32_t)(a.N + 32 * i), v[0], v[1]);
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) sum[i][h][q] += __uint_as_float(v[h][q]);
+            }
+          i0 += a.chain;
+          if (!ok || i0 >= nk) break;
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(aempty0 + 8u * (uint32_t)buf);
+          if (++buf == a.nbuf) {
+            buf = 0;
+            ++use;
+          }
+        }
+      } else {
+        if (ok) ok = mbar_wait_idle(s.afull + buf, (uint32_t)use & 1u, a.spin);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      }
       const uint32_t tl = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(buf * 2 * a.N);
       if (!PAIR && a.splits > 1) {   // the part of the columns: all that is left of it is summed below
-        for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {   // (N is at most 64)
+          const int c0 = 16 * side + 32 * i;
+          if (c0 >= t.n) break;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            uint32_t v[16];
-            if (ok && nk > 0) tmem_ld16(tl + (uint32_t)(h * a.N + c0), v);
+            float v[16];
+            if constexpr (SUMS) {
 #pragma unroll
-            for (int q = 0; q < 16; ++q) red[(h * a.N + c0 + q) * 128 + r] = !ok ? __uint_as_float(kLost) : nk > 0 ? __uint_as_float(v[q]) : 0.f;
+              for (int q = 0; q < 16; ++q) v[q] = sum[i][h][q];
+            } else {
+              uint32_t d[16];
+              if (ok && nk > 0) tmem_ld16(tl + (uint32_t)(h * a.N + c0), d);
+#pragma unroll
+              for (int q = 0; q < 16; ++q) v[q] = nk > 0 ? __uint_as_float(d[q]) : 0.f;
+            }
+#pragma unroll
+            for (int q = 0; q < 16; ++q) red[(h * a.N + c0 + q) * 128 + r] = ok ? v[q] : __uint_as_float(kLost);
           }
         }
       } else if (!ok) {
         for (int c = side; c < t.n; c += 2) {
           const int64_t at = (int64_t)(t.p0 + c) * a.y_ld + m;
-          if (in0) store_y(a.y, a.y_type, at, __uint_as_float(kLost));
-          if (!GLU && in1) store_y(a.y, a.y_type, at + 128, __uint_as_float(kLost));
+          if (in0) keep(static_cast<Y*>(a.y) + at, __uint_as_float(kLost));
+          if (!GLU && in1) keep(static_cast<Y*>(a.y) + at + 128, __uint_as_float(kLost));
         }
-      } else if (a.y_vec) {
+      } else if (!SUMS && a.y_vec) {
         // bf16 rows on 16-byte boundaries: rows lie along the lanes of tensor memory; turned by way of shared memory a row of y
         // goes out 16 bytes a lane
         // (a row is 64 bytes; its 16-byte pieces are turned by its number, so that no two of eight rows meet in a bank)
@@ -629,28 +686,31 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           __syncwarp();
         }
       } else {
-        const auto go_out = [&](auto* y) {   // a row of the matrix a lane
-          for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
-            uint32_t v[2][16];
-            tmem_ld16(tl + (uint32_t)c0, v[0]);
-            tmem_ld16(tl + (uint32_t)(a.N + c0), v[1]);
-#pragma unroll
-            for (int q = 0; q < 16; ++q) {
-              const float f = factor[c0 + q];
-              const float v0 = __uint_as_float(v[0][q]) * (F8 ? s0 * f : f), v1 = __uint_as_float(v[1][q]) * (F8 ? s1 * f : f);
-              if (c0 + q >= t.n) continue;
-              auto* at = y + (int64_t)(t.p0 + c0 + q) * a.y_ld + m;
-              if constexpr (GLU) {
-                if (in0) keep(at, silu(v0, v1));
-              } else {
-                if (in0) keep(at, v0);
-                if (in1) keep(at + 128, v1);
-              }
-            }
+        // a row of the matrix a lane
+        const auto put = [&](int c, float g, float u) {   // column c of both tiles
+          if (c >= t.n) return;
+          const float f = factor[c], v0 = g * (F8 ? s0 * f : f), v1 = u * (F8 ? s1 * f : f);
+          Y* at = static_cast<Y*>(a.y) + (int64_t)(t.p0 + c) * a.y_ld + m;
+          if constexpr (GLU) {
+            if (in0) keep(at, silu(v0, v1));
+          } else {
+            if (in0) keep(at, v0);
+            if (in1) keep(at + 128, v1);
           }
         };
-        if (a.y_type == BITSMOE_F32) go_out(static_cast<float*>(a.y));
-        else go_out(static_cast<__nv_bfloat16*>(a.y));
+        if constexpr (SUMS) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) put(16 * side + 32 * i + q, sum[i][0][q], sum[i][1][q]);
+        } else {
+          for (int c0 = 16 * side; c0 < t.n; c0 += 32) {
+            uint32_t v[2][16];
+            tmem_ld16_two(tl + (uint32_t)c0, tl + (uint32_t)(a.N + c0), v[0], v[1]);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) put(c0 + q, __uint_as_float(v[0][q]), __uint_as_float(v[1][q]));
+          }
+        }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
@@ -685,10 +745,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           if (mh < a.rows) v[h] *= F8 ? f * __ldg((GLU && h ? a.us + t.e * a.u_sld : a.ws + t.e * a.w_sld) + mh) : f;
         }
         if constexpr (GLU) {
-          if (m < a.rows) store_y(a.y, a.y_type, at, silu(v[0], v[1]));
+          if (m < a.rows) keep(static_cast<Y*>(a.y) + at, silu(v[0], v[1]));
         } else {
-          if (m < a.rows) store_y(a.y, a.y_type, at, v[0]);
-          if (m + 128 < a.rows) store_y(a.y, a.y_type, at + 128, v[1]);
+          if (m < a.rows) keep(static_cast<Y*>(a.y) + at, v[0]);
+          if (m + 128 < a.rows) keep(static_cast<Y*>(a.y) + at + 128, v[1]);
         }
       }
     }
@@ -755,10 +815,10 @@ int clusters_at_once(int dev, int n) {
   return c;
 }
 
-template <bool F8, bool GLU, bool PAIR>
+template <bool F8, bool GLU, bool PAIR, bool SUMS>
 cudaError_t launch_tc_as(const ExpertArgs& a, const CUtensorMap& wm, const CUtensorMap& um, int64_t groups, int dev, cudaStream_t st) {
-  auto kern = k_expert_tc<F8, GLU, PAIR>;
-  const cudaError_t e = allow_shared<k_expert_tc<F8, GLU, PAIR>>(dev, kTcShared);
+  auto kern = k_expert_tc<F8, GLU, PAIR, SUMS>;
+  const cudaError_t e = allow_shared<k_expert_tc<F8, GLU, PAIR, SUMS>>(dev, kTcShared);
   if (e != cudaSuccess) return e;
   const unsigned size = PAIR ? 2u : (unsigned)a.splits;
   cudaLaunchAttribute attr[2];
@@ -777,9 +837,10 @@ cudaError_t launch_tc_as(const ExpertArgs& a, const CUtensorMap& wm, const CUten
   return cudaLaunchKernelEx(&cfg, kern, wm, um, a);
 }
 
-template <bool F8, bool GLU>
+template <bool F8, bool GLU, bool SUMS>
 cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um, int dev, int sms, cudaStream_t st) {
   a.N = tile_rows(a.P, a.E);
+  if (SUMS) a.N = std::min(a.N, kFewRows);   // (what registers hold)
   bool pair = a.N > kFewRows;
   if (pair) {
     // Pairs where a third of them have a tile; else smaller tiles of single CTAs, over which the columns can be split too.  One
@@ -797,19 +858,21 @@ cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um
   a.nk = (a.cols + (F8 ? 127 : 63)) / (F8 ? 128 : 64);
   a.w_next = a.w_eld != 0;
   a.u_next = a.u_eld != 0;
-  a.nbuf = 4 * a.N <= 512 ? 2 : 1;
+  a.nbuf = std::min(SUMS ? kAccumulators : 2, 512 / (2 * a.N));
   const int64_t most = std::min<int64_t>(a.P, (int64_t)a.P / a.N + a.E) * a.mt;   // tiles at most
   // Few tiles: the columns over clusters of as many CTAs as the SMs hold (one token by 4096 x 4096 9.8 us, unsplit 24.0; through
   // gate and up of eight experts of 768 x 2048 11.6 and 14.8).
   a.splits = 1;
   if (!pair)   // (clusters that do not all run at once would take a second turn)
     for (int n = 8; n > 1 && a.splits == 1; n /= 2)
-      if (most * n <= sms && a.nk >= 2 * n && most <= clusters_at_once<k_expert_tc<F8, GLU, false>>(dev, n)) a.splits = n;
+      if (most * n <= sms && a.nk >= 2 * n && most <= clusters_at_once<k_expert_tc<F8, GLU, false, SUMS>>(dev, n)) a.splits = n;
   a.sps = (a.nk + a.splits - 1) / a.splits;
   const size_t room = kTcShared - 1024 - sizeof(TcShared) - (a.splits > 1 ? (size_t)a.N * 1024 : 0);
   a.stages = std::min(kStagesMost, (int)(room / (kATile + (size_t)a.N * (pair ? 64 : 128))));
-  if (pair) return launch_tc_as<F8, GLU, true>(a, wm, um, std::min<int64_t>({most, sms / 2, kPairsMost}), dev, st);
-  return launch_tc_as<F8, GLU, false>(a, wm, um, std::min<int64_t>(most, sms / a.splits), dev, st);
+  a.chain = F8 ? 8 : 2;   // 32 additions, of bf16 8 (products of 8 bits leave less to cut off); twice that: errors 1.5 times, 697 us in place of 748
+  if constexpr (!SUMS)
+    if (pair) return launch_tc_as<F8, GLU, true, false>(a, wm, um, std::min<int64_t>({most, sms / 2, kPairsMost}), dev, st);
+  return launch_tc_as<F8, GLU, false, SUMS>(a, wm, um, std::min<int64_t>(most, sms / a.splits), dev, st);
 }
 
 int matrices_check(const bitsmoe_expert_matrices* m) {
@@ -875,7 +938,6 @@ extern "C" int bitsmoe_expert_product(const bitsmoe_expert_product_args* args, v
   a.xs = g.x_scales;
   a.x_ld = g.x_ld;
   a.y = g.y;
-  a.y_type = g.y_type;
   a.y_ld = g.y_ld;
   a.y_vec = g.y_type == BITSMOE_BF16 && on_boundaries(g.y, g.y_ld, 2, g.P);
   a.spin = debug_wait_clocks() > 0 ? debug_wait_clocks() : kWaitClocks;
@@ -887,7 +949,12 @@ extern "C" int bitsmoe_expert_product(const bitsmoe_expert_product_args* args, v
   std::memset(&wm, 0, sizeof(wm));
   std::memset(&um, 0, sizeof(um));
   a.w_vec = tc_maps(a, f8, &wm, &um);
-  e = f8 ? (a.up ? launch_tc<true, true>(a, wm, um, dev, sms, st) : launch_tc<true, false>(a, wm, um, dev, sms, st))
-         : (a.up ? launch_tc<false, true>(a, wm, um, dev, sms, st) : launch_tc<false, false>(a, wm, um, dev, sms, st));
+  const auto go = [&](auto f8_, auto glu) {
+    constexpr bool kF8 = decltype(f8_)::value, kGlu = decltype(glu)::value;
+    return g.y_type == BITSMOE_F32 ? launch_tc<kF8, kGlu, true>(a, wm, um, dev, sms, st) : launch_tc<kF8, kGlu, false>(a, wm, um, dev, sms, st);
+  };
+  constexpr std::true_type yes;
+  constexpr std::false_type no;
+  e = f8 ? (a.up ? go(yes, yes) : go(yes, no)) : (a.up ? go(no, yes) : go(no, no));
   return e == cudaSuccess ? BITSMOE_OK : record_cuda_error((int)e);
 }

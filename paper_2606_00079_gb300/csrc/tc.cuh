@@ -253,6 +253,18 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "memory");
 }
 
+// 16 columns from each of two places, one wait.
+__device__ __forceinline__ void tmem_ld16_two(uint32_t from_v, uint32_t from_w, uint32_t (&v)[16], uint32_t (&w)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%32];\n"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%33];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=&r"(v[0]), "=&r"(v[1]), "=&r"(v[2]), "=&r"(v[3]), "=&r"(v[4]), "=&r"(v[5]), "=&r"(v[6]), "=&r"(v[7]), "=&r"(v[8]), "=&r"(v[9]), "=&r"(v[10]), "=&r"(v[11]), "=&r"(v[12]), "=&r"(v[13]), "=&r"(v[14]), "=&r"(v[15]),
+        "=&r"(w[0]), "=&r"(w[1]), "=&r"(w[2]), "=&r"(w[3]), "=&r"(w[4]), "=&r"(w[5]), "=&r"(w[6]), "=&r"(w[7]), "=&r"(w[8]), "=&r"(w[9]), "=&r"(w[10]), "=&r"(w[11]), "=&r"(w[12]), "=&r"(w[13]), "=&r"(w[14]), "=&r"(w[15])
+      : "r"(from_v), "r"(from_w)
+      : "memory");
+}
+
 // 16 columns of 32 lanes as two halves of 16 lanes, asynchronous (tmem_wait): v[h][4 j ..] of lane l are columns 8 j + 2 (l % 4), + 1
 // of rows 16 h + l / 4 and, in the last two, + 8: the fragments that store_transposed takes.
 __device__ __forceinline__ void tmem_ld_fragments(uint32_t taddr, uint32_t (&v)[2][8]) {

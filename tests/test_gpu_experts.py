@@ -418,8 +418,8 @@ def test_expert_product_lost_waits(env, kind, ty, glu, fan):
     off = torch.arange(0, P + 1, P // E, dtype=torch.int32).cuda()
     idx = torch.randint(0, 2 * P, (P,), generator=g, dtype=torch.int32).cuda() if fan else None
     kw = dict(index=idx, fan=max(fan, 1), up=up)
-    ref = bm.expert_product(w, x, off, **kw)
     for dt in (torch.float32, torch.bfloat16):
+        ref = bm.expert_product(w, x, off, dtype=dt, **kw)
         for with_status in (True, False):
             buf = torch.full((P, R + 8), 7.0, dtype=dt, device="cuda")
             y, status = buf[:, :R], torch.zeros(1, dtype=torch.int32, device="cuda")
@@ -432,10 +432,10 @@ def test_expert_product_lost_waits(env, kind, ty, glu, fan):
             assert int(status.item()) == (bm.ERR_CODE["TIMEOUT"] if with_status else 0)
             lost = torch.isnan(y)
             assert bool(lost[:rows, :cols].all()) and not bool(lost.all())
-            assert torch.equal(y[~lost], ref.to(dt)[~lost])
+            assert torch.equal(y[~lost], ref[~lost])
             assert (buf[:, R:] == 7).all()
             status.zero_()
-            assert torch.equal(bm.expert_product(w, x, off, y=y, status=status, **kw), ref.to(dt))
+            assert torch.equal(bm.expert_product(w, x, off, y=y, status=status, **kw), ref)
             assert int(status.item()) == 0
 
 
@@ -443,8 +443,8 @@ def test_expert_product_lost_waits(env, kind, ty, glu, fan):
 @pytest.mark.parametrize("R", [64, 250, 256, 300, 1000])
 @pytest.mark.parametrize("shift", [0, 1, 8])
 def test_expert_product_16_bit_results(env, ty, R, shift):
-    """bf16 rows of y on 16-byte boundaries (turned on their way out) and off them: the same bits, and the fp32 results
-    rounded once; nothing beside them is touched."""
+    """bf16 rows of y on 16-byte boundaries (turned on their way out) and off them: the same bits; nothing beside them is
+    touched."""
     torch, bm = env
     g = torch.Generator().manual_seed(R)
     C = 320
@@ -453,12 +453,12 @@ def test_expert_product_16_bit_results(env, ty, R, shift):
     x, xs, _ = pitched(torch, torch.randn(700, C, generator=g), ty)
     off = torch.tensor([1, 3, 300, 300, 698], dtype=torch.int32).cuda()
     for u_ in (None, wrap(bm, up, us)):
-        f = torch.full((700, R), 7.0, device="cuda")
-        bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, up=u_, y=f)
+        other = torch.full((700, (R + 7) // 8 * 8 + (8 if shift == 1 else 1)), 7.0, dtype=torch.bfloat16, device="cuda")[:, :R]
+        bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, up=u_, y=other)
         buf = torch.full((700, (R + 24) // 8 * 8 + (1 if shift == 1 else 0)), 7.0, dtype=torch.bfloat16, device="cuda")
         y = buf[:, shift:shift + R]
         bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, up=u_, y=y)
-        assert torch.equal(y, f.bfloat16())
+        assert torch.equal(y, other)
         rest = buf.clone()
         rest[:, shift:shift + R] = 7.0
         assert (rest == 7).all() and (y[0] == 7).all() and (y[698:] == 7).all()
@@ -712,3 +712,25 @@ def test_swiglu_of_large_gates(env, T, E, R, out):
     want = torch.cat([(gd[e] / (1 + torch.exp(-gd[e])) * 1.5).expand(o[e + 1] - o[e], R) for e in range(E)])
     rel = 12 * u if out == "f32" else 2.0 ** -8 + 13 * u
     assert ((y - want).abs() <= rel * want.abs()).all()
+
+
+@pytest.mark.parametrize("E,P", [(1, 3), (5, 300), (4, 2000)])   # columns split, and whole
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+def test_fp32_results_of_many_columns(env, E, P, ty):
+    """Sums of products of one sign, where cutting off adds up.  Registers add what accumulators of at most 8 additions (bf16; 32)
+    hold: of 8 (32) additions that lose less than 2^-23 of the sum so far each, their n sums u each, and the clusters' 8; the
+    scales' products, and the decoded values' roundings in fp32, 5."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(E)
+    C, R = 8192, 300
+    w, ws, _ = pitched(torch, torch.rand(E, R, C, generator=g) + 0.1, ty)
+    x, xs, _ = pitched(torch, torch.rand(P, C, generator=g) + 0.1, ty)
+    off = torch.linspace(0, P, E + 1).int().cuda()
+    w, x = wrap(bm, w, ws), wrap(bm, x, xs)
+    y = bm.expert_product(w, x, off, dtype=torch.float32).double()
+    wd = w.double() if ty == "bf16" else bm.rowscale_dequantize(w).double()
+    xd = x.double() if ty == "bf16" else bm.rowscale_dequantize(x).double()
+    o = off.tolist()
+    want = torch.cat([xd[o[e]:o[e + 1]] @ wd[e].T for e in range(E)])
+    chains, adds = (64, 8) if ty == "bf16" else (8, 32)
+    assert ((y - want).abs() <= (2 * adds + chains + 8 + 5) * u * want).all()
