@@ -145,6 +145,9 @@ __device__ __forceinline__ int row_of(const ExpertArgs& a, int p) {
 constexpr int kXWarps = 4, kOutWarps = 8, kOutThreads = 32 * kOutWarps;
 constexpr int kTcThreads = 32 * (4 + kXWarps + kOutWarps);
 constexpr int kFewRows = 64;                 // rows of y of a tile from which on pairs take it
+constexpr int kSumRows = 128;                // rows of y of a tile of many fp32 results
+constexpr int kSumRegs = 184, kOtherRegs = 72;   // registers of the warps that hold their sums, and of the others (128 at launch)
+static_assert(32 * kOutWarps * kSumRegs + 32 * (4 + kXWarps) * kOtherRegs <= 128 * kTcThreads && kOutWarps % 4 == 0 && kXWarps % 4 == 0, "");
 constexpr int kStagesMost = 8, kAccumulators = 4;
 constexpr uint32_t kATile = 2 * 128 * 128;   // bytes of a stage's tiles of the matrices
 constexpr int kTcShared = 227 * 1024;        // (all of an SM's, as of every kernel that allocates tensor memory)
@@ -291,17 +294,18 @@ __device__ __forceinline__ float silu(float g, float u) {
 
 // SUMS: fp32 results.  The tensor core cuts off what an addition has below fp32: 500 of them (8000 columns of bf16) lose 7e-6
 // of a sum, of SiLU of it twice that; nothing beside the half step of a result in bf16, but 8 times what sums in fp32 lose.  So
-// an accumulator takes a few steps, and registers add those up to nearest: 2e-7, and 3e-7.  They hold the sums of 64 rows of y;
-// larger products read the matrices more often for it and L2 bounds them (gate and up of 128 experts of 768 x 2048, us, fp32
-// and bf16: 1 token 13.5 and 12.4, 256 124 and 119, 8192 748 and 297).
-template <bool F8, bool GLU, bool PAIR, bool SUMS>
+// an accumulator takes a few steps, and registers add those up to nearest: 2e-7, and 3e-7.  They hold the sums of SUMS rows of
+// y, 64 or 128; large products read the matrices more often for it and L2 bounds them (gate and up of 128 experts of 768 x 2048,
+// us, fp32 and bf16: 1 token 13.5 and 12.4, 256 124 and 119, 8192 581 and 300).
+template <bool F8, bool GLU, bool PAIR, int SUMS>
 __global__ void __launch_bounds__(kTcThreads, 1)
     k_expert_tc(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ ExpertArgs a) {
   constexpr int kCols = F8 ? 128 : 64;         // columns of a stage
   constexpr int kRows = GLU ? 128 : 256;       // rows of y's width that a CTA covers
   constexpr int kUnit = PAIR ? 32 : 16;        // rows of y of a tile are a multiple of it, as the MMA takes them
   constexpr int kBoth = PAIR ? 2 : 1;          // CTAs that share a tile
-  using Y = std::conditional_t<SUMS, float, __nv_bfloat16>;
+  constexpr bool kSplit = !PAIR && SUMS <= kFewRows;
+  using Y = std::conditional_t<(SUMS > 0), float, __nv_bfloat16>;
   static_assert(!(SUMS && PAIR), "");
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -361,170 +365,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   };
   bool ok = true;
 
-  if (wid == 0) {
-    if (lane == 0 && a.w_vec) {
-      const uint32_t full0 = at0(s.full);
-      int st = 0, u = 0, n = 0;
-      for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
-        const Tile t = tile_of(a, s.groups, tile, kUnit);
-        const int m0 = (kBoth * t.m + half) * kRows;
-        for (int i = 0; i < nk; ++i, ++n) {
-          if (u > 0) ok = mbar_wait(s.empty + st, (uint32_t)(u - 1) & 1u, a.spin);
-          if (!ok) break;
-          const uint32_t bar = full0 + 8u * (uint32_t)st, dst = smem_u32(sm) + (uint32_t)st * stage;
-          if (half == 0) mbar_expect_tx(s.full + st, kBoth * kATile);   // of both CTAs
-          tma_load_3d<PAIR>(dst, &wmap, (k0 + i) * kCols, m0, t.e * a.w_next, bar);   // 256 rows, with U 128
-          if (GLU) tma_load_3d<PAIR>(dst + kATile / 2, &umap, (k0 + i) * kCols, m0, t.e * a.u_next, bar);
-          if (++st == a.stages) {
-            st = 0;
-            ++u;
-          }
-        }
-      }
-      // copies in flight, of both CTAs (after a timeout an arrival of the phase may be missing)
-      if (half == 0)
-        for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok ? kWaitClocks : a.spin);
-    }
-    __syncwarp();
-  } else if (wid == 1 && half == 0) {
-    const uint32_t one = elect_one();
-    const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(sm) + kATile);
-    uint32_t empty[kBoth], afull[kBoth];
-#pragma unroll
-    for (int r = 0; r < kBoth; ++r) {
-      empty[r] = PAIR ? cluster_address(smem_u32(s.empty), (uint32_t)r) : smem_u32(s.empty);
-      afull[r] = PAIR ? cluster_address(smem_u32(s.afull), (uint32_t)r) : smem_u32(s.afull);
-    }
-    int st = 0, u = 0, buf = 0, use = 0;
-    for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
-      const int n = (tile_of(a, s.groups, tile, kUnit).n + kUnit - 1) / kUnit * kUnit;
-      const uint32_t idesc = idesc_of<F8, PAIR>(n);
-      int i0 = 0;
-      do {   // (once, but of fp32 results)
-        if (use > 0) ok = mbar_wait(s.aempty + buf, (uint32_t)(use - 1) & 1u, a.spin);
-        ok = __all_sync(0xFFFFFFFFu, ok);
-        if (!ok) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t acc = tmem + (uint32_t)(buf * 2 * a.N);
-        const int last = SUMS ? min(i0 + a.chain, nk) : nk;
-        for (int i = i0; i < last; ++i) {
-          ok = mbar_try_wait(s.full + st, (uint32_t)u & 1u) || mbar_wait(s.full + st, (uint32_t)u & 1u, a.spin);
-          ok = __all_sync(0xFFFFFFFFu, ok);
-          if (!ok) break;
-          if (!PAIR) fence_proxy_async();   // x's rows: generic writes -> tensor-core reads
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint64_t o = (uint64_t)((uint32_t)st * (stage >> 4));
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              mma_of<F8, PAIR>(one, acc + (uint32_t)(h * a.N), da + o + h * (kATile >> 5) + 2 * k, db + o + 2 * k, idesc, (uint32_t)((i - i0) | k));
-          if (!(a.lose && (i | it | (int)blockIdx.x) == 0))
-#pragma unroll
-            for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, empty[r] + 8u * (uint32_t)st);
-          if (++st == a.stages) {
-            st = 0;
-            ++u;
-          }
-        }
-        if (!ok) break;
-#pragma unroll
-        for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, afull[r] + 8u * (uint32_t)buf);
-        if (++buf == a.nbuf) {
-          buf = 0;
-          ++use;
-        }
-        i0 = last;
-      } while (SUMS && i0 < nk);
-      if (!ok) break;
-    }
-    if (!ok) {
-      mma_commit_at<PAIR>(one, smem_u32(&s.drained));
-      mbar_wait(&s.drained, 0u);
-    }
-    __syncwarp();
-  } else if (PAIR && wid == 2) {
-    if (lane == 0) {
-      const uint32_t full0 = at0(s.full);
-      int st = 0, u = 0;
-      for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it))
-        for (int i = 0; i < nk; ++i) {
-          ok = mbar_wait(s.xfull + st, (uint32_t)u & 1u, a.spin);
-          if (!ok) break;
-          fence_proxy_async();   // generic writes -> tensor-core reads
-          mbar_arrive_cluster(full0 + 8u * (uint32_t)st);
-          if (++st == a.stages) {
-            st = 0;
-            ++u;
-          }
-        }
-    }
-    __syncwarp();
-  } else if (PAIR && wid == 3) {
-    plan_waves(a, s.groups, s.waves, ntiles, step, first, kUnit);
-  } else if (wid >= 4 && wid < 4 + kXWarps) {
-    const int g = tid - 128, chunk = g & 7, r0 = g >> 3;   // 16 bytes of rows r0 + kXRows j
-    const uint32_t at = (uint32_t)r0 * 128u + (uint32_t)((chunk ^ (r0 & 7)) << 4);
-    const int width = a.cols * (F8 ? 1 : 2);
-    constexpr int kPasses = (PAIR ? 128 : kFewRows) / kXRows;
-    int st = 0, u = 0;
-    for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
-      const Tile t = tile_of(a, s.groups, tile, kUnit);
-      const int mine = (t.n + kUnit - 1) / kUnit * kUnit / kBoth;   // rows of this CTA
-      const uint8_t* src[kPasses];
-#pragma unroll
-      for (int j = 0; j < kPasses; ++j) {
-        const int r = r0 + kXRows * j, q = half * mine + r;
-        const int row = r < mine && q < t.n ? row_of(a, t.p0 + q) : -1;
-        src[j] = row < 0 ? nullptr : static_cast<const uint8_t*>(a.x) + (int64_t)row * a.x_ld * (F8 ? 1 : 2) + chunk * 16;
-      }
-      for (int i = 0; i < nk; ++i) {
-        if (u > 0) ok = mbar_try_wait(s.empty + st, (uint32_t)(u - 1) & 1u) || mbar_wait(s.empty + st, (uint32_t)(u - 1) & 1u, a.spin);
-        ok = __all_sync(0xFFFFFFFFu, ok);
-        if (!ok) break;
-        const uint32_t dst = smem_u32(sm) + (uint32_t)st * stage + kATile + at;
-        const int b = (k0 + i) * 128, left = min(max(width - b - chunk * 16, 0), 16);
-        uint64_t* there = (PAIR ? s.xfull : s.full) + st;
-        const auto put = [&](uint32_t to, const uint4& v) {
-          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-        };
-        if (!a.w_vec) {   // the matrices too: rows r0 + kXRows j of the two tiles
-          const int m0 = (kBoth * t.m + half) * kRows;
-#pragma unroll 4
-          for (int j = 0; j < 256 / kXRows; ++j) {
-            const int r = r0 + kXRows * j;
-            const bool up = GLU && r >= 128;
-            const int m = m0 + (up ? r - 128 : r);
-            const uint8_t* row = static_cast<const uint8_t*>(up ? a.up : a.w) +
-                                 ((int64_t)t.e * (up ? a.u_eld : a.w_eld) + (int64_t)m * (up ? a.u_ld : a.w_ld)) * (F8 ? 1 : 2);
-            put(dst - kATile + (uint32_t)j * (kXRows * 128u), load16_anywhere(row + b + chunk * 16, m < a.rows ? left : 0));
-          }
-        }
-        if (a.x_vec) {
-#pragma unroll
-          for (int j = 0; j < kPasses; ++j)
-            if (r0 + kXRows * j < mine) {
-              const int bytes = src[j] ? left : 0;
-              cp_async16(dst + (uint32_t)j * (kXRows * 128u), bytes ? src[j] + b : static_cast<const uint8_t*>(a.x), bytes);
-            }
-          cp_async_arrive(there);
-        } else {   // rows off 16-byte boundaries
-#pragma unroll
-          for (int j = 0; j < kPasses; ++j)
-            if (r0 + kXRows * j < mine) {
-              put(dst + (uint32_t)j * (kXRows * 128u), load16_anywhere(src[j] ? src[j] + b : static_cast<const uint8_t*>(a.x), src[j] ? left : 0));
-            }
-          mbar_arrive(there);
-        }
-        if (++st == a.stages) {
-          st = 0;
-          ++u;
-        }
-      }
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncwarp();
-  } else if (wid >= 4 + kXWarps) {
+  if (wid >= 4 + kXWarps) {
+    if constexpr (SUMS > kFewRows) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));   // (128 sums a thread)
     const int quarter = wid & 3, side = (wid - 4 - kXWarps) >> 2;
     const uint32_t aempty0 = at0(s.aempty);
     int buf = 0, use = 0;
@@ -548,10 +390,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (in1) s1 = GLU ? __ldg(a.us + t.e * a.u_sld + m) : __ldg(a.ws + t.e * a.w_sld + m + 128);
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kOutThreads) : "memory");   // (a warp that passes has read the factors of two tiles ago)
-      float sum[SUMS ? 2 : 1][2][16];   // columns 16 side + 32 i + q of both tiles
-      if constexpr (SUMS) {
+      float sum[SUMS ? SUMS / 32 : 1][2][16];   // columns 16 side + 32 i + q of both tiles
+      if constexpr (SUMS > 0) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < SUMS / 32; ++i)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -562,7 +404,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t tl = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(buf * 2 * a.N + 16 * side);
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < SUMS / 32; ++i)
             if (ok && nk > 0 && 16 * side + 32 * i < t.n) {
               uint32_t v[2][16];
               tmem_ld16_two(tl + (uint32_t)(32 * i), tl + (uint32_t)(a.N + 32 * i), v[0], v[1]);
@@ -587,7 +429,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
       const uint32_t tl = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(buf * 2 * a.N);
-      if (!PAIR && a.splits > 1) {   // the part of the columns: all that is left of it is summed below
+      if (kSplit && a.splits > 1) {   // the part of the columns: all that is left of it is summed below
 #pragma unroll
         for (int i = 0; i < 2; ++i) {   // (N is at most 64)
           const int c0 = 16 * side + 32 * i;
@@ -595,9 +437,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float v[16];
-            if constexpr (SUMS) {
+            if constexpr (SUMS > 0) {
 #pragma unroll
-              for (int q = 0; q < 16; ++q) v[q] = sum[i][h][q];
+              for (int q = 0; q < 16; ++q) v[q] = sum[kSplit ? i : 0][h][q];
             } else {
               uint32_t d[16];
               if (ok && nk > 0) tmem_ld16(tl + (uint32_t)(h * a.N + c0), d);
@@ -698,9 +540,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             if (in1) keep(at + 128, v1);
           }
         };
-        if constexpr (SUMS) {
+        if constexpr (SUMS > 0) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < SUMS / 32; ++i)
 #pragma unroll
             for (int q = 0; q < 16; ++q) put(16 * side + 32 * i + q, sum[i][0][q], sum[i][1][q]);
         } else {
@@ -721,13 +563,179 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         ++use;
       }
     }
+  } else {
+    if constexpr (SUMS > kFewRows) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (wid == 0) {
+      if (lane == 0 && a.w_vec) {
+        const uint32_t full0 = at0(s.full);
+        int st = 0, u = 0, n = 0;
+        for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
+          const Tile t = tile_of(a, s.groups, tile, kUnit);
+          const int m0 = (kBoth * t.m + half) * kRows;
+          for (int i = 0; i < nk; ++i, ++n) {
+            if (u > 0) ok = mbar_wait(s.empty + st, (uint32_t)(u - 1) & 1u, a.spin);
+            if (!ok) break;
+            const uint32_t bar = full0 + 8u * (uint32_t)st, dst = smem_u32(sm) + (uint32_t)st * stage;
+            if (half == 0) mbar_expect_tx(s.full + st, kBoth * kATile);   // of both CTAs
+            tma_load_3d<PAIR>(dst, &wmap, (k0 + i) * kCols, m0, t.e * a.w_next, bar);   // 256 rows, with U 128
+            if (GLU) tma_load_3d<PAIR>(dst + kATile / 2, &umap, (k0 + i) * kCols, m0, t.e * a.u_next, bar);
+            if (++st == a.stages) {
+              st = 0;
+              ++u;
+            }
+          }
+        }
+        // copies in flight, of both CTAs (after a timeout an arrival of the phase may be missing)
+        if (half == 0)
+          for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok ? kWaitClocks : a.spin);
+      }
+      __syncwarp();
+    } else if (wid == 1 && half == 0) {
+      const uint32_t one = elect_one();
+      const uint64_t da = sw128_desc(smem_u32(sm)), db = sw128_desc(smem_u32(sm) + kATile);
+      uint32_t empty[kBoth], afull[kBoth];
+#pragma unroll
+      for (int r = 0; r < kBoth; ++r) {
+        empty[r] = PAIR ? cluster_address(smem_u32(s.empty), (uint32_t)r) : smem_u32(s.empty);
+        afull[r] = PAIR ? cluster_address(smem_u32(s.afull), (uint32_t)r) : smem_u32(s.afull);
+      }
+      int st = 0, u = 0, buf = 0, use = 0;
+      for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
+        const int n = (tile_of(a, s.groups, tile, kUnit).n + kUnit - 1) / kUnit * kUnit;
+        const uint32_t idesc = idesc_of<F8, PAIR>(n);
+        int i0 = 0;
+        do {   // (once, but of fp32 results)
+          if (use > 0) ok = mbar_wait(s.aempty + buf, (uint32_t)(use - 1) & 1u, a.spin);
+          ok = __all_sync(0xFFFFFFFFu, ok);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t acc = tmem + (uint32_t)(buf * 2 * a.N);
+          const int last = SUMS ? min(i0 + a.chain, nk) : nk;
+          for (int i = i0; i < last; ++i) {
+            ok = mbar_try_wait(s.full + st, (uint32_t)u & 1u) || mbar_wait(s.full + st, (uint32_t)u & 1u, a.spin);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            if (!PAIR) fence_proxy_async();   // x's rows: generic writes -> tensor-core reads
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint64_t o = (uint64_t)((uint32_t)st * (stage >> 4));
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                mma_of<F8, PAIR>(one, acc + (uint32_t)(h * a.N), da + o + h * (kATile >> 5) + 2 * k, db + o + 2 * k, idesc, (uint32_t)((i - i0) | k));
+            if (!(a.lose && (i | it | (int)blockIdx.x) == 0))
+#pragma unroll
+              for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, empty[r] + 8u * (uint32_t)st);
+            if (++st == a.stages) {
+              st = 0;
+              ++u;
+            }
+          }
+          if (!ok) break;
+#pragma unroll
+          for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, afull[r] + 8u * (uint32_t)buf);
+          if (++buf == a.nbuf) {
+            buf = 0;
+            ++use;
+          }
+          i0 = last;
+        } while (SUMS && i0 < nk);
+        if (!ok) break;
+      }
+      if (!ok) {
+        mma_commit_at<PAIR>(one, smem_u32(&s.drained));
+        mbar_wait(&s.drained, 0u);
+      }
+      __syncwarp();
+    } else if (PAIR && wid == 2) {
+      if (lane == 0) {
+        const uint32_t full0 = at0(s.full);
+        int st = 0, u = 0;
+        for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it))
+          for (int i = 0; i < nk; ++i) {
+            ok = mbar_wait(s.xfull + st, (uint32_t)u & 1u, a.spin);
+            if (!ok) break;
+            fence_proxy_async();   // generic writes -> tensor-core reads
+            mbar_arrive_cluster(full0 + 8u * (uint32_t)st);
+            if (++st == a.stages) {
+              st = 0;
+              ++u;
+            }
+          }
+      }
+      __syncwarp();
+    } else if (PAIR && wid == 3) {
+      plan_waves(a, s.groups, s.waves, ntiles, step, first, kUnit);
+    } else if (wid >= 4) {
+      const int g = tid - 128, chunk = g & 7, r0 = g >> 3;   // 16 bytes of rows r0 + kXRows j
+      const uint32_t at = (uint32_t)r0 * 128u + (uint32_t)((chunk ^ (r0 & 7)) << 4);
+      const int width = a.cols * (F8 ? 1 : 2);
+      constexpr int kPasses = (PAIR || SUMS > kFewRows ? 128 : kFewRows) / kXRows;
+      int st = 0, u = 0;
+      for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
+        const Tile t = tile_of(a, s.groups, tile, kUnit);
+        const int mine = (t.n + kUnit - 1) / kUnit * kUnit / kBoth;   // rows of this CTA
+        const uint8_t* src[kPasses];
+#pragma unroll
+        for (int j = 0; j < kPasses; ++j) {
+          const int r = r0 + kXRows * j, q = half * mine + r;
+          const int row = r < mine && q < t.n ? row_of(a, t.p0 + q) : -1;
+          src[j] = row < 0 ? nullptr : static_cast<const uint8_t*>(a.x) + (int64_t)row * a.x_ld * (F8 ? 1 : 2) + chunk * 16;
+        }
+        for (int i = 0; i < nk; ++i) {
+          if (u > 0) ok = mbar_try_wait(s.empty + st, (uint32_t)(u - 1) & 1u) || mbar_wait(s.empty + st, (uint32_t)(u - 1) & 1u, a.spin);
+          ok = __all_sync(0xFFFFFFFFu, ok);
+          if (!ok) break;
+          const uint32_t dst = smem_u32(sm) + (uint32_t)st * stage + kATile + at;
+          const int b = (k0 + i) * 128, left = min(max(width - b - chunk * 16, 0), 16);
+          uint64_t* there = (PAIR ? s.xfull : s.full) + st;
+          const auto put = [&](uint32_t to, const uint4& v) {
+            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+          };
+          if (!a.w_vec) {   // the matrices too: rows r0 + kXRows j of the two tiles
+            const int m0 = (kBoth * t.m + half) * kRows;
+#pragma unroll 4
+            for (int j = 0; j < 256 / kXRows; ++j) {
+              const int r = r0 + kXRows * j;
+              const bool up = GLU && r >= 128;
+              const int m = m0 + (up ? r - 128 : r);
+              const uint8_t* row = static_cast<const uint8_t*>(up ? a.up : a.w) +
+                                   ((int64_t)t.e * (up ? a.u_eld : a.w_eld) + (int64_t)m * (up ? a.u_ld : a.w_ld)) * (F8 ? 1 : 2);
+              put(dst - kATile + (uint32_t)j * (kXRows * 128u), load16_anywhere(row + b + chunk * 16, m < a.rows ? left : 0));
+            }
+          }
+          if (a.x_vec) {
+#pragma unroll
+            for (int j = 0; j < kPasses; ++j)
+              if (r0 + kXRows * j < mine) {
+                const int bytes = src[j] ? left : 0;
+                cp_async16(dst + (uint32_t)j * (kXRows * 128u), bytes ? src[j] + b : static_cast<const uint8_t*>(a.x), bytes);
+              }
+            cp_async_arrive(there);
+          } else {   // rows off 16-byte boundaries
+#pragma unroll
+            for (int j = 0; j < kPasses; ++j)
+              if (r0 + kXRows * j < mine) {
+                put(dst + (uint32_t)j * (kXRows * 128u), load16_anywhere(src[j] ? src[j] + b : static_cast<const uint8_t*>(a.x), src[j] ? left : 0));
+              }
+            mbar_arrive(there);
+          }
+          if (++st == a.stages) {
+            st = 0;
+            ++u;
+          }
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncwarp();
+    }
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   // no CTA leaves while another may still reach its shared or tensor memory
-  if (PAIR || a.splits > 1) cluster_sync();
+  if (PAIR || (kSplit && a.splits > 1)) cluster_sync();
   else __syncthreads();
-  if (!PAIR && a.splits > 1) {
+  if (kSplit && a.splits > 1) {
     if (first < ntiles) {
       // every CTA has its part of the tile in shared memory; each sums and stores its share of the results
       const Tile t = tile_of(a, s.groups, first, kUnit);
@@ -815,7 +823,7 @@ int clusters_at_once(int dev, int n) {
   return c;
 }
 
-template <bool F8, bool GLU, bool PAIR, bool SUMS>
+template <bool F8, bool GLU, bool PAIR, int SUMS>
 cudaError_t launch_tc_as(const ExpertArgs& a, const CUtensorMap& wm, const CUtensorMap& um, int64_t groups, int dev, cudaStream_t st) {
   auto kern = k_expert_tc<F8, GLU, PAIR, SUMS>;
   const cudaError_t e = allow_shared<k_expert_tc<F8, GLU, PAIR, SUMS>>(dev, kTcShared);
@@ -840,8 +848,16 @@ cudaError_t launch_tc_as(const ExpertArgs& a, const CUtensorMap& wm, const CUten
 template <bool F8, bool GLU, bool SUMS>
 cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um, int dev, int sms, cudaStream_t st) {
   a.N = tile_rows(a.P, a.E);
-  if (SUMS) a.N = std::min(a.N, kFewRows);   // (what registers hold)
-  bool pair = a.N > kFewRows;
+  bool pair = !SUMS && a.N > kFewRows, many = SUMS && a.N > kFewRows;
+  if (many) {
+    // A tile of 128 rows takes 1.5 times as long as one of 64 (L2 bounds both, and the matrices' part of it is the same).  Gate and
+    // up of 128 experts of 768 x 2048 (us, tiles of 128 and of 64): 8192 tokens 581 and 748, 1024 160 and 150; 1200 rows by 4096 x
+    // 4096 (160 and 304 tiles) 80 and 72.
+    const int64_t experts = std::min(a.P, a.E), tall = GLU ? 128 : 256;
+    const auto waves = [&](int n) { return (experts * ((a.P / experts + n - 1) / n) * ((a.rows + tall - 1) / tall) + sms - 1) / sms; };
+    many = 3 * waves(kSumRows) < 2 * waves(kFewRows);
+    a.N = many ? kSumRows : kFewRows;
+  }
   if (pair) {
     // Pairs where a third of them have a tile; else smaller tiles of single CTAs, over which the columns can be split too.  One
     // matrix of 4096 x 4096 (us, pairs and single): 100 rows of y (8 tiles of pairs) 30 and 13, 300 (16) 31 and 26; two of
@@ -863,16 +879,20 @@ cudaError_t launch_tc(ExpertArgs a, const CUtensorMap& wm, const CUtensorMap& um
   // Few tiles: the columns over clusters of as many CTAs as the SMs hold (one token by 4096 x 4096 9.8 us, unsplit 24.0; through
   // gate and up of eight experts of 768 x 2048 11.6 and 14.8).
   a.splits = 1;
-  if (!pair)   // (clusters that do not all run at once would take a second turn)
+  if (!pair && !many)   // (clusters that do not all run at once would take a second turn)
     for (int n = 8; n > 1 && a.splits == 1; n /= 2)
-      if (most * n <= sms && a.nk >= 2 * n && most <= clusters_at_once<k_expert_tc<F8, GLU, false, SUMS>>(dev, n)) a.splits = n;
+      if (most * n <= sms && a.nk >= 2 * n && most <= clusters_at_once<k_expert_tc<F8, GLU, false, SUMS ? kFewRows : 0>>(dev, n)) a.splits = n;
   a.sps = (a.nk + a.splits - 1) / a.splits;
   const size_t room = kTcShared - 1024 - sizeof(TcShared) - (a.splits > 1 ? (size_t)a.N * 1024 : 0);
   a.stages = std::min(kStagesMost, (int)(room / (kATile + (size_t)a.N * (pair ? 64 : 128))));
-  a.chain = F8 ? 8 : 2;   // 32 additions, of bf16 8 (products of 8 bits leave less to cut off); twice that: errors 1.5 times, 697 us in place of 748
-  if constexpr (!SUMS)
-    if (pair) return launch_tc_as<F8, GLU, true, false>(a, wm, um, std::min<int64_t>({most, sms / 2, kPairsMost}), dev, st);
-  return launch_tc_as<F8, GLU, false, SUMS>(a, wm, um, std::min<int64_t>(most, sms / a.splits), dev, st);
+  a.chain = F8 ? 8 : 2;   // 32 additions, of bf16 8 (products of 8 bits leave less to cut off); twice that: errors 1.5 times, a tenth less time
+  if constexpr (SUMS) {
+    if (many) return launch_tc_as<F8, GLU, false, kSumRows>(a, wm, um, std::min<int64_t>(most, sms), dev, st);
+    return launch_tc_as<F8, GLU, false, kFewRows>(a, wm, um, std::min<int64_t>(most, sms / a.splits), dev, st);
+  } else {
+    if (pair) return launch_tc_as<F8, GLU, true, 0>(a, wm, um, std::min<int64_t>({most, sms / 2, kPairsMost}), dev, st);
+    return launch_tc_as<F8, GLU, false, 0>(a, wm, um, std::min<int64_t>(most, sms / a.splits), dev, st);
+  }
 }
 
 int matrices_check(const bitsmoe_expert_matrices* m) {
