@@ -1152,6 +1152,7 @@ def expert_product(w, x, offsets, index=None, fan: int = 1, up=None, dtype=None,
     w, up: the experts' matrices (torch bf16, experts x rows x cols, or a Rowscale of such codes); x: rows x cols of the
     same kind; offsets, index: int32 vectors (`route`'s offsets and pairs, with fan = top_k).  y (P x w's rows, P the
     length of index, or x's rows; float32 unless `dtype` or y says bfloat16): rows that no expert has are not written.
+    float32 results are summed to nearest, and of large products take up to twice the time of bfloat16 ones.
     `status`: an optional int32 tensor of one element that receives a device-side timeout.  Rows and matrices on 16-byte
     boundaries are read fastest; of large products bf16 rows of x off them are copied to a temporary first."""
     torch = _torch or _load_torch()
