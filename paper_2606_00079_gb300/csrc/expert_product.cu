@@ -139,8 +139,9 @@ __device__ __forceinline__ int row_of(const ExpertArgs& a, int p) {
 // few tiles the columns are split over a cluster, whose CTAs add their partial tiles through distributed shared memory in rank
 // order.
 //
-// Gate and up of 128 experts of 768 x 2048 in bf16: 8192 tokens 298 us (1.4 PFLOP/s; the card's power bounds it), 32 tokens 86 (the
-// matrices at 5.4 TB/s and a launch), one 14.  A matrix of 8 experts of 14336 x 4096 in 8 bits, 8192 rows: 330 us, 2.9 PFLOP/s.
+// Gate and up of 128 experts of 768 x 2048 in bf16: 8192 tokens 298 us (1.4 PFLOP/s; the card's power bounds it), 32 tokens 86, 8
+// tokens 48 under a profiler (the matrices of the experts that have one, 258 MB: DRAM), one 14.  A matrix of 8 experts of 14336 x
+// 4096 in 8 bits, 8192 rows: 330 us, 2.9 PFLOP/s.
 // ---------------------------------------------------------------------------
 // Warps: 0 matrices, 1 MMA, 2 rows of x that are there (of a pair), 3 the tiles to come (of a pair), four of rows of x, eight of
 // results.  (Eight of x's fill a stage faster, 685 clocks in place of 780 of the MMAs' 1024, but many large products are bound
