@@ -229,9 +229,10 @@ def test_expert_product_rows_of_x_off_the_boundaries(env, ty, counts, R, C, shif
     off = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).cuda()
     idx = torch.randint(0, 2 * P, (P,), generator=g, dtype=torch.int32).cuda()
     for kw in (dict(), dict(index=idx, fan=2, up=wrap(bm, up, us))):
-        a = bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, **kw)
-        b = bm.expert_product(wrap(bm, w, ws), wrap(bm, off_x, xs), off, **kw)
-        assert torch.equal(a, b)
+        for dt in (torch.float32, torch.bfloat16):
+            a = bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, dtype=dt, **kw)
+            b = bm.expert_product(wrap(bm, w, ws), wrap(bm, off_x, xs), off, dtype=dt, **kw)
+            assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("ty", ["bf16", "e4m3"])
@@ -254,10 +255,11 @@ def test_expert_product_matrices_off_the_boundaries(env, ty, counts, R, C, shift
         return v
     off = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).cuda()
     for u_ in (None, up):
-        a = bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, up=None if u_ is None else wrap(bm, u_, us))
-        for xx in (x, moved(x)):
-            b = bm.expert_product(wrap(bm, moved(w), ws), wrap(bm, xx, xs), off, up=None if u_ is None else wrap(bm, moved(u_), us))
-            assert torch.equal(a, b)
+        for dt in (torch.float32, torch.bfloat16):
+            a = bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, up=None if u_ is None else wrap(bm, u_, us), dtype=dt)
+            for xx in (x, moved(x)):
+                b = bm.expert_product(wrap(bm, moved(w), ws), wrap(bm, xx, xs), off, up=None if u_ is None else wrap(bm, moved(u_), us), dtype=dt)
+                assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("E,most,R,C,ty,glu", [(128, 6, 96, 256, "bf16", True), (300, 3, 40, 128, "e4m3", False), (1024, 2, 16, 64, "bf16", False),
@@ -266,6 +268,18 @@ def test_expert_product_many_experts_and_tiles(env, E, most, R, C, ty, glu):
     rng = np.random.default_rng([E, most])
     run_product(env, ragged(rng, E, most), R, C, ty, glu, fan=4, out="f32", lead=3, tail=5)
     run_product(env, ragged(rng, E, most), R, C, ty, glu, fan=0, out="bf16")
+
+
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("shift", [0, 3])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_expert_product_large(env, ty, glu, shift, out):
+    """Many rows an expert, several turns of every CTA, more than one chain of sums of an fp32 result."""
+    rng = np.random.default_rng(12)
+    counts = rng.integers(200, 700, 12)
+    counts[4] = 0
+    run_product(env, counts, 1300, 1230, ty, glu, fan=2, out=out, shift=shift, lead=2, tail=3)
 
 
 def test_expert_product_deep(env):
@@ -396,8 +410,9 @@ def test_expert_product_in_a_graph_and_on_a_stream(env):
 
 
 # experts, rows of a matrix, columns, rows of y, first rows of y and of the matrices that are lost with block 0's first tile:
-# pairs (many rows an expert), single CTAs (few), columns split over a cluster (few tiles: all of the tile is lost)
-LOST = {"pairs": (12, 700, 4096, 1200, 64, 128), "single": (80, 520, 4096, 400, 5, 128), "split": (3, 520, 8192, 15, 5, 128)}
+# pairs (many rows an expert; fp32: single CTAs), large (fp32: tiles of 128 rows), single CTAs (few), columns split over a
+# cluster (few tiles: all of the tile is lost)
+LOST = {"pairs": (12, 700, 4096, 1200, 64, 128), "large": (12, 2600, 4096, 4800, 64, 128), "single": (80, 520, 4096, 400, 5, 128), "split": (3, 520, 8192, 15, 5, 128)}
 
 
 @pytest.mark.parametrize("kind", sorted(LOST))
@@ -477,6 +492,7 @@ def test_expert_product_waves_of_unequal_tiles(env):
     x = torch.randn(P, C, device="cuda").to(torch.bfloat16)
     for up in (None, torch.randn(E, R, C, device="cuda").to(torch.bfloat16)):
         y = bm.expert_product(w, x, off, up=up)
+        half = bm.expert_product(w, x, off, up=up, dtype=torch.bfloat16).float()   # (by pairs of CTAs)
         o = off.tolist()
         for e in range(E):
             if o[e] == o[e + 1]:
@@ -491,6 +507,7 @@ def test_expert_product_waves_of_unequal_tiles(env):
             else:
                 want, tol = a, (C + 16) * 2.0 ** -22 * m
             assert ((y[o[e]:o[e + 1]] - want).abs() <= tol).all(), e
+            assert ((half[o[e]:o[e + 1]] - want).abs() <= tol + 2.0 ** -8 * (want.abs() + tol)).all(), e
 
 
 def test_expert_products_beside_the_forward_on_another_stream(env):
