@@ -327,10 +327,12 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       prefetch_map(&wmap);
       if (GLU) prefetch_map(&umap);
     }
+    // arrivals of the threads that fill a stage: with the matrices stored beside x's copies two each (see there)
+    const uint32_t fills = 32 * kXWarps * (!a.w_vec && a.x_vec ? 2 : 1);
     for (int i = 0; i < a.stages; ++i) {
       // the matrices' bytes (if by TMA), x's rows (a pair's first CTA's: of both)
-      mbar_init_n(s.full + i, (a.w_vec ? 1 : 0) + (PAIR ? 2 : 32 * kXWarps));
-      mbar_init_n(s.xfull + i, 32 * kXWarps);
+      mbar_init_n(s.full + i, (a.w_vec ? 1 : 0) + (PAIR ? 2 : fills));
+      mbar_init_n(s.xfull + i, fills);
       mbar_init_n(s.empty + i, 1);
     }
     for (int i = 0; i < kAccumulators; ++i) {
@@ -717,6 +719,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 cp_async16(dst + (uint32_t)j * (kXRows * 128u), bytes ? src[j] + b : static_cast<const uint8_t*>(a.x), bytes);
               }
             cp_async_arrive(there);
+            if (!a.w_vec) mbar_arrive(there);   // (that one stands for the copies alone, this one for the plain stores)
           } else {   // rows off 16-byte boundaries
 #pragma unroll
             for (int j = 0; j < kPasses; ++j)

@@ -246,3 +246,17 @@ def test_product_and_combine_oracles():
     np.testing.assert_allclose(out[0], base[0] + wt[0, 0] * x[0])
     np.testing.assert_allclose(out[1], base[1] + wt[1, 0] * x[5] + wt[1, 1] * x[2])
     np.testing.assert_allclose(out[2], base[2] + wt[2, 1] * x[1])
+
+
+def test_what_hands_a_stage_over():
+    """Threads that store matrices into a stage beside asynchronous copies of x arrive on its barrier twice: once their copies
+    are there, and, as that stands for the copies alone, for their stores."""
+    import os
+    import re
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "paper_2606_00079_gb300/csrc/expert_product.cu"), encoding="utf-8") as f:
+        src = f.read()
+    copies = re.findall(r"cp_async_arrive\((\w+)\);\n\s*(.*)", src)
+    assert copies and all(re.match(r"if \(!a\.w_vec\) mbar_arrive\(%s\);" % bar, after) for bar, after in copies)
+    fills = re.search(r"fills = 32 \* kXWarps \* \(!a\.w_vec && a\.x_vec \? 2 : 1\);", src)
+    assert fills and re.search(r"mbar_init_n\(s\.xfull \+ i, fills\)", src) and re.search(r"\(PAIR \? 2 : fills\)", src)

@@ -262,6 +262,28 @@ def test_expert_product_matrices_off_the_boundaries(env, ty, counts, R, C, shift
                 assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("E,P,R,C", [(3, 100, 300, 1030), (40, 400, 200, 2050)])
+def test_expert_product_matrices_off_the_boundaries_beside_copies(env, ty, E, P, R, C):
+    """Matrices that threads store into a stage beside their own asynchronous copies of x, more steps than stages: the bits of
+    matrices on boundaries, every time."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(P)
+    w, ws, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
+    up, us, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
+    w1, up1 = (torch.zeros(E, R, C + 1, dtype=torch.uint8 if ty == "e4m3" else torch.bfloat16, device="cuda").view(w.dtype)[..., 1:] for _ in range(2))
+    for a, b in ((w1, w), (up1, up)):
+        (a.view(torch.uint8) if ty == "e4m3" else a).copy_(b.view(torch.uint8) if ty == "e4m3" else b)
+    x, xs, _ = pitched(torch, torch.randn(P, C, generator=g), ty)
+    x = wrap(bm, x, xs)
+    off = torch.linspace(0, P, E + 1).int().cuda()
+    for u_, u1_ in ((None, None), (wrap(bm, up, us), wrap(bm, up1, us))):
+        for dt in (torch.float32, torch.bfloat16):
+            ref = bm.expert_product(wrap(bm, w, ws), x, off, up=u_, dtype=dt)
+            for _ in range(10):
+                assert torch.equal(bm.expert_product(wrap(bm, w1, ws), x, off, up=u1_, dtype=dt), ref)
+
+
 @pytest.mark.parametrize("E,most,R,C,ty,glu", [(128, 6, 96, 256, "bf16", True), (300, 3, 40, 128, "e4m3", False), (1024, 2, 16, 64, "bf16", False),
                                                (60, 40, 320, 512, "e4m3", True), (7, 400, 384, 256, "bf16", True), (5, 600, 520, 384, "e4m3", False)])
 def test_expert_product_many_experts_and_tiles(env, E, most, R, C, ty, glu):
