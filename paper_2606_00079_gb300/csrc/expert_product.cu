@@ -619,7 +619,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           const uint32_t acc = tmem + (uint32_t)(buf * 2 * a.N);
           const int last = SUMS ? min(i0 + a.chain, nk) : nk;
           for (int i = i0; i < last; ++i) {
-            ok = mbar_try_wait(s.full + st, (uint32_t)u & 1u) || mbar_wait(s.full + st, (uint32_t)u & 1u, a.spin);
+            if constexpr (PAIR) ok = mbar_wait_shared_cluster(s.full + st, (uint32_t)u & 1u, a.spin);   // (also the other CTA's)
+            else ok = mbar_try_wait(s.full + st, (uint32_t)u & 1u) || mbar_wait(s.full + st, (uint32_t)u & 1u, a.spin);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
             if (!PAIR) fence_proxy_async();   // x's rows: generic writes -> tensor-core reads
@@ -663,7 +664,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             ok = mbar_wait(s.xfull + st, (uint32_t)u & 1u, a.spin);
             if (!ok) break;
             fence_proxy_async();   // generic writes -> tensor-core reads
-            mbar_arrive_cluster(full0 + 8u * (uint32_t)st);
+            mbar_release_shared_cluster(full0 + 8u * (uint32_t)st);
             if (++st == a.stages) {
               st = 0;
               ++u;

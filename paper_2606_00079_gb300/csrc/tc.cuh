@@ -150,10 +150,29 @@ __device__ __forceinline__ uint32_t cluster_address(uint32_t saddr, uint32_t ran
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
   return r;
 }
-// One arrival on a barrier of any CTA of the cluster.  It orders nothing for other CTAs' threads (a release at cluster scope took
-// about 1 us): what it stands for is in shared memory behind a proxy fence, or in tensor memory behind tcgen05's.
+// One arrival on a barrier of any CTA of the cluster that orders no ordinary memory: for what lies in tensor memory, behind
+// tcgen05's fences.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// The same for what lies in this CTA's shared memory (this thread's writes, and those that it has waited for): who waits by
+// mbar_wait_shared_cluster sees it.  The fences are held to shared memory: a whole release at cluster scope takes about 1 us
+// each (8192 tokens through gate and up of 128 experts of 768 x 2048 412 us; by two warps in turn 350; these 298).
+__device__ __forceinline__ void mbar_release_shared_cluster(uint32_t bar) {
+  asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+  mbar_arrive_cluster(bar);
+}
+__device__ __forceinline__ bool mbar_wait_shared_cluster(uint64_t* bar, uint32_t parity, long long limit) {
+  const long long t0 = clock64();
+  for (;;) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    if (ok) break;
+    if (clock64() - t0 > limit) return false;
+  }
+  asm volatile("fence.acquire.sync_restrict::shared::cluster.cluster;" ::: "memory");
+  return true;
 }
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t ncols) {   // one full warp of each CTA
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(ncols) : "memory");

@@ -260,3 +260,24 @@ def test_what_hands_a_stage_over():
     assert copies and all(re.match(r"if \(!a\.w_vec\) mbar_arrive\(%s\);" % bar, after) for bar, after in copies)
     fills = re.search(r"fills = 32 \* kXWarps \* \(!a\.w_vec && a\.x_vec \? 2 : 1\);", src)
     assert fills and re.search(r"mbar_init_n\(s\.xfull \+ i, fills\)", src) and re.search(r"\(PAIR \? 2 : fills\)", src)
+
+
+def test_what_hands_a_stage_to_the_other_cta():
+    """A pair's second CTA hands the rows in its shared memory over to the first one's products by a release at the cluster's
+    scope, and the first one's wait for it acquires at that scope; a relaxed arrival alone stands only for tensor memory."""
+    import os
+    import re
+    folder = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2606_00079_gb300/csrc")
+    with open(os.path.join(folder, "expert_product.cu"), encoding="utf-8") as f:
+        src = f.read()
+    with open(os.path.join(folder, "tc.cuh"), encoding="utf-8") as f:
+        tc = f.read()
+
+    def body(name):
+        return re.search(r"%s\(.*?\n}\n" % name, tc, re.S).group()
+    relaxed = re.findall(r"mbar_arrive_cluster\((\w+)", src)
+    assert relaxed and set(relaxed) == {"aempty0"}
+    assert "mbar_release_shared_cluster(full0 + " in src and "mbar_wait_shared_cluster(s.full + st" in src
+    release, wait = body("void mbar_release_shared_cluster"), body("bool mbar_wait_shared_cluster")
+    assert 0 < release.index("fence.release.sync_restrict::shared::cta.cluster;") < release.index("mbar_arrive_cluster(bar)")
+    assert 0 < wait.index("mbarrier.try_wait.parity.relaxed.cluster") < wait.index("fence.acquire.sync_restrict::shared::cluster.cluster;")

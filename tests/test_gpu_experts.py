@@ -284,6 +284,45 @@ def test_expert_product_matrices_off_the_boundaries_beside_copies(env, ty, E, P,
                 assert torch.equal(bm.expert_product(wrap(bm, w1, ws), x, off, up=u1_, dtype=dt), ref)
 
 
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("matrices", [0, 1])
+@pytest.mark.parametrize("rows", [0, 1])
+def test_expert_product_of_pairs_on_and_off_the_boundaries(env, ty, matrices, rows):
+    """Pairs of CTAs (100 rows each of 15 experts: 30 tiles of pairs, with U 45; below the size from which rows of x are copied),
+    more steps than stages: every way that matrices and rows of x reach a stage, the same bits every time, and within the
+    bounds of the values."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(2 * matrices + rows)
+    E, P, R, C = 15, 1500, 600, 1500
+    w, ws, wv = pitched(torch, torch.randn(E, R, C, generator=g) / C ** 0.5, ty)
+    up, us, _ = pitched(torch, torch.randn(E, R, C, generator=g) / C ** 0.5, ty)
+    x, xs, xv = pitched(torch, torch.randn(P, C, generator=g), ty)
+    assert P * R * C <= 2 ** 31   # (rows of x: read as they lie)
+
+    def off_by_one(t):
+        flat = torch.zeros(*t.shape[:-1], C + 3, dtype=torch.uint8 if ty == "e4m3" else torch.bfloat16, device="cuda").view(t.dtype)[..., 1:1 + C]
+        (flat.view(torch.uint8) if ty == "e4m3" else flat).copy_(t.view(torch.uint8) if ty == "e4m3" else t)
+        return flat
+    counts = torch.full((E,), P // E)
+    counts[3], counts[4] = 0, 2 * (P // E)
+    off = torch.cat([torch.zeros(1, dtype=torch.long), counts.cumsum(0)]).int().cuda()
+    idx = torch.randperm(P, generator=g).int()
+    kw = dict(index=idx.cuda(), dtype=torch.bfloat16)
+    w1, up1, x1 = (off_by_one(t) if m else t for t, m in ((w, matrices), (up, matrices), (x, rows)))
+    for glu in (False, True):
+        ref = bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, up=wrap(bm, up, us) if glu else None, **kw)
+        for _ in range(8):
+            y = bm.expert_product(wrap(bm, w1, ws), wrap(bm, x1, xs), off, up=wrap(bm, up1, us) if glu else None, **kw)
+            assert torch.equal(y, ref)
+        if not glu:
+            o = off.tolist()
+            for e in range(E):
+                xr = xv[idx.numpy()[o[e]:o[e + 1]]]
+                want, mag = xr @ wv[e].T, np.abs(xr) @ np.abs(wv[e]).T
+                tol = (C + 8) * 2.0 ** -23 * mag + 8 * u * np.abs(want)
+                assert (np.abs(ref[o[e]:o[e + 1]].double().cpu().numpy() - want) <= tol + 2.0 ** -8 * (np.abs(want) + tol)).all()
+
+
 @pytest.mark.parametrize("E,most,R,C,ty,glu", [(128, 6, 96, 256, "bf16", True), (300, 3, 40, 128, "e4m3", False), (1024, 2, 16, 64, "bf16", False),
                                                (60, 40, 320, 512, "e4m3", True), (7, 400, 384, 256, "bf16", True), (5, 600, 520, 384, "e4m3", False)])
 def test_expert_product_many_experts_and_tiles(env, E, most, R, C, ty, glu):
