@@ -178,7 +178,9 @@ int bitsmoe_forward_plan(const bitsmoe_layer* layer, int T, int top_k);
  * product and of the products grouped by expert (whose own status words then say so), to `spin_clocks` SM
  * clocks (<= 0: the default, about one second), and when skip_arrival is 1 let
  * block 0 skip an arrival (the former: at their first grid barrier, the latter:
- * at a stage in shared memory), so that the bounded waits for it run out.  The
+ * at a stage in shared memory), so that the bounded waits for it run out; when
+ * it is 2, block 0 of products grouped by expert in pairs of blocks leaves out the
+ * one that says which tiles come next (the other kernels run as ever).  The
  * calls after it report
  * BITSMOE_ERR_TIMEOUT through the device status word and return; the workspace
  * is left ready for the next call.  With skip_arrival = 1 the bit allocation's

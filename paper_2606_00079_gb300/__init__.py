@@ -1264,6 +1264,6 @@ def bitsmoe_debug_shift_expert_records(layer, e: int, delta: int) -> None:
 
 
 def bitsmoe_debug_wait_limit(skip_arrival: int, spin_clocks: int) -> None:
-    """Testing hook: bound the fused kernels' waits to spin_clocks SM clocks (0: default) and let
-    block 0 skip its first grid-barrier arrival (skip_arrival = 1)."""
+    """Testing hook: bound the kernels' waits to spin_clocks SM clocks (0: default) and let block 0 skip
+    an arrival (skip_arrival = 1), or the plan of its tiles in products grouped by expert (2)."""
     _check(_lib().bitsmoe_debug_wait_limit(skip_arrival, spin_clocks), "bitsmoe_debug_wait_limit")

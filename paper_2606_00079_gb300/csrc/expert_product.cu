@@ -43,7 +43,7 @@ struct ExpertArgs {
   int chain;             // steps that an accumulator takes (fp32 results: a few)
   int w_next, u_next;    // 1: an expert has matrices of its own (0: one stands for all)
   long long spin;
-  int lose;
+  int lose, lose_plan;   // testing hook: block 0 leaves out an arrival (a stage's, the plan's)
   int* status;
 };
 
@@ -162,8 +162,12 @@ constexpr int kXRows = 4 * kXWarps;          // rows that one pass of x's warps 
 // the most work had 10 to 15 % more than the average.  So warp 3 gives the largest tiles of a wave to the pairs that have had the
 // least so far.  Every CTA works that out for itself, for all pairs, ahead of its tiles.
 constexpr int kPairsMost = 96, kAhead = 4;   // waves whose tiles are known ahead
+struct Plan {
+  alignas(16) int2 of[kPairsMost];   // keys of the tiles of a wave, and the pairs' loads
+  int by_rank[kPairsMost];           // work by the tiles' rank
+};
 struct Waves {
-  int keys[kPairsMost], loads[kPairsMost], by_rank[kPairsMost];   // of the tiles of a wave; of the pairs; work by the tiles' rank
+  Plan plan;
   int tile[kAhead];
   uint64_t known[kAhead], done[kAhead];
 };
@@ -176,10 +180,6 @@ struct TcShared {
   uint32_t slot;
   alignas(16) uint8_t turn[kOutWarps][2][1024];   // 16 rows of y of a warp's 32 results each (of both tiles), on their way out
 };
-
-// What is stored for results that a wait that ran out has lost.  A warp whose wait ran out passes nothing on: who waits for
-// it runs out as well, up to the warps that store.
-constexpr uint32_t kLost = 0x7FC00000u;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {   // the rest of the 16 are zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -222,70 +222,117 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   return v;
 }
 
-// By one warp: this pair's tile of every wave (the first: its own number).
-__device__ __forceinline__ void plan_waves(const ExpertArgs& a, const Groups& g, Waves& s, int ntiles, int pairs, int pair, int unit) {
-  constexpr int kEach = kPairsMost / 32;
-  const int lane = threadIdx.x & 31;
-  const auto work = [&](int tile) {   // of a tile: its rows, and what a tile costs whatever they are
-    const int n = tile_of(a, g, tile, unit).n;
-    return max((n + unit - 1) / unit * unit, 96) + 16;
-  };
-  mbar_arrive(lane == 0, s.known);   // (the first wave's phase)
-  int load[kEach];   // of pairs lane + 32 i
+// What a tile costs: its rows, and what it costs whatever they are.
+__device__ __forceinline__ int work_of(const ExpertArgs& a, const Groups& g, int tile, int unit) {
+  const int n = tile_of(a, g, tile, unit).n;
+  return max((n + unit - 1) / unit * unit, 96) + 16;
+}
+// By one warp: the pairs' work so far, of pairs lane + 32 i, and this pair's tile of a wave (ntiles: none).  The first wave's
+// is the pair's own number; the later ones are asked for one after the other.
+constexpr int kEach = kPairsMost / 32;
+struct Loads {
+  int v[kEach];
+};
+__device__ __forceinline__ Loads first_wave(const ExpertArgs& a, const Groups& g, int ntiles, int pairs, int unit) {
+  Loads load;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int p = (threadIdx.x & 31) + 32 * i;
+    load.v[i] = p < pairs && p < ntiles ? work_of(a, g, p, unit) : 0;
+  }
+  return load;
+}
+__device__ __forceinline__ int plan_wave(const ExpertArgs& a, const Groups& g, Plan& s, Loads& load, int wave, int ntiles, int pairs, int pair, int unit) {
+  const int lane = threadIdx.x & 31, t0 = wave * pairs, n = min(pairs, ntiles - t0);
+  int w[kEach], key[kEach], low = 0x7FFFFFFF;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if (lane + 32 * i < pairs) low = min(low, load.v[i]);
+  low = __reduce_min_sync(0xFFFFFFFFu, low);
+  __syncwarp();
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const int p = lane + 32 * i;
-    load[i] = p < pairs && p < ntiles ? work(p) : 0;
+    load.v[i] -= low;
+    w[i] = p < n ? work_of(a, g, t0 + p, unit) : 0;   // (a pair without a tile: last)
+    key[i] = w[i] * 128 + 127 - p;                    // no two alike
+    s.of[p] = p < pairs ? make_int2(key[i], load.v[i] * 128 + p) : make_int2(-1, 0x7FFFFFFF);   // (past the pairs: before nobody)
   }
+  __syncwarp();
+  int tile_rank[kEach] = {}, load_rank[kEach] = {};
+#pragma unroll 4
+  for (int q = 0; q < pairs; q += 2) {
+    const uint4 two = lds128(s.of + q);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int mine = load.v[i] * 128 + lane + 32 * i;
+      tile_rank[i] += ((int)two.x > key[i]) + ((int)two.z > key[i]);
+      load_rank[i] += ((int)two.y < mine) + ((int)two.w < mine);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if (lane + 32 * i < pairs) s.by_rank[tile_rank[i]] = w[i];
+  __syncwarp();
+  int mine = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int p = lane + 32 * i;
+    if (p == pair) mine = load_rank[i];
+    if (p < pairs) load.v[i] += s.by_rank[load_rank[i]];
+  }
+  mine = __shfl_sync(0xFFFFFFFFu, mine, pair & 31);
+  int tile = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int p = lane + 32 * i;
+    if (p < pairs && tile_rank[i] == mine) tile = p < n ? t0 + p : ntiles;
+  }
+  return __reduce_max_sync(0xFFFFFFFFu, tile);
+}
+// By one warp: this pair's tile of every wave, ahead of its other warps.  False: a wait for them ran out.
+__device__ __forceinline__ bool plan_waves(const ExpertArgs& a, const Groups& g, Waves& s, int ntiles, int pairs, int pair, int unit) {
+  const bool first = (threadIdx.x & 31) == 0;
+  mbar_arrive(first, s.known);   // (the first wave's phase)
+  Loads load = first_wave(a, g, ntiles, pairs, unit);
   for (int wave = 1; (int64_t)wave * pairs < ntiles; ++wave) {
-    if (wave >= kAhead && !mbar_wait_idle(s.done + wave % kAhead, (uint32_t)(wave / kAhead - 1) & 1u, 4 * (a.spin + kWaitClocks))) return;
-    const int t0 = wave * pairs, n = min(pairs, ntiles - t0);
-    int w[kEach], key[kEach], low = 0x7FFFFFFF;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if (lane + 32 * i < pairs) low = min(low, load[i]);
-    low = __reduce_min_sync(0xFFFFFFFFu, low);
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int p = lane + 32 * i;
-      load[i] -= low;
-      w[i] = p < n ? work(t0 + p) : 0;   // (a pair without a tile: last)
-      key[i] = w[i] * 128 + 127 - p;     // no two alike
-      if (p < pairs) {
-        s.keys[p] = key[i];
-        s.loads[p] = load[i] * 128 + p;
-      }
+    if (wave >= kAhead &&
+        !__all_sync(0xFFFFFFFFu, mbar_wait_idle(s.done + wave % kAhead, (uint32_t)(wave / kAhead - 1) & 1u, 4 * (a.spin + kWaitClocks))))
+      return false;
+    const int tile = plan_wave(a, g, s.plan, load, wave, ntiles, pairs, pair, unit);
+    if (first) s.tile[wave % kAhead] = tile;
+    mbar_arrive(first && !(a.lose_plan && wave == 1 && blockIdx.x == 0), s.known + wave % kAhead);
+  }
+  return true;
+}
+
+// What is stored for results that a wait that ran out has lost.  A warp whose wait ran out passes nothing on: who waits for
+// it runs out as well, up to the warps that store.
+constexpr uint32_t kLost = 0x7FC00000u;
+
+// Results of a lane's rows m (and m + 128) of a lost tile; `side`: which half of the rows of y.
+template <typename Y, bool GLU>
+__device__ __forceinline__ void lose_tile(const ExpertArgs& a, const Tile& t, int m, int side) {
+  for (int c = side; c < t.n; c += 2) {
+    const int64_t at = (int64_t)(t.p0 + c) * a.y_ld + m;
+    if (m < a.rows) keep(static_cast<Y*>(a.y) + at, __uint_as_float(kLost));
+    if (!GLU && m + 128 < a.rows) keep(static_cast<Y*>(a.y) + at + 128, __uint_as_float(kLost));
+  }
+}
+// Where a storing warp's wait for the plan ran out: it works out by itself which tiles from wave `from` on are lost.
+template <bool GLU>
+__device__ __noinline__ void lose_waves(const ExpertArgs& a, const Groups& g, Plan& plan, uint64_t* done, int from, int ntiles, int pairs, int pair,
+                                        int unit, int half, int side) {
+  const int lane = threadIdx.x & 31, quarter = threadIdx.x >> 5 & 3;
+  Loads load = first_wave(a, g, ntiles, pairs, unit);
+  for (int wave = 1; (int64_t)wave * pairs < ntiles; ++wave) {
+    const int tile = plan_wave(a, g, plan, load, wave, ntiles, pairs, pair, unit);
+    if (wave < from) continue;
+    if (tile < ntiles) {
+      const Tile t = tile_of(a, g, tile, unit);
+      lose_tile<__nv_bfloat16, GLU>(a, t, (2 * t.m + half) * (GLU ? 128 : 256) + 32 * quarter + lane, side);
     }
-    __syncwarp();
-    int tile_rank[kEach] = {}, load_rank[kEach] = {};
-    for (int q = 0; q < pairs; ++q) {
-      const int k = s.keys[q], l = s.loads[q];
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        tile_rank[i] += k > key[i];
-        load_rank[i] += l < load[i] * 128 + lane + 32 * i;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if (lane + 32 * i < pairs) s.by_rank[tile_rank[i]] = w[i];
-    __syncwarp();
-    int mine = 0;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int p = lane + 32 * i;
-      if (p == pair) mine = load_rank[i];
-      if (p < pairs) load[i] += s.by_rank[load_rank[i]];
-    }
-    mine = __shfl_sync(0xFFFFFFFFu, mine, pair & 31);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int p = lane + 32 * i;
-      if (p < pairs && tile_rank[i] == mine) s.tile[wave % kAhead] = p < n ? t0 + p : ntiles;
-    }
-    __syncwarp();
-    mbar_arrive(lane == 0, s.known + wave % kAhead);
+    mbar_arrive(lane == 0, done + wave % kAhead);
   }
 }
 
@@ -311,7 +358,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   constexpr int kBoth = PAIR ? 2 : 1;          // CTAs that share a tile
   constexpr bool kSplit = !PAIR && SUMS <= kFewRows;
   using Y = std::conditional_t<(SUMS > 0), float, __nv_bfloat16>;
-  static_assert(!(SUMS && PAIR), "");
+  static_assert(!(SUMS && PAIR) && sizeof(Plan) <= sizeof(TcShared::turn[0]), "");
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t stage = kATile + (uint32_t)(a.N / kBoth) * 128;
@@ -364,20 +411,29 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const auto at0 = [&](const void* p) {   // the same place in a pair's first CTA, else here
     return PAIR ? cluster_address(smem_u32(p), 0) : smem_u32(p);
   };
-  // The tile after `tile`, this group's of wave `wave` (ntiles: none).
-  const auto next_tile = [&](int tile, int wave) {
+  bool ok = true, planned = true;   // waits: of the stages and accumulators, for the plan
+  // The tile after `tile`, this group's of wave `wave` (ntiles: none, or, where `planned` is false, not known).  By a whole
+  // warp, whose lanes go on together, or by one lane.
+  const auto next_tile = [&](int tile, int wave, auto whole) {
     if (!PAIR) return tile + step;
-    if ((int64_t)wave * step >= ntiles || !mbar_wait(s.waves.known + wave % kAhead, (uint32_t)(wave / kAhead) & 1u, a.spin)) return ntiles;
+    if ((int64_t)wave * step >= ntiles) return ntiles;
+    bool there = mbar_wait(s.waves.known + wave % kAhead, (uint32_t)(wave / kAhead) & 1u, a.spin);
+    if constexpr (decltype(whole)::value) there = __all_sync(0xFFFFFFFFu, there);
+    if (!there) {
+      planned = false;
+      return ntiles;
+    }
     return *reinterpret_cast<volatile int*>(s.waves.tile + wave % kAhead);
   };
-  bool ok = true;
+  constexpr std::true_type whole_warp;
+  constexpr std::false_type one_lane;
 
   if (wid >= 4 + kXWarps) {
     if constexpr (SUMS > kFewRows) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));   // (128 sums a thread)
     const int quarter = wid & 3, side = (wid - 4 - kXWarps) >> 2;
     const uint32_t aempty0 = at0(s.aempty);
     int buf = 0, use = 0;
-    for (int tile = first, it = 0; tile < ntiles; tile = next_tile(tile, ++it)) {
+    for (int tile = first, it = 0; tile < ntiles;) {
       const Tile t = tile_of(a, s.groups, tile, kUnit);
       float* factor = s.factor[it & 1];
       {
@@ -458,11 +514,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           }
         }
       } else if (!ok) {
-        for (int c = side; c < t.n; c += 2) {
-          const int64_t at = (int64_t)(t.p0 + c) * a.y_ld + m;
-          if (in0) keep(static_cast<Y*>(a.y) + at, __uint_as_float(kLost));
-          if (!GLU && in1) keep(static_cast<Y*>(a.y) + at + 128, __uint_as_float(kLost));
-        }
+        lose_tile<Y, GLU>(a, t, m, side);
       } else if (!SUMS && a.y_vec) {
         // bf16 rows on 16-byte boundaries: rows lie along the lanes of tensor memory; turned by way of shared memory a row of y
         // goes out 16 bytes a lane
@@ -569,6 +621,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         buf = 0;
         ++use;
       }
+      tile = next_tile(tile, ++it, whole_warp);
+      if constexpr (PAIR)
+        if (!planned)   // (the warp's own memory for results on their way out: there are none)
+          lose_waves<GLU>(a, s.groups, *reinterpret_cast<Plan*>(s.turn[wid - 4 - kXWarps]), s.waves.done, it, ntiles, step, first, kUnit, half, side);
     }
   } else {
     if constexpr (SUMS > kFewRows) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
@@ -576,7 +632,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (lane == 0 && a.w_vec) {
         const uint32_t full0 = at0(s.full);
         int st = 0, u = 0, n = 0;
-        for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
+        for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it, one_lane)) {
           const Tile t = tile_of(a, s.groups, tile, kUnit);
           const int m0 = (kBoth * t.m + half) * kRows;
           for (int i = 0; i < nk; ++i, ++n) {
@@ -594,7 +650,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         }
         // copies in flight, of both CTAs (after a timeout an arrival of the phase may be missing)
         if (half == 0)
-          for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok ? kWaitClocks : a.spin);
+          for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok && planned ? kWaitClocks : a.spin);
       }
       __syncwarp();
     } else if (wid == 1 && half == 0) {
@@ -607,7 +663,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         afull[r] = PAIR ? cluster_address(smem_u32(s.afull), (uint32_t)r) : smem_u32(s.afull);
       }
       int st = 0, u = 0, buf = 0, use = 0;
-      for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
+      for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it, whole_warp)) {
         const int n = (tile_of(a, s.groups, tile, kUnit).n + kUnit - 1) / kUnit * kUnit;
         const uint32_t idesc = idesc_of<F8, PAIR>(n);
         int i0 = 0;
@@ -650,7 +706,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         } while (SUMS && i0 < nk);
         if (!ok) break;
       }
-      if (!ok) {
+      if (!ok || !planned) {
         mma_commit_at<PAIR>(one, smem_u32(&s.drained));
         mbar_wait(&s.drained, 0u);
       }
@@ -659,7 +715,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (lane == 0) {
         const uint32_t full0 = at0(s.full);
         int st = 0, u = 0;
-        for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it))
+        for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it, one_lane))
           for (int i = 0; i < nk; ++i) {
             ok = mbar_wait(s.xfull + st, (uint32_t)u & 1u, a.spin);
             if (!ok) break;
@@ -673,14 +729,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       }
       __syncwarp();
     } else if (PAIR && wid == 3) {
-      plan_waves(a, s.groups, s.waves, ntiles, step, first, kUnit);
+      planned = plan_waves(a, s.groups, s.waves, ntiles, step, first, kUnit);
     } else if (wid >= 4) {
       const int g = tid - 128, chunk = g & 7, r0 = g >> 3;   // 16 bytes of rows r0 + kXRows j
       const uint32_t at = (uint32_t)r0 * 128u + (uint32_t)((chunk ^ (r0 & 7)) << 4);
       const int width = a.cols * (F8 ? 1 : 2);
       constexpr int kPasses = (PAIR || SUMS > kFewRows ? 128 : kFewRows) / kXRows;
       int st = 0, u = 0;
-      for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it)) {
+      for (int tile = first, it = 0; tile < ntiles && ok; tile = next_tile(tile, ++it, whole_warp)) {
         const Tile t = tile_of(a, s.groups, tile, kUnit);
         const int mine = (t.n + kUnit - 1) / kUnit * kUnit / kBoth;   // rows of this CTA
         const uint8_t* src[kPasses];
@@ -772,7 +828,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     __syncwarp();
     cluster_sync();
   }
-  if (!ok && a.status) atomicCAS(a.status, 0, BITSMOE_ERR_TIMEOUT);
+  if (!(ok && planned) && a.status) atomicCAS(a.status, 0, BITSMOE_ERR_TIMEOUT);
   if (wid == 1) {
     __syncwarp();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -971,6 +1027,7 @@ extern "C" int bitsmoe_expert_product(const bitsmoe_expert_product_args* args, v
   a.y_vec = g.y_type == BITSMOE_BF16 && on_boundaries(g.y, g.y_ld, 2, g.P);
   a.spin = debug_wait_clocks() > 0 ? debug_wait_clocks() : kWaitClocks;
   a.lose = debug_skip_arrival();
+  a.lose_plan = debug_skip_plan();
   a.status = g.status;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   a.x_vec = g.x_rows > 0 && on_boundaries(g.x, g.x_ld, f8 ? 1 : 2, g.x_rows);

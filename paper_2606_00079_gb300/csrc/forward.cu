@@ -1611,7 +1611,7 @@ int forward_impl(const void* x, const float* logits, int T, int top_k, const bit
     ma.meta = L->d_meta;
     ma.msa = L->d_msa;
     ma.spin = g_dbg_spin.load() > 0 ? g_dbg_spin.load() : kWaitClocks;
-    ma.lose = g_dbg_skip.load() | (g_dbg_bounds.load() == 2 ? 2 : 0);
+    ma.lose = bmoe::debug_skip_arrival() | (g_dbg_bounds.load() == 2 ? 2 : 0);
     p.zmax = reinterpret_cast<uint32_t*>(wb + w.zmax);
     if (!p.decode && T > kSplitTokens) p.sb = reinterpret_cast<uint16_t*>(wb + w.sb);
   }
@@ -1621,7 +1621,7 @@ int forward_impl(const void* x, const float* logits, int T, int top_k, const bit
     if (ci >= 0) {
       f2.sync = reinterpret_cast<uint32_t*>(wb + w.sync);
       f2.tab = L->d_f2 + L->f2_off[ci];
-      f2.dbg = g_dbg_skip.load() | (g_dbg_bounds.load() ? 2 : 0);
+      f2.dbg = bmoe::debug_skip_arrival() | (g_dbg_bounds.load() ? 2 : 0);
       f2.prefetch_io = host_io ? 0 : 1;   // no L2 prefetch of host memory mapped into the address space
       const long long sp = g_dbg_spin.load();
       if (sp > 0) f2.spin = sp;
@@ -1637,7 +1637,7 @@ int forward_impl(const void* x, const float* logits, int T, int top_k, const bit
   if (p.decode && L->meta_ok && fused_plan(hd, T, top_k, L->seg_bytes, L->ul_max_chunks, p.s16, sms, &fa)) {
     // one token: the whole layer in one persistent kernel
     fa.sync = reinterpret_cast<uint32_t*>(wb + w.sync);
-    fa.dbg = g_dbg_skip.load() | (g_dbg_bounds.load() ? 2 : 0);
+    fa.dbg = bmoe::debug_skip_arrival() | (g_dbg_bounds.load() ? 2 : 0);
     if (g_dbg_spin.load() > 0) fa.spin = g_dbg_spin.load();
     fa.cst = L->d_cst;
     fa.dst = L->d_dst;
@@ -1912,7 +1912,8 @@ int noalloc_scratch(int device, cudaStream_t st, void** out) {
 
 namespace bmoe {
 int record_cuda_error(int cuda_error) { return cuda_fail(static_cast<cudaError_t>(cuda_error)); }
-int debug_skip_arrival() { return g_dbg_skip.load(); }
+int debug_skip_arrival() { return g_dbg_skip.load() == 1; }
+int debug_skip_plan() { return g_dbg_skip.load() == 2; }
 long long debug_wait_clocks() { return g_dbg_spin.load(); }
 }  // namespace bmoe
 
@@ -2227,7 +2228,7 @@ int bitsmoe_debug_single_token_kernel(int which) {
 }
 
 int bitsmoe_debug_wait_limit(int skip_arrival, long long spin_clocks) {
-  g_dbg_skip.store(skip_arrival ? 1 : 0);
+  g_dbg_skip.store(skip_arrival == 2 ? 2 : skip_arrival ? 1 : 0);
   g_dbg_spin.store(spin_clocks > 0 ? spin_clocks : 0);
   return BITSMOE_OK;
 }

@@ -32,6 +32,7 @@ int record_cuda_error(int cuda_error);
 
 // Testing hook (bitsmoe_debug_wait_limit): whether a skipped arrival is asked for, and the waits' bound (0: default).
 int debug_skip_arrival();
+int debug_skip_plan();   // (of a pair's plan of tiles, in products grouped by expert)
 long long debug_wait_clocks();
 
 // Supported quantisation groups and their checks.

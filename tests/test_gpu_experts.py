@@ -516,6 +516,45 @@ def test_expert_product_lost_waits(env, kind, ty, glu, fan):
 
 
 @pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("strips", [2, 8])   # 192 tiles of pairs, and 768
+def test_expert_product_lost_plan(env, ty, glu, strips):
+    """Pairs of CTAs with several waves of tiles; block 0's warps are not told which tiles come after the first.  The call
+    reports it, every result is NaN or as ever (none keeps what y held), and the next call is as ever."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(strips)
+    E, C, P, wide = 48, 256, 24000, 256 if glu else 512   # two tiles of 256 and 244 rows of y an expert, by 256 or 512 of the matrices
+    R = wide * (strips - 1) + 60
+    w, ws, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
+    up, us, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty) if glu else (None, None, None)
+    x, xs, _ = pitched(torch, torch.randn(P, C, generator=g), ty)
+    w, x = wrap(bm, w, ws), wrap(bm, x, xs)
+    kw = dict(up=wrap(bm, up, us) if glu else None, dtype=torch.bfloat16)
+    off = torch.arange(0, P + 1, P // E, dtype=torch.int32).cuda()
+    ref = bm.expert_product(w, x, off, **kw)
+    assert bool(torch.isfinite(ref).all())
+    for with_status in (True, False):
+        buf = torch.full((P, R + 8), 77.0, dtype=torch.bfloat16, device="cuda")
+        y, status = buf[:, :R], torch.zeros(1, dtype=torch.int32, device="cuda")
+        bm.bitsmoe_debug_wait_limit(2, 2_000_000)
+        try:
+            bm.expert_product(w, x, off, y=y, status=status if with_status else None, **kw)
+            torch.cuda.synchronize()
+        finally:
+            bm.bitsmoe_debug_wait_limit(0, 0)
+        assert int(status.item()) == (bm.ERR_CODE["TIMEOUT"] if with_status else 0)
+        lost = torch.isnan(y)
+        assert bool(lost.any()) and torch.equal(y[~lost], ref[~lost])
+        # a pair has one tile of a wave: of the first it is there, of the others lost
+        pairs = torch.cuda.get_device_properties(0).multi_processor_count // 2
+        assert 244 * 60 <= int(lost.sum()) <= (2 * E * strips - 1) // pairs * 256 * wide
+        assert (buf[:, R:] == 77).all()
+        status.zero_()
+        assert torch.equal(bm.expert_product(w, x, off, y=y, status=status, **kw), ref)
+        assert int(status.item()) == 0
+
+
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
 @pytest.mark.parametrize("R", [64, 250, 256, 300, 1000])
 @pytest.mark.parametrize("shift", [0, 1, 8])
 def test_expert_product_16_bit_results(env, ty, R, shift):
