@@ -336,6 +336,32 @@ __device__ __noinline__ void lose_waves(const ExpertArgs& a, const Groups& g, Pl
   }
 }
 
+// A finished sum times its two scales.  The scales' product comes first where it is a normal number (as where a warp's scales
+// are known to give only such); else the sum takes one of them first, so that nothing on the way lies outside what sum and
+// result span: the larger, or a zero.
+__device__ __forceinline__ float scaled(float sum, float f, float s) {
+  const float p = f * s;
+  if (fabsf(p) >= 0x1p-126f && fabsf(p) <= 0x1.fffffep127f) return sum * p;
+  const bool first = fabsf(f) > fabsf(s);
+  const float large = first ? f : s, small = first ? s : f;
+  return small == 0.f ? sum * small * large : sum * large * small;
+}
+// Least and largest magnitude (bits) of finite or infinite scales other than zeros.
+struct Span {
+  uint32_t least = 0x7F800000u, most = 0u;
+  __device__ __forceinline__ void add(float v) {
+    const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
+    if (b - 1u < 0x7F800000u) {
+      least = min(least, b);
+      most = max(most, b);
+    }
+  }
+  __device__ __forceinline__ void of_warp() {
+    least = __reduce_min_sync(0xFFFFFFFFu, least);
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+  }
+};
+
 // SiLU(g) u.  The quotient's denominator is 1 .. 2, so that the fast one (2 units in the last place) holds for every g.  Gate
 // and up of 128 experts of 768 x 2048, 8192 tokens 294 to 300 us; with an exact division 340, with the fast exponential (which loses
 // 1.2 |g| units) 288.
@@ -453,6 +479,17 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (in1) s1 = GLU ? __ldg(a.us + t.e * a.u_sld + m) : __ldg(a.ws + t.e * a.w_sld + m + 128);
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kOutThreads) : "memory");   // (a warp that passes has read the factors of two tiles ago)
+      bool wide = false;   // products of the warp's scales may leave the normal range
+      if (F8) {
+        Span fs, ws;
+        for (int i = lane; i < t.n; i += 32) fs.add(factor[i]);
+        ws.add(s0);
+        ws.add(s1);
+        fs.of_warp();
+        ws.of_warp();
+        wide = !(__uint_as_float(fs.least) * __uint_as_float(ws.least) >= 0x1p-126f) ||
+               !(__uint_as_float(fs.most) * __uint_as_float(ws.most) <= 0x1.fffffep127f);
+      }
       float sum[SUMS ? SUMS / 32 : 1][2][16];   // columns 16 side + 32 i + q of both tiles
       if constexpr (SUMS > 0) {
 #pragma unroll
@@ -515,7 +552,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         }
       } else if (!ok) {
         lose_tile<Y, GLU>(a, t, m, side);
-      } else if (!SUMS && a.y_vec) {
+      } else if (!SUMS && a.y_vec && !wide) {
         // bf16 rows on 16-byte boundaries: rows lie along the lanes of tensor memory; turned by way of shared memory a row of y
         // goes out 16 bytes a lane
         // (a row is 64 bytes; its 16-byte pieces are turned by its number, so that no two of eight rows meet in a bank)
@@ -588,9 +625,22 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         }
       } else {
         // a row of the matrix a lane
+        if (F8 && SUMS && wide) {   // (apart: a choice for each sum took 535 us in place of 510, 8192 rows of 14336 x 4096)
+#pragma unroll
+          for (int i = 0; i < (SUMS ? SUMS / 32 : 0); ++i)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+              const float f = factor[16 * side + 32 * i + q];
+              sum[i][0][q] = scaled(sum[i][0][q], f, s0);
+              sum[i][1][q] = scaled(sum[i][1][q], f, s1);
+            }
+          s0 = s1 = 1.f;
+        }
         const auto put = [&](int c, float g, float u) {   // column c of both tiles
           if (c >= t.n) return;
-          const float f = factor[c], v0 = g * (F8 ? s0 * f : f), v1 = u * (F8 ? s1 * f : f);
+          const float f = SUMS && wide ? 1.f : factor[c];   // (fp32 results: scaled above)
+          const float v0 = !F8 ? g * f : !SUMS && wide ? scaled(g, f, s0) : g * (s0 * f);
+          const float v1 = !F8 ? u * f : !SUMS && wide ? scaled(u, f, s1) : u * (s1 * f);
           Y* at = static_cast<Y*>(a.y) + (int64_t)(t.p0 + c) * a.y_ld + m;
           if constexpr (GLU) {
             if (in0) keep(at, silu(v0, v1));
@@ -815,7 +865,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int mh = GLU ? m : m + 128 * h;
-          if (mh < a.rows) v[h] *= F8 ? f * __ldg((GLU && h ? a.us + t.e * a.u_sld : a.ws + t.e * a.w_sld) + mh) : f;
+          if (mh < a.rows) v[h] = F8 ? scaled(v[h], f, __ldg((GLU && h ? a.us + t.e * a.u_sld : a.ws + t.e * a.w_sld) + mh)) : v[h] * f;
         }
         if constexpr (GLU) {
           if (m < a.rows) keep(static_cast<Y*>(a.y) + at, silu(v[0], v[1]));

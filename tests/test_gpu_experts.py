@@ -831,6 +831,54 @@ def test_swiglu_of_large_gates(env, T, E, R, out):
     assert ((y - want).abs() <= rel * want.abs()).all()
 
 
+# columns split; single CTAs; pairs, and of fp32 results tiles of 64 and of 128 rows of y
+@pytest.mark.parametrize("E,P,R", [(1, 3, 300), (40, 300, 200), (12, 3000, 700), (3, 4000, 2700)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("shift", [0, 1])   # of y
+def test_scales_whose_product_leaves_the_range(env, E, P, R, out, glu, shift):
+    """Rows' scales from 2^-100 to 2^120, as the coder gives them, and zeros.  The codes are small whole numbers, so the sums are
+    exact: a result is its sum times both scales, two roundings of fp32 (and SiLU's 12, and half a step of bf16), wherever the
+    sum, the scaled sums and the result are normal numbers or zeros, whatever the scales' product alone is."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(P + R)
+    C = 288
+
+    def coded(*shape):
+        codes = torch.randint(-2, 3, (*shape, C), generator=g).float()
+        codes.view(-1, C)[::7] = 0   # (sums that are zero)
+        e = torch.tensor([-100.0, -75, -60, -8, 0, 3, 60, 70, 120])[torch.randint(0, 9, shape, generator=g)]
+        s = (2.0 ** e.double() * (1 + torch.rand(shape, generator=g).double()) / 2).float()
+        s[torch.rand(shape, generator=g) < 0.02] = 0
+        return bm.Rowscale(codes.to(torch.float8_e4m3fn).cuda(), s.cuda()), codes.double(), s.double()
+    w, wv, ws = coded(E, R)
+    up, uv, us = coded(E, R) if glu else (None, None, None)
+    x, xv, xs = coded(P)
+    off = torch.linspace(0, P, E + 1).int()
+    dt = torch.float32 if out == "f32" else torch.bfloat16
+    y = torch.zeros(P, R + 8 - R % 8 + shift, dtype=dt, device="cuda")[:, shift:shift + R]
+    bm.expert_product(w, x, off.cuda(), up=up, y=y)
+    got, o, low, high = y.double().cpu(), off.tolist(), 2.0 ** -126, 2.0 ** 127
+    normal = lambda v: (v == 0) | ((v.abs() >= low) & (v.abs() <= high))
+    checked = 0
+    for e in range(E):
+        a, b = o[e], o[e + 1]
+        want = (xv[a:b] @ wv[e].T) * xs[a:b, None] * ws[e]
+        ok, rel = normal(want), 3 * u
+        if glu:
+            other = (xv[a:b] @ uv[e].T) * xs[a:b, None] * us[e]
+            ok = ok & normal(other) & (want.abs() < 80)   # (SiLU of others underflows, or is the gate itself)
+            silu = want / (1 + torch.exp(-want))
+            ok = ok & normal(silu)
+            want = silu * other
+            ok, rel = ok & normal(want), (3 * 81 + 3 + 12) * u   # (|SiLU'(g) g| is at most (1 + |g|) |SiLU(g)|)
+        tol = rel * want.abs() + (2.0 ** -8 * want.abs() * (1 + rel) if out == "bf16" else 0)
+        d = (got[a:b] - want).abs()
+        assert bool((d <= tol)[ok].all()), (e, int((~(d <= tol) & ok).sum()), int(ok.sum()))
+        checked += int((ok & (want != 0)).sum())
+    assert checked > P
+
+
 @pytest.mark.parametrize("E,P", [(1, 3), (5, 300), (4, 2000)])   # columns split, and whole
 @pytest.mark.parametrize("ty", ["bf16", "e4m3"])
 def test_fp32_results_of_many_columns(env, E, P, ty):
