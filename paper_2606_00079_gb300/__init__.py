@@ -1154,7 +1154,8 @@ def expert_product(w, x, offsets, index=None, fan: int = 1, up=None, dtype=None,
     length of index, or x's rows; float32 unless `dtype` or y says bfloat16): rows that no expert has are not written.
     float32 results are summed to nearest, and of large products take up to twice the time of bfloat16 ones.
     `status`: an optional int32 tensor of one element that receives a device-side timeout.  Rows and matrices on 16-byte
-    boundaries are read fastest; of large products bf16 rows of x off them are copied to a temporary first."""
+    boundaries are read fastest; of large products bf16 rows of x off them (up to four for each of y) are copied to a
+    temporary first."""
     torch = _torch or _load_torch()
     where = "expert_product"
     coded = isinstance(w, Rowscale)
@@ -1183,9 +1184,12 @@ def expert_product(w, x, offsets, index=None, fan: int = 1, up=None, dtype=None,
             _refuse(where, f"index has {P} entries", "SHAPE")
     if not 1 <= fan <= _MAX_ROWS:
         _refuse(where, f"fan is {fan}")
-    # Large products: rows of x off 16-byte boundaries are brought onto them first (us with and without, 16 experts of 1001
-    # x 2041, 64 rows 16 and 16, 4800 38 and 122, 64000 296 and 1180).
-    if not coded and x_rows > 0 and (x_ptr % 16 or (x_ld % 8 and x_rows > 1)) and P * wc.rows * wc.cols > 1 << 31:
+    # Large products: rows of x off 16-byte boundaries are brought onto them first, unless x has many more than y (us with and
+    # without; bf16 results of one matrix of 4096 x 4095 on boundaries: 1100 rows of y, as many of x 43 and 141, 4 times as many
+    # 54 and 163, 64 times 247 and 165; gate and up of 16 experts of 1001 x 2041 off them: 4800 rows 265 and 422, 4 times 285
+    # and 421, 64 times 716 and 423; 600 rows, so below the size, 144 and 166).
+    if (not coded and 0 < x_rows <= 4 * P and (x_ptr % 16 or (x_ld % 8 and x_rows > 1))
+            and P * wc.rows * wc.cols > 1 << 31):
         ld = (wc.cols + 7) & ~7
         rows = torch.empty((x_rows, ld), dtype=torch.bfloat16, device=dev)
         _check(_lib().bitsmoe_microscale_align(x_ptr, x_ld, x_rows, wc.cols, rows.data_ptr(), ld, _raw_stream(dev.index)),

@@ -323,6 +323,31 @@ def test_expert_product_of_pairs_on_and_off_the_boundaries(env, ty, matrices, ro
                 assert (np.abs(ref[o[e]:o[e + 1]].double().cpu().numpy() - want) <= tol + 2.0 ** -8 * (np.abs(want) + tol)).all()
 
 
+@pytest.mark.parametrize("times", [1, 4, 5, 60])
+def test_expert_product_of_few_of_many_rows_off_the_boundaries(env, times):
+    """Large products of rows of x off boundaries: x is copied only where it has up to four rows for each of y, whatever it holds
+    beside them; the same bits either way."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(times)
+    E, P, R, C = 2, 600, 2048, 2047
+    n = times * P
+    w, _, _ = pitched(torch, torch.randn(E, R, C, generator=g), "bf16")
+    x = torch.randn(n, C, dtype=torch.bfloat16, device="cuda")   # (an odd pitch)
+    off = torch.tensor([0, 250, P], dtype=torch.int32).cuda()
+    idx = torch.randint(0, n, (P,), generator=g, dtype=torch.int32).cuda()
+    y = torch.zeros(P, R, device="cuda")
+    assert P * R * C > 2 ** 31
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    bm.expert_product(w, x, off, index=idx, y=y)
+    used = torch.cuda.max_memory_allocated() - before
+    assert (n * 2048 * 2 <= used < n * 2048 * 2 + 2 ** 21) if times <= 4 else used == 0
+    rows = torch.zeros(P, 2048, dtype=torch.bfloat16, device="cuda")[:, :C]
+    rows.copy_(x[idx.long()])
+    assert torch.equal(bm.expert_product(w, rows, off), y)
+
+
 @pytest.mark.parametrize("E,most,R,C,ty,glu", [(128, 6, 96, 256, "bf16", True), (300, 3, 40, 128, "e4m3", False), (1024, 2, 16, 64, "bf16", False),
                                                (60, 40, 320, 512, "e4m3", True), (7, 400, 384, 256, "bf16", True), (5, 600, 520, 384, "e4m3", False)])
 def test_expert_product_many_experts_and_tiles(env, E, most, R, C, ty, glu):
