@@ -751,8 +751,10 @@ typedef struct bitsmoe_expert_matrices {
  *              up NULL or of w's type and sizes
  *   x          device, x_rows x w->cols of w->type, rows x_ld elements apart;
  *              x_scales: its rows' scales (fp32, device) where w is coded, else not read
- *   offsets    device, experts + 1 int32, ascending, between 0 and P (others are taken
- *              as the nearest such value)
+ *   offsets    device, experts + 1 int32, ascending, between 0 and P.  Values outside
+ *              are taken as 0 or P, and an expert whose rows would end before they begin
+ *              has none.  Where they do not ascend, so that rows belong to several
+ *              experts, y's rows hold any values; nothing outside y's rows is touched
  *   index      device, P int32, or NULL; an entry between offsets[0] and
  *              offsets[experts] whose q is not a row of x gives a row of NaN
  *   P          rows of y (0 .. 2^24); those that no expert has are not touched

@@ -428,6 +428,26 @@ def test_expert_product_rows_that_are_not_there(env, ty, shift):
     assert torch.isfinite(y).all()
 
 
+@pytest.mark.parametrize("E,P,R,C", [(6, 20, 130, 1100), (200, 400, 130, 200), (40, 3000, 600, 200)])   # split columns, single CTAs, pairs
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_expert_product_offsets_that_do_not_ascend(env, E, P, R, C, out):
+    """Every second expert has all rows, so that there are many more tiles than rows of y allow: nothing but y's rows is
+    touched, and the next call is as ever."""
+    torch, bm = env
+    dt = torch.float32 if out == "f32" else torch.bfloat16
+    w, x = torch.randn(E, R, C, device="cuda").bfloat16(), torch.randn(P, C, device="cuda").bfloat16()
+    good = torch.linspace(0, P, E + 1).int().cuda()
+    ref = bm.expert_product(w, x, good, up=w, dtype=dt)
+    bad = torch.tensor([(-1, P + 1)[e % 2] for e in range(E + 1)], dtype=torch.int32).cuda()
+    buf = torch.full((P + 2, R + 3), 77.0, dtype=dt, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    bm.expert_product(w, x, bad, up=w, y=buf[1:1 + P, 1:1 + R], status=status)
+    rest = buf.clone()
+    rest[1:1 + P, 1:1 + R] = 77.0
+    assert bool((rest == 77).all()) and int(status.item()) == 0
+    assert torch.equal(bm.expert_product(w, x, good, up=w, dtype=dt), ref)
+
+
 def test_expert_product_nothing_to_do(env):
     torch, bm = env
     w = torch.randn(2, 8, 16, device="cuda").to(torch.bfloat16)
