@@ -448,6 +448,63 @@ def test_expert_product_offsets_that_do_not_ascend(env, E, P, R, C, out):
     assert torch.equal(bm.expert_product(w, x, good, up=w, dtype=dt), ref)
 
 
+def far_apart(torch, big, x, gap):
+    """x's rows (or matrices), gap elements of `big` apart."""
+    view = big.view(x.dtype).as_strided(x.shape, ((gap, x.shape[2] + 16, 1) if x.dim() == 3 else (gap, 1)))
+    (view.view(torch.uint8) if x.dtype is torch.float8_e4m3fn else view).copy_(x.view(torch.uint8) if x.dtype is torch.float8_e4m3fn else x)
+    return view
+
+
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("P,R", [(6, 300), (300, 96), (1600, 520)])   # split columns, single CTAs, (with U) pairs
+@pytest.mark.parametrize("shift", [0, 1])   # of the gaps: on 16-byte boundaries and off them
+def test_expert_product_past_32_bits(env, ty, P, R, shift):
+    """Rows of x and y, and matrices, of which the last begin past 2^32 elements: the bits of the same close together."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(P + R)
+    E, C = 12, 272
+    w, ws, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
+    x, xs, _ = pitched(torch, torch.randn(P, C, generator=g), ty)
+    off = torch.linspace(0, P, E + 1).int().cuda()
+    one = 2 if ty == "bf16" else 1
+    big = [torch.empty((2 ** 32 + 2 ** 26) * b, dtype=torch.uint8, device="cuda") for b in (one, one, 2)]
+    gap_w, gap_p = (2 ** 32 // (E - 1) + 1) // 16 * 16 + 16 + shift, (2 ** 32 // (P - 1) + 1) // 16 * 16 + 16 + shift
+    wide_w, wide_x = far_apart(torch, big[0], w, gap_w), far_apart(torch, big[1], x, gap_p)
+    y = far_apart(torch, big[2], torch.zeros(P, R, dtype=torch.bfloat16, device="cuda"), gap_p)
+    assert min((E - 1) * gap_w, (P - 1) * gap_p) >= 2 ** 32
+    for up, wide_up in ((None, None), (wrap(bm, w, ws), wrap(bm, wide_w, ws))):
+        ref = bm.expert_product(wrap(bm, w, ws), wrap(bm, x, xs), off, up=up, dtype=torch.bfloat16)
+        y.zero_()
+        bm.expert_product(wrap(bm, wide_w, ws), wrap(bm, wide_x, xs), off, up=wide_up, y=y)
+        assert torch.equal(y, ref)
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+def test_rows_and_sums_past_32_bits(env, shift):
+    """The coder, its inverse, the norm to 8 bits and the weighted sum on rows of which the last begin past 2^32 elements."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(7)
+    T, k, D = 9, 3, 264
+    gap = 2 ** 32 // (T - 1) + 16 + shift
+    big = [torch.empty(2 ** 32 + 2 ** 26, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    codes = torch.empty(2 ** 32 + 2 ** 26, dtype=torch.uint8, device="cuda")
+    x = torch.randn(T, D, generator=g).bfloat16().cuda()
+    wide, back = far_apart(torch, big[0], x, gap), far_apart(torch, big[1], torch.zeros_like(x), gap)
+    q = bm.Rowscale(far_apart(torch, codes, torch.zeros(T, D, dtype=torch.float8_e4m3fn, device="cuda"), gap), torch.zeros(T, device="cuda"))
+    ref = bm.rowscale_quantize(x)
+    bm.rowscale_quantize(wide, q)
+    assert torch.equal(q.codes.view(torch.uint8), ref.codes.view(torch.uint8)) and torch.equal(q.scales, ref.scales)
+    bm.rowscale_dequantize(q, out=back)
+    assert torch.equal(back, bm.rowscale_dequantize(ref, torch.bfloat16))
+    ref = bm.block_norm(x, x_dtype=torch.float8_e4m3fn)[1]
+    bm.block_norm(wide, x=q)
+    assert torch.equal(q.codes.view(torch.uint8), ref.codes.view(torch.uint8)) and torch.equal(q.scales, ref.scales)
+    places = torch.randint(-1, T, (T, k), generator=g, dtype=torch.int32).cuda()
+    weights = torch.rand(T, k, generator=g).cuda()
+    bm.expert_combine(wide, places, weights, out=back)
+    assert torch.equal(back, bm.expert_combine(x, places, weights, dtype=torch.bfloat16))
+
+
 def test_expert_product_nothing_to_do(env):
     torch, bm = env
     w = torch.randn(2, 8, 16, device="cuda").to(torch.bfloat16)
