@@ -139,9 +139,10 @@ __device__ __forceinline__ int row_of(const ExpertArgs& a, int p) {
 // few tiles the columns are split over a cluster, whose CTAs add their partial tiles through distributed shared memory in rank
 // order.
 //
-// Gate and up of 128 experts of 768 x 2048 in bf16: 8192 tokens 298 us (1.4 PFLOP/s; the card's power bounds it), 32 tokens 86, 8
-// tokens 48 under a profiler (the matrices of the experts that have one, 258 MB: DRAM), one 14.  A matrix of 8 experts of 14336 x
-// 4096 in 8 bits, 8192 rows: 330 us, 2.9 PFLOP/s.
+// Gate and up of 128 experts of 768 x 2048 in bf16 (the kernel alone, replayed from a graph): 8192 tokens 300 us (1.4 PFLOP/s;
+// the card's power bounds it, at a stretch 337), 32 tokens 85, one 13.9 with its matrices from DRAM (11.7 from L2); 8 tokens 54
+// under a profiler (the matrices of the experts that have one, 302 MB: DRAM).  A matrix of 8 experts of 14336 x 4096 in 8 bits,
+// 8192 rows: 333 us, 2.9 PFLOP/s (at a stretch 381).
 // ---------------------------------------------------------------------------
 // Warps: 0 matrices, 1 MMA, 2 rows of x that are there (of a pair), 3 the tiles to come (of a pair), four of rows of x, eight of
 // results.  (Eight of x's fill a stage faster, 685 clocks in place of 780 of the MMAs' 1024, but many large products are bound
@@ -374,7 +375,7 @@ __device__ __forceinline__ float silu(float g, float u) {
 // of a sum, of SiLU of it twice that; nothing beside the half step of a result in bf16, but 8 times what sums in fp32 lose.  So
 // an accumulator takes a few steps, and registers add those up to nearest: 2e-7, and 3e-7.  They hold the sums of SUMS rows of
 // y, 64 or 128; large products read the matrices more often for it and L2 bounds them (gate and up of 128 experts of 768 x 2048,
-// us, fp32 and bf16: 1 token 13.5 and 12.4, 256 124 and 119, 8192 581 and 300).
+// us, fp32 and bf16: 1 token 14.6 and 13.9, 256 121 and 117, 8192 581 and 300).
 template <bool F8, bool GLU, bool PAIR, int SUMS>
 __global__ void __launch_bounds__(kTcThreads, 1)
     k_expert_tc(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ ExpertArgs a) {
