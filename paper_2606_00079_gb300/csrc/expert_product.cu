@@ -155,6 +155,7 @@ constexpr int kSumRows = 128;                // rows of y of a tile of many fp32
 constexpr int kSumRegs = 184, kOtherRegs = 72;   // registers of the warps that hold their sums, and of the others (128 at launch)
 static_assert(32 * kOutWarps * kSumRegs + 32 * (4 + kXWarps) * kOtherRegs <= 128 * kTcThreads && kOutWarps % 4 == 0 && kXWarps % 4 == 0, "");
 constexpr int kStagesMost = 8, kAccumulators = 4;
+constexpr long long kCopyClocks = 1 << 21;   // what a copy in flight is given where a wait has run out (1 ms)
 constexpr uint32_t kATile = 2 * 128 * 128;   // bytes of a stage's tiles of the matrices
 constexpr int kTcShared = 227 * 1024;        // (all of an SM's, as of every kernel that allocates tensor memory)
 constexpr int kXRows = 4 * kXWarps;          // rows that one pass of x's warps brings
@@ -699,9 +700,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             }
           }
         }
-        // copies in flight, of both CTAs (after a timeout an arrival of the phase may be missing)
-        if (half == 0)
-          for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(s.full + j % a.stages, (uint32_t)(j / a.stages) & 1u, ok && planned ? kWaitClocks : a.spin);
+        // copies in flight: they are there, or (a pair's second CTA, whose copies the first one's barriers count) products have
+        // read them; after a timeout an arrival may be missing, and the wait is longer than a copy takes
+        uint64_t* bars = half == 0 ? s.full : s.empty;
+        const long long most = ok && planned ? kWaitClocks : max(a.spin, kCopyClocks);
+        for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(bars + j % a.stages, (uint32_t)(j / a.stages) & 1u, most);
       }
       __syncwarp();
     } else if (wid == 1 && half == 0) {
@@ -757,10 +760,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         } while (SUMS && i0 < nk);
         if (!ok) break;
       }
-      if (!ok || !planned) {
-        mma_commit_at<PAIR>(one, smem_u32(&s.drained));
-        mbar_wait(&s.drained, 0u);
-      }
+      // products in flight: who waits for their results may have given up
+#pragma unroll
+      for (int r = 0; r < kBoth; ++r) mma_commit_at<PAIR>(one, PAIR ? cluster_address(smem_u32(&s.drained), (uint32_t)r) : smem_u32(&s.drained));
+      mbar_wait(&s.drained, 0u);
       __syncwarp();
     } else if (PAIR && wid == 2) {
       if (lane == 0) {
@@ -851,6 +854,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   // no CTA leaves while another may still reach its shared or tensor memory
   if (PAIR || (kSplit && a.splits > 1)) cluster_sync();
   else __syncthreads();
+  if (PAIR && half == 1 && wid == 1) mbar_wait(&s.drained, 0u);   // (the last arrival that comes from the first CTA)
   if (kSplit && a.splits > 1) {
     if (first < ntiles) {
       // every CTA has its part of the tile in shared memory; each sums and stores its share of the results
