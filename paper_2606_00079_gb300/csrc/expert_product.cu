@@ -214,6 +214,14 @@ __device__ __forceinline__ uint4 load16_anywhere(const uint8_t* p, int n) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
+// Whether all of THREADS threads (whole warps, barrier 1) say so; a barrier of theirs.
+template <int THREADS>
+__device__ __forceinline__ bool all_of(bool v) {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n bar.red.and.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
+               : "=r"(r) : "r"((uint32_t)v), "n"(THREADS) : "memory");
+  return r != 0;
+}
 __device__ __forceinline__ void cluster_sync() {   // converged warps
   asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
@@ -299,7 +307,7 @@ __device__ __forceinline__ bool plan_waves(const ExpertArgs& a, const Groups& g,
   Loads load = first_wave(a, g, ntiles, pairs, unit);
   for (int wave = 1; (int64_t)wave * pairs < ntiles; ++wave) {
     if (wave >= kAhead &&
-        !__all_sync(0xFFFFFFFFu, mbar_wait_idle(s.done + wave % kAhead, (uint32_t)(wave / kAhead - 1) & 1u, 4 * (a.spin + kWaitClocks))))
+        !__all_sync(0xFFFFFFFFu, mbar_wait_idle(s.done + wave % kAhead, (uint32_t)(wave / kAhead - 1) & 1u, 2 * a.spin)))
       return false;
     const int tile = plan_wave(a, g, s.plan, load, wave, ntiles, pairs, pair, unit);
     if (first) s.tile[wave % kAhead] = tile;
@@ -323,8 +331,8 @@ __device__ __forceinline__ void lose_tile(const ExpertArgs& a, const Tile& t, in
 }
 // Where a storing warp's wait for the plan ran out: it works out by itself which tiles from wave `from` on are lost.
 template <bool GLU>
-__device__ __noinline__ void lose_waves(const ExpertArgs& a, const Groups& g, Plan& plan, uint64_t* done, int from, int ntiles, int pairs, int pair,
-                                        int unit, int half, int side) {
+__device__ __noinline__ void lose_waves(const ExpertArgs& a, const Groups& g, Plan& plan, int from, int ntiles, int pairs, int pair, int unit,
+                                        int half, int side) {
   const int lane = threadIdx.x & 31, quarter = threadIdx.x >> 5 & 3;
   Loads load = first_wave(a, g, ntiles, pairs, unit);
   for (int wave = 1; (int64_t)wave * pairs < ntiles; ++wave) {
@@ -334,7 +342,6 @@ __device__ __noinline__ void lose_waves(const ExpertArgs& a, const Groups& g, Pl
       const Tile t = tile_of(a, g, tile, unit);
       lose_tile<__nv_bfloat16, GLU>(a, t, (2 * t.m + half) * (GLU ? 128 : 256) + 32 * quarter + lane, side);
     }
-    mbar_arrive(lane == 0, done + wave % kAhead);
   }
 }
 
@@ -461,8 +468,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const int quarter = wid & 3, side = (wid - 4 - kXWarps) >> 2;
     const uint32_t aempty0 = at0(s.aempty);
     int buf = 0, use = 0;
-    for (int tile = first, it = 0; tile < ntiles;) {
-      const Tile t = tile_of(a, s.groups, tile, kUnit);
+    for (int tile = first, it = 0;;) {
+      if (!PAIR && tile >= ntiles) break;
+      const Tile t = tile < ntiles ? tile_of(a, s.groups, tile, kUnit) : Tile{0, 0, 0, 0};
       float* factor = s.factor[it & 1];
       {
         const int r = tid - 32 * (4 + kXWarps);
@@ -480,7 +488,15 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (in0) s0 = __ldg(a.ws + t.e * a.w_sld + m);
         if (in1) s1 = GLU ? __ldg(a.us + t.e * a.u_sld + m) : __ldg(a.ws + t.e * a.w_sld + m + 128);
       }
-      asm volatile("bar.sync 1, %0;" ::"n"(kOutThreads) : "memory");   // (a warp that passes has read the factors of two tiles ago)
+      // (a warp that passes has read the factors of two tiles ago)
+      if constexpr (PAIR) {
+        planned = all_of<kOutThreads>(planned);   // the warps that store go on together, or lose the rest together
+        if (!planned)   // (the warp's own memory for results on their way out: there are none)
+          lose_waves<GLU>(a, s.groups, *reinterpret_cast<Plan*>(s.turn[wid - 4 - kXWarps]), it, ntiles, step, first, kUnit, half, side);
+        if (!planned || tile >= ntiles) break;
+      } else {
+        asm volatile("bar.sync 1, %0;" ::"n"(kOutThreads) : "memory");
+      }
       bool wide = false;   // products of the warp's scales may leave the normal range
       if (F8) {
         Span fs, ws;
@@ -667,16 +683,15 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(aempty0 + 8u * (uint32_t)buf);
-      if (PAIR) mbar_arrive(lane == 0, s.waves.done + it % kAhead);   // (everyone else is past this tile, or has given up)
+      // (A warp whose wait ran out arrives nowhere: it may be ahead of the others, who may still read this tile's place in the
+      // plan, or its accumulators.  What waits for it runs out as well.)
+      if (lane == 0 && ok) mbar_arrive_cluster(aempty0 + 8u * (uint32_t)buf);
+      if (PAIR) mbar_arrive(lane == 0 && ok, s.waves.done + it % kAhead);   // (everyone else is past this tile)
       if (++buf == a.nbuf) {
         buf = 0;
         ++use;
       }
       tile = next_tile(tile, ++it, whole_warp);
-      if constexpr (PAIR)
-        if (!planned)   // (the warp's own memory for results on their way out: there are none)
-          lose_waves<GLU>(a, s.groups, *reinterpret_cast<Plan*>(s.turn[wid - 4 - kXWarps]), s.waves.done, it, ntiles, step, first, kUnit, half, side);
     }
   } else {
     if constexpr (SUMS > kFewRows) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
