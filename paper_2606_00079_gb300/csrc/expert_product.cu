@@ -320,14 +320,16 @@ __device__ __forceinline__ bool plan_waves(const ExpertArgs& a, const Groups& g,
 // it runs out as well, up to the warps that store.
 constexpr uint32_t kLost = 0x7FC00000u;
 
-// Results of a lane's rows m (and m + 128) of a lost tile; `side`: which half of the rows of y.
+// A lane's results of a lost tile, those that it would have stored: of the matrix's rows m (and m + 128) and every other 16 rows
+// of y.
 template <typename Y, bool GLU>
 __device__ __forceinline__ void lose_tile(const ExpertArgs& a, const Tile& t, int m, int side) {
-  for (int c = side; c < t.n; c += 2) {
-    const int64_t at = (int64_t)(t.p0 + c) * a.y_ld + m;
-    if (m < a.rows) keep(static_cast<Y*>(a.y) + at, __uint_as_float(kLost));
-    if (!GLU && m + 128 < a.rows) keep(static_cast<Y*>(a.y) + at + 128, __uint_as_float(kLost));
-  }
+  for (int c0 = 16 * side; c0 < t.n; c0 += 32)
+    for (int c = c0; c < min(c0 + 16, t.n); ++c) {
+      const int64_t at = (int64_t)(t.p0 + c) * a.y_ld + m;
+      if (m < a.rows) keep(static_cast<Y*>(a.y) + at, __uint_as_float(kLost));
+      if (!GLU && m + 128 < a.rows) keep(static_cast<Y*>(a.y) + at + 128, __uint_as_float(kLost));
+    }
 }
 // Where a storing warp's wait for the plan ran out: it works out by itself which tiles from wave `from` on are lost.
 template <bool GLU>

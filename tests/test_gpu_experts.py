@@ -656,6 +656,38 @@ def test_expert_product_lost_plan(env, ty, glu, strips):
         assert int(status.item()) == 0
 
 
+@pytest.mark.parametrize("kind", sorted(LOST) + ["waves"])
+@pytest.mark.parametrize("ty", ["bf16", "e4m3"])
+@pytest.mark.parametrize("glu", [False, True])
+def test_expert_product_short_waits(env, kind, ty, glu):
+    """Waits bounded to less than what they take, so that they run out in some warps and not in others, at any place: results
+    are NaN (and the call says so) or as ever, and the next call is as ever."""
+    torch, bm = env
+    g = torch.Generator().manual_seed(9)
+    E, R, C, P = LOST[kind][:4] if kind != "waves" else (48, 2100, 256, 24000)
+    w, ws, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty)
+    up, us, _ = pitched(torch, torch.randn(E, R, C, generator=g), ty) if glu else (None, None, None)
+    x, xs, _ = pitched(torch, torch.randn(P, C, generator=g), ty)
+    w, x = wrap(bm, w, ws), wrap(bm, x, xs)
+    kw = dict(up=wrap(bm, up, us) if glu else None)
+    off = torch.arange(0, P + 1, P // E, dtype=torch.int32).cuda()
+    for dt in (torch.float32, torch.bfloat16):
+        ref = bm.expert_product(w, x, off, dtype=dt, **kw)
+        for clocks in (1, 100, 500, 1000, 2000, 3000, 5000, 8000, 15000, 40000):
+            y, status = torch.full((P, R), 77.0, dtype=dt, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+            bm.bitsmoe_debug_wait_limit(0, clocks)
+            try:
+                bm.expert_product(w, x, off, y=y, status=status, **kw)
+                torch.cuda.synchronize()
+            finally:
+                bm.bitsmoe_debug_wait_limit(0, 0)
+            lost = torch.isnan(y)
+            assert torch.equal(y[~lost], ref[~lost]), clocks
+            assert int(status.item()) == bm.ERR_CODE["TIMEOUT"] or (int(status.item()) == 0 and not bool(lost.any())), clocks
+            status.zero_()
+            assert torch.equal(bm.expert_product(w, x, off, y=y, status=status, **kw), ref) and int(status.item()) == 0
+
+
 @pytest.mark.parametrize("ty", ["bf16", "e4m3"])
 @pytest.mark.parametrize("R", [64, 250, 256, 300, 1000])
 @pytest.mark.parametrize("shift", [0, 1, 8])
