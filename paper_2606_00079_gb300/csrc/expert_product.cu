@@ -720,7 +720,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         // copies in flight: they are there, or (a pair's second CTA, whose copies the first one's barriers count) products have
         // read them; after a timeout an arrival may be missing, and the wait is longer than a copy takes
         uint64_t* bars = half == 0 ? s.full : s.empty;
-        const long long most = ok && planned ? kWaitClocks : max(a.spin, kCopyClocks);
+        const long long most = half == 0 && ok && planned ? kWaitClocks : max(a.spin, kCopyClocks);   // (the first CTA may have given up)
         for (int j = max(0, n - a.stages); j < n; ++j) mbar_wait(bars + j % a.stages, (uint32_t)(j / a.stages) & 1u, most);
       }
       __syncwarp();
